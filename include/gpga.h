@@ -16,7 +16,8 @@
  * Data layout: every state array is node-major fp32, row i = node i, with a
  * common leading dimension ld >= d (in floats).  All pointers named *_dev are
  * DEVICE pointers owned by the caller.  The library owns the context, small scratch for
- * reductions and per-sample coefficients, and, a device, the memory through which gpga_run exchanges
+ * reductions and per-sample coefficients, that of the language-model operators (as large as their calls
+ * need), and, a device, the memory through which gpga_run exchanges
  * margins and iterates on stored features (option "rows_run"; as large as the launches made so far
  * need, n x d x 8 bytes for each of their up to 32 iterations, at most 64 MiB of these, and the margins;
  * all contexts share it, and what is over 8 MiB of it goes with the last one).  Work is enqueued on the stream given to
@@ -377,6 +378,69 @@ gpga_status gpga_tune(gpga_ctx* ctx, int32_t launches);
  *       sums, 0 = a reduction pass followed or no trace is attached).  These three and step_path do not synchronise.
  * EINVAL for an unknown name. */
 gpga_status gpga_query(gpga_ctx* ctx, const char* name, double* value_out);
+
+/* ---- operators of language models, on the nodes' own parameters ----
+ * What stands between the tokens of n nodes and the gradients in g_dev, for a caller whose objective is a language
+ * model.  Node i's parameters are row i of the live X; an operator reads them at a column offset and writes their
+ * gradient to the same columns of g_dev (accumulate = 0: replaced; 1: added to what is there).  The other columns
+ * of g_dev are not touched, and k does not change: a gpga_step follows when all of g_dev has been written.
+ *
+ * Activations are n * T rows, row i*T + t = token t of node i, T >= 0 tokens a node, of D (or V) elements of one
+ * type, fp32, bf16 or fp16, with a common leading dimension ld (in elements) for all activations of a call.  Pointers need
+ * the alignment of their elements.  Arithmetic and sums are fp32 or wider; results are rounded to the activations' type
+ * once, to nearest even.  An output may take the exact place of an input of the call; any other overlap of an output with
+ * an input, another output or a bound array is EINVAL (columns of one wider array do not overlap).  tokens_dev and
+ * labels_dev are n x T int32.  Results do not depend on the order in which workgroups run: the same call gives the same
+ * bits.  Asynchronous on the bound stream, but for scratch that has to grow (the embedding's and the layer norm's
+ * gradients and the loss use some; it is kept for later calls). */
+typedef enum { GPGA_F32 = 0, GPGA_BF16 = 1, GPGA_F16 = 2 } gpga_dtype;
+
+/* y[i,t,:] = scale * E_i[tokens[i,t],:], E_i the V x D table (row-major, dense) in columns table_off .. table_off + V*D
+ * of x_i.  A token below 0 is padding: its row is 0.  A token of V or more is never used as an address: its row is NaN. */
+gpga_status gpga_embed(gpga_ctx* ctx, const int32_t* tokens_dev, int32_t T, int64_t table_off, int32_t V, int32_t D,
+                       float scale, void* y_dev, int64_t ld, int32_t dtype);
+/* The gradient of that table: dE_i[v,:] = scale * sum of dy[i,t,:] over the t with tokens[i,t] = v (added in the order
+ * of t; 0 where there is none), into columns table_off .. of row i of g_dev.  Padding takes no part; a token of V or
+ * more makes the block of its node NaN.  With accumulate = 1 only rows of tokens that occur are touched.  n*V < 2^31. */
+gpga_status gpga_embed_grad(gpga_ctx* ctx, const int32_t* tokens_dev, int32_t T, int64_t table_off, int32_t V, int32_t D,
+                            float scale, const void* dy_dev, int64_t ld, int32_t dtype, int32_t accumulate);
+
+/* y = residual + mask * x / (1 - p) (residual_dev NULL: without it).  The mask is never stored: it is a function of
+ * (seed, layer, node i, iteration k, t, c), so the same call with x_dev = the gradient of y and residual_dev = NULL, at the
+ * same k, is the backward pass.  Element c of row t stays iff its lot is at least q = round(65536 p), and is then
+ * multiplied by 65536 / (65536 - q); lots 2j and 2j+1 of columns 8(c/8) .. 8(c/8)+7 are the lower and the upper 16 bits
+ * of r_j, where r0..r3 are Philox4x32-10 (as below gpga_problem_synthetic) of the counter
+ * (t * ceil(D/8) + c/8, i, k, 4 + 256 layer).  0 <= p < 1 with q < 65536, 0 <= layer < 2^24, T * ceil(D/8) < 2^32. */
+gpga_status gpga_dropout(gpga_ctx* ctx, const void* x_dev, const void* residual_dev, int32_t T, int32_t D, int64_t ld,
+                         int32_t dtype, float p, uint64_t seed, int32_t layer, void* y_dev);
+
+/* u = residual + mask * x / (1 - p), dropout and residual as above (p = 0, residual_dev = NULL: u = x);
+ * y = gamma_i * (u - mean) * rstd + beta_i with mean and variance (divisor D) over the row, rstd = (variance + eps)^-1/2;
+ * gamma_i and beta_i are D floats each in columns gamma_off .. and beta_off .. of x_i.  u_dev (may be NULL) receives u,
+ * stats_dev (may be NULL) n*T pairs (mean, rstd) of fp32; the backward pass needs both.  y comes from u before it is
+ * rounded.  A row without variance gives beta_i (eps > 0). */
+gpga_status gpga_layer_norm(gpga_ctx* ctx, const void* x_dev, const void* residual_dev, int32_t T, int32_t D, int64_t ld,
+                            int32_t dtype, float p, uint64_t seed, int32_t layer, int64_t gamma_off, int64_t beta_off,
+                            float eps, void* u_dev, void* y_dev, float* stats_dev);
+/* Backward: with h = gamma_i * dy and xh = (u - mean) * rstd, du = rstd * (h - mean(h) - xh * mean(h * xh)) + more
+ * (more_dev: what else reaches u, e.g. along the residual stream; may be NULL), the gradient of the residual;
+ * dx = mask * du / (1 - p), the gradient of x (dx_dev is NULL iff p == 0, where it is du);
+ * d gamma_i = sum over t of dy * xh and d beta_i = sum over t of dy into g_dev.  p, seed, layer and k as in the forward
+ * pass. */
+gpga_status gpga_layer_norm_grad(gpga_ctx* ctx, const void* dy_dev, const void* u_dev, const float* stats_dev,
+                                 const void* more_dev, int32_t T, int32_t D, int64_t ld, int32_t dtype, float p,
+                                 uint64_t seed, int32_t layer, int64_t gamma_off, int64_t beta_off, void* du_dev,
+                                 void* dx_dev, int32_t accumulate);
+
+/* Cross-entropy of softmax(z) over V classes, averaged over each node's N_i tokens with a label >= 0 (a label below 0
+ * is not counted): loss_dev[i] = 1/N_i sum of -ln softmax(z[i,t,:])[labels[i,t]], n floats on the device as
+ * gpga_aga_step and gpga_node_mean take them; dlogits_dev (NULL: the loss alone; may be logits_dev) receives
+ * grad_scale / N_i * (softmax(z) - onehot(label)), 0 in rows that are not counted.  grad_scale is for gradients that
+ * fp16 could not hold.  A node without a counted token has loss 0 and gradient 0.  A label of V or more is never used as
+ * an address: its row of the gradient and the loss of its node are NaN.  A logit of -inf is a class that is left out;
+ * +inf, NaN, or nothing but -inf in a counted row make it NaN. */
+gpga_status gpga_token_loss(gpga_ctx* ctx, const void* logits_dev, const int32_t* labels_dev, int32_t T, int32_t V,
+                            int64_t ld, int32_t dtype, float grad_scale, float* loss_dev, void* dlogits_dev);
 
 /* Measurement aid, not part of the method: a plain streaming kernel over `bytes`
  * (a multiple of 16) per array of device memory on hip_stream, with the same 128-bit

@@ -20,6 +20,7 @@ GPGA_TOPO_GRID, GPGA_TOPO_EXPO, GPGA_TOPO_CUSTOM = 4, 5, 6
 TOPOLOGY = {"ring": GPGA_TOPO_RING, "expo1": GPGA_TOPO_EXPO1, "none": GPGA_TOPO_NONE,
             "full": GPGA_TOPO_FULL, "grid": GPGA_TOPO_GRID, "expo": GPGA_TOPO_EXPO,
             "custom": GPGA_TOPO_CUSTOM}
+GPGA_F32, GPGA_BF16, GPGA_F16 = 0, 1, 2
 _STATUS_NAME = {0: "GPGA_OK", 1: "GPGA_EINVAL", 2: "GPGA_ENOMEM", 3: "GPGA_EDEVICE", 4: "GPGA_ESTATE"}
 
 #: every symbol include/gpga.h declares: (name, restype, argtypes)
@@ -68,6 +69,20 @@ SIGNATURES = [
     ("gpga_set_option", _c.c_int, [_ctx_p, _c.c_char_p, _c.c_int64]),
     ("gpga_tune", _c.c_int, [_ctx_p, _c.c_int32]),
     ("gpga_query", _c.c_int, [_ctx_p, _c.c_char_p, _c.POINTER(_c.c_double)]),
+    ("gpga_embed", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_int32, _c.c_int64, _c.c_int32, _c.c_int32, _c.c_float,
+                              _c.c_void_p, _c.c_int64, _c.c_int32]),
+    ("gpga_embed_grad", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_int32, _c.c_int64, _c.c_int32, _c.c_int32, _c.c_float,
+                                   _c.c_void_p, _c.c_int64, _c.c_int32, _c.c_int32]),
+    ("gpga_dropout", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int64, _c.c_int32,
+                                _c.c_float, _c.c_uint64, _c.c_int32, _c.c_void_p]),
+    ("gpga_layer_norm", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int64, _c.c_int32,
+                                   _c.c_float, _c.c_uint64, _c.c_int32, _c.c_int64, _c.c_int64, _c.c_float,
+                                   _c.c_void_p, _c.c_void_p, _c.c_void_p]),
+    ("gpga_layer_norm_grad", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32,
+                                        _c.c_int32, _c.c_int64, _c.c_int32, _c.c_float, _c.c_uint64, _c.c_int32,
+                                        _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int32]),
+    ("gpga_token_loss", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int64, _c.c_int32,
+                                   _c.c_float, _c.c_void_p, _c.c_void_p]),
     ("gpga_probe_stream", _c.c_int, [_c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64,
                                      _c.c_int32, _c.c_void_p]),
     ("gpga_last_error", _c.c_char_p, [_ctx_p]),
@@ -304,6 +319,37 @@ def gpga_query(ctx, name: str) -> float:
     out = ctypes.c_double()
     _check(ctx, _lib.gpga_query(ctx, name.encode(), ctypes.byref(out)))
     return out.value
+
+
+def gpga_embed(ctx, tokens, T: int, table_off: int, V: int, D: int, scale: float, y, ld: int, dtype: int):
+    """tokens: n x T int32; y: n*T rows of D elements (``dtype``: GPGA_F32, GPGA_BF16 or GPGA_F16), ``ld`` apart."""
+    _check(ctx, _lib.gpga_embed(ctx, _ptr(tokens), T, table_off, V, D, scale, _ptr(y), ld, dtype))
+
+
+def gpga_embed_grad(ctx, tokens, T: int, table_off: int, V: int, D: int, scale: float, dy, ld: int, dtype: int,
+                    accumulate: bool = False):
+    _check(ctx, _lib.gpga_embed_grad(ctx, _ptr(tokens), T, table_off, V, D, scale, _ptr(dy), ld, dtype, int(accumulate)))
+
+
+def gpga_dropout(ctx, x, residual, T: int, D: int, ld: int, dtype: int, p: float, seed: int, layer: int, y):
+    _check(ctx, _lib.gpga_dropout(ctx, _ptr(x), _ptr(residual), T, D, ld, dtype, p, seed, layer, _ptr(y)))
+
+
+def gpga_layer_norm(ctx, x, residual, T: int, D: int, ld: int, dtype: int, p: float, seed: int, layer: int,
+                    gamma_off: int, beta_off: int, eps: float, u, y, stats):
+    _check(ctx, _lib.gpga_layer_norm(ctx, _ptr(x), _ptr(residual), T, D, ld, dtype, p, seed, layer, gamma_off, beta_off,
+                                     eps, _ptr(u), _ptr(y), _ptr(stats)))
+
+
+def gpga_layer_norm_grad(ctx, dy, u, stats, more, T: int, D: int, ld: int, dtype: int, p: float, seed: int, layer: int,
+                         gamma_off: int, beta_off: int, du, dx, accumulate: bool = False):
+    _check(ctx, _lib.gpga_layer_norm_grad(ctx, _ptr(dy), _ptr(u), _ptr(stats), _ptr(more), T, D, ld, dtype, p, seed,
+                                          layer, gamma_off, beta_off, _ptr(du), _ptr(dx), int(accumulate)))
+
+
+def gpga_token_loss(ctx, logits, labels, T: int, V: int, ld: int, dtype: int, grad_scale: float, loss, dlogits=None):
+    _check(ctx, _lib.gpga_token_loss(ctx, _ptr(logits), _ptr(labels), T, V, ld, dtype, grad_scale, _ptr(loss),
+                                     _ptr(dlogits)))
 
 
 def gpga_probe_stream(kind: int, src, dst, nbytes: int, stream=None, src2=None, inout=None, blocks_per_cu: int = 0):

@@ -221,6 +221,10 @@ struct gpga_ctx {
     float* aga_loss = nullptr;  // n minibatch losses (library-owned; used by gpga_run)
     size_t aga_loss_cap = 0;
 
+    // language-model operators: scratch of the call under way on the bound stream (library-owned)
+    char* op_scratch = nullptr;
+    size_t op_scratch_cap = 0;  // bytes
+
     char err[256] = {0};
 };
 

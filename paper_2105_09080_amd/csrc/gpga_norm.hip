@@ -1,0 +1,474 @@
+// Dropout with a residual sum, and layer norm of that sum, forward and backward, with a gamma and a beta for each node.
+//
+//   u = residual + mask * x * factor                                (dropout alone: y = u)
+//   y = gamma_i * (u - mean(u)) * rstd + beta_i,  rstd = 1 / sqrt(var(u) + eps)
+// backward, with h = gamma_i * dy and xh = (u - mean) * rstd:
+//   du = rstd * (h - mean(h) - xh * mean(h * xh)) + more,  dx = mask * du * factor
+//   dgamma_i = sum over t of dy * xh,  dbeta_i = sum over t of dy
+//
+// The mask is made anew wherever it is needed (gpga_rows.hpp).  Mean, variance and the backward means are fp32 sums over
+// values in registers; the variance is that of the differences from the mean, not a difference of sums.  y comes from u
+// before u is rounded for its own store.
+#include "gpga_rows.hpp"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kLongThreads = 1024;  // rows that do not fit into a workgroup's registers
+
+uint32_t blocks_for(int64_t items, int64_t per_block) { return (uint32_t)((items + per_block - 1) / per_block); }
+
+template <typename E>
+struct NormArgs {
+    typedef typename E::mem mem;
+    int32_t T, D;
+    int64_t ld, ldx;         // of the activations, of X and g
+    uint32_t per_node;       // workgroups of a node
+    DropArgs drop;
+    float eps;
+    const mem* x;            // forward: x; backward: dy
+    const mem* side;         // forward: residual; backward: more (may be NULL)
+    const mem* u_in;         // backward
+    mem* u;                  // forward: u (may be NULL); backward: du
+    mem* y;                  // forward: y; backward: dx (may be NULL)
+    float* stats;            // n*T pairs; forward: may be NULL
+    const float* gamma;      // columns of node 0 in X
+    const float* beta;
+    float* partial;          // backward: n * per_node * 2 * D
+};
+
+// ---- dropout ----------------------------------------------------------------------------------------------------------
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_dropout(NormArgs<E> a, int lanes_log2) {
+    const uint32_t node = blockIdx.x / a.per_node;
+    const int32_t t = (int32_t)((blockIdx.x - node * a.per_node) * (uint32_t)(kThreads >> lanes_log2)) + (int32_t)(threadIdx.x >> lanes_log2);
+    if (t >= a.T) return;
+    const int64_t row = ((int64_t)node * a.T + t) * a.ld;
+    const DropNode mask(a.drop, node);
+    const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
+    for (uint32_t q = threadIdx.x & ((1u << lanes_log2) - 1u); q < octs; q += 1u << lanes_log2) {
+        const int32_t c = (int32_t)q * kOct;
+        float v[kOct];
+        row_load<E>(a.x + row, c, a.D, v);
+        if (a.drop.drop) mask.apply(a.drop, (uint32_t)t * octs + q, v);
+        if (a.side) {
+            float r[kOct];
+            row_load<E>(a.side + row, c, a.D, r);
+#pragma unroll
+            for (int j = 0; j < kOct; ++j) v[j] += r[j];
+        }
+        row_store<E>(a.y + row, c, a.D, v);
+    }
+}
+
+// u of eight columns, before rounding.
+template <typename E>
+__device__ __forceinline__ void norm_input(const NormArgs<E>& a, const DropNode& mask, int64_t row, uint32_t group, int32_t c, float* v) {
+    row_load<E>(a.x + row, c, a.D, v);
+    if (a.drop.drop) mask.apply(a.drop, group, v);
+    if (a.side) {
+        float r[kOct];
+        row_load<E>(a.side + row, c, a.D, r);
+#pragma unroll
+        for (int j = 0; j < kOct; ++j) v[j] += r[j];
+    }
+}
+
+// y of eight columns from u.
+template <typename E>
+__device__ __forceinline__ void norm_output(const NormArgs<E>& a, uint32_t node, int64_t row, int32_t c, float mean, float rstd, const float* u) {
+    float gm[kOct], bt[kOct], y[kOct];
+    row_load<ElemF32>(a.gamma + (int64_t)node * a.ldx, c, a.D, gm);
+    row_load<ElemF32>(a.beta + (int64_t)node * a.ldx, c, a.D, bt);
+#pragma unroll
+    for (int j = 0; j < kOct; ++j) y[j] = (u[j] - mean) * rstd * gm[j] + bt[j];
+    row_store<E>(a.y + row, c, a.D, y);
+}
+
+// ---- forward: L lanes a row, N pieces of eight columns a lane, the row in registers ----------------------------------------
+template <typename E, int L, int N>
+__global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm(NormArgs<E> a) {
+    constexpr int kRows = L > kThreads ? 1 : kThreads / L;  // rows of a workgroup
+    __shared__ float s_sum[L > kWave ? L / kWave : 1];
+    const uint32_t node = blockIdx.x / a.per_node;
+    const int32_t t = (int32_t)((blockIdx.x - node * a.per_node) * kRows + threadIdx.x / L);
+    if (t >= a.T) return;  // all lanes of a row; whole workgroups where a sum spans wavefronts
+    const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
+    const int32_t lane = threadIdx.x & (L - 1);
+    const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
+    const DropNode mask(a.drop, node);
+    float u[N][kOct];
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int32_t q = lane + k * L, c = q * kOct;
+        if (c < a.D) {
+            norm_input<E>(a, mask, row, (uint32_t)t * octs + q, c, u[k]);
+#pragma unroll
+            for (int j = 0; j < kOct; ++j)
+                if (c + j < a.D) sum += u[k][j];
+        }
+    }
+    const float inv = 1.f / (float)a.D, mean = lanes_sum<L>(sum, s_sum) * inv;
+    float var = 0.f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int32_t c = (lane + k * L) * kOct;
+#pragma unroll
+        for (int j = 0; j < kOct; ++j)
+            if (c + j < a.D) var += (u[k][j] - mean) * (u[k][j] - mean);
+    }
+    const float rstd = 1.f / sqrtf(lanes_sum<L>(var, s_sum) * inv + a.eps);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int32_t c = (lane + k * L) * kOct;
+        if (c < a.D) {
+            if (a.u) row_store<E>(a.u + row, c, a.D, u[k]);
+            norm_output<E>(a, node, row, c, mean, rstd, u[k]);
+        }
+    }
+    if (a.stats && lane == 0) {
+        a.stats[2 * r] = mean;
+        a.stats[2 * r + 1] = rstd;
+    }
+}
+
+// Longer rows: one workgroup a row, which reads it three times (from the caches after the first).
+template <typename E>
+__global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs<E> a) {
+    __shared__ float s_sum[kLongThreads / kWave];
+    const uint32_t node = blockIdx.x / a.per_node;
+    const int32_t t = (int32_t)(blockIdx.x - node * a.per_node);
+    const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
+    const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
+    const DropNode mask(a.drop, node);
+    float sum = 0.f, var = 0.f, u[kOct];
+    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
+        norm_input<E>(a, mask, row, (uint32_t)t * octs + q, (int32_t)q * kOct, u);
+#pragma unroll
+        for (int j = 0; j < kOct; ++j) sum += (int32_t)q * kOct + j < a.D ? u[j] : 0.f;
+    }
+    const float inv = 1.f / (float)a.D, mean = lanes_sum<kLongThreads>(sum, s_sum) * inv;
+    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
+        norm_input<E>(a, mask, row, (uint32_t)t * octs + q, (int32_t)q * kOct, u);
+#pragma unroll
+        for (int j = 0; j < kOct; ++j) var += (int32_t)q * kOct + j < a.D ? (u[j] - mean) * (u[j] - mean) : 0.f;
+    }
+    const float rstd = 1.f / sqrtf(lanes_sum<kLongThreads>(var, s_sum) * inv + a.eps);
+    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
+        const int32_t c = (int32_t)q * kOct;
+        norm_input<E>(a, mask, row, (uint32_t)t * octs + q, c, u);
+        if (a.u) row_store<E>(a.u + row, c, a.D, u);
+        norm_output<E>(a, node, row, c, mean, rstd, u);
+    }
+    if (a.stats && threadIdx.x == 0) {
+        a.stats[2 * r] = mean;
+        a.stats[2 * r + 1] = rstd;
+    }
+}
+
+// ---- backward -----------------------------------------------------------------------------------------------------------
+// dy and xh of eight columns.
+template <typename E>
+__device__ __forceinline__ void grad_input(const NormArgs<E>& a, int64_t row, int32_t c, float mean, float rstd, float* dy, float* xh) {
+    row_load<E>(a.x + row, c, a.D, dy);
+    row_load<E>(a.u_in + row, c, a.D, xh, mean);
+#pragma unroll
+    for (int j = 0; j < kOct; ++j) xh[j] = (xh[j] - mean) * rstd;
+}
+// du and dx of eight columns.
+template <typename E>
+__device__ __forceinline__ void grad_output(const NormArgs<E>& a, const DropNode& mask, int64_t row, uint32_t group, int32_t c, float rstd, float m1,
+                                            float m2, const float* h, const float* xh) {
+    float du[kOct], more[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.side) row_load<E>(a.side + row, c, a.D, more);
+#pragma unroll
+    for (int j = 0; j < kOct; ++j) du[j] = rstd * (h[j] - m1 - xh[j] * m2) + more[j];
+    row_store<E>(a.u + row, c, a.D, du);
+    if (a.y) {
+        if (a.drop.drop) mask.apply(a.drop, group, du);
+        row_store<E>(a.y + row, c, a.D, du);
+    }
+}
+
+// L lanes a row.  A workgroup takes the rows t = strip, strip + strips, ... of a node kRows at a time, keeps its sums for
+// dgamma and dbeta in registers, and leaves them in `partial`.
+template <typename E, int L, int N>
+__global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormArgs<E> a) {
+    constexpr int kBlock = L > kThreads ? L : kThreads, kRows = kBlock / L;
+    __shared__ float s_sum[L > kWave ? L / kWave : 1];
+    __shared__ float s_part[kRows > 1 ? 2 * L * N * kOct : 1];
+    const uint32_t node = blockIdx.x / a.per_node, strip = blockIdx.x - node * a.per_node;
+    const int32_t lane = threadIdx.x & (L - 1), sub = threadIdx.x / L;
+    const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
+    const DropNode mask(a.drop, node);
+    const float inv = 1.f / (float)a.D;
+    float gm[N][kOct], dg[N][kOct], db[N][kOct];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int32_t c = (lane + k * L) * kOct;
+        if (c < a.D) row_load<ElemF32>(a.gamma + (int64_t)node * a.ldx, c, a.D, gm[k]);
+#pragma unroll
+        for (int j = 0; j < kOct; ++j) dg[k][j] = db[k][j] = 0.f;
+    }
+    for (int64_t t = (int64_t)strip * kRows + sub; t < a.T; t += (int64_t)a.per_node * kRows) {  // all lanes of a row alike
+        const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
+        const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1];
+        float dy[N][kOct], xh[N][kOct];
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int32_t c = (lane + k * L) * kOct;
+            if (c < a.D) {
+                grad_input<E>(a, row, c, mean, rstd, dy[k], xh[k]);
+#pragma unroll
+                for (int j = 0; j < kOct; ++j) {
+                    dg[k][j] += dy[k][j] * xh[k][j];
+                    db[k][j] += dy[k][j];
+                    dy[k][j] *= gm[k][j];  // h
+                    s1 += dy[k][j];
+                    s2 += dy[k][j] * xh[k][j];
+                }
+            }
+        }
+        s1 = lanes_sum<L>(s1, s_sum) * inv;
+        s2 = lanes_sum<L>(s2, s_sum) * inv;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int32_t q = lane + k * L, c = q * kOct;
+            if (c < a.D) grad_output<E>(a, mask, row, (uint32_t)t * octs + (uint32_t)q, c, rstd, s1, s2, dy[k], xh[k]);
+        }
+    }
+    // the rows of a workgroup one after another
+    float* out = a.partial + (int64_t)blockIdx.x * 2 * a.D;
+    if (kRows > 1) {
+        for (int turn = 0; turn < kRows; ++turn) {
+            if (sub == turn) {
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+#pragma unroll
+                    for (int j = 0; j < kOct; ++j) {
+                        const int32_t at = ((k * kOct + j) * L + lane) * 2;  // neighbouring lanes side by side
+                        s_part[at] = turn ? s_part[at] + dg[k][j] : dg[k][j];
+                        s_part[at + 1] = turn ? s_part[at + 1] + db[k][j] : db[k][j];
+                    }
+            }
+            __syncthreads();
+        }
+        if (sub == 0) {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+#pragma unroll
+                for (int j = 0; j < kOct; ++j) {
+                    const int32_t at = ((k * kOct + j) * L + lane) * 2;
+                    dg[k][j] = s_part[at];
+                    db[k][j] = s_part[at + 1];
+                }
+        }
+    }
+    if (sub == 0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int32_t c = (lane + k * L) * kOct;
+            if (c < a.D) {
+                row_store<ElemF32>(out, c, a.D, dg[k]);
+                row_store<ElemF32>(out + a.D, c, a.D, db[k]);
+            }
+        }
+    }
+}
+
+// Longer rows: sums over the tokens first (a lane a column, the tokens dealt to strips), since du may take dy's place; then du
+// and dx, one workgroup a row.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_norm_grad_columns(NormArgs<E> a, uint32_t column_blocks) {
+    const uint32_t node = blockIdx.x / (a.per_node * column_blocks), in_node = blockIdx.x - node * a.per_node * column_blocks;
+    const uint32_t strip = in_node / column_blocks;
+    const int64_t c = (int64_t)(in_node - strip * column_blocks) * kThreads + threadIdx.x;
+    if (c >= a.D) return;
+    float dg = 0.f, db = 0.f;
+    for (int64_t t = strip; t < a.T; t += a.per_node) {
+        const int64_t r = (int64_t)node * a.T + t;
+        const float dy = E::get(a.x[r * a.ld + c]);
+        dg += dy * ((E::get(a.u_in[r * a.ld + c]) - a.stats[2 * r]) * a.stats[2 * r + 1]);
+        db += dy;
+    }
+    float* out = a.partial + ((int64_t)node * a.per_node + strip) * 2 * a.D;
+    out[c] = dg;
+    out[a.D + c] = db;
+}
+template <typename E>
+__global__ __launch_bounds__(kLongThreads) void k_norm_grad_long(NormArgs<E> a) {
+    __shared__ float s_sum[kLongThreads / kWave];
+    const uint32_t node = blockIdx.x / (uint32_t)a.T;
+    const uint32_t t = blockIdx.x - node * (uint32_t)a.T;
+    const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
+    const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
+    const DropNode mask(a.drop, node);
+    const float inv = 1.f / (float)a.D, mean = a.stats[2 * r], rstd = a.stats[2 * r + 1];
+    const float* gamma = a.gamma + (int64_t)node * a.ldx;
+    float s1 = 0.f, s2 = 0.f, h[kOct], xh[kOct], gm[kOct];
+    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
+        grad_input<E>(a, row, (int32_t)q * kOct, mean, rstd, h, xh);
+        row_load<ElemF32>(gamma, (int32_t)q * kOct, a.D, gm);
+#pragma unroll
+        for (int j = 0; j < kOct; ++j) {
+            s1 += gm[j] * h[j];
+            s2 += gm[j] * h[j] * xh[j];
+        }
+    }
+    s1 = lanes_sum<kLongThreads>(s1, s_sum) * inv;
+    s2 = lanes_sum<kLongThreads>(s2, s_sum) * inv;
+    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
+        const int32_t c = (int32_t)q * kOct;
+        grad_input<E>(a, row, c, mean, rstd, h, xh);
+        row_load<ElemF32>(gamma, c, a.D, gm);
+#pragma unroll
+        for (int j = 0; j < kOct; ++j) h[j] *= gm[j];
+        grad_output<E>(a, mask, row, t * octs + q, c, rstd, s1, s2, h, xh);
+    }
+}
+
+// Adds the strips of a node: 64 columns a workgroup, its wavefronts share the strips; a fixed order.
+__global__ __launch_bounds__(kThreads) void k_norm_grad_join(const float* __restrict__ partial, uint32_t strips, int32_t D, uint32_t blocks_per_node,
+                                                             bool accumulate, float* __restrict__ g_gamma, float* __restrict__ g_beta, int64_t ldg) {
+    constexpr int kWaves = kThreads / kWave;
+    __shared__ float s_part[kWaves][kWave];
+    const uint32_t node = blockIdx.x / blocks_per_node;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t c = (int64_t)(blockIdx.x - node * blocks_per_node) * kWave + lane;  // 0 .. 2D-1: gamma's columns, then beta's
+    const float* from = partial + (int64_t)node * strips * 2 * D + c;
+    float sum = 0.f;
+    if (c < 2 * (int64_t)D)
+        for (uint32_t k = wave; k < strips; k += kWaves) sum += from[(int64_t)k * 2 * D];
+    s_part[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < 2 * (int64_t)D) {
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) sum += s_part[w][lane];
+        float* out = (c < D ? g_gamma + c : g_beta + (c - D)) + (int64_t)node * ldg;
+        *out = accumulate ? *out + sum : sum;
+    }
+}
+
+// Lanes a row and pieces a lane by the number of eights in it: the smallest that hold it.  f gets both as constants.
+template <int V>
+struct Const {
+    static constexpr int value = V;
+};
+template <typename F>
+bool with_row_shape(int32_t octs, F&& f) {
+    if (octs <= 16) f(Const<16>(), Const<1>());
+    else if (octs <= 32) f(Const<32>(), Const<1>());
+    else if (octs <= 64) f(Const<32>(), Const<2>());
+    else if (octs <= 96) f(Const<32>(), Const<3>());
+    else if (octs <= 128) f(Const<64>(), Const<2>());
+    else if (octs <= 192) f(Const<64>(), Const<3>());
+    else if (octs <= 256) f(Const<256>(), Const<1>());
+    else if (octs <= 512) f(Const<256>(), Const<2>());
+    else if (octs <= 1024) f(Const<512>(), Const<2>());
+    else return false;
+    return true;
+}
+
+// Strips of a node: four workgroups a compute unit over all nodes, no more than there are rows for.
+uint32_t norm_grad_strips(const RowsShape& s) {
+    const int64_t most = 1024 / s.n > 1 ? 1024 / s.n : 1;
+    return (uint32_t)(s.T < most ? (s.T > 0 ? s.T : 1) : most);
+}
+
+}  // namespace
+
+hipError_t launch_dropout(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* x, const void* residual, void* y) {
+    return with_elem(s.dtype, [&](auto e) {
+        typedef decltype(e) E;
+        typedef typename E::mem M;
+        NormArgs<E> a = {};
+        a.T = s.T;
+        a.D = s.D;
+        a.ld = s.ld;
+        a.drop = drop;
+        a.x = static_cast<const M*>(x);
+        a.side = static_cast<const M*>(residual);
+        a.y = static_cast<M*>(y);
+        const int32_t octs = (s.D + kOct - 1) / kOct;
+        int lanes_log2 = 0;
+        while (lanes_log2 < 8 && (1 << lanes_log2) < octs) ++lanes_log2;
+        a.per_node = blocks_for(s.T, kThreads >> lanes_log2);
+        k_dropout<E><<<dim3(a.per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, lanes_log2);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_norm(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* x, const void* residual, int64_t gamma_off,
+                       int64_t beta_off, float eps, void* u, void* y, float* stats) {
+    return with_elem(s.dtype, [&](auto e) {
+        typedef decltype(e) E;
+        typedef typename E::mem M;
+        NormArgs<E> a = {};
+        a.T = s.T;
+        a.D = s.D;
+        a.ld = s.ld;
+        a.ldx = c->ld;
+        a.drop = drop;
+        a.eps = eps;
+        a.x = static_cast<const M*>(x);
+        a.side = static_cast<const M*>(residual);
+        a.u = static_cast<M*>(u);
+        a.y = static_cast<M*>(y);
+        a.stats = stats;
+        a.gamma = c->x + gamma_off;
+        a.beta = c->x + beta_off;
+        const bool held = with_row_shape((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
+            constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
+            a.per_node = blocks_for(s.T, kBlock / L);
+            k_norm<E, L, N><<<dim3(a.per_node * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
+        });
+        if (!held) {
+            a.per_node = (uint32_t)s.T;
+            k_norm_long<E><<<dim3(a.per_node * (uint32_t)s.n), dim3(kLongThreads), 0, c->stream>>>(a);
+        }
+        return hipGetLastError();
+    });
+}
+
+size_t norm_grad_scratch(const RowsShape& s) { return (size_t)s.n * norm_grad_strips(s) * 2 * (size_t)s.D * sizeof(float); }
+
+hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* dy, const void* u, const float* stats,
+                            const void* more, int64_t gamma_off, int64_t beta_off, void* du, void* dx, bool accumulate, void* scratch) {
+    const uint32_t strips = norm_grad_strips(s);
+    const hipError_t e = with_elem(s.dtype, [&](auto el) {
+        typedef decltype(el) E;
+        typedef typename E::mem M;
+        NormArgs<E> a = {};
+        a.T = s.T;
+        a.D = s.D;
+        a.ld = s.ld;
+        a.ldx = c->ld;
+        a.drop = drop;
+        a.x = static_cast<const M*>(dy);
+        a.side = static_cast<const M*>(more);
+        a.u_in = static_cast<const M*>(u);
+        a.u = static_cast<M*>(du);
+        a.y = static_cast<M*>(dx);
+        a.stats = const_cast<float*>(stats);
+        a.gamma = c->x + gamma_off;
+        a.partial = static_cast<float*>(scratch);
+        a.per_node = strips;
+        const bool held = with_row_shape((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
+            constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
+            k_norm_grad<E, L, N><<<dim3(strips * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
+        });
+        if (!held) {
+            const uint32_t column_blocks = blocks_for(s.D, kThreads);
+            k_norm_grad_columns<E><<<dim3(strips * column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, column_blocks);
+            if (s.T > 0) k_norm_grad_long<E><<<dim3((uint32_t)s.T * (uint32_t)s.n), dim3(kLongThreads), 0, c->stream>>>(a);
+        }
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    const uint32_t blocks = blocks_for(2 * (int64_t)s.D, kWave);
+    k_norm_grad_join<<<dim3(blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(static_cast<const float*>(scratch), strips, s.D, blocks, accumulate,
+                                                                                  c->g + gamma_off, c->g + beta_off, c->ld);
+    return hipGetLastError();
+}

@@ -9,6 +9,9 @@ import torch
 from . import binding as B
 
 
+_DTYPE = {torch.float32: B.GPGA_F32, torch.bfloat16: B.GPGA_BF16, torch.float16: B.GPGA_F16}
+
+
 class Simulation:
     """n simulated nodes with d parameters each on one GPU.
 
@@ -171,6 +174,117 @@ class Simulation:
         out = torch.empty(self.d, dtype=torch.float32, device=self.device)
         B.gpga_mean(self.ctx, out)
         return out
+
+    # -- operators of language models --------------------------------------------------
+    # Activations are (n, T, D) tensors whose tokens lie a common number of elements apart (rows of a wider tensor are
+    # fine); parameters are named by their column offset in X, their gradients land in the same columns of G.  What the
+    # calls return is allocated for, and written on, the simulation's stream.
+    def _empty(self, shape, dtype, ld: int | None = None):
+        """Memory of the simulation's stream; rows ``ld`` elements apart if that is more than the last dimension."""
+        width = shape[-1] if ld is None else ld
+        if torch.cuda.current_stream(self.device) == self.stream:
+            t = torch.empty((*shape[:-1], width), dtype=dtype, device=self.device)
+        else:
+            with torch.cuda.stream(self.stream):
+                t = torch.empty((*shape[:-1], width), dtype=dtype, device=self.device)
+        return t if width == shape[-1] else t[..., : shape[-1]]
+
+    def _tokens(self, t: torch.Tensor) -> int:
+        """Tokens a node of an (n, T) int32 tensor."""
+        if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != self.n or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError(f"expected a contiguous (n = {self.n}, T) int32 tensor on the GPU, got {tuple(t.shape)} {t.dtype}")
+        return t.shape[1]
+
+    def _rows(self, first: torch.Tensor, *others):
+        """(T, D, ld, dtype) of activations of one call."""
+        if first.dim() != 3 or first.shape[0] != self.n or first.dtype not in _DTYPE or not first.is_cuda:
+            raise ValueError(f"expected an (n = {self.n}, T, D) fp32, bf16 or fp16 tensor on the GPU, got {tuple(first.shape)} {first.dtype}")
+        _, T, D = first.shape
+        ld = first.stride(1) if T > 1 else first.stride(0) if self.n > 1 else D
+        for t in (first, *others):
+            if t is None:
+                continue
+            if t.shape != first.shape or t.dtype != first.dtype or t.device != first.device:
+                raise ValueError("the activations of a call differ in shape, type or device")
+            if t.numel() and (ld < D or (D > 1 and t.stride(2) != 1) or (T > 1 and t.stride(1) != ld) or
+                              (self.n > 1 and t.stride(0) != T * ld)):
+                raise ValueError("the activations of a call need rows that are dense and a common number of elements apart")
+        return T, D, max(ld, D), _DTYPE[first.dtype]
+
+    def _used(self, *tensors):
+        """Memory that another stream allocated is not handed out again before this stream is through with it."""
+        if torch.cuda.current_stream(self.device) != self.stream:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
+    def embed(self, tokens: torch.Tensor, table_off: int, V: int, D: int, *, scale: float = 1.0,
+              dtype: torch.dtype = torch.float32) -> torch.Tensor:
+        """scale * E_i[tokens]: (n, T, D); tokens below 0 give zeros."""
+        T = self._tokens(tokens)
+        y = self._empty((self.n, T, D), dtype)
+        B.gpga_embed(self.ctx, tokens, T, table_off, V, D, scale, y, D, _DTYPE[dtype])
+        self._used(tokens)
+        return y
+
+    def embed_grad(self, tokens: torch.Tensor, dy: torch.Tensor, table_off: int, V: int, *, scale: float = 1.0,
+                   accumulate: bool = False):
+        """Gradient of the table into G[:, table_off : table_off + V*D]."""
+        T, D, ld, dt = self._rows(dy)
+        if self._tokens(tokens) != T:
+            raise ValueError("tokens and dy differ in their tokens a node")
+        B.gpga_embed_grad(self.ctx, tokens, T, table_off, V, D, scale, dy, ld, dt, accumulate)
+        self._used(tokens, dy)
+
+    def dropout(self, x: torch.Tensor, p: float, *, seed: int, layer: int = 0, residual: torch.Tensor | None = None,
+                out: torch.Tensor | None = None) -> torch.Tensor:
+        """residual + mask * x / (1 - p), the mask that of iteration k; with x = a gradient, its backward pass."""
+        T, D, ld, dt = self._rows(x, residual, out)
+        y = self._empty((self.n, T, D), x.dtype, ld=ld) if out is None else out
+        B.gpga_dropout(self.ctx, x, residual, T, D, ld, dt, p, seed, layer, y)
+        self._used(x, residual, out)
+        return y
+
+    def layer_norm(self, x: torch.Tensor, gamma_off: int, beta_off: int, *, eps: float = 1e-5,
+                   residual: torch.Tensor | None = None, p: float = 0.0, seed: int = 0, layer: int = 0):
+        """(y, u, stats): layer norm y of u = residual + dropout(x); u is x itself where there is neither."""
+        T, D, ld, dt = self._rows(x, residual)
+        y = self._empty((self.n, T, D), x.dtype, ld=ld)
+        plain = residual is None and p == 0.0
+        u = x if plain else self._empty((self.n, T, D), x.dtype, ld=ld)
+        stats = self._empty((self.n, T, 2), torch.float32)
+        B.gpga_layer_norm(self.ctx, x, residual, T, D, ld, dt, p, seed, layer, gamma_off, beta_off, eps,
+                          None if plain else u, y, stats)
+        self._used(x, residual)
+        return y, u, stats
+
+    def layer_norm_grad(self, dy: torch.Tensor, u: torch.Tensor, stats: torch.Tensor, gamma_off: int, beta_off: int, *,
+                        p: float = 0.0, seed: int = 0, layer: int = 0, more: torch.Tensor | None = None,
+                        accumulate: bool = False):
+        """(du, dx): gradients of the residual and of x; those of gamma and beta land in G.  dx is du where p is 0."""
+        T, D, ld, dt = self._rows(dy, u, more)
+        if stats.dtype != torch.float32 or tuple(stats.shape) != (self.n, T, 2) or not stats.is_contiguous():
+            raise ValueError("stats are the (n, T, 2) fp32 pairs that layer_norm returns")
+        du = self._empty((self.n, T, D), dy.dtype, ld=ld)
+        drops = int(float(np.float32(p)) * 65536 + 0.5) > 0     # p as the library keeps it
+        dx = self._empty((self.n, T, D), dy.dtype, ld=ld) if drops else None
+        B.gpga_layer_norm_grad(self.ctx, dy, u, stats, more, T, D, ld, dt, p, seed, layer, gamma_off, beta_off, du, dx,
+                               accumulate)
+        self._used(dy, u, stats, more)
+        return du, du if dx is None else dx
+
+    def token_loss(self, logits: torch.Tensor, labels: torch.Tensor, *, grad=True, grad_scale: float = 1.0):
+        """(loss, dlogits): n mean losses, and the gradient (None if ``grad`` is False, in the tensor ``grad`` if it
+        is one, e.g. ``logits`` itself)."""
+        into = grad if isinstance(grad, torch.Tensor) else None
+        T, V, ld, dt = self._rows(logits, into)
+        if self._tokens(labels) != T:
+            raise ValueError("labels and logits differ in their tokens a node")
+        loss = self._empty((self.n,), torch.float32)
+        dlogits = into if into is not None else self._empty((self.n, T, V), logits.dtype, ld=ld) if grad else None
+        B.gpga_token_loss(self.ctx, logits, labels, T, V, ld, dt, grad_scale, loss, dlogits)
+        self._used(logits, labels, into)
+        return loss, dlogits
 
     def tune(self, launches: int = 16):
         """Let the pacing controllers settle (state arrays are left with unspecified contents)."""

@@ -1,0 +1,569 @@
+"""The language-model operators on the GPU against the float64 oracle, through the C ABI: every element type, lengths of
+zero and one, odd and strided rows, masks that leave nothing, infinities, tokens out of range, reruns, other streams,
+captured graphs, refusals.
+
+Tolerances.  u is the unit roundoff of the activations' type (2^-24, 2^-8, 2^-11); a result is rounded to it once, so it
+may be off by u|result| (half the smallest subnormal for fp16).  Before that all arithmetic is fp32: a sum of terms is off by
+at most 2^-24 times the length of the longest chain of additions times the sum of their magnitudes.  Chains: the tokens of a
+table row for the embedding; 64 for a sum over a row held by 16 to 1024 lanes (at most 32 terms a lane for rows up to
+32768, then at most 6 + 16); the tokens of a node + 64 for the gradients of gamma and beta.  exp is good to
+2^-23 (|argument| + 2) relative.
+"""
+import numpy as np
+import pytest
+
+from oracle import token_oracle as orc
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": (torch.float32, 2.0 ** -24, 0.0), "bf16": (torch.bfloat16, 2.0 ** -8, 0.0), "f16": (torch.float16, 2.0 ** -11, 2.0 ** -25)}
+E32 = 2.0 ** -24
+TINY = 1e-37          # what fp32 flushes
+
+
+@pytest.fixture(scope="module")
+def hx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2105_09080_amd import harness
+    return harness
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def make_sim(hx, n, d, seed, ld=None, **kw):
+    rng = np.random.default_rng(seed)
+    X = rng.normal(size=(n, d)).astype(np.float32)
+    sim = hx.Simulation(n, d, topology="ring", H=4, lr=0.1, ld=ld, **kw)
+    sim.set_state(X=X)
+    return sim, X, rng
+
+
+def rows(rng, shape, dtype, pad=0, scale=1.0):
+    """An (n, T, D) device tensor whose rows lie D + pad elements apart."""
+    n, T, D = shape
+    t = torch.zeros((n, T, D + pad), dtype=dtype, device="cuda")
+    t[..., :D] = torch.as_tensor(rng.normal(size=shape) * scale).to(dtype).cuda()
+    return t[..., :D]
+
+
+def close(got, want, tol, what):
+    got, tol = host(got) if isinstance(got, torch.Tensor) else got, np.broadcast_to(tol, want.shape)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), f"{what}: NaN in other places"
+    fine = ~np.isnan(want)
+    inf = np.isinf(want)
+    assert np.array_equal(got[inf], want[inf]), f"{what}: infinities differ"
+    fine &= ~inf
+    off = np.abs(got[fine] - want[fine]) - tol[fine]
+    assert off.size == 0 or off.max() <= 0, f"{what}: {off.max():.3e} over the tolerance at {np.argmax(off)} of {off.size}"
+
+
+def some_tokens(rng, n, T, V, kind):
+    if kind == "same":
+        return np.full((n, T), V - 1)
+    if kind == "padding":
+        return np.full((n, T), -1)
+    tok = np.minimum((V + 1.0) ** rng.random((n, T)) - 1, V - 1).astype(np.int64)   # frequencies fall as 1 / rank
+    if kind == "mixed":
+        tok[rng.random((n, T)) < 0.2] = -7
+    return tok
+
+
+EMBED = [  # n, T, V, D, off, padding of the rows, tokens
+    (1, 1, 1, 1, 0, 0, "zipf"), (3, 5, 7, 8, 0, 0, "mixed"), (2, 33, 100, 257, 3, 0, "mixed"), (1, 1, 1000, 768, 0, 0, "zipf"),
+    (5, 64, 13, 129, 1, 7, "zipf"), (2, 500, 40, 24, 0, 8, "mixed"), (1, 300, 3, 1030, 5, 1, "same"), (2, 70, 9, 16, 0, 0, "padding"),
+    (1, 9, 50, 4100, 2, 0, "zipf"), (3, 0, 5, 8, 0, 0, "zipf"), (2, 1500, 700, 31, 0, 1, "zipf"), (1, 4097, 2, 65, 0, 0, "mixed"),
+]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,T,V,D,off,pad,kind", EMBED)
+def test_embedding(hx, n, T, V, D, off, pad, kind, dtype):
+    dt, u, sub = TYPES[dtype]
+    sim, X, rng = make_sim(hx, n, off + V * D + 3, seed=T + V, ld=off + V * D + 5)
+    tokens = some_tokens(rng, n, T, V, kind)
+    tok_d = torch.as_tensor(tokens, dtype=torch.int32).cuda()
+    y = sim.embed(tok_d, off, V, D, scale=1.37, dtype=dt)
+    want = orc.embed(X[:, off:off + V * D].reshape(n, V, D), tokens, float(np.float32(1.37)))
+    close(y, want, (u + 2 * E32) * np.abs(want) + sub, "y")
+
+    dy = rows(rng, (n, T, D), dt, pad)
+    before = rng.normal(size=sim.G.shape).astype(np.float32)
+    g, size, count = orc.embed_grad(tokens, host(dy), V, float(np.float32(1.37)))
+    for accumulate in (False, True):
+        sim.set_state(G=before)
+        sim.embed_grad(tok_d, dy, off, V, scale=1.37, accumulate=accumulate)
+        got = host(sim.G)
+        had = before[:, off:off + V * D].reshape(n, V, D).astype(np.float64) * accumulate
+        tol = E32 * (count + 2) * size + 2 * E32 * np.abs(had + g)
+        close(got[:, off:off + V * D].reshape(n, V, D), had + g, tol, f"gradient, accumulate={accumulate}")
+        assert np.array_equal(got[:, :off], before[:, :off]) and np.array_equal(got[:, off + V * D:], before[:, off + V * D:])
+        if accumulate:
+            untouched = np.broadcast_to(count == 0, g.shape)
+            assert np.array_equal(got[:, off:off + V * D].reshape(n, V, D)[untouched],
+                                  before[:, off:off + V * D].reshape(n, V, D)[untouched])
+    sim.close()
+
+
+@pytest.mark.parametrize("T", [4095, 4096, 4097, 8192, 9001, 20000])
+@pytest.mark.parametrize("V", [2, 255, 256, 257, 70_000])
+def test_embedding_gradient_across_the_tiles_of_the_sort(hx, T, V):
+    n, D = 2, 8
+    sim, X, rng = make_sim(hx, n, V * D, seed=T + V)
+    tokens = rng.integers(-1, V, size=(n, T))
+    tokens[0, : T // 3] = V // 2                                # a run across tiles and chunks
+    dy = rows(rng, (n, T, D), torch.float32)
+    tok_d = torch.as_tensor(tokens, dtype=torch.int32).cuda()
+    sim.embed_grad(tok_d, dy, 0, V, scale=0.5)
+    g, size, count = orc.embed_grad(tokens, host(dy), V, 0.5)
+    close(sim.G.reshape(n, V, D), g, E32 * (count + 2) * size, "gradient")
+    first = sim.G.clone()
+    sim.embed_grad(tok_d, dy, 0, V, scale=0.5)
+    assert torch.equal(first, sim.G), "a second run gives other bits"
+    sim.close()
+
+
+def test_tokens_out_of_range_are_no_addresses(hx):
+    n, T, V, D = 3, 40, 11, 24
+    sim, X, rng = make_sim(hx, n, V * D + 2, seed=5)
+    tokens = some_tokens(rng, n, T, V, "mixed")
+    tokens[1, 7], tokens[1, 20], tokens[2, 3] = V, 2 ** 31 - 1, -2 ** 31
+    tok_d = torch.as_tensor(tokens.astype(np.int32)).cuda()
+    want = orc.embed(X[:, :V * D].reshape(n, V, D), tokens, 1.0)
+    close(sim.embed(tok_d, 0, V, D), want, 2 * E32 * np.abs(want), "y")
+    dy = rows(rng, (n, T, D), torch.float32)
+    for accumulate in (False, True):
+        sim.set_state(G=np.ones(sim.G.shape))
+        sim.embed_grad(tok_d, dy, 0, V, accumulate=accumulate)
+        got = host(sim.G)
+        assert np.isnan(got[1, :V * D]).all() and np.isfinite(got[[0, 2]]).all() and (got[:, V * D:] == 1).all()
+    sim.close()
+
+
+def test_tables_beyond_32_bit_offsets(hx):
+    n, V, D = 2, 1_100_000, 2000                                # 2.2e9 floats a node: 17.6 GB an array
+    sim = hx.Simulation(n, V * D, topology="none", H=0, lr=0.1)
+    tokens = torch.tensor([[0, V - 1, 5], [V - 1, V - 2, V - 1]], dtype=torch.int32, device="cuda")
+    x = sim.X.view(n, V, D)
+    for i in range(n):
+        for t in tokens[i].tolist():
+            x[i, t] = torch.randn(D, device="cuda")
+    y = sim.embed(tokens, 0, V, D, scale=1.0)
+    for i in range(n):
+        assert torch.equal(y[i], x[i][tokens[i].long()])
+    dy = torch.randn((n, 3, D), device="cuda")
+    sim.G.fill_(1.0)
+    sim.embed_grad(tokens, dy, 0, V)
+    g = sim.G.view(n, V, D)
+    assert torch.equal(g[0, V - 1], dy[0, 1]) and torch.equal(g[1, V - 2], dy[1, 1])
+    assert torch.equal(g[1, V - 1], dy[1, 0] + dy[1, 2])
+    assert int(torch.count_nonzero(g[0])) == 3 * D and int(torch.count_nonzero(g[1])) == 2 * D
+    sim.close()
+
+
+NORM = [  # n, T, D, gamma's column, padding of the rows
+    (1, 1, 1, 0, 0), (2, 3, 7, 1, 0), (3, 5, 8, 0, 0), (2, 17, 127, 3, 1), (2, 9, 128, 0, 8), (1, 33, 129, 2, 0), (2, 6, 257, 0, 3),
+    (2, 10, 768, 0, 0), (1, 5, 770, 1, 0), (2, 4, 1024, 0, 0), (1, 7, 1537, 5, 2), (1, 3, 2049, 0, 0), (1, 2, 4096, 0, 8),
+    (2, 3, 4099, 1, 0), (1, 2, 8192, 0, 0), (1, 3, 8193, 7, 0), (1, 1, 16391, 0, 1), (3, 0, 40, 0, 0), (1, 1100, 96, 0, 0), (40, 3, 65, 2, 5),
+]
+
+
+def dropped_bound(x, residual, factor):
+    """Magnitude that the rounding of residual + x * factor goes by."""
+    return np.abs(x) * factor + (0.0 if residual is None else np.abs(residual))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("p,with_residual", [(0.0, False), (0.0, True), (0.1, True), (0.75, False)])
+@pytest.mark.parametrize("n,T,D,off,pad", NORM)
+def test_dropout_and_layer_norm(hx, n, T, D, off, pad, p, with_residual, dtype):
+    dt, u, sub = TYPES[dtype]
+    sim, X, rng = make_sim(hx, n, off + 2 * D + 1, seed=D + T)
+    goff, boff, eps, seed, layer, k = off, off + D, 1e-3, 0xFEDCBA9876543210, 12345, 77
+    sim.set_state(k=k)
+    gamma, beta = X[:, goff:goff + D], X[:, boff:boff + D]
+    x = rows(rng, (n, T, D), dt, pad)
+    residual = rows(rng, (n, T, D), dt, pad) if with_residual else None
+    hx_, hr = host(x), None if residual is None else host(residual)
+    want_u = orc.dropout(hx_, hr, p, seed, layer, k)
+    mag = dropped_bound(hx_, hr, 1 / (1 - p) + 1e-3)
+    tol_u = u * np.abs(want_u) + 3 * E32 * mag + sub
+
+    close(sim.dropout(x, p, seed=seed, layer=layer, residual=residual), want_u, tol_u, "dropout")
+    y, got_u, stats = sim.layer_norm(x, goff, boff, eps=eps, residual=residual, p=p, seed=seed, layer=layer)
+    close(got_u, want_u, tol_u, "u")
+    if T:
+        want_y, mean, rstd = orc.layer_norm(want_u, gamma, beta, eps)
+        size = mag.mean(axis=2)                                  # of the terms of the mean
+        tol_mean = 66 * E32 * size
+        close(stats[..., 0], mean, tol_mean, "mean")
+        # variance: 68 roundings of each square, and what an error of the mean and of u moves a difference by
+        spread = np.sqrt(np.maximum(1 / rstd ** 2 - eps, 0))
+        diff = tol_mean + 3 * E32 * mag.max(axis=2)
+        tol_var = 72 * E32 * spread ** 2 + 2 * spread * diff + diff ** 2
+        tol_rstd = 0.5 * rstd ** 3 * tol_var * 1.01 + 4 * E32 * rstd
+        close(stats[..., 1], rstd, tol_rstd, "rstd")
+        g, b = np.abs(gamma[:, None, :]), np.abs(beta[:, None, :])
+        xh = np.abs(want_u - mean[..., None]) * rstd[..., None]
+        tol_y = u * np.abs(want_y) + sub + g * (xh * (tol_rstd / rstd)[..., None] + rstd[..., None] * (tol_mean[..., None] + 3 * E32 * mag)) \
+            + 6 * E32 * (g * xh + b)
+        close(y, want_y, tol_y, "y")
+    sim.close()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("p,with_more,accumulate", [(0.0, False, False), (0.0, True, True), (0.25, True, False)])
+@pytest.mark.parametrize("n,T,D,off,pad", NORM)
+def test_layer_norm_gradient(hx, n, T, D, off, pad, p, with_more, accumulate, dtype):
+    dt, u, sub = TYPES[dtype]
+    sim, X, rng = make_sim(hx, n, off + 2 * D + 1, seed=D + T + 1)
+    goff, boff, seed, layer, k = off + D, off, 99, 3, 5          # beta before gamma
+    sim.set_state(k=k)
+    gamma = X[:, goff:goff + D]
+    dy, un = rows(rng, (n, T, D), dt, pad), rows(rng, (n, T, D), dt, pad, 2.0)
+    more = rows(rng, (n, T, D), dt, pad) if with_more else None
+    hu, hdy = host(un), host(dy)
+    mean = hu.mean(axis=2).astype(np.float32) if T else np.zeros((n, 0), np.float32)
+    rstd = (1 / np.sqrt(hu.var(axis=2) + 1e-3)).astype(np.float32) if T else mean
+    stats = torch.as_tensor(np.stack([mean, rstd], axis=2)).cuda()
+    before = rng.normal(size=sim.G.shape).astype(np.float32)
+    sim.set_state(G=before)
+    du, dx = sim.layer_norm_grad(dy, un, stats, goff, boff, p=p, seed=seed, layer=layer, more=more, accumulate=accumulate)
+    mean, rstd = mean.astype(np.float64), rstd.astype(np.float64)
+    want, dgamma, dbeta = orc.layer_norm_grad(hdy, hu, mean, rstd, gamma)
+    xh = np.abs((hu - mean[..., None]) * rstd[..., None])
+    h = np.abs(hdy * gamma[:, None, :])
+    hm = 0.0 if more is None else host(more)
+    if T:
+        # xh is off by 2 roundings (the difference of exact values, the product); h by one; 66 for the means
+        tol32 = rstd[..., None] * E32 * (8 * h + 70 * h.mean(axis=2, keepdims=True) + xh * 76 * (h * xh).mean(axis=2, keepdims=True)) \
+            + 2 * E32 * np.abs(hm)
+        want = want + hm
+        close(du, want, u * np.abs(want) + 2 * E32 * np.abs(want) + tol32 + sub, "du")
+        if p == 0.0:
+            assert dx is du
+        else:
+            keep, factor = orc.dropout_keep(n, T, D, p, seed, layer, k)
+            wx = np.where(keep, want * factor, 0.0)
+            close(dx, wx, np.where(keep, u * np.abs(wx) + 3 * E32 * np.abs(wx) + factor * tol32 + sub, 0.0), "dx")
+    got = host(sim.G)
+    for name, at, w, size in (("dgamma", goff, dgamma, (np.abs(hdy) * xh).sum(axis=1)), ("dbeta", boff, dbeta, np.abs(hdy).sum(axis=1))):
+        had = before[:, at:at + D].astype(np.float64) * accumulate
+        close(got[:, at:at + D], had + w, E32 * (T + 66) * size + 2 * E32 * np.abs(had + w), name)
+    assert np.array_equal(got[:, :off], before[:, :off]) and np.array_equal(got[:, off + 2 * D:], before[:, off + 2 * D:])
+    sim.close()
+
+
+def test_layer_norm_gradient_along_a_direction(hx):
+    """The gradients against a central difference of the forward pass, all fp32, dropout on: a step of 2^-6 in every
+    argument, whose own error is of third order (below 2^-12 of the sum's terms here) beside rounding of the two sums."""
+    n, T, D, p = 2, 6, 40, 0.25
+    sim, X, rng = make_sim(hx, n, 2 * D, seed=3)
+    w = rng.normal(size=(n, T, D))
+    x0, r0 = rng.normal(size=(n, T, D)), rng.normal(size=(n, T, D))
+    sx, sr, sp = rng.normal(size=x0.shape), rng.normal(size=x0.shape), rng.normal(size=X.shape)
+
+    def value(step):
+        sim.set_state(X=X + step * sp)
+        x = torch.as_tensor(x0 + step * sx, dtype=torch.float32).cuda()
+        r = torch.as_tensor(r0 + step * sr, dtype=torch.float32).cuda()
+        y, u, stats = sim.layer_norm(x, 0, D, eps=1e-2, residual=r, p=p, seed=8)
+        return (host(y) * w).sum(), u, stats
+
+    h = 2.0 ** -6
+    slope = (value(h)[0] - value(-h)[0]) / (2 * h)
+    _, u, stats = value(0.0)
+    sim.G.zero_()
+    du, dx = sim.layer_norm_grad(torch.as_tensor(w, dtype=torch.float32).cuda(), u, stats, 0, D, p=p, seed=8)
+    inner = (host(du) * sr).sum() + (host(dx) * sx).sum() + (host(sim.G) * sp).sum()
+    size = np.abs(host(du) * sr).sum() + np.abs(host(dx) * sx).sum() + np.abs(host(sim.G) * sp).sum()
+    assert abs(slope - inner) <= 2.0 ** -12 * size
+    sim.close()
+
+
+def test_rows_without_variance_and_rows_with_infinities(hx):
+    n, T, D = 2, 4, 100
+    sim, X, rng = make_sim(hx, n, 2 * D, seed=1)
+    x = torch.full((n, T, D), 3.0, device="cuda")
+    x[0, 1, 5], x[1, 2, 7] = float("inf"), float("nan")
+    y, u, stats = sim.layer_norm(x, 0, D)
+    got = host(y)
+    for i in range(n):
+        for t in range(T):
+            if (i, t) in ((0, 1), (1, 2)):
+                assert np.isnan(got[i, t]).all()
+            else:
+                assert np.allclose(got[i, t], X[i, D:], rtol=0, atol=64 * E32 * 3.0 / np.sqrt(1e-5) * np.abs(X[i, :D]).max())
+    # what is dropped may be anything
+    keep, _ = orc.dropout_keep(n, T, D, 0.5, 4, 0, 0)
+    bad = torch.where(torch.as_tensor(keep).cuda(), torch.ones((), device="cuda"), torch.full((), float("inf"), device="cuda"))
+    bad[~torch.as_tensor(keep).cuda() & (torch.rand((n, T, D), device="cuda") < 0.5)] = float("nan")
+    assert np.array_equal(host(sim.dropout(bad, 0.5, seed=4)), keep * 2.0)
+    sim.close()
+
+
+def test_dropout_in_place_and_backward(hx):
+    n, T, D = 3, 50, 77
+    sim, X, rng = make_sim(hx, n, 4, seed=2)
+    x = rows(rng, (n, T, D), torch.float32)
+    want = sim.dropout(x, 0.3, seed=6, layer=2)
+    mask = sim.dropout(torch.ones_like(x), 0.3, seed=6, layer=2)
+    assert torch.equal(want, x * mask)
+    residual = rows(rng, (n, T, D), torch.float32)
+    both = sim.dropout(x, 0.3, seed=6, layer=2, residual=residual)
+    assert sim.dropout(x.clone(), 0.3, seed=6, layer=2, residual=residual, out=residual) is residual
+    assert torch.equal(residual, both)
+    y = x.clone()
+    sim.dropout(y, 0.3, seed=6, layer=2, out=y)
+    assert torch.equal(y, want)
+    sim.set_state(k=1)
+    assert not torch.equal(sim.dropout(x, 0.3, seed=6, layer=2), want)
+    sim.close()
+
+
+LOSS = [  # n, T, V, padding of the rows
+    (1, 1, 1, 0), (2, 3, 2, 0), (3, 5, 7, 1), (2, 4, 64, 0), (2, 9, 257, 3), (1, 40, 1000, 0), (2, 3, 2049, 0), (1, 5, 5003, 5),
+    (2, 6, 8200, 0), (1, 3, 32000, 0), (1, 2, 40001, 1), (4, 1, 128000, 0), (1, 1, 300007, 0), (3, 0, 10, 0), (30, 11, 50, 2),
+    (1, 600, 33, 0), (2, 300, 3001, 0), (1, 520, 9000, 0),
+]
+
+
+def loss_bounds(z, labels, dz, scale, u, sub):
+    """Tolerances of the mean losses and of the gradient (see the top of the file)."""
+    counted = labels >= 0
+    N = np.maximum(counted.sum(axis=1), 1)
+    with np.errstate(invalid="ignore", over="ignore"):
+        top = np.where(np.isneginf(z).all(axis=2, keepdims=True), 0.0, z.max(axis=2, keepdims=True))
+        arg = np.where(np.isfinite(z), np.abs(z - top), 0.0)
+        q = np.exp(z - top)
+        total = q.sum(axis=2, keepdims=True)
+        q = q / total
+        rel = 2 * E32 * ((q * (arg + 2)).sum(axis=2) + 40)      # of the sum of exp
+        pick = np.take_along_axis(arg, np.clip(labels, 0, z.shape[2] - 1)[..., None], axis=2)[..., 0]
+        tol_row = rel + 4 * E32 * (np.log(total[..., 0]) + pick)
+        tol_loss = np.where(counted, tol_row, 0.0).sum(axis=1) / N
+        loss_size = np.where(counted, np.log(total[..., 0]) + pick, 0.0).sum(axis=1) / N
+        a = (abs(scale) / N)[:, None, None]
+        onehot = np.zeros_like(z)
+        np.put_along_axis(onehot, np.clip(labels, 0, z.shape[2] - 1)[..., None], 1.0, axis=2)
+        tol_dz = u * np.abs(dz) + sub + a * (q * (2 * E32 * (arg + 4) + rel[..., None]) + 4 * E32 * onehot) + TINY
+    return tol_loss + 2 * E32 * loss_size, np.where(counted[..., None], tol_dz, 0.0)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,T,V,pad", LOSS)
+def test_token_loss(hx, n, T, V, pad, dtype):
+    dt, u, sub = TYPES[dtype]
+    sim, X, rng = make_sim(hx, n, 4, seed=V + T)
+    z = rows(rng, (n, T, V), dt, pad, 3.0)
+    labels = rng.integers(0, V, size=(n, T))
+    labels[rng.random((n, T)) < 0.2] = -100
+    lab_d = torch.as_tensor(labels, dtype=torch.int32).cuda()
+    scale = 64.0
+    hz = host(z)
+    loss, dz = orc.token_loss(hz, labels, scale)
+    tol_loss, tol_dz = loss_bounds(hz, labels, dz, scale, u, sub) if T else (0.0, 0.0)
+    got_loss, got_dz = sim.token_loss(z, lab_d, grad_scale=scale)
+    close(got_loss, loss, tol_loss, "loss")
+    close(got_dz, dz, tol_dz, "gradient")
+    alone, none = sim.token_loss(z, lab_d, grad=False)
+    assert none is None
+    close(alone, loss, tol_loss, "loss without a gradient")
+    again_loss, again_dz = sim.token_loss(z, lab_d, grad_scale=scale)
+    assert torch.equal(got_loss, again_loss) and torch.equal(got_dz, again_dz), "a second run gives other bits"
+    place = z.clone() if pad == 0 else z
+    in_place_loss, same = sim.token_loss(place, lab_d, grad=place, grad_scale=scale)
+    assert same is place and torch.equal(place, got_dz) and torch.equal(in_place_loss, got_loss)
+    sim.close()
+
+
+@pytest.mark.parametrize("V", [5, 300, 3000, 20000, 70000])
+def test_token_loss_of_masked_and_broken_logits(hx, V):
+    n, T = 5, 6
+    sim, X, rng = make_sim(hx, n, 4, seed=V)
+    z = rng.normal(size=(n, T, V)).astype(np.float32)
+    labels = rng.integers(1, V - 1, size=(n, T))
+    z[0, 0, 1:] = -np.inf                                        # one class left: the label's logit is gone, loss = inf
+    z[0, 1] = -np.inf
+    z[0, 1, labels[0, 1]] = 2.0                                  # one class left and it is the label: loss 0
+    z[1, 2] = -np.inf                                            # nothing left
+    z[2, 3, 0] = np.nan
+    z[3, 1, V - 1] = np.inf
+    z[4, 0] = np.finfo(np.float32).min                           # all at the type's lowest value: uniform
+    z[4, 1, :-1] = np.finfo(np.float32).min
+    z[4, 2] += 3e5                                               # far from 0: no digits of the loss are lost
+    labels[1, 0] = -1
+    labels[4, 5] = -1
+    z[4, 5] = np.nan                                             # not counted: whatever is there
+    z_d, lab_d = torch.as_tensor(z).cuda(), torch.as_tensor(labels, dtype=torch.int32).cuda()
+    loss, dz = orc.token_loss(z, labels)
+    loss[3] = np.nan                                             # exp(inf - inf)
+    dz[3, 1] = np.nan
+    tol_loss, tol_dz = loss_bounds(z.astype(np.float64), labels, dz, 1.0, E32, 0.0)
+    got_loss, got_dz = sim.token_loss(z_d, lab_d)
+    close(got_loss, loss, tol_loss, "loss")
+    close(got_dz, dz, tol_dz, "gradient")
+    labels[2, 0] = V                                             # no address
+    labels[0, 0] = 2 ** 31 - 1
+    got_loss, got_dz = sim.token_loss(z_d, torch.as_tensor(labels, dtype=torch.int32).cuda())
+    assert np.isnan(host(got_loss)[[0, 2]]).all() and np.isnan(host(got_dz)[2, 0]).all() and np.isnan(host(got_dz)[0, 0]).all()
+    assert np.isfinite(host(got_dz)[0, 1]).all()
+    sim.close()
+
+
+def test_token_loss_gradient_along_a_direction(hx):
+    n, T, V = 2, 5, 60
+    sim, X, rng = make_sim(hx, n, 4, seed=9)
+    z, step = rng.normal(size=(n, T, V)), rng.normal(size=(n, T, V))
+    labels = torch.as_tensor(rng.integers(-1, V, size=(n, T)), dtype=torch.int32).cuda()
+    at = lambda h: host(sim.token_loss(torch.as_tensor(z + h * step, dtype=torch.float32).cuda(), labels, grad=False)[0])
+    slope = (at(2.0 ** -6) - at(-2.0 ** -6)) * 2.0 ** 5
+    _, dz = sim.token_loss(torch.as_tensor(z, dtype=torch.float32).cuda(), labels)
+    inner, size = (host(dz) * step).sum(axis=(1, 2)), np.abs(host(dz) * step).sum(axis=(1, 2))
+    assert (np.abs(slope - inner) <= 2.0 ** -10 * size + 1e-5).all()
+    sim.close()
+
+
+def _all_operators(sim, tokens, labels, x, head):
+    """One pass through every operator, as a small model would chain them (head: what stands between norm and logits)."""
+    V, D = 50, 24
+    e = sim.embed(tokens, 0, V, D, scale=2.0)
+    y, u, stats = sim.layer_norm(e, V * D, V * D + D, residual=x, p=0.2, seed=3)
+    z = sim.dropout(y, 0.1, seed=3, layer=1)
+    loss, dz = sim.token_loss(z, labels)
+    dy = sim.dropout(dz, 0.1, seed=3, layer=1)
+    du, dx = sim.layer_norm_grad(dy, u, stats, V * D, V * D + D, p=0.2, seed=3)
+    sim.embed_grad(tokens, dx, 0, V, scale=2.0)
+    return loss, du
+
+
+def _chain_inputs(rng, n, T):
+    tokens = torch.as_tensor(rng.integers(-1, 50, size=(n, T)), dtype=torch.int32).cuda()
+    labels = torch.as_tensor(rng.integers(-1, 24, size=(n, T)), dtype=torch.int32).cuda()
+    return tokens, labels, rows(rng, (n, T, 24), torch.float32)
+
+
+def test_other_streams_and_growing_scratch(hx):
+    n = 4
+    main, X, rng = make_sim(hx, n, 50 * 24 + 48, seed=11)
+    side = torch.cuda.Stream()
+    other, _, _ = make_sim(hx, n, 50 * 24 + 48, seed=11, stream=side)
+    for T in (3, 700, 5000, 20):
+        tokens, labels, x = _chain_inputs(rng, n, T)
+        want = [t.clone() for t in _all_operators(main, tokens, labels, x, None)] + [main.G.clone()]
+        side.wait_stream(torch.cuda.current_stream())
+        got = _all_operators(other, tokens, labels, x, None)       # called from the main stream, runs on the side stream
+        torch.cuda.current_stream().wait_stream(side)
+        for w, g in zip(want, [*got, other.G]):
+            assert torch.equal(w, g)
+    main.close()
+    other.close()
+
+
+def test_captured_into_a_graph(hx):
+    n, T = 4, 300
+    side = torch.cuda.Stream()
+    sim, X, rng = make_sim(hx, n, 50 * 24 + 48, seed=12, stream=side)
+    tokens, labels, x = _chain_inputs(rng, n, T)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        _all_operators(sim, tokens, labels, x, None)               # scratch grows here, not in the capture
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = _all_operators(sim, tokens, labels, x, None)
+        for turn in range(4):
+            x.copy_(torch.randn_like(x))
+            tokens.copy_(torch.randint(-1, 50, tokens.shape, device="cuda", dtype=torch.int32))
+            graph.replay()
+            side.synchronize()
+            replayed = [t.clone() for t in (*got, sim.G)]
+            eager = [*_all_operators(sim, tokens, labels, x, None), sim.G]
+            side.synchronize()
+            for r, e in zip(replayed, eager):
+                assert torch.equal(r, e), f"replay {turn}"
+    sim.close()
+
+
+def test_refusals(hx):
+    from paper_2105_09080_amd import binding as B
+    n, V, D, T = 2, 6, 8, 3
+    sim, X, rng = make_sim(hx, n, V * D + 2 * D, seed=0)
+    tok = torch.zeros((n, T), dtype=torch.int32, device="cuda")
+    a, b, c = (torch.zeros((n, T, D), device="cuda") for _ in range(3))
+    st, loss = torch.zeros((n, T, 2), device="cuda"), torch.zeros(n, device="cuda")
+    goff = V * D
+    sim.G.fill_(7.0)
+
+    def no(call, *args, status=B.GPGA_EINVAL, says=""):
+        with pytest.raises(B.GpgaError) as e:
+            call(sim.ctx, *args)
+        assert e.value.status == status and says in str(e.value), str(e.value)
+
+    embed = lambda **k: [k.get("tok", tok), k.get("T", T), k.get("off", 0), k.get("V", V), k.get("D", D), k.get("scale", 1.0), k.get("y", a),
+                         k.get("ld", D), k.get("dtype", 0)]
+    for kw, says in ((dict(T=-1), "T ="), (dict(off=-1), "table"), (dict(off=2 * D + 1), "table"), (dict(V=0), "V ="), (dict(D=0), "D ="),
+                     (dict(V=2 ** 31 - 1), "V ="), (dict(V=2 ** 20, D=2 ** 20, ld=2 ** 20), "table"), (dict(scale=float("nan")), "scale"),
+                     (dict(y=None), "NULL"), (dict(tok=None), "NULL"), (dict(ld=D - 1), "ld ="), (dict(dtype=3), "dtype"),
+                     (dict(y=a.data_ptr() + 2), "aligned"), (dict(tok=tok.data_ptr() + 2), "aligned"), (dict(y=sim.X.data_ptr()), "bound array"),
+                     (dict(y=sim.g.data_ptr()), "bound array"), (dict(T=2 ** 30, ld=2 ** 50), "rows")):
+        no(B.gpga_embed, *embed(**kw), says=says)
+    no(B.gpga_embed_grad, tok, T, 0, V, D, 1.0, None, D, 0, False, says="NULL")
+    no(B.gpga_embed_grad, tok, T, 0, V, D, float("inf"), a, D, 0, False, says="scale")
+    assert B.raw_status("gpga_embed_grad", sim.ctx, tok.data_ptr(), T, 0, V, D, 1.0, a.data_ptr(), D, 0, 2) == B.GPGA_EINVAL
+    for p, says in ((-0.1, "p ="), (1.0, "p ="), (float("nan"), "p ="), (1 - 2.0 ** -18, "nothing")):
+        no(B.gpga_dropout, a, None, T, D, D, 0, p, 1, 0, b, says=says)
+    no(B.gpga_dropout, a, None, T, D, D, 0, 0.1, 1, 1 << 24, b, says="layer")
+    no(B.gpga_dropout, a, None, T, D, D, 0, 0.1, 1, -1, b, says="layer")
+    no(B.gpga_dropout, a, b, T, D, D, 0, 0.1, 1, 0, b.data_ptr() + 4, says="overlap")
+    no(B.gpga_dropout, a, None, 2 ** 29, D * 16, D * 16, 0, 0.1, 1, 0, b, says="2^32")
+    norm = lambda **k: [k.get("x", a), None, T, D, D, 0, 0.0, 1, 0, k.get("g", goff), k.get("b", goff + D), k.get("eps", 1e-5), k.get("u", None),
+                        k.get("y", b), st]
+    for kw, says in ((dict(g=-1), "gamma"), (dict(b=goff + D + 1), "beta"), (dict(eps=-1.0), "eps"), (dict(y=None), "NULL"), (dict(x=None), "NULL"),
+                     (dict(u=b), "overlap")):
+        no(B.gpga_layer_norm, *norm(**kw), says=says)
+    grad = lambda **k: [k.get("dy", a), b, k.get("st", st), None, T, D, D, 0, k.get("p", 0.0), 1, 0, goff, k.get("b", goff + D), k.get("du", c),
+                        k.get("dx", None), False]
+    for kw, says in ((dict(st=None), "NULL"), (dict(du=None), "NULL"), (dict(p=0.5), "dx_dev"), (dict(dx=a.data_ptr() + 4), "overlap"),
+                     (dict(b=goff + 1), "overlap"), (dict(dx=torch.zeros_like(a)), "dx_dev")):
+        no(B.gpga_layer_norm_grad, *grad(**kw), says=says)
+    no(B.gpga_token_loss, None, tok, T, D, D, 0, 1.0, loss, None, says="NULL")
+    no(B.gpga_token_loss, a, None, T, D, D, 0, 1.0, loss, None, says="NULL")
+    no(B.gpga_token_loss, a, tok, T, D, D, 0, 1.0, None, None, says="loss_dev")
+    no(B.gpga_token_loss, a, tok, T, D, D, 0, float("inf"), loss, None, says="grad_scale")
+    no(B.gpga_token_loss, a, tok, T, 0, D, 0, 1.0, loss, None, says="row")
+    assert (host(sim.G) == 7.0).all()
+    # columns of one wider array do not overlap
+    wide = torch.zeros((n, T, 2 * D), device="cuda")
+    B.gpga_dropout(sim.ctx, wide[..., :D], None, T, D, 2 * D, 0, 0.5, 1, 0, wide[..., D:])
+    unbound = B.gpga_create(n, V * D, "ring", 0, 0.1, 0.0)
+    assert B.raw_status("gpga_embed", unbound, tok.data_ptr(), T, 0, V, D, 1.0, a.data_ptr(), D, 0) == B.GPGA_ESTATE
+    B.gpga_destroy(unbound)
+    for bad in (tok.long(), tok[:1], tok.t()):
+        with pytest.raises(ValueError):
+            sim.embed(bad, 0, V, D)
+    for x in (a[:1], a.double(), a.transpose(1, 2), a[:, :1].expand(n, T, D)):
+        with pytest.raises(ValueError):
+            sim.dropout(x, 0.5, seed=0)
+    with pytest.raises(ValueError):
+        sim.dropout(a, 0.5, seed=0, residual=b.half())
+    sim.close()
+
+
+def test_operators_leave_the_iteration_as_it_was(hx):
+    """k, X and the columns of G that are no operator's stay; a step afterwards takes the gradients that were written."""
+    n, V, D, T = 4, 10, 8, 20
+    sim, X, rng = make_sim(hx, n, V * D + 5, seed=21)
+    sim.G.fill_(1.0)
+    tok = torch.as_tensor(rng.integers(0, V, size=(n, T)), dtype=torch.int32).cuda()
+    sim.embed_grad(tok, rows(rng, (n, T, D), torch.float32), 0, V)
+    assert sim.k == 0 and np.array_equal(host(sim.X), X.astype(np.float64)) and (host(sim.G)[:, V * D:] == 1).all()
+    g = host(sim.G)
+    sim.step()
+    half = X - np.float32(0.1) * g
+    want = (half + np.roll(half, 1, axis=0) + np.roll(half, -1, axis=0)) / 3
+    assert sim.k == 1 and np.abs(host(sim.X) - want).max() < 1e-5 * np.abs(want).max()
+    sim.close()
