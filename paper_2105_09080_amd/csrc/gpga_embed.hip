@@ -190,38 +190,172 @@ __global__ __launch_bounds__(kThreads) void k_merge(const uint32_t* __restrict__
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------------------------
-// A wavefront takes rows of the table in turn: the items of a row lie side by side in the sorted order, and their rows of dy
-// are added in the order of their positions.
+// The items of a row of the table lie side by side in the sorted order, and their rows of dy are added in that order, which is
+// the order of their positions.  A wavefront adds up to kRun items.  Longer rows (frequent tokens) are cut where the sorted
+// order reaches a multiple of kRun: a wavefront for each such chunk leaves the sum of its part in `partial`, and
+// k_embed_join adds the parts.  A chunk holds parts of at most two long rows, one that reaches its first item (slot 0) and
+// one that reaches its last (slot 1, unless it is the same).
+constexpr int kRun = 32;
+constexpr int kTurns = 4;               // column turns kept in registers at once
+constexpr int kTurnCols = kWave * 4;    // four columns a lane: an fp32 store of a wavefront is 1 KiB without gaps
+
+struct GradArgs {
+    const uint32_t* keys;   // sorted, T a node
+    const int32_t* pos;
+    const int32_t* start;   // V + 1 a node
+    int32_t T, V, D;
+    int64_t ld, ldg;
+    float scale;
+    int32_t accumulate;
+    uint32_t chunks;            // of a node
+    uint32_t chunk_blocks;      // workgroups of a node that take chunks; the others take rows
+    uint32_t blocks_per_node;
+    uint32_t rows_per_wave;     // 1 .. 64
+    float* partial;             // n x chunks x 2 x D
+    float* g;                   // the table's columns of node 0
+};
+
+// sum[k] = sum of columns (first_turn + k) * kTurnCols + 4 * lane .. + 3 over `count` <= 64 rows of dy; lane e holds the position of row e.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void k_embed_grad(const uint32_t* __restrict__ keys, const int32_t* __restrict__ pos,
-                                                         const int32_t* __restrict__ start, int32_t T, int32_t V, int32_t D,
-                                                         const typename E::mem* __restrict__ dy, int64_t ld, float scale, bool accumulate,
-                                                         uint32_t rows_per_block, uint32_t blocks_per_node, float* __restrict__ g, int64_t ldg) {
-    const uint32_t node = blockIdx.x / blocks_per_node, b = blockIdx.x - node * blocks_per_node;
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const bool bad = T > 0 && keys[(int64_t)node * T + T - 1] == (uint32_t)V + 1u;
-    const int32_t* at = pos + (int64_t)node * T;
-    const int32_t* begin = start + (int64_t)node * (V + 1ll);
-    const typename E::mem* rows = dy + (int64_t)node * T * ld;
-    const int64_t last = ((int64_t)b + 1) * rows_per_block < V ? ((int64_t)b + 1) * rows_per_block : V;
-    for (int64_t v = (int64_t)b * rows_per_block + wave; v < last; v += kThreads / kWave) {
-        const int32_t from = begin[v], to = begin[v + 1];
-        if (accumulate && from == to && !bad) continue;
-        float* out = g + (int64_t)node * ldg + v * D;
-        for (int32_t c = lane * kOct; c < D; c += kWave * kOct) {
-            float sum[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            for (int32_t e = from; e < to; ++e) {
-                float v8[kOct];
-                row_load<E>(rows + (int64_t)at[e] * ld, c, D, v8);
+__device__ __forceinline__ void sum_rows(const typename E::mem* __restrict__ rows, int64_t ld, int32_t D, int32_t at, int32_t count, int32_t c0,
+                                         float (*sum)[4]) {
 #pragma unroll
-                for (int j = 0; j < kOct; ++j) sum[j] += v8[j];
-            }
-            float had[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (accumulate) row_load<ElemF32>(out, c, D, had);
+    for (int k = 0; k < kTurns; ++k)
 #pragma unroll
-            for (int j = 0; j < kOct; ++j) sum[j] = bad ? __builtin_nanf("") : had[j] + scale * sum[j];
-            row_store<ElemF32>(out, c, D, sum);
+        for (int j = 0; j < 4; ++j) sum[k][j] = 0.f;
+    constexpr int kAhead = 4;  // rows whose loads are under way together
+    int32_t e = 0;
+    for (; e + kAhead <= count; e += kAhead) {
+        float v[kAhead][kTurns][4];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const typename E::mem* row = rows + (int64_t)__builtin_amdgcn_readlane(at, e + i) * ld;
+#pragma unroll
+            for (int k = 0; k < kTurns; ++k)
+                if (c0 + k * kTurnCols < D) row_load4<E>(row, c0 + k * kTurnCols, D, v[i][k]);
         }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int k = 0; k < kTurns; ++k)
+                if (c0 + k * kTurnCols < D)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum[k][j] += v[i][k][j];
+    }
+    for (; e < count; ++e) {
+        const typename E::mem* row = rows + (int64_t)__builtin_amdgcn_readlane(at, e) * ld;
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k)
+            if (c0 + k * kTurnCols < D) {
+                float v[4];
+                row_load4<E>(row, c0 + k * kTurnCols, D, v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[k][j] += v[j];
+            }
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_embed_grad(GradArgs a, const typename E::mem* __restrict__ dy) {
+    const uint32_t node = blockIdx.x / a.blocks_per_node, b = blockIdx.x - node * a.blocks_per_node;
+    const int lane = threadIdx.x & (kWave - 1);
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t* keys = a.keys + (int64_t)node * a.T;
+    const int32_t* pos = a.pos + (int64_t)node * a.T;
+    const int32_t* start = a.start + (int64_t)node * (a.V + 1ll);
+    const typename E::mem* rows = dy + (int64_t)node * a.T * a.ld;
+    float sum[kTurns][4];
+    if (b < a.chunk_blocks) {
+        const uint32_t chunk = b * (kThreads / kWave) + wave;
+        if (chunk >= a.chunks) return;
+        const int32_t first = (int32_t)chunk * kRun, end = a.T - first < kRun ? a.T : first + kRun;
+        const uint32_t head = keys[first], tail = keys[end - 1];
+        float* part = a.partial + ((int64_t)node * a.chunks + chunk) * 2 * a.D;
+        for (int slot = 0; slot < 2; ++slot) {
+            const uint32_t key = slot ? tail : head;
+            if (key >= (uint32_t)a.V || (slot && tail == head)) continue;
+            const int32_t row_from = start[key], row_to = start[key + 1];
+            if (row_to - row_from <= kRun) continue;
+            const int32_t from = slot ? row_from : first, to = row_to < end ? row_to : end;
+            const int32_t at = pos[from + (lane < to - from ? lane : 0)];
+            for (int32_t c0 = lane * 4; c0 - lane * 4 < a.D; c0 += kTurns * kTurnCols) {
+                sum_rows<E>(rows, a.ld, a.D, at, to - from, c0, sum);
+#pragma unroll
+                for (int k = 0; k < kTurns; ++k)
+                    if (c0 + k * kTurnCols < a.D) row_store4<ElemF32>(part + (int64_t)slot * a.D, c0 + k * kTurnCols, a.D, sum[k]);
+            }
+        }
+        return;
+    }
+    const bool bad = a.T > 0 && keys[a.T - 1] == (uint32_t)a.V + 1u;
+    const int64_t v0 = ((int64_t)(b - a.chunk_blocks) * (kThreads / kWave) + wave) * a.rows_per_wave;
+    const int32_t mine = a.V - v0 < (int64_t)a.rows_per_wave ? (int32_t)(a.V - v0) : (int32_t)a.rows_per_wave;
+    if (mine <= 0) return;
+    const int32_t begin = start[v0 + (lane < mine ? lane : mine)], next = start[v0 + (lane < mine ? lane + 1 : mine)];
+    uint64_t todo = __ballot(lane < mine && (bad || (next - begin <= kRun && (next > begin || !a.accumulate))));
+    while (todo) {
+        const int r = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        const int32_t from = __builtin_amdgcn_readlane(begin, r), count = bad ? 0 : __builtin_amdgcn_readlane(next, r) - from;
+        float* out = a.g + (int64_t)node * a.ldg + (v0 + r) * a.D;
+        const int32_t at = count ? pos[from + (lane < count ? lane : 0)] : 0;
+        for (int32_t c0 = lane * 4; c0 - lane * 4 < a.D; c0 += kTurns * kTurnCols) {
+            sum_rows<E>(rows, a.ld, a.D, at, count, c0, sum);
+#pragma unroll
+            for (int k = 0; k < kTurns; ++k) {
+                const int32_t c = c0 + k * kTurnCols;
+                if (c >= a.D) break;
+                float had[4] = {0.f, 0.f, 0.f, 0.f};
+                if (a.accumulate) row_load4<ElemF32>(out, c, a.D, had);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[k][j] = bad ? __builtin_nanf("") : had[j] + a.scale * sum[k][j];
+                row_store4<ElemF32>(out, c, a.D, sum[k]);
+            }
+        }
+    }
+}
+
+// Adds the parts of each long row, kTurnCols columns a workgroup: the one whose chunk holds the row's first item.  Its wavefronts
+// take contiguous shares of the parts; everything in a fixed order.
+__global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a, uint32_t column_blocks) {
+    constexpr int kWaves = kThreads / kWave;
+    __shared__ float s_part[kWaves][kTurnCols];
+    const uint32_t unit = blockIdx.x / column_blocks, node = unit / a.chunks, chunk = unit - node * a.chunks;
+    const uint32_t* keys = a.keys + (int64_t)node * a.T;
+    const int32_t* start = a.start + (int64_t)node * (a.V + 1ll);
+    const int32_t first = (int32_t)chunk * kRun, end = a.T - first < kRun ? a.T : first + kRun;
+    const uint32_t key = keys[end - 1];
+    if (key >= (uint32_t)a.V || keys[a.T - 1] == (uint32_t)a.V + 1u) return;
+    const int32_t row_from = start[key], row_to = start[key + 1];
+    if (row_from < first || row_to - row_from <= kRun) return;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int32_t c = (int32_t)(blockIdx.x - unit * column_blocks) * kTurnCols + lane * 4;
+    const uint32_t parts = (uint32_t)(row_to - 1) / kRun - chunk + 1, share = (parts + kWaves - 1) / kWaves;
+    const uint32_t from = wave * share, to = from + share < parts ? from + share : parts;
+    const float* part = a.partial + ((int64_t)node * a.chunks + chunk) * 2 * a.D;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c < a.D) {
+#pragma unroll 4
+        for (uint32_t p = from; p < to; ++p) {
+            float v[4];
+            row_load4<ElemF32>(part + ((int64_t)p * 2 + (p == 0 && row_from > first ? 1 : 0)) * a.D, c, a.D, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] += v[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s_part[wave][j * kWave + lane] = sum[j];
+    __syncthreads();
+    if (wave == 0 && c < a.D) {
+        float* out = a.g + (int64_t)node * a.ldg + (int64_t)key * a.D;
+        float had[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.accumulate) row_load4<ElemF32>(out, c, a.D, had);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            for (int w = 1; w < kWaves; ++w) sum[j] += s_part[w][j * kWave + lane];
+            sum[j] = had[j] + a.scale * sum[j];
+        }
+        row_store4<ElemF32>(out, c, a.D, sum);
     }
 }
 
@@ -229,10 +363,10 @@ uint32_t blocks_for(int64_t items, int64_t per_block) { return (uint32_t)((items
 
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
-// Scratch of the gradient: sorted keys and positions (of the tiles, and merged where there are several), row starts.
+// Scratch of the gradient: sorted keys and positions (of the tiles, and merged where there are several), row starts, parts of long rows.
 struct GradSpace {
-    size_t items, tile_keys, tile_pos, keys, pos, start, bytes;
-    uint32_t tiles;
+    size_t items, tile_keys, tile_pos, keys, pos, start, partial, bytes;
+    uint32_t tiles, chunks;
     GradSpace(const RowsShape& s, int32_t V) {
         items = (size_t)s.n * (size_t)s.T;
         tiles = s.T > 0 ? blocks_for(s.T, kTile) : 0;
@@ -242,7 +376,9 @@ struct GradSpace {
         keys = tiles > 1 ? 2 * one : tile_keys;
         pos = tiles > 1 ? 3 * one : tile_pos;
         start = (tiles > 1 ? 4 : 2) * one;
-        bytes = start + padded((size_t)s.n * ((size_t)V + 1) * 4);
+        partial = start + padded((size_t)s.n * ((size_t)V + 1) * 4);
+        chunks = s.T > kRun ? blocks_for(s.T, kRun) : 0;  // no row is long otherwise
+        bytes = partial + padded((size_t)s.n * chunks * 2 * (size_t)s.D * 4);
     }
 };
 
@@ -293,12 +429,31 @@ hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_
                                                                                    ints(space.start));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const uint32_t rows_per_block = 16, per_node = blocks_for(V, rows_per_block);
-    return with_elem(s.dtype, [&](auto el) {
+    GradArgs a = {};
+    a.keys = words(space.keys);
+    a.pos = ints(space.pos);
+    a.start = ints(space.start);
+    a.T = s.T;
+    a.V = V;
+    a.D = s.D;
+    a.ld = s.ld;
+    a.ldg = c->ld;
+    a.scale = scale;
+    a.accumulate = accumulate;
+    a.chunks = space.chunks;
+    a.chunk_blocks = blocks_for(a.chunks, kThreads / kWave);
+    const int64_t spread = (int64_t)s.n * V / 16384;
+    a.rows_per_wave = (uint32_t)(spread < 1 ? 1 : spread < 4 ? spread : 4);
+    a.blocks_per_node = a.chunk_blocks + blocks_for(V, (int64_t)a.rows_per_wave * (kThreads / kWave));
+    a.partial = reinterpret_cast<float*>(base + space.partial);
+    a.g = c->g + table_off;
+    hipError_t e2 = with_elem(s.dtype, [&](auto el) {
         typedef decltype(el) E;
-        k_embed_grad<E><<<dim3(per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(words(space.keys), ints(space.pos), ints(space.start), s.T, V, s.D,
-                                                                                         static_cast<const typename E::mem*>(dy), s.ld, scale, accumulate,
-                                                                                         rows_per_block, per_node, c->g + table_off, c->ld);
+        k_embed_grad<E><<<dim3(a.blocks_per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, static_cast<const typename E::mem*>(dy));
         return hipGetLastError();
     });
+    if (e2 != hipSuccess || !a.chunks) return e2;
+    const uint32_t column_blocks = blocks_for(s.D, kTurnCols);
+    k_embed_join<<<dim3(a.chunks * column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, column_blocks);
+    return hipGetLastError();
 }

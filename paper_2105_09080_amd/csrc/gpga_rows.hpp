@@ -30,6 +30,17 @@ struct ElemF32 {
             v[4 + j] = b[j];
         }
     }
+    static __device__ __forceinline__ void load4(const mem* p, float* v) {
+        const vec a = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = a[j];
+    }
+    static __device__ __forceinline__ void store4(mem* p, const float* v) {
+        vec a;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = v[j];
+        *reinterpret_cast<vec*>(p) = a;
+    }
     static __device__ __forceinline__ void store8(mem* p, const float* v) {
         vec a, b;
 #pragma unroll
@@ -47,12 +58,18 @@ struct Elem16 {
     typedef M mem;
     typedef M vec __attribute__((ext_vector_type(8), aligned(2)));
     typedef float wide __attribute__((ext_vector_type(8)));
+    typedef M vec4 __attribute__((ext_vector_type(4), aligned(2)));
     static __device__ __forceinline__ float get(mem v) { return (float)v; }
     static __device__ __forceinline__ mem put(float v) { return (mem)v; }  // to nearest, ties to even
     static __device__ __forceinline__ void load8(const mem* p, float* v) {
         const wide w = __builtin_convertvector(*reinterpret_cast<const vec*>(p), wide);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = w[j];
+    }
+    static __device__ __forceinline__ void load4(const mem* p, float* v) {
+        const v4f w = __builtin_convertvector(*reinterpret_cast<const vec4*>(p), v4f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = w[j];
     }
     static __device__ __forceinline__ void store8(mem* p, const float* v) {
         wide w;
@@ -81,6 +98,27 @@ __device__ __forceinline__ void row_store(typename E::mem* row, int32_t c, int32
     } else {
 #pragma unroll
         for (int j = 0; j < kOct; ++j)
+            if (c + j < D) row[c + j] = E::put(v[j]);
+    }
+}
+
+// Columns c .. c+3 in the same way.
+template <typename E>
+__device__ __forceinline__ void row_load4(const typename E::mem* row, int32_t c, int32_t D, float* v) {
+    if (c + 4 <= D) {
+        E::load4(row + c, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = c + j < D ? E::get(row[c + j]) : 0.f;
+    }
+}
+template <typename E>
+__device__ __forceinline__ void row_store4(typename E::mem* row, int32_t c, int32_t D, const float* v) {
+    if (c + 4 <= D) {
+        E::store4(row + c, v);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
             if (c + j < D) row[c + j] = E::put(v[j]);
     }
 }
