@@ -45,15 +45,43 @@ __global__ __launch_bounds__(kThreads) void k_embed(const int32_t* __restrict__ 
 // ---- sorting the tokens of a node ---------------------------------------------------------------------------------------
 // A workgroup sorts a tile of kTile (token, position) pairs in LDS, least significant digit first and stable, so equal
 // tokens stay in the order of their positions; k_merge puts the tiles of a node together.  Keys: the token, V for padding,
-// V + 1 for a token that is out of range.
+// V + 1 for a token that is out of range.  The workgroups behind those zero the table's columns of g, which takes longer than
+// the sort and waits for nothing.
 constexpr int kSortThreads = 1024;
 constexpr int kSortItems = 4;
 constexpr int kTile = kSortThreads * kSortItems;
 constexpr int kSortWaves = kSortThreads / kWave;
 constexpr int kDigits = 256;
 
+struct ZeroArgs {
+    uint32_t first_block;   // workgroups from here on zero
+    uint32_t per_node;
+    int64_t count, ldg;     // floats of a node's block, distance of the blocks
+    float* g;
+};
+constexpr int kZeroUnits = 4;  // pieces of four floats a lane
+constexpr int kZeroCols = kZeroUnits * kSortThreads * 4;
+
+__device__ __forceinline__ void zero_block(const ZeroArgs& z, uint32_t b) {
+    const uint32_t node = b / z.per_node;
+    const int64_t base = (int64_t)(b - node * z.per_node) * kZeroCols;
+    float* g = z.g + (int64_t)node * z.ldg;
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < kZeroUnits; ++u) {
+        const int64_t e = base + (int64_t)(u * kSortThreads + threadIdx.x) * 4;
+        if (e + 4 <= z.count) ElemF32::store4(g + e, zero);
+        else
+            for (int64_t k = e; k < z.count; ++k) g[k] = 0.f;
+    }
+}
+
 __global__ __launch_bounds__(kSortThreads) void k_sort_tile(const int32_t* __restrict__ tokens, int32_t T, int32_t V, uint32_t tiles, int bits,
-                                                            uint32_t* __restrict__ keys, int32_t* __restrict__ pos) {
+                                                            uint32_t* __restrict__ keys, int32_t* __restrict__ pos, ZeroArgs zero) {
+    if (blockIdx.x >= zero.first_block) {
+        zero_block(zero, blockIdx.x - zero.first_block);
+        return;
+    }
     __shared__ uint32_t s_key[kTile];
     __shared__ uint16_t s_pos[kTile];
     __shared__ uint32_t s_count[kSortWaves][kDigits];
@@ -157,180 +185,136 @@ __device__ __forceinline__ int32_t keys_below(const uint32_t* __restrict__ keys,
     return lo;
 }
 
-// Merges the sorted tiles of every node by rank (an item's place is its place in its tile plus the items of the other tiles
-// that come before it) and finds where each row of the table begins in the sorted order: start[v] = items with a key
-// below v, v = 0 .. V.  The first `merge_blocks` workgroups of a node merge, the others find.
-__global__ __launch_bounds__(kThreads) void k_merge(const uint32_t* __restrict__ tile_keys, const int32_t* __restrict__ tile_pos, int32_t T, int32_t V,
-                                                    uint32_t tiles, uint32_t merge_blocks, uint32_t blocks_per_node, uint32_t* __restrict__ keys,
-                                                    int32_t* __restrict__ pos, int32_t* __restrict__ start) {
-    const uint32_t node = blockIdx.x / blocks_per_node, b = blockIdx.x - node * blocks_per_node;
+// Merges the sorted tiles of every node by rank: an item's place is its place in its tile plus the items of the other tiles
+// that come before it.
+__global__ __launch_bounds__(kThreads) void k_merge(const uint32_t* __restrict__ tile_keys, const int32_t* __restrict__ tile_pos, int32_t T, uint32_t tiles,
+                                                    uint32_t blocks_per_node, uint32_t* __restrict__ keys, int32_t* __restrict__ pos) {
+    const uint32_t node = blockIdx.x / blocks_per_node;
+    const int32_t e = (int32_t)((blockIdx.x - node * blocks_per_node) * kThreads + threadIdx.x);
+    if (e >= T) return;
     const uint32_t* mine = tile_keys + (int64_t)node * T;
-    if (b < merge_blocks) {
-        const int32_t e = (int32_t)(b * kThreads + threadIdx.x);
-        if (e >= T) return;
-        const uint32_t own = (uint32_t)e / kTile, key = mine[e];
-        int32_t to = e - (int32_t)own * kTile;
-        for (uint32_t k = 0; k < tiles; ++k) {
-            if (k == own) continue;
-            const int32_t base = (int32_t)k * kTile, count = T - base < kTile ? T - base : kTile;
-            to += keys_below(mine + base, count, k < own ? key + 1u : key);  // equal tokens of earlier tiles come first
-        }
-        keys[(int64_t)node * T + to] = key;
-        pos[(int64_t)node * T + to] = tile_pos[(int64_t)node * T + e];
-    } else {
-        const uint32_t v = (b - merge_blocks) * kThreads + threadIdx.x;
-        if (v > (uint32_t)V) return;
-        int32_t below = 0;
-        for (uint32_t k = 0; k < tiles; ++k) {
-            const int32_t base = (int32_t)k * kTile, count = T - base < kTile ? T - base : kTile;
-            below += keys_below(mine + base, count, v);
-        }
-        start[(int64_t)node * (V + 1ll) + v] = below;
+    const uint32_t own = (uint32_t)e / kTile, key = mine[e];
+    int32_t to = e - (int32_t)own * kTile;
+    for (uint32_t k = 0; k < tiles; ++k) {
+        if (k == own) continue;
+        const int32_t base = (int32_t)k * kTile, count = T - base < kTile ? T - base : kTile;
+        to += keys_below(mine + base, count, k < own ? key + 1u : key);  // equal tokens of earlier tiles come first
     }
+    keys[(int64_t)node * T + to] = key;
+    pos[(int64_t)node * T + to] = tile_pos[(int64_t)node * T + e];
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------------------------
 // The items of a row of the table lie side by side in the sorted order, and their rows of dy are added in that order, which is
-// the order of their positions.  A wavefront adds up to kRun items.  Longer rows (frequent tokens) are cut where the sorted
-// order reaches a multiple of kRun: a wavefront for each such chunk leaves the sum of its part in `partial`, and
-// k_embed_join adds the parts.  A chunk holds parts of at most two long rows, one that reaches its first item (slot 0) and
-// one that reaches its last (slot 1, unless it is the same).
+// the order of their positions.  A wavefront takes kTurnCols columns of kRun consecutive items, whatever rows they belong to, so frequent
+// tokens cost no more than others.  A row that lies within its items goes straight to g; of a row that reaches into other chunks
+// it leaves a part in `partial` (slot 0: the row of its first item, slot 1: the row of its last item where that is another),
+// and k_embed_join adds the parts.  Rows without items hold the zeros of the sort's launch, or what g is to be added to.
 constexpr int kRun = 32;
-constexpr int kTurns = 4;               // column turns kept in registers at once
-constexpr int kTurnCols = kWave * 4;    // four columns a lane: an fp32 store of a wavefront is 1 KiB without gaps
+constexpr int kAhead = 8;               // items whose rows are loaded together
+constexpr int kTurnCols = kWave * 4;    // columns of a wavefront, four a lane: an fp32 store is 1 KiB without gaps
 
 struct GradArgs {
     const uint32_t* keys;   // sorted, T a node
     const int32_t* pos;
-    const int32_t* start;   // V + 1 a node
+    uint32_t n;
     int32_t T, V, D;
     int64_t ld, ldg;
     float scale;
     int32_t accumulate;
     uint32_t chunks;            // of a node
-    uint32_t chunk_blocks;      // workgroups of a node that take chunks; the others take rows
-    uint32_t blocks_per_node;
-    uint32_t rows_per_wave;     // 1 .. 64
+    uint32_t column_blocks;     // of kTurnCols
     float* partial;             // n x chunks x 2 x D
     float* g;                   // the table's columns of node 0
 };
 
-// sum[k] = sum of columns (first_turn + k) * kTurnCols + 4 * lane .. + 3 over `count` <= 64 rows of dy; lane e holds the position of row e.
-template <typename E>
-__device__ __forceinline__ void sum_rows(const typename E::mem* __restrict__ rows, int64_t ld, int32_t D, int32_t at, int32_t count, int32_t c0,
-                                         float (*sum)[4]) {
+// A node with a token that is out of range: the last key in its order.
+__device__ __forceinline__ bool out_of_range(const uint32_t* keys, const GradArgs& a) { return keys[a.T - 1] == (uint32_t)a.V + 1u; }
+
+// Four columns of a row of g from their sum and what g holds.
+__device__ __forceinline__ void put_sum(const GradArgs& a, float* out, int32_t c, const float* had, const float* sum) {
+    float v[4];
 #pragma unroll
-    for (int k = 0; k < kTurns; ++k)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum[k][j] = 0.f;
-    constexpr int kAhead = 4;  // rows whose loads are under way together
-    int32_t e = 0;
-    for (; e + kAhead <= count; e += kAhead) {
-        float v[kAhead][kTurns][4];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const typename E::mem* row = rows + (int64_t)__builtin_amdgcn_readlane(at, e + i) * ld;
-#pragma unroll
-            for (int k = 0; k < kTurns; ++k)
-                if (c0 + k * kTurnCols < D) row_load4<E>(row, c0 + k * kTurnCols, D, v[i][k]);
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-            for (int k = 0; k < kTurns; ++k)
-                if (c0 + k * kTurnCols < D)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) sum[k][j] += v[i][k][j];
-    }
-    for (; e < count; ++e) {
-        const typename E::mem* row = rows + (int64_t)__builtin_amdgcn_readlane(at, e) * ld;
-#pragma unroll
-        for (int k = 0; k < kTurns; ++k)
-            if (c0 + k * kTurnCols < D) {
-                float v[4];
-                row_load4<E>(row, c0 + k * kTurnCols, D, v);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum[k][j] += v[j];
-            }
-    }
+    for (int j = 0; j < 4; ++j) v[j] = had[j] + a.scale * sum[j];
+    row_store4<ElemF32>(out, c, a.D, v);
 }
 
-template <typename E>
+template <typename E, bool kAdd>
 __global__ __launch_bounds__(kThreads) void k_embed_grad(GradArgs a, const typename E::mem* __restrict__ dy) {
-    const uint32_t node = blockIdx.x / a.blocks_per_node, b = blockIdx.x - node * a.blocks_per_node;
     const int lane = threadIdx.x & (kWave - 1);
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t wave = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t unit = wave / a.column_blocks, node = unit / a.chunks, chunk = unit - node * a.chunks;
+    if (node >= a.n) return;
     const uint32_t* keys = a.keys + (int64_t)node * a.T;
-    const int32_t* pos = a.pos + (int64_t)node * a.T;
-    const int32_t* start = a.start + (int64_t)node * (a.V + 1ll);
-    const typename E::mem* rows = dy + (int64_t)node * a.T * a.ld;
-    float sum[kTurns][4];
-    if (b < a.chunk_blocks) {
-        const uint32_t chunk = b * (kThreads / kWave) + wave;
-        if (chunk >= a.chunks) return;
-        const int32_t first = (int32_t)chunk * kRun, end = a.T - first < kRun ? a.T : first + kRun;
-        const uint32_t head = keys[first], tail = keys[end - 1];
-        float* part = a.partial + ((int64_t)node * a.chunks + chunk) * 2 * a.D;
-        for (int slot = 0; slot < 2; ++slot) {
-            const uint32_t key = slot ? tail : head;
-            if (key >= (uint32_t)a.V || (slot && tail == head)) continue;
-            const int32_t row_from = start[key], row_to = start[key + 1];
-            if (row_to - row_from <= kRun) continue;
-            const int32_t from = slot ? row_from : first, to = row_to < end ? row_to : end;
-            const int32_t at = pos[from + (lane < to - from ? lane : 0)];
-            for (int32_t c0 = lane * 4; c0 - lane * 4 < a.D; c0 += kTurns * kTurnCols) {
-                sum_rows<E>(rows, a.ld, a.D, at, to - from, c0, sum);
-#pragma unroll
-                for (int k = 0; k < kTurns; ++k)
-                    if (c0 + k * kTurnCols < a.D) row_store4<ElemF32>(part + (int64_t)slot * a.D, c0 + k * kTurnCols, a.D, sum[k]);
-            }
-        }
+    if (out_of_range(keys, a)) {  // NaN everywhere: a share of the block for each wavefront
+        const int64_t all = (int64_t)a.V * a.D, shares = (int64_t)a.chunks * a.column_blocks, share = (all + shares - 1) / shares;
+        const int64_t from = (wave - (int64_t)node * shares) * share, to = from + share < all ? from + share : all;
+        for (int64_t e = from + lane; e < to; e += kWave) a.g[(int64_t)node * a.ldg + e] = __builtin_nanf("");
         return;
     }
-    const bool bad = a.T > 0 && keys[a.T - 1] == (uint32_t)a.V + 1u;
-    const int64_t v0 = ((int64_t)(b - a.chunk_blocks) * (kThreads / kWave) + wave) * a.rows_per_wave;
-    const int32_t mine = a.V - v0 < (int64_t)a.rows_per_wave ? (int32_t)(a.V - v0) : (int32_t)a.rows_per_wave;
-    if (mine <= 0) return;
-    const int32_t begin = start[v0 + (lane < mine ? lane : mine)], next = start[v0 + (lane < mine ? lane + 1 : mine)];
-    uint64_t todo = __ballot(lane < mine && (bad || (next - begin <= kRun && (next > begin || !a.accumulate))));
-    while (todo) {
-        const int r = __builtin_ctzll(todo);
-        todo &= todo - 1;
-        const int32_t from = __builtin_amdgcn_readlane(begin, r), count = bad ? 0 : __builtin_amdgcn_readlane(next, r) - from;
-        float* out = a.g + (int64_t)node * a.ldg + (v0 + r) * a.D;
-        const int32_t at = count ? pos[from + (lane < count ? lane : 0)] : 0;
-        for (int32_t c0 = lane * 4; c0 - lane * 4 < a.D; c0 += kTurns * kTurnCols) {
-            sum_rows<E>(rows, a.ld, a.D, at, count, c0, sum);
+    const int32_t first = (int32_t)chunk * kRun, count = a.T - first < kRun ? a.T - first : kRun;
+    const uint32_t key = keys[first + (lane < count ? lane : count - 1)];
+    const int32_t at = a.pos[(int64_t)node * a.T + first + (lane < count ? lane : count - 1)];
+    const uint32_t before = chunk ? keys[first - 1] : 0xffffffffu, after = first + count < a.T ? keys[first + count] : 0xffffffffu;
+    const uint32_t down = __shfl_down(key, 1, kWave);
+    // items that are the last of their row here, and those of padding, which is behind all rows
+    const uint64_t last = __ballot(lane < count && (lane == count - 1 || key != down)), padding = __ballot(lane < count && key >= (uint32_t)a.V);
+    const int real = padding ? __builtin_ctzll(padding) : count;
+    const int32_t c = (int32_t)(wave - unit * a.column_blocks) * kTurnCols + lane * 4;
+    const bool on = c < a.D;
+    const typename E::mem* rows = dy + (int64_t)node * a.T * a.ld;
+    float* g = a.g + (int64_t)node * a.ldg;
+    float* part = a.partial + ((int64_t)node * a.chunks + chunk) * 2 * a.D;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    bool fresh = true;  // the row began within the chunk
+    for (int e = 0; e < real; e += kAhead) {
+        float v[kAhead][4], had[kAhead][4];
 #pragma unroll
-            for (int k = 0; k < kTurns; ++k) {
-                const int32_t c = c0 + k * kTurnCols;
-                if (c >= a.D) break;
-                float had[4] = {0.f, 0.f, 0.f, 0.f};
-                if (a.accumulate) row_load4<ElemF32>(out, c, a.D, had);
+        for (int i = 0; i < kAhead; ++i) {
+            if (e + i < real && on) {
+                row_load4<E>(rows + (int64_t)__builtin_amdgcn_readlane(at, e + i) * a.ld, c, a.D, v[i]);
+                if (kAdd && (last >> (e + i) & 1))
+                    row_load4<ElemF32>(g + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)key, e + i) * a.D, c, a.D, had[i]);
+            }
+            if (!kAdd || !(last >> (e + i) & 1)) had[i][0] = had[i][1] = had[i][2] = had[i][3] = 0.f;
+        }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum[k][j] = bad ? __builtin_nanf("") : had[j] + a.scale * sum[k][j];
-                row_store4<ElemF32>(out, c, a.D, sum[k]);
+        for (int i = 0; i < kAhead; ++i) {
+            if (e + i < real && on) {
+                if (e + i == 0) fresh = (uint32_t)__builtin_amdgcn_readlane((int)key, 0) != before;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] += v[i][j];
+                if (last >> (e + i) & 1) {
+                    const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, e + i);
+                    const bool goes_on = e + i == count - 1 && row == after;
+                    // slot 0 if the row holds the first item too
+                    if (fresh && !goes_on) put_sum(a, g + (int64_t)row * a.D, c, had[i], sum);
+                    else row_store4<ElemF32>(part + (row == (uint32_t)__builtin_amdgcn_readlane((int)key, 0) ? 0 : a.D), c, a.D, sum);
+                    sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
+                    fresh = true;
+                }
             }
         }
     }
 }
 
-// Adds the parts of each long row, kTurnCols columns a workgroup: the one whose chunk holds the row's first item.  Its wavefronts
-// take contiguous shares of the parts; everything in a fixed order.
-__global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a, uint32_t column_blocks) {
+// Adds the parts of each row that reaches into several chunks, kTurnCols columns a workgroup: the one of the chunk in which the
+// row begins.  Its wavefronts take contiguous shares of the parts; everything in a fixed order.
+__global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a) {
     constexpr int kWaves = kThreads / kWave;
     __shared__ float s_part[kWaves][kTurnCols];
-    const uint32_t unit = blockIdx.x / column_blocks, node = unit / a.chunks, chunk = unit - node * a.chunks;
+    const uint32_t unit = blockIdx.x / a.column_blocks, node = unit / a.chunks, chunk = unit - node * a.chunks;
     const uint32_t* keys = a.keys + (int64_t)node * a.T;
-    const int32_t* start = a.start + (int64_t)node * (a.V + 1ll);
-    const int32_t first = (int32_t)chunk * kRun, end = a.T - first < kRun ? a.T : first + kRun;
-    const uint32_t key = keys[end - 1];
-    if (key >= (uint32_t)a.V || keys[a.T - 1] == (uint32_t)a.V + 1u) return;
-    const int32_t row_from = start[key], row_to = start[key + 1];
-    if (row_from < first || row_to - row_from <= kRun) return;
+    const int32_t first = (int32_t)chunk * kRun, next = first + kRun;
+    if (next >= a.T) return;  // the last chunk: nothing goes on
+    const uint32_t key = keys[next - 1];
+    if (key != keys[next] || key >= (uint32_t)a.V || out_of_range(keys, a)) return;
+    const bool from_first = keys[first] == key;
+    if (from_first && chunk && keys[first - 1] == key) return;  // begins earlier
+    const uint32_t parts = (uint32_t)(keys_below(keys + next, a.T - next, key + 1u) + kRun - 1) / kRun + 1;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int32_t c = (int32_t)(blockIdx.x - unit * column_blocks) * kTurnCols + lane * 4;
-    const uint32_t parts = (uint32_t)(row_to - 1) / kRun - chunk + 1, share = (parts + kWaves - 1) / kWaves;
+    const int32_t c = (int32_t)(blockIdx.x - unit * a.column_blocks) * kTurnCols + lane * 4;
+    const uint32_t share = (parts + kWaves - 1) / kWaves;
     const uint32_t from = wave * share, to = from + share < parts ? from + share : parts;
     const float* part = a.partial + ((int64_t)node * a.chunks + chunk) * 2 * a.D;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -338,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a, uint32_t co
 #pragma unroll 4
         for (uint32_t p = from; p < to; ++p) {
             float v[4];
-            row_load4<ElemF32>(part + ((int64_t)p * 2 + (p == 0 && row_from > first ? 1 : 0)) * a.D, c, a.D, v);
+            row_load4<ElemF32>(part + ((int64_t)p * 2 + (p == 0 && !from_first ? 1 : 0)) * a.D, c, a.D, v);
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[j] += v[j];
         }
@@ -347,15 +331,13 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a, uint32_t co
     for (int j = 0; j < 4; ++j) s_part[wave][j * kWave + lane] = sum[j];
     __syncthreads();
     if (wave == 0 && c < a.D) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            for (int w = 1; w < kWaves; ++w) sum[j] += s_part[w][j * kWave + lane];
         float* out = a.g + (int64_t)node * a.ldg + (int64_t)key * a.D;
         float had[4] = {0.f, 0.f, 0.f, 0.f};
         if (a.accumulate) row_load4<ElemF32>(out, c, a.D, had);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            for (int w = 1; w < kWaves; ++w) sum[j] += s_part[w][j * kWave + lane];
-            sum[j] = had[j] + a.scale * sum[j];
-        }
-        row_store4<ElemF32>(out, c, a.D, sum);
+        put_sum(a, out, c, had, sum);
     }
 }
 
@@ -363,11 +345,11 @@ uint32_t blocks_for(int64_t items, int64_t per_block) { return (uint32_t)((items
 
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
-// Scratch of the gradient: sorted keys and positions (of the tiles, and merged where there are several), row starts, parts of long rows.
+// Scratch of the gradient: sorted keys and positions (of the tiles, and merged where there are several), parts of rows.
 struct GradSpace {
-    size_t items, tile_keys, tile_pos, keys, pos, start, partial, bytes;
+    size_t items, tile_keys, tile_pos, keys, pos, partial, bytes;
     uint32_t tiles, chunks;
-    GradSpace(const RowsShape& s, int32_t V) {
+    explicit GradSpace(const RowsShape& s) {
         items = (size_t)s.n * (size_t)s.T;
         tiles = s.T > 0 ? blocks_for(s.T, kTile) : 0;
         const size_t one = padded(items * 4);
@@ -375,9 +357,8 @@ struct GradSpace {
         tile_pos = one;
         keys = tiles > 1 ? 2 * one : tile_keys;
         pos = tiles > 1 ? 3 * one : tile_pos;
-        start = (tiles > 1 ? 4 : 2) * one;
-        partial = start + padded((size_t)s.n * ((size_t)V + 1) * 4);
-        chunks = s.T > kRun ? blocks_for(s.T, kRun) : 0;  // no row is long otherwise
+        partial = (tiles > 1 ? 4 : 2) * one;
+        chunks = s.T > 0 ? blocks_for(s.T, kRun) : 0;
         bytes = partial + padded((size_t)s.n * chunks * 2 * (size_t)s.D * 4);
     }
 };
@@ -406,33 +387,40 @@ hipError_t launch_embed(const gpga_ctx* c, const RowsShape& s, const int32_t* to
     });
 }
 
-size_t embed_grad_scratch(const RowsShape& s, int32_t V) { return GradSpace(s, V).bytes; }
+size_t embed_grad_scratch(const RowsShape& s) { return GradSpace(s).bytes; }
 
 hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_t* tokens, int64_t table_off, int32_t V, float scale,
                              const void* dy, bool accumulate, void* scratch) {
-    const GradSpace space(s, V);
+    const GradSpace space(s);
     char* base = static_cast<char*>(scratch);
     auto words = [&](size_t at) { return reinterpret_cast<uint32_t*>(base + at); };
     auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(base + at); };
-    if (space.tiles) {
-        int bits = 0;
-        while (bits < 32 && ((uint32_t)V + 1u) >> bits) ++bits;
-        k_sort_tile<<<dim3(space.tiles * (uint32_t)s.n), dim3(kSortThreads), 0, c->stream>>>(tokens, s.T, V, space.tiles, bits, words(space.tile_keys),
-                                                                                           ints(space.tile_pos));
+    int bits = 0;
+    while (bits < 32 && ((uint32_t)V + 1u) >> bits) ++bits;
+    ZeroArgs zero = {};
+    zero.first_block = space.tiles * (uint32_t)s.n;
+    zero.count = (int64_t)V * s.D;
+    zero.per_node = accumulate ? 0 : blocks_for(zero.count, kZeroCols);
+    zero.ldg = c->ld;
+    zero.g = c->g + table_off;
+    const uint32_t blocks = zero.first_block + zero.per_node * (uint32_t)s.n;
+    if (blocks) {
+        k_sort_tile<<<dim3(blocks), dim3(kSortThreads), 0, c->stream>>>(tokens, s.T, V, space.tiles, bits, words(space.tile_keys), ints(space.tile_pos), zero);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const uint32_t merge_blocks = space.tiles > 1 ? blocks_for(s.T, kThreads) : 0;
-    const uint32_t merge_per_node = merge_blocks + blocks_for((int64_t)V + 1, kThreads);
-    k_merge<<<dim3(merge_per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(words(space.tile_keys), ints(space.tile_pos), s.T, V, space.tiles,
-                                                                                   merge_blocks, merge_per_node, words(space.keys), ints(space.pos),
-                                                                                   ints(space.start));
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (s.T == 0) return hipSuccess;
+    if (space.tiles > 1) {
+        const uint32_t per_node = blocks_for(s.T, kThreads);
+        k_merge<<<dim3(per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(words(space.tile_keys), ints(space.tile_pos), s.T, space.tiles, per_node,
+                                                                                 words(space.keys), ints(space.pos));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     GradArgs a = {};
+    a.n = (uint32_t)s.n;
     a.keys = words(space.keys);
     a.pos = ints(space.pos);
-    a.start = ints(space.start);
     a.T = s.T;
     a.V = V;
     a.D = s.D;
@@ -441,19 +429,18 @@ hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_
     a.scale = scale;
     a.accumulate = accumulate;
     a.chunks = space.chunks;
-    a.chunk_blocks = blocks_for(a.chunks, kThreads / kWave);
-    const int64_t spread = (int64_t)s.n * V / 16384;
-    a.rows_per_wave = (uint32_t)(spread < 1 ? 1 : spread < 4 ? spread : 4);
-    a.blocks_per_node = a.chunk_blocks + blocks_for(V, (int64_t)a.rows_per_wave * (kThreads / kWave));
+    a.column_blocks = blocks_for(s.D, kTurnCols);
     a.partial = reinterpret_cast<float*>(base + space.partial);
     a.g = c->g + table_off;
-    hipError_t e2 = with_elem(s.dtype, [&](auto el) {
+    const hipError_t e = with_elem(s.dtype, [&](auto el) {
         typedef decltype(el) E;
-        k_embed_grad<E><<<dim3(a.blocks_per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, static_cast<const typename E::mem*>(dy));
+        const dim3 grid(blocks_for((int64_t)a.chunks * a.column_blocks * s.n, kThreads / kWave));
+        const typename E::mem* rows = static_cast<const typename E::mem*>(dy);
+        if (accumulate) k_embed_grad<E, true><<<grid, dim3(kThreads), 0, c->stream>>>(a, rows);
+        else k_embed_grad<E, false><<<grid, dim3(kThreads), 0, c->stream>>>(a, rows);
         return hipGetLastError();
     });
-    if (e2 != hipSuccess || !a.chunks) return e2;
-    const uint32_t column_blocks = blocks_for(s.D, kTurnCols);
-    k_embed_join<<<dim3(a.chunks * column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, column_blocks);
+    if (e != hipSuccess || a.chunks < 2) return e;
+    k_embed_join<<<dim3(a.chunks * a.column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a);
     return hipGetLastError();
 }

@@ -174,7 +174,7 @@ struct RowsShape {
 };
 
 hipError_t launch_embed(const gpga_ctx* c, const RowsShape& s, const int32_t* tokens, int64_t table_off, int32_t V, float scale, void* y);
-size_t embed_grad_scratch(const RowsShape& s, int32_t V);
+size_t embed_grad_scratch(const RowsShape& s);
 hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_t* tokens, int64_t table_off, int32_t V, float scale,
                              const void* dy, bool accumulate, void* scratch);
 hipError_t launch_dropout(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* x, const void* residual, void* y);
