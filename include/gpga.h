@@ -385,8 +385,8 @@ gpga_status gpga_query(gpga_ctx* ctx, const char* name, double* value_out);
  * gradient to the same columns of g_dev (accumulate = 0: replaced; 1: added to what is there).  The other columns
  * of g_dev are not touched, and k does not change: a gpga_step follows when all of g_dev has been written.
  *
- * Activations are n * T rows, row i*T + t = token t of node i, T >= 0 tokens a node, of D (or V) elements of one
- * type, fp32, bf16 or fp16, with a common leading dimension ld (in elements) for all activations of a call.  Pointers need
+ * Activations are n * T rows, row i*T + t = token t of node i, 0 <= T <= 2^30 tokens a node, n*T < 2^31, of D (or V) <= 2^30
+ * elements of one type, fp32, bf16 or fp16, with a common leading dimension ld (in elements) for all activations of a call.  Pointers need
  * the alignment of their elements.  Arithmetic and sums are fp32 or wider; results are rounded to the activations' type
  * once, to nearest even.  An output may take the exact place of an input of the call; any other overlap of an output with
  * an input, another output or a bound array is EINVAL (columns of one wider array do not overlap).  tokens_dev and

@@ -12,11 +12,15 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---- lookup ----------------------------------------------------------------------------------------------------------
-// 2^lanes_log2 lanes a row, eight columns a lane and turn.  One workgroup for each kThreads >> lanes_log2 rows of a node.
+// 2^lanes_log2 lanes a row, eight columns a lane and turn, kTurns turns' loads under way together.  One workgroup for each
+// kThreads >> lanes_log2 rows of a node.
+constexpr int kTurns = 3;
+
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_embed(const int32_t* __restrict__ tokens, const float* __restrict__ table, int64_t ldx,
                                                     int32_t V, int32_t D, int32_t T, uint32_t blocks_per_node, int lanes_log2, float scale,
                                                     typename E::mem* __restrict__ y, int64_t ld) {
+    typedef Elem<float, E::kNarrow> P;
     const uint32_t node = blockIdx.x / blocks_per_node;
     const int32_t t = (int32_t)((blockIdx.x - node * blocks_per_node) * (uint32_t)(kThreads >> lanes_log2)) + (int32_t)(threadIdx.x >> lanes_log2);
     if (t >= T) return;
@@ -26,19 +30,23 @@ __global__ __launch_bounds__(kThreads) void k_embed(const int32_t* __restrict__ 
     const float other = tok < 0 ? 0.f : __builtin_nanf("");
     const float* src = table + (int64_t)node * ldx + (int64_t)(real ? tok : 0) * D;
     typename E::mem* dst = y + row * ld;
-    const int32_t step = kOct << lanes_log2;
-#pragma unroll 2
-    for (int32_t c = (int32_t)(threadIdx.x & ((1u << lanes_log2) - 1u)) * kOct; c < D; c += step) {
-        float v[kOct];
-        if (real) {
-            row_load<ElemF32>(src, c, D, v);
+    const int32_t step = kOct << lanes_log2, mine = (int32_t)(threadIdx.x & ((1u << lanes_log2) - 1u)) * kOct;
+    for (int32_t c0 = 0; c0 < D; c0 += kTurns * step) {
+        Piece<P, kOct> in[kTurns];
 #pragma unroll
-            for (int j = 0; j < kOct; ++j) v[j] *= scale;
-        } else {
+        for (int k = 0; k < kTurns; ++k)
+            if (c0 + k * step < D) in[k] = piece_load<kOct, P>(src, c0 + k * step + mine, D);
 #pragma unroll
-            for (int j = 0; j < kOct; ++j) v[j] = other;
+        for (int k = 0; k < kTurns; ++k) {
+            const int32_t c = c0 + k * step + mine;
+            if (c < D) {
+                float v[kOct];
+                piece_get<kOct, P>(in[k], c, D, v);
+#pragma unroll
+                for (int j = 0; j < kOct; ++j) v[j] = real ? v[j] * scale : other;
+                piece_put<kOct, E>(dst, c, D, v);
+            }
         }
-        row_store<E>(dst, c, D, v);
     }
 }
 
@@ -70,9 +78,7 @@ __device__ __forceinline__ void zero_block(const ZeroArgs& z, uint32_t b) {
 #pragma unroll
     for (int u = 0; u < kZeroUnits; ++u) {
         const int64_t e = base + (int64_t)(u * kSortThreads + threadIdx.x) * 4;
-        if (e + 4 <= z.count) ElemF32::store4(g + e, zero);
-        else
-            for (int64_t k = e; k < z.count; ++k) g[k] = 0.f;
+        if (e < z.count) piece_put<4, ElemF32>(g + e, 0, z.count - e < 4 ? (int32_t)(z.count - e) : 4, zero);
     }
 }
 
@@ -232,15 +238,17 @@ struct GradArgs {
 __device__ __forceinline__ bool out_of_range(const uint32_t* keys, const GradArgs& a) { return keys[a.T - 1] == (uint32_t)a.V + 1u; }
 
 // Four columns of a row of g from their sum and what g holds.
+template <typename P>
 __device__ __forceinline__ void put_sum(const GradArgs& a, float* out, int32_t c, const float* had, const float* sum) {
     float v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = had[j] + a.scale * sum[j];
-    row_store4<ElemF32>(out, c, a.D, v);
+    piece_put<4, P>(out, c, a.D, v);
 }
 
 template <typename E, bool kAdd>
 __global__ __launch_bounds__(kThreads) void k_embed_grad(GradArgs a, const typename E::mem* __restrict__ dy) {
+    typedef Elem<float, E::kNarrow> P;
     const int lane = threadIdx.x & (kWave - 1);
     const uint32_t wave = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const uint32_t unit = wave / a.column_blocks, node = unit / a.chunks, chunk = unit - node * a.chunks;
@@ -268,28 +276,33 @@ __global__ __launch_bounds__(kThreads) void k_embed_grad(GradArgs a, const typen
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
     bool fresh = true;  // the row began within the chunk
     for (int e = 0; e < real; e += kAhead) {
-        float v[kAhead][4], had[kAhead][4];
+        Piece<E, 4> in[kAhead];
+        Piece<P, 4> held[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (e + i < real && on) {
-                row_load4<E>(rows + (int64_t)__builtin_amdgcn_readlane(at, e + i) * a.ld, c, a.D, v[i]);
-                if (kAdd && (last >> (e + i) & 1))
-                    row_load4<ElemF32>(g + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)key, e + i) * a.D, c, a.D, had[i]);
-            }
-            if (!kAdd || !(last >> (e + i) & 1)) had[i][0] = had[i][1] = had[i][2] = had[i][3] = 0.f;
+            const int item = e + i < real ? e + i : real - 1;  // loads without a branch: the last item again
+            in[i] = piece_load<4, E>(rows + (int64_t)__builtin_amdgcn_readlane(at, item) * a.ld, c, a.D);
+            if (kAdd && (last >> item & 1))
+                held[i] = piece_load<4, P>(g + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)key, item) * a.D, c, a.D);
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (e + i < real && on) {
+            if (e + i < real) {
+                float v[4];
+                piece_get<4, E>(in[i], c, a.D, v);
                 if (e + i == 0) fresh = (uint32_t)__builtin_amdgcn_readlane((int)key, 0) != before;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum[j] += v[i][j];
+                for (int j = 0; j < 4; ++j) sum[j] += v[j];
                 if (last >> (e + i) & 1) {
                     const uint32_t row = (uint32_t)__builtin_amdgcn_readlane((int)key, e + i);
                     const bool goes_on = e + i == count - 1 && row == after;
-                    // slot 0 if the row holds the first item too
-                    if (fresh && !goes_on) put_sum(a, g + (int64_t)row * a.D, c, had[i], sum);
-                    else row_store4<ElemF32>(part + (row == (uint32_t)__builtin_amdgcn_readlane((int)key, 0) ? 0 : a.D), c, a.D, sum);
+                    if (on) {
+                        float had[4] = {0.f, 0.f, 0.f, 0.f};
+                        if (kAdd) piece_get<4, P>(held[i], c, a.D, had);
+                        // slot 0 if the row holds the first item too
+                        if (fresh && !goes_on) put_sum<P>(a, g + (int64_t)row * a.D, c, had, sum);
+                        else piece_put<4, P>(part + (row == (uint32_t)__builtin_amdgcn_readlane((int)key, 0) ? 0 : a.D), c, a.D, sum);
+                    }
                     sum[0] = sum[1] = sum[2] = sum[3] = 0.f;
                     fresh = true;
                 }
@@ -300,6 +313,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_grad(GradArgs a, const typen
 
 // Adds the parts of each row that reaches into several chunks, kTurnCols columns a workgroup: the one of the chunk in which the
 // row begins.  Its wavefronts take contiguous shares of the parts; everything in a fixed order.
+template <typename P>
 __global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a) {
     constexpr int kWaves = kThreads / kWave;
     __shared__ float s_part[kWaves][kTurnCols];
@@ -322,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a) {
 #pragma unroll 4
         for (uint32_t p = from; p < to; ++p) {
             float v[4];
-            row_load4<ElemF32>(part + ((int64_t)p * 2 + (p == 0 && !from_first ? 1 : 0)) * a.D, c, a.D, v);
+            piece_read<4, P>(part + ((int64_t)p * 2 + (p == 0 && !from_first ? 1 : 0)) * a.D, c, a.D, v);
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[j] += v[j];
         }
@@ -336,8 +350,8 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a) {
             for (int w = 1; w < kWaves; ++w) sum[j] += s_part[w][j * kWave + lane];
         float* out = a.g + (int64_t)node * a.ldg + (int64_t)key * a.D;
         float had[4] = {0.f, 0.f, 0.f, 0.f};
-        if (a.accumulate) row_load4<ElemF32>(out, c, a.D, had);
-        put_sum(a, out, c, had, sum);
+        if (a.accumulate) piece_read<4, P>(out, c, a.D, had);
+        put_sum<P>(a, out, c, had, sum);
     }
 }
 
@@ -379,12 +393,13 @@ hipError_t launch_embed(const gpga_ctx* c, const RowsShape& s, const int32_t* to
         }
     }
     const uint32_t per_node = blocks_for(s.T, kThreads >> lanes_log2);
-    return with_elem(s.dtype, [&](auto e) {
+    auto launch = [&](auto e) {
         typedef decltype(e) E;
         k_embed<E><<<dim3(per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(tokens, c->x + table_off, c->ld, V, s.D, s.T, per_node, lanes_log2,
                                                                                     scale, static_cast<typename E::mem*>(y), s.ld);
         return hipGetLastError();
-    });
+    };
+    return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }
 
 size_t embed_grad_scratch(const RowsShape& s) { return GradSpace(s).bytes; }
@@ -432,15 +447,16 @@ hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_
     a.column_blocks = blocks_for(s.D, kTurnCols);
     a.partial = reinterpret_cast<float*>(base + space.partial);
     a.g = c->g + table_off;
-    const hipError_t e = with_elem(s.dtype, [&](auto el) {
+    auto launch = [&](auto el) {
         typedef decltype(el) E;
         const dim3 grid(blocks_for((int64_t)a.chunks * a.column_blocks * s.n, kThreads / kWave));
         const typename E::mem* rows = static_cast<const typename E::mem*>(dy);
         if (accumulate) k_embed_grad<E, true><<<grid, dim3(kThreads), 0, c->stream>>>(a, rows);
         else k_embed_grad<E, false><<<grid, dim3(kThreads), 0, c->stream>>>(a, rows);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || a.chunks < 2) return e;
+        k_embed_join<Elem<float, E::kNarrow>><<<dim3(a.chunks * a.column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a);
         return hipGetLastError();
-    });
-    if (e != hipSuccess || a.chunks < 2) return e;
-    k_embed_join<<<dim3(a.chunks * a.column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a);
-    return hipGetLastError();
+    };
+    return s.D < 4 ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }

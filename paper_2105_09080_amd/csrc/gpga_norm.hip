@@ -38,7 +38,8 @@ struct NormArgs {
 };
 
 // ---- dropout ----------------------------------------------------------------------------------------------------------
-template <typename E>
+// 2^lanes_log2 lanes a row, one piece a lane and turn.
+template <typename E, bool kSide>
 __global__ __launch_bounds__(kThreads) void k_dropout(NormArgs<E> a, int lanes_log2) {
     const uint32_t node = blockIdx.x / a.per_node;
     const int32_t t = (int32_t)((blockIdx.x - node * a.per_node) * (uint32_t)(kThreads >> lanes_log2)) + (int32_t)(threadIdx.x >> lanes_log2);
@@ -48,27 +49,31 @@ __global__ __launch_bounds__(kThreads) void k_dropout(NormArgs<E> a, int lanes_l
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     for (uint32_t q = threadIdx.x & ((1u << lanes_log2) - 1u); q < octs; q += 1u << lanes_log2) {
         const int32_t c = (int32_t)q * kOct;
+        const Piece<E, kOct> in = piece_load<kOct, E>(a.x + row, c, a.D);
+        Piece<E, kOct> side;
+        if (kSide) side = piece_load<kOct, E>(a.side + row, c, a.D);
         float v[kOct];
-        row_load<E>(a.x + row, c, a.D, v);
+        piece_get<kOct, E>(in, c, a.D, v);
         if (a.drop.drop) mask.apply(a.drop, (uint32_t)t * octs + q, v);
-        if (a.side) {
+        if (kSide) {
             float r[kOct];
-            row_load<E>(a.side + row, c, a.D, r);
+            piece_get<kOct, E>(side, c, a.D, r);
 #pragma unroll
             for (int j = 0; j < kOct; ++j) v[j] += r[j];
         }
-        row_store<E>(a.y + row, c, a.D, v);
+        piece_put<kOct, E>(a.y + row, c, a.D, v);
     }
 }
 
 // u of eight columns, before rounding.
 template <typename E>
-__device__ __forceinline__ void norm_input(const NormArgs<E>& a, const DropNode& mask, int64_t row, uint32_t group, int32_t c, float* v) {
-    row_load<E>(a.x + row, c, a.D, v);
+__device__ __forceinline__ void norm_input(const NormArgs<E>& a, const DropNode& mask, const Piece<E, kOct>& x, const Piece<E, kOct>& side,
+                                           uint32_t group, int32_t c, float* v) {
+    piece_get<kOct, E>(x, c, a.D, v);
     if (a.drop.drop) mask.apply(a.drop, group, v);
     if (a.side) {
         float r[kOct];
-        row_load<E>(a.side + row, c, a.D, r);
+        piece_get<kOct, E>(side, c, a.D, r);
 #pragma unroll
         for (int j = 0; j < kOct; ++j) v[j] += r[j];
     }
@@ -77,53 +82,56 @@ __device__ __forceinline__ void norm_input(const NormArgs<E>& a, const DropNode&
 // y of eight columns from u.
 template <typename E>
 __device__ __forceinline__ void norm_output(const NormArgs<E>& a, uint32_t node, int64_t row, int32_t c, float mean, float rstd, const float* u) {
+    typedef Elem<float, E::kNarrow> P;
     float gm[kOct], bt[kOct], y[kOct];
-    row_load<ElemF32>(a.gamma + (int64_t)node * a.ldx, c, a.D, gm);
-    row_load<ElemF32>(a.beta + (int64_t)node * a.ldx, c, a.D, bt);
+    piece_read<kOct, P>(a.gamma + (int64_t)node * a.ldx, c, a.D, gm);
+    piece_read<kOct, P>(a.beta + (int64_t)node * a.ldx, c, a.D, bt);
 #pragma unroll
     for (int j = 0; j < kOct; ++j) y[j] = (u[j] - mean) * rstd * gm[j] + bt[j];
-    row_store<E>(a.y + row, c, a.D, y);
+    piece_put<kOct, E>(a.y + row, c, a.D, y);
 }
 
-// ---- forward: L lanes a row, N pieces of eight columns a lane, the row in registers ----------------------------------------
+// ---- forward: L lanes a row, N pieces a lane, the row in registers ----------------------------------------------------------
 template <typename E, int L, int N>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm(NormArgs<E> a) {
     constexpr int kRows = L > kThreads ? 1 : kThreads / L;  // rows of a workgroup
-    __shared__ float s_sum[L > kWave ? L / kWave : 1];
+    __shared__ float s_sum[2][L > kWave ? L / kWave : 1];
     const uint32_t node = blockIdx.x / a.per_node;
     const int32_t t = (int32_t)((blockIdx.x - node * a.per_node) * kRows + threadIdx.x / L);
-    if (t >= a.T) return;  // all lanes of a row; whole workgroups where a sum spans wavefronts
+    if (t >= a.T) return;  // all lanes of a row; no workgroup whose sums span wavefronts
     const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
     const int32_t lane = threadIdx.x & (L - 1);
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     const DropNode mask(a.drop, node);
-    float u[N][kOct];
-    float sum = 0.f;
+    Piece<E, kOct> x[N], side[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        x[k] = piece_load<kOct, E>(a.x + row, (lane + k * L) * kOct, a.D);
+        if (a.side) side[k] = piece_load<kOct, E>(a.side + row, (lane + k * L) * kOct, a.D);
+    }
+    float u[N][kOct], sum[1] = {0.f}, var[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int32_t q = lane + k * L, c = q * kOct;
-        if (c < a.D) {
-            norm_input<E>(a, mask, row, (uint32_t)t * octs + q, c, u[k]);
+        norm_input<E>(a, mask, x[k], side[k], (uint32_t)t * octs + q, c, u[k]);
 #pragma unroll
-            for (int j = 0; j < kOct; ++j)
-                if (c + j < a.D) sum += u[k][j];
-        }
+        for (int j = 0; j < kOct; ++j) sum[0] += c + j < a.D ? u[k][j] : 0.f;
     }
-    const float inv = 1.f / (float)a.D, mean = lanes_sum<L>(sum, s_sum) * inv;
-    float var = 0.f;
+    lanes_sum<L>(sum, s_sum[0]);
+    const float inv = 1.f / (float)a.D, mean = sum[0] * inv;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int32_t c = (lane + k * L) * kOct;
 #pragma unroll
-        for (int j = 0; j < kOct; ++j)
-            if (c + j < a.D) var += (u[k][j] - mean) * (u[k][j] - mean);
+        for (int j = 0; j < kOct; ++j) var[0] += c + j < a.D ? (u[k][j] - mean) * (u[k][j] - mean) : 0.f;
     }
-    const float rstd = 1.f / sqrtf(lanes_sum<L>(var, s_sum) * inv + a.eps);
+    lanes_sum<L>(var, s_sum[1]);
+    const float rstd = 1.f / sqrtf(var[0] * inv + a.eps);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int32_t c = (lane + k * L) * kOct;
         if (c < a.D) {
-            if (a.u) row_store<E>(a.u + row, c, a.D, u[k]);
+            if (a.u) piece_put<kOct, E>(a.u + row, c, a.D, u[k]);
             norm_output<E>(a, node, row, c, mean, rstd, u[k]);
         }
     }
@@ -136,29 +144,38 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm(NormArgs<E
 // Longer rows: one workgroup a row, which reads it three times (from the caches after the first).
 template <typename E>
 __global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs<E> a) {
-    __shared__ float s_sum[kLongThreads / kWave];
+    __shared__ float s_sum[2][kLongThreads / kWave];
     const uint32_t node = blockIdx.x / a.per_node;
     const int32_t t = (int32_t)(blockIdx.x - node * a.per_node);
     const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     const DropNode mask(a.drop, node);
-    float sum = 0.f, var = 0.f, u[kOct];
+    float sum[1] = {0.f}, var[1] = {0.f}, u[kOct];
+    auto input = [&](uint32_t q) {
+        const int32_t c = (int32_t)q * kOct;
+        const Piece<E, kOct> x = piece_load<kOct, E>(a.x + row, c, a.D);
+        Piece<E, kOct> side;
+        if (a.side) side = piece_load<kOct, E>(a.side + row, c, a.D);
+        norm_input<E>(a, mask, x, side, (uint32_t)t * octs + q, c, u);
+    };
     for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
-        norm_input<E>(a, mask, row, (uint32_t)t * octs + q, (int32_t)q * kOct, u);
+        input(q);
 #pragma unroll
-        for (int j = 0; j < kOct; ++j) sum += (int32_t)q * kOct + j < a.D ? u[j] : 0.f;
+        for (int j = 0; j < kOct; ++j) sum[0] += (int32_t)q * kOct + j < a.D ? u[j] : 0.f;
     }
-    const float inv = 1.f / (float)a.D, mean = lanes_sum<kLongThreads>(sum, s_sum) * inv;
+    lanes_sum<kLongThreads>(sum, s_sum[0]);
+    const float inv = 1.f / (float)a.D, mean = sum[0] * inv;
     for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
-        norm_input<E>(a, mask, row, (uint32_t)t * octs + q, (int32_t)q * kOct, u);
+        input(q);
 #pragma unroll
-        for (int j = 0; j < kOct; ++j) var += (int32_t)q * kOct + j < a.D ? (u[j] - mean) * (u[j] - mean) : 0.f;
+        for (int j = 0; j < kOct; ++j) var[0] += (int32_t)q * kOct + j < a.D ? (u[j] - mean) * (u[j] - mean) : 0.f;
     }
-    const float rstd = 1.f / sqrtf(lanes_sum<kLongThreads>(var, s_sum) * inv + a.eps);
+    lanes_sum<kLongThreads>(var, s_sum[1]);
+    const float rstd = 1.f / sqrtf(var[0] * inv + a.eps);
     for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
         const int32_t c = (int32_t)q * kOct;
-        norm_input<E>(a, mask, row, (uint32_t)t * octs + q, c, u);
-        if (a.u) row_store<E>(a.u + row, c, a.D, u);
+        input(q);
+        if (a.u) piece_put<kOct, E>(a.u + row, c, a.D, u);
         norm_output<E>(a, node, row, c, mean, rstd, u);
     }
     if (a.stats && threadIdx.x == 0) {
@@ -168,89 +185,114 @@ __global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs<E> a) {
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------------------
-// dy and xh of eight columns.
-template <typename E>
-__device__ __forceinline__ void grad_input(const NormArgs<E>& a, int64_t row, int32_t c, float mean, float rstd, float* dy, float* xh) {
-    row_load<E>(a.x + row, c, a.D, dy);
-    row_load<E>(a.u_in + row, c, a.D, xh, mean);
+// What a lane has of a row: dy, u and the residual stream's gradient, as they lie in memory.
+template <typename E, int N>
+struct GradRow {
+    Piece<E, kOct> dy[N], u[N], more[N];
+    float mean, rstd;
+};
+template <int L, int N, typename E>
+__device__ __forceinline__ void grad_load(const NormArgs<E>& a, int64_t r, int32_t lane, GradRow<E, N>& in) {
+    const int64_t row = r * a.ld;
 #pragma unroll
-    for (int j = 0; j < kOct; ++j) xh[j] = (xh[j] - mean) * rstd;
+    for (int k = 0; k < N; ++k) {
+        const int32_t c = (lane + k * L) * kOct;
+        in.dy[k] = piece_load<kOct, E>(a.x + row, c, a.D);
+        in.u[k] = piece_load<kOct, E>(a.u_in + row, c, a.D);
+        if (a.side) in.more[k] = piece_load<kOct, E>(a.side + row, c, a.D);
+    }
+    in.mean = a.stats[2 * r];
+    in.rstd = a.stats[2 * r + 1];
+}
+// dy and xh of eight columns; 0 past the end of the row.
+template <typename E>
+__device__ __forceinline__ void grad_input(const Piece<E, kOct>& dy_in, const Piece<E, kOct>& u_in, int32_t c, int32_t D, float mean, float rstd,
+                                           float* dy, float* xh) {
+    piece_get<kOct, E>(dy_in, c, D, dy);
+    piece_get<kOct, E>(u_in, c, D, xh);
+#pragma unroll
+    for (int j = 0; j < kOct; ++j) {
+        xh[j] = c + j < D ? (xh[j] - mean) * rstd : 0.f;
+        dy[j] = c + j < D ? dy[j] : 0.f;
+    }
 }
 // du and dx of eight columns.
 template <typename E>
-__device__ __forceinline__ void grad_output(const NormArgs<E>& a, const DropNode& mask, int64_t row, uint32_t group, int32_t c, float rstd, float m1,
-                                            float m2, const float* h, const float* xh) {
+__device__ __forceinline__ void grad_output(const NormArgs<E>& a, const DropNode& mask, const Piece<E, kOct>& more_in, int64_t row, uint32_t group,
+                                            int32_t c, float rstd, float m1, float m2, const float* h, const float* xh) {
     float du[kOct], more[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (a.side) row_load<E>(a.side + row, c, a.D, more);
+    if (a.side) piece_get<kOct, E>(more_in, c, a.D, more);
 #pragma unroll
     for (int j = 0; j < kOct; ++j) du[j] = rstd * (h[j] - m1 - xh[j] * m2) + more[j];
-    row_store<E>(a.u + row, c, a.D, du);
+    piece_put<kOct, E>(a.u + row, c, a.D, du);
     if (a.y) {
-        if (a.drop.drop) mask.apply(a.drop, group, du);
-        row_store<E>(a.y + row, c, a.D, du);
+        mask.apply(a.drop, group, du);
+        piece_put<kOct, E>(a.y + row, c, a.D, du);
     }
 }
 
 // L lanes a row.  A workgroup takes the rows t = strip, strip + strips, ... of a node kRows at a time, keeps its sums for
-// dgamma and dbeta in registers, and leaves them in `partial`.
+// dgamma and dbeta in registers, and leaves them in `partial`.  A row's loads are issued while the one before it is worked on.
 template <typename E, int L, int N>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormArgs<E> a) {
+    typedef Elem<float, E::kNarrow> P;
     constexpr int kBlock = L > kThreads ? L : kThreads, kRows = kBlock / L;
-    __shared__ float s_sum[L > kWave ? L / kWave : 1];
+    __shared__ float s_sum[2][L > kWave ? 2 * L / kWave : 1];
     __shared__ float s_part[kRows > 1 ? 2 * L * N * kOct : 1];
     const uint32_t node = blockIdx.x / a.per_node, strip = blockIdx.x - node * a.per_node;
     const int32_t lane = threadIdx.x & (L - 1), sub = threadIdx.x / L;
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     const DropNode mask(a.drop, node);
     const float inv = 1.f / (float)a.D;
+    const int64_t first_row = (int64_t)node * a.T, stride = (int64_t)a.per_node * kRows;
+    int64_t t = (int64_t)strip * kRows + sub;
+    GradRow<E, N> next;
+    if (t < a.T) grad_load<L, N, E>(a, first_row + t, lane, next);
     float gm[N][kOct], dg[N][kOct], db[N][kOct];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int32_t c = (lane + k * L) * kOct;
-        if (c < a.D) row_load<ElemF32>(a.gamma + (int64_t)node * a.ldx, c, a.D, gm[k]);
+        piece_read<kOct, P>(a.gamma + (int64_t)node * a.ldx, c, a.D, gm[k]);
 #pragma unroll
         for (int j = 0; j < kOct; ++j) dg[k][j] = db[k][j] = 0.f;
     }
-    for (int64_t t = (int64_t)strip * kRows + sub; t < a.T; t += (int64_t)a.per_node * kRows) {  // all lanes of a row alike
-        const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
-        const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1];
-        float dy[N][kOct], xh[N][kOct];
-        float s1 = 0.f, s2 = 0.f;
+    int turn = 0;
+    for (; t < a.T; t += stride, turn ^= 1) {  // all lanes of a row alike
+        const int64_t row = (first_row + t) * a.ld;
+        const GradRow<E, N> in = next;
+        if (t + stride < a.T) grad_load<L, N, E>(a, first_row + t + stride, lane, next);
+        float h[N][kOct], xh[N][kOct], s[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int32_t c = (lane + k * L) * kOct;
-            if (c < a.D) {
-                grad_input<E>(a, row, c, mean, rstd, dy[k], xh[k]);
+            grad_input<E>(in.dy[k], in.u[k], (lane + k * L) * kOct, a.D, in.mean, in.rstd, h[k], xh[k]);
 #pragma unroll
-                for (int j = 0; j < kOct; ++j) {
-                    dg[k][j] += dy[k][j] * xh[k][j];
-                    db[k][j] += dy[k][j];
-                    dy[k][j] *= gm[k][j];  // h
-                    s1 += dy[k][j];
-                    s2 += dy[k][j] * xh[k][j];
-                }
+            for (int j = 0; j < kOct; ++j) {
+                dg[k][j] += h[k][j] * xh[k][j];
+                db[k][j] += h[k][j];
+                h[k][j] *= gm[k][j];
+                s[0] += h[k][j];
+                s[1] += h[k][j] * xh[k][j];
             }
         }
-        s1 = lanes_sum<L>(s1, s_sum) * inv;
-        s2 = lanes_sum<L>(s2, s_sum) * inv;
+        lanes_sum<L>(s, s_sum[turn]);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const int32_t q = lane + k * L, c = q * kOct;
-            if (c < a.D) grad_output<E>(a, mask, row, (uint32_t)t * octs + (uint32_t)q, c, rstd, s1, s2, dy[k], xh[k]);
+            if (c < a.D) grad_output<E>(a, mask, in.more[k], row, (uint32_t)t * octs + (uint32_t)q, c, in.rstd, s[0] * inv, s[1] * inv, h[k], xh[k]);
         }
     }
     // the rows of a workgroup one after another
     float* out = a.partial + (int64_t)blockIdx.x * 2 * a.D;
     if (kRows > 1) {
-        for (int turn = 0; turn < kRows; ++turn) {
-            if (sub == turn) {
+        for (int part = 0; part < kRows; ++part) {
+            if (sub == part) {
 #pragma unroll
                 for (int k = 0; k < N; ++k)
 #pragma unroll
                     for (int j = 0; j < kOct; ++j) {
-                        const int32_t at = ((k * kOct + j) * L + lane) * 2;  // neighbouring lanes side by side
-                        s_part[at] = turn ? s_part[at] + dg[k][j] : dg[k][j];
-                        s_part[at + 1] = turn ? s_part[at + 1] + db[k][j] : db[k][j];
+                        float* at = s_part + ((k * kOct + j) * 2) * L + lane;
+                        at[0] = part ? at[0] + dg[k][j] : dg[k][j];
+                        at[L] = part ? at[L] + db[k][j] : db[k][j];
                     }
             }
             __syncthreads();
@@ -260,9 +302,9 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormA
             for (int k = 0; k < N; ++k)
 #pragma unroll
                 for (int j = 0; j < kOct; ++j) {
-                    const int32_t at = ((k * kOct + j) * L + lane) * 2;
-                    dg[k][j] = s_part[at];
-                    db[k][j] = s_part[at + 1];
+                    const float* at = s_part + ((k * kOct + j) * 2) * L + lane;
+                    dg[k][j] = at[0];
+                    db[k][j] = at[L];
                 }
         }
     }
@@ -271,8 +313,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormA
         for (int k = 0; k < N; ++k) {
             const int32_t c = (lane + k * L) * kOct;
             if (c < a.D) {
-                row_store<ElemF32>(out, c, a.D, dg[k]);
-                row_store<ElemF32>(out + a.D, c, a.D, db[k]);
+                piece_put<kOct, P>(out, c, a.D, dg[k]);
+                piece_put<kOct, P>(out + a.D, c, a.D, db[k]);
             }
         }
     }
@@ -299,33 +341,37 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_columns(NormArgs<E> a, u
 }
 template <typename E>
 __global__ __launch_bounds__(kLongThreads) void k_norm_grad_long(NormArgs<E> a) {
-    __shared__ float s_sum[kLongThreads / kWave];
+    __shared__ float s_sum[2 * kLongThreads / kWave];
     const uint32_t node = blockIdx.x / (uint32_t)a.T;
     const uint32_t t = blockIdx.x - node * (uint32_t)a.T;
-    const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
+    const int64_t r = (int64_t)node * a.T + t;
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     const DropNode mask(a.drop, node);
-    const float inv = 1.f / (float)a.D, mean = a.stats[2 * r], rstd = a.stats[2 * r + 1];
     const float* gamma = a.gamma + (int64_t)node * a.ldx;
-    float s1 = 0.f, s2 = 0.f, h[kOct], xh[kOct], gm[kOct];
-    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
-        grad_input<E>(a, row, (int32_t)q * kOct, mean, rstd, h, xh);
-        row_load<ElemF32>(gamma, (int32_t)q * kOct, a.D, gm);
-#pragma unroll
-        for (int j = 0; j < kOct; ++j) {
-            s1 += gm[j] * h[j];
-            s2 += gm[j] * h[j] * xh[j];
-        }
-    }
-    s1 = lanes_sum<kLongThreads>(s1, s_sum) * inv;
-    s2 = lanes_sum<kLongThreads>(s2, s_sum) * inv;
-    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
+    float s[2] = {0.f, 0.f}, h[kOct], xh[kOct];
+    GradRow<E, 1> in;
+    auto input = [&](uint32_t q) {
         const int32_t c = (int32_t)q * kOct;
-        grad_input<E>(a, row, c, mean, rstd, h, xh);
-        row_load<ElemF32>(gamma, c, a.D, gm);
+        float gm[kOct];
+        grad_load<kLongThreads, 1, E>(a, r, (int32_t)q, in);
+        piece_read<kOct, ElemF32>(gamma, c, a.D, gm);
+        grad_input<E>(in.dy[0], in.u[0], c, a.D, in.mean, in.rstd, h, xh);
 #pragma unroll
         for (int j = 0; j < kOct; ++j) h[j] *= gm[j];
-        grad_output<E>(a, mask, row, t * octs + q, c, rstd, s1, s2, h, xh);
+    };
+    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
+        input(q);
+#pragma unroll
+        for (int j = 0; j < kOct; ++j) {
+            s[0] += h[j];
+            s[1] += h[j] * xh[j];
+        }
+    }
+    lanes_sum<kLongThreads>(s, s_sum);
+    const float inv = 1.f / (float)a.D;
+    for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
+        input(q);
+        grad_output<E>(a, mask, in.more[0], r * a.ld, t * octs + q, (int32_t)q * kOct, in.rstd, s[0] * inv, s[1] * inv, h, xh);
     }
 }
 
@@ -339,8 +385,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_join(const float* __rest
     const int64_t c = (int64_t)(blockIdx.x - node * blocks_per_node) * kWave + lane;  // 0 .. 2D-1: gamma's columns, then beta's
     const float* from = partial + (int64_t)node * strips * 2 * D + c;
     float sum = 0.f;
-    if (c < 2 * (int64_t)D)
+    if (c < 2 * (int64_t)D) {
+#pragma unroll 8
         for (uint32_t k = wave; k < strips; k += kWaves) sum += from[(int64_t)k * 2 * D];
+    }
     s_part[wave][lane] = sum;
     __syncthreads();
     if (wave == 0 && c < 2 * (int64_t)D) {
@@ -356,9 +404,10 @@ template <int V>
 struct Const {
     static constexpr int value = V;
 };
-template <typename F>
+template <typename E, typename F>
 bool with_row_shape(int32_t octs, F&& f) {
-    if (octs <= 16) f(Const<16>(), Const<1>());
+    if constexpr (E::kNarrow) f(Const<16>(), Const<1>());
+    else if (octs <= 16) f(Const<16>(), Const<1>());
     else if (octs <= 32) f(Const<32>(), Const<1>());
     else if (octs <= 64) f(Const<32>(), Const<2>());
     else if (octs <= 96) f(Const<32>(), Const<3>());
@@ -371,16 +420,16 @@ bool with_row_shape(int32_t octs, F&& f) {
     return true;
 }
 
-// Strips of a node: four workgroups a compute unit over all nodes, no more than there are rows for.
+// Strips of a node: two workgroups a compute unit over all nodes, no more than there are rows for.
 uint32_t norm_grad_strips(const RowsShape& s) {
-    const int64_t most = 1024 / s.n > 1 ? 1024 / s.n : 1;
+    const int64_t most = 512 / s.n > 1 ? 512 / s.n : 1;
     return (uint32_t)(s.T < most ? (s.T > 0 ? s.T : 1) : most);
 }
 
 }  // namespace
 
 hipError_t launch_dropout(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* x, const void* residual, void* y) {
-    return with_elem(s.dtype, [&](auto e) {
+    auto launch = [&](auto e) {
         typedef decltype(e) E;
         typedef typename E::mem M;
         NormArgs<E> a = {};
@@ -395,14 +444,17 @@ hipError_t launch_dropout(const gpga_ctx* c, const RowsShape& s, const DropArgs&
         int lanes_log2 = 0;
         while (lanes_log2 < 8 && (1 << lanes_log2) < octs) ++lanes_log2;
         a.per_node = blocks_for(s.T, kThreads >> lanes_log2);
-        k_dropout<E><<<dim3(a.per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, lanes_log2);
+        const dim3 grid(a.per_node * (uint32_t)s.n);
+        if (residual) k_dropout<E, true><<<grid, dim3(kThreads), 0, c->stream>>>(a, lanes_log2);
+        else k_dropout<E, false><<<grid, dim3(kThreads), 0, c->stream>>>(a, lanes_log2);
         return hipGetLastError();
-    });
+    };
+    return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }
 
 hipError_t launch_norm(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* x, const void* residual, int64_t gamma_off,
                        int64_t beta_off, float eps, void* u, void* y, float* stats) {
-    return with_elem(s.dtype, [&](auto e) {
+    auto launch = [&](auto e) {
         typedef decltype(e) E;
         typedef typename E::mem M;
         NormArgs<E> a = {};
@@ -419,17 +471,20 @@ hipError_t launch_norm(const gpga_ctx* c, const RowsShape& s, const DropArgs& dr
         a.stats = stats;
         a.gamma = c->x + gamma_off;
         a.beta = c->x + beta_off;
-        const bool held = with_row_shape((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
+        const bool held = with_row_shape<E>((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
             constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
             a.per_node = blocks_for(s.T, kBlock / L);
             k_norm<E, L, N><<<dim3(a.per_node * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
         });
-        if (!held) {
-            a.per_node = (uint32_t)s.T;
-            k_norm_long<E><<<dim3(a.per_node * (uint32_t)s.n), dim3(kLongThreads), 0, c->stream>>>(a);
+        if constexpr (!E::kNarrow) {
+            if (!held) {
+                a.per_node = (uint32_t)s.T;
+                k_norm_long<E><<<dim3(a.per_node * (uint32_t)s.n), dim3(kLongThreads), 0, c->stream>>>(a);
+            }
         }
         return hipGetLastError();
-    });
+    };
+    return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }
 
 size_t norm_grad_scratch(const RowsShape& s) { return (size_t)s.n * norm_grad_strips(s) * 2 * (size_t)s.D * sizeof(float); }
@@ -437,7 +492,7 @@ size_t norm_grad_scratch(const RowsShape& s) { return (size_t)s.n * norm_grad_st
 hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* dy, const void* u, const float* stats,
                             const void* more, int64_t gamma_off, int64_t beta_off, void* du, void* dx, bool accumulate, void* scratch) {
     const uint32_t strips = norm_grad_strips(s);
-    const hipError_t e = with_elem(s.dtype, [&](auto el) {
+    auto launch = [&](auto el) {
         typedef decltype(el) E;
         typedef typename E::mem M;
         NormArgs<E> a = {};
@@ -455,17 +510,20 @@ hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArg
         a.gamma = c->x + gamma_off;
         a.partial = static_cast<float*>(scratch);
         a.per_node = strips;
-        const bool held = with_row_shape((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
+        const bool held = with_row_shape<E>((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
             constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
             k_norm_grad<E, L, N><<<dim3(strips * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
         });
-        if (!held) {
-            const uint32_t column_blocks = blocks_for(s.D, kThreads);
-            k_norm_grad_columns<E><<<dim3(strips * column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, column_blocks);
-            if (s.T > 0) k_norm_grad_long<E><<<dim3((uint32_t)s.T * (uint32_t)s.n), dim3(kLongThreads), 0, c->stream>>>(a);
+        if constexpr (!E::kNarrow) {
+            if (!held) {
+                const uint32_t column_blocks = blocks_for(s.D, kThreads);
+                k_norm_grad_columns<E><<<dim3(strips * column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, column_blocks);
+                if (s.T > 0) k_norm_grad_long<E><<<dim3((uint32_t)s.T * (uint32_t)s.n), dim3(kLongThreads), 0, c->stream>>>(a);
+            }
         }
         return hipGetLastError();
-    });
+    };
+    const hipError_t e = s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
     if (e != hipSuccess) return e;
     const uint32_t blocks = blocks_for(2 * (int64_t)s.D, kWave);
     k_norm_grad_join<<<dim3(blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(static_cast<const float*>(scratch), strips, s.D, blocks, accumulate,

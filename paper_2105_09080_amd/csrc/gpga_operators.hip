@@ -49,6 +49,7 @@ gpga_status reserve(gpga_ctx* c, size_t bytes) {
 int64_t elem_size(int32_t dtype) { return dtype == GPGA_F32 ? 4 : 2; }
 
 constexpr int32_t kMaxTokens = 1 << 30;     // token numbers of a node are 32-bit
+constexpr int32_t kMaxRow = 1 << 30;        // and so are column numbers
 constexpr int64_t kMaxGroups = 0x7fffffff;  // workgroups of a launch
 
 // An array of rows as a call sees it.
@@ -76,7 +77,7 @@ gpga_status check_ready(gpga_ctx* c) {
 gpga_status check_rows(gpga_ctx* c, const RowsShape& s, const Array* arrays, int count) {
     if (s.dtype < GPGA_F32 || s.dtype > GPGA_F16) return fail(c, GPGA_EINVAL, "dtype %d is not a gpga_dtype", s.dtype);
     if (s.T < 0 || s.T > kMaxTokens) return fail(c, GPGA_EINVAL, "T = %d must be 0..%d", s.T, kMaxTokens);
-    if (s.D < 1) return fail(c, GPGA_EINVAL, "a row has %d elements: at least 1 is needed", s.D);
+    if (s.D < 1 || s.D > kMaxRow) return fail(c, GPGA_EINVAL, "a row has %d elements: it needs 1..%d", s.D, kMaxRow);
     if (s.ld < s.D) return fail(c, GPGA_EINVAL, "ld = %lld is smaller than the %d elements of a row", (long long)s.ld, s.D);
     const int64_t size = elem_size(s.dtype), rows = (int64_t)s.n * s.T;
     int64_t bytes = 0;
@@ -264,7 +265,7 @@ gpga_status gpga_token_loss(gpga_ctx* c, const void* logits, const int32_t* labe
     if (!loss || (reinterpret_cast<uintptr_t>(loss) & 3u)) return fail(c, GPGA_EINVAL, "loss_dev must be a 4-byte aligned device pointer");
     if (T > 0 && !logits) return fail(c, GPGA_EINVAL, "logits_dev must not be NULL");
     DeviceGuard guard(c->device);
-    GPGA_TRY(reserve(c, token_loss_scratch(s)));
+    GPGA_TRY(reserve(c, token_loss_scratch(s, c->num_cus)));
     const hipError_t e = launch_token_loss(c, s, logits, labels, grad_scale, loss, dlogits, c->op_scratch);
     return e == hipSuccess ? GPGA_OK : hip_fail(c, e, "token loss kernel launch");
 }

@@ -11,134 +11,169 @@
 
 constexpr uint32_t TAG_DROPOUT = 4u;  // low byte of the fourth counter word, the layer above it
 
-// ---- element types -------------------------------------------------------------------------------------------------
-// Eight elements at a time.  Rows need only the alignment of an element: gfx950 takes 16-byte global accesses at any
-// address, so a wide access is the same instruction for every leading dimension and column offset.
+// ---- element types and pieces of a row -------------------------------------------------------------------------------
+// A lane owns W consecutive columns of a row at a time, a piece (8 where the rows are those of activations, 4 where fp32 rows of
+// g are written).  Rows need only the alignment of an element: gfx950 takes 16-byte global accesses at any address, so a wide
+// access is the same instruction for every leading dimension and column offset.
+//
+// The last piece of a row whose D no W divides, and pieces behind the row, are read at column D - W instead, so loads need no
+// branch and many are under way together; piece_get then moves the columns to their places.  What a piece holds of other
+// lanes' columns is dropped there, so an output may take the place of an input.  Kinds with kNarrow read element by element:
+// they are for rows shorter than a piece.
+constexpr int kOct = 8;
 
-constexpr int kOct = 8;  // columns a lane owns in one piece (one Philox call gives the dropout lots of eight)
-
-struct ElemF32 {
-    typedef float mem;
-    typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
-    static __device__ __forceinline__ float get(mem v) { return v; }
-    static __device__ __forceinline__ mem put(float v) { return v; }
-    static __device__ __forceinline__ void load8(const mem* p, float* v) {
-        const vec a = *reinterpret_cast<const vec*>(p), b = *reinterpret_cast<const vec*>(p + 4);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] = a[j];
-            v[4 + j] = b[j];
-        }
-    }
-    static __device__ __forceinline__ void load4(const mem* p, float* v) {
-        const vec a = *reinterpret_cast<const vec*>(p);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = a[j];
-    }
-    static __device__ __forceinline__ void store4(mem* p, const float* v) {
-        vec a;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = v[j];
-        *reinterpret_cast<vec*>(p) = a;
-    }
-    static __device__ __forceinline__ void store8(mem* p, const float* v) {
-        vec a, b;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            a[j] = v[j];
-            b[j] = v[4 + j];
-        }
-        *reinterpret_cast<vec*>(p) = a;
-        *reinterpret_cast<vec*>(p + 4) = b;
-    }
-};
-
-template <typename M>
-struct Elem16 {
+template <typename M, bool kNarrow_>
+struct Elem {
     typedef M mem;
-    typedef M vec __attribute__((ext_vector_type(8), aligned(2)));
-    typedef float wide __attribute__((ext_vector_type(8)));
-    typedef M vec4 __attribute__((ext_vector_type(4), aligned(2)));
+    static constexpr bool kNarrow = kNarrow_;
     static __device__ __forceinline__ float get(mem v) { return (float)v; }
     static __device__ __forceinline__ mem put(float v) { return (mem)v; }  // to nearest, ties to even
-    static __device__ __forceinline__ void load8(const mem* p, float* v) {
-        const wide w = __builtin_convertvector(*reinterpret_cast<const vec*>(p), wide);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = w[j];
-    }
-    static __device__ __forceinline__ void load4(const mem* p, float* v) {
-        const v4f w = __builtin_convertvector(*reinterpret_cast<const vec4*>(p), v4f);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = w[j];
-    }
-    static __device__ __forceinline__ void store8(mem* p, const float* v) {
-        wide w;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = v[j];
-        *reinterpret_cast<vec*>(p) = __builtin_convertvector(w, vec);
-    }
 };
-typedef Elem16<__bf16> ElemBF16;
-typedef Elem16<_Float16> ElemF16;
+typedef Elem<float, false> ElemF32;
 
-// Columns c .. c+7 of a row of D; columns past the end read as `fill` and are not stored.
-template <typename E>
-__device__ __forceinline__ void row_load(const typename E::mem* row, int32_t c, int32_t D, float* v, float fill = 0.f) {
-    if (c + kOct <= D) {
-        E::load8(row + c, v);
-    } else {
+template <typename E, int W>
+struct Piece {
+    static constexpr int kWords = W * (int)sizeof(typename E::mem) / 4;
+    uint32_t w[kWords];
+};
+
+template <int W, typename E>
+__device__ __forceinline__ Piece<E, W> piece_load(const typename E::mem* row, int32_t c, int32_t D) {
+    typedef typename E::mem M;
+    Piece<E, W> p;
+    if constexpr (E::kNarrow) {
+        M v[W];
 #pragma unroll
-        for (int j = 0; j < kOct; ++j) v[j] = c + j < D ? E::get(row[c + j]) : fill;
+        for (int j = 0; j < W; ++j) v[j] = c + j < D ? row[c + j] : (M)0.f;
+        __builtin_memcpy(p.w, v, sizeof(p.w));
+    } else {
+        constexpr int kLoad = Piece<E, W>::kWords < 4 ? Piece<E, W>::kWords : 4;
+        typedef uint32_t vec __attribute__((ext_vector_type(kLoad), aligned(alignof(M))));
+        const M* at = row + (c + W <= D ? c : D - W);
+#pragma unroll
+        for (int k = 0; k < Piece<E, W>::kWords / kLoad; ++k) {
+            const vec v = reinterpret_cast<const vec*>(at)[k];
+#pragma unroll
+            for (int j = 0; j < kLoad; ++j) p.w[k * kLoad + j] = v[j];
+        }
+    }
+    return p;
+}
+
+// Columns c .. c+W-1 in fp32; 0 past the end of the row.  Of no meaning for c >= D.
+template <int W, typename E>
+__device__ __forceinline__ void piece_get(Piece<E, W> p, int32_t c, int32_t D, float* v) {
+    typedef typename E::mem M;
+    constexpr int N = Piece<E, W>::kWords, kPerWord = 4 / (int)sizeof(M);
+    if (!E::kNarrow && D % W) {
+        const bool tail = c + W > D;
+        const uint32_t gone = (uint32_t)(W - D % W);  // columns before c that a last piece holds
+#pragma unroll
+        for (int step = N / 2; step > 0; step >>= 1)
+            if (gone / kPerWord & step) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) p.w[k] = tail ? (k + step < N ? p.w[k + step] : 0u) : p.w[k];
+            }
+        if (kPerWord == 2 && (gone & 1)) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) p.w[k] = tail ? (k + 1 < N ? p.w[k + 1] << 16 : 0u) | p.w[k] >> 16 : p.w[k];
+        }
+    }
+    if constexpr (sizeof(M) == 4) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[j] = __builtin_bit_cast(float, p.w[j]);
+    } else {
+        typedef M pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            if constexpr (__is_same(M, __bf16)) {
+                v[2 * k] = __builtin_bit_cast(float, p.w[k] << 16);
+                v[2 * k + 1] = __builtin_bit_cast(float, p.w[k] & 0xffff0000u);
+            } else {
+                const pair h = __builtin_bit_cast(pair, p.w[k]);
+                v[2 * k] = (float)h[0];
+                v[2 * k + 1] = (float)h[1];
+            }
+        }
     }
 }
-template <typename E>
-__device__ __forceinline__ void row_store(typename E::mem* row, int32_t c, int32_t D, const float* v) {
-    if (c + kOct <= D) {
-        E::store8(row + c, v);
+
+// Both for one piece.
+template <int W, typename E>
+__device__ __forceinline__ void piece_read(const typename E::mem* row, int32_t c, int32_t D, float* v) {
+    piece_get<W, E>(piece_load<W, E>(row, c, D), c, D, v);
+}
+
+// Columns c .. of the row, as many as there are, c < D.
+template <int W, typename E>
+__device__ __forceinline__ void piece_put(typename E::mem* row, int32_t c, int32_t D, const float* v) {
+    typedef typename E::mem M;
+    typedef M vec __attribute__((ext_vector_type(W), aligned(alignof(M))));
+    typedef float wide __attribute__((ext_vector_type(W)));
+    if (!E::kNarrow && c + W <= D) {
+        wide f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) f[j] = v[j];
+        *reinterpret_cast<vec*>(row + c) = __builtin_convertvector(f, vec);
     } else {
 #pragma unroll
-        for (int j = 0; j < kOct; ++j)
+        for (int j = 0; j < W; ++j)
             if (c + j < D) row[c + j] = E::put(v[j]);
     }
 }
 
-// Columns c .. c+3 in the same way.
-template <typename E>
-__device__ __forceinline__ void row_load4(const typename E::mem* row, int32_t c, int32_t D, float* v) {
-    if (c + 4 <= D) {
-        E::load4(row + c, v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = c + j < D ? E::get(row[c + j]) : 0.f;
-    }
+// ---- sums and maxima over the lanes that share a row -----------------------------------------------------------------------
+// All of an aligned group of L lanes of a wavefront, L = 16, 32 or 64; every lane gets the same bits.  Lanes of 16 by DPP
+// (exchange with the neighbour, the pair, the mirrored eight, the mirrored sixteen), rows of 16 by the swaps of gfx950; no
+// LDS.
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf, 0xf, true));
 }
-template <typename E>
-__device__ __forceinline__ void row_store4(typename E::mem* row, int32_t c, int32_t D, const float* v) {
-    if (c + 4 <= D) {
-        E::store4(row + c, v);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (c + j < D) row[c + j] = E::put(v[j]);
+template <int L, typename F>
+__device__ __forceinline__ float wave_all(float v, F&& f) {
+    v = f(v, dpp<0xb1>(v));
+    v = f(v, dpp<0x4e>(v));
+    v = f(v, dpp<0x141>(v));
+    v = f(v, dpp<0x140>(v));
+    if constexpr (L > 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(s[0]), __uint_as_float(s[1]));
     }
-}
-
-// ---- sums over the L lanes that share a row ---------------------------------------------------------------------------
-// L <= 64: lanes of one wavefront; else the whole workgroup of L lanes, through `lds` (L / 64 floats).  Every lane gets the
-// same bits.
-template <int L>
-__device__ __forceinline__ float lanes_sum(float v, float* lds) {
-#pragma unroll
-    for (int off = (L < kWave ? L : kWave) / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
-    if (L > kWave) {
-        __syncthreads();  // lds may still be read by the sum before this one
-        if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = v;
-        __syncthreads();
-        v = 0.f;
-#pragma unroll
-        for (int w = 0; w < L / kWave; ++w) v += lds[w];
+    if constexpr (L > 32) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(s[0]), __uint_as_float(s[1]));
     }
     return v;
+}
+template <int L>
+__device__ __forceinline__ float wave_sum(float v) {
+    return wave_all<L>(v, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ float wave_max(float v) {
+    return wave_all<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// Sums of K values over L lanes; for L > 64 over the whole workgroup of L lanes, through `lds` (K * L / 64 floats), which no
+// lane may still be reading: two sums in a row need different ones.
+template <int L, int K>
+__device__ __forceinline__ void lanes_sum(float (&v)[K], float* lds) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = wave_sum<(L < kWave ? L : kWave)>(v[k]);
+    if constexpr (L > kWave) {
+        if ((threadIdx.x & (kWave - 1)) == 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) lds[threadIdx.x / kWave * K + k] = v[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] = lds[k];
+#pragma unroll
+            for (int w = 1; w < L / kWave; ++w) v[k] += lds[w * K + k];
+        }
+    }
 }
 
 // ---- dropout ---------------------------------------------------------------------------------------------------------
@@ -183,16 +218,24 @@ hipError_t launch_norm(const gpga_ctx* c, const RowsShape& s, const DropArgs& dr
 size_t norm_grad_scratch(const RowsShape& s);
 hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* dy, const void* u, const float* stats,
                             const void* more, int64_t gamma_off, int64_t beta_off, void* du, void* dx, bool accumulate, void* scratch);
-size_t token_loss_scratch(const RowsShape& s);
+size_t token_loss_scratch(const RowsShape& s, int num_cus);
 hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* logits, const int32_t* labels, float grad_scale, float* loss,
                              void* dlogits, void* scratch);
 
-// Calls f with a value of the element type that `dtype` names.
+// Calls f with a value of the kind of element that `dtype` names; the narrow kinds are for rows shorter than a piece.
 template <typename F>
 inline hipError_t with_elem(int32_t dtype, F&& f) {
     switch (dtype) {
-        case GPGA_F32: return f(ElemF32());
-        case GPGA_BF16: return f(ElemBF16());
-        default: return f(ElemF16());
+        case GPGA_F32: return f(Elem<float, false>());
+        case GPGA_BF16: return f(Elem<__bf16, false>());
+        default: return f(Elem<_Float16, false>());
+    }
+}
+template <typename F>
+inline hipError_t with_narrow_elem(int32_t dtype, F&& f) {
+    switch (dtype) {
+        case GPGA_F32: return f(Elem<float, true>());
+        case GPGA_BF16: return f(Elem<__bf16, true>());
+        default: return f(Elem<_Float16, true>());
     }
 }

@@ -6,143 +6,427 @@
 // The loss is a sum of two terms that are both at least 0: m is never added to the logarithm, so large logits cost no
 // digits.  A label of V or more is never an address: the loss of its node and its row of dz are NaN.  A node without a
 // counted token has loss 0 (NaN would spread to every node with the next gossip step).
+//
+// A row is read once: L lanes hold it as exp(z - m_lane) in fp32, m_lane the largest value of the lane, and one pass over
+// the lanes joins maxima and sums; the gradient is what is held times exp(m_lane - m) a / (N sum).  Few or very long rows are cut
+// into pieces for a workgroup each, and a second launch reads them again for the gradient.
 #include "gpga_rows.hpp"
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCountThreads = 256;
+constexpr float kLowest = -3.402823466e38f;  // stands for -inf as a maximum: -inf - kLowest is -inf and not NaN
+
+uint32_t blocks_for(int64_t items, int64_t per_block) { return (uint32_t)((items + per_block - 1) / per_block); }
 
 template <typename E>
 struct LossArgs {
     typedef typename E::mem mem;
     int32_t T, V;
     int64_t ld;
+    uint32_t per_node;     // workgroups of a node
     const mem* z;
     const int32_t* labels;
-    mem* dz;            // may be NULL
-    float* row_loss;    // n*T
-    const int32_t* count;  // n: counted tokens
+    mem* dz;               // may be NULL
+    float* row_loss;       // n*T
+    const int32_t* count;  // n: counted tokens; NULL: a workgroup counts the labels of its node itself
     float grad_scale;
+    uint32_t* left;        // counters, one a node, kLossLeftStride apart; NULL: k_loss_mean follows
+    float* loss;           // n
+    // rows in pieces
+    uint32_t pieces;       // of a row
+    int32_t piece;         // columns of one, a multiple of kOct * kThreads
+    float* parts;          // n*T x pieces pairs (maximum, sum)
 };
 
-__device__ __forceinline__ double wave_sum(double v) {
+__device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
     for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
     return v;
 }
 
-// Counted tokens of each node; a workgroup a node.
-__global__ __launch_bounds__(kCountThreads) void k_count(const int32_t* __restrict__ labels, int32_t T, int32_t* __restrict__ count) {
-    __shared__ int32_t s_count[kCountThreads / kWave];
+// Counted tokens among labels[0 .. T), by a workgroup of `threads`; `lds` one word a wavefront.  Holds a barrier.
+__device__ __forceinline__ int32_t count_labels(const int32_t* __restrict__ labels, int32_t T, int32_t threads, int32_t* lds) {
     int32_t mine = 0;
-    for (int32_t t = threadIdx.x; t < T; t += kCountThreads) mine += labels[(int64_t)blockIdx.x * T + t] >= 0;
-    for (int off = kWave / 2; off > 0; off >>= 1) mine += __shfl_xor(mine, off, kWave);
-    if ((threadIdx.x & (kWave - 1)) == 0) s_count[threadIdx.x / kWave] = mine;
+    for (int32_t t = threadIdx.x; t < T; t += threads) mine += __builtin_popcountll(__ballot(labels[t] >= 0));
+    if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = mine;  // its turns are those of the wavefront
+    __syncthreads();
+    mine = 0;
+    for (int32_t w = 0; w < threads / kWave; ++w) mine += lds[w];
+    return mine;
+}
+
+// loss = sum over the node's rows / counted tokens, by a workgroup of `threads`; double, a fixed order.  row(t) is the loss of row t.
+template <typename F>
+__device__ __forceinline__ void node_loss(int32_t T, int32_t threads, int32_t counted, double* lds, float* loss, F&& row) {
+    double mine = 0.0;
+    for (int32_t t = threadIdx.x; t < T; t += threads) mine += (double)row(t);
+    mine = wave_sum64(mine);
+    if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kCountThreads / kWave; ++w) mine += s_count[w];
-        count[blockIdx.x] = mine;
+        for (int32_t w = 1; w < threads / kWave; ++w) mine += lds[w];
+        *loss = counted > 0 ? (float)(mine / counted) : 0.f;
+    }
+}
+
+// Whether this workgroup is the last of its node, once what thread 0 stored for the others has arrived; said in *last, for after a
+// barrier.  The counter is 0 again for the next launch.
+__device__ __forceinline__ void note_end(uint32_t* left, uint32_t workgroups, int32_t* last) {
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    const bool is = __hip_atomic_fetch_add(left, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == workgroups - 1;
+    if (is) __hip_atomic_store(left, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *last = is;
+}
+
+__global__ __launch_bounds__(kThreads) void k_count(const int32_t* __restrict__ labels, int32_t T, int32_t* __restrict__ count) {
+    __shared__ int32_t s_count[kThreads / kWave];
+    const int32_t n = count_labels(labels + (int64_t)blockIdx.x * T, T, kThreads, s_count);
+    if (threadIdx.x == 0) count[blockIdx.x] = n;
+}
+
+__global__ __launch_bounds__(kThreads) void k_loss_mean(const float* __restrict__ row_loss, const int32_t* __restrict__ count, int32_t T,
+                                                        float* __restrict__ loss) {
+    __shared__ double s_sum[kThreads / kWave];
+    const float* rows = row_loss + (int64_t)blockIdx.x * T;
+    node_loss(T, kThreads, count[blockIdx.x], s_sum, loss + blockIdx.x, [&](int32_t t) { return rows[t]; });
+}
+
+// ---- rows held in registers: L lanes a row, N pieces of eight columns a lane ------------------------------------------------
+template <typename E, int L, int N>
+__global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossArgs<E> a) {
+    constexpr int kBlock = L > kThreads ? L : kThreads, kRows = kBlock / L, kWaves = kBlock / kWave, kRowWaves = L / kWave;
+    __shared__ float s_max[kWaves], s_sum[kWaves];
+    __shared__ int32_t s_count[kWaves], s_last;
+    __shared__ double s_total[kWaves];
+    const uint32_t node = blockIdx.x / a.per_node;
+    const int32_t t = (int32_t)((blockIdx.x - node * a.per_node) * kRows + threadIdx.x / L);
+    const int64_t r = (int64_t)node * a.T + t;
+    const int32_t lane = threadIdx.x & (L - 1);
+    const int32_t* labels = a.labels + (int64_t)node * a.T;
+    const int32_t label = t < a.T ? labels[t] : -1;
+    const typename E::mem* z = a.z + r * a.ld;
+    Piece<E, kOct> in[N];
+    float picked = 0.f;
+    const bool bad = label >= a.V;
+    if (label >= 0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) in[k] = piece_load<kOct, E>(z, (lane + k * L) * kOct, a.V);
+        picked = E::get(z[bad ? 0 : label]);
+    }
+    const int32_t counted = a.count ? a.count[node] : count_labels(labels, a.T, kBlock, s_count);
+    float e[N][kOct], mine = kLowest, sum = 0.f, top = 0.f, share = 1.f;
+    if (label >= 0) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int32_t c = (lane + k * L) * kOct;
+            piece_get<kOct, E>(in[k], c, a.V, e[k]);
+#pragma unroll
+            for (int j = 0; j < kOct; ++j) {
+                e[k][j] = c + j < a.V ? e[k][j] : -INFINITY;
+                mine = fmaxf(mine, e[k][j]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int j = 0; j < kOct; ++j) {
+                e[k][j] = __expf(e[k][j] - mine);
+                sum += e[k][j];
+            }
+        top = wave_max<kWave>(mine);
+        sum = wave_sum<kWave>(sum * __expf(mine - top));
+    }
+    if constexpr (L > kWave) {
+        if ((threadIdx.x & (kWave - 1)) == 0) {
+            s_max[threadIdx.x / kWave] = top;
+            s_sum[threadIdx.x / kWave] = sum;
+        }
+        __syncthreads();  // from here on dz may take the place of z
+        top = s_max[0];
+#pragma unroll
+        for (int w = 1; w < kRowWaves; ++w) top = fmaxf(top, s_max[w]);
+        sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) sum += s_sum[w] * __expf(s_max[w] - top);
+    }
+    if (lane == 0 && t < a.T) {
+        const float loss = label < 0 ? 0.f : bad ? __builtin_nanf("") : logf(sum) + (top - picked);
+        __hip_atomic_store(a.row_loss + r, loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (a.left) {
+        if (kRows > 1) {
+            asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+            __syncthreads();
+        }
+        if (threadIdx.x == 0) note_end(a.left + (int64_t)node * kLossLeftStride, a.per_node, &s_last);
+    }
+    if (a.dz && t < a.T) {
+        typename E::mem* dz = a.dz + r * a.ld;
+        if (label < 0) {
+            const float zero[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int32_t c = (lane + k * L) * kOct;
+                if (c < a.V) piece_put<kOct, E>(dz, c, a.V, zero);
+            }
+        } else {
+            const float scale = bad ? __builtin_nanf("") : a.grad_scale / (float)counted;
+            share = __expf(mine - top) * (scale / sum);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int32_t c = (lane + k * L) * kOct;
+                if (c < a.V) {
+#pragma unroll
+                    for (int j = 0; j < kOct; ++j) e[k][j] = e[k][j] * share - (c + j == label ? scale : 0.f);
+                    piece_put<kOct, E>(dz, c, a.V, e[k]);
+                }
+            }
+        }
+    }
+    if (a.left) {
+        __syncthreads();
+        if (s_last)
+            node_loss(a.T, kBlock, counted, s_total, a.loss + node, [&](int32_t k) {
+                return __hip_atomic_load(a.row_loss + (int64_t)node * a.T + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            });
+    }
+}
+
+// ---- rows in pieces: a workgroup for each ------------------------------------------------------------------------------------
+// Maximum and sum of exp(z - maximum) of a row from those of its pieces, by a wavefront; all lanes get them.
+struct MaxSum {
+    float top, sum;
+};
+__device__ __forceinline__ MaxSum join_parts(const float* parts, uint32_t pieces) {
+    const uint32_t lane = threadIdx.x & (kWave - 1);
+    auto part = [&](uint32_t k) { return __hip_atomic_load(parts + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+    MaxSum mine = {kLowest, 0.f}, all;
+    for (uint32_t k = lane; k < pieces; k += kWave) {
+        const float top = part(2 * k), sum = part(2 * k + 1), most = fmaxf(mine.top, top);
+        mine.sum = mine.sum * __expf(mine.top - most) + sum * __expf(top - most);
+        mine.top = most;
+    }
+    all.top = wave_max<kWave>(mine.top);
+    all.sum = wave_sum<kWave>(mine.sum * __expf(mine.top - all.top));
+    return all;
+}
+
+// Loss of a node whose rows are in pieces, by a workgroup: a wavefront a row in turn.
+template <typename E>
+__device__ __forceinline__ void node_loss_parts(const LossArgs<E>& a, uint32_t node, int32_t* s_count, double* s_total) {
+    constexpr int kWaves = kThreads / kWave;
+    const int64_t first = (int64_t)node * a.T;
+    const int32_t counted = count_labels(a.labels + first, a.T, kThreads, s_count), wave = threadIdx.x / kWave;
+    double mine = 0.0;
+    for (int32_t t = wave; t < a.T; t += kWaves) {
+        const int64_t r = first + t;
+        const int32_t label = a.labels[r];
+        if (label < 0) continue;
+        const MaxSum all = join_parts(a.parts + r * 2 * a.pieces, a.pieces);
+        mine += label >= a.V ? (double)__builtin_nanf("") : (double)(logf(all.sum) + (all.top - E::get(a.z[r * a.ld + label])));
+    }
+    if ((threadIdx.x & (kWave - 1)) == 0) s_total[wave] = mine;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kWaves; ++w) mine += s_total[w];
+        a.loss[node] = counted > 0 ? (float)(mine / counted) : 0.f;
     }
 }
 
 template <typename E>
-__global__ __launch_bounds__(kThreads) void k_token_loss(LossArgs<E> a) {
-    __shared__ float s_max[kThreads / kWave], s_sum[kThreads / kWave];
-    const int64_t r = blockIdx.x;
-    const int32_t label = a.labels[r];
-    const typename E::mem* z = a.z + r * a.ld;
-    typename E::mem* dz = a.dz ? a.dz + r * a.ld : nullptr;
-    if (label < 0) {
-        if (threadIdx.x == 0) a.row_loss[r] = 0.f;
-        if (dz) {
-            const float zero[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            for (int32_t c = threadIdx.x * kOct; c < a.V; c += kThreads * kOct) row_store<E>(dz, c, a.V, zero);
+__global__ __launch_bounds__(kThreads) void k_loss_parts(LossArgs<E> a) {
+    constexpr int kWaves = kThreads / kWave;
+    __shared__ float s_max[kWaves], s_sum[kWaves];
+    __shared__ int32_t s_count[kWaves], s_last;
+    __shared__ double s_total[kWaves];
+    const int64_t r = blockIdx.x / a.pieces;
+    const uint32_t node = (uint32_t)(r / a.T), piece = blockIdx.x - (uint32_t)r * a.pieces;
+    if (a.labels[r] >= 0) {
+        const int32_t from = (int32_t)piece * a.piece, to = a.V - from < a.piece ? a.V : from + a.piece;
+        const typename E::mem* z = a.z + r * a.ld;
+        float top = kLowest, sum = 0.f;
+        for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) {
+            float v[kOct], most = top;
+            piece_read<kOct, E>(z, c, a.V, v);
+#pragma unroll
+            for (int j = 0; j < kOct; ++j) {
+                v[j] = c + j < a.V ? v[j] : -INFINITY;
+                most = fmaxf(most, v[j]);
+            }
+            sum *= __expf(top - most);
+            top = most;
+#pragma unroll
+            for (int j = 0; j < kOct; ++j) sum += __expf(v[j] - top);
         }
+        float all = wave_max<kWave>(top);
+        sum = wave_sum<kWave>(sum * __expf(top - all));
+        if ((threadIdx.x & (kWave - 1)) == 0) {
+            s_max[threadIdx.x / kWave] = all;
+            s_sum[threadIdx.x / kWave] = sum;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < kWaves; ++w) all = fmaxf(all, s_max[w]);
+            sum = 0.f;
+            for (int w = 0; w < kWaves; ++w) sum += s_sum[w] * __expf(s_max[w] - all);
+            float* part = a.parts + (r * a.pieces + piece) * 2;
+            __hip_atomic_store(part, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(part + 1, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    if (!a.left) return;  // k_loss_join follows
+    if (threadIdx.x == 0) note_end(a.left + (int64_t)node * kLossLeftStride, a.per_node, &s_last);
+    __syncthreads();
+    if (!s_last) return;
+    node_loss_parts<E>(a, node, s_count, s_total);
+}
+
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_loss_join(LossArgs<E> a) {
+    __shared__ int32_t s_count[kThreads / kWave];
+    __shared__ double s_total[kThreads / kWave];
+    node_loss_parts<E>(a, blockIdx.x, s_count, s_total);
+}
+
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_loss_parts_grad(LossArgs<E> a) {
+    __shared__ int32_t s_count[kThreads / kWave];
+    const int64_t r = blockIdx.x / a.pieces;
+    const uint32_t node = (uint32_t)(r / a.T), piece = blockIdx.x - (uint32_t)r * a.pieces;
+    const int32_t label = a.labels[r];
+    const int32_t from = (int32_t)piece * a.piece, to = a.V - from < a.piece ? a.V : from + a.piece;
+    const typename E::mem* z = a.z + r * a.ld;
+    typename E::mem* dz = a.dz + r * a.ld;
+    float v[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (label < 0) {
+        for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) piece_put<kOct, E>(dz, c, a.V, v);
         return;
     }
-    const int64_t node = r / a.T;
-    float top = -INFINITY, v[kOct];
-    bool nan = false;
-    for (int32_t c = threadIdx.x * kOct; c < a.V; c += kThreads * kOct) {
-        row_load<E>(z, c, a.V, v, -INFINITY);
+    const int32_t counted = a.count ? a.count[node] : count_labels(a.labels + (int64_t)node * a.T, a.T, kThreads, s_count);
+    const MaxSum all = join_parts(a.parts + r * 2 * a.pieces, a.pieces);
+    const float scale = label >= a.V ? __builtin_nanf("") : a.grad_scale / (float)counted, share = scale / all.sum;
+    for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) {
+        piece_read<kOct, E>(z, c, a.V, v);
 #pragma unroll
-        for (int j = 0; j < kOct; ++j) {
-            top = fmaxf(top, v[j]);
-            nan |= v[j] != v[j];
-        }
-    }
-#pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-    if ((threadIdx.x & (kWave - 1)) == 0) s_max[threadIdx.x / kWave] = top;
-    __syncthreads();
-    for (int w = 0; w < kThreads / kWave; ++w) top = fmaxf(top, s_max[w]);
-    float sum = nan ? __builtin_nanf("") : 0.f;
-    for (int32_t c = threadIdx.x * kOct; c < a.V; c += kThreads * kOct) {
-        row_load<E>(z, c, a.V, v, -INFINITY);
-#pragma unroll
-        for (int j = 0; j < kOct; ++j) sum += c + j < a.V ? __expf(v[j] - top) : 0.f;
-    }
-    sum = lanes_sum<kThreads>(sum, s_sum);
-    const bool bad = label >= a.V;
-    const float picked = E::get(z[bad ? 0 : label]);
-    __syncthreads();  // dz may take the place of z
-    if (threadIdx.x == 0) a.row_loss[r] = bad ? __builtin_nanf("") : logf(sum) + (top - picked);
-    if (!dz) return;
-    const float scale = bad ? __builtin_nanf("") : a.grad_scale / (float)a.count[node];
-    const float part = scale / sum;
-    for (int32_t c = threadIdx.x * kOct; c < a.V; c += kThreads * kOct) {
-        row_load<E>(z, c, a.V, v);
-#pragma unroll
-        for (int j = 0; j < kOct; ++j) v[j] = __expf(v[j] - top) * part - (c + j == label ? scale : 0.f);
-        row_store<E>(dz, c, a.V, v);
+        for (int j = 0; j < kOct; ++j) v[j] = __expf(v[j] - all.top) * share - (c + j == label ? scale : 0.f);
+        piece_put<kOct, E>(dz, c, a.V, v);
     }
 }
 
-// Mean over the counted tokens of each node; sums in double, a fixed order.
-__global__ __launch_bounds__(kCountThreads) void k_loss_mean(const float* __restrict__ row_loss, const int32_t* __restrict__ count, int32_t T,
-                                                             float* __restrict__ loss) {
-    __shared__ double s_sum[kCountThreads / kWave];
-    double mine = 0.0;
-    for (int32_t t = threadIdx.x; t < T; t += kCountThreads) mine += (double)row_loss[(int64_t)blockIdx.x * T + t];
-    mine = wave_sum(mine);
-    if ((threadIdx.x & (kWave - 1)) == 0) s_sum[threadIdx.x / kWave] = mine;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kCountThreads / kWave; ++w) mine += s_sum[w];
-        const int32_t n = count[blockIdx.x];
-        loss[blockIdx.x] = n > 0 ? (float)(mine / n) : 0.f;
-    }
+template <int V>
+struct Const {
+    static constexpr int value = V;
+};
+// Lanes a row and pieces a lane by the number of eights in it: the smallest that hold it.
+template <typename E, typename F>
+bool with_row_shape(int32_t octs, F&& f) {
+    if constexpr (E::kNarrow) f(Const<64>(), Const<1>());
+    else if (octs <= 64) f(Const<64>(), Const<1>());
+    else if (octs <= 128) f(Const<64>(), Const<2>());
+    else if (octs <= 256) f(Const<64>(), Const<4>());
+    else if (octs <= 512) f(Const<256>(), Const<2>());
+    else if (octs <= 1024) f(Const<256>(), Const<4>());
+    else if (octs <= 2048) f(Const<1024>(), Const<2>());
+    else if (octs <= 4096) f(Const<1024>(), Const<4>());
+    else if (octs <= 8192) f(Const<1024>(), Const<8>());
+    else return false;
+    return true;
 }
+
+// Rows are cut into pieces where no workgroup holds one, and where there are fewer long rows than compute units.
+constexpr int32_t kPieceUnit = kOct * kThreads;
+struct Cut {
+    uint32_t pieces = 0;  // 0: rows are held
+    int32_t piece = 0;
+    Cut(const RowsShape& s, int num_cus) {
+        const int64_t rows = (int64_t)s.n * s.T;
+        if (s.D <= 65536 && !(s.D > 8192 && rows < num_cus)) return;
+        const int64_t units = ((int64_t)s.D + kPieceUnit - 1) / kPieceUnit, wanted = rows < 4 * num_cus ? 4 * num_cus / (rows > 0 ? rows : 1) : 1;
+        const int64_t each = wanted < units ? units / wanted : 1;
+        piece = (int32_t)(each * kPieceUnit < s.D ? each * kPieceUnit : s.D);
+        pieces = (uint32_t)(((int64_t)s.D + piece - 1) / piece);
+    }
+};
 
 }  // namespace
 
-size_t token_loss_scratch(const RowsShape& s) { return ((size_t)s.n * (size_t)s.T + (size_t)s.n) * 4; }
+size_t token_loss_scratch(const RowsShape& s, int num_cus) {
+    const Cut cut(s, num_cus);
+    return ((size_t)s.n * (size_t)s.T * (cut.pieces ? 2 * cut.pieces : 1) + (size_t)s.n) * 4;
+}
 
 hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* logits, const int32_t* labels, float grad_scale, float* loss,
                              void* dlogits, void* scratch) {
+    const Cut cut(s, c->num_cus);
     int32_t* count = static_cast<int32_t*>(scratch);
-    float* row_loss = reinterpret_cast<float*>(count + s.n);
-    k_count<<<dim3((uint32_t)s.n), dim3(kCountThreads), 0, c->stream>>>(labels, s.T, count);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && s.T > 0) {
-        e = with_elem(s.dtype, [&](auto el) {
-            typedef decltype(el) E;
-            LossArgs<E> a = {};
-            a.T = s.T;
-            a.V = s.D;
-            a.ld = s.ld;
-            a.z = static_cast<const typename E::mem*>(logits);
-            a.labels = labels;
-            a.dz = static_cast<typename E::mem*>(dlogits);
-            a.row_loss = row_loss;
-            a.count = count;
-            a.grad_scale = grad_scale;
-            k_token_loss<E><<<dim3((uint32_t)s.n * (uint32_t)s.T), dim3(kThreads), 0, c->stream>>>(a);
+    float* rows = reinterpret_cast<float*>(count + s.n);
+    // the launch's last workgroup of a node adds up its losses, unless so many end there that they would queue for the counter
+    constexpr int64_t kMostAtCounter = 2048;
+    auto counter = [&](int64_t per_node) { return c->loss_left && s.n <= 65535 && per_node <= kMostAtCounter ? c->loss_left : nullptr; };
+    auto count_launch = [&]() {
+        k_count<<<dim3((uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(labels, s.T, count);
+        return hipGetLastError();
+    };
+    auto launch = [&](auto el) {
+        typedef decltype(el) E;
+        LossArgs<E> a = {};
+        a.T = s.T;
+        a.V = s.D;
+        a.ld = s.ld;
+        a.z = static_cast<const typename E::mem*>(logits);
+        a.labels = labels;
+        a.dz = static_cast<typename E::mem*>(dlogits);
+        a.grad_scale = grad_scale;
+        a.loss = loss;
+        const uint32_t all = (uint32_t)s.n * (uint32_t)s.T;
+        if (cut.pieces) {
+            if constexpr (!E::kNarrow) {
+                a.pieces = cut.pieces;
+                a.piece = cut.piece;
+                a.parts = rows;
+                a.per_node = (uint32_t)s.T * cut.pieces;
+                a.left = counter((int64_t)s.T * cut.pieces);
+                k_loss_parts<E><<<dim3(all * cut.pieces), dim3(kThreads), 0, c->stream>>>(a);
+                hipError_t e = hipGetLastError();
+                if (e == hipSuccess && !a.left) {
+                    k_loss_join<E><<<dim3((uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a);
+                    e = hipGetLastError();
+                }
+                if (e != hipSuccess || !a.dz) return e;
+                if (s.T > 4 * kThreads) {
+                    a.count = count;
+                    e = count_launch();
+                    if (e != hipSuccess) return e;
+                }
+                k_loss_parts_grad<E><<<dim3(all * cut.pieces), dim3(kThreads), 0, c->stream>>>(a);
+            }
             return hipGetLastError();
+        }
+        a.row_loss = rows;
+        hipError_t e = hipSuccess;
+        with_row_shape<E>((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
+            constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
+            a.per_node = blocks_for(s.T, kBlock / L);
+            a.left = counter(a.per_node);
+            // the labels of a node are counted beside the loads of a row where they are few to its columns
+            if (!a.left || s.T > 4 * L) {
+                a.count = count;
+                e = count_launch();
+            }
+            if (e != hipSuccess) return;
+            k_loss_held<E, L, N><<<dim3(a.per_node * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
+            e = hipGetLastError();
         });
+        if (e != hipSuccess || a.left) return e;
+        k_loss_mean<<<dim3((uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(rows, count, s.T, loss);
+        return hipGetLastError();
+    };
+    if (s.T == 0) {  // losses of 0
+        const hipError_t e = count_launch();
+        if (e != hipSuccess) return e;
+        k_loss_mean<<<dim3((uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(rows, count, 0, loss);
+        return hipGetLastError();
     }
-    if (e != hipSuccess) return e;
-    k_loss_mean<<<dim3((uint32_t)s.n), dim3(kCountThreads), 0, c->stream>>>(row_loss, count, s.T, loss);
-    return hipGetLastError();
+    return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }
