@@ -325,8 +325,12 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a) {
     if (key != keys[next] || key >= (uint32_t)a.V || out_of_range(keys, a)) return;
     const bool from_first = keys[first] == key;
     if (from_first && chunk && keys[first - 1] == key) return;  // begins earlier
-    const uint32_t parts = (uint32_t)(keys_below(keys + next, a.T - next, key + 1u) + kRun - 1) / kRun + 1;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    uint32_t parts = 1;  // this chunk's and those of the chunks that begin with the row
+    for (uint64_t same = ~0ull; same == ~0ull; parts += (uint32_t)__builtin_popcountll(same)) {
+        const int64_t at = first + (int64_t)(parts + lane) * kRun;
+        same = __ballot(at < a.T && keys[at < a.T ? at : 0] == key);
+    }
     const int32_t c = (int32_t)(blockIdx.x - unit * a.column_blocks) * kTurnCols + lane * 4;
     const uint32_t share = (parts + kWaves - 1) / kWaves;
     const uint32_t from = wave * share, to = from + share < parts ? from + share : parts;

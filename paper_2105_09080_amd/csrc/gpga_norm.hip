@@ -65,6 +65,12 @@ __global__ __launch_bounds__(kThreads) void k_dropout(NormArgs<E> a, int lanes_l
     }
 }
 
+// What columns past the end of the row hold.
+__device__ __forceinline__ void past_end(float* v, int32_t c, int32_t D, float value) {
+#pragma unroll
+    for (int j = 0; j < kOct; ++j) v[j] = c + j < D ? v[j] : value;
+}
+
 // u of eight columns, before rounding.
 template <typename E>
 __device__ __forceinline__ void norm_input(const NormArgs<E>& a, const DropNode& mask, const Piece<E, kOct>& x, const Piece<E, kOct>& side,
@@ -114,16 +120,18 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm(NormArgs<E
     for (int k = 0; k < N; ++k) {
         const int32_t q = lane + k * L, c = q * kOct;
         norm_input<E>(a, mask, x[k], side[k], (uint32_t)t * octs + q, c, u[k]);
+        if (c + kOct > a.D) past_end(u[k], c, a.D, 0.f);
 #pragma unroll
-        for (int j = 0; j < kOct; ++j) sum[0] += c + j < a.D ? u[k][j] : 0.f;
+        for (int j = 0; j < kOct; ++j) sum[0] += u[k][j];
     }
     lanes_sum<L>(sum, s_sum[0]);
     const float inv = 1.f / (float)a.D, mean = sum[0] * inv;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int32_t c = (lane + k * L) * kOct;
+        if (c + kOct > a.D) past_end(u[k], c, a.D, mean);
 #pragma unroll
-        for (int j = 0; j < kOct; ++j) var[0] += c + j < a.D ? (u[k][j] - mean) * (u[k][j] - mean) : 0.f;
+        for (int j = 0; j < kOct; ++j) var[0] += (u[k][j] - mean) * (u[k][j] - mean);
     }
     lanes_sum<L>(var, s_sum[1]);
     const float rstd = 1.f / sqrtf(var[0] * inv + a.eps);
@@ -211,9 +219,10 @@ __device__ __forceinline__ void grad_input(const Piece<E, kOct>& dy_in, const Pi
     piece_get<kOct, E>(dy_in, c, D, dy);
     piece_get<kOct, E>(u_in, c, D, xh);
 #pragma unroll
-    for (int j = 0; j < kOct; ++j) {
-        xh[j] = c + j < D ? (xh[j] - mean) * rstd : 0.f;
-        dy[j] = c + j < D ? dy[j] : 0.f;
+    for (int j = 0; j < kOct; ++j) xh[j] = (xh[j] - mean) * rstd;
+    if (c + kOct > D) {
+        past_end(dy, c, D, 0.f);
+        past_end(xh, c, D, 0.f);
     }
 }
 // du and dx of eight columns.

@@ -92,6 +92,17 @@ __global__ __launch_bounds__(kThreads) void k_loss_mean(const float* __restrict_
     node_loss(T, kThreads, count[blockIdx.x], s_sum, loss + blockIdx.x, [&](int32_t t) { return rows[t]; });
 }
 
+// Columns past the end of the row take no part.
+__device__ __forceinline__ void past_end(float* v, int32_t c, int32_t V) {
+#pragma unroll
+    for (int j = 0; j < kOct; ++j) v[j] = c + j < V ? v[j] : -INFINITY;
+}
+// v[at] -= by
+__device__ __forceinline__ void less_at(float* v, int32_t at, float by) {
+#pragma unroll
+    for (int j = 0; j < kOct; ++j) v[j] -= j == at ? by : 0.f;
+}
+
 // ---- rows held in registers: L lanes a row, N pieces of eight columns a lane ------------------------------------------------
 template <typename E, int L, int N>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossArgs<E> a) {
@@ -121,11 +132,9 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
         for (int k = 0; k < N; ++k) {
             const int32_t c = (lane + k * L) * kOct;
             piece_get<kOct, E>(in[k], c, a.V, e[k]);
+            if (c + kOct > a.V) past_end(e[k], c, a.V);
 #pragma unroll
-            for (int j = 0; j < kOct; ++j) {
-                e[k][j] = c + j < a.V ? e[k][j] : -INFINITY;
-                mine = fmaxf(mine, e[k][j]);
-            }
+            for (int j = 0; j < kOct; ++j) mine = fmaxf(mine, e[k][j]);
         }
 #pragma unroll
         for (int k = 0; k < N; ++k)
@@ -178,7 +187,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
                 const int32_t c = (lane + k * L) * kOct;
                 if (c < a.V) {
 #pragma unroll
-                    for (int j = 0; j < kOct; ++j) e[k][j] = e[k][j] * share - (c + j == label ? scale : 0.f);
+                    for (int j = 0; j < kOct; ++j) e[k][j] *= share;
+                    if ((uint32_t)(label - c) < kOct) less_at(e[k], label - c, scale);
                     piece_put<kOct, E>(dz, c, a.V, e[k]);
                 }
             }
@@ -249,11 +259,9 @@ __global__ __launch_bounds__(kThreads) void k_loss_parts(LossArgs<E> a) {
         for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) {
             float v[kOct], most = top;
             piece_read<kOct, E>(z, c, a.V, v);
+            if (c + kOct > a.V) past_end(v, c, a.V);
 #pragma unroll
-            for (int j = 0; j < kOct; ++j) {
-                v[j] = c + j < a.V ? v[j] : -INFINITY;
-                most = fmaxf(most, v[j]);
-            }
+            for (int j = 0; j < kOct; ++j) most = fmaxf(most, v[j]);
             sum *= __expf(top - most);
             top = most;
 #pragma unroll
@@ -309,7 +317,8 @@ __global__ __launch_bounds__(kThreads) void k_loss_parts_grad(LossArgs<E> a) {
     for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) {
         piece_read<kOct, E>(z, c, a.V, v);
 #pragma unroll
-        for (int j = 0; j < kOct; ++j) v[j] = __expf(v[j] - all.top) * share - (c + j == label ? scale : 0.f);
+        for (int j = 0; j < kOct; ++j) v[j] = __expf(v[j] - all.top) * share;
+        if ((uint32_t)(label - c) < kOct) less_at(v, label - c, scale);
         piece_put<kOct, E>(dz, c, a.V, v);
     }
 }

@@ -9,6 +9,14 @@ import torch
 from . import binding as B
 
 
+def _current_stream(index: int) -> int:
+    """Address of torch's current stream on a device."""
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# the same without building a Stream object (0.1 us for 2), where this torch has it
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
+
 _DTYPE = {torch.float32: B.GPGA_F32, torch.bfloat16: B.GPGA_BF16, torch.float16: B.GPGA_F16}
 
 
@@ -29,6 +37,7 @@ class Simulation:
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._device_index, self._stream_address = self.stream.device.index, self.stream.cuda_stream
         self.ctx = B.gpga_create(n, d, topology, H, lr, momentum)
         with torch.cuda.stream(self.stream):
             self._bufs = [torch.empty((n, self.ld), dtype=torch.float32, device=self.device) for _ in range(2)]
@@ -179,15 +188,26 @@ class Simulation:
     # Activations are (n, T, D) tensors whose tokens lie a common number of elements apart (rows of a wider tensor are
     # fine); parameters are named by their column offset in X, their gradients land in the same columns of G.  What the
     # calls return is allocated for, and written on, the simulation's stream.
-    def _empty(self, shape, dtype, ld: int | None = None):
-        """Memory of the simulation's stream; rows ``ld`` elements apart if that is more than the last dimension."""
-        width = shape[-1] if ld is None else ld
-        if torch.cuda.current_stream(self.device) == self.stream:
-            t = torch.empty((*shape[:-1], width), dtype=dtype, device=self.device)
-        else:
+    def _foreign(self) -> bool:
+        """Whether torch's current stream is another one than the simulation's."""
+        return _current_stream(self._device_index) != self._stream_address
+
+    def _empty(self, shape, dtype, foreign: bool):
+        """Memory of the simulation's stream."""
+        if not foreign:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _like(self, x: torch.Tensor, ld: int, foreign: bool):
+        """Memory for activations beside ``x``: rows as far apart."""
+        if foreign:
             with torch.cuda.stream(self.stream):
-                t = torch.empty((*shape[:-1], width), dtype=dtype, device=self.device)
-        return t if width == shape[-1] else t[..., : shape[-1]]
+                return self._like(x, ld, False)
+        if x.is_contiguous():
+            return torch.empty_like(x)
+        n, T, D = x.shape
+        return torch.empty((n, T, ld), dtype=x.dtype, device=self.device)[..., :D]
 
     def _tokens(self, t: torch.Tensor) -> int:
         """Tokens a node of an (n, T) int32 tensor."""
@@ -197,34 +217,37 @@ class Simulation:
 
     def _rows(self, first: torch.Tensor, *others):
         """(T, D, ld, dtype) of activations of one call."""
-        if first.dim() != 3 or first.shape[0] != self.n or first.dtype not in _DTYPE or not first.is_cuda:
-            raise ValueError(f"expected an (n = {self.n}, T, D) fp32, bf16 or fp16 tensor on the GPU, got {tuple(first.shape)} {first.dtype}")
-        _, T, D = first.shape
-        ld = first.stride(1) if T > 1 else first.stride(0) if self.n > 1 else D
+        shape, dtype = first.shape, first.dtype
+        if len(shape) != 3 or shape[0] != self.n or dtype not in _DTYPE or not first.is_cuda:
+            raise ValueError(f"expected an (n = {self.n}, T, D) fp32, bf16 or fp16 tensor on the GPU, got {tuple(shape)} {dtype}")
+        n, T, D = shape
+        ld = D if first.is_contiguous() else first.stride(1) if T > 1 else first.stride(0) if n > 1 else D
         for t in (first, *others):
             if t is None:
                 continue
-            if t.shape != first.shape or t.dtype != first.dtype or t.device != first.device:
+            if t.shape != shape or t.dtype != dtype or t.device != first.device:
                 raise ValueError("the activations of a call differ in shape, type or device")
+            if ld == D and t.is_contiguous():
+                continue
             if t.numel() and (ld < D or (D > 1 and t.stride(2) != 1) or (T > 1 and t.stride(1) != ld) or
-                              (self.n > 1 and t.stride(0) != T * ld)):
+                              (n > 1 and t.stride(0) != T * ld)):
                 raise ValueError("the activations of a call need rows that are dense and a common number of elements apart")
-        return T, D, max(ld, D), _DTYPE[first.dtype]
+        return T, D, max(ld, D), _DTYPE[dtype]
 
     def _used(self, *tensors):
         """Memory that another stream allocated is not handed out again before this stream is through with it."""
-        if torch.cuda.current_stream(self.device) != self.stream:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.stream)
 
     def embed(self, tokens: torch.Tensor, table_off: int, V: int, D: int, *, scale: float = 1.0,
               dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """scale * E_i[tokens]: (n, T, D); tokens below 0 give zeros."""
-        T = self._tokens(tokens)
-        y = self._empty((self.n, T, D), dtype)
+        T, foreign = self._tokens(tokens), self._foreign()
+        y = self._empty((self.n, T, D), dtype, foreign)
         B.gpga_embed(self.ctx, tokens, T, table_off, V, D, scale, y, D, _DTYPE[dtype])
-        self._used(tokens)
+        if foreign:
+            self._used(tokens)
         return y
 
     def embed_grad(self, tokens: torch.Tensor, dy: torch.Tensor, table_off: int, V: int, *, scale: float = 1.0,
@@ -234,43 +257,49 @@ class Simulation:
         if self._tokens(tokens) != T:
             raise ValueError("tokens and dy differ in their tokens a node")
         B.gpga_embed_grad(self.ctx, tokens, T, table_off, V, D, scale, dy, ld, dt, accumulate)
-        self._used(tokens, dy)
+        if self._foreign():
+            self._used(tokens, dy)
 
     def dropout(self, x: torch.Tensor, p: float, *, seed: int, layer: int = 0, residual: torch.Tensor | None = None,
                 out: torch.Tensor | None = None) -> torch.Tensor:
         """residual + mask * x / (1 - p), the mask that of iteration k; with x = a gradient, its backward pass."""
         T, D, ld, dt = self._rows(x, residual, out)
-        y = self._empty((self.n, T, D), x.dtype, ld=ld) if out is None else out
+        foreign = self._foreign()
+        y = self._like(x, ld, foreign) if out is None else out
         B.gpga_dropout(self.ctx, x, residual, T, D, ld, dt, p, seed, layer, y)
-        self._used(x, residual, out)
+        if foreign:
+            self._used(x, residual, out)
         return y
 
     def layer_norm(self, x: torch.Tensor, gamma_off: int, beta_off: int, *, eps: float = 1e-5,
                    residual: torch.Tensor | None = None, p: float = 0.0, seed: int = 0, layer: int = 0):
         """(y, u, stats): layer norm y of u = residual + dropout(x); u is x itself where there is neither."""
         T, D, ld, dt = self._rows(x, residual)
-        y = self._empty((self.n, T, D), x.dtype, ld=ld)
+        foreign = self._foreign()
         plain = residual is None and p == 0.0
-        u = x if plain else self._empty((self.n, T, D), x.dtype, ld=ld)
-        stats = self._empty((self.n, T, 2), torch.float32)
-        B.gpga_layer_norm(self.ctx, x, residual, T, D, ld, dt, p, seed, layer, gamma_off, beta_off, eps,
-                          None if plain else u, y, stats)
-        self._used(x, residual)
-        return y, u, stats
+        y = self._like(x, ld, foreign)
+        u = None if plain else self._like(x, ld, foreign)
+        stats = self._empty((self.n, T, 2), torch.float32, foreign)
+        B.gpga_layer_norm(self.ctx, x, residual, T, D, ld, dt, p, seed, layer, gamma_off, beta_off, eps, u, y, stats)
+        if foreign:
+            self._used(x, residual)
+        return y, x if plain else u, stats
 
     def layer_norm_grad(self, dy: torch.Tensor, u: torch.Tensor, stats: torch.Tensor, gamma_off: int, beta_off: int, *,
                         p: float = 0.0, seed: int = 0, layer: int = 0, more: torch.Tensor | None = None,
                         accumulate: bool = False):
         """(du, dx): gradients of the residual and of x; those of gamma and beta land in G.  dx is du where p is 0."""
         T, D, ld, dt = self._rows(dy, u, more)
-        if stats.dtype != torch.float32 or tuple(stats.shape) != (self.n, T, 2) or not stats.is_contiguous():
+        if stats.dtype != torch.float32 or stats.shape != (self.n, T, 2) or not stats.is_contiguous() or not stats.is_cuda:
             raise ValueError("stats are the (n, T, 2) fp32 pairs that layer_norm returns")
-        du = self._empty((self.n, T, D), dy.dtype, ld=ld)
-        drops = int(float(np.float32(p)) * 65536 + 0.5) > 0     # p as the library keeps it
-        dx = self._empty((self.n, T, D), dy.dtype, ld=ld) if drops else None
+        foreign = self._foreign()
+        du = self._like(dy, ld, foreign)
+        drops = p != 0.0 and int(float(np.float32(p)) * 65536 + 0.5) > 0     # p as the library keeps it
+        dx = self._like(dy, ld, foreign) if drops else None
         B.gpga_layer_norm_grad(self.ctx, dy, u, stats, more, T, D, ld, dt, p, seed, layer, gamma_off, beta_off, du, dx,
                                accumulate)
-        self._used(dy, u, stats, more)
+        if foreign:
+            self._used(dy, u, stats, more)
         return du, du if dx is None else dx
 
     def token_loss(self, logits: torch.Tensor, labels: torch.Tensor, *, grad=True, grad_scale: float = 1.0):
@@ -280,10 +309,12 @@ class Simulation:
         T, V, ld, dt = self._rows(logits, into)
         if self._tokens(labels) != T:
             raise ValueError("labels and logits differ in their tokens a node")
-        loss = self._empty((self.n,), torch.float32)
-        dlogits = into if into is not None else self._empty((self.n, T, V), logits.dtype, ld=ld) if grad else None
+        foreign = self._foreign()
+        loss = self._empty((self.n,), torch.float32, foreign)
+        dlogits = into if into is not None else self._like(logits, ld, foreign) if grad else None
         B.gpga_token_loss(self.ctx, logits, labels, T, V, ld, dt, grad_scale, loss, dlogits)
-        self._used(logits, labels, into)
+        if foreign:
+            self._used(logits, labels, into)
         return loss, dlogits
 
     def tune(self, launches: int = 16):
