@@ -401,7 +401,8 @@ gpga_status gpga_embed(gpga_ctx* ctx, const int32_t* tokens_dev, int32_t T, int6
                        float scale, void* y_dev, int64_t ld, int32_t dtype);
 /* The gradient of that table: dE_i[v,:] = scale * sum of dy[i,t,:] over the t with tokens[i,t] = v (added in the order
  * of t; 0 where there is none), into columns table_off .. of row i of g_dev.  Padding takes no part; a token of V or
- * more makes the block of its node NaN.  With accumulate = 1 only rows of tokens that occur are touched.  n*V < 2^31. */
+ * more makes the block of its node NaN.  With accumulate = 1 only rows of tokens that occur are touched.
+ * n*V*D < 10^12. */
 gpga_status gpga_embed_grad(gpga_ctx* ctx, const int32_t* tokens_dev, int32_t T, int64_t table_off, int32_t V, int32_t D,
                             float scale, const void* dy_dev, int64_t ld, int32_t dtype, int32_t accumulate);
 

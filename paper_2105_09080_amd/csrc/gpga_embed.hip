@@ -19,7 +19,7 @@ constexpr int kTurns = 3;
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_embed(const int32_t* __restrict__ tokens, const float* __restrict__ table, int64_t ldx,
                                                     int32_t V, int32_t D, int32_t T, uint32_t blocks_per_node, int lanes_log2, float scale,
-                                                    typename E::mem* __restrict__ y, int64_t ld) {
+                                                    typename E::mem* __restrict__ y, int64_t ld, bool stream) {
     typedef Elem<float, E::kNarrow> P;
     const uint32_t node = blockIdx.x / blocks_per_node;
     const int32_t t = (int32_t)((blockIdx.x - node * blocks_per_node) * (uint32_t)(kThreads >> lanes_log2)) + (int32_t)(threadIdx.x >> lanes_log2);
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kThreads) void k_embed(const int32_t* __restrict__ 
                 piece_get<kOct, P>(in[k], c, D, v);
 #pragma unroll
                 for (int j = 0; j < kOct; ++j) v[j] = real ? v[j] * scale : other;
-                piece_put<kOct, E>(dst, c, D, v);
+                piece_put<kOct, E>(dst, c, D, v, stream);
             }
         }
     }
@@ -67,19 +67,14 @@ struct ZeroArgs {
     int64_t count, ldg;     // floats of a node's block, distance of the blocks
     float* g;
 };
-constexpr int kZeroUnits = 4;  // pieces of four floats a lane
-constexpr int kZeroCols = kZeroUnits * kSortThreads * 4;
+// One piece of four floats a lane: 786 MB are zeroed in 118 us beside the sort; four pieces a lane took 126.
+constexpr int kZeroCols = kSortThreads * 4;
 
 __device__ __forceinline__ void zero_block(const ZeroArgs& z, uint32_t b) {
     const uint32_t node = b / z.per_node;
-    const int64_t base = (int64_t)(b - node * z.per_node) * kZeroCols;
-    float* g = z.g + (int64_t)node * z.ldg;
+    const int64_t e = (int64_t)(b - node * z.per_node) * kZeroCols + threadIdx.x * 4;
     const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int u = 0; u < kZeroUnits; ++u) {
-        const int64_t e = base + (int64_t)(u * kSortThreads + threadIdx.x) * 4;
-        if (e < z.count) piece_put<4, ElemF32>(g + e, 0, z.count - e < 4 ? (int32_t)(z.count - e) : 4, zero);
-    }
+    if (e < z.count) piece_put<4, ElemF32>(z.g + (int64_t)node * z.ldg + e, 0, z.count - e < 4 ? (int32_t)(z.count - e) : 4, zero);
 }
 
 __global__ __launch_bounds__(kSortThreads) void k_sort_tile(const int32_t* __restrict__ tokens, int32_t T, int32_t V, uint32_t tiles, int bits,
@@ -216,7 +211,7 @@ __global__ __launch_bounds__(kThreads) void k_merge(const uint32_t* __restrict__
 // tokens cost no more than others.  A row that lies within its items goes straight to g; of a row that reaches into other chunks
 // it leaves a part in `partial` (slot 0: the row of its first item, slot 1: the row of its last item where that is another),
 // and k_embed_join adds the parts.  Rows without items hold the zeros of the sort's launch, or what g is to be added to.
-constexpr int kRun = 32;
+constexpr int kRun = 16;
 constexpr int kAhead = 8;               // items whose rows are loaded together
 constexpr int kTurnCols = kWave * 4;    // columns of a wavefront, four a lane: an fp32 store is 1 KiB without gaps
 
@@ -400,7 +395,7 @@ hipError_t launch_embed(const gpga_ctx* c, const RowsShape& s, const int32_t* to
     auto launch = [&](auto e) {
         typedef decltype(e) E;
         k_embed<E><<<dim3(per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(tokens, c->x + table_off, c->ld, V, s.D, s.T, per_node, lanes_log2,
-                                                                                    scale, static_cast<typename E::mem*>(y), s.ld);
+                                                                                    scale, static_cast<typename E::mem*>(y), s.ld, stream_rows(s));
         return hipGetLastError();
     };
     return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);

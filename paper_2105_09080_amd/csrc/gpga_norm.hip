@@ -25,6 +25,7 @@ struct NormArgs {
     int64_t ld, ldx;         // of the activations, of X and g
     uint32_t per_node;       // workgroups of a node
     DropArgs drop;
+    bool stream;             // activations pass by the caches
     float eps;
     const mem* x;            // forward: x; backward: dy
     const mem* side;         // forward: residual; backward: more (may be NULL)
@@ -49,9 +50,9 @@ __global__ __launch_bounds__(kThreads) void k_dropout(NormArgs<E> a, int lanes_l
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     for (uint32_t q = threadIdx.x & ((1u << lanes_log2) - 1u); q < octs; q += 1u << lanes_log2) {
         const int32_t c = (int32_t)q * kOct;
-        const Piece<E, kOct> in = piece_load<kOct, E>(a.x + row, c, a.D);
+        const Piece<E, kOct> in = piece_load<kOct, E>(a.x + row, c, a.D, a.stream);
         Piece<E, kOct> side;
-        if (kSide) side = piece_load<kOct, E>(a.side + row, c, a.D);
+        if (kSide) side = piece_load<kOct, E>(a.side + row, c, a.D, a.stream);
         float v[kOct];
         piece_get<kOct, E>(in, c, a.D, v);
         if (a.drop.drop) mask.apply(a.drop, (uint32_t)t * octs + q, v);
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void k_dropout(NormArgs<E> a, int lanes_l
 #pragma unroll
             for (int j = 0; j < kOct; ++j) v[j] += r[j];
         }
-        piece_put<kOct, E>(a.y + row, c, a.D, v);
+        piece_put<kOct, E>(a.y + row, c, a.D, v, a.stream);
     }
 }
 
@@ -94,7 +95,7 @@ __device__ __forceinline__ void norm_output(const NormArgs<E>& a, uint32_t node,
     piece_read<kOct, P>(a.beta + (int64_t)node * a.ldx, c, a.D, bt);
 #pragma unroll
     for (int j = 0; j < kOct; ++j) y[j] = (u[j] - mean) * rstd * gm[j] + bt[j];
-    piece_put<kOct, E>(a.y + row, c, a.D, y);
+    piece_put<kOct, E>(a.y + row, c, a.D, y, a.stream);
 }
 
 // ---- forward: L lanes a row, N pieces a lane, the row in registers ----------------------------------------------------------
@@ -112,8 +113,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm(NormArgs<E
     Piece<E, kOct> x[N], side[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        x[k] = piece_load<kOct, E>(a.x + row, (lane + k * L) * kOct, a.D);
-        if (a.side) side[k] = piece_load<kOct, E>(a.side + row, (lane + k * L) * kOct, a.D);
+        x[k] = piece_load<kOct, E>(a.x + row, (lane + k * L) * kOct, a.D, a.stream);
+        if (a.side) side[k] = piece_load<kOct, E>(a.side + row, (lane + k * L) * kOct, a.D, a.stream);
     }
     float u[N][kOct], sum[1] = {0.f}, var[1] = {0.f};
 #pragma unroll
@@ -139,7 +140,7 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm(NormArgs<E
     for (int k = 0; k < N; ++k) {
         const int32_t c = (lane + k * L) * kOct;
         if (c < a.D) {
-            if (a.u) piece_put<kOct, E>(a.u + row, c, a.D, u[k]);
+            if (a.u) piece_put<kOct, E>(a.u + row, c, a.D, u[k], a.stream);
             norm_output<E>(a, node, row, c, mean, rstd, u[k]);
         }
     }
@@ -194,20 +195,20 @@ __global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs<E> a) {
 
 // ---- backward -----------------------------------------------------------------------------------------------------------
 // What a lane has of a row: dy, u and the residual stream's gradient, as they lie in memory.
-template <typename E, int N>
+template <typename E, int N, bool kSide>
 struct GradRow {
-    Piece<E, kOct> dy[N], u[N], more[N];
+    Piece<E, kOct> dy[N], u[N], more[kSide ? N : 1];
     float mean, rstd;
 };
-template <int L, int N, typename E>
-__device__ __forceinline__ void grad_load(const NormArgs<E>& a, int64_t r, int32_t lane, GradRow<E, N>& in) {
+template <int L, int N, typename E, bool kSide>
+__device__ __forceinline__ void grad_load(const NormArgs<E>& a, int64_t r, int32_t lane, GradRow<E, N, kSide>& in) {
     const int64_t row = r * a.ld;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int32_t c = (lane + k * L) * kOct;
         in.dy[k] = piece_load<kOct, E>(a.x + row, c, a.D);
         in.u[k] = piece_load<kOct, E>(a.u_in + row, c, a.D);
-        if (a.side) in.more[k] = piece_load<kOct, E>(a.side + row, c, a.D);
+        if (kSide) in.more[k] = piece_load<kOct, E>(a.side + row, c, a.D);
     }
     in.mean = a.stats[2 * r];
     in.rstd = a.stats[2 * r + 1];
@@ -226,28 +227,59 @@ __device__ __forceinline__ void grad_input(const Piece<E, kOct>& dy_in, const Pi
     }
 }
 // du and dx of eight columns.
-template <typename E>
+template <bool kSide, typename E>
 __device__ __forceinline__ void grad_output(const NormArgs<E>& a, const DropNode& mask, const Piece<E, kOct>& more_in, int64_t row, uint32_t group,
                                             int32_t c, float rstd, float m1, float m2, const float* h, const float* xh) {
     float du[kOct], more[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (a.side) piece_get<kOct, E>(more_in, c, a.D, more);
+    if (kSide) piece_get<kOct, E>(more_in, c, a.D, more);
 #pragma unroll
     for (int j = 0; j < kOct; ++j) du[j] = rstd * (h[j] - m1 - xh[j] * m2) + more[j];
-    piece_put<kOct, E>(a.u + row, c, a.D, du);
+    piece_put<kOct, E>(a.u + row, c, a.D, du, a.stream);
     if (a.y) {
         mask.apply(a.drop, group, du);
-        piece_put<kOct, E>(a.y + row, c, a.D, du);
+        piece_put<kOct, E>(a.y + row, c, a.D, du, a.stream);
     }
 }
 
+// Sum over the rows that a wavefront works on side by side, L lanes each; lane by lane.
+template <int L>
+__device__ __forceinline__ float other_rows_sum(float v) {
+    if constexpr (L <= 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    if constexpr (L <= 32) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    return v;
+}
+// Eight floats in LDS.
+struct OctInLds {
+    static __device__ __forceinline__ void store(float* p, const float* v) {
+        v4f* to = reinterpret_cast<v4f*>(p);
+        to[0] = v4f{v[0], v[1], v[2], v[3]};
+        to[1] = v4f{v[4], v[5], v[6], v[7]};
+    }
+    static __device__ __forceinline__ void add(const float* p, float* v) {
+        const v4f* from = reinterpret_cast<const v4f*>(p);
+        const v4f a = from[0], b = from[1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] += a[j];
+            v[4 + j] += b[j];
+        }
+    }
+};
+
 // L lanes a row.  A workgroup takes the rows t = strip, strip + strips, ... of a node kRows at a time, keeps its sums for
 // dgamma and dbeta in registers, and leaves them in `partial`.  A row's loads are issued while the one before it is worked on.
-template <typename E, int L, int N>
+template <typename E, int L, int N, bool kSide>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormArgs<E> a) {
     typedef Elem<float, E::kNarrow> P;
     constexpr int kBlock = L > kThreads ? L : kThreads, kRows = kBlock / L;
     __shared__ float s_sum[2][L > kWave ? 2 * L / kWave : 1];
-    __shared__ float s_part[kRows > 1 ? 2 * L * N * kOct : 1];
+    __shared__ __align__(16) float s_part[kRows > 1 ? 2 * L * N * kOct : 4];
     const uint32_t node = blockIdx.x / a.per_node, strip = blockIdx.x - node * a.per_node;
     const int32_t lane = threadIdx.x & (L - 1), sub = threadIdx.x / L;
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
@@ -255,8 +287,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormA
     const float inv = 1.f / (float)a.D;
     const int64_t first_row = (int64_t)node * a.T, stride = (int64_t)a.per_node * kRows;
     int64_t t = (int64_t)strip * kRows + sub;
-    GradRow<E, N> next;
-    if (t < a.T) grad_load<L, N, E>(a, first_row + t, lane, next);
+    GradRow<E, N, kSide> next;
+    if (t < a.T) grad_load<L, N, E, kSide>(a, first_row + t, lane, next);
     float gm[N][kOct], dg[N][kOct], db[N][kOct];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -268,8 +300,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormA
     int turn = 0;
     for (; t < a.T; t += stride, turn ^= 1) {  // all lanes of a row alike
         const int64_t row = (first_row + t) * a.ld;
-        const GradRow<E, N> in = next;
-        if (t + stride < a.T) grad_load<L, N, E>(a, first_row + t + stride, lane, next);
+        const GradRow<E, N, kSide> in = next;
+        if (t + stride < a.T) grad_load<L, N, E, kSide>(a, first_row + t + stride, lane, next);
         float h[N][kOct], xh[N][kOct], s[2] = {0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -287,34 +319,38 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormA
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const int32_t q = lane + k * L, c = q * kOct;
-            if (c < a.D) grad_output<E>(a, mask, in.more[k], row, (uint32_t)t * octs + (uint32_t)q, c, in.rstd, s[0] * inv, s[1] * inv, h[k], xh[k]);
+            if (c < a.D) grad_output<kSide, E>(a, mask, in.more[kSide ? k : 0], row, (uint32_t)t * octs + (uint32_t)q, c, in.rstd, s[0] * inv, s[1] * inv, h[k], xh[k]);
         }
     }
-    // the rows of a workgroup one after another
     float* out = a.partial + (int64_t)blockIdx.x * 2 * a.D;
-    if (kRows > 1) {
-        for (int part = 0; part < kRows; ++part) {
-            if (sub == part) {
+    if constexpr (kRows > 1) {
+        // rows of one wavefront by the swaps of lanes, the wavefronts one after another through LDS
 #pragma unroll
-                for (int k = 0; k < N; ++k)
+        for (int k = 0; k < N; ++k)
 #pragma unroll
-                    for (int j = 0; j < kOct; ++j) {
-                        float* at = s_part + ((k * kOct + j) * 2) * L + lane;
-                        at[0] = part ? at[0] + dg[k][j] : dg[k][j];
-                        at[L] = part ? at[L] + db[k][j] : db[k][j];
-                    }
+            for (int j = 0; j < kOct; ++j) {
+                dg[k][j] = other_rows_sum<L>(dg[k][j]);
+                db[k][j] = other_rows_sum<L>(db[k][j]);
+            }
+        const int wave = threadIdx.x / kWave;
+        float* mine = s_part + (threadIdx.x & (L - 1)) * kOct;
+        for (int w = 1; w < kBlock / kWave; ++w) {
+            if (wave == w && (threadIdx.x & (kWave - 1)) < L) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    OctInLds::store(mine + (2 * k) * L * kOct, dg[k]);
+                    OctInLds::store(mine + (2 * k + 1) * L * kOct, db[k]);
+                }
             }
             __syncthreads();
-        }
-        if (sub == 0) {
+            if (sub == 0) {
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-#pragma unroll
-                for (int j = 0; j < kOct; ++j) {
-                    const float* at = s_part + ((k * kOct + j) * 2) * L + lane;
-                    dg[k][j] = at[0];
-                    db[k][j] = at[L];
+                for (int k = 0; k < N; ++k) {
+                    OctInLds::add(mine + (2 * k) * L * kOct, dg[k]);
+                    OctInLds::add(mine + (2 * k + 1) * L * kOct, db[k]);
                 }
+            }
+            __syncthreads();
         }
     }
     if (sub == 0) {
@@ -348,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_columns(NormArgs<E> a, u
     out[c] = dg;
     out[a.D + c] = db;
 }
-template <typename E>
+template <typename E, bool kSide>
 __global__ __launch_bounds__(kLongThreads) void k_norm_grad_long(NormArgs<E> a) {
     __shared__ float s_sum[2 * kLongThreads / kWave];
     const uint32_t node = blockIdx.x / (uint32_t)a.T;
@@ -358,11 +394,11 @@ __global__ __launch_bounds__(kLongThreads) void k_norm_grad_long(NormArgs<E> a) 
     const DropNode mask(a.drop, node);
     const float* gamma = a.gamma + (int64_t)node * a.ldx;
     float s[2] = {0.f, 0.f}, h[kOct], xh[kOct];
-    GradRow<E, 1> in;
+    GradRow<E, 1, kSide> in;
     auto input = [&](uint32_t q) {
         const int32_t c = (int32_t)q * kOct;
         float gm[kOct];
-        grad_load<kLongThreads, 1, E>(a, r, (int32_t)q, in);
+        grad_load<kLongThreads, 1, E, kSide>(a, r, (int32_t)q, in);
         piece_read<kOct, ElemF32>(gamma, c, a.D, gm);
         grad_input<E>(in.dy[0], in.u[0], c, a.D, in.mean, in.rstd, h, xh);
 #pragma unroll
@@ -380,7 +416,7 @@ __global__ __launch_bounds__(kLongThreads) void k_norm_grad_long(NormArgs<E> a) 
     const float inv = 1.f / (float)a.D;
     for (uint32_t q = threadIdx.x; q < octs; q += kLongThreads) {
         input(q);
-        grad_output<E>(a, mask, in.more[0], r * a.ld, t * octs + q, (int32_t)q * kOct, in.rstd, s[0] * inv, s[1] * inv, h, xh);
+        grad_output<kSide, E>(a, mask, in.more[0], r * a.ld, t * octs + q, (int32_t)q * kOct, in.rstd, s[0] * inv, s[1] * inv, h, xh);
     }
 }
 
@@ -446,6 +482,7 @@ hipError_t launch_dropout(const gpga_ctx* c, const RowsShape& s, const DropArgs&
         a.D = s.D;
         a.ld = s.ld;
         a.drop = drop;
+        a.stream = stream_rows(s);
         a.x = static_cast<const M*>(x);
         a.side = static_cast<const M*>(residual);
         a.y = static_cast<M*>(y);
@@ -472,6 +509,7 @@ hipError_t launch_norm(const gpga_ctx* c, const RowsShape& s, const DropArgs& dr
         a.ld = s.ld;
         a.ldx = c->ld;
         a.drop = drop;
+        a.stream = stream_rows(s);
         a.eps = eps;
         a.x = static_cast<const M*>(x);
         a.side = static_cast<const M*>(residual);
@@ -510,6 +548,7 @@ hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArg
         a.ld = s.ld;
         a.ldx = c->ld;
         a.drop = drop;
+        a.stream = stream_rows(s);
         a.x = static_cast<const M*>(dy);
         a.side = static_cast<const M*>(more);
         a.u_in = static_cast<const M*>(u);
@@ -521,13 +560,17 @@ hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArg
         a.per_node = strips;
         const bool held = with_row_shape<E>((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
             constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
-            k_norm_grad<E, L, N><<<dim3(strips * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
+            const dim3 grid(strips * (uint32_t)s.n);
+            if (more) k_norm_grad<E, L, N, true><<<grid, dim3(kBlock), 0, c->stream>>>(a);
+            else k_norm_grad<E, L, N, false><<<grid, dim3(kBlock), 0, c->stream>>>(a);
         });
         if constexpr (!E::kNarrow) {
             if (!held) {
                 const uint32_t column_blocks = blocks_for(s.D, kThreads);
                 k_norm_grad_columns<E><<<dim3(strips * column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, column_blocks);
-                if (s.T > 0) k_norm_grad_long<E><<<dim3((uint32_t)s.T * (uint32_t)s.n), dim3(kLongThreads), 0, c->stream>>>(a);
+                const dim3 grid((uint32_t)s.T * (uint32_t)s.n);
+                if (s.T > 0 && more) k_norm_grad_long<E, true><<<grid, dim3(kLongThreads), 0, c->stream>>>(a);
+                else if (s.T > 0) k_norm_grad_long<E, false><<<grid, dim3(kLongThreads), 0, c->stream>>>(a);
             }
         }
         return hipGetLastError();

@@ -185,7 +185,7 @@ gpga_status gpga_embed_grad(gpga_ctx* c, const int32_t* tokens, int32_t T, int64
     if (!std::isfinite(scale)) return fail(c, GPGA_EINVAL, "scale must be finite");
     if (accumulate != 0 && accumulate != 1) return fail(c, GPGA_EINVAL, "accumulate must be 0 or 1");
     if (T > 0 && !dy) return fail(c, GPGA_EINVAL, "dy_dev must not be NULL");
-    if ((int64_t)c->n * V > kMaxGroups) return fail(c, GPGA_EINVAL, "n * V must be below 2^31");
+    if ((double)c->n * V * D / 1024 > 1e9) return fail(c, GPGA_EINVAL, "n * V * D must be below 10^12");
     DeviceGuard guard(c->device);
     GPGA_TRY(reserve(c, embed_grad_scratch(s)));
     const hipError_t e = launch_embed_grad(c, s, tokens, table_off, V, scale, dy, accumulate != 0, c->op_scratch);

@@ -37,8 +37,13 @@ struct Piece {
     uint32_t w[kWords];
 };
 
+// Keeps the compiler from merging the two kinds of access into one plain one.
+__device__ __forceinline__ void own_branch() { asm volatile(""); }
+
+// `stream` (uniform): the access leaves no copy behind in the L2 caches, for arrays that they could not hold until the next
+// operator comes (stream_rows below).
 template <int W, typename E>
-__device__ __forceinline__ Piece<E, W> piece_load(const typename E::mem* row, int32_t c, int32_t D) {
+__device__ __forceinline__ Piece<E, W> piece_load(const typename E::mem* row, int32_t c, int32_t D, bool stream = false) {
     typedef typename E::mem M;
     Piece<E, W> p;
     if constexpr (E::kNarrow) {
@@ -52,7 +57,15 @@ __device__ __forceinline__ Piece<E, W> piece_load(const typename E::mem* row, in
         const M* at = row + (c + W <= D ? c : D - W);
 #pragma unroll
         for (int k = 0; k < Piece<E, W>::kWords / kLoad; ++k) {
-            const vec v = reinterpret_cast<const vec*>(at)[k];
+            const vec* from = reinterpret_cast<const vec*>(at) + k;
+            vec v;
+            if (stream) {
+                own_branch();
+                v = __builtin_nontemporal_load(from);
+                own_branch();
+            } else {
+                v = *from;
+            }
 #pragma unroll
             for (int j = 0; j < kLoad; ++j) p.w[k * kLoad + j] = v[j];
         }
@@ -106,7 +119,7 @@ __device__ __forceinline__ void piece_read(const typename E::mem* row, int32_t c
 
 // Columns c .. of the row, as many as there are, c < D.
 template <int W, typename E>
-__device__ __forceinline__ void piece_put(typename E::mem* row, int32_t c, int32_t D, const float* v) {
+__device__ __forceinline__ void piece_put(typename E::mem* row, int32_t c, int32_t D, const float* v, bool stream = false) {
     typedef typename E::mem M;
     typedef M vec __attribute__((ext_vector_type(W), aligned(alignof(M))));
     typedef float wide __attribute__((ext_vector_type(W)));
@@ -114,7 +127,15 @@ __device__ __forceinline__ void piece_put(typename E::mem* row, int32_t c, int32
         wide f;
 #pragma unroll
         for (int j = 0; j < W; ++j) f[j] = v[j];
-        *reinterpret_cast<vec*>(row + c) = __builtin_convertvector(f, vec);
+        vec* to = reinterpret_cast<vec*>(row + c);
+        const vec out = __builtin_convertvector(f, vec);
+        if (stream) {
+            own_branch();
+            __builtin_nontemporal_store(out, to);
+            own_branch();
+        } else {
+            *to = out;
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < W; ++j)
@@ -221,6 +242,11 @@ hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArg
 size_t token_loss_scratch(const RowsShape& s, int num_cus);
 hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* logits, const int32_t* labels, float grad_scale, float* loss,
                              void* dlogits, void* scratch);
+
+// Whether accesses to an activation array stream past the L2 caches (4 MiB for each of 8 XCDs): arrays of 32 MiB and more.
+inline bool stream_rows(const RowsShape& s) {
+    return (int64_t)s.n * s.T * s.D * (s.dtype == GPGA_F32 ? 4 : 2) >= 32ll << 20;
+}
 
 // Calls f with a value of the kind of element that `dtype` names; the narrow kinds are for rows shorter than a piece.
 template <typename F>

@@ -31,6 +31,7 @@ struct LossArgs {
     float* row_loss;       // n*T
     const int32_t* count;  // n: counted tokens; NULL: a workgroup counts the labels of its node itself
     float grad_scale;
+    bool stream;           // rows pass by the caches
     uint32_t* left;        // counters, one a node, kLossLeftStride apart; NULL: k_loss_mean follows
     float* loss;           // n
     // rows in pieces
@@ -122,7 +123,7 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
     const bool bad = label >= a.V;
     if (label >= 0) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) in[k] = piece_load<kOct, E>(z, (lane + k * L) * kOct, a.V);
+        for (int k = 0; k < N; ++k) in[k] = piece_load<kOct, E>(z, (lane + k * L) * kOct, a.V, a.stream);
         picked = E::get(z[bad ? 0 : label]);
     }
     const int32_t counted = a.count ? a.count[node] : count_labels(labels, a.T, kBlock, s_count);
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const int32_t c = (lane + k * L) * kOct;
-                if (c < a.V) piece_put<kOct, E>(dz, c, a.V, zero);
+                if (c < a.V) piece_put<kOct, E>(dz, c, a.V, zero, a.stream);
             }
         } else {
             const float scale = bad ? __builtin_nanf("") : a.grad_scale / (float)counted;
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
 #pragma unroll
                     for (int j = 0; j < kOct; ++j) e[k][j] *= share;
                     if ((uint32_t)(label - c) < kOct) less_at(e[k], label - c, scale);
-                    piece_put<kOct, E>(dz, c, a.V, e[k]);
+                    piece_put<kOct, E>(dz, c, a.V, e[k], a.stream);
                 }
             }
         }
@@ -387,6 +388,7 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
         a.labels = labels;
         a.dz = static_cast<typename E::mem*>(dlogits);
         a.grad_scale = grad_scale;
+        a.stream = stream_rows(s);
         a.loss = loss;
         const uint32_t all = (uint32_t)s.n * (uint32_t)s.T;
         if (cut.pieces) {
