@@ -51,15 +51,16 @@ __global__ __launch_bounds__(kThreads) void k_embed(const int32_t* __restrict__ 
 }
 
 // ---- sorting the tokens of a node ---------------------------------------------------------------------------------------
-// A workgroup sorts a tile of kTile (token, position) pairs in LDS, least significant digit first and stable, so equal
-// tokens stay in the order of their positions; k_merge puts the tiles of a node together.  Keys: the token, V for padding,
-// V + 1 for a token that is out of range.  The workgroups behind those zero the table's columns of g, which takes longer than
-// the sort and waits for nothing.
+// A workgroup sorts a tile of (token, position) pairs in LDS, least significant digit first and stable, so equal tokens stay in
+// the order of their positions; k_merge puts the tiles of a node together where there are several.  Keys: the token, V for
+// padding, V + 1 for a token that is out of range.  Digits have up to 10 bits: counting them costs one step a bit whatever their
+// width, and a pass over the tile more is what costs.  The workgroups behind those zero the table's columns of g, which takes
+// longer than the sort and waits for nothing.
 constexpr int kSortThreads = 1024;
-constexpr int kSortItems = 4;
-constexpr int kTile = kSortThreads * kSortItems;
 constexpr int kSortWaves = kSortThreads / kWave;
-constexpr int kDigits = 256;
+constexpr int kTile = 8 * kSortThreads;       // items of a tile, the last one's fewer
+constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
+static_assert(kDigits == kSortThreads, "a thread a digit");
 
 struct ZeroArgs {
     uint32_t first_block;   // workgroups from here on zero
@@ -77,96 +78,102 @@ __device__ __forceinline__ void zero_block(const ZeroArgs& z, uint32_t b) {
     if (e < z.count) piece_put<4, ElemF32>(z.g + (int64_t)node * z.ldg + e, 0, z.count - e < 4 ? (int32_t)(z.count - e) : 4, zero);
 }
 
+// kItems items a thread: 8, or fewer where no tile has more.
+template <int kItems>
 __global__ __launch_bounds__(kSortThreads) void k_sort_tile(const int32_t* __restrict__ tokens, int32_t T, int32_t V, uint32_t tiles, int bits,
                                                             uint32_t* __restrict__ keys, int32_t* __restrict__ pos, ZeroArgs zero) {
     if (blockIdx.x >= zero.first_block) {
         zero_block(zero, blockIdx.x - zero.first_block);
         return;
     }
-    __shared__ uint32_t s_key[kTile];
-    __shared__ uint16_t s_pos[kTile];
-    __shared__ uint32_t s_count[kSortWaves][kDigits];
-    __shared__ uint32_t s_total[kDigits / kWave];
+    __shared__ uint32_t s_key[kItems * kSortThreads];
+    __shared__ uint16_t s_pos[kItems * kSortThreads];
+    __shared__ uint16_t s_count[kSortWaves][kDigits];
+    __shared__ uint32_t s_total[kSortWaves];
     const uint32_t node = blockIdx.x / tiles;
     const int32_t base = (int32_t)(blockIdx.x - node * tiles) * kTile;
     const int64_t from = (int64_t)node * T + base;
     const int32_t count = T - base < kTile ? T - base : kTile;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int32_t first = wave * kWave * kSortItems + lane;  // item j of a lane: first + j * 64
+    const int32_t first = wave * kWave * kItems + lane;  // item j of a lane: first + j * 64
 
-    uint32_t key[kSortItems];
-    uint16_t at[kSortItems];
+    uint32_t key[kItems];
+    uint16_t at[kItems];
 #pragma unroll
-    for (int j = 0; j < kSortItems; ++j) {
+    for (int j = 0; j < kItems; ++j) {
         const int32_t e = first + j * kWave;
+        const int32_t tok = tokens[from + (e < count ? e : 0)];
         at[j] = (uint16_t)e;
-        key[j] = 0xffffffffu;  // past the end: behind everything
-        if (e < count) {
-            const int32_t tok = tokens[from + e];
-            key[j] = tok < 0 ? (uint32_t)V : tok >= V ? (uint32_t)V + 1u : (uint32_t)tok;
-        }
+        // past the end: behind everything
+        key[j] = e >= count ? 0xffffffffu : tok < 0 ? (uint32_t)V : tok >= V ? (uint32_t)V + 1u : (uint32_t)tok;
     }
-    const int passes = (bits + 7) / 8, width = (bits + passes - 1) / passes;
+    const int passes = (bits + kDigitBits - 1) / kDigitBits, width = (bits + passes - 1) / passes;
     const uint32_t mask = (1u << width) - 1u;
     for (int pass = 0; pass < passes; ++pass) {
-        for (int d = threadIdx.x; d < kSortWaves * kDigits; d += kSortThreads) (&s_count[0][0])[d] = 0u;
+        for (int d = threadIdx.x; d < kSortWaves * kDigits / 2; d += kSortThreads) reinterpret_cast<uint32_t*>(&s_count[0][0])[d] = 0u;
         __syncthreads();
-        uint32_t rank[kSortItems];
+        // lanes whose item has the same digit, one step a bit: peers &= ~(ballot ^ own bit on all places)
+        uint32_t rank[kItems], low[kItems], high[kItems];
 #pragma unroll
-        for (int j = 0; j < kSortItems; ++j) {
-            const uint32_t digit = (key[j] >> (pass * width)) & mask;
-            uint64_t peers = ~0ull;
-            for (int b = 0; b < width; ++b) {
-                const uint64_t set = __ballot((digit >> b) & 1u);
-                peers &= ((digit >> b) & 1u) ? set : ~set;
+        for (int j = 0; j < kItems; ++j) low[j] = high[j] = 0xffffffffu;
+        for (int b = 0; b < width; ++b) {
+#pragma unroll
+            for (int j = 0; j < kItems; ++j) {
+                const int32_t own = (int32_t)(key[j] << (31 - pass * width - b)) >> 31;
+                const uint64_t set = __ballot(own != 0);
+                low[j] = __builtin_amdgcn_bitop3_b32(low[j], (uint32_t)set, (uint32_t)own, 0x90);
+                high[j] = __builtin_amdgcn_bitop3_b32(high[j], (uint32_t)(set >> 32), (uint32_t)own, 0x90);
             }
+        }
+#pragma unroll
+        for (int j = 0; j < kItems; ++j) {
+            const uint64_t peers = (uint64_t)high[j] << 32 | low[j];
             const uint32_t before = __builtin_popcountll(peers & ((1ull << lane) - 1ull));
             // one lane a digit counts for all its peers; a wavefront's LDS accesses stay in order
-            volatile uint32_t* counter = &s_count[wave][digit];
+            volatile uint16_t* counter = &s_count[wave][(key[j] >> (pass * width)) & mask];
             const uint32_t had = *counter;
             __builtin_amdgcn_wave_barrier();
-            if (before == 0) *counter = had + (uint32_t)__builtin_popcountll(peers);
+            if (before == 0) *counter = (uint16_t)(had + (uint32_t)__builtin_popcountll(peers));
             __builtin_amdgcn_wave_barrier();
             rank[j] = had + before;
         }
         __syncthreads();
         // where each wavefront's items of a digit begin: digits in order, wavefronts in order within a digit
-        uint32_t total = 0, ahead = 0;
-        if (threadIdx.x < kDigits) {
-            for (int w = 0; w < kSortWaves; ++w) total += s_count[w][threadIdx.x];
-            ahead = total;
-            for (int off = 1; off < kWave; off <<= 1) {
-                const uint32_t up = __shfl_up(ahead, off, kWave);
-                if (lane >= off) ahead += up;
-            }
-            if (lane == kWave - 1) s_total[wave] = ahead;
+        uint32_t total = 0, ahead;
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) total += s_count[w][threadIdx.x];
+        ahead = total;
+#pragma unroll
+        for (int off = 1; off < kWave; off <<= 1) {
+            const uint32_t up = __shfl_up(ahead, off, kWave);
+            if (lane >= off) ahead += up;
         }
+        if (lane == kWave - 1) s_total[wave] = ahead;
         __syncthreads();
-        if (threadIdx.x < kDigits) {
-            uint32_t at_digit = ahead - total;
-            for (int w = 0; w < wave; ++w) at_digit += s_total[w];
-            for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t held = s_count[w][threadIdx.x];
-                s_count[w][threadIdx.x] = at_digit;
-                at_digit += held;
-            }
+        uint32_t begin = ahead - total;
+        for (int w = 0; w < wave; ++w) begin += s_total[w];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t held = s_count[w][threadIdx.x];
+            s_count[w][threadIdx.x] = (uint16_t)begin;
+            begin += held;
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kSortItems; ++j) {
+        for (int j = 0; j < kItems; ++j) {
             const uint32_t to = s_count[wave][(key[j] >> (pass * width)) & mask] + rank[j];
             s_key[to] = key[j];
             s_pos[to] = at[j];
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kSortItems; ++j) {
+        for (int j = 0; j < kItems; ++j) {
             key[j] = s_key[first + j * kWave];
             at[j] = s_pos[first + j * kWave];
         }
     }
 #pragma unroll
-    for (int j = 0; j < kSortItems; ++j) {
+    for (int j = 0; j < kItems; ++j) {
         const int32_t e = first + j * kWave;
         if (e < count) {
             keys[from + e] = key[j];
@@ -354,6 +361,11 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a) {
     }
 }
 
+template <int V>
+struct Const {
+    static constexpr int value = V;
+};
+
 uint32_t blocks_for(int64_t items, int64_t per_block) { return (uint32_t)((items + per_block - 1) / per_block); }
 
 size_t padded(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -419,7 +431,13 @@ hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_
     zero.g = c->g + table_off;
     const uint32_t blocks = zero.first_block + zero.per_node * (uint32_t)s.n;
     if (blocks) {
-        k_sort_tile<<<dim3(blocks), dim3(kSortThreads), 0, c->stream>>>(tokens, s.T, V, space.tiles, bits, words(space.tile_keys), ints(space.tile_pos), zero);
+        auto sort = [&](auto items) {
+            k_sort_tile<decltype(items)::value><<<dim3(blocks), dim3(kSortThreads), 0, c->stream>>>(tokens, s.T, V, space.tiles, bits, words(space.tile_keys),
+                                                                                                  ints(space.tile_pos), zero);
+        };
+        if (s.T <= kSortThreads) sort(Const<1>());
+        else if (s.T <= 4 * kSortThreads) sort(Const<4>());
+        else sort(Const<8>());
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -108,8 +108,8 @@ def test_embedding(hx, n, T, V, D, off, pad, kind, dtype):
     sim.close()
 
 
-@pytest.mark.parametrize("T", [4095, 4096, 4097, 8192, 9001, 20000])
-@pytest.mark.parametrize("V", [2, 255, 256, 257, 70_000])
+@pytest.mark.parametrize("T", [1024, 1025, 4095, 4096, 4097, 8191, 8192, 8193, 20000])
+@pytest.mark.parametrize("V", [2, 255, 256, 257, 1021, 1023, 1024, 70_000])
 def test_embedding_gradient_across_the_tiles_of_the_sort(hx, T, V):
     n, D = 2, 8
     sim, X, rng = make_sim(hx, n, V * D, seed=T + V)
