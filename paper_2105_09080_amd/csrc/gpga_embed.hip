@@ -68,14 +68,23 @@ struct ZeroArgs {
     int64_t count, ldg;     // floats of a node's block, distance of the blocks
     float* g;
 };
-// One piece of four floats a lane: 786 MB are zeroed in 118 us beside the sort; four pieces a lane took 126.
+// One piece of four floats a lane: 786 MB are zeroed in 118 us beside the sort; four pieces a lane took 126.  The pieces are
+// those of the 128-byte lines of memory, wherever in one the block begins: with pieces counted from its beginning 526 MB took
+// 102 us at 8 bytes past a boundary.
 constexpr int kZeroCols = kSortThreads * 4;
 
 __device__ __forceinline__ void zero_block(const ZeroArgs& z, uint32_t b) {
     const uint32_t node = b / z.per_node;
-    const int64_t e = (int64_t)(b - node * z.per_node) * kZeroCols + threadIdx.x * 4;
+    float* g = z.g + (int64_t)node * z.ldg;
+    const int64_t before = (int64_t)(reinterpret_cast<uintptr_t>(g) / 4 % 32);  // floats of the first line in front of the block
+    const int64_t e = (int64_t)(b - node * z.per_node) * kZeroCols + threadIdx.x * 4 - before;
     const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-    if (e < z.count) piece_put<4, ElemF32>(z.g + (int64_t)node * z.ldg + e, 0, z.count - e < 4 ? (int32_t)(z.count - e) : 4, zero);
+    if (e >= 0 && e + 4 <= z.count) {
+        piece_put<4, ElemF32>(g + e, 0, 4, zero);
+    } else {
+        for (int j = 0; j < 4; ++j)
+            if (e + j >= 0 && e + j < z.count) g[e + j] = 0.f;
+    }
 }
 
 // kItems items a thread: 8, or fewer where no tile has more.
@@ -221,6 +230,7 @@ __global__ __launch_bounds__(kThreads) void k_merge(const uint32_t* __restrict__
 constexpr int kRun = 16;
 constexpr int kAhead = 8;               // items whose rows are loaded together
 constexpr int kTurnCols = kWave * 4;    // columns of a wavefront, four a lane: an fp32 store is 1 KiB without gaps
+constexpr int kMostTurns = 16;          // wavefronts of a workgroup, all of one chunk: the lines that two share stay on one XCD
 
 struct GradArgs {
     const uint32_t* keys;   // sorted, T a node
@@ -232,12 +242,10 @@ struct GradArgs {
     int32_t accumulate;
     uint32_t chunks;            // of a node
     uint32_t column_blocks;     // of kTurnCols
+    uint32_t column_groups;     // workgroups that these make
     float* partial;             // n x chunks x 2 x D
     float* g;                   // the table's columns of node 0
 };
-
-// A node with a token that is out of range: the last key in its order.
-__device__ __forceinline__ bool out_of_range(const uint32_t* keys, const GradArgs& a) { return keys[a.T - 1] == (uint32_t)a.V + 1u; }
 
 // Four columns of a row of g from their sum and what g holds.
 template <typename P>
@@ -249,28 +257,26 @@ __device__ __forceinline__ void put_sum(const GradArgs& a, float* out, int32_t c
 }
 
 template <typename E, bool kAdd>
-__global__ __launch_bounds__(kThreads) void k_embed_grad(GradArgs a, const typename E::mem* __restrict__ dy) {
+__global__ __launch_bounds__(kMostTurns * kWave) void k_embed_grad(GradArgs a, const typename E::mem* __restrict__ dy) {
     typedef Elem<float, E::kNarrow> P;
     const int lane = threadIdx.x & (kWave - 1);
-    const uint32_t wave = blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const uint32_t unit = wave / a.column_blocks, node = unit / a.chunks, chunk = unit - node * a.chunks;
-    if (node >= a.n) return;
+    const uint32_t unit = blockIdx.x / a.column_groups, group = blockIdx.x - unit * a.column_groups, node = unit / a.chunks, chunk = unit - node * a.chunks;
     const uint32_t* keys = a.keys + (int64_t)node * a.T;
-    if (out_of_range(keys, a)) {  // NaN everywhere: a share of the block for each wavefront
-        const int64_t all = (int64_t)a.V * a.D, shares = (int64_t)a.chunks * a.column_blocks, share = (all + shares - 1) / shares;
-        const int64_t from = (wave - (int64_t)node * shares) * share, to = from + share < all ? from + share : all;
-        for (int64_t e = from + lane; e < to; e += kWave) a.g[(int64_t)node * a.ldg + e] = __builtin_nanf("");
-        return;
-    }
     const int32_t first = (int32_t)chunk * kRun, count = a.T - first < kRun ? a.T - first : kRun;
     const uint32_t key = keys[first + (lane < count ? lane : count - 1)];
     const int32_t at = a.pos[(int64_t)node * a.T + first + (lane < count ? lane : count - 1)];
-    const uint32_t before = chunk ? keys[first - 1] : 0xffffffffu, after = first + count < a.T ? keys[first + count] : 0xffffffffu;
+    const uint32_t end = keys[a.T - 1], before = chunk ? keys[first - 1] : 0xffffffffu, after = first + count < a.T ? keys[first + count] : 0xffffffffu;
+    if (end == (uint32_t)a.V + 1u) {  // a token was out of range: NaN everywhere, a share of the block for each workgroup
+        const int64_t all = (int64_t)a.V * a.D, shares = (int64_t)a.chunks * a.column_groups, share = (all + shares - 1) / shares;
+        const int64_t from = ((int64_t)chunk * a.column_groups + group) * share, to = from + share < all ? from + share : all;
+        for (int64_t e = from + threadIdx.x; e < to; e += blockDim.x) a.g[(int64_t)node * a.ldg + e] = __builtin_nanf("");
+        return;
+    }
     const uint32_t down = __shfl_down(key, 1, kWave);
     // items that are the last of their row here, and those of padding, which is behind all rows
     const uint64_t last = __ballot(lane < count && (lane == count - 1 || key != down)), padding = __ballot(lane < count && key >= (uint32_t)a.V);
     const int real = padding ? __builtin_ctzll(padding) : count;
-    const int32_t c = (int32_t)(wave - unit * a.column_blocks) * kTurnCols + lane * 4;
+    const int32_t c = (int32_t)(group * blockDim.x + threadIdx.x) * 4;
     const bool on = c < a.D;
     const typename E::mem* rows = dy + (int64_t)node * a.T * a.ld;
     float* g = a.g + (int64_t)node * a.ldg;
@@ -313,51 +319,84 @@ __global__ __launch_bounds__(kThreads) void k_embed_grad(GradArgs a, const typen
     }
 }
 
-// Adds the parts of each row that reaches into several chunks, kTurnCols columns a workgroup: the one of the chunk in which the
-// row begins.  Its wavefronts take contiguous shares of the parts; everything in a fixed order.
+// Adds the parts of each row that reaches into several chunks, kTurnCols columns a wavefront: the one of the chunk in which the row
+// begins.  Rows of more than kLongRow parts are added by the workgroup, a contiguous share for each of its wavefronts.
+// Everything in a fixed order.
+constexpr int kLongRow = 8;
+
 template <typename P>
-__global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a) {
+__device__ __forceinline__ void add_parts(const GradArgs& a, const float* part, uint32_t from, uint32_t to, bool second, int32_t c, float* sum) {
+#pragma unroll 8
+    for (uint32_t p = from; p < to; ++p) {
+        float v[4];
+        piece_read<4, P>(part + ((int64_t)p * 2 + (p == 0 && second ? 1 : 0)) * a.D, c, a.D, v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] += v[j];
+    }
+}
+template <typename P>
+__device__ __forceinline__ void put_row(const GradArgs& a, uint32_t node, uint32_t key, int32_t c, const float* sum) {
+    float* out = a.g + (int64_t)node * a.ldg + (int64_t)key * a.D;
+    float had[4] = {0.f, 0.f, 0.f, 0.f};
+    if (a.accumulate) piece_read<4, P>(out, c, a.D, had);
+    put_sum<P>(a, out, c, had, sum);
+}
+
+template <typename P>
+__global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a, uint32_t blocks_per_node) {
     constexpr int kWaves = kThreads / kWave;
     __shared__ float s_part[kWaves][kTurnCols];
-    const uint32_t unit = blockIdx.x / a.column_blocks, node = unit / a.chunks, chunk = unit - node * a.chunks;
-    const uint32_t* keys = a.keys + (int64_t)node * a.T;
-    const int32_t first = (int32_t)chunk * kRun, next = first + kRun;
-    if (next >= a.T) return;  // the last chunk: nothing goes on
-    const uint32_t key = keys[next - 1];
-    if (key != keys[next] || key >= (uint32_t)a.V || out_of_range(keys, a)) return;
-    const bool from_first = keys[first] == key;
-    if (from_first && chunk && keys[first - 1] == key) return;  // begins earlier
+    __shared__ uint32_t s_parts[kWaves], s_key[kWaves];
+    __shared__ bool s_second[kWaves];
+    const uint32_t unit = blockIdx.x / a.column_blocks, node = unit / blocks_per_node, chunk0 = (unit - node * blocks_per_node) * kWaves;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    uint32_t parts = 1;  // this chunk's and those of the chunks that begin with the row
-    for (uint64_t same = ~0ull; same == ~0ull; parts += (uint32_t)__builtin_popcountll(same)) {
-        const int64_t at = first + (int64_t)(parts + lane) * kRun;
-        same = __ballot(at < a.T && keys[at < a.T ? at : 0] == key);
-    }
+    const uint32_t chunk = chunk0 + wave;
+    const uint32_t* keys = a.keys + (int64_t)node * a.T;
     const int32_t c = (int32_t)(blockIdx.x - unit * a.column_blocks) * kTurnCols + lane * 4;
-    const uint32_t share = (parts + kWaves - 1) / kWaves;
-    const uint32_t from = wave * share, to = from + share < parts ? from + share : parts;
-    const float* part = a.partial + ((int64_t)node * a.chunks + chunk) * 2 * a.D;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    if (c < a.D) {
-#pragma unroll 4
-        for (uint32_t p = from; p < to; ++p) {
-            float v[4];
-            piece_read<4, P>(part + ((int64_t)p * 2 + (p == 0 && !from_first ? 1 : 0)) * a.D, c, a.D, v);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum[j] += v[j];
+    const float* parts_of_node = a.partial + (int64_t)node * a.chunks * 2 * a.D;
+    const int64_t first = (int64_t)chunk * kRun, next = first + kRun;
+    uint32_t parts = 0, key = 0;
+    bool second = false;
+    if (next < a.T) {  // otherwise nothing goes on from here
+        const uint32_t at_first = keys[first], on = keys[next], ahead = chunk ? keys[first - 1] : 0xffffffffu, end = keys[a.T - 1];
+        key = keys[next - 1];
+        second = at_first != key;
+        // the row goes on, is a row, and begins here
+        if (key == on && key < (uint32_t)a.V && end <= (uint32_t)a.V && (second || ahead != key)) {
+            parts = 1;  // this chunk's and those of the chunks that begin with the row
+            for (uint64_t same = ~0ull; same == ~0ull; parts += (uint32_t)__builtin_popcountll(same)) {
+                const int64_t at = first + (int64_t)(parts + lane) * kRun;
+                same = __ballot(at < a.T && keys[at < a.T ? at : 0] == key);
+            }
         }
     }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) s_part[wave][j * kWave + lane] = sum[j];
+    if (parts && parts <= kLongRow && c < a.D) {
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        add_parts<P>(a, parts_of_node + (int64_t)chunk * 2 * a.D, 0, parts, second, c, sum);
+        put_row<P>(a, node, key, c, sum);
+    }
+    if (lane == 0) {
+        s_parts[wave] = parts;
+        s_key[wave] = key;
+        s_second[wave] = second;
+    }
     __syncthreads();
-    if (wave == 0 && c < a.D) {
+    for (int w = 0; w < kWaves; ++w) {
+        parts = s_parts[w];
+        if (parts <= kLongRow) continue;
+        const uint32_t share = (parts + kWaves - 1) / kWaves, from = wave * share, to = from + share < parts ? from + share : parts;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if (c < a.D) add_parts<P>(a, parts_of_node + (int64_t)(chunk0 + w) * 2 * a.D, from, to, s_second[w], c, sum);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            for (int w = 1; w < kWaves; ++w) sum[j] += s_part[w][j * kWave + lane];
-        float* out = a.g + (int64_t)node * a.ldg + (int64_t)key * a.D;
-        float had[4] = {0.f, 0.f, 0.f, 0.f};
-        if (a.accumulate) piece_read<4, P>(out, c, a.D, had);
-        put_sum<P>(a, out, c, had, sum);
+        for (int j = 0; j < 4; ++j) s_part[wave][j * kWave + lane] = sum[j];
+        __syncthreads();
+        if (wave == 0 && c < a.D) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                for (int v = 1; v < kWaves; ++v) sum[j] += s_part[v][j * kWave + lane];
+            put_row<P>(a, node, s_key[w], c, sum);
+        }
+        __syncthreads();
     }
 }
 
@@ -407,7 +446,7 @@ hipError_t launch_embed(const gpga_ctx* c, const RowsShape& s, const int32_t* to
     auto launch = [&](auto e) {
         typedef decltype(e) E;
         k_embed<E><<<dim3(per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(tokens, c->x + table_off, c->ld, V, s.D, s.T, per_node, lanes_log2,
-                                                                                    scale, static_cast<typename E::mem*>(y), s.ld, stream_rows(s));
+                                                                                    scale, static_cast<typename E::mem*>(y), s.ld, stream_rows(s, y));
         return hipGetLastError();
     };
     return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
@@ -426,7 +465,7 @@ hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_
     ZeroArgs zero = {};
     zero.first_block = space.tiles * (uint32_t)s.n;
     zero.count = (int64_t)V * s.D;
-    zero.per_node = accumulate ? 0 : blocks_for(zero.count, kZeroCols);
+    zero.per_node = accumulate ? 0 : blocks_for(zero.count + 31, kZeroCols);
     zero.ldg = c->ld;
     zero.g = c->g + table_off;
     const uint32_t blocks = zero.first_block + zero.per_node * (uint32_t)s.n;
@@ -462,17 +501,19 @@ hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_
     a.accumulate = accumulate;
     a.chunks = space.chunks;
     a.column_blocks = blocks_for(s.D, kTurnCols);
+    a.column_groups = blocks_for(a.column_blocks, kMostTurns);
     a.partial = reinterpret_cast<float*>(base + space.partial);
     a.g = c->g + table_off;
     auto launch = [&](auto el) {
         typedef decltype(el) E;
-        const dim3 grid(blocks_for((int64_t)a.chunks * a.column_blocks * s.n, kThreads / kWave));
+        const dim3 grid(a.chunks * a.column_groups * (uint32_t)s.n), block(kWave * blocks_for(a.column_blocks, a.column_groups));
         const typename E::mem* rows = static_cast<const typename E::mem*>(dy);
-        if (accumulate) k_embed_grad<E, true><<<grid, dim3(kThreads), 0, c->stream>>>(a, rows);
-        else k_embed_grad<E, false><<<grid, dim3(kThreads), 0, c->stream>>>(a, rows);
+        if (accumulate) k_embed_grad<E, true><<<grid, block, 0, c->stream>>>(a, rows);
+        else k_embed_grad<E, false><<<grid, block, 0, c->stream>>>(a, rows);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || a.chunks < 2) return e;
-        k_embed_join<Elem<float, E::kNarrow>><<<dim3(a.chunks * a.column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a);
+        const uint32_t per_node = blocks_for(a.chunks, kThreads / kWave);
+        k_embed_join<Elem<float, E::kNarrow>><<<dim3(per_node * a.column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, per_node);
         return hipGetLastError();
     };
     return s.D < 4 ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);

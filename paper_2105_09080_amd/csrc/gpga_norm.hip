@@ -482,7 +482,7 @@ hipError_t launch_dropout(const gpga_ctx* c, const RowsShape& s, const DropArgs&
         a.D = s.D;
         a.ld = s.ld;
         a.drop = drop;
-        a.stream = stream_rows(s);
+        a.stream = stream_rows(s, x, residual, y);
         a.x = static_cast<const M*>(x);
         a.side = static_cast<const M*>(residual);
         a.y = static_cast<M*>(y);
@@ -509,7 +509,7 @@ hipError_t launch_norm(const gpga_ctx* c, const RowsShape& s, const DropArgs& dr
         a.ld = s.ld;
         a.ldx = c->ld;
         a.drop = drop;
-        a.stream = stream_rows(s);
+        a.stream = stream_rows(s, x, residual, u, y);
         a.eps = eps;
         a.x = static_cast<const M*>(x);
         a.side = static_cast<const M*>(residual);
@@ -548,7 +548,7 @@ hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArg
         a.ld = s.ld;
         a.ldx = c->ld;
         a.drop = drop;
-        a.stream = stream_rows(s);
+        a.stream = stream_rows(s, du, dx);
         a.x = static_cast<const M*>(dy);
         a.side = static_cast<const M*>(more);
         a.u_in = static_cast<const M*>(u);

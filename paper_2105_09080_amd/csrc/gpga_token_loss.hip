@@ -107,7 +107,7 @@ __device__ __forceinline__ void less_at(float* v, int32_t at, float by) {
 // ---- rows held in registers: L lanes a row, N pieces of eight columns a lane ------------------------------------------------
 template <typename E, int L, int N>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossArgs<E> a) {
-    constexpr int kBlock = L > kThreads ? L : kThreads, kRows = kBlock / L, kWaves = kBlock / kWave, kRowWaves = L / kWave;
+    constexpr int kBlock = L > kThreads ? L : kThreads, kRows = kBlock / L, kWaves = kBlock / kWave, kRowWaves = L / kWave, kLanes = L < kWave ? L : kWave;
     __shared__ float s_max[kWaves], s_sum[kWaves];
     __shared__ int32_t s_count[kWaves], s_last;
     __shared__ double s_total[kWaves];
@@ -144,8 +144,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
                 e[k][j] = __expf(e[k][j] - mine);
                 sum += e[k][j];
             }
-        top = wave_max<kWave>(mine);
-        sum = wave_sum<kWave>(sum * __expf(mine - top));
+        top = wave_max<kLanes>(mine);
+        sum = wave_sum<kLanes>(sum * __expf(mine - top));
     }
     if constexpr (L > kWave) {
         if ((threadIdx.x & (kWave - 1)) == 0) {
@@ -205,42 +205,52 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
 }
 
 // ---- rows in pieces: a workgroup for each ------------------------------------------------------------------------------------
-// Maximum and sum of exp(z - maximum) of a row from those of its pieces, by a wavefront; all lanes get them.
+// Maximum and sum of exp(z - maximum) of a row from those of its pieces, by an aligned group of lanes (a power of two up to 64); all
+// of them get both.
 struct MaxSum {
     float top, sum;
 };
-__device__ __forceinline__ MaxSum join_parts(const float* parts, uint32_t pieces) {
-    const uint32_t lane = threadIdx.x & (kWave - 1);
+__device__ __forceinline__ MaxSum join_parts(const float* parts, uint32_t pieces, uint32_t lanes) {
     auto part = [&](uint32_t k) { return __hip_atomic_load(parts + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-    MaxSum mine = {kLowest, 0.f}, all;
-    for (uint32_t k = lane; k < pieces; k += kWave) {
-        const float top = part(2 * k), sum = part(2 * k + 1), most = fmaxf(mine.top, top);
-        mine.sum = mine.sum * __expf(mine.top - most) + sum * __expf(top - most);
-        mine.top = most;
+    MaxSum all = {kLowest, 0.f};
+    for (uint32_t k = threadIdx.x & (lanes - 1); k < pieces; k += lanes) {
+        const float top = part(2 * k), sum = part(2 * k + 1), most = fmaxf(all.top, top);
+        all.sum = all.sum * __expf(all.top - most) + sum * __expf(top - most);
+        all.top = most;
     }
-    all.top = wave_max<kWave>(mine.top);
-    all.sum = wave_sum<kWave>(mine.sum * __expf(mine.top - all.top));
+    for (uint32_t off = lanes / 2; off > 0; off >>= 1) {
+        const float top = __shfl_xor(all.top, off, kWave), sum = __shfl_xor(all.sum, off, kWave), most = fmaxf(all.top, top);
+        all.sum = all.sum * __expf(all.top - most) + sum * __expf(top - most);
+        all.top = most;
+    }
     return all;
 }
+__device__ __forceinline__ uint32_t join_lanes(uint32_t pieces) {
+    uint32_t lanes = 1;
+    while (lanes < pieces && lanes < kWave) lanes *= 2;
+    return lanes;
+}
 
-// Loss of a node whose rows are in pieces, by a workgroup: a wavefront a row in turn.
+// Loss of a node whose rows are in pieces, by a workgroup: a group of lanes a row in turn.
 template <typename E>
 __device__ __forceinline__ void node_loss_parts(const LossArgs<E>& a, uint32_t node, int32_t* s_count, double* s_total) {
-    constexpr int kWaves = kThreads / kWave;
     const int64_t first = (int64_t)node * a.T;
-    const int32_t counted = count_labels(a.labels + first, a.T, kThreads, s_count), wave = threadIdx.x / kWave;
+    const int32_t counted = count_labels(a.labels + first, a.T, kThreads, s_count);
+    const uint32_t lanes = join_lanes(a.pieces);
     double mine = 0.0;
-    for (int32_t t = wave; t < a.T; t += kWaves) {
+    for (int64_t t = threadIdx.x / lanes; t < a.T; t += kThreads / lanes) {
         const int64_t r = first + t;
         const int32_t label = a.labels[r];
+        const float picked = label >= 0 && label < a.V ? E::get(a.z[r * a.ld + label]) : __builtin_nanf("");
         if (label < 0) continue;
-        const MaxSum all = join_parts(a.parts + r * 2 * a.pieces, a.pieces);
-        mine += label >= a.V ? (double)__builtin_nanf("") : (double)(logf(all.sum) + (all.top - E::get(a.z[r * a.ld + label])));
+        const MaxSum all = join_parts(a.parts + r * 2 * a.pieces, a.pieces, lanes);
+        if ((threadIdx.x & (lanes - 1)) == 0) mine += (double)(logf(all.sum) + (all.top - picked));
     }
-    if ((threadIdx.x & (kWave - 1)) == 0) s_total[wave] = mine;
+    mine = wave_sum64(mine);
+    if ((threadIdx.x & (kWave - 1)) == 0) s_total[threadIdx.x / kWave] = mine;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kWaves; ++w) mine += s_total[w];
+        for (int w = 1; w < kThreads / kWave; ++w) mine += s_total[w];
         a.loss[node] = counted > 0 ? (float)(mine / counted) : 0.f;
     }
 }
@@ -313,7 +323,7 @@ __global__ __launch_bounds__(kThreads) void k_loss_parts_grad(LossArgs<E> a) {
         return;
     }
     const int32_t counted = a.count ? a.count[node] : count_labels(a.labels + (int64_t)node * a.T, a.T, kThreads, s_count);
-    const MaxSum all = join_parts(a.parts + r * 2 * a.pieces, a.pieces);
+    const MaxSum all = join_parts(a.parts + r * 2 * a.pieces, a.pieces, kWave);
     const float scale = label >= a.V ? __builtin_nanf("") : a.grad_scale / (float)counted, share = scale / all.sum;
     for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) {
         piece_read<kOct, E>(z, c, a.V, v);
@@ -331,7 +341,9 @@ struct Const {
 // Lanes a row and pieces a lane by the number of eights in it: the smallest that hold it.
 template <typename E, typename F>
 bool with_row_shape(int32_t octs, F&& f) {
-    if constexpr (E::kNarrow) f(Const<64>(), Const<1>());
+    if constexpr (E::kNarrow) f(Const<16>(), Const<1>());
+    else if (octs <= 16) f(Const<16>(), Const<1>());
+    else if (octs <= 32) f(Const<32>(), Const<1>());
     else if (octs <= 64) f(Const<64>(), Const<1>());
     else if (octs <= 128) f(Const<64>(), Const<2>());
     else if (octs <= 256) f(Const<64>(), Const<4>());
@@ -372,7 +384,7 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
     int32_t* count = static_cast<int32_t*>(scratch);
     float* rows = reinterpret_cast<float*>(count + s.n);
     // the launch's last workgroup of a node adds up its losses, unless so many end there that they would queue for the counter
-    constexpr int64_t kMostAtCounter = 2048;
+    constexpr int64_t kMostAtCounter = 64;
     auto counter = [&](int64_t per_node) { return c->loss_left && s.n <= 65535 && per_node <= kMostAtCounter ? c->loss_left : nullptr; };
     auto count_launch = [&]() {
         k_count<<<dim3((uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(labels, s.T, count);
@@ -388,7 +400,7 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
         a.labels = labels;
         a.dz = static_cast<typename E::mem*>(dlogits);
         a.grad_scale = grad_scale;
-        a.stream = stream_rows(s);
+        a.stream = stream_rows(s, logits, dlogits);
         a.loss = loss;
         const uint32_t all = (uint32_t)s.n * (uint32_t)s.T;
         if (cut.pieces) {
@@ -421,7 +433,7 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
             a.per_node = blocks_for(s.T, kBlock / L);
             a.left = counter(a.per_node);
             // the labels of a node are counted beside the loads of a row where they are few to its columns
-            if (!a.left || s.T > 4 * L) {
+            if (!a.left || s.T > 4 * kBlock) {
                 a.count = count;
                 e = count_launch();
             }
