@@ -34,6 +34,7 @@ _TAG_GENERIC = 11
 _TAG_SIM_XSTAR = 12
 _TAG_SIM_FEAT = 13
 _TAG_SIM_LABEL = 14
+_TAG_TEXT = 15
 
 #: Named workloads.  ``H == 0`` encodes "never average" (H -> infinity).
 #: ``topologies`` lists the mixing graphs the workload is run with.
@@ -166,3 +167,23 @@ def slab_columns(d: int, n_slabs: int, width: int, align: int = 4) -> np.ndarray
         starts[-1] = d - width
     cols = (starts[:, None] + np.arange(width, dtype=np.int64)[None, :]).ravel()
     return np.unique(cols)
+
+
+def markov_text(iters: int, n: int, sequences: int, length: int, V: int, seed: int = 0, shared: float = 0.6, own: float = 0.2):
+    """Synthetic text for a language model on n nodes: (iters, n, sequences, length + 1) int32 tokens below V.
+
+    The token after (a, b) is a fixed random successor of b with probability ``shared`` (the same one on all nodes), one
+    of a that is the node's own with probability ``own`` (what makes the nodes' data differ), else uniform.  A piece has
+    ``length`` + 1 tokens: the inputs and, one place on, what they are to predict.
+    """
+    g = _rng(seed, _TAG_TEXT)
+    common = g.integers(0, V, size=V)
+    node = g.integers(0, V, size=(n, V))
+    text = np.empty((iters, n, sequences, length + 1), dtype=np.int32)
+    text[..., :2] = g.integers(0, V, size=(iters, n, sequences, 2))
+    i = np.arange(n)[None, :, None]
+    for t in range(2, length + 1):
+        a, b, u = text[..., t - 2], text[..., t - 1], g.random((iters, n, sequences))
+        pick = np.where(u < shared, common[b], node[i, a])
+        text[..., t] = np.where(u < shared + own, pick, g.integers(0, V, size=u.shape))
+    return text
