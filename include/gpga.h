@@ -16,8 +16,8 @@
  * Data layout: every state array is node-major fp32, row i = node i, with a
  * common leading dimension ld >= d (in floats).  All pointers named *_dev are
  * DEVICE pointers owned by the caller.  The library owns the context, small scratch for
- * reductions and per-sample coefficients, that of the language-model operators (as large as their calls
- * need), and, a device, the memory through which gpga_run exchanges
+ * reductions and per-sample coefficients, that of the language-model operators (what their largest call
+ * needs, and the smaller ones it has outgrown, up to twice as much again), and, a device, the memory through which gpga_run exchanges
  * margins and iterates on stored features (option "rows_run"; as large as the launches made so far
  * need, n x d x 8 bytes for each of their up to 32 iterations, at most 64 MiB of these, and the margins;
  * all contexts share it, and what is over 8 MiB of it goes with the last one).  Work is enqueued on the stream given to
@@ -389,10 +389,11 @@ gpga_status gpga_query(gpga_ctx* ctx, const char* name, double* value_out);
  * elements of one type, fp32, bf16 or fp16, with a common leading dimension ld (in elements) for all activations of a call.  Pointers need
  * the alignment of their elements.  Arithmetic and sums are fp32 or wider; results are rounded to the activations' type
  * once, to nearest even.  An output may take the exact place of an input of the call; any other overlap of an output with
- * an input, another output or a bound array is EINVAL (columns of one wider array do not overlap).  tokens_dev and
+ * an input, another output or a bound array is EINVAL (columns of one wider array do not overlap), and so are inputs of a
+ * gradient within g_dev.  tokens_dev and
  * labels_dev are n x T int32.  Results do not depend on the order in which workgroups run: the same call gives the same
- * bits.  Asynchronous on the bound stream, but for scratch that has to grow (the embedding's and the layer norm's
- * gradients and the loss use some; it is kept for later calls). */
+ * bits.  Asynchronous on the bound stream; the embedding's and the layer norm's gradients and the loss use scratch, which
+ * grows with the largest call and stays until gpga_destroy (a first call of its size cannot be captured into a graph). */
 typedef enum { GPGA_F32 = 0, GPGA_BF16 = 1, GPGA_F16 = 2 } gpga_dtype;
 
 /* y[i,t,:] = scale * E_i[tokens[i,t],:], E_i the V x D table (row-major, dense) in columns table_off .. table_off + V*D

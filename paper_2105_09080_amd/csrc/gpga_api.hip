@@ -308,6 +308,7 @@ gpga_status gpga_destroy(gpga_ctx* c) {
     if (c->aga_loss) (void)hipFree(c->aga_loss);
     if (c->partials) (void)hipFree(c->partials);
     if (c->op_scratch) (void)hipFree(c->op_scratch);
+    for (int k = 0; k < c->op_outgrown_count; ++k) (void)hipFree(c->op_outgrown[k]);
     if (c->pace_states) (void)hipFree(c->pace_states);
     gang_leave(c);
     free_csr_device(c);

@@ -102,6 +102,8 @@ enum StepPath : int { PATH_NONE = 0, PATH_WALK = 1, PATH_CYCLES = 2, PATH_GLOBAL
                       PATH_TWO_PASS = 6, PATH_SMALL_RUN = 7, PATH_COLUMN_RUN = 8, PATH_ROWS_STEP = 9,
                       PATH_CIRCULANT = 10, PATH_VIRTUAL_STEP = 11, PATH_ROWS_RUN = 12 };
 
+constexpr int kMaxOutgrown = 128;  // each scratch is half as large again as the one before it: more than memory has room for
+
 constexpr int kLossLeftStride = 32;  // counters of gpga_ctx::loss_left, a line each
 
 struct gpga_ctx {
@@ -221,9 +223,12 @@ struct gpga_ctx {
     float* aga_loss = nullptr;  // n minibatch losses (library-owned; used by gpga_run)
     size_t aga_loss_cap = 0;
 
-    // language-model operators: scratch of the call under way on the bound stream (library-owned)
+    // language-model operators: scratch of the call under way on the bound stream (library-owned), and the smaller ones before it,
+    // which launches under way and captured graphs may still use
     char* op_scratch = nullptr;
     size_t op_scratch_cap = 0;  // bytes
+    char* op_outgrown[kMaxOutgrown] = {nullptr};
+    int op_outgrown_count = 0;
 
     char err[256] = {0};
 };

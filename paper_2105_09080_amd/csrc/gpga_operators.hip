@@ -32,17 +32,21 @@ struct DeviceGuard {
     }
 };
 
-// Scratch of one call; calls follow each other on the bound stream, so they share it.
+// Scratch of one call; calls follow each other on the bound stream, so they share it.  What it outgrows stays until the context
+// goes: a captured graph may hold its address.
 gpga_status reserve(gpga_ctx* c, size_t bytes) {
     if (c->op_scratch_cap >= bytes) return GPGA_OK;
-    hipError_t e = hipStreamSynchronize(c->stream);
-    if (e != hipSuccess) return hip_fail(c, e, "hipStreamSynchronize");
-    if (c->op_scratch) (void)hipFree(c->op_scratch);
-    c->op_scratch = nullptr;
-    c->op_scratch_cap = 0;
-    e = hipMalloc(reinterpret_cast<void**>(&c->op_scratch), bytes);
+    constexpr size_t kLeast = (size_t)1 << 20;
+    size_t want = c->op_scratch_cap + c->op_scratch_cap / 2;
+    if (want < bytes) want = bytes;
+    if (want < kLeast) want = kLeast;
+    if (c->op_scratch && c->op_outgrown_count == kMaxOutgrown) return fail(c, GPGA_ENOMEM, "scratch has grown %d times", kMaxOutgrown);
+    char* more = nullptr;
+    const hipError_t e = hipMalloc(reinterpret_cast<void**>(&more), want);
     if (e != hipSuccess) return hip_fail(c, e, "hipMalloc(scratch)");
-    c->op_scratch_cap = bytes;
+    if (c->op_scratch) c->op_outgrown[c->op_outgrown_count++] = c->op_scratch;
+    c->op_scratch = more;
+    c->op_scratch_cap = want;
     return GPGA_OK;
 }
 
@@ -73,8 +77,9 @@ gpga_status check_ready(gpga_ctx* c) {
     return GPGA_OK;
 }
 
-// Shape and arrays common to all operators.  Outputs may take the place of an input exactly, and overlap nothing else.
-gpga_status check_rows(gpga_ctx* c, const RowsShape& s, const Array* arrays, int count) {
+// Shape and arrays common to all operators.  Outputs may take the place of an input exactly, and overlap nothing else; no input of a
+// call that writes gradients lies in g.
+gpga_status check_rows(gpga_ctx* c, const RowsShape& s, const Array* arrays, int count, bool writes_g = false) {
     if (s.dtype < GPGA_F32 || s.dtype > GPGA_F16) return fail(c, GPGA_EINVAL, "dtype %d is not a gpga_dtype", s.dtype);
     if (s.T < 0 || s.T > kMaxTokens) return fail(c, GPGA_EINVAL, "T = %d must be 0..%d", s.T, kMaxTokens);
     if (s.D < 1 || s.D > kMaxRow) return fail(c, GPGA_EINVAL, "a row has %d elements: it needs 1..%d", s.D, kMaxRow);
@@ -94,18 +99,38 @@ gpga_status check_rows(gpga_ctx* c, const RowsShape& s, const Array* arrays, int
         if (!arrays[k].p) continue;
         const uintptr_t p = reinterpret_cast<uintptr_t>(arrays[k].p);
         if (p & (uintptr_t)(size - 1)) return fail(c, GPGA_EINVAL, "%s is not aligned to its elements", arrays[k].name);
-        if (!arrays[k].out) continue;
         for (const auto& h : held) {
+            if (!arrays[k].out && !(writes_g && h.p == c->g)) continue;
             const uintptr_t q = reinterpret_cast<uintptr_t>(h.p);
             if (h.p && p < q + state && q < p + (uintptr_t)bytes)
                 return fail(c, GPGA_EINVAL, "%s overlaps the bound array %s", arrays[k].name, h.name);
         }
+        if (!arrays[k].out) continue;
         for (int j = 0; j < count; ++j) {
             if (j == k || !arrays[j].p || (arrays[j].p == arrays[k].p && !arrays[j].out)) continue;
             if (rows_meet(arrays[k].p, arrays[j].p, rows, s.ld * size, s.D * size))
                 return fail(c, GPGA_EINVAL, "%s and %s overlap", arrays[k].name, arrays[j].name);
         }
     }
+    return GPGA_OK;
+}
+
+// `floats` of fp32 that the call reads or writes beside its rows: they share no byte with an output or, written, with any array.
+gpga_status check_floats(gpga_ctx* c, const RowsShape& s, const char* name, const float* p, int64_t floats, bool out, const Array* arrays, int count) {
+    if (!p || !floats) return GPGA_OK;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p), to = from + (uintptr_t)floats * sizeof(float);
+    auto meets = [&](const void* q, int64_t bytes) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(q);
+        return q && from < at + (uintptr_t)bytes && at < to;
+    };
+    const int64_t size = elem_size(s.dtype), rows = (int64_t)s.n * s.T;
+    for (int k = 0; k < count; ++k)
+        if (rows && (out || arrays[k].out) && meets(arrays[k].p, ((rows - 1) * s.ld + s.D) * size))
+            return fail(c, GPGA_EINVAL, "%s and %s overlap", name, arrays[k].name);
+    const int64_t state = (int64_t)c->n * c->ld * (int64_t)sizeof(float);
+    const float* held[4] = {c->x, c->x_new, c->m, c->g};
+    for (const float* h : held)
+        if ((out || h == c->g) && meets(h, state)) return fail(c, GPGA_EINVAL, "%s overlaps a bound array", name);
     return GPGA_OK;
 }
 
@@ -180,7 +205,7 @@ gpga_status gpga_embed_grad(gpga_ctx* c, const int32_t* tokens, int32_t T, int64
     const RowsShape s = {c->n, T, D, ld, dtype};
     const Array arrays[] = {{"dy_dev", dy, false}};
     GPGA_TRY(check_table(c, table_off, V, D));
-    GPGA_TRY(check_rows(c, s, arrays, 1));
+    GPGA_TRY(check_rows(c, s, arrays, 1, true));
     GPGA_TRY(check_ints(c, "tokens_dev", tokens, T));
     if (!std::isfinite(scale)) return fail(c, GPGA_EINVAL, "scale must be finite");
     if (accumulate != 0 && accumulate != 1) return fail(c, GPGA_EINVAL, "accumulate must be 0 or 1");
@@ -219,6 +244,7 @@ gpga_status gpga_layer_norm(gpga_ctx* c, const void* x, const void* residual, in
     GPGA_TRY(check_columns(c, "beta", beta_off, D));
     if (!(std::isfinite(eps) && eps >= 0.f)) return fail(c, GPGA_EINVAL, "eps must be finite and >= 0");
     if (reinterpret_cast<uintptr_t>(stats) & 3u) return fail(c, GPGA_EINVAL, "stats_dev is not 4-byte aligned");
+    GPGA_TRY(check_floats(c, s, "stats_dev", stats, 2 * (int64_t)c->n * T, true, arrays, 4));
     DropArgs drop;
     GPGA_TRY(make_drop(c, s, p, seed, layer, &drop));
     if (T == 0) return GPGA_OK;
@@ -235,12 +261,13 @@ gpga_status gpga_layer_norm_grad(gpga_ctx* c, const void* dy, const void* u, con
     GPGA_TRY(check_ready(c));
     const RowsShape s = {c->n, T, D, ld, dtype};
     const Array arrays[] = {{"dy_dev", dy, false}, {"u_dev", u, false}, {"more_dev", more, false}, {"du_dev", du, true}, {"dx_dev", dx, true}};
-    GPGA_TRY(check_rows(c, s, arrays, 5));
+    GPGA_TRY(check_rows(c, s, arrays, 5, true));
     GPGA_TRY(check_columns(c, "gamma", gamma_off, D));
     GPGA_TRY(check_columns(c, "beta", beta_off, D));
     if (gamma_off < beta_off + D && beta_off < gamma_off + D) return fail(c, GPGA_EINVAL, "the columns of gamma and beta overlap");
     if (reinterpret_cast<uintptr_t>(stats) & 3u) return fail(c, GPGA_EINVAL, "stats_dev is not 4-byte aligned");
     if (accumulate != 0 && accumulate != 1) return fail(c, GPGA_EINVAL, "accumulate must be 0 or 1");
+    GPGA_TRY(check_floats(c, s, "stats_dev", stats, 2 * (int64_t)c->n * T, false, arrays, 5));
     DropArgs drop;
     GPGA_TRY(make_drop(c, s, p, seed, layer, &drop));
     if (T > 0 && (!dy || !u || !stats || !du)) return fail(c, GPGA_EINVAL, "dy_dev, u_dev, stats_dev and du_dev must not be NULL");
@@ -264,6 +291,7 @@ gpga_status gpga_token_loss(gpga_ctx* c, const void* logits, const int32_t* labe
     if (!std::isfinite(grad_scale)) return fail(c, GPGA_EINVAL, "grad_scale must be finite");
     if (!loss || (reinterpret_cast<uintptr_t>(loss) & 3u)) return fail(c, GPGA_EINVAL, "loss_dev must be a 4-byte aligned device pointer");
     if (T > 0 && !logits) return fail(c, GPGA_EINVAL, "logits_dev must not be NULL");
+    GPGA_TRY(check_floats(c, s, "loss_dev", loss, c->n, true, arrays, 2));
     DeviceGuard guard(c->device);
     GPGA_TRY(reserve(c, token_loss_scratch(s, c->num_cus)));
     const hipError_t e = launch_token_loss(c, s, logits, labels, grad_scale, loss, dlogits, c->op_scratch);

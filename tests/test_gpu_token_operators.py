@@ -488,6 +488,29 @@ def test_captured_into_a_graph(hx):
     sim.close()
 
 
+def test_a_graph_outlives_the_scratch_it_was_captured_with(hx):
+    n, T = 4, 40
+    side = torch.cuda.Stream()
+    sim, X, rng = make_sim(hx, n, 50 * 24 + 48, seed=13, stream=side)
+    tokens, labels, x = _chain_inputs(rng, n, T)
+    large = _chain_inputs(rng, n, 60_000)                          # its gradients need more than the first megabyte
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        want = [t.clone() for t in (*_all_operators(sim, tokens, labels, x, None), sim.G)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            got = _all_operators(sim, tokens, labels, x, None)
+        for _ in range(3):
+            other = [t.clone() for t in (*_all_operators(sim, *large, None), sim.G)]
+            graph.replay()
+            side.synchronize()
+            for w, g in zip(want, (*got, sim.G)):
+                assert torch.equal(w, g)
+            for o, g in zip(other, (*_all_operators(sim, *large, None), sim.G)):
+                assert torch.equal(o, g)
+    sim.close()
+
+
 def test_refusals(hx):
     from paper_2105_09080_amd import binding as B
     n, V, D, T = 2, 6, 8, 3
@@ -530,6 +553,12 @@ def test_refusals(hx):
     for kw, says in ((dict(st=None), "NULL"), (dict(du=None), "NULL"), (dict(p=0.5), "dx_dev"), (dict(dx=a.data_ptr() + 4), "overlap"),
                      (dict(b=goff + 1), "overlap"), (dict(dx=torch.zeros_like(a)), "dx_dev")):
         no(B.gpga_layer_norm_grad, *grad(**kw), says=says)
+    no(B.gpga_embed_grad, tok, T, 0, V, D, 1.0, sim.g.data_ptr(), D, 0, False, says="bound array")
+    no(B.gpga_layer_norm_grad, *grad(dy=sim.g.data_ptr()), says="bound array")
+    no(B.gpga_layer_norm_grad, *grad(st=c.data_ptr()), says="stats_dev")
+    no(B.gpga_layer_norm, *norm()[:-1], b.data_ptr(), says="stats_dev")
+    no(B.gpga_token_loss, a, tok, T, D, D, 0, 1.0, sim.X.data_ptr(), None, says="loss_dev")
+    no(B.gpga_token_loss, a, tok, T, D, D, 0, 1.0, b.data_ptr() + 8, b, says="loss_dev")
     no(B.gpga_token_loss, None, tok, T, D, D, 0, 1.0, loss, None, says="NULL")
     no(B.gpga_token_loss, a, None, T, D, D, 0, 1.0, loss, None, says="NULL")
     no(B.gpga_token_loss, a, tok, T, D, D, 0, 1.0, None, None, says="loss_dev")
