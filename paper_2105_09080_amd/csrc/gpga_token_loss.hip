@@ -10,6 +10,10 @@
 // A row is read once: L lanes hold it as exp(z - m_lane) in fp32, m_lane the largest value of the lane, and one pass over
 // the lanes joins maxima and sums; the gradient is what is held times exp(m_lane - m) a / (N sum).  Few or very long rows are cut
 // into pieces for a workgroup each, and a second launch reads them again for the gradient.
+//
+// Bound by the logits' bytes: 8 x 512 rows of 32000 bf16 with the gradient in 90 us (5.5 TB/s; three readings of a row took 164).  A
+// compute unit holds two such rows, so loads, sums and stores of two rows overlap and no more; holding rows as they lie in
+// memory and taking exp twice was slower at every number of lanes (130 to 180 us, registers).  One row of 128000 fp32 a node: 5 us.
 #include "gpga_rows.hpp"
 
 namespace {

@@ -108,7 +108,7 @@ def test_embedding(hx, n, T, V, D, off, pad, kind, dtype):
     sim.close()
 
 
-@pytest.mark.parametrize("T", [1024, 1025, 4095, 4096, 4097, 8191, 8192, 8193, 20000])
+@pytest.mark.parametrize("T", [1024, 1025, 4095, 4096, 4097, 8191, 8192, 8193, 20000, 40_000])
 @pytest.mark.parametrize("V", [2, 255, 256, 257, 1021, 1023, 1024, 70_000])
 def test_embedding_gradient_across_the_tiles_of_the_sort(hx, T, V):
     n, D = 2, 8
