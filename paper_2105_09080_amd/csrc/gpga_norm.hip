@@ -11,7 +11,7 @@
 // before u is rounded for its own store.
 //
 // All of it is bound by the bytes of the activations: a row is read once, held in the registers of the lanes that share it, and
-// its results are written once.  As many lanes share a row as hold it in one to three pieces each (16 to 64 of a wavefront,
+// its results are written once.  As many lanes share a row as hold it in one to three pieces each (8 to 64 of a wavefront,
 // whose sums need no LDS, then a workgroup); rows of more than 8192 columns are read again.
 #include "gpga_rows.hpp"
 
@@ -254,6 +254,7 @@ __device__ __forceinline__ void grad_output(const NormArgs<E>& a, const DropNode
 // Sum over the rows that a wavefront works on side by side, L lanes each; lane by lane.
 template <int L>
 __device__ __forceinline__ float other_rows_sum(float v) {
+    if constexpr (L <= 8) v += dpp<0x128>(v);  // the eight lanes beside
     if constexpr (L <= 16) {
         const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
@@ -482,7 +483,8 @@ struct Const {
 };
 template <typename E, typename F>
 bool with_row_shape(int32_t octs, F&& f) {
-    if constexpr (E::kNarrow) f(Const<16>(), Const<1>());
+    if constexpr (E::kNarrow) f(Const<8>(), Const<1>());
+    else if (octs <= 8) f(Const<8>(), Const<1>());
     else if (octs <= 16) f(Const<16>(), Const<1>());
     else if (octs <= 32) f(Const<32>(), Const<1>());
     else if (octs <= 64) f(Const<32>(), Const<2>());

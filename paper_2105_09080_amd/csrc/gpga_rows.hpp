@@ -144,7 +144,7 @@ __device__ __forceinline__ void piece_put(typename E::mem* row, int32_t c, int32
 }
 
 // ---- sums and maxima over the lanes that share a row -----------------------------------------------------------------------
-// All of an aligned group of L lanes of a wavefront, L = 16, 32 or 64; every lane gets the same bits.  Lanes of 16 by DPP
+// All of an aligned group of L lanes of a wavefront, L = 8, 16, 32 or 64; every lane gets the same bits.  Lanes of 16 by DPP
 // (exchange with the neighbour, the pair, the mirrored eight, the mirrored sixteen), rows of 16 by the swaps of gfx950; no
 // LDS.
 template <int kCtrl>
@@ -156,7 +156,7 @@ __device__ __forceinline__ float wave_all(float v, F&& f) {
     v = f(v, dpp<0xb1>(v));
     v = f(v, dpp<0x4e>(v));
     v = f(v, dpp<0x141>(v));
-    v = f(v, dpp<0x140>(v));
+    if constexpr (L > 8) v = f(v, dpp<0x140>(v));
     if constexpr (L > 16) {
         const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = f(__uint_as_float(s[0]), __uint_as_float(s[1]));

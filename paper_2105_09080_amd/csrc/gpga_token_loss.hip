@@ -19,6 +19,7 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kNodeThreads = 1024;  // of the launches that take a node a workgroup
 constexpr float kLowest = -3.402823466e38f;  // stands for -inf as a maximum: -inf - kLowest is -inf and not NaN
 
 uint32_t blocks_for(int64_t items, int64_t per_block) { return (uint32_t)((items + per_block - 1) / per_block); }
@@ -53,8 +54,11 @@ __device__ __forceinline__ double wave_sum64(double v) {
 // Counted tokens among labels[0 .. T), by a workgroup of `threads`; `lds` one word a wavefront.  Holds a barrier.
 __device__ __forceinline__ int32_t count_labels(const int32_t* __restrict__ labels, int32_t T, int32_t threads, int32_t* lds) {
     int32_t mine = 0;
-    for (int32_t t = threadIdx.x; t < T; t += threads) mine += __builtin_popcountll(__ballot(labels[t] >= 0));
-    if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = mine;  // its turns are those of the wavefront
+#pragma unroll 4
+    for (int32_t t = threadIdx.x; t < T; t += threads) mine += labels[t] >= 0 ? 1 : 0;
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1) mine += __shfl_xor(mine, off, kWave);
+    if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = mine;
     __syncthreads();
     mine = 0;
     for (int32_t w = 0; w < threads / kWave; ++w) mine += lds[w];
@@ -65,7 +69,13 @@ __device__ __forceinline__ int32_t count_labels(const int32_t* __restrict__ labe
 template <typename F>
 __device__ __forceinline__ void node_loss(int32_t T, int32_t threads, int32_t counted, double* lds, float* loss, F&& row) {
     double mine = 0.0;
-    for (int32_t t = threadIdx.x; t < T; t += threads) mine += (double)row(t);
+    for (int64_t t = threadIdx.x; t < T; t += 4 * threads) {  // four loads under way
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = t + k * threads < T ? row((int32_t)(t + k * threads)) : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mine += (double)v[k];
+    }
     mine = wave_sum64(mine);
     if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = mine;
     __syncthreads();
@@ -84,20 +94,20 @@ __device__ __forceinline__ void note_end(uint32_t* left, uint32_t workgroups, in
     *last = is;
 }
 
-__global__ __launch_bounds__(kThreads) void k_count(const int32_t* __restrict__ labels, int32_t T, int32_t* __restrict__ count) {
-    __shared__ int32_t s_count[kThreads / kWave];
-    const int32_t n = count_labels(labels + (int64_t)blockIdx.x * T, T, kThreads, s_count);
+__global__ __launch_bounds__(kNodeThreads) void k_count(const int32_t* __restrict__ labels, int32_t T, int32_t* __restrict__ count) {
+    __shared__ int32_t s_count[kNodeThreads / kWave];
+    const int32_t n = count_labels(labels + (int64_t)blockIdx.x * T, T, kNodeThreads, s_count);
     if (threadIdx.x == 0) count[blockIdx.x] = n;
 }
 
 // Where the losses of a node are not added up by the last workgroup of the launch that makes them.
-__global__ __launch_bounds__(kThreads) void k_loss_mean(const float* __restrict__ row_loss, const int32_t* __restrict__ labels, int32_t T,
+__global__ __launch_bounds__(kNodeThreads) void k_loss_mean(const float* __restrict__ row_loss, const int32_t* __restrict__ labels, int32_t T,
                                                         float* __restrict__ loss) {
-    __shared__ int32_t s_count[kThreads / kWave];
-    __shared__ double s_sum[kThreads / kWave];
+    __shared__ int32_t s_count[kNodeThreads / kWave];
+    __shared__ double s_sum[kNodeThreads / kWave];
     const float* rows = row_loss + (int64_t)blockIdx.x * T;
-    const int32_t counted = count_labels(labels + (int64_t)blockIdx.x * T, T, kThreads, s_count);
-    node_loss(T, kThreads, counted, s_sum, loss + blockIdx.x, [&](int32_t t) { return rows[t]; });
+    const int32_t counted = count_labels(labels + (int64_t)blockIdx.x * T, T, kNodeThreads, s_count);
+    node_loss(T, kNodeThreads, counted, s_sum, loss + blockIdx.x, [&](int32_t t) { return rows[t]; });
 }
 
 // Columns past the end of the row take no part.
@@ -395,7 +405,7 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
     constexpr int64_t kMostAtCounter = 256;
     auto counter = [&](int64_t per_node) { return c->loss_left && s.n <= 65535 && per_node <= kMostAtCounter ? c->loss_left : nullptr; };
     auto count_launch = [&]() {
-        k_count<<<dim3((uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(labels, s.T, count);
+        k_count<<<dim3((uint32_t)s.n), dim3(kNodeThreads), 0, c->stream>>>(labels, s.T, count);
         return hipGetLastError();
     };
     auto launch = [&](auto el) {
@@ -450,11 +460,11 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
             e = hipGetLastError();
         });
         if (e != hipSuccess || a.left) return e;
-        k_loss_mean<<<dim3((uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(rows, labels, s.T, loss);
+        k_loss_mean<<<dim3((uint32_t)s.n), dim3(kNodeThreads), 0, c->stream>>>(rows, labels, s.T, loss);
         return hipGetLastError();
     };
     if (s.T == 0) {  // losses of 0
-        k_loss_mean<<<dim3((uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(rows, labels, 0, loss);
+        k_loss_mean<<<dim3((uint32_t)s.n), dim3(kNodeThreads), 0, c->stream>>>(rows, labels, 0, loss);
         return hipGetLastError();
     }
     return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
