@@ -221,6 +221,100 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
     }
 }
 
+// ---- rows that registers do not hold: columns from .. to of a row, by kLanes lanes ------------------------------------------
+constexpr int kPiecesAhead = 4;  // of a lane, whose loads are under way together
+
+// Running maximum and sum of exp(z - maximum) of a lane.
+template <typename E, int kLanes>
+__device__ __forceinline__ void sweep_sum(const typename E::mem* z, int32_t from, int32_t to, int32_t V, float* top_out, float* sum_out) {
+    float top = kLowest, sum = 0.f;
+    for (int32_t c0 = from + (int32_t)threadIdx.x * kOct; c0 < to; c0 += kPiecesAhead * kLanes * kOct) {
+        Piece<E, kOct> in[kPiecesAhead];
+#pragma unroll
+        for (int k = 0; k < kPiecesAhead; ++k) in[k] = piece_load<kOct, E>(z, c0 + k * kLanes * kOct, V);
+#pragma unroll
+        for (int k = 0; k < kPiecesAhead; ++k) {
+            const int32_t c = c0 + k * kLanes * kOct;
+            if (c >= to) break;
+            float v[kOct], most = top;
+            piece_get<kOct, E>(in[k], c, V, v);
+            if (c + kOct > V) past_end(v, c, V);
+#pragma unroll
+            for (int j = 0; j < kOct; ++j) most = fmaxf(most, v[j]);
+            sum *= __expf(top - most);
+            top = most;
+#pragma unroll
+            for (int j = 0; j < kOct; ++j) sum += __expf(v[j] - top);
+        }
+    }
+    *top_out = top;
+    *sum_out = sum;
+}
+// The gradient, exp(z - top) * share less scale at the label.
+template <typename E, int kLanes>
+__device__ __forceinline__ void sweep_grad(const typename E::mem* z, typename E::mem* dz, int32_t from, int32_t to, int32_t V, int32_t label, float top,
+                                           float share, float scale, bool stream) {
+    for (int32_t c0 = from + (int32_t)threadIdx.x * kOct; c0 < to; c0 += kPiecesAhead * kLanes * kOct) {
+        Piece<E, kOct> in[kPiecesAhead];
+#pragma unroll
+        for (int k = 0; k < kPiecesAhead; ++k) in[k] = piece_load<kOct, E>(z, c0 + k * kLanes * kOct, V);
+#pragma unroll
+        for (int k = 0; k < kPiecesAhead; ++k) {
+            const int32_t c = c0 + k * kLanes * kOct;
+            if (c >= to) break;
+            float v[kOct];
+            piece_get<kOct, E>(in[k], c, V, v);
+#pragma unroll
+            for (int j = 0; j < kOct; ++j) v[j] = __expf(v[j] - top) * share;
+            if ((uint32_t)(label - c) < kOct) less_at(v, label - c, scale);
+            piece_put<kOct, E>(dz, c, V, v, stream);
+        }
+    }
+}
+
+// A workgroup a row, read twice for the gradient: the second time from the cache in front of memory, which holds the rows of the 512 workgroups that
+// are under way (8 x 256 rows of 100000 bf16: 179 us; in two launches, between which it loses them, 247).
+template <typename E, int kLanes>
+__global__ __launch_bounds__(kLanes) void k_loss_swept(LossArgs<E> a) {
+    constexpr int kWaves = kLanes / kWave;
+    __shared__ float s_max[kWaves], s_sum[kWaves];
+    __shared__ int32_t s_count[kWaves];
+    const uint32_t node = blockIdx.x / a.per_node;
+    const int64_t r = blockIdx.x;
+    const int32_t* labels = a.labels + (int64_t)node * a.T;
+    const int32_t label = a.labels[r];
+    const typename E::mem* z = a.z + r * a.ld;
+    typename E::mem* dz = a.dz ? a.dz + r * a.ld : nullptr;
+    if (label < 0) {
+        if (threadIdx.x == 0) a.row_loss[r] = 0.f;
+        const float zero[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int32_t c = threadIdx.x * kOct; dz && c < a.V; c += kLanes * kOct) piece_put<kOct, E>(dz, c, a.V, zero, a.stream);
+        return;
+    }
+    const bool bad = label >= a.V;
+    const float picked = E::get(z[bad ? 0 : label]);
+    const int32_t counted = !dz ? 0 : a.count ? a.count[node] : count_labels(labels, a.T, kLanes, s_count);
+    float top, sum;
+    sweep_sum<E, kLanes>(z, 0, a.V, a.V, &top, &sum);
+    const float most = wave_max<kWave>(top);
+    sum = wave_sum<kWave>(sum * __expf(top - most));
+    if ((threadIdx.x & (kWave - 1)) == 0) {
+        s_max[threadIdx.x / kWave] = most;
+        s_sum[threadIdx.x / kWave] = sum;
+    }
+    __syncthreads();  // from here on dz may take the place of z
+    top = s_max[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_max[w]);
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += s_sum[w] * __expf(s_max[w] - top);
+    if (threadIdx.x == 0) a.row_loss[r] = bad ? __builtin_nanf("") : logf(sum) + (top - picked);
+    if (!dz) return;
+    const float scale = bad ? __builtin_nanf("") : a.grad_scale / (float)counted;
+    sweep_grad<E, kLanes>(z, dz, 0, a.V, a.V, label, top, scale / sum, scale, a.stream);
+}
+
 // ---- rows in pieces: a workgroup for each ------------------------------------------------------------------------------------
 // Maximum and sum of exp(z - maximum) of a row from those of its pieces, by an aligned group of lanes (a power of two up to 64); all
 // of them get both.
@@ -283,18 +377,8 @@ __global__ __launch_bounds__(kThreads) void k_loss_parts(LossArgs<E> a) {
     if (a.labels[r] >= 0) {
         const int32_t from = (int32_t)piece * a.piece, to = a.V - from < a.piece ? a.V : from + a.piece;
         const typename E::mem* z = a.z + r * a.ld;
-        float top = kLowest, sum = 0.f;
-        for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) {
-            float v[kOct], most = top;
-            piece_read<kOct, E>(z, c, a.V, v);
-            if (c + kOct > a.V) past_end(v, c, a.V);
-#pragma unroll
-            for (int j = 0; j < kOct; ++j) most = fmaxf(most, v[j]);
-            sum *= __expf(top - most);
-            top = most;
-#pragma unroll
-            for (int j = 0; j < kOct; ++j) sum += __expf(v[j] - top);
-        }
+        float top, sum;
+        sweep_sum<E, kThreads>(z, from, to, a.V, &top, &sum);
         float all = wave_max<kWave>(top);
         sum = wave_sum<kWave>(sum * __expf(top - all));
         if ((threadIdx.x & (kWave - 1)) == 0) {
@@ -334,28 +418,23 @@ __global__ __launch_bounds__(kThreads) void k_loss_parts_grad(LossArgs<E> a) {
     const int32_t from = (int32_t)piece * a.piece, to = a.V - from < a.piece ? a.V : from + a.piece;
     const typename E::mem* z = a.z + r * a.ld;
     typename E::mem* dz = a.dz + r * a.ld;
-    float v[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (label < 0) {
-        for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) piece_put<kOct, E>(dz, c, a.V, v);
+        const float zero[kOct] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) piece_put<kOct, E>(dz, c, a.V, zero);
         return;
     }
     const int32_t counted = a.count ? a.count[node] : count_labels(a.labels + (int64_t)node * a.T, a.T, kThreads, s_count);
     const MaxSum all = join_parts(a.parts + r * 2 * a.pieces, a.pieces, kWave);
     const float scale = label >= a.V ? __builtin_nanf("") : a.grad_scale / (float)counted, share = scale / all.sum;
-    for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) {
-        piece_read<kOct, E>(z, c, a.V, v);
-#pragma unroll
-        for (int j = 0; j < kOct; ++j) v[j] = __expf(v[j] - all.top) * share;
-        if ((uint32_t)(label - c) < kOct) less_at(v, label - c, scale);
-        piece_put<kOct, E>(dz, c, a.V, v);
-    }
+    sweep_grad<E, kThreads>(z, dz, from, to, a.V, label, all.top, share, scale, a.stream);
 }
 
 template <int V>
 struct Const {
     static constexpr int value = V;
 };
-// Lanes a row and pieces a lane by the number of eights in it: the smallest that hold it.
+// Lanes a row and pieces a lane by the number of eights in it: the smallest that hold it, at most four pieces while there are lanes, so
+// that a compute unit has room for several rows (8 x 512 rows of 12000 bf16: 41 us with 3 x 512, 51 with 2 x 1024).
 template <typename E, typename F>
 bool with_row_shape(int32_t octs, F&& f) {
     if constexpr (E::kNarrow) f(Const<16>(), Const<1>());
@@ -365,22 +444,26 @@ bool with_row_shape(int32_t octs, F&& f) {
     else if (octs <= 128) f(Const<64>(), Const<2>());
     else if (octs <= 256) f(Const<64>(), Const<4>());
     else if (octs <= 512) f(Const<256>(), Const<2>());
+    else if (octs <= 768) f(Const<256>(), Const<3>());
     else if (octs <= 1024) f(Const<256>(), Const<4>());
-    else if (octs <= 2048) f(Const<1024>(), Const<2>());
+    else if (octs <= 1536) f(Const<512>(), Const<3>());
+    else if (octs <= 2048) f(Const<512>(), Const<4>());
+    else if (octs <= 3072) f(Const<1024>(), Const<3>());
     else if (octs <= 4096) f(Const<1024>(), Const<4>());
-    else if (octs <= 8192) f(Const<1024>(), Const<8>());
     else return false;
     return true;
 }
 
-// Rows are cut into pieces where no workgroup holds one, and where there are fewer long rows than compute units.
+constexpr int32_t kHeldAlone = 8192;  // longest rows that are held for the loss alone
+
+// Long rows are cut into pieces where there are fewer of them than compute units.
 constexpr int32_t kPieceUnit = kOct * kThreads;
 struct Cut {
     uint32_t pieces = 0;  // 0: rows are held
     int32_t piece = 0;
     Cut(const RowsShape& s, int num_cus) {
         const int64_t rows = (int64_t)s.n * s.T;
-        if (s.D <= 65536 && !(s.D > 8192 && rows < num_cus)) return;
+        if (s.D <= 8192 || rows >= num_cus) return;
         const int64_t units = ((int64_t)s.D + kPieceUnit - 1) / kPieceUnit, wanted = rows < 4 * num_cus ? 4 * num_cus / (rows > 0 ? rows : 1) : 1;
         const int64_t each = wanted < units ? units / wanted : 1;
         piece = (int32_t)(each * kPieceUnit < s.D ? each * kPieceUnit : s.D);
@@ -446,7 +529,7 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
         }
         a.row_loss = rows;
         hipError_t e = hipSuccess;
-        with_row_shape<E>((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
+        auto held_launch = [&](auto l, auto k) {
             constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
             a.per_node = blocks_for(s.T, kBlock / L);
             a.left = counter(a.per_node);
@@ -458,7 +541,22 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
             if (e != hipSuccess) return;
             k_loss_held<E, L, N><<<dim3(a.per_node * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
             e = hipGetLastError();
-        });
+        };
+        // the loss alone needs no row held: 8 x 512 rows of 32000 bf16 46 us, held 60
+        const bool held = !(s.D > kHeldAlone && !dlogits) && with_row_shape<E>((s.D + kOct - 1) / kOct, held_launch);
+        if constexpr (!E::kNarrow) {
+            if (!held) {
+                a.per_node = (uint32_t)s.T;
+                if (dlogits && s.T > 4 * kNodeThreads) {
+                    a.count = count;
+                    e = count_launch();
+                }
+                if (e != hipSuccess) return e;
+                if (dlogits) k_loss_swept<E, kNodeThreads><<<dim3(all), dim3(kNodeThreads), 0, c->stream>>>(a);
+                else k_loss_swept<E, 512><<<dim3(all), dim3(512), 0, c->stream>>>(a);
+                e = hipGetLastError();
+            }
+        }
         if (e != hipSuccess || a.left) return e;
         k_loss_mean<<<dim3((uint32_t)s.n), dim3(kNodeThreads), 0, c->stream>>>(rows, labels, s.T, loss);
         return hipGetLastError();

@@ -327,7 +327,7 @@ def test_dropout_in_place_and_backward(hx):
 LOSS = [  # n, T, V, padding of the rows
     (1, 1, 1, 0), (2, 3, 2, 0), (3, 5, 7, 1), (2, 4, 64, 0), (2, 9, 257, 3), (1, 40, 1000, 0), (2, 3, 2049, 0), (1, 5, 5003, 5),
     (2, 6, 8200, 0), (1, 3, 32000, 0), (1, 2, 40001, 1), (4, 1, 128000, 0), (1, 1, 300007, 0), (3, 0, 10, 0), (30, 11, 50, 2),
-    (1, 600, 33, 0), (2, 300, 3001, 0), (1, 520, 9000, 0),
+    (1, 600, 33, 0), (2, 300, 3001, 0), (1, 520, 9000, 0), (2, 130, 33003, 1), (1, 257, 40000, 0), (1, 270, 20000, 0), (3, 90, 8193, 0),
 ]
 
 
@@ -380,9 +380,9 @@ def test_token_loss(hx, n, T, V, pad, dtype):
     sim.close()
 
 
-@pytest.mark.parametrize("V", [5, 300, 3000, 20000, 70000])
-def test_token_loss_of_masked_and_broken_logits(hx, V):
-    n, T = 5, 6
+@pytest.mark.parametrize("V,T", [(5, 6), (300, 6), (3000, 6), (20000, 6), (70000, 6), (10000, 60), (40000, 60)])
+def test_token_loss_of_masked_and_broken_logits(hx, V, T):
+    n = 5
     sim, X, rng = make_sim(hx, n, 4, seed=V)
     z = rng.normal(size=(n, T, V)).astype(np.float32)
     labels = rng.integers(1, V - 1, size=(n, T))
@@ -406,6 +406,7 @@ def test_token_loss_of_masked_and_broken_logits(hx, V):
     got_loss, got_dz = sim.token_loss(z_d, lab_d)
     close(got_loss, loss, tol_loss, "loss")
     close(got_dz, dz, tol_dz, "gradient")
+    close(sim.token_loss(z_d, lab_d, grad=False)[0], loss, tol_loss, "loss without a gradient")
     labels[2, 0] = V                                             # no address
     labels[0, 0] = 2 ** 31 - 1
     got_loss, got_dz = sim.token_loss(z_d, torch.as_tensor(labels, dtype=torch.int32).cuda())
