@@ -7,9 +7,10 @@
 // digits.  A label of V or more is never an address: the loss of its node and its row of dz are NaN.  A node without a
 // counted token has loss 0 (NaN would spread to every node with the next gossip step).
 //
-// A row is read once: L lanes hold it as exp(z - m_lane) in fp32, m_lane the largest value of the lane, and one pass over
-// the lanes joins maxima and sums; the gradient is what is held times exp(m_lane - m) a / (N sum).  Few or very long rows are cut
-// into pieces for a workgroup each, and a second launch reads them again for the gradient.
+// Three forms.  Rows of up to 32768 columns are read once: L lanes hold a row as exp(z - m_lane) in fp32, m_lane the largest value
+// of the lane, and one pass over the lanes joins maxima and sums; the gradient is what is held times exp(m_lane - m) a / (N sum).
+// Longer ones are swept twice by a workgroup, the second time out of the cache.  Where there are fewer rows than compute units,
+// long ones are cut into pieces for a workgroup each, and a second launch reads them again for the gradient.
 //
 // Bound by the logits' bytes: 8 x 512 rows of 32000 bf16 with the gradient in 90 us (5.5 TB/s; three readings of a row took 164).  A
 // compute unit holds two such rows, so loads, sums and stores of two rows overlap and no more; holding rows as they lie in
@@ -423,7 +424,7 @@ __global__ __launch_bounds__(kThreads) void k_loss_parts_grad(LossArgs<E> a) {
         for (int32_t c = from + (int32_t)threadIdx.x * kOct; c < to; c += kThreads * kOct) piece_put<kOct, E>(dz, c, a.V, zero);
         return;
     }
-    const int32_t counted = a.count ? a.count[node] : count_labels(a.labels + (int64_t)node * a.T, a.T, kThreads, s_count);
+    const int32_t counted = count_labels(a.labels + (int64_t)node * a.T, a.T, kThreads, s_count);
     const MaxSum all = join_parts(a.parts + r * 2 * a.pieces, a.pieces, kWave);
     const float scale = label >= a.V ? __builtin_nanf("") : a.grad_scale / (float)counted, share = scale / all.sum;
     sweep_grad<E, kThreads>(z, dz, from, to, a.V, label, all.top, share, scale, a.stream);
@@ -459,12 +460,12 @@ constexpr int32_t kHeldAlone = 8192;  // longest rows that are held for the loss
 // Long rows are cut into pieces where there are fewer of them than compute units.
 constexpr int32_t kPieceUnit = kOct * kThreads;
 struct Cut {
-    uint32_t pieces = 0;  // 0: rows are held
+    uint32_t pieces = 0;  // 0: a row is one workgroup's or less
     int32_t piece = 0;
     Cut(const RowsShape& s, int num_cus) {
         const int64_t rows = (int64_t)s.n * s.T;
-        if (s.D <= 8192 || rows >= num_cus) return;
-        const int64_t units = ((int64_t)s.D + kPieceUnit - 1) / kPieceUnit, wanted = rows < 4 * num_cus ? 4 * num_cus / (rows > 0 ? rows : 1) : 1;
+        if (s.D <= 8192 || rows == 0 || rows >= num_cus) return;
+        const int64_t units = ((int64_t)s.D + kPieceUnit - 1) / kPieceUnit, wanted = 4 * num_cus / rows;
         const int64_t each = wanted < units ? units / wanted : 1;
         piece = (int32_t)(each * kPieceUnit < s.D ? each * kPieceUnit : s.D);
         pieces = (uint32_t)(((int64_t)s.D + piece - 1) / piece);
@@ -518,11 +519,6 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
                     e = hipGetLastError();
                 }
                 if (e != hipSuccess || !a.dz) return e;
-                if (s.T > 4 * kThreads) {
-                    a.count = count;
-                    e = count_launch();
-                    if (e != hipSuccess) return e;
-                }
                 k_loss_parts_grad<E><<<dim3(all * cut.pieces), dim3(kThreads), 0, c->stream>>>(a);
             }
             return hipGetLastError();
