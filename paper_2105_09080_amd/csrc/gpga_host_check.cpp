@@ -22,6 +22,7 @@
 #include "gpga_rows_deal.hpp"
 #include "gpga_rows_run.hpp"
 #include "gpga_schedule.hpp"
+#include "gpga_spans.hpp"
 
 namespace {
 
@@ -601,9 +602,40 @@ void circulant_matrices() {
     }
 }
 
+// Overlap of rows with a span of bytes and with other rows, against a walk over every byte.
+void overlaps() {
+    const uintptr_t base = 1 << 20;
+    auto at = [](uintptr_t a) { return reinterpret_cast<const void*>(a); };
+    int64_t checked = 0, met = 0;
+    for (int64_t rows = 1; rows <= 4; ++rows)
+        for (int64_t width = 1; width <= 4; ++width)
+            for (int64_t step = width; step <= width + 4; ++step) {
+                const RowBytes r = {at(base), rows, step, width};
+                auto in_rows = [&](int64_t b) { return b >= 0 && b / step < rows && b % step < width; };
+                for (int64_t off = -12; off <= rows * step + 4; ++off) {
+                    const void* q = at(base + (uintptr_t)off);
+                    for (int64_t bytes = 0; bytes <= 12; ++bytes) {
+                        bool want = false;
+                        for (int64_t b = off; b < off + bytes; ++b) want = want || in_rows(b);
+                        expect(rows_meet_span(r, q, bytes) == want, "rows and a span");
+                        ++checked;
+                        met += want;
+                    }
+                    bool want = false;
+                    for (int64_t b = 0; b < rows * step; ++b) want = want || (in_rows(b) && in_rows(b + off));
+                    expect(rows_meet(r, q) == want, "rows and rows");
+                }
+            }
+    // the last columns of a wider array end where that ends, whatever the leading dimension
+    expect(!rows_meet_span({at(base + 64), 6, 128, 64}, at(base + 6 * 128), 1 << 20), "an array behind a wider one");
+    expect(rows_meet_span({at(base + 64), 6, 128, 64}, at(base + 6 * 128 - 1), 1 << 20), "one byte of it");
+    std::printf("overlaps checked %" PRId64 " met %" PRId64 "\n", checked, met);
+}
+
 }  // namespace
 
 int main() {
+    overlaps();
     exchange_buffers();
     circulant_matrices();
     node_run_sizes();

@@ -5,6 +5,7 @@
 #include <cstdio>
 
 #include "gpga_rows.hpp"
+#include "gpga_spans.hpp"
 
 namespace {
 
@@ -63,13 +64,10 @@ struct Array {
     bool out;
 };
 
-// Rows of `width` bytes every `step` bytes from a and b on: do any share a byte?  (Columns of one wider array do not.)
-bool rows_meet(const void* a, const void* b, int64_t rows, int64_t step, int64_t width) {
-    const uintptr_t lo = reinterpret_cast<uintptr_t>(a < b ? a : b), hi = reinterpret_cast<uintptr_t>(a < b ? b : a);
-    const uintptr_t span = (uintptr_t)((rows - 1) * step + width);
-    if (hi - lo >= span) return false;
-    const int64_t apart = (int64_t)((hi - lo) % (uintptr_t)step);
-    return !(apart >= width && apart + width <= step);
+// The bytes of an array of rows of the call's shape, T > 0.
+RowBytes row_bytes(const RowsShape& s, const void* p) {
+    const int64_t size = elem_size(s.dtype);
+    return {p, (int64_t)s.n * s.T, s.ld * size, s.D * size};
 }
 
 gpga_status check_ready(gpga_ctx* c) {
@@ -90,25 +88,23 @@ gpga_status check_rows(gpga_ctx* c, const RowsShape& s, const Array* arrays, int
     if (__builtin_mul_overflow(rows, s.ld, &bytes) || __builtin_mul_overflow(bytes, size, &bytes) || bytes > (1ll << 56))
         return fail(c, GPGA_EINVAL, "%lld rows of ld = %lld are more than can be addressed", (long long)rows, (long long)s.ld);
     if (s.T == 0) return GPGA_OK;  // no row is touched
-    const uintptr_t state = (uintptr_t)c->n * (uintptr_t)c->ld * sizeof(float);
+    const int64_t state = (int64_t)c->n * c->ld * (int64_t)sizeof(float);
     const struct {
         const char* name;
         const float* p;
     } held[4] = {{"x", c->x}, {"x_new", c->x_new}, {"m", c->m}, {"g", c->g}};
     for (int k = 0; k < count; ++k) {
         if (!arrays[k].p) continue;
-        const uintptr_t p = reinterpret_cast<uintptr_t>(arrays[k].p);
-        if (p & (uintptr_t)(size - 1)) return fail(c, GPGA_EINVAL, "%s is not aligned to its elements", arrays[k].name);
+        if (reinterpret_cast<uintptr_t>(arrays[k].p) & (uintptr_t)(size - 1)) return fail(c, GPGA_EINVAL, "%s is not aligned to its elements", arrays[k].name);
         for (const auto& h : held) {
             if (!arrays[k].out && !(writes_g && h.p == c->g)) continue;
-            const uintptr_t q = reinterpret_cast<uintptr_t>(h.p);
-            if (h.p && p < q + state && q < p + (uintptr_t)bytes)
+            if (h.p && rows_meet_span(row_bytes(s, arrays[k].p), h.p, state))
                 return fail(c, GPGA_EINVAL, "%s overlaps the bound array %s", arrays[k].name, h.name);
         }
         if (!arrays[k].out) continue;
         for (int j = 0; j < count; ++j) {
             if (j == k || !arrays[j].p || (arrays[j].p == arrays[k].p && !arrays[j].out)) continue;
-            if (rows_meet(arrays[k].p, arrays[j].p, rows, s.ld * size, s.D * size))
+            if (rows_meet(row_bytes(s, arrays[k].p), arrays[j].p))
                 return fail(c, GPGA_EINVAL, "%s and %s overlap", arrays[k].name, arrays[j].name);
         }
     }
@@ -118,19 +114,15 @@ gpga_status check_rows(gpga_ctx* c, const RowsShape& s, const Array* arrays, int
 // `floats` of fp32 that the call reads or writes beside its rows: they share no byte with an output or, written, with any array.
 gpga_status check_floats(gpga_ctx* c, const RowsShape& s, const char* name, const float* p, int64_t floats, bool out, const Array* arrays, int count) {
     if (!p || !floats) return GPGA_OK;
-    const uintptr_t from = reinterpret_cast<uintptr_t>(p), to = from + (uintptr_t)floats * sizeof(float);
-    auto meets = [&](const void* q, int64_t bytes) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(q);
-        return q && from < at + (uintptr_t)bytes && at < to;
-    };
-    const int64_t size = elem_size(s.dtype), rows = (int64_t)s.n * s.T;
+    const int64_t bytes = floats * (int64_t)sizeof(float);
     for (int k = 0; k < count; ++k)
-        if (rows && (out || arrays[k].out) && meets(arrays[k].p, ((rows - 1) * s.ld + s.D) * size))
+        if (s.T > 0 && arrays[k].p && (out || arrays[k].out) && rows_meet_span(row_bytes(s, arrays[k].p), p, bytes))
             return fail(c, GPGA_EINVAL, "%s and %s overlap", name, arrays[k].name);
     const int64_t state = (int64_t)c->n * c->ld * (int64_t)sizeof(float);
     const float* held[4] = {c->x, c->x_new, c->m, c->g};
     for (const float* h : held)
-        if ((out || h == c->g) && meets(h, state)) return fail(c, GPGA_EINVAL, "%s overlaps a bound array", name);
+        if (h && (out || h == c->g) && rows_meet_span({h, 1, state, state}, p, bytes))
+            return fail(c, GPGA_EINVAL, "%s overlaps a bound array", name);
     return GPGA_OK;
 }
 

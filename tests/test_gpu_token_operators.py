@@ -597,3 +597,45 @@ def test_operators_leave_the_iteration_as_it_was(hx):
     want = (half + np.roll(half, 1, axis=0) + np.roll(half, -1, axis=0)) / 3
     assert sim.k == 1 and np.abs(host(sim.X) - want).max() < 1e-5 * np.abs(want).max()
     sim.close()
+
+
+def test_rows_end_where_their_last_element_does(hx):
+    """Arrays back to back in one buffer: the last columns of a wider array directly in front of a bound one share no byte with it,
+    and an element further they do; what a call has beside its rows may lie between two of them."""
+    from paper_2105_09080_amd import binding as B
+    n, T, D, V, d = 2, 3, 8, 4, 48
+    words = 2 * D * n * T
+    buffer = torch.zeros(words + 3 * n * d, device="cuda")
+    wide, state = buffer[:words].view(n, T, 2 * D), [buffer[words + k * n * d:][:n * d].view(n, d) for k in range(3)]
+    ctx = B.gpga_create(n, d, "ring", 0, 0.1, 0.0)
+    tok = torch.zeros((n, T), dtype=torch.int32, device="cuda")
+    x = torch.randn((n, T, 2 * D), device="cuda")
+    out = wide[..., D:]
+    stream = torch.cuda.current_stream().cuda_stream
+    for first in range(3):                                         # each of x, x_new and g behind the rows
+        order = state[first:] + state[:first]
+        B.gpga_bind(ctx, order[0], order[1], None, order[2], d, stream)
+        order[0].copy_(torch.randn((n, d), device="cuda"))
+        B.gpga_dropout(ctx, x[..., D:], None, T, D, 2 * D, 0, 0.0, 1, 0, out)
+        assert torch.equal(out, x[..., D:])
+        B.gpga_embed(ctx, tok, T, 0, V, D, 1.0, out, 2 * D, 0)
+        assert torch.equal(out, order[0][:, None, :D].expand(n, T, D))
+        B.gpga_embed_grad(ctx, tok, T, 0, V, D, 1.0, out, 2 * D, 0, False)
+        assert torch.allclose(order[2][:, :D], 3 * order[0][:, :D])
+        for call in (lambda p: B.gpga_dropout(ctx, x[..., D:], None, T, D, 2 * D, 0, 0.0, 1, 0, p),
+                     lambda p: B.gpga_embed(ctx, tok, T, 0, V, D, 1.0, p, 2 * D, 0)):
+            with pytest.raises(B.GpgaError, match="bound array"):
+                call(out.data_ptr() + 4)
+    one = B.gpga_create(1, d, "none", 0, 0.1, 0.0)
+    B.gpga_bind(one, state[0][:1], state[1][:1], None, state[2][:1], d, stream)
+    wide = torch.randn((1, 2, 4 * D), device="cuda")               # x | y | 2 pairs (mean, rstd) of statistics | nothing
+    wide[..., 2 * D:] = 0
+    norm = lambda stats: B.gpga_layer_norm(one, wide, None, 2, D, 4 * D, 0, 0.0, 1, 0, 0, D, 1e-5, None, wide[..., D:], stats)
+    norm(wide[0, 0, 2 * D:].data_ptr())
+    assert torch.allclose(wide[0, 0, 2 * D:2 * D + 4:2], wide[0, :, :D].mean(dim=1), atol=1e-5) and (wide[0, 0, 2 * D + 4:] == 0).all()
+    for stats in (wide[0, 0, 2 * D - 1:], wide[0, 0, 4 * D - 3:]):  # the last element of y; the first of the next row's x
+        with pytest.raises(B.GpgaError, match="stats_dev"):
+            norm(stats.data_ptr())
+    torch.cuda.synchronize()
+    B.gpga_destroy(ctx)
+    B.gpga_destroy(one)

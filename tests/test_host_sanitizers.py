@@ -140,3 +140,9 @@ def test_pacing_controller_finds_and_follows_the_edge_of_a_launch_model(facts):
         assert 0.985 * edge <= mean <= 1.012 * edge
         assert int(v["settle"]) <= 48 and int(v["drop_recover"]) <= 12
     assert [f for f in facts if f[0] == "pace_model_limit"]
+
+
+def test_overlaps_go_by_the_bytes_that_rows_have(facts):
+    """The overlap checks of the language-model operators, against a walk over every byte of small arrays."""
+    row, = [f for f in facts if f[0] == "overlaps"]
+    assert int(row[2]) > 20_000 and 0 < int(row[4]) < int(row[2])
