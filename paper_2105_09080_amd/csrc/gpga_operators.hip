@@ -134,9 +134,15 @@ gpga_status check_columns(gpga_ctx* c, const char* name, int64_t off, int64_t co
     return GPGA_OK;
 }
 
-gpga_status check_ints(gpga_ctx* c, const char* name, const int32_t* p, int32_t T) {
-    if (T > 0 && !p) return fail(c, GPGA_EINVAL, "%s must not be NULL", name);
+// Tokens or labels, n * T of them, after check_rows: they share no byte with an output of the call.
+gpga_status check_ints(gpga_ctx* c, const RowsShape& s, const char* name, const int32_t* p, const Array* arrays, int count, bool writes_g = false) {
+    if (s.T > 0 && !p) return fail(c, GPGA_EINVAL, "%s must not be NULL", name);
     if (reinterpret_cast<uintptr_t>(p) & 3u) return fail(c, GPGA_EINVAL, "%s is not 4-byte aligned", name);
+    const int64_t bytes = (int64_t)s.n * s.T * (int64_t)sizeof(int32_t), state = (int64_t)c->n * c->ld * (int64_t)sizeof(float);
+    for (int k = 0; k < count; ++k)
+        if (s.T > 0 && arrays[k].p && arrays[k].out && rows_meet_span(row_bytes(s, arrays[k].p), p, bytes))
+            return fail(c, GPGA_EINVAL, "%s and %s overlap", name, arrays[k].name);
+    if (writes_g && rows_meet_span({c->g, 1, state, state}, p, bytes)) return fail(c, GPGA_EINVAL, "%s overlaps the bound array g", name);
     return GPGA_OK;
 }
 
@@ -181,7 +187,7 @@ gpga_status gpga_embed(gpga_ctx* c, const int32_t* tokens, int32_t T, int64_t ta
     const Array arrays[] = {{"y_dev", y, true}};
     GPGA_TRY(check_table(c, table_off, V, D));
     GPGA_TRY(check_rows(c, s, arrays, 1));
-    GPGA_TRY(check_ints(c, "tokens_dev", tokens, T));
+    GPGA_TRY(check_ints(c, s, "tokens_dev", tokens, arrays, 1));
     if (!std::isfinite(scale)) return fail(c, GPGA_EINVAL, "scale must be finite");
     if (T == 0) return GPGA_OK;
     if (!y) return fail(c, GPGA_EINVAL, "y_dev must not be NULL");
@@ -198,7 +204,7 @@ gpga_status gpga_embed_grad(gpga_ctx* c, const int32_t* tokens, int32_t T, int64
     const Array arrays[] = {{"dy_dev", dy, false}};
     GPGA_TRY(check_table(c, table_off, V, D));
     GPGA_TRY(check_rows(c, s, arrays, 1, true));
-    GPGA_TRY(check_ints(c, "tokens_dev", tokens, T));
+    GPGA_TRY(check_ints(c, s, "tokens_dev", tokens, arrays, 1, true));
     if (!std::isfinite(scale)) return fail(c, GPGA_EINVAL, "scale must be finite");
     if (accumulate != 0 && accumulate != 1) return fail(c, GPGA_EINVAL, "accumulate must be 0 or 1");
     if (T > 0 && !dy) return fail(c, GPGA_EINVAL, "dy_dev must not be NULL");
@@ -279,11 +285,13 @@ gpga_status gpga_token_loss(gpga_ctx* c, const void* logits, const int32_t* labe
     const RowsShape s = {c->n, T, V, ld, dtype};
     const Array arrays[] = {{"logits_dev", logits, false}, {"dlogits_dev", dlogits, true}};
     GPGA_TRY(check_rows(c, s, arrays, 2));
-    GPGA_TRY(check_ints(c, "labels_dev", labels, T));
+    GPGA_TRY(check_ints(c, s, "labels_dev", labels, arrays, 2));
     if (!std::isfinite(grad_scale)) return fail(c, GPGA_EINVAL, "grad_scale must be finite");
     if (!loss || (reinterpret_cast<uintptr_t>(loss) & 3u)) return fail(c, GPGA_EINVAL, "loss_dev must be a 4-byte aligned device pointer");
     if (T > 0 && !logits) return fail(c, GPGA_EINVAL, "logits_dev must not be NULL");
     GPGA_TRY(check_floats(c, s, "loss_dev", loss, c->n, true, arrays, 2));
+    const int64_t losses = (int64_t)c->n * (int64_t)sizeof(float), ints = (int64_t)c->n * T * (int64_t)sizeof(int32_t);
+    if (rows_meet_span({loss, 1, losses, losses}, labels, ints)) return fail(c, GPGA_EINVAL, "labels_dev and loss_dev overlap");
     DeviceGuard guard(c->device);
     GPGA_TRY(reserve(c, token_loss_scratch(s, c->num_cus)));
     const hipError_t e = launch_token_loss(c, s, logits, labels, grad_scale, loss, dlogits, c->op_scratch);

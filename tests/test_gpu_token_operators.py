@@ -639,3 +639,37 @@ def test_rows_end_where_their_last_element_does(hx):
     torch.cuda.synchronize()
     B.gpga_destroy(ctx)
     B.gpga_destroy(one)
+
+
+def test_tokens_and_labels_within_an_output_are_refused(hx):
+    from paper_2105_09080_amd import binding as B
+    n, V, D, T = 2, 6, 8, 3
+    sim, X, rng = make_sim(hx, n, V * D, seed=0)
+    words = torch.zeros(n * T * (2 * D + 1) + n, device="cuda")    # rows of D in the first half of 2 D, then as many ints, then n losses
+    y, ints, loss = words[:n * T * 2 * D].view(n, T, 2 * D)[..., :D], words[n * T * 2 * D:][:n * T], words[-n:]
+    z = torch.randn((n, T, 2 * D), device="cuda")
+    dy = z[..., :D]
+    at = lambda t, off: t.data_ptr() + 4 * off
+    embed = lambda tokens: B.gpga_embed(sim.ctx, tokens, T, 0, V, D, 1.0, y, 2 * D, 0)
+    grad = lambda tokens: B.gpga_embed_grad(sim.ctx, tokens, T, 0, V, D, 1.0, dy, 2 * D, 0, False)
+    token_loss = lambda labels: B.gpga_token_loss(sim.ctx, dy, labels, T, D, 2 * D, 0, 1.0, loss, y)
+    sim.G.fill_(7.0)
+    for call, place, says in ((embed, at(y, 0), "tokens_dev and y_dev"), (embed, at(y, D - 1), "tokens_dev and y_dev"),
+                              (embed, at(y, -n * T + 1), "tokens_dev and y_dev"), (embed, at(y, 2 * D - n * T + 1), "tokens_dev and y_dev"),
+                              (grad, sim.g.data_ptr(), "bound array g"), (grad, at(sim.g, n * V * D - 1), "bound array g"),
+                              (grad, at(sim.g, -n * T + 1), "bound array g"), (token_loss, at(y, 2 * D + 3), "labels_dev and dlogits_dev"),
+                              (token_loss, at(loss, 0), "labels_dev and loss_dev"), (token_loss, at(loss, 1 - n * T), "labels_dev and loss_dev")):
+        with pytest.raises(B.GpgaError) as e:
+            call(place)
+        assert e.value.status == B.GPGA_EINVAL and says in str(e.value), str(e.value)
+    assert (host(sim.G) == 7.0).all() and (host(words) == 0).all()
+    embed(ints)                                                    # directly behind the rows, and between two of them
+    assert torch.equal(y, sim.X[:, None, :D].expand(n, T, D))
+    token_loss(ints)
+    want = orc.token_loss(host(dy), np.zeros((n, T), np.int64))
+    close(loss, want[0], 1e-5, "loss")
+    y.fill_(0.0)
+    embed(at(y, D))
+    assert torch.equal(y, sim.X[:, None, :D].expand(n, T, D))
+    grad(at(y, D))
+    sim.close()
