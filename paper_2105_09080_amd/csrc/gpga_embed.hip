@@ -22,10 +22,10 @@ constexpr int kTurns = 3;
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_embed(const int32_t* __restrict__ tokens, const float* __restrict__ table, int64_t ldx,
                                                     int32_t V, int32_t D, int32_t T, uint32_t blocks_per_node, int lanes_log2, float scale,
-                                                    typename E::mem* __restrict__ y, int64_t ld, bool stream) {
+                                                    typename E::mem* __restrict__ y, int64_t ld, bool stream, uint32_t first_block) {
     typedef Elem<float, E::kNarrow> P;
-    const uint32_t node = blockIdx.x / blocks_per_node;
-    const int32_t t = (int32_t)((blockIdx.x - node * blocks_per_node) * (uint32_t)(kThreads >> lanes_log2)) + (int32_t)(threadIdx.x >> lanes_log2);
+    const uint32_t block = first_block + blockIdx.x, node = block / blocks_per_node;
+    const int32_t t = (int32_t)((block - node * blocks_per_node) * (uint32_t)(kThreads >> lanes_log2)) + (int32_t)(threadIdx.x >> lanes_log2);
     if (t >= T) return;
     const int64_t row = (int64_t)node * T + t;
     const int32_t tok = tokens[row];
@@ -66,7 +66,7 @@ constexpr int kDigitBits = 10, kDigits = 1 << kDigitBits;
 static_assert(kDigits == kSortThreads, "a thread a digit");
 
 struct ZeroArgs {
-    uint32_t first_block;   // workgroups from here on zero
+    uint32_t sorting;       // workgroups; those behind them zero
     uint32_t per_node;
     int64_t count, ldg;     // floats of a node's block, distance of the blocks
     float* g;
@@ -93,17 +93,18 @@ __device__ __forceinline__ void zero_block(const ZeroArgs& z, uint32_t b) {
 // kItems items a thread: 8, or fewer where no tile has more.
 template <int kItems>
 __global__ __launch_bounds__(kSortThreads) void k_sort_tile(const int32_t* __restrict__ tokens, int32_t T, int32_t V, uint32_t tiles, int bits,
-                                                            uint32_t* __restrict__ keys, int32_t* __restrict__ pos, ZeroArgs zero) {
-    if (blockIdx.x >= zero.first_block) {
-        zero_block(zero, blockIdx.x - zero.first_block);
+                                                            uint32_t* __restrict__ keys, int32_t* __restrict__ pos, ZeroArgs zero, uint32_t first_block) {
+    const uint32_t block = first_block + blockIdx.x;
+    if (block >= zero.sorting) {
+        zero_block(zero, block - zero.sorting);
         return;
     }
     __shared__ uint32_t s_key[kItems * kSortThreads];
     __shared__ uint16_t s_pos[kItems * kSortThreads];
     __shared__ uint16_t s_count[kSortWaves][kDigits];
     __shared__ uint32_t s_total[kSortWaves];
-    const uint32_t node = blockIdx.x / tiles;
-    const int32_t base = (int32_t)(blockIdx.x - node * tiles) * kTile;
+    const uint32_t node = block / tiles;
+    const int32_t base = (int32_t)(block - node * tiles) * kTile;
     const int64_t from = (int64_t)node * T + base;
     const int32_t count = T - base < kTile ? T - base : kTile;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -243,7 +244,7 @@ constexpr int kMostTurns = 16;          // wavefronts of a workgroup, all of one
 struct GradArgs {
     const uint32_t* keys;   // sorted, T a node
     const int32_t* pos;
-    uint32_t n;
+    uint32_t n, first_block;
     int32_t T, V, D;
     int64_t ld, ldg;
     float scale;
@@ -268,7 +269,8 @@ template <typename E, bool kAdd>
 __global__ __launch_bounds__(kMostTurns * kWave) void k_embed_grad(GradArgs a, const typename E::mem* __restrict__ dy) {
     typedef Elem<float, E::kNarrow> P;
     const int lane = threadIdx.x & (kWave - 1);
-    const uint32_t unit = blockIdx.x / a.column_groups, group = blockIdx.x - unit * a.column_groups, node = unit / a.chunks, chunk = unit - node * a.chunks;
+    const uint32_t block = a.first_block + blockIdx.x;
+    const uint32_t unit = block / a.column_groups, group = block - unit * a.column_groups, node = unit / a.chunks, chunk = unit - node * a.chunks;
     const uint32_t* keys = a.keys + (int64_t)node * a.T;
     const int32_t first = (int32_t)chunk * kRun, count = a.T - first < kRun ? a.T - first : kRun;
     const uint32_t key = keys[first + (lane < count ? lane : count - 1)];
@@ -356,11 +358,11 @@ __global__ __launch_bounds__(kThreads) void k_embed_join(GradArgs a, uint32_t bl
     __shared__ float s_part[kWaves][kTurnCols];
     __shared__ uint32_t s_parts[kWaves], s_key[kWaves];
     __shared__ bool s_second[kWaves];
-    const uint32_t unit = blockIdx.x / a.column_blocks, node = unit / blocks_per_node, chunk0 = (unit - node * blocks_per_node) * kWaves;
+    const uint32_t block = a.first_block + blockIdx.x, unit = block / a.column_blocks, node = unit / blocks_per_node, chunk0 = (unit - node * blocks_per_node) * kWaves;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const uint32_t chunk = chunk0 + wave;
     const uint32_t* keys = a.keys + (int64_t)node * a.T;
-    const int32_t c = (int32_t)(blockIdx.x - unit * a.column_blocks) * kTurnCols + lane * 4;
+    const int32_t c = (int32_t)(block - unit * a.column_blocks) * kTurnCols + lane * 4;
     const float* parts_of_node = a.partial + (int64_t)node * a.chunks * 2 * a.D;
     const int64_t first = (int64_t)chunk * kRun, next = first + kRun;
     uint32_t parts = 0, key = 0;
@@ -452,9 +454,10 @@ hipError_t launch_embed(const gpga_ctx* c, const RowsShape& s, const int32_t* to
     const uint32_t per_node = blocks_for(s.T, kThreads >> lanes_log2);
     auto launch = [&](auto e) {
         typedef decltype(e) E;
-        k_embed<E><<<dim3(per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(tokens, c->x + table_off, c->ld, V, s.D, s.T, per_node, lanes_log2,
-                                                                                    scale, static_cast<typename E::mem*>(y), s.ld, stream_rows(s, y));
-        return hipGetLastError();
+        return launch_blocks((uint64_t)per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+            k_embed<E><<<grid, dim3(kThreads), 0, c->stream>>>(tokens, c->x + table_off, c->ld, V, s.D, s.T, per_node, lanes_log2, scale,
+                                                               static_cast<typename E::mem*>(y), s.ld, stream_rows(s, y), first);
+        });
     };
     return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }
@@ -470,30 +473,27 @@ hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_
     int bits = 0;
     while (bits < 32 && ((uint32_t)V + 1u) >> bits) ++bits;
     ZeroArgs zero = {};
-    zero.first_block = space.tiles * (uint32_t)s.n;
+    zero.sorting = space.tiles * (uint32_t)s.n;
     zero.count = (int64_t)V * s.D;
     zero.per_node = accumulate ? 0 : blocks_for(zero.count + 31, kZeroCols);
     zero.ldg = c->ld;
     zero.g = c->g + table_off;
-    const uint32_t blocks = zero.first_block + zero.per_node * (uint32_t)s.n;
-    if (blocks) {
-        auto sort = [&](auto items) {
-            k_sort_tile<decltype(items)::value><<<dim3(blocks), dim3(kSortThreads), 0, c->stream>>>(tokens, s.T, V, space.tiles, bits, words(space.keys[0]),
-                                                                                                  ints(space.pos[0]), zero);
-        };
-        if (s.T <= kSortThreads) sort(Const<1>());
-        else if (s.T <= 4 * kSortThreads) sort(Const<4>());
-        else sort(Const<8>());
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
+    const uint64_t blocks = zero.sorting + (uint64_t)zero.per_node * s.n;
+    auto sort = [&](auto items) {
+        return launch_blocks(blocks, kSortThreads, [&](uint32_t first, dim3 grid) {
+            k_sort_tile<decltype(items)::value><<<grid, dim3(kSortThreads), 0, c->stream>>>(tokens, s.T, V, space.tiles, bits, words(space.keys[0]),
+                                                                                           ints(space.pos[0]), zero, first);
+        });
+    };
+    hipError_t e = s.T <= kSortThreads ? sort(Const<1>()) : s.T <= 4 * kSortThreads ? sort(Const<4>()) : sort(Const<8>());
+    if (e != hipSuccess) return e;
     if (s.T == 0) return hipSuccess;
     uint32_t *keys = words(space.keys[0]), *other_keys = words(space.keys[1]);
     int32_t *pos = ints(space.pos[0]), *other_pos = ints(space.pos[1]);
     for (int64_t run = kTile; run < s.T; run *= 2) {
         const uint32_t per_node = blocks_for(s.T, kThreads);
         k_merge<<<dim3(per_node * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(keys, pos, s.T, run, per_node, other_keys, other_pos);
-        const hipError_t e = hipGetLastError();
+        e = hipGetLastError();
         if (e != hipSuccess) return e;
         std::swap(keys, other_keys);
         std::swap(pos, other_pos);
@@ -516,15 +516,19 @@ hipError_t launch_embed_grad(const gpga_ctx* c, const RowsShape& s, const int32_
     a.g = c->g + table_off;
     auto launch = [&](auto el) {
         typedef decltype(el) E;
-        const dim3 grid(a.chunks * a.column_groups * (uint32_t)s.n), block(kWave * blocks_for(a.column_blocks, a.column_groups));
+        const uint32_t threads = kWave * blocks_for(a.column_blocks, a.column_groups);
         const typename E::mem* rows = static_cast<const typename E::mem*>(dy);
-        if (accumulate) k_embed_grad<E, true><<<grid, block, 0, c->stream>>>(a, rows);
-        else k_embed_grad<E, false><<<grid, block, 0, c->stream>>>(a, rows);
-        const hipError_t e = hipGetLastError();
+        e = launch_blocks((uint64_t)a.chunks * a.column_groups * s.n, threads, [&](uint32_t first, dim3 grid) {
+            a.first_block = first;
+            if (accumulate) k_embed_grad<E, true><<<grid, dim3(threads), 0, c->stream>>>(a, rows);
+            else k_embed_grad<E, false><<<grid, dim3(threads), 0, c->stream>>>(a, rows);
+        });
         if (e != hipSuccess || a.chunks < 2) return e;
         const uint32_t per_node = blocks_for(a.chunks, kThreads / kWave);
-        k_embed_join<Elem<float, E::kNarrow>><<<dim3(per_node * a.column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, per_node);
-        return hipGetLastError();
+        return launch_blocks((uint64_t)per_node * a.column_blocks * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+            a.first_block = first;
+            k_embed_join<Elem<float, E::kNarrow>><<<grid, dim3(kThreads), 0, c->stream>>>(a, per_node);
+        });
     };
     return s.D < 4 ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }

@@ -632,10 +632,39 @@ void overlaps() {
     std::printf("overlaps checked %" PRId64 " met %" PRId64 "\n", checked, met);
 }
 
+// Workgroups of the language-model operators over several launches: each once, in order, every launch below 2^32 work-items.
+void launches() {
+    int64_t sizes = 0, several = 0;
+    for (uint32_t threads : {64u, 256u, 320u, 512u, 1024u})
+        for (uint64_t limit : {0ull, 1ull, 1ull << 32})  // workgroups of as many launches as fill these
+            for (int64_t off = -3; off <= 3; ++off) {
+                const int64_t at = (int64_t)(limit / threads) + off;
+                for (int64_t blocks : {at, 2 * at, 3 * at + 1, at + 12345}) {
+                    if (blocks < 0 || blocks > (1ll << 32)) continue;
+                    uint64_t next = 0, count = 0;
+                    const int status = for_launches((uint64_t)blocks, threads, [&](uint32_t first, uint32_t n) {
+                        expect(first == next && n > 0 && (uint64_t)n * threads < (1ull << 32), "a launch");
+                        next += n;
+                        ++count;
+                        return 0;
+                    });
+                    expect(status == 0 && next == (uint64_t)blocks, "every workgroup once");
+                    const uint64_t most = ((1ull << 32) - 1) / threads;
+                    expect(count == ((uint64_t)blocks + most - 1) / most, "no more launches than needed");
+                    ++sizes;
+                    several += count > 1;
+                }
+            }
+    int calls = 0;
+    expect(for_launches(1ull << 32, 1024, [&](uint32_t, uint32_t) { return ++calls == 2 ? 7 : 0; }) == 7 && calls == 2, "ends at the first error");
+    std::printf("launches sizes %" PRId64 " several %" PRId64 "\n", sizes, several);
+}
+
 }  // namespace
 
 int main() {
     overlaps();
+    launches();
     exchange_buffers();
     circulant_matrices();
     node_run_sizes();

@@ -28,6 +28,7 @@ struct NormArgs {
     int32_t T, D;
     int64_t ld, ldx;         // of the activations, of X and g
     uint32_t per_node;       // workgroups of a node
+    uint32_t first_block;    // of the launch
     DropArgs drop;
     bool stream;             // activations pass by the caches
     float eps;
@@ -50,8 +51,8 @@ struct NormArgs {
 // streams; the generator (18 quarter-rate products for eight elements) runs beside it.
 template <typename E, bool kSide>
 __global__ __launch_bounds__(kThreads) void k_dropout(NormArgs<E> a, int lanes_log2) {
-    const uint32_t node = blockIdx.x / a.per_node;
-    const int32_t t = (int32_t)((blockIdx.x - node * a.per_node) * (uint32_t)(kThreads >> lanes_log2)) + (int32_t)(threadIdx.x >> lanes_log2);
+    const uint32_t block = a.first_block + blockIdx.x, node = block / a.per_node;
+    const int32_t t = (int32_t)((block - node * a.per_node) * (uint32_t)(kThreads >> lanes_log2)) + (int32_t)(threadIdx.x >> lanes_log2);
     if (t >= a.T) return;
     const int64_t row = ((int64_t)node * a.T + t) * a.ld;
     const DropNode mask(a.drop, node);
@@ -113,8 +114,8 @@ template <typename E, int L, int N>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm(NormArgs<E> a) {
     constexpr int kRows = L > kThreads ? 1 : kThreads / L;  // rows of a workgroup
     __shared__ float s_sum[2][L > kWave ? L / kWave : 1];
-    const uint32_t node = blockIdx.x / a.per_node;
-    const int32_t t = (int32_t)((blockIdx.x - node * a.per_node) * kRows + threadIdx.x / L);
+    const uint32_t block = a.first_block + blockIdx.x, node = block / a.per_node;
+    const int32_t t = (int32_t)((block - node * a.per_node) * kRows + threadIdx.x / L);
     if (t >= a.T) return;  // all lanes of a row; no workgroup whose sums span wavefronts
     const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
     const int32_t lane = threadIdx.x & (L - 1);
@@ -164,8 +165,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm(NormArgs<E
 template <typename E>
 __global__ __launch_bounds__(kLongThreads) void k_norm_long(NormArgs<E> a) {
     __shared__ float s_sum[2][kLongThreads / kWave];
-    const uint32_t node = blockIdx.x / a.per_node;
-    const int32_t t = (int32_t)(blockIdx.x - node * a.per_node);
+    const uint32_t block = a.first_block + blockIdx.x, node = block / a.per_node;
+    const int32_t t = (int32_t)(block - node * a.per_node);
     const int64_t r = (int64_t)node * a.T + t, row = r * a.ld;
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     const DropNode mask(a.drop, node);
@@ -305,7 +306,7 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormA
     constexpr int kBlock = L > kThreads ? L : kThreads, kRows = kBlock / L;
     __shared__ float s_sum[2][L > kWave ? 2 * L / kWave : 1];
     __shared__ __align__(16) float s_part[kRows > 1 ? 2 * L * N * kOct : 4];
-    const uint32_t node = blockIdx.x / a.per_node, strip = blockIdx.x - node * a.per_node;
+    const uint32_t block = a.first_block + blockIdx.x, node = block / a.per_node, strip = block - node * a.per_node;
     const int32_t lane = threadIdx.x & (L - 1), sub = threadIdx.x / L;
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     const DropNode mask(a.drop, node);
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormA
             const int32_t c = (lane + k * L) * kOct;
             if (c >= a.D) continue;
             if (a.partial) {
-                float* out = a.partial + (int64_t)blockIdx.x * 2 * a.D;
+                float* out = a.partial + (int64_t)block * 2 * a.D;
                 piece_put<kOct, P>(out, c, a.D, dg[k]);
                 piece_put<kOct, P>(out + a.D, c, a.D, db[k]);
             } else {
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormA
 // and dx, one workgroup a row.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_norm_grad_columns(NormArgs<E> a, uint32_t column_blocks) {
-    const uint32_t node = blockIdx.x / (a.per_node * column_blocks), in_node = blockIdx.x - node * a.per_node * column_blocks;
+    const uint32_t block = a.first_block + blockIdx.x, node = block / (a.per_node * column_blocks), in_node = block - node * a.per_node * column_blocks;
     const uint32_t strip = in_node / column_blocks;
     const int64_t c = (int64_t)(in_node - strip * column_blocks) * kThreads + threadIdx.x;
     if (c >= a.D) return;
@@ -416,8 +417,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad_columns(NormArgs<E> a, u
 template <typename E, bool kSide>
 __global__ __launch_bounds__(kLongThreads) void k_norm_grad_long(NormArgs<E> a) {
     __shared__ float s_sum[2 * kLongThreads / kWave];
-    const uint32_t node = blockIdx.x / (uint32_t)a.T;
-    const uint32_t t = blockIdx.x - node * (uint32_t)a.T;
+    const uint32_t block = a.first_block + blockIdx.x, node = block / (uint32_t)a.T;
+    const uint32_t t = block - node * (uint32_t)a.T;
     const int64_t r = (int64_t)node * a.T + t;
     const uint32_t octs = ((uint32_t)a.D + kOct - 1) / kOct;
     const DropNode mask(a.drop, node);
@@ -452,12 +453,12 @@ __global__ __launch_bounds__(kLongThreads) void k_norm_grad_long(NormArgs<E> a) 
 // Adds the strips of a node: 64 columns a workgroup, its wavefronts share the strips, eight loads under way; a fixed order.  4 us, a chain
 // of two trips to memory.
 __global__ __launch_bounds__(kThreads) void k_norm_grad_join(const float* __restrict__ partial, uint32_t strips, int32_t D, uint32_t blocks_per_node,
-                                                             bool accumulate, float* __restrict__ g_gamma, float* __restrict__ g_beta, int64_t ldg) {
+                                                             bool accumulate, float* __restrict__ g_gamma, float* __restrict__ g_beta, int64_t ldg, uint32_t first_block) {
     constexpr int kWaves = kThreads / kWave;
     __shared__ float s_part[kWaves][kWave];
-    const uint32_t node = blockIdx.x / blocks_per_node;
+    const uint32_t block = first_block + blockIdx.x, node = block / blocks_per_node;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t c = (int64_t)(blockIdx.x - node * blocks_per_node) * kWave + lane;  // 0 .. 2D-1: gamma's columns, then beta's
+    const int64_t c = (int64_t)(block - node * blocks_per_node) * kWave + lane;  // 0 .. 2D-1: gamma's columns, then beta's
     const float* from = partial + (int64_t)node * strips * 2 * D + c;
     float sum = 0.f;
     if (c < 2 * (int64_t)D) {
@@ -526,18 +527,19 @@ hipError_t launch_dropout(const gpga_ctx* c, const RowsShape& s, const DropArgs&
         int lanes_log2 = 0;
         while (lanes_log2 < 8 && (1 << lanes_log2) < octs) ++lanes_log2;
         a.per_node = blocks_for(s.T, kThreads >> lanes_log2);
-        const dim3 grid(a.per_node * (uint32_t)s.n);
-        if (residual) k_dropout<E, true><<<grid, dim3(kThreads), 0, c->stream>>>(a, lanes_log2);
-        else k_dropout<E, false><<<grid, dim3(kThreads), 0, c->stream>>>(a, lanes_log2);
-        return hipGetLastError();
+        return launch_blocks((uint64_t)a.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+            a.first_block = first;
+            if (residual) k_dropout<E, true><<<grid, dim3(kThreads), 0, c->stream>>>(a, lanes_log2);
+            else k_dropout<E, false><<<grid, dim3(kThreads), 0, c->stream>>>(a, lanes_log2);
+        });
     };
     return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }
 
 hipError_t launch_norm(const gpga_ctx* c, const RowsShape& s, const DropArgs& drop, const void* x, const void* residual, int64_t gamma_off,
                        int64_t beta_off, float eps, void* u, void* y, float* stats) {
-    auto launch = [&](auto e) {
-        typedef decltype(e) E;
+    auto launch = [&](auto el) {
+        typedef decltype(el) E;
         typedef typename E::mem M;
         NormArgs<E> a = {};
         a.T = s.T;
@@ -554,18 +556,25 @@ hipError_t launch_norm(const gpga_ctx* c, const RowsShape& s, const DropArgs& dr
         a.stats = stats;
         a.gamma = c->x + gamma_off;
         a.beta = c->x + beta_off;
+        hipError_t e = hipSuccess;
         const bool held = with_row_shape<E>((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
             constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
             a.per_node = blocks_for(s.T, kBlock / L);
-            k_norm<E, L, N><<<dim3(a.per_node * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
+            e = launch_blocks((uint64_t)a.per_node * s.n, kBlock, [&](uint32_t first, dim3 grid) {
+                a.first_block = first;
+                k_norm<E, L, N><<<grid, dim3(kBlock), 0, c->stream>>>(a);
+            });
         });
         if constexpr (!E::kNarrow) {
             if (!held) {
                 a.per_node = (uint32_t)s.T;
-                k_norm_long<E><<<dim3(a.per_node * (uint32_t)s.n), dim3(kLongThreads), 0, c->stream>>>(a);
+                e = launch_blocks((uint64_t)a.per_node * s.n, kLongThreads, [&](uint32_t first, dim3 grid) {
+                    a.first_block = first;
+                    k_norm_long<E><<<grid, dim3(kLongThreads), 0, c->stream>>>(a);
+                });
             }
         }
-        return hipGetLastError();
+        return e;
     };
     return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }
@@ -598,27 +607,37 @@ hipError_t launch_norm_grad(const gpga_ctx* c, const RowsShape& s, const DropArg
         a.g_beta = c->g + beta_off;
         a.accumulate = accumulate;
         a.per_node = strips;
+        hipError_t e = hipSuccess;
         const bool held = with_row_shape<E>((s.D + kOct - 1) / kOct, [&](auto l, auto k) {
             constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
-            const dim3 grid(strips * (uint32_t)s.n);
-            if (more) k_norm_grad<E, L, N, true><<<grid, dim3(kBlock), 0, c->stream>>>(a);
-            else k_norm_grad<E, L, N, false><<<grid, dim3(kBlock), 0, c->stream>>>(a);
+            e = launch_blocks((uint64_t)strips * s.n, kBlock, [&](uint32_t first, dim3 grid) {
+                a.first_block = first;
+                if (more) k_norm_grad<E, L, N, true><<<grid, dim3(kBlock), 0, c->stream>>>(a);
+                else k_norm_grad<E, L, N, false><<<grid, dim3(kBlock), 0, c->stream>>>(a);
+            });
         });
         if constexpr (!E::kNarrow) {
             if (!held) {
                 const uint32_t column_blocks = blocks_for(s.D, kThreads);
-                k_norm_grad_columns<E><<<dim3(strips * column_blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(a, column_blocks);
-                const dim3 grid((uint32_t)s.T * (uint32_t)s.n);
-                if (s.T > 0 && more) k_norm_grad_long<E, true><<<grid, dim3(kLongThreads), 0, c->stream>>>(a);
-                else if (s.T > 0) k_norm_grad_long<E, false><<<grid, dim3(kLongThreads), 0, c->stream>>>(a);
+                e = launch_blocks((uint64_t)strips * column_blocks * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+                    a.first_block = first;
+                    k_norm_grad_columns<E><<<grid, dim3(kThreads), 0, c->stream>>>(a, column_blocks);
+                });
+                if (e != hipSuccess) return e;
+                e = launch_blocks((uint64_t)s.T * s.n, kLongThreads, [&](uint32_t first, dim3 grid) {
+                    a.first_block = first;
+                    if (more) k_norm_grad_long<E, true><<<grid, dim3(kLongThreads), 0, c->stream>>>(a);
+                    else k_norm_grad_long<E, false><<<grid, dim3(kLongThreads), 0, c->stream>>>(a);
+                });
             }
         }
-        return hipGetLastError();
+        return e;
     };
     const hipError_t e = s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
     if (e != hipSuccess || direct) return e;
     const uint32_t blocks = blocks_for(2 * (int64_t)s.D, kWave);
-    k_norm_grad_join<<<dim3(blocks * (uint32_t)s.n), dim3(kThreads), 0, c->stream>>>(static_cast<const float*>(scratch), strips, s.D, blocks, accumulate,
-                                                                                  c->g + gamma_off, c->g + beta_off, c->ld);
-    return hipGetLastError();
+    return launch_blocks((uint64_t)blocks * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+        k_norm_grad_join<<<grid, dim3(kThreads), 0, c->stream>>>(static_cast<const float*>(scratch), strips, s.D, blocks, accumulate, c->g + gamma_off,
+                                                                 c->g + beta_off, c->ld, first);
+    });
 }

@@ -5,7 +5,6 @@
 #include <cstdio>
 
 #include "gpga_rows.hpp"
-#include "gpga_spans.hpp"
 
 namespace {
 
@@ -55,7 +54,7 @@ int64_t elem_size(int32_t dtype) { return dtype == GPGA_F32 ? 4 : 2; }
 
 constexpr int32_t kMaxTokens = 1 << 30;     // token numbers of a node are 32-bit
 constexpr int32_t kMaxRow = 1 << 30;        // and so are column numbers
-constexpr int64_t kMaxGroups = 0x7fffffff;  // workgroups of a launch
+constexpr int64_t kMaxGroups = 0x7fffffff;  // rows of all nodes, and workgroups: numbered in 32 bits over all launches of a kernel
 
 // An array of rows as a call sees it.
 struct Array {

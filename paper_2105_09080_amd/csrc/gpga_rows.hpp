@@ -8,6 +8,7 @@
 
 #include "gpga_internal.hpp"
 #include "gpga_rng.hpp"
+#include "gpga_spans.hpp"
 
 constexpr uint32_t TAG_DROPOUT = 4u;  // low byte of the fourth counter word, the layer above it
 
@@ -252,6 +253,15 @@ inline bool stream_rows(const RowsShape& s, P... arrays) {
     uintptr_t at = (uintptr_t)(s.ld * size);
     for (const void* p : {static_cast<const void*>(arrays)...}) at |= reinterpret_cast<uintptr_t>(p);
     return (at & 15u) == 0 && (int64_t)s.n * s.T * s.D * size >= 32ll << 20;
+}
+
+// Launches `blocks` workgroups of `threads`: f(first, grid) launches those from number `first` on.
+template <typename F>
+inline hipError_t launch_blocks(uint64_t blocks, uint32_t threads, F&& f) {
+    return for_launches(blocks, threads, [&](uint32_t first, uint32_t count) {
+        f(first, dim3(count));
+        return hipGetLastError();
+    });
 }
 
 // Calls f with a value of the kind of element that `dtype` names; the narrow kinds are for rows shorter than a piece.

@@ -1,5 +1,5 @@
-// Which bytes the arrays of a call have, and whether two of them share any: the overlap checks of the language-model operators.
-// Host only, no HIP.
+// Host arithmetic of the language-model operators, without HIP: which bytes the arrays of a call have and whether two of them
+// share any, and how many launches a number of workgroups takes.
 #pragma once
 
 #include <cstdint>
@@ -28,4 +28,15 @@ inline bool rows_meet(const RowBytes& a, const void* q) {
     if (hi - lo >= (uintptr_t)((a.rows - 1) * a.step + a.width)) return false;
     const int64_t apart = (int64_t)((hi - lo) % (uintptr_t)a.step);
     return !(apart >= a.width && apart + a.width <= a.step);
+}
+
+// HIP takes fewer than 2^32 work-items a launch.  Calls f(first, count) for the workgroups first .. first + count - 1 of each launch that
+// `blocks` workgroups of `threads` need, in order, until one returns something other than Ok.  blocks <= 2^32.
+template <typename F>
+inline auto for_launches(uint64_t blocks, uint32_t threads, F&& f) -> decltype(f(0u, 0u)) {
+    const uint64_t most = 0xffffffffull / threads;
+    decltype(f(0u, 0u)) status{};
+    for (uint64_t first = 0; first < blocks && status == decltype(status){}; first += most)
+        status = f((uint32_t)first, (uint32_t)(blocks - first < most ? blocks - first : most));
+    return status;
 }

@@ -31,6 +31,7 @@ struct LossArgs {
     int32_t T, V;
     int64_t ld;
     uint32_t per_node;     // workgroups of a node
+    uint32_t first_block;  // of the launch
     const mem* z;
     const int32_t* labels;
     mem* dz;               // may be NULL
@@ -95,20 +96,23 @@ __device__ __forceinline__ void note_end(uint32_t* left, uint32_t workgroups, in
     *last = is;
 }
 
-__global__ __launch_bounds__(kNodeThreads) void k_count(const int32_t* __restrict__ labels, int32_t T, int32_t* __restrict__ count) {
+__global__ __launch_bounds__(kNodeThreads) void k_count(const int32_t* __restrict__ labels, int32_t T, int32_t* __restrict__ count,
+                                                    uint32_t first_block) {
     __shared__ int32_t s_count[kNodeThreads / kWave];
-    const int32_t n = count_labels(labels + (int64_t)blockIdx.x * T, T, kNodeThreads, s_count);
-    if (threadIdx.x == 0) count[blockIdx.x] = n;
+    const uint32_t node = first_block + blockIdx.x;
+    const int32_t n = count_labels(labels + (int64_t)node * T, T, kNodeThreads, s_count);
+    if (threadIdx.x == 0) count[node] = n;
 }
 
 // Where the losses of a node are not added up by the last workgroup of the launch that makes them.
 __global__ __launch_bounds__(kNodeThreads) void k_loss_mean(const float* __restrict__ row_loss, const int32_t* __restrict__ labels, int32_t T,
-                                                        float* __restrict__ loss) {
+                                                        float* __restrict__ loss, uint32_t first_block) {
     __shared__ int32_t s_count[kNodeThreads / kWave];
     __shared__ double s_sum[kNodeThreads / kWave];
-    const float* rows = row_loss + (int64_t)blockIdx.x * T;
-    const int32_t counted = count_labels(labels + (int64_t)blockIdx.x * T, T, kNodeThreads, s_count);
-    node_loss(T, kNodeThreads, counted, s_sum, loss + blockIdx.x, [&](int32_t t) { return rows[t]; });
+    const uint32_t node = first_block + blockIdx.x;
+    const float* rows = row_loss + (int64_t)node * T;
+    const int32_t counted = count_labels(labels + (int64_t)node * T, T, kNodeThreads, s_count);
+    node_loss(T, kNodeThreads, counted, s_sum, loss + node, [&](int32_t t) { return rows[t]; });
 }
 
 // Columns past the end of the row take no part.
@@ -129,8 +133,8 @@ __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_loss_held(LossA
     __shared__ float s_max[kWaves], s_sum[kWaves];
     __shared__ int32_t s_count[kWaves], s_last;
     __shared__ double s_total[kWaves];
-    const uint32_t node = blockIdx.x / a.per_node;
-    const int32_t t = (int32_t)((blockIdx.x - node * a.per_node) * kRows + threadIdx.x / L);
+    const uint32_t block = a.first_block + blockIdx.x, node = block / a.per_node;
+    const int32_t t = (int32_t)((block - node * a.per_node) * kRows + threadIdx.x / L);
     const int64_t r = (int64_t)node * a.T + t;
     const int32_t lane = threadIdx.x & (L - 1);
     const int32_t* labels = a.labels + (int64_t)node * a.T;
@@ -280,8 +284,8 @@ __global__ __launch_bounds__(kLanes) void k_loss_swept(LossArgs<E> a) {
     constexpr int kWaves = kLanes / kWave;
     __shared__ float s_max[kWaves], s_sum[kWaves];
     __shared__ int32_t s_count[kWaves];
-    const uint32_t node = blockIdx.x / a.per_node;
-    const int64_t r = blockIdx.x;
+    const uint32_t block = a.first_block + blockIdx.x, node = block / a.per_node;
+    const int64_t r = block;
     const int32_t* labels = a.labels + (int64_t)node * a.T;
     const int32_t label = a.labels[r];
     const typename E::mem* z = a.z + r * a.ld;
@@ -489,8 +493,14 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
     constexpr int64_t kMostAtCounter = 256;
     auto counter = [&](int64_t per_node) { return c->loss_left && s.n <= 65535 && per_node <= kMostAtCounter ? c->loss_left : nullptr; };
     auto count_launch = [&]() {
-        k_count<<<dim3((uint32_t)s.n), dim3(kNodeThreads), 0, c->stream>>>(labels, s.T, count);
-        return hipGetLastError();
+        return launch_blocks((uint64_t)s.n, kNodeThreads, [&](uint32_t first, dim3 grid) {
+            k_count<<<grid, dim3(kNodeThreads), 0, c->stream>>>(labels, s.T, count, first);
+        });
+    };
+    auto mean_launch = [&]() {
+        return launch_blocks((uint64_t)s.n, kNodeThreads, [&](uint32_t first, dim3 grid) {
+            k_loss_mean<<<grid, dim3(kNodeThreads), 0, c->stream>>>(rows, labels, s.T, loss, first);
+        });
     };
     auto launch = [&](auto el) {
         typedef decltype(el) E;
@@ -535,8 +545,10 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
                 e = count_launch();
             }
             if (e != hipSuccess) return;
-            k_loss_held<E, L, N><<<dim3(a.per_node * (uint32_t)s.n), dim3(kBlock), 0, c->stream>>>(a);
-            e = hipGetLastError();
+            e = launch_blocks((uint64_t)a.per_node * s.n, kBlock, [&](uint32_t first, dim3 grid) {
+                a.first_block = first;
+                k_loss_held<E, L, N><<<grid, dim3(kBlock), 0, c->stream>>>(a);
+            });
         };
         // the loss alone needs no row held: 8 x 512 rows of 32000 bf16 46 us, held 60
         const bool held = !(s.D > kHeldAlone && !dlogits) && with_row_shape<E>((s.D + kOct - 1) / kOct, held_launch);
@@ -548,18 +560,16 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
                     e = count_launch();
                 }
                 if (e != hipSuccess) return e;
-                if (dlogits) k_loss_swept<E, kNodeThreads><<<dim3(all), dim3(kNodeThreads), 0, c->stream>>>(a);
-                else k_loss_swept<E, 512><<<dim3(all), dim3(512), 0, c->stream>>>(a);
-                e = hipGetLastError();
+                e = launch_blocks(all, dlogits ? kNodeThreads : 512, [&](uint32_t first, dim3 grid) {
+                    a.first_block = first;
+                    if (dlogits) k_loss_swept<E, kNodeThreads><<<grid, dim3(kNodeThreads), 0, c->stream>>>(a);
+                    else k_loss_swept<E, 512><<<grid, dim3(512), 0, c->stream>>>(a);
+                });
             }
         }
         if (e != hipSuccess || a.left) return e;
-        k_loss_mean<<<dim3((uint32_t)s.n), dim3(kNodeThreads), 0, c->stream>>>(rows, labels, s.T, loss);
-        return hipGetLastError();
+        return mean_launch();
     };
-    if (s.T == 0) {  // losses of 0
-        k_loss_mean<<<dim3((uint32_t)s.n), dim3(kNodeThreads), 0, c->stream>>>(rows, labels, 0, loss);
-        return hipGetLastError();
-    }
+    if (s.T == 0) return mean_launch();  // losses of 0
     return s.D < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
 }

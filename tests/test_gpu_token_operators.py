@@ -673,3 +673,77 @@ def test_tokens_and_labels_within_an_output_are_refused(hx):
     assert torch.equal(y, sim.X[:, None, :D].expand(n, T, D))
     grad(at(y, D))
     sim.close()
+
+
+def room(gb):
+    """Skips a test that needs more device memory than there is."""
+    torch.cuda.empty_cache()
+    free = torch.cuda.mem_get_info()[0] / 1e9
+    if free < gb:
+        pytest.skip(f"needs {gb} GB of device memory, {free:.0f} are free")
+
+
+def test_more_work_items_than_a_launch_takes_in_rows(hx):
+    """HIP refuses a launch of 2^32 work-items: rows of few columns pass that within the n*T < 2^31 of the header.  The last rows are
+    compared with the same rows by themselves, bit for bit (layer norm, the loss) or with the table's rows (the lookup)."""
+    room(45)
+    from paper_2105_09080_amd import binding as B
+    R, tail = (1 << 29) + 4321, 5000                               # eight lanes a row in the norm, sixteen in the loss, four in the lookup of D = 24
+    sim, X, rng = make_sim(hx, 1, 64, seed=31)
+    x = torch.empty((1, R, 2), dtype=torch.float16, device="cuda").normal_()
+    y = torch.full_like(x, float("nan"))
+    B.gpga_layer_norm(sim.ctx, x, None, R, 2, 2, B.GPGA_F16, 0.0, 0, 0, 0, 2, 1e-5, None, y, None)
+    for part in (slice(0, tail), slice(R // 2, R // 2 + tail), slice(R - tail, R)):
+        assert torch.equal(y[:, part], sim.layer_norm(x[:, part].contiguous(), 0, 2)[0])
+    assert bool(torch.isfinite(y).all())
+    labels = torch.randint(-1, 2, (1, R), dtype=torch.int32, device="cuda")
+    scale = float(1 << 29)                                         # gradients of a mean over 2^28 rows, in fp16
+    loss, dz = sim.token_loss(x, labels, grad_scale=scale)
+    counted = (labels >= 0).sum().item()
+    z = x.double().view(R, 2)
+    want = torch.nn.functional.softplus(z[:, 1] - z[:, 0]) + torch.where(labels[0] == 1, z[:, 0] - z[:, 1], 0.0)
+    want = torch.where(labels[0] >= 0, want, 0.0).sum().item() / counted
+    del z
+    assert abs(loss.item() - want) <= 1e-6 * want
+    for part in (slice(0, tail), slice(R - tail, R)):
+        q = torch.softmax(x[0, part].double(), dim=1)
+        q.scatter_add_(1, labels[0, part, None].clamp(min=0).long(), -torch.ones((tail, 1), dtype=torch.float64, device="cuda"))
+        q = torch.where((labels[0, part] >= 0)[:, None], q * (scale / counted), 0.0)
+        assert bool(((dz[0, part].double() - q).abs() <= 2.0 ** -11 * q.abs() + 2.0 ** -20 * scale / counted + 2.0 ** -25).all())
+    sim.close()
+
+
+def test_more_work_items_than_a_launch_takes_in_nodes(hx):
+    """A workgroup of 1024 a node in the mean of the losses: 2^22 nodes and more."""
+    n = (1 << 22) + 7
+    sim = hx.Simulation(n, 4, topology="none", H=0, lr=0.1)
+    z = torch.randn((n, 1, 2), device="cuda")
+    labels = torch.randint(-1, 2, (n, 1), dtype=torch.int32, device="cuda")
+    loss, _ = sim.token_loss(z, labels, grad=False)
+    want = torch.nn.functional.softplus((z[:, 0, 1] - z[:, 0, 0]).double()) + torch.where(labels[:, 0] == 1, (z[:, 0, 0] - z[:, 0, 1]).double(), 0.0)
+    assert bool(((loss.double() - torch.where(labels[:, 0] >= 0, want, 0.0)).abs() <= 1e-5).all())
+    sim.close()
+
+
+def test_more_work_items_than_a_launch_takes_in_a_table(hx):
+    """Tables of 2^34 floats and more in all: the zeros of their gradient are a quarter as many work-items."""
+    n, V, D, T = 2, (1 << 22) + 3, 2048, 300
+    room(3 * 4e-9 * n * V * D + 2)
+    sim = hx.Simulation(n, V * D, topology="none", H=0, lr=0.1)
+    sim.G.fill_(1.0)
+    tokens = torch.randint(0, V, (n, T), dtype=torch.int32, device="cuda")
+    tokens[:, :7], tokens[:, 7:9] = V - 1, -1
+    dy = torch.randn((n, T, D), device="cuda")
+    sim.embed_grad(tokens, dy, 0, V)
+    for i in range(n):
+        g = sim.G[i].view(V, D)
+        seen = tokens[i][tokens[i] >= 0].unique().long()
+        for v in seen.tolist()[::37] + [V - 1]:
+            assert torch.allclose(g[v], dy[i][tokens[i] == v].sum(dim=0), rtol=1e-5, atol=1e-5)
+        assert bool(g[seen].any(dim=1).all())
+        g[seen] = 0.0
+        step = 1 << 20
+        assert not any(bool(g[k:k + step].any()) for k in range(0, V, step))
+    sim.close()
+    del g, sim
+    torch.cuda.empty_cache()

@@ -146,3 +146,9 @@ def test_overlaps_go_by_the_bytes_that_rows_have(facts):
     """The overlap checks of the language-model operators, against a walk over every byte of small arrays."""
     row, = [f for f in facts if f[0] == "overlaps"]
     assert int(row[2]) > 20_000 and 0 < int(row[4]) < int(row[2])
+
+
+def test_launches_stay_below_the_limit_of_work_items(facts):
+    """2^32 work-items are refused by HIP: workgroups beyond go into launches of their own, each number once and in order."""
+    row, = [f for f in facts if f[0] == "launches"]
+    assert int(row[4]) > 50 and int(row[4]) < int(row[2])
