@@ -37,13 +37,14 @@ class Simulation:
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
-        self._device_index, self._stream_address = self.stream.device.index, self.stream.cuda_stream
+        self._stream_address = self.stream.cuda_stream
         self.ctx = B.gpga_create(n, d, topology, H, lr, momentum)
         with torch.cuda.stream(self.stream):
             self._bufs = [torch.empty((n, self.ld), dtype=torch.float32, device=self.device) for _ in range(2)]
             need_m = (momentum != 0.0) if alloc_m is None else alloc_m
             self.m = torch.zeros((n, self.ld), dtype=torch.float32, device=self.device) if need_m else None
             self.g = torch.zeros((n, self.ld), dtype=torch.float32, device=self.device)
+        self._device_index = self.g.get_device()
         self._addr = {t.data_ptr(): t for t in self._bufs}
         B.gpga_bind(self.ctx, self._bufs[0], self._bufs[1], self.m, self.g, self.ld, self.stream.cuda_stream)
         self._keep = []
@@ -212,15 +213,18 @@ class Simulation:
 
     def _tokens(self, t: torch.Tensor) -> int:
         """Tokens a node of an (n, T) int32 tensor."""
-        if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != self.n or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError(f"expected a contiguous (n = {self.n}, T) int32 tensor on the GPU, got {tuple(t.shape)} {t.dtype}")
+        if (t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != self.n or not t.is_contiguous() or
+                t.get_device() != self._device_index):
+            raise ValueError(f"expected a contiguous (n = {self.n}, T) int32 tensor on the simulation's GPU, "
+                             f"got {tuple(t.shape)} {t.dtype} on {t.device}")
         return t.shape[1]
 
     def _rows(self, first: torch.Tensor, *others):
         """(T, D, ld, dtype) of activations of one call."""
         shape, dtype = first.shape, first.dtype
-        if len(shape) != 3 or shape[0] != self.n or dtype not in _DTYPE or not first.is_cuda:
-            raise ValueError(f"expected an (n = {self.n}, T, D) fp32, bf16 or fp16 tensor on the GPU, got {tuple(shape)} {dtype}")
+        if len(shape) != 3 or shape[0] != self.n or dtype not in _DTYPE or first.get_device() != self._device_index:
+            raise ValueError(f"expected an (n = {self.n}, T, D) fp32, bf16 or fp16 tensor on the simulation's GPU, "
+                             f"got {tuple(shape)} {dtype} on {first.device}")
         n, T, D = shape
         ld = D if first.is_contiguous() else first.stride(1) if T > 1 else first.stride(0) if n > 1 else D
         for t in (first, *others):
@@ -291,7 +295,7 @@ class Simulation:
                         accumulate: bool = False):
         """(du, dx): gradients of the residual and of x; those of gamma and beta land in G.  dx is du where p is 0."""
         T, D, ld, dt = self._rows(dy, u, more)
-        if stats.dtype != torch.float32 or stats.shape != (self.n, T, 2) or not stats.is_contiguous() or not stats.is_cuda:
+        if stats.dtype != torch.float32 or stats.shape != (self.n, T, 2) or not stats.is_contiguous() or stats.device != dy.device:
             raise ValueError("stats are the (n, T, 2) fp32 pairs that layer_norm returns")
         foreign = self._foreign()
         du = self._like(dy, ld, foreign)
