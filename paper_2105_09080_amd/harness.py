@@ -189,7 +189,8 @@ class Simulation:
     # -- operators of language models --------------------------------------------------
     # Activations are (n, T, D) tensors whose tokens lie a common number of elements apart (rows of a wider tensor are
     # fine); parameters are named by their column offset in X, their gradients land in the same columns of G.  What the
-    # calls return is allocated for, and written on, the simulation's stream.
+    # calls return is allocated for, and written on, the simulation's stream.  The gradients are calls of their own: torch's
+    # autograd knows nothing of these, so activations that it follows are refused (hand over x.detach(), or call under no_grad).
     def _foreign(self) -> bool:
         """Whether torch's current stream is another one than the simulation's."""
         return _current_stream(self._device_index) != self._stream_address
@@ -227,9 +228,12 @@ class Simulation:
                              f"got {tuple(shape)} {dtype} on {first.device}")
         n, T, D = shape
         ld = D if first.is_contiguous() else first.stride(1) if T > 1 else first.stride(0) if n > 1 else D
+        followed = torch.is_grad_enabled()
         for t in (first, *others):
             if t is None:
                 continue
+            if followed and t.requires_grad:
+                raise ValueError("an activation requires grad: these calls are not recorded for torch's backward()")
             if t.shape != shape or t.dtype != dtype or t.device != first.device:
                 raise ValueError("the activations of a call differ in shape, type or device")
             if ld == D and t.is_contiguous():

@@ -36,3 +36,20 @@ def test_tensors_of_another_device_are_refused(sim, fake, other):
                  lambda: sim.token_loss(x, tok1), lambda: sim.token_loss(x, tok, grad=x1)):
         with pytest.raises(ValueError, match="GPU|device|stats"):
             call()
+
+
+def test_tensors_that_autograd_follows_are_refused(sim, fake):
+    """What comes back would be cut off from them without a word."""
+    tok, x, stats = fake(2, 3, dtype=torch.int32), fake(2, 3, 8), fake(2, 3, 2)
+    leaf = fake(2, 3, 8).requires_grad_()
+    for w in (leaf, leaf * 2):
+        calls = (lambda: sim.embed_grad(tok, w, 0, 4), lambda: sim.dropout(w, 0.5, seed=1), lambda: sim.dropout(x, 0.5, seed=1, residual=w),
+                 lambda: sim.dropout(x, 0.5, seed=1, out=w), lambda: sim.layer_norm(w, 0, 8), lambda: sim.layer_norm(x, 0, 8, residual=w),
+                 lambda: sim.layer_norm_grad(w, x, stats, 0, 8), lambda: sim.layer_norm_grad(x, w, stats, 0, 8),
+                 lambda: sim.layer_norm_grad(x, x, stats, 0, 8, more=w), lambda: sim.token_loss(w, tok), lambda: sim.token_loss(x, tok, grad=w))
+        for call in calls:
+            with pytest.raises(ValueError, match="requires grad"):
+                call()
+        assert sim._rows(w.detach(), x)[:2] == (3, 8)
+        with torch.no_grad():
+            assert sim._rows(w, x)[:2] == (3, 8)
