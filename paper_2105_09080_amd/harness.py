@@ -58,13 +58,12 @@ class Simulation:
     # -- state access -----------------------------------------------------------
     @property
     def X(self) -> torch.Tensor:
-        """Live iterates, (n, d): the bound buffer, or a view of its first d columns."""
-        x = self._addr[B.gpga_current_x(self.ctx)]
-        return x if self.ld == self.d else x[:, : self.d]
+        """Live iterates, (n, d) view of the (n, ld) buffer."""
+        return self._addr[B.gpga_current_x(self.ctx)][:, : self.d]
 
     @property
     def G(self) -> torch.Tensor:
-        return self.g if self.ld == self.d else self.g[:, : self.d]
+        return self.g[:, : self.d]
 
     @property
     def M(self):

@@ -53,3 +53,18 @@ def test_tensors_that_autograd_follows_are_refused(sim, fake):
         assert sim._rows(w.detach(), x)[:2] == (3, 8)
         with torch.no_grad():
             assert sim._rows(w, x)[:2] == (3, 8)
+
+
+@pytest.mark.parametrize("ld", [64, 70])
+def test_the_state_that_is_handed_out_is_a_view(sim, monkeypatch, ld):
+    """Its shape is the caller's to change; the bound buffer keeps its own."""
+    from paper_2105_09080_amd import harness
+    sim.ld, buf, sim.g = ld, torch.zeros(2, ld), torch.ones(2, ld)
+    sim._addr = {buf.data_ptr(): buf}
+    monkeypatch.setattr(harness.B, "gpga_current_x", lambda ctx: buf.data_ptr())
+    for name, whole in (("X", buf), ("G", sim.g)):
+        getattr(sim, name).t_()
+        getattr(sim, name).unsqueeze_(0)
+        assert getattr(sim, name).shape == (2, 64) and whole.shape == (2, ld) and getattr(sim, name).data_ptr() == whole.data_ptr()
+        getattr(sim, name).fill_(3.0)
+        assert bool((whole[:, :64] == 3.0).all())
