@@ -127,6 +127,13 @@ def _check(ctx, status: int):
         raise GpgaError(status, (msg or b"").decode())
 
 
+def _int32(*values):
+    """Refuses what ctypes would cut to its lower 32 bits (negative ones that fit are the library's to refuse)."""
+    for v in values:
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise GpgaError(GPGA_EINVAL, f"{v} does not fit 32 bits")
+
+
 # ---- one function per C entry point -----------------------------------------
 
 def gpga_create(n: int, d: int, topology, H: int, lr: float, momentum: float):
@@ -323,31 +330,43 @@ def gpga_query(ctx, name: str) -> float:
 
 def gpga_embed(ctx, tokens, T: int, table_off: int, V: int, D: int, scale: float, y, ld: int, dtype: int):
     """tokens: n x T int32; y: n*T rows of D elements (``dtype``: GPGA_F32, GPGA_BF16 or GPGA_F16), ``ld`` apart."""
+    if (T | V | D) >> 31:
+        _int32(T, V, D)
     _check(ctx, _lib.gpga_embed(ctx, _ptr(tokens), T, table_off, V, D, scale, _ptr(y), ld, dtype))
 
 
 def gpga_embed_grad(ctx, tokens, T: int, table_off: int, V: int, D: int, scale: float, dy, ld: int, dtype: int,
                     accumulate: bool = False):
+    if (T | V | D) >> 31:
+        _int32(T, V, D)
     _check(ctx, _lib.gpga_embed_grad(ctx, _ptr(tokens), T, table_off, V, D, scale, _ptr(dy), ld, dtype, int(accumulate)))
 
 
 def gpga_dropout(ctx, x, residual, T: int, D: int, ld: int, dtype: int, p: float, seed: int, layer: int, y):
+    if (T | D | layer) >> 31:
+        _int32(T, D, layer)
     _check(ctx, _lib.gpga_dropout(ctx, _ptr(x), _ptr(residual), T, D, ld, dtype, p, seed, layer, _ptr(y)))
 
 
 def gpga_layer_norm(ctx, x, residual, T: int, D: int, ld: int, dtype: int, p: float, seed: int, layer: int,
                     gamma_off: int, beta_off: int, eps: float, u, y, stats):
+    if (T | D | layer) >> 31:
+        _int32(T, D, layer)
     _check(ctx, _lib.gpga_layer_norm(ctx, _ptr(x), _ptr(residual), T, D, ld, dtype, p, seed, layer, gamma_off, beta_off,
                                      eps, _ptr(u), _ptr(y), _ptr(stats)))
 
 
 def gpga_layer_norm_grad(ctx, dy, u, stats, more, T: int, D: int, ld: int, dtype: int, p: float, seed: int, layer: int,
                          gamma_off: int, beta_off: int, du, dx, accumulate: bool = False):
+    if (T | D | layer) >> 31:
+        _int32(T, D, layer)
     _check(ctx, _lib.gpga_layer_norm_grad(ctx, _ptr(dy), _ptr(u), _ptr(stats), _ptr(more), T, D, ld, dtype, p, seed,
                                           layer, gamma_off, beta_off, _ptr(du), _ptr(dx), int(accumulate)))
 
 
 def gpga_token_loss(ctx, logits, labels, T: int, V: int, ld: int, dtype: int, grad_scale: float, loss, dlogits=None):
+    if (T | V) >> 31:
+        _int32(T, V)
     _check(ctx, _lib.gpga_token_loss(ctx, _ptr(logits), _ptr(labels), T, V, ld, dtype, grad_scale, _ptr(loss),
                                      _ptr(dlogits)))
 

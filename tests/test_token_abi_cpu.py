@@ -33,3 +33,26 @@ def test_a_null_context_is_refused(name):
     from paper_2105_09080_amd import binding as B
     types = next(types for n, _, types in B.SIGNATURES if n == name)
     assert B.raw_status(name, *[None if t is ctypes.c_void_p else 0 for t in types]) == B.GPGA_EINVAL
+
+
+@pytest.mark.parametrize("wide", [2 ** 31, 2 ** 32 + 5, -2 ** 31 - 1, -2 ** 32 + 5])
+def test_numbers_that_do_not_fit_their_argument_are_refused(wide):
+    """Cut to 32 bits a vocabulary of 2^32 + 5 would be one of 5, and layer 2^32 would have the masks of layer 0."""
+    from paper_2105_09080_amd import binding as B
+    calls = {"gpga_embed": (("T", "V", "D"), lambda T=1, V=1, D=1: B.gpga_embed(None, None, T, 0, V, D, 1.0, None, 1, 0)),
+             "gpga_embed_grad": (("T", "V", "D"), lambda T=1, V=1, D=1: B.gpga_embed_grad(None, None, T, 0, V, D, 1.0, None, 1, 0)),
+             "gpga_dropout": (("T", "D", "layer"), lambda T=1, D=1, layer=0: B.gpga_dropout(None, None, None, T, D, 1, 0, 0.1, 1, layer, None)),
+             "gpga_layer_norm": (("T", "D", "layer"), lambda T=1, D=1, layer=0: B.gpga_layer_norm(
+                 None, None, None, T, D, 1, 0, 0.1, 1, layer, 0, 0, 1e-5, None, None, None)),
+             "gpga_layer_norm_grad": (("T", "D", "layer"), lambda T=1, D=1, layer=0: B.gpga_layer_norm_grad(
+                 None, None, None, None, None, T, D, 1, 0, 0.1, 1, layer, 0, 0, None, None)),
+             "gpga_token_loss": (("T", "V"), lambda T=1, V=1: B.gpga_token_loss(None, None, None, T, V, 1, 0, 1.0, None))}
+    assert tuple(calls) == NAMES
+    for names, call in calls.values():
+        for name in names:
+            with pytest.raises(B.GpgaError, match="32 bits") as e:
+                call(**{name: wide})
+            assert e.value.status == B.GPGA_EINVAL
+            with pytest.raises(B.GpgaError) as e:                  # what fits reaches the library: no context
+                call(**{name: -1})
+            assert "32 bits" not in str(e.value) and e.value.status == B.GPGA_EINVAL
