@@ -251,6 +251,8 @@ class Simulation:
     def embed(self, tokens: torch.Tensor, table_off: int, V: int, D: int, *, scale: float = 1.0,
               dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """scale * E_i[tokens]: (n, T, D); tokens below 0 give zeros."""
+        if dtype not in _DTYPE:
+            raise ValueError(f"dtype must be fp32, bf16 or fp16, got {dtype}")
         T, foreign = self._tokens(tokens), self._foreign()
         y = self._empty((self.n, T, D), dtype, foreign)
         B.gpga_embed(self.ctx, tokens, T, table_off, V, D, scale, y, D, _DTYPE[dtype])
@@ -302,7 +304,7 @@ class Simulation:
             raise ValueError("stats are the (n, T, 2) fp32 pairs that layer_norm returns")
         foreign = self._foreign()
         du = self._like(dy, ld, foreign)
-        drops = p != 0.0 and int(float(np.float32(p)) * 65536 + 0.5) > 0     # p as the library keeps it
+        drops = 0.0 < p < 1.0 and int(float(np.float32(p)) * 65536 + 0.5) > 0    # p as the library keeps it; others are its to refuse
         dx = self._like(dy, ld, foreign) if drops else None
         B.gpga_layer_norm_grad(self.ctx, dy, u, stats, more, T, D, ld, dt, p, seed, layer, gamma_off, beta_off, du, dx,
                                accumulate)

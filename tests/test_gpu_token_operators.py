@@ -747,3 +747,19 @@ def test_more_work_items_than_a_launch_takes_in_a_table(hx):
     sim.close()
     del g, sim
     torch.cuda.empty_cache()
+
+
+def test_types_and_probabilities_are_refused_in_the_calls_own_way(hx):
+    from paper_2105_09080_amd import binding as B
+    sim, X, rng = make_sim(hx, 2, 64, seed=0)
+    tok, x, stats = torch.zeros((2, 3), dtype=torch.int32, device="cuda"), torch.zeros((2, 3, 8), device="cuda"), torch.zeros((2, 3, 2), device="cuda")
+    for dtype in (torch.float64, torch.int32):
+        with pytest.raises(ValueError, match="dtype"):
+            sim.embed(tok, 0, 4, 8, dtype=dtype)
+    for p in (float("nan"), float("inf"), -0.5, 1.0, 1.0 - 1e-9):
+        for call in (lambda: sim.dropout(x, p, seed=1), lambda: sim.layer_norm(x, 0, 8, p=p), lambda: sim.layer_norm_grad(x, x, stats, 0, 8, p=p)):
+            with pytest.raises(B.GpgaError, match="p = ") as e:
+                call()
+            assert e.value.status == B.GPGA_EINVAL
+    assert sim.layer_norm_grad(x, x, stats, 0, 8, p=1e-9)[1] is not None   # keeps everything: dx is du
+    sim.close()
