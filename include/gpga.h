@@ -393,7 +393,12 @@ gpga_status gpga_query(gpga_ctx* ctx, const char* name, double* value_out);
  * gradient within g_dev.  tokens_dev and
  * labels_dev are n x T int32.  Results do not depend on the order in which workgroups run: the same call gives the same
  * bits.  Asynchronous on the bound stream; the embedding's and the layer norm's gradients and the loss use scratch, which
- * grows with the largest call and stays until gpga_destroy (a first call of its size cannot be captured into a graph). */
+ * grows with the largest call and stays until gpga_destroy (a first call of its size cannot be captured into a graph).  All
+ * calls of a context share it: after gpga_bind with another stream, and for a graph that is replayed on another stream, the
+ * caller sees to it that they follow each other.
+ * A captured call keeps what it was called with: the array that was the live X then (after an odd number of gpga_steps since,
+ * the other one is), and the k of the dropout mask, which is the same in every replay.  A training loop captures an even
+ * number of iterations with their steps, and other masks take another capture (or a call that is not captured). */
 typedef enum { GPGA_F32 = 0, GPGA_BF16 = 1, GPGA_F16 = 2 } gpga_dtype;
 
 /* y[i,t,:] = scale * E_i[tokens[i,t],:], E_i the V x D table (row-major, dense) in columns table_off .. table_off + V*D

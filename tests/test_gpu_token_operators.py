@@ -763,3 +763,34 @@ def test_types_and_probabilities_are_refused_in_the_calls_own_way(hx):
             assert e.value.status == B.GPGA_EINVAL
     assert sim.layer_norm_grad(x, x, stats, 0, 8, p=1e-9)[1] is not None   # keeps everything: dx is du
     sim.close()
+
+
+def test_a_captured_call_keeps_its_iterates_and_its_iteration(hx):
+    """What the header says of captured calls: the array of X that was live then, and the mask of that k."""
+    n, T, V, D, p = 2, 9, 7, 8, 0.5
+    side = torch.cuda.Stream()
+    sim, X, rng = make_sim(hx, n, V * D, seed=41, stream=side)
+    tok = torch.as_tensor(rng.integers(0, V, size=(n, T)), dtype=torch.int32).cuda()
+    sim.set_state(k=4)
+    torch.cuda.synchronize()
+    run = lambda: (sim.embed(tok, 0, V, D), sim.dropout(torch.ones((n, T, D), device="cuda"), p, seed=5))
+    with torch.cuda.stream(side):
+        run()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            y, mask = run()
+        first, k0_mask = sim.X, host(run()[1])
+        for turn in range(1, 4):
+            sim.G.normal_()
+            sim.step()
+            y.fill_(0.0)
+            mask.fill_(-1.0)
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(y, first.view(n, V, D)[torch.arange(n, device="cuda")[:, None], tok.long()])
+            assert np.array_equal(host(mask), k0_mask)
+            eager = run()
+            side.synchronize()
+            assert torch.equal(y, eager[0]) == (turn % 2 == 0) and not np.array_equal(host(eager[1]), k0_mask)
+    sim.close()
