@@ -794,3 +794,145 @@ def test_a_captured_call_keeps_its_iterates_and_its_iteration(hx):
             side.synchronize()
             assert torch.equal(y, eager[0]) == (turn % 2 == 0) and not np.array_equal(host(eager[1]), k0_mask)
     sim.close()
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,T,V,pad", [(1, 200, 9000, 0), (2, 100, 9001, 3), (3, 80, 30000, 0)])
+def test_token_loss_of_rows_in_pieces_that_a_launch_joins(hx, n, T, V, pad, dtype):
+    """Fewer rows than compute units, more pieces a node than meet at a counter."""
+    test_token_loss(hx, n, T, V, pad, dtype)
+
+
+def test_broken_logits_in_pieces_that_a_launch_joins(hx):
+    test_token_loss_of_masked_and_broken_logits(hx, 12000, 50)
+
+
+# Arrays of 32 MiB and more whose rows begin on 16-byte boundaries pass by the caches; the same call on addresses one element on
+# does not.  Neither reads or computes anything else, so the bits are the same.
+LARGE = [("f32", 3, 2100, 1340, 0), ("bf16", 3, 4200, 1333, 11), ("f32", 2, 520, 8200, 0), ("f16", 2, 2060, 4104, 0), ("f32", 40, 4100, 52, 0)]
+
+
+def blank(shape, ld, dtype, elements):
+    """An (n, T, D) tensor of NaN, rows `ld` elements apart, its address `elements` behind a 16-byte boundary."""
+    n, T, D = shape
+    flat = torch.full((n * T * ld + 16,), float("nan"), dtype=dtype, device="cuda")
+    out = flat[elements:elements + n * T * ld].view(n, T, ld)[..., :D]
+    assert out.stride() == (T * ld, ld, 1) and out.data_ptr() % 16 == (elements * out.element_size()) % 16
+    return out
+
+
+def off_by(t, elements):
+    """A copy of such a tensor at another address."""
+    return blank(t.shape, t.stride(1), t.dtype, elements).copy_(t)
+
+
+def raw(t):
+    """(T, D, ld, dtype number) as the C calls take them."""
+    return t.shape[1], t.shape[2], t.stride(1), {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[t.dtype]
+
+
+@pytest.mark.parametrize("dtype,n,T,D,pad", LARGE)
+def test_large_arrays_that_pass_by_the_caches(hx, dtype, n, T, D, pad):
+    from paper_2105_09080_amd import binding as B
+    dt = TYPES[dtype][0]
+    V, p, seed = 300, 0.2, 77
+    sim, X, rng = make_sim(hx, n, V * D + 2 * D, seed=D)
+    tok = torch.as_tensor(some_tokens(rng, n, T, V, "mixed"), dtype=torch.int32).cuda()
+    make = lambda: blank((n, T, D), D + pad, dt, 0).normal_()
+    x, residual, dy = make(), make(), make()
+    assert x.element_size() * n * T * D >= 32 << 20 and x.stride(1) * x.element_size() % 16 == 0
+    _, _, ld, code = raw(x)
+    results = []
+    for off in (0, 1):
+        xs, rs, ds = off_by(x, off), off_by(residual, off), off_by(dy, off)
+        new = lambda: blank((n, T, D), ld, dt, off)
+        e, drop, u, y, du, dx, stats = new(), new(), new(), new(), new(), new(), torch.zeros((n, T, 2), device="cuda")
+        B.gpga_embed(sim.ctx, tok, T, 0, V, D, 1.5, e, ld, code)
+        B.gpga_dropout(sim.ctx, xs, rs, T, D, ld, code, p, seed, 1, drop)
+        B.gpga_layer_norm(sim.ctx, xs, rs, T, D, ld, code, p, seed, 2, V * D, V * D + D, 1e-5, u, y, stats)
+        sim.G.zero_()
+        B.gpga_layer_norm_grad(sim.ctx, ds, u, stats, rs, T, D, ld, code, p, seed, 2, V * D, V * D + D, du, dx)
+        B.gpga_embed_grad(sim.ctx, tok, T, 0, V, D, 1.5, dx, ld, code)
+        results.append([e, drop, u, y, stats, du, dx, sim.G.clone()])
+    for a, b in zip(*results):
+        assert bool(torch.isfinite(a).all()) and torch.equal(a, b)
+    # and some rows against the oracle
+    at = slice(0, 3)
+    want = orc.dropout(host(x[:, at]), host(residual[:, at]), p, seed, 1, 0)
+    _, u_, sub = TYPES[dtype]
+    close(results[0][1][:, at], want, u_ * np.abs(want) + 3 * E32 * dropped_bound(host(x[:, at]), host(residual[:, at]), 1.26) + sub, "dropout")
+    want = orc.embed(X[:, :V * D].reshape(n, V, D), tok[:, T - 3:].cpu().numpy(), 1.5)
+    close(results[0][0][:, T - 3:], want, (u_ + 2 * E32) * np.abs(want) + sub, "lookup")
+    sim.close()
+
+
+@pytest.mark.parametrize("dtype,n,T,V,pad", [("f32", 2, 300, 16004, 0), ("bf16", 3, 500, 12001, 7), ("f16", 2, 300, 32768, 0), ("bf16", 1, 600, 40000, 0)])
+def test_large_logits_that_pass_by_the_caches(hx, dtype, n, T, V, pad):
+    dt, u, sub = TYPES[dtype]
+    sim, X, rng = make_sim(hx, n, 4, seed=V)
+    z = blank((n, T, V), V + pad, dt, 0).normal_()
+    labels = torch.randint(-1, V, (n, T), dtype=torch.int32, device="cuda")
+    assert z.element_size() * n * T * V >= 32 << 20 and z.stride(1) * z.element_size() % 16 == 0
+    results = []
+    for off in (0, 1):
+        zs, dz = off_by(z, off), blank((n, T, V), V + pad, dt, off)
+        loss, _ = sim.token_loss(zs, labels, grad=dz, grad_scale=8.0)
+        alone, _ = sim.token_loss(zs, labels, grad=False)
+        results.append([loss, alone, dz])
+        in_place, _ = sim.token_loss(zs, labels, grad=zs, grad_scale=8.0)
+        assert torch.equal(in_place, loss) and torch.equal(zs, dz)
+    for a, b in zip(*results):
+        assert bool(torch.isfinite(a).all()) and torch.equal(a, b)
+    counted = (labels >= 0).sum(dim=1)
+    for t in (0, T // 2, T - 1):
+        q = torch.softmax(z[:, t].double(), dim=1)
+        q.scatter_add_(1, labels[:, t, None].clamp(min=0).long(), -torch.ones((n, 1), dtype=torch.float64, device="cuda"))
+        q = host(torch.where((labels[:, t] >= 0)[:, None], q * (8.0 / counted)[:, None], 0.0))
+        close(results[0][2][:, t], q, u * np.abs(q) + 1e-5 * 8.0 / host(counted)[:, None] + sub, "gradient")
+    sim.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D,pad", [(5, 0), (40, 0), (61, 3), (129, 0), (768, 0), (1023, 2), (1537, 0), (5003, 1), (8192, 0), (8203, 0)])
+@pytest.mark.parametrize("T", [5, 37])
+def test_layer_norm_in_the_place_of_its_inputs(hx, T, D, pad, dtype):
+    """Every output in the exact place of every input of its call, two at a time where there are two, bit for bit."""
+    from paper_2105_09080_amd import binding as B
+    dt, n, p, seed = TYPES[dtype][0], 3, 0.25, 9
+    sim, X, rng = make_sim(hx, n, 2 * D, seed=D)
+    inputs_ = [rows(rng, (n, T, D), dt, pad) for _ in range(3)]
+    _, _, ld, code = raw(inputs_[0])
+    copies = lambda: [t._base.clone()[..., :D] if t._base is not None else t.clone() for t in inputs_]
+    assert all(t.stride() == s.stride() for t, s in zip(copies(), inputs_))
+
+    def forward(x, r, u, y):
+        stats = torch.zeros((n, T, 2), device="cuda")
+        B.gpga_layer_norm(sim.ctx, x, r, T, D, ld, code, p, seed, 0, 0, D, 1e-5, u, y, stats)
+        return u.clone(), y.clone(), stats
+
+    def backward(dy, u, more, du, dx):
+        sim.G.zero_()
+        B.gpga_layer_norm_grad(sim.ctx, dy, u, stats, more, T, D, ld, code, p, seed, 0, 0, D, du, dx)
+        return du.clone(), dx.clone(), sim.G.clone()
+
+    x, r, s = copies()
+    free = copies()
+    want = forward(x, r, free[0], free[1])
+    stats = want[2]
+    for places in ((0, 1), (1, 0), (0, None), (1, None), (None, 0), (None, 1)):
+        x, r, s = copies()
+        free = copies()
+        u, y = (free[k] if at is None else (x, r)[at] for k, at in enumerate(places))
+        for g, w in zip(forward(x, r, u, y), want):
+            assert torch.equal(g, w), places
+    dy, u, more = copies()
+    free = copies()
+    want = backward(dy, u, more, free[0], free[1])
+    assert all(bool(torch.isfinite(w).all()) for w in want)
+    for places in ((0, 1), (1, 0), (0, 2), (2, 0), (1, 2), (2, 1), (0, None), (None, 0), (None, 1), (None, 2)):
+        ins = copies()
+        free = copies()
+        du, dx = (free[k] if at is None else ins[at] for k, at in enumerate(places))
+        for g, w in zip(backward(*ins, du, dx), want):
+            assert torch.equal(g, w), places
+    sim.close()
