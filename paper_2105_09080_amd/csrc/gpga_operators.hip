@@ -42,8 +42,16 @@ gpga_status reserve(gpga_ctx* c, size_t bytes) {
     if (want < kLeast) want = kLeast;
     if (c->op_scratch && c->op_outgrown_count == kMaxOutgrown) return fail(c, GPGA_ENOMEM, "scratch has grown %d times", kMaxOutgrown);
     char* more = nullptr;
-    const hipError_t e = hipMalloc(reinterpret_cast<void**>(&more), want);
-    if (e != hipSuccess) return hip_fail(c, e, "hipMalloc(scratch)");
+    hipError_t e = hipMalloc(reinterpret_cast<void**>(&more), want);
+    if (e == hipErrorOutOfMemory && want > bytes) {  // what is needed, where half as much again is not to be had
+        (void)hipGetLastError();
+        want = bytes;
+        e = hipMalloc(reinterpret_cast<void**>(&more), want);
+    }
+    if (e != hipSuccess) {
+        (void)hipGetLastError();  // reported here, not by the next call's launch
+        return hip_fail(c, e, "hipMalloc(scratch)");
+    }
     if (c->op_scratch) c->op_outgrown[c->op_outgrown_count++] = c->op_scratch;
     c->op_scratch = more;
     c->op_scratch_cap = want;

@@ -936,3 +936,40 @@ def test_layer_norm_in_the_place_of_its_inputs(hx, T, D, pad, dtype):
         for g, w in zip(backward(*ins, du, dx), want):
             assert torch.equal(g, w), places
     sim.close()
+
+
+def test_scratch_that_cannot_be_had_fails_one_call_and_no_other(hx):
+    """ENOMEM, with nothing launched; smaller calls go on, and so does the same one when there is memory again.  Where half as
+    much again as the last scratch is not to be had, what is needed is enough."""
+    from paper_2105_09080_amd import binding as B
+    V, D, GB = 5, 2048, 1 << 30
+    room(60)
+    sim, X, rng = make_sim(hx, 1, V * D, seed=51)
+    tokens = lambda T: torch.arange(T, dtype=torch.int32, device="cuda").view(1, T) % V
+    dy = torch.ones((1, 5 << 20, D), dtype=torch.float16, device="cuda")     # 20 GB; scratch is a quarter of that
+    free = lambda: torch.cuda.mem_get_info()[0]
+
+    def grad(T):
+        sim.G.fill_(7.0)
+        sim.embed_grad(tokens(T), dy[:, :T], 0, V, scale=1.0)
+        return [int(v) for v in sim.G.view(V, D)[:, 3].tolist()], T // V
+
+    grad(100)
+    torch.cuda.empty_cache()
+    filler = torch.empty(free() - 3 * GB, dtype=torch.uint8, device="cuda")
+    with pytest.raises(B.GpgaError, match="scratch") as e:
+        grad(4 << 20)                                              # 4 GB
+    assert e.value.status == B.GPGA_ENOMEM and bool((sim.G == 7.0).all())
+    got, each = grad(100)                                          # the error is not the next call's
+    assert got == [each] * V
+    del filler
+    torch.cuda.empty_cache()
+    got, each = grad(4 << 20)
+    assert all(abs(v - each) <= 1 for v in got)
+    torch.cuda.empty_cache()
+    filler = torch.empty(free() - 11 * GB // 2, dtype=torch.uint8, device="cuda")
+    got, each = grad(9 << 19)                                      # 4.5 GB; half as much again as before are 6
+    assert all(abs(v - each) <= 1 for v in got)
+    sim.close()
+    del filler, dy, sim
+    torch.cuda.empty_cache()
