@@ -19,6 +19,9 @@ _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream
 
 _DTYPE = {torch.float32: B.GPGA_F32, torch.bfloat16: B.GPGA_BF16, torch.float16: B.GPGA_F16}
 
+# smallest p that drops anything: the library keeps p as fp32 and then to 16 bits, so what rounds to 2^-17 or more
+_LEAST_P = 2.0 ** -17 * (1 - 2.0 ** -25)
+
 
 class Simulation:
     """n simulated nodes with d parameters each on one GPU.
@@ -59,11 +62,12 @@ class Simulation:
     @property
     def X(self) -> torch.Tensor:
         """Live iterates, (n, d) view of the (n, ld) buffer."""
-        return self._addr[B.gpga_current_x(self.ctx)][:, : self.d]
+        x = self._addr[B.gpga_current_x(self.ctx)]
+        return x[...] if self.ld == self.d else x[:, : self.d]     # the same view; a whole one takes half the time
 
     @property
     def G(self) -> torch.Tensor:
-        return self.g[:, : self.d]
+        return self.g[...] if self.ld == self.d else self.g[:, : self.d]
 
     @property
     def M(self):
@@ -227,13 +231,12 @@ class Simulation:
                              f"got {tuple(shape)} {dtype} on {first.device}")
         n, T, D = shape
         ld = D if first.is_contiguous() else first.stride(1) if T > 1 else first.stride(0) if n > 1 else D
-        followed = torch.is_grad_enabled()
         for t in (first, *others):
             if t is None:
                 continue
-            if followed and t.requires_grad:
+            if t.requires_grad and torch.is_grad_enabled():
                 raise ValueError("an activation requires grad: these calls are not recorded for torch's backward()")
-            if t.shape != shape or t.dtype != dtype or t.device != first.device:
+            if t is not first and (t.shape != shape or t.dtype != dtype or t.get_device() != self._device_index):
                 raise ValueError("the activations of a call differ in shape, type or device")
             if ld == D and t.is_contiguous():
                 continue
@@ -300,11 +303,11 @@ class Simulation:
                         accumulate: bool = False):
         """(du, dx): gradients of the residual and of x; those of gamma and beta land in G.  dx is du where p is 0."""
         T, D, ld, dt = self._rows(dy, u, more)
-        if stats.dtype != torch.float32 or stats.shape != (self.n, T, 2) or not stats.is_contiguous() or stats.device != dy.device:
+        if stats.dtype != torch.float32 or stats.shape != (self.n, T, 2) or not stats.is_contiguous() or stats.get_device() != self._device_index:
             raise ValueError("stats are the (n, T, 2) fp32 pairs that layer_norm returns")
         foreign = self._foreign()
         du = self._like(dy, ld, foreign)
-        drops = 0.0 < p < 1.0 and int(float(np.float32(p)) * 65536 + 0.5) > 0    # p as the library keeps it; others are its to refuse
+        drops = _LEAST_P <= p < 1.0     # others keep everything, or are the library's to refuse
         dx = self._like(dy, ld, foreign) if drops else None
         B.gpga_layer_norm_grad(self.ctx, dy, u, stats, more, T, D, ld, dt, p, seed, layer, gamma_off, beta_off, du, dx,
                                accumulate)

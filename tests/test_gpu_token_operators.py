@@ -973,3 +973,18 @@ def test_scratch_that_cannot_be_had_fails_one_call_and_no_other(hx):
     sim.close()
     del filler, dy, sim
     torch.cuda.empty_cache()
+
+
+def test_the_smallest_probability_that_drops_anything(hx):
+    """layer_norm_grad makes a dx of its own exactly where the library asks for one (it refuses both mistakes)."""
+    sim, X, rng = make_sim(hx, 1, 64, seed=0)
+    x, stats = rows(rng, (1, 3, 8), torch.float32), torch.ones((1, 3, 2), device="cuda")
+    edge = 2.0 ** -17 * (1 - 2.0 ** -25)                           # half way from the fp32 number below 2^-17
+    for p in (0.0, 1e-300, 2.0 ** -18, 2.0 ** -17 * (1 - 2.0 ** -24), np.nextafter(edge, 0.0), edge, np.nextafter(edge, 1.0), 2.0 ** -17, 1e-5, 0.5,
+              1.0 - 2.0 ** -17, 1.0 - 2.0 ** -16):
+        keeps = int(float(np.float32(p)) * 65536 + 0.5)
+        if keeps == 65536:
+            continue                                               # leaves nothing: refused
+        du, dx = sim.layer_norm_grad(x, x, stats, 0, 8, p=float(p))
+        assert (dx is du) == (keeps == 0), p
+    sim.close()
