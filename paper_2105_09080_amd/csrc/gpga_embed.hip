@@ -71,9 +71,10 @@ struct ZeroArgs {
     int64_t count, ldg;     // floats of a node's block, distance of the blocks
     float* g;
 };
-// One piece of four floats a lane: 786 MB are zeroed in 118 us beside the sort; four pieces a lane took 126.  The pieces are
-// those of the 128-byte lines of memory, wherever in one the block begins: with pieces counted from its beginning 526 MB took
-// 102 us at 8 bytes past a boundary.
+// One piece of four floats a lane: 786 MB are zeroed in 125 us (110 at least) beside the sort of 4096 tokens a node, and in 118 beside
+// that of 8192, whose LDS leaves a compute unit one workgroup; with four pieces a lane the whole gradient took 169 us, with one
+// 160.  The pieces are those of the 128-byte lines of memory, wherever in one the block begins: with pieces counted from its
+// beginning 526 MB took 102 us at 8 bytes past a boundary, so 94.
 constexpr int kZeroCols = kSortThreads * 4;
 
 __device__ __forceinline__ void zero_block(const ZeroArgs& z, uint32_t b) {
@@ -232,7 +233,7 @@ __global__ __launch_bounds__(kThreads) void k_merge(const uint32_t* __restrict__
 // it leaves a part in `partial` (slot 0: the row of its first item, slot 1: the row of its last item where that is another),
 // and k_embed_join adds the parts.  Rows without items hold the zeros of the sort's launch, or what g is to be added to.
 //
-// 8 x 4096 tokens, 32000 x 768 fp32 rows a node, bf16: zeros 119 us (6.6 TB/s) with the sort beside them, sums 31, joins 6; a
+// 8 x 4096 tokens, 32000 x 768 fp32 rows a node, bf16: zeros 125 us (6.3 TB/s) with the sort beside them, sums 31, joins 5.6; a
 // wavefront a row of the table, which the most frequent token keeps for its 250 rows of dy, took 848 in all.  The sums after so
 // large a fill wait (68 MB in 31 us; longer chunks and more loads under way change nothing); leaving used rows out of the zeros, to
 // zero beside the sums, mixes reads and writes and took 170 to 218 in all.

@@ -298,8 +298,9 @@ __device__ __forceinline__ void put_weights(float* g, int32_t c, int32_t D, bool
 
 // L lanes a row.  A workgroup takes the rows t = strip, strip + strips, ... of a node kRows at a time, keeps its sums for
 // dgamma and dbeta in registers, and leaves them in `partial`.  A row's loads are issued while the one before it is worked on:
-// the registers (209 for three pieces of bf16) leave two wavefronts a SIMD, and without that 8 x 4096 rows of 768 bf16 took 50 to
-// 54 us against 43, all in (4.7 TB/s; 37 here, 4 in the join of 512 partial sums).
+// the registers (209 for three pieces of bf16; 255 and 24 more for fp32 with `more`, which leaves one) leave two wavefronts a SIMD,
+// and without that 8 x 4096 rows of 768 bf16 took 50 to 54 us against 43, all in (4.7 TB/s; traced one by one 42.5 here and 4.7
+// in the join of 512 partial sums).
 template <typename E, int L, int N, bool kSide>
 __global__ __launch_bounds__(L > kThreads ? L : kThreads) void k_norm_grad(NormArgs<E> a) {
     typedef Elem<float, E::kNarrow> P;
@@ -499,8 +500,11 @@ bool with_row_shape(int32_t octs, F&& f) {
     return true;
 }
 
-// Strips of a node: two workgroups a compute unit over all nodes, no more than there are rows for; a single one for few rows, whose
-// sums then need no launch of their own (8 x 16 rows of 768 bf16: 9.1 us against 7.4, a launch and 4.0).
+// Strips of a node: two workgroups a compute unit over all nodes, no more than there are rows (where a workgroup takes several rows
+// side by side some strips have none and add zeros: 512 rows of 768 on one node 16.9 us); a single one for few rows, whose sums
+// then need no launch of their own.  us a call, bf16, one strip and as many as rows: 8 x 16 x 768 14.0 and 15.7, 64 x 4 x 8192
+// 13.7 and 18.2, 64 x 16 x 8192 25.8 and 32.6; but 64 x 16 x 2048 16.3 and 15.5, 8 x 16 x 8192 22.6 and 15.3, where a workgroup
+// takes its rows one after another and few nodes leave the card empty.
 constexpr int32_t kFewRows = 16;
 uint32_t norm_grad_strips(const RowsShape& s) {
     if (s.T <= kFewRows && s.D <= kHeldColumns) return 1;

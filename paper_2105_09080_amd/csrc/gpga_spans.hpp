@@ -30,7 +30,7 @@ inline bool rows_meet(const RowBytes& a, const void* q) {
     return !(apart >= a.width && apart + a.width <= a.step);
 }
 
-// HIP takes fewer than 2^32 work-items a launch.  Calls f(first, count) for the workgroups first .. first + count - 1 of each launch that
+// A launch has fewer than 2^32 work-items; of more, what is over 2^32 is run and no error is reported.  Calls f(first, count) for the workgroups first .. first + count - 1 of each launch that
 // `blocks` workgroups of `threads` need, in order, until one returns something other than Ok.  blocks <= 2^32.
 template <typename F>
 inline auto for_launches(uint64_t blocks, uint32_t threads, F&& f) -> decltype(f(0u, 0u)) {

@@ -438,8 +438,9 @@ template <int V>
 struct Const {
     static constexpr int value = V;
 };
-// Lanes a row and pieces a lane by the number of eights in it: the smallest that hold it, at most four pieces while there are lanes, so
-// that a compute unit has room for several rows (8 x 512 rows of 12000 bf16: 41 us with 3 x 512, 51 with 2 x 1024).
+// Lanes a row and pieces a lane by the number of eights in it: the smallest that hold it.  Up to 16384 columns at most 512 lanes, so that
+// a compute unit has room for several rows (8 x 512 rows of 12000 bf16: 41 us with 3 x 512, 51 with 2 x 1024); above, it has two
+// whatever their length (8 x 512 rows of 20000 bf16 take 70 us, of 32000 91).
 template <typename E, typename F>
 bool with_row_shape(int32_t octs, F&& f) {
     if constexpr (E::kNarrow) f(Const<16>(), Const<1>());
@@ -539,7 +540,7 @@ hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* 
             constexpr int L = decltype(l)::value, N = decltype(k)::value, kBlock = L > kThreads ? L : kThreads;
             a.per_node = blocks_for(s.T, kBlock / L);
             a.left = counter(a.per_node);
-            // few labels of a node are counted beside the loads of a row
+            // few labels of a node are counted by the workgroup of a row itself, behind that row's loads
             if (s.T > 4 * kBlock) {
                 a.count = count;
                 e = count_launch();
