@@ -449,6 +449,27 @@ gpga_status gpga_layer_norm_grad(gpga_ctx* ctx, const void* dy_dev, const void* 
 gpga_status gpga_token_loss(gpga_ctx* ctx, const void* logits_dev, const int32_t* labels_dev, int32_t T, int32_t V,
                             int64_t ld, int32_t dtype, float grad_scale, float* loss_dev, void* dlogits_dev);
 
+/* Gated feed-forward block: with the row-major matrices Wg_i, Wu_i (F x D each, columns gate_off .. and up_off .. of x_i) and Wd_i
+ * (D x F, columns down_off ..), for every token
+ *     a = Wg_i x, b = Wu_i x (F values each), y = Wd_i h with h = act(a) * b element by element;
+ * GPGA_SILU: act(v) = v / (1 + exp(-v)), GPGA_GELU: act(v) = v (1 + erf(v / sqrt 2)) / 2.  hidden_dev (NULL: not kept) receives
+ * a and b, n*T dense rows [a | b] of 2F elements of the activations' type; y comes from a and b before they are rounded.
+ * 1 <= D, F <= 2^21, D*F with both rounded up to multiples of 64 below 2^30.
+ * Products are made of fp16 pieces of the operands, scaled by powers of two, with fp32 sums: with fp32 activations two
+ * pieces each (2^-22 of an operand's largest value in its row), with fp16 two of one operand and one (2^-11) of the other, with bf16 one
+ * each; the gradients of the matrices take two whatever the type.  A token with an infinity or NaN in its row of x, or whose |a b| may
+ * pass 2^126, gets NaN; so does all of a node whose matrices hold an infinity. */
+typedef enum { GPGA_SILU = 0, GPGA_GELU = 1 } gpga_activation;
+gpga_status gpga_gated_ff(gpga_ctx* ctx, const void* x_dev, int32_t T, int32_t D, int32_t F, int64_t ld, int32_t dtype,
+                          int32_t act, int64_t gate_off, int64_t up_off, int64_t down_off, void* hidden_dev, void* y_dev);
+/* Backward, from the gradient dy of y, x and the kept [a | b]: with dh = Wd_i^T dy, da = dh * b * act'(a) and db = dh * act(a),
+ * dx = Wg_i^T da + Wu_i^T db, and into g_dev the sums over the node's tokens dWg_i = sum da x^T, dWu_i = sum db x^T,
+ * dWd_i = sum dy h^T.  The three column blocks must not overlap.  T = 0 leaves zeros (or, added, nothing).  An infinity or NaN in dy, x
+ * or hidden makes the node's gradients NaN. */
+gpga_status gpga_gated_ff_grad(gpga_ctx* ctx, const void* dy_dev, const void* x_dev, const void* hidden_dev, int32_t T,
+                               int32_t D, int32_t F, int64_t ld, int32_t dtype, int32_t act, int64_t gate_off,
+                               int64_t up_off, int64_t down_off, void* dx_dev, int32_t accumulate);
+
 /* Measurement aid, not part of the method: a plain streaming kernel over `bytes`
  * (a multiple of 16) per array of device memory on hip_stream, with the same 128-bit
  * non-temporal accesses as the fused step.  kind 0 reads src_dev (dst_dev: any

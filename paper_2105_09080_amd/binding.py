@@ -21,6 +21,8 @@ TOPOLOGY = {"ring": GPGA_TOPO_RING, "expo1": GPGA_TOPO_EXPO1, "none": GPGA_TOPO_
             "full": GPGA_TOPO_FULL, "grid": GPGA_TOPO_GRID, "expo": GPGA_TOPO_EXPO,
             "custom": GPGA_TOPO_CUSTOM}
 GPGA_F32, GPGA_BF16, GPGA_F16 = 0, 1, 2
+GPGA_SILU, GPGA_GELU = 0, 1
+ACTIVATION = {"silu": GPGA_SILU, "gelu": GPGA_GELU}
 _STATUS_NAME = {0: "GPGA_OK", 1: "GPGA_EINVAL", 2: "GPGA_ENOMEM", 3: "GPGA_EDEVICE", 4: "GPGA_ESTATE"}
 
 #: every symbol include/gpga.h declares: (name, restype, argtypes)
@@ -83,6 +85,11 @@ SIGNATURES = [
                                         _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p, _c.c_int32]),
     ("gpga_token_loss", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int64, _c.c_int32,
                                    _c.c_float, _c.c_void_p, _c.c_void_p]),
+    ("gpga_gated_ff", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_int64, _c.c_int32, _c.c_int32,
+                                 _c.c_int64, _c.c_int64, _c.c_int64, _c.c_void_p, _c.c_void_p]),
+    ("gpga_gated_ff_grad", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int32,
+                                      _c.c_int64, _c.c_int32, _c.c_int32, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_void_p,
+                                      _c.c_int32]),
     ("gpga_probe_stream", _c.c_int, [_c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64,
                                      _c.c_int32, _c.c_void_p]),
     ("gpga_last_error", _c.c_char_p, [_ctx_p]),
@@ -369,6 +376,22 @@ def gpga_token_loss(ctx, logits, labels, T: int, V: int, ld: int, dtype: int, gr
         _int32(T, V)
     _check(ctx, _lib.gpga_token_loss(ctx, _ptr(logits), _ptr(labels), T, V, ld, dtype, grad_scale, _ptr(loss),
                                      _ptr(dlogits)))
+
+
+def gpga_gated_ff(ctx, x, T: int, D: int, F: int, ld: int, dtype: int, act: int, gate_off: int, up_off: int, down_off: int,
+                  hidden, y):
+    """hidden: n*T dense rows of 2F elements that receive [a | b], or None."""
+    if (T | D | F) >> 31:
+        _int32(T, D, F)
+    _check(ctx, _lib.gpga_gated_ff(ctx, _ptr(x), T, D, F, ld, dtype, act, gate_off, up_off, down_off, _ptr(hidden), _ptr(y)))
+
+
+def gpga_gated_ff_grad(ctx, dy, x, hidden, T: int, D: int, F: int, ld: int, dtype: int, act: int, gate_off: int, up_off: int,
+                       down_off: int, dx, accumulate: bool = False):
+    if (T | D | F) >> 31:
+        _int32(T, D, F)
+    _check(ctx, _lib.gpga_gated_ff_grad(ctx, _ptr(dy), _ptr(x), _ptr(hidden), T, D, F, ld, dtype, act, gate_off, up_off,
+                                        down_off, _ptr(dx), int(accumulate)))
 
 
 def gpga_probe_stream(kind: int, src, dst, nbytes: int, stream=None, src2=None, inout=None, blocks_per_cu: int = 0):

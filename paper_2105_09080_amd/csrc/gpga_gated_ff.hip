@@ -1,0 +1,732 @@
+// Gated feed-forward block on the nodes' own matrices (include/gpga.h), forward and backward.
+//
+//   a = x Wg^T, b = x Wu^T, h = act(a) b, y = h Wd^T                     x, y: T x D a node; a, b, h: T x F
+//   dh = dy Wd, da = dh b act'(a), db = dh act(a), dx = da Wg + db Wu,
+//   dWg = da^T x, dWu = db^T x, dWd = dy^T h
+//
+// The products run on the matrix units (gpga_product.hpp) from halves with power-of-two scales.  Which operands get two halves follows
+// from the result: what is fp32 in the end (gradients of parameters; everything with fp32 activations) gets two wherever an operand is
+// not exact in one; what is rounded to fp16 gets two for one operand of each product, so that it is off by little more than its own
+// rounding; what is rounded to bf16 (by up to 2^-8) gets one (2^-11) everywhere.
+// Scales: rows of x and of the matrices by their largest value; rows of h, da and db, which are rounded in the epilogue that makes
+// them, by bounds that are known before (Cauchy-Schwarz for a and b, the sum of |dy| for dh): some 2^8 .. 2^14 above typical values,
+// which halves' 29 binades below 2^15 have room for.
+#include "gpga_pack.hpp"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPackRows = kThreads / kWave;  // a wavefront a row
+
+// ---- activation functions -------------------------------------------------------------------------------------------------
+// silu(v) = v s, s = 1 / (1 + exp(-v)); silu' = s + v s (1 - s).  gelu(v) = v P, P = (1 + erf(v / sqrt 2)) / 2; gelu' = P + v exp(-v^2/2) /
+// sqrt(2 pi).  |act(v)| <= |v|, |act'| <= 1.13.
+template <int Act>
+__device__ __forceinline__ float act_value(float v) {
+    if constexpr (Act == GPGA_SILU) return v / (1.f + __expf(-v));
+    return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+}
+template <int Act>
+__device__ __forceinline__ void act_both(float v, float* value, float* slope) {
+    if constexpr (Act == GPGA_SILU) {
+        const float e = __expf(-v), s = 1.f / (1.f + e);
+        *value = v * s;
+        *slope = s + *value * (e > 1e30f ? 1.f : e * s);
+    } else {
+        const float p = 0.5f * (1.f + erff(v * 0.70710678118654752f));
+        *value = v * p;
+        *slope = p + v * (__expf(-0.5f * v * v) * 0.39894228040143268f);
+    }
+}
+
+// ---- rows as halves -------------------------------------------------------------------------------------------------------
+// The three matrices of every node: rows of gate, up (D long) and down (F long), each with a scale of its own, or gate and up
+// with one scale a node.
+struct PackMatrices {
+    const float* gate;
+    const float* up;
+    const float* down;
+    int64_t ldx;
+    int32_t D, F;
+    half_t *gu, *wd;              // planes: (n, 2 F', D') and (n, D', F'), ' padded
+    int64_t gu_plane, wd_plane;
+    float *gu_inv, *wd_inv;       // n x 2F', n x D'
+    float* norms;                 // n x 2F' row norms of gate and up, or NULL
+    const float* node_max;        // largest |gate|, |up| of a node in kMaxParts parts, or NULL: scales by row
+    uint32_t gu_blocks, per_node, first_block;
+};
+constexpr int kMaxParts = 64;
+
+template <typename E, int PGU, int PD>
+__global__ __launch_bounds__(kThreads) void k_ff_pack_matrices(PackMatrices a) {
+    const uint32_t block = a.first_block + blockIdx.x, node = block / a.per_node;
+    const int32_t in = (int32_t)(block % a.per_node), wave = threadIdx.x / kWave;
+    const int32_t D2 = padded(a.D), F2 = padded(a.F);
+    if (in < (int32_t)a.gu_blocks) {
+        const int32_t row = in * kPackRows + wave, f = row < F2 ? row : row - F2;
+        const float* from = (row < F2 ? a.gate : a.up) + (int64_t)node * a.ldx + (int64_t)f * a.D;
+        half_t* to = a.gu + ((int64_t)node * 2 * F2 + row) * D2;
+        Scale s = {0.f, 0.f};
+        if (a.node_max) {
+            const float* part = a.node_max + (int64_t)node * kMaxParts;
+            s = scale_for(wave_all<kWave>(part[threadIdx.x & (kWave - 1)], max_nan));
+        }
+        const RowStat r = pack_row<E, PGU>(from, f < a.F ? a.D : 0, D2, nullptr, a.node_max ? &s : nullptr, to, a.gu_plane);
+        if ((threadIdx.x & (kWave - 1)) == 0) {
+            a.gu_inv[(int64_t)node * 2 * F2 + row] = r.down;
+            if (a.norms) a.norms[(int64_t)node * 2 * F2 + row] = r.norm * r.down;
+        }
+    } else {
+        const int32_t row = (in - (int32_t)a.gu_blocks) * kPackRows + wave;
+        const RowStat r = pack_row<E, PD>(a.down + (int64_t)node * a.ldx + (int64_t)row * a.F, row < a.D ? a.F : 0, F2, nullptr, nullptr,
+                                          a.wd + ((int64_t)node * D2 + row) * F2, a.wd_plane);
+        if ((threadIdx.x & (kWave - 1)) == 0) a.wd_inv[(int64_t)node * D2 + row] = r.down;
+    }
+}
+
+// Largest |gate| and |up| of a node, in kMaxParts parts.
+__global__ __launch_bounds__(kThreads) void k_ff_max(const float* gate, const float* up, int64_t ldx, int64_t count, float* part, uint32_t first) {
+    const uint32_t block = first + blockIdx.x, node = block / kMaxParts, p = block % kMaxParts;
+    float m = 0.f;
+    for (int64_t e = (int64_t)p * kThreads + threadIdx.x; e < count; e += (int64_t)kMaxParts * kThreads) {
+        m = max_nan(m, fabsf(gate[(int64_t)node * ldx + e]));
+        m = max_nan(m, fabsf(up[(int64_t)node * ldx + e]));
+    }
+    m = wave_all<kWave>(m, max_nan);
+    __shared__ float s[kPackRows];
+    if ((threadIdx.x & (kWave - 1)) == 0) s[threadIdx.x / kWave] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) part[block] = max_nan(max_nan(s[0], s[1]), max_nan(s[2], s[3]));
+}
+
+// Rows of activations of a chunk of tokens, a wavefront a row.
+struct PackRows {
+    const void* src;
+    int64_t ld, node;          // elements between rows, between nodes
+    int32_t rows, cols;        // real ones of a node
+    half_t* dst;               // (n, rows', cols')
+    int64_t plane;
+    float* inv;                // n x rows'
+    uint32_t per_node, first_block;
+    __device__ __forceinline__ bool at(int32_t* node_, int32_t* row, int32_t* row2) const {
+        const uint32_t block = first_block + blockIdx.x;
+        *node_ = (int32_t)(block / per_node);
+        *row = (int32_t)(block % per_node) * kPackRows + threadIdx.x / kWave;
+        *row2 = padded(rows);
+        return true;
+    }
+};
+
+// Forward: x as halves, and the scale of its row of h: |a|, |b| <= |x| max |w|, |h| <= |a| |b|.
+template <typename E, int P>
+__global__ __launch_bounds__(kThreads) void k_ff_pack_x(PackRows a, const float* norms, int32_t norm_count, float* h_up, float* h_inv) {
+    int32_t node, row, rows2;
+    a.at(&node, &row, &rows2);
+    const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1);
+    float w = 0.f;
+    for (int32_t f = threadIdx.x; f < norm_count; f += kThreads) w = max_nan(w, norms[(int64_t)node * norm_count + f]);
+    w = wave_all<kWave>(w, max_nan);
+    __shared__ float s_w[kPackRows];
+    if (lane == 0) s_w[threadIdx.x / kWave] = w;
+    __syncthreads();
+    w = max_nan(max_nan(s_w[0], s_w[1]), max_nan(s_w[2], s_w[3]));
+    const typename E::mem* from = static_cast<const typename E::mem*>(a.src) + (int64_t)node * a.node + (int64_t)row * a.ld;
+    const RowStat r = pack_row<E, P>(from, row < a.rows ? a.cols : 0, cols2, nullptr, nullptr, a.dst + ((int64_t)node * rows2 + row) * cols2, a.plane);
+    if (lane == 0) {
+        const int64_t at = (int64_t)node * rows2 + row;
+        const float most = r.norm * r.down * w;
+        const Scale s = scale_for(most * most * 1.0001f);
+        a.inv[at] = r.down;
+        h_up[at] = s.up;
+        h_inv[at] = s.down;
+    }
+}
+
+// Backward: dy times the scales of the down matrix's rows as halves, and the scales of its token's rows of [da | db] and h, from
+// |dh| <= sum |dy| |w| and the largest |a|, |b| of the token.  For the products over tokens, da = da' / up and so on leaves factors
+// that go into the other operand (k_ff_pack_tokens): the largest |x| / up and |dy| / up of a workgroup's tokens.
+template <typename E, int P>
+__global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackRows a, const float* wd_inv, const void* x, const void* hidden, int32_t F,
+                                                         int64_t hidden_node, float* da_up, float* da_inv, float* h_up, float* h_inv, float* part) {
+    typedef typename E::mem M;
+    int32_t node, row, rows2;
+    a.at(&node, &row, &rows2);
+    const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1);
+    const bool real = row < a.rows;
+    const int64_t from = (int64_t)node * a.node + (int64_t)row * a.ld, at = (int64_t)node * rows2 + row;
+    const RowStat r = pack_row<E, P>(static_cast<const M*>(a.src) + from, real ? a.cols : 0, cols2, wd_inv + (int64_t)node * cols2, nullptr,
+                                     a.dst + at * cols2, a.plane);
+    float xm = 0.f, ym = 0.f, am = 0.f, bm = 0.f;
+    if (real) {
+        const M* h = static_cast<const M*>(hidden) + (int64_t)node * hidden_node + (int64_t)row * 2 * F;
+        xm = row_max<E>(static_cast<const M*>(x) + from, a.cols);
+        ym = row_max<E>(static_cast<const M*>(a.src) + from, a.cols);
+        am = row_max<E>(h, F);
+        bm = row_max<E>(h + F, F);
+    }
+    const float dh = r.sum * r.down * 32768.f * 1.0001f;
+    const Scale sa = scale_for(dh * max_nan(1.14f * bm, am)), sh = scale_for(am * bm);
+    if (lane == 0) {
+        a.inv[at] = r.down;
+        da_up[at] = sa.up;
+        da_inv[at] = sa.down;
+        h_up[at] = sh.up;
+        h_inv[at] = sh.down;
+    }
+    __shared__ float s[2][kPackRows];
+    if (lane == 0) {
+        s[0][threadIdx.x / kWave] = xm * sa.down;
+        s[1][threadIdx.x / kWave] = ym * sh.down;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        const float* q = s[threadIdx.x];
+        part[((int64_t)node * 2 + threadIdx.x) * a.per_node + blockIdx.x + a.first_block - (uint64_t)node * a.per_node] =
+            max_nan(max_nan(q[0], q[1]), max_nan(q[2], q[3]));
+    }
+}
+
+// x / up (which = 0) or dy / up (1) of every token as halves with one scale a node.
+template <typename E, int P>
+__global__ __launch_bounds__(kThreads) void k_ff_pack_tokens(PackRows a, const float* row_inv, const float* dy_inv, const float* part, uint32_t parts,
+                                                             int which, float* node_inv) {
+    int32_t node, row, rows2;
+    a.at(&node, &row, &rows2);
+    const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1);
+    const float* from = part + ((int64_t)node * 2 + which) * parts;
+    float w = 0.f;
+    for (uint32_t p = threadIdx.x; p < parts; p += kThreads) w = max_nan(w, from[p]);
+    w = wave_all<kWave>(w, max_nan);
+    __shared__ float s_w[kPackRows];
+    if (lane == 0) s_w[threadIdx.x / kWave] = w;
+    __syncthreads();
+    const Scale node_scale = scale_for(max_nan(max_nan(s_w[0], s_w[1]), max_nan(s_w[2], s_w[3])));
+    const int64_t at = (int64_t)node * rows2 + row;
+    const float inv = row < a.rows ? row_inv[at] : 0.f;
+    Scale s = {inv * node_scale.up, 0.f};
+    const typename E::mem* src = static_cast<const typename E::mem*>(a.src) + (int64_t)node * a.node + (int64_t)row * a.ld;
+    pack_row<E, P>(src, row < a.rows ? a.cols : 0, cols2, nullptr, &s, a.dst + at * cols2, a.plane);
+    if (row == 0 && lane == 0) node_inv[node] = node_scale.down;
+}
+
+// ---- products ---------------------------------------------------------------------------------------------------------------
+struct FfProduct {
+    Operand A, B;
+    TileGrid grid;
+    uint32_t first_block;
+    int32_t M, N, K;          // real rows and columns, padded terms
+    const float* row_inv;     // scales of A's rows, n x rows of A's memory (or of k_ff_pack_tokens, one a node)
+    const float* col_inv;     // of B's rows
+    int64_t row_batch, col_batch;
+    int32_t F;
+    // activations in or out
+    void* out;
+    int64_t out_ld, out_node;
+    void* hidden;
+    int64_t hidden_node;
+    // planes out
+    half_t *h, *da;
+    int64_t h_plane, da_plane;
+    const float *h_up, *da_up;
+    // gradients out
+    float* g;
+    int64_t g_ld, off0, off1;  // columns of gate's and up's blocks
+    int accumulate;
+};
+
+// Four columns of a row of activations, as many as there are.
+template <typename E>
+__device__ __forceinline__ void put4(typename E::mem* row, int32_t col, int32_t cols, v4f v) {
+    typedef typename E::mem M;
+    typedef M vec __attribute__((ext_vector_type(4), aligned(alignof(M))));
+    if (col + 4 <= cols) {
+        *reinterpret_cast<vec*>(row + col) = __builtin_convertvector(v, vec);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (col + k < cols) row[col + k] = E::put(v[k]);
+    }
+}
+template <typename E>
+__device__ __forceinline__ v4f get4(const typename E::mem* row, int32_t col, int32_t cols) {
+    typedef typename E::mem M;
+    typedef M vec __attribute__((ext_vector_type(4), aligned(alignof(M))));
+    if (col + 4 <= cols) return __builtin_convertvector(*reinterpret_cast<const vec*>(row + col), v4f);
+    v4f v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (col + k < cols) v[k] = E::get(row[col + k]);
+    return v;
+}
+
+// h = act(x Wg^T) (x Wu^T): a wavefront's blocks of 32 columns are gate and up of the same 32 f's in turn.
+template <typename S, typename E, int Act, int PH>
+__global__ __launch_bounds__(S::Threads) void k_ff_up(FfProduct a) {
+    __shared__ __align__(16) char lds[2 * S::Stage];
+    static_assert(S::NI == 2, "gate and up");
+    int32_t node, ti, tj;
+    if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
+    const int32_t F2 = padded(a.F), m0 = ti * S::BM, f0 = tj * (S::BN / 2);
+    acc16 acc[S::NI][S::MI];
+    product_tile<S>(a.A, a.B, node, m0, 0, a.K, lds, acc,
+                    [&](int row) { return (row >> 5 & 1) * F2 + min(f0 + (row >> 6) * 32 + (row & 31), F2 - 1); });
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t T2 = a.A.rows;
+    typedef typename E::mem M;
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+        const int32_t row = m0 + wave / S::WN * (S::BM / S::WM) + i * 32 + (lane & 31);
+        if (row >= a.M) continue;
+        const int64_t at = node * T2 + row;
+        const float xi = a.row_inv[at], up = a.h_up[at];
+        const float* wi = a.col_inv + (int64_t)node * 2 * F2;
+        M* hid = static_cast<M*>(a.hidden) + (int64_t)node * a.hidden_node + (int64_t)row * 2 * a.F;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int32_t f = f0 + wave % S::WN * 32 + q * 8 + (lane >> 5) * 4;
+            if (f >= F2) continue;
+            const v4f gi = *reinterpret_cast<const v4f*>(wi + f), ui = *reinterpret_cast<const v4f*>(wi + F2 + f);
+            v4f va, vb, h;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                va[k] = acc[0][i][q * 4 + k] * (xi * gi[k]);
+                vb[k] = acc[1][i][q * 4 + k] * (xi * ui[k]);
+                h[k] = act_value<Act>(va[k]) * vb[k] * up;
+            }
+            store_planes<PH>(a.h + at * F2 + f, a.h_plane, h);
+            if (a.hidden) {
+                put4<E>(hid, f, a.F, va);
+                put4<E>(hid + a.F, f, a.F, vb);
+            }
+        }
+    }
+}
+
+// Activations out: rows' scales times columns' scales (col_batch < 0: one a node).
+template <typename S, typename E>
+__global__ __launch_bounds__(S::Threads) void k_ff_rows(FfProduct a) {
+    __shared__ __align__(16) char lds[2 * S::Stage];
+    int32_t node, ti, tj;
+    if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
+    const int32_t m0 = ti * S::BM, n0 = tj * S::BN;
+    acc16 acc[S::NI][S::MI];
+    product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return min(n0 + row, a.B.rows - 1); });
+    typedef typename E::mem M;
+    each_quad<S>(acc, m0, n0, [&](int32_t row, int32_t col, v4f v) {
+        if (row >= a.M || col >= a.N) return;
+        const float r = a.row_inv[node * a.row_batch + row];
+        v4f c;
+        if (S::ColsB) {
+            const float w = a.col_inv[node * a.col_batch];
+            c = v4f{w, w, w, w};
+        } else {
+            c = *reinterpret_cast<const v4f*>(a.col_inv + node * a.col_batch + col);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] *= r * c[k];
+        put4<E>(static_cast<M*>(a.out) + node * a.out_node + (int64_t)row * a.out_ld, col, a.N, v);
+    });
+}
+
+// dh = dy Wd, and from it and the kept [a | b] the rows of [da | db] and h as halves.  Rows behind the last token are zeros: the
+// products over tokens take them along.
+template <typename S, typename E, int Act, int PA, int PH>
+__global__ __launch_bounds__(S::Threads) void k_ff_down_grad(FfProduct a) {
+    __shared__ __align__(16) char lds[2 * S::Stage];
+    int32_t node, ti, tj;
+    if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
+    const int32_t F2 = padded(a.F), T2 = a.A.rows, m0 = ti * S::BM, n0 = tj * S::BN;
+    acc16 acc[S::NI][S::MI];
+    product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return row; });
+    typedef typename E::mem M;
+    each_quad<S>(acc, m0, n0, [&](int32_t row, int32_t f, v4f dh) {
+        if (row >= T2 || f >= F2) return;
+        const int64_t at = (int64_t)node * T2 + row;
+        v4f da = {0.f, 0.f, 0.f, 0.f}, db = da, h = da;
+        if (row < a.M) {
+            const M* hid = static_cast<const M*>(a.hidden) + (int64_t)node * a.hidden_node + (int64_t)row * 2 * a.F;
+            const v4f va = get4<E>(hid, f, a.F), vb = get4<E>(hid + a.F, f, a.F);
+            const float inv = a.row_inv[at], da_up = a.da_up[at], h_up = a.h_up[at];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float value, slope;
+                act_both<Act>(va[k], &value, &slope);
+                const float d = dh[k] * inv;
+                da[k] = d * vb[k] * slope * da_up;
+                db[k] = d * value * da_up;
+                h[k] = value * vb[k] * h_up;
+            }
+        }
+        store_planes<PA>(a.da + at * 2 * F2 + f, a.da_plane, da);
+        store_planes<PA>(a.da + at * 2 * F2 + F2 + f, a.da_plane, db);
+        store_planes<PH>(a.h + at * F2 + f, a.h_plane, h);
+    });
+}
+
+// Gradients of matrices: rows of the gate's block, then (from F' on) of the up's; or of the down matrix's alone (off1 < 0).
+template <typename S>
+__global__ __launch_bounds__(S::Threads) void k_ff_matrix_grad(FfProduct a) {
+    __shared__ __align__(16) char lds[2 * S::Stage];
+    int32_t node, ti, tj;
+    if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
+    const int32_t m0 = ti * S::BM, n0 = tj * S::BN;
+    acc16 acc[S::NI][S::MI];
+    product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return row; });
+    const float inv = a.row_inv[node];
+    each_quad<S>(acc, m0, n0, [&](int32_t row, int32_t col, v4f v) {
+        int64_t off = a.off0;
+        if (a.off1 >= 0 && row >= a.A.ld / 2) {
+            row -= a.A.ld / 2;
+            off = a.off1;
+        }
+        if (row >= a.M || col >= a.N) return;
+        float* to = a.g + (int64_t)node * a.g_ld + off + (int64_t)row * a.N;
+        v4f o = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+        if (a.accumulate) o += get4<ElemF32>(to, col, a.N);
+        put4<ElemF32>(to, col, a.N, o);
+    });
+}
+
+__global__ __launch_bounds__(kThreads) void k_ff_zero(float* g, int64_t g_ld, int64_t off0, int64_t off1, int64_t off2, int64_t count, uint32_t per_node,
+                                                      uint32_t first) {
+    const uint32_t block = first + blockIdx.x, node = block / per_node;
+    const int64_t e = (int64_t)(block % per_node) * kThreads + threadIdx.x;
+    if (e >= count) return;
+    float* row = g + (int64_t)node * g_ld;
+    row[off0 + e] = row[off1 + e] = row[off2 + e] = 0.f;
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------------------
+// Scratch of a call: blocks of a multiple of 256 bytes, handed out in order; without memory it counts.
+struct Carve {
+    char* base;
+    size_t used = 0;
+    template <typename P>
+    P* take(int64_t count) {
+        P* p = base ? reinterpret_cast<P*>(base + used) : nullptr;
+        used += ((size_t)count * sizeof(P) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+// Tokens of a node that go through together: scratch stays below some 4 GiB (and the least of a tile, whatever the width).
+int32_t chunk_tokens(const FfShape& s, int64_t halves) {
+    const int64_t bytes = 2 * halves * s.n;
+    const int64_t most = ((int64_t)4 << 30) / bytes / 256 * 256;
+    const int64_t want = most < 256 ? 256 : most;
+    return s.T < want ? s.T : (int32_t)want;
+}
+
+struct FfScratch {
+    int32_t chunk;
+    int px, pgu, pd, ph, pa;  // planes
+    half_t *gu, *wd, *x, *h, *dy, *da, *tok_x, *tok_y;
+    float *gu_inv, *wd_inv, *norms, *node_max, *x_inv, *h_up, *h_inv, *da_up, *da_inv, *part, *node_inv;
+};
+
+FfScratch carve_ff(const FfShape& s, bool grad, char* base, size_t* bytes) {
+    FfScratch w = {};
+    const bool f32 = s.dtype == GPGA_F32;
+    const int32_t D2 = padded(s.D), F2 = padded(s.F);
+    Carve c = {base};
+    w.px = f32 ? 2 : 1;
+    if (!grad) {
+        w.pgu = w.pd = s.dtype == GPGA_BF16 ? 1 : 2;
+        w.ph = f32 ? 2 : 1;
+        w.chunk = chunk_tokens(s, (int64_t)w.px * D2 + (int64_t)w.ph * F2);
+    } else {
+        w.pgu = f32 ? 2 : 1;
+        w.pd = w.ph = w.pa = 2;
+        w.chunk = chunk_tokens(s, (int64_t)3 * w.px * D2 + (int64_t)6 * F2);
+    }
+    const int64_t n = s.n, T2 = padded(w.chunk);
+    w.gu = c.take<half_t>(n * 2 * F2 * D2 * w.pgu);
+    w.wd = c.take<half_t>(n * F2 * D2 * w.pd);
+    w.gu_inv = c.take<float>(n * 2 * F2);
+    w.wd_inv = c.take<float>(n * D2);
+    w.h = c.take<half_t>(n * T2 * F2 * w.ph);
+    w.x_inv = c.take<float>(n * T2);
+    w.h_up = c.take<float>(n * T2);
+    w.h_inv = c.take<float>(n * T2);
+    if (!grad) {
+        w.norms = c.take<float>(n * 2 * F2);
+        w.x = c.take<half_t>(n * T2 * D2 * w.px);
+    } else {
+        w.node_max = c.take<float>(n * kMaxParts);
+        w.dy = c.take<half_t>(n * T2 * D2 * w.px);
+        w.tok_x = c.take<half_t>(n * T2 * D2 * w.px);
+        w.tok_y = c.take<half_t>(n * T2 * D2 * w.px);
+        w.da = c.take<half_t>(n * T2 * 2 * F2 * w.pa);
+        w.da_up = c.take<float>(n * T2);
+        w.da_inv = c.take<float>(n * T2);
+        w.part = c.take<float>(n * 2 * (T2 / kPackRows));
+        w.node_inv = c.take<float>(2 * n);
+    }
+    *bytes = c.used;
+    return w;
+}
+
+Operand rows_operand(const half_t* p, int64_t n, int32_t rows, int32_t cols) { return {p, n * rows * cols, (int64_t)rows * cols, cols, rows}; }
+
+// Tiles of 256 x 256 (8 wavefronts) where they fill the card, of 128 x 128 (4) otherwise.
+template <typename F>
+hipError_t launch_product(const gpga_ctx* c, FfProduct& a, int32_t rows, int32_t cols, bool wide, F&& f) {
+    const int32_t side = wide ? 256 : 128;
+    a.grid.tm = (rows + side - 1) / side;
+    a.grid.tn = (cols + side - 1) / side;
+    a.grid.total = (uint32_t)a.grid.tm * (uint32_t)a.grid.tn * (uint32_t)c->n;
+    return launch_blocks(a.grid.blocks(), wide ? 512 : 256, [&](uint32_t first, dim3 grid) {
+        a.first_block = first;
+        f(grid);
+    });
+}
+bool wide_tiles(const gpga_ctx* c, int64_t rows, int64_t cols) {
+    return ((rows + 255) / 256) * ((cols + 255) / 256) * c->n >= c->num_cus * 3 / 4;
+}
+
+template <int PA, int PB, bool CA, bool CB>
+using Wide = Tile<256, 256, 2, 4, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
+template <int PA, int PB, bool CA, bool CB>
+using Narrow = Tile<128, 128, 2, 2, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
+
+// f(a constant) for the kind of activation.
+template <int V>
+struct Const {
+    static constexpr int value = V;
+};
+template <typename F>
+void with_act(int32_t act, F&& f) {
+    if (act == GPGA_SILU) f(Const<GPGA_SILU>());
+    else f(Const<GPGA_GELU>());
+}
+
+PackMatrices pack_matrices(const gpga_ctx* c, const FfShape& s, const FfScratch& w) {
+    const int32_t D2 = padded(s.D), F2 = padded(s.F);
+    PackMatrices a = {};
+    a.gate = c->x + s.gate_off;
+    a.up = c->x + s.up_off;
+    a.down = c->x + s.down_off;
+    a.ldx = c->ld;
+    a.D = s.D;
+    a.F = s.F;
+    a.gu = w.gu;
+    a.wd = w.wd;
+    a.gu_plane = (int64_t)s.n * 2 * F2 * D2;
+    a.wd_plane = (int64_t)s.n * F2 * D2;
+    a.gu_inv = w.gu_inv;
+    a.wd_inv = w.wd_inv;
+    a.norms = w.norms;
+    a.node_max = w.node_max;
+    a.gu_blocks = (uint32_t)(2 * F2 / kPackRows);
+    a.per_node = a.gu_blocks + (uint32_t)(D2 / kPackRows);
+    return a;
+}
+
+template <int PGU, int PD>
+hipError_t launch_pack_matrices(const gpga_ctx* c, const FfShape& s, PackMatrices a) {
+    return launch_blocks((uint64_t)a.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+        a.first_block = first;
+        if (s.D < kOct || s.F < kOct) k_ff_pack_matrices<Elem<float, true>, PGU, PD><<<grid, dim3(kThreads), 0, c->stream>>>(a);
+        else k_ff_pack_matrices<Elem<float, false>, PGU, PD><<<grid, dim3(kThreads), 0, c->stream>>>(a);
+    });
+}
+
+#define GPGA_LAUNCH(call)                        \
+    do {                                         \
+        const hipError_t e_ = (call);            \
+        if (e_ != hipSuccess) return e_;         \
+    } while (0)
+
+template <typename E>
+hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hidden, void* y, char* scratch) {
+    typedef typename E::mem M;
+    constexpr bool kF32 = sizeof(M) == 4, kBf16 = __is_same(M, __bf16);
+    constexpr int PX = kF32 ? 2 : 1, PW = kBf16 ? 1 : 2, PH = PX;
+    size_t bytes;
+    const FfScratch w = carve_ff(s, false, scratch, &bytes);
+    const int32_t D2 = padded(s.D), F2 = padded(s.F);
+    GPGA_LAUNCH((launch_pack_matrices<PW, PW>(c, s, pack_matrices(c, s, w))));
+    for (int32_t t0 = 0; t0 < s.T; t0 += w.chunk) {
+        const int32_t T = s.T - t0 < w.chunk ? s.T - t0 : w.chunk, T2 = padded(T);
+        PackRows p = {static_cast<const M*>(x) + (int64_t)t0 * s.ld, s.ld, (int64_t)s.T * s.ld, T, s.D, w.x, (int64_t)s.n * T2 * D2, w.x_inv,
+                      (uint32_t)(T2 / kPackRows), 0};
+        GPGA_LAUNCH(launch_blocks((uint64_t)p.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+            p.first_block = first;
+            k_ff_pack_x<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(p, w.norms, 2 * F2, w.h_up, w.h_inv);
+        }));
+        FfProduct a = {};
+        a.A = rows_operand(w.x, s.n, T2, D2);
+        a.B = rows_operand(w.gu, s.n, 2 * F2, D2);
+        a.M = T;
+        a.K = D2;
+        a.F = s.F;
+        a.row_inv = w.x_inv;
+        a.col_inv = w.gu_inv;
+        a.hidden = hidden ? static_cast<M*>(hidden) + (int64_t)t0 * 2 * s.F : nullptr;
+        a.hidden_node = (int64_t)s.T * 2 * s.F;
+        a.h = w.h;
+        a.h_plane = (int64_t)s.n * T2 * F2;
+        a.h_up = w.h_up;
+        const bool wide = wide_tiles(c, T, 2 * F2);
+        GPGA_LAUNCH(launch_product(c, a, T, 2 * F2, wide, [&](dim3 grid) {
+            with_act(s.act, [&](auto act) {
+                constexpr int kAct = decltype(act)::value;
+                if (wide) k_ff_up<Wide<PX, PW, false, false>, E, kAct, PH><<<grid, dim3(512), 0, c->stream>>>(a);
+                else k_ff_up<Narrow<PX, PW, false, false>, E, kAct, PH><<<grid, dim3(256), 0, c->stream>>>(a);
+            });
+        }));
+        FfProduct b = {};
+        b.A = rows_operand(w.h, s.n, T2, F2);
+        b.B = rows_operand(w.wd, s.n, D2, F2);
+        b.M = T;
+        b.N = s.D;
+        b.K = F2;
+        b.row_inv = w.h_inv;
+        b.row_batch = T2;
+        b.col_inv = w.wd_inv;
+        b.col_batch = D2;
+        b.out = static_cast<M*>(y) + (int64_t)t0 * s.ld;
+        b.out_ld = s.ld;
+        b.out_node = (int64_t)s.T * s.ld;
+        const bool wide2 = wide_tiles(c, T, D2);
+        GPGA_LAUNCH(launch_product(c, b, T, D2, wide2, [&](dim3 grid) {
+            if (wide2) k_ff_rows<Wide<PH, PW, false, false>, E><<<grid, dim3(512), 0, c->stream>>>(b);
+            else k_ff_rows<Narrow<PH, PW, false, false>, E><<<grid, dim3(256), 0, c->stream>>>(b);
+        }));
+    }
+    return hipSuccess;
+}
+
+template <typename E>
+hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const void* x, const void* hidden, void* dx, bool accumulate, char* scratch) {
+    typedef typename E::mem M;
+    constexpr bool kF32 = sizeof(M) == 4, kBf16 = __is_same(M, __bf16);
+    constexpr int PX = kF32 ? 2 : 1, PGU = kF32 ? 2 : 1, PDX = kBf16 ? 1 : 2;
+    size_t bytes;
+    const FfScratch w = carve_ff(s, true, scratch, &bytes);
+    const int32_t D2 = padded(s.D), F2 = padded(s.F);
+    const int64_t n = s.n;
+    GPGA_LAUNCH(launch_blocks((uint64_t)kMaxParts * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+        k_ff_max<<<grid, dim3(kThreads), 0, c->stream>>>(c->x + s.gate_off, c->x + s.up_off, c->ld, (int64_t)s.F * s.D, w.node_max, first);
+    }));
+    GPGA_LAUNCH((launch_pack_matrices<PGU, 2>(c, s, pack_matrices(c, s, w))));
+    for (int32_t t0 = 0; t0 < s.T; t0 += w.chunk) {
+        const int32_t T = s.T - t0 < w.chunk ? s.T - t0 : w.chunk, T2 = padded(T);
+        const int64_t skip = (int64_t)t0 * s.ld;
+        const M* hid = static_cast<const M*>(hidden) + (int64_t)t0 * 2 * s.F;
+        const int64_t hidden_node = (int64_t)s.T * 2 * s.F;
+        PackRows p = {static_cast<const M*>(dy) + skip, s.ld, (int64_t)s.T * s.ld, T, s.D, w.dy, n * T2 * D2, w.x_inv, (uint32_t)(T2 / kPackRows), 0};
+        GPGA_LAUNCH(launch_blocks((uint64_t)p.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+            p.first_block = first;
+            k_ff_pack_dy<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(p, w.wd_inv, static_cast<const M*>(x) + skip, hid, s.F, hidden_node, w.da_up,
+                                                                        w.da_inv, w.h_up, w.h_inv, w.part);
+        }));
+        for (int which = 0; which < 2; ++which) {
+            p.src = static_cast<const M*>(which ? dy : x) + skip;
+            p.dst = which ? w.tok_y : w.tok_x;
+            GPGA_LAUNCH(launch_blocks((uint64_t)p.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+                p.first_block = first;
+                k_ff_pack_tokens<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(p, which ? w.h_inv : w.da_inv, w.x_inv, w.part, p.per_node, which,
+                                                                               w.node_inv + which * n);
+            }));
+        }
+        FfProduct a = {};
+        a.A = rows_operand(w.dy, n, T2, D2);
+        a.B = rows_operand(w.wd, n, D2, F2);
+        a.M = T;
+        a.K = D2;
+        a.F = s.F;
+        a.row_inv = w.x_inv;
+        a.hidden = const_cast<M*>(hid);
+        a.hidden_node = hidden_node;
+        a.h = w.h;
+        a.h_plane = n * T2 * F2;
+        a.h_up = w.h_up;
+        a.da = w.da;
+        a.da_plane = n * T2 * 2 * F2;
+        a.da_up = w.da_up;
+        const bool wide = wide_tiles(c, T2, F2);
+        GPGA_LAUNCH(launch_product(c, a, T2, F2, wide, [&](dim3 grid) {
+            with_act(s.act, [&](auto act) {
+                constexpr int kAct = decltype(act)::value;
+                if (wide) k_ff_down_grad<Wide<PX, 2, false, true>, E, kAct, 2, 2><<<grid, dim3(512), 0, c->stream>>>(a);
+                else k_ff_down_grad<Narrow<PX, 2, false, true>, E, kAct, 2, 2><<<grid, dim3(256), 0, c->stream>>>(a);
+            });
+        }));
+        FfProduct b = {};
+        b.A = rows_operand(w.da, n, T2, 2 * F2);
+        b.B = rows_operand(w.gu, n, 2 * F2, D2);
+        b.M = T;
+        b.N = s.D;
+        b.K = 2 * F2;
+        b.row_inv = w.da_inv;
+        b.row_batch = T2;
+        b.col_inv = w.gu_inv;
+        b.col_batch = 2 * F2;
+        b.out = static_cast<M*>(dx) + skip;
+        b.out_ld = s.ld;
+        b.out_node = (int64_t)s.T * s.ld;
+        const bool wide2 = wide_tiles(c, T, D2);
+        GPGA_LAUNCH(launch_product(c, b, T, D2, wide2, [&](dim3 grid) {
+            if (wide2) k_ff_rows<Wide<PDX, PGU, false, true>, E><<<grid, dim3(512), 0, c->stream>>>(b);
+            else k_ff_rows<Narrow<PDX, PGU, false, true>, E><<<grid, dim3(256), 0, c->stream>>>(b);
+        }));
+        FfProduct g = {};
+        g.A = rows_operand(w.da, n, T2, 2 * F2);
+        g.B = rows_operand(w.tok_x, n, T2, D2);
+        g.M = s.F;
+        g.N = s.D;
+        g.K = T2;
+        g.row_inv = w.node_inv;
+        g.g = c->g;
+        g.g_ld = c->ld;
+        g.off0 = s.gate_off;
+        g.off1 = s.up_off;
+        g.accumulate = accumulate || t0 > 0;
+        const bool wide3 = wide_tiles(c, 2 * F2, D2);
+        GPGA_LAUNCH(launch_product(c, g, 2 * F2, D2, wide3, [&](dim3 grid) {
+            if (wide3) k_ff_matrix_grad<Wide<2, PX, true, true>><<<grid, dim3(512), 0, c->stream>>>(g);
+            else k_ff_matrix_grad<Narrow<2, PX, true, true>><<<grid, dim3(256), 0, c->stream>>>(g);
+        }));
+        g.A = rows_operand(w.tok_y, n, T2, D2);
+        g.B = rows_operand(w.h, n, T2, F2);
+        g.M = s.D;
+        g.N = s.F;
+        g.row_inv = w.node_inv + n;
+        g.off0 = s.down_off;
+        g.off1 = -1;
+        const bool wide4 = wide_tiles(c, D2, F2);
+        GPGA_LAUNCH(launch_product(c, g, D2, F2, wide4, [&](dim3 grid) {
+            if (wide4) k_ff_matrix_grad<Wide<PX, 2, true, true>><<<grid, dim3(512), 0, c->stream>>>(g);
+            else k_ff_matrix_grad<Narrow<PX, 2, true, true>><<<grid, dim3(256), 0, c->stream>>>(g);
+        }));
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+size_t gated_ff_scratch(const FfShape& s, bool grad) {
+    size_t bytes;
+    carve_ff(s, grad, nullptr, &bytes);
+    return s.T ? bytes : 0;
+}
+
+hipError_t launch_gated_ff(const gpga_ctx* c, const FfShape& s, const void* x, void* hidden, void* y, void* scratch) {
+    auto launch = [&](auto e) { return forward<decltype(e)>(c, s, x, hidden, y, static_cast<char*>(scratch)); };
+    return s.D < kOct || s.F < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
+}
+
+hipError_t launch_gated_ff_grad(const gpga_ctx* c, const FfShape& s, const void* dy, const void* x, const void* hidden, void* dx, bool accumulate,
+                                void* scratch) {
+    if (s.T == 0) {
+        if (accumulate) return hipSuccess;
+        const int64_t count = (int64_t)s.F * s.D;
+        const uint32_t per_node = (uint32_t)((count + kThreads - 1) / kThreads);
+        return launch_blocks((uint64_t)per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+            k_ff_zero<<<grid, dim3(kThreads), 0, c->stream>>>(c->g, c->ld, s.gate_off, s.up_off, s.down_off, count, per_node, first);
+        });
+    }
+    auto launch = [&](auto e) { return backward<decltype(e)>(c, s, dy, x, hidden, dx, accumulate, static_cast<char*>(scratch)); };
+    return s.D < kOct || s.F < kOct ? with_narrow_elem(s.dtype, launch) : with_elem(s.dtype, launch);
+}

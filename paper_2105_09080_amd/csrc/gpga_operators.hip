@@ -118,10 +118,9 @@ gpga_status check_rows(gpga_ctx* c, const RowsShape& s, const Array* arrays, int
     return GPGA_OK;
 }
 
-// `floats` of fp32 that the call reads or writes beside its rows: they share no byte with an output or, written, with any array.
-gpga_status check_floats(gpga_ctx* c, const RowsShape& s, const char* name, const float* p, int64_t floats, bool out, const Array* arrays, int count) {
-    if (!p || !floats) return GPGA_OK;
-    const int64_t bytes = floats * (int64_t)sizeof(float);
+// `bytes` in one piece that the call reads or writes beside its rows: they share none with an output or, written, with any array.
+gpga_status check_bytes(gpga_ctx* c, const RowsShape& s, const char* name, const void* p, int64_t bytes, bool out, const Array* arrays, int count) {
+    if (!p || !bytes) return GPGA_OK;
     for (int k = 0; k < count; ++k)
         if (s.T > 0 && arrays[k].p && (out || arrays[k].out) && rows_meet_span(row_bytes(s, arrays[k].p), p, bytes))
             return fail(c, GPGA_EINVAL, "%s and %s overlap", name, arrays[k].name);
@@ -131,6 +130,9 @@ gpga_status check_floats(gpga_ctx* c, const RowsShape& s, const char* name, cons
         if (h && (out || h == c->g) && rows_meet_span({h, 1, state, state}, p, bytes))
             return fail(c, GPGA_EINVAL, "%s overlaps a bound array", name);
     return GPGA_OK;
+}
+gpga_status check_floats(gpga_ctx* c, const RowsShape& s, const char* name, const float* p, int64_t floats, bool out, const Array* arrays, int count) {
+    return check_bytes(c, s, name, p, floats * (int64_t)sizeof(float), out, arrays, count);
 }
 
 // `count` parameters of every node from column `off` on.
@@ -174,6 +176,22 @@ gpga_status make_drop(gpga_ctx* c, const RowsShape& s, float p, uint64_t seed, i
     out->drop = drop;
     out->factor = (float)(65536.0 / (65536.0 - (double)drop));
     return GPGA_OK;
+}
+
+// Width, kind and matrices of a gated feed-forward block; the kept [a | b], n * T dense rows of 2 F elements.
+gpga_status check_gated_ff(gpga_ctx* c, const RowsShape& s, const FfShape& f, const void* hidden, bool out, const Array* arrays, int count) {
+    constexpr int32_t kMost = 1 << 21;
+    if (f.D > kMost || f.F < 1 || f.F > kMost) return fail(c, GPGA_EINVAL, "D = %d and F = %d must be 1..%d", f.D, f.F, kMost);
+    const int64_t D64 = ((int64_t)f.D + 63) / 64 * 64, F64 = ((int64_t)f.F + 63) / 64 * 64;
+    if (D64 * F64 >= 1ll << 30) return fail(c, GPGA_EINVAL, "D x F = %d x %d, each rounded up to a multiple of 64, must be below 2^30", f.D, f.F);
+    if (f.act != GPGA_SILU && f.act != GPGA_GELU) return fail(c, GPGA_EINVAL, "act %d is not a gpga_activation", f.act);
+    const int64_t matrix = (int64_t)f.F * f.D, bytes = (int64_t)s.n * s.T * 2 * f.F * elem_size(s.dtype);
+    gpga_status st = check_columns(c, "gate", f.gate_off, matrix);
+    if (st == GPGA_OK) st = check_columns(c, "up", f.up_off, matrix);
+    if (st == GPGA_OK) st = check_columns(c, "down", f.down_off, matrix);
+    if (st != GPGA_OK) return st;
+    if (reinterpret_cast<uintptr_t>(hidden) & (uintptr_t)(elem_size(s.dtype) - 1)) return fail(c, GPGA_EINVAL, "hidden_dev is not aligned to its elements");
+    return check_bytes(c, s, "hidden_dev", hidden, bytes, out, arrays, count);
 }
 
 #define GPGA_TRY(call)                        \
@@ -303,6 +321,49 @@ gpga_status gpga_token_loss(gpga_ctx* c, const void* logits, const int32_t* labe
     GPGA_TRY(reserve(c, token_loss_scratch(s, c->num_cus)));
     const hipError_t e = launch_token_loss(c, s, logits, labels, grad_scale, loss, dlogits, c->op_scratch);
     return e == hipSuccess ? GPGA_OK : hip_fail(c, e, "token loss kernel launch");
+}
+
+gpga_status gpga_gated_ff(gpga_ctx* c, const void* x, int32_t T, int32_t D, int32_t F, int64_t ld, int32_t dtype, int32_t act, int64_t gate_off,
+                          int64_t up_off, int64_t down_off, void* hidden, void* y) {
+    if (!c) return GPGA_EINVAL;
+    GPGA_TRY(check_ready(c));
+    const RowsShape s = {c->n, T, D, ld, dtype};
+    const FfShape f = {c->n, T, D, F, ld, dtype, act, gate_off, up_off, down_off};
+    const Array arrays[] = {{"x_dev", x, false}, {"y_dev", y, true}};
+    GPGA_TRY(check_rows(c, s, arrays, 2));
+    GPGA_TRY(check_gated_ff(c, s, f, hidden, true, arrays, 2));
+    if (T == 0) return GPGA_OK;
+    if (!x || !y) return fail(c, GPGA_EINVAL, "x_dev and y_dev must not be NULL");
+    DeviceGuard guard(c->device);
+    GPGA_TRY(reserve(c, gated_ff_scratch(f, false)));
+    const hipError_t e = launch_gated_ff(c, f, x, hidden, y, c->op_scratch);
+    return e == hipSuccess ? GPGA_OK : hip_fail(c, e, "feed-forward kernel launch");
+}
+
+gpga_status gpga_gated_ff_grad(gpga_ctx* c, const void* dy, const void* x, const void* hidden, int32_t T, int32_t D, int32_t F, int64_t ld, int32_t dtype,
+                               int32_t act, int64_t gate_off, int64_t up_off, int64_t down_off, void* dx, int32_t accumulate) {
+    if (!c) return GPGA_EINVAL;
+    GPGA_TRY(check_ready(c));
+    const RowsShape s = {c->n, T, D, ld, dtype};
+    const FfShape f = {c->n, T, D, F, ld, dtype, act, gate_off, up_off, down_off};
+    const Array arrays[] = {{"dy_dev", dy, false}, {"x_dev", x, false}, {"dx_dev", dx, true}};
+    GPGA_TRY(check_rows(c, s, arrays, 3, true));
+    GPGA_TRY(check_gated_ff(c, s, f, hidden, false, arrays, 3));
+    const int64_t matrix = (int64_t)F * D;
+    const struct {
+        const char* name;
+        int64_t off;
+    } blocks[3] = {{"gate", gate_off}, {"up", up_off}, {"down", down_off}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j < i; ++j)
+            if (blocks[i].off < blocks[j].off + matrix && blocks[j].off < blocks[i].off + matrix)
+                return fail(c, GPGA_EINVAL, "the columns of %s and %s overlap", blocks[j].name, blocks[i].name);
+    if (accumulate != 0 && accumulate != 1) return fail(c, GPGA_EINVAL, "accumulate must be 0 or 1");
+    if (T > 0 && (!dy || !x || !hidden || !dx)) return fail(c, GPGA_EINVAL, "dy_dev, x_dev, hidden_dev and dx_dev must not be NULL");
+    DeviceGuard guard(c->device);
+    GPGA_TRY(reserve(c, gated_ff_scratch(f, true)));
+    const hipError_t e = launch_gated_ff_grad(c, f, dy, x, hidden, dx, accumulate != 0, c->op_scratch);
+    return e == hipSuccess ? GPGA_OK : hip_fail(c, e, "feed-forward gradient kernel launch");
 }
 
 }  // extern "C"

@@ -244,6 +244,18 @@ size_t token_loss_scratch(const RowsShape& s, int num_cus);
 hipError_t launch_token_loss(const gpga_ctx* c, const RowsShape& s, const void* logits, const int32_t* labels, float grad_scale, float* loss,
                              void* dlogits, void* scratch);
 
+// Gated feed-forward block (gpga_gated_ff.hip): T tokens a node, matrices at column offsets of X.
+struct FfShape {
+    int32_t n, T, D, F;
+    int64_t ld;
+    int32_t dtype, act;
+    int64_t gate_off, up_off, down_off;
+};
+size_t gated_ff_scratch(const FfShape& s, bool grad);
+hipError_t launch_gated_ff(const gpga_ctx* c, const FfShape& s, const void* x, void* hidden, void* y, void* scratch);
+hipError_t launch_gated_ff_grad(const gpga_ctx* c, const FfShape& s, const void* dy, const void* x, const void* hidden, void* dx, bool accumulate,
+                                void* scratch);
+
 // Whether accesses to activation arrays stream past the L2 caches (4 MiB for each of 8 XCDs): arrays of 32 MiB and more whose rows
 // begin on 16-byte boundaries.  Streaming stores that end within a line are written by themselves: 8 x 1537 rows of 3642
 // bf16 took 35 us with them and 25 without.

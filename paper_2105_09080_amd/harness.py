@@ -330,6 +330,40 @@ class Simulation:
             self._used(logits, labels, into)
         return loss, dlogits
 
+    def gated_ff(self, x: torch.Tensor, gate_off: int, up_off: int, down_off: int, F: int, *, act: str = "silu",
+                 keep: bool = False):
+        """(y, hidden): y = Wd_i (act(Wg_i x) * Wu_i x); hidden = [Wg_i x | Wu_i x], (n, T, 2F), for the backward pass if
+        ``keep``, else None."""
+        T, D, ld, dt = self._rows(x)
+        if act not in B.ACTIVATION:
+            raise ValueError(f"act must be one of {sorted(B.ACTIVATION)}, got {act!r}")
+        foreign = self._foreign()
+        y = self._like(x, ld, foreign)
+        hidden = self._empty((self.n, T, 2 * F), x.dtype, foreign) if keep else None
+        B.gpga_gated_ff(self.ctx, x, T, D, F, ld, dt, B.ACTIVATION[act], gate_off, up_off, down_off, hidden, y)
+        if foreign:
+            self._used(x)
+        return y, hidden
+
+    def gated_ff_grad(self, dy: torch.Tensor, x: torch.Tensor, hidden: torch.Tensor, gate_off: int, up_off: int, down_off: int,
+                      *, act: str = "silu", accumulate: bool = False) -> torch.Tensor:
+        """dx; the gradients of the three matrices land in G."""
+        T, D, ld, dt = self._rows(dy, x)
+        if act not in B.ACTIVATION:
+            raise ValueError(f"act must be one of {sorted(B.ACTIVATION)}, got {act!r}")
+        if (hidden.dtype != x.dtype or hidden.dim() != 3 or hidden.shape[:2] != (self.n, T) or hidden.shape[2] % 2 or
+                not hidden.is_contiguous() or hidden.get_device() != self._device_index):
+            raise ValueError("hidden is the contiguous (n, T, 2F) tensor of the activations' type that gated_ff keeps, on the simulation's GPU")
+        if hidden.requires_grad and torch.is_grad_enabled():
+            raise ValueError("an activation requires grad: these calls are not recorded for torch's backward()")
+        foreign = self._foreign()
+        dx = self._like(dy, ld, foreign)
+        B.gpga_gated_ff_grad(self.ctx, dy, x, hidden, T, D, hidden.shape[2] // 2, ld, dt, B.ACTIVATION[act], gate_off, up_off,
+                             down_off, dx, accumulate)
+        if foreign:
+            self._used(dy, x, hidden)
+        return dx
+
     def tune(self, launches: int = 16):
         """Let the pacing controllers settle (state arrays are left with unspecified contents)."""
         B.gpga_tune(self.ctx, launches)
