@@ -470,6 +470,19 @@ gpga_status gpga_gated_ff_grad(gpga_ctx* ctx, const void* dy_dev, const void* x_
                                int32_t D, int32_t F, int64_t ld, int32_t dtype, int32_t act, int64_t gate_off,
                                int64_t up_off, int64_t down_off, void* dx_dev, int32_t accumulate);
 
+/* Orthogonalised updates: in every node's row of g_dev the `count` row-major matrices of rows x cols that lie one after another from
+ * column `off` on are replaced, each by scale * X after `steps` (0..64) Newton-Schulz steps
+ *     X <- a X + b (X X^T) X + c (X X^T)^2 X          (rows > cols: the same from the other side, X^T X)
+ * from X = U / (|U|_F + eps): singular values s become a s + b s^3 + c s^5 a step, singular vectors stay.  velocity_dev NULL: U is
+ * the gradient g found there; else it holds n x (count * rows * cols) dense floats of the caller's, V <- mu V + g, and U = V, or
+ * g + mu V with nesterov = 1 (mu > 0).  A gpga_step then takes the updates as it takes gradients; with a context momentum it sums them
+ * up in m, so momentum belongs in one of the two places.  A matrix of zeros gives zeros; one with an infinity or NaN gives NaN, whole.
+ * Sides up to 2^21, their product with both rounded up to multiples of 64 below 2^30, n * count <= 2^24.
+ * Products are made of two fp16 pieces an operand with fp32 sums.  EINVAL if the coefficients let a singular value of at most 1
+ * pass 64 in these steps.  Asynchronous; scratch as above. */
+gpga_status gpga_orthogonalize(gpga_ctx* ctx, int64_t off, int32_t rows, int32_t cols, int32_t count, float* velocity_dev,
+                               float mu, int32_t nesterov, int32_t steps, float a, float b, float c, float eps, float scale);
+
 /* Measurement aid, not part of the method: a plain streaming kernel over `bytes`
  * (a multiple of 16) per array of device memory on hip_stream, with the same 128-bit
  * non-temporal accesses as the fused step.  kind 0 reads src_dev (dst_dev: any

@@ -90,6 +90,8 @@ SIGNATURES = [
     ("gpga_gated_ff_grad", _c.c_int, [_ctx_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int32, _c.c_int32, _c.c_int32,
                                       _c.c_int64, _c.c_int32, _c.c_int32, _c.c_int64, _c.c_int64, _c.c_int64, _c.c_void_p,
                                       _c.c_int32]),
+    ("gpga_orthogonalize", _c.c_int, [_ctx_p, _c.c_int64, _c.c_int32, _c.c_int32, _c.c_int32, _c.c_void_p, _c.c_float,
+                                      _c.c_int32, _c.c_int32, _c.c_float, _c.c_float, _c.c_float, _c.c_float, _c.c_float]),
     ("gpga_probe_stream", _c.c_int, [_c.c_int32, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_int64,
                                      _c.c_int32, _c.c_void_p]),
     ("gpga_last_error", _c.c_char_p, [_ctx_p]),
@@ -392,6 +394,14 @@ def gpga_gated_ff_grad(ctx, dy, x, hidden, T: int, D: int, F: int, ld: int, dtyp
         _int32(T, D, F)
     _check(ctx, _lib.gpga_gated_ff_grad(ctx, _ptr(dy), _ptr(x), _ptr(hidden), T, D, F, ld, dtype, act, gate_off, up_off,
                                         down_off, _ptr(dx), int(accumulate)))
+
+
+def gpga_orthogonalize(ctx, off: int, rows: int, cols: int, count: int, velocity, mu: float, nesterov: bool, steps: int, a: float,
+                       b: float, c: float, eps: float, scale: float):
+    """velocity: n x (count * rows * cols) dense floats, updated in place, or None."""
+    if (rows | cols | count | steps) >> 31:
+        _int32(rows, cols, count, steps)
+    _check(ctx, _lib.gpga_orthogonalize(ctx, off, rows, cols, count, _ptr(velocity), mu, int(nesterov), steps, a, b, c, eps, scale))
 
 
 def gpga_probe_stream(kind: int, src, dst, nbytes: int, stream=None, src2=None, inout=None, blocks_per_cu: int = 0):

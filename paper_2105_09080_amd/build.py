@@ -15,7 +15,8 @@ OBJ_DIR = os.path.join(PKG_DIR, "_build")
 SOURCES = ["gpga_api.hip", "gpga_step.hip", "gpga_mix.hip", "gpga_graph.hip", "gpga_grad.hip", "gpga_reduce.hip",
            "gpga_column.hip", "gpga_rows_step.hip", "gpga_circ.hip", "gpga_virtual_step.hip",
            "gpga_rows_run.hip", "gpga_gang.hip", "gpga_static.hip", "gpga_operators.hip", "gpga_embed.hip",
-           "gpga_norm.hip", "gpga_token_loss.hip", "gpga_gated_ff.hip"]
+           "gpga_norm.hip", "gpga_token_loss.hip", "gpga_gated_ff.hip",
+           "gpga_orthogonalize.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC",

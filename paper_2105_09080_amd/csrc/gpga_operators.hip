@@ -366,4 +366,38 @@ gpga_status gpga_gated_ff_grad(gpga_ctx* c, const void* dy, const void* x, const
     return e == hipSuccess ? GPGA_OK : hip_fail(c, e, "feed-forward gradient kernel launch");
 }
 
+gpga_status gpga_orthogonalize(gpga_ctx* c, int64_t off, int32_t rows, int32_t cols, int32_t count, float* velocity, float mu, int32_t nesterov,
+                               int32_t steps, float a, float b, float cc, float eps, float scale) {
+    if (!c) return GPGA_EINVAL;
+    GPGA_TRY(check_ready(c));
+    constexpr int32_t kMost = 1 << 21;
+    if (rows < 1 || cols < 1 || rows > kMost || cols > kMost) return fail(c, GPGA_EINVAL, "a matrix of %d x %d: sides must be 1..%d", rows, cols, kMost);
+    const int64_t R64 = ((int64_t)rows + 63) / 64 * 64, C64 = ((int64_t)cols + 63) / 64 * 64;
+    if (R64 * C64 >= 1ll << 30) return fail(c, GPGA_EINVAL, "%d x %d, each rounded up to a multiple of 64, must be below 2^30", rows, cols);
+    if (count < 1) return fail(c, GPGA_EINVAL, "count = %d must be at least 1", count);
+    const int64_t size = (int64_t)rows * cols;
+    if (count > c->d / size) return fail(c, GPGA_EINVAL, "%d matrices of %d x %d are not within d = %lld", count, rows, cols, (long long)c->d);
+    if ((int64_t)c->n * count > 1 << 24) return fail(c, GPGA_EINVAL, "n * count must be at most 2^24");
+    GPGA_TRY(check_columns(c, "matrices", off, size * count));
+    if (!(mu >= 0.f && mu < 1.f)) return fail(c, GPGA_EINVAL, "mu = %g must be in [0, 1)", (double)mu);
+    if (!velocity && mu != 0.f) return fail(c, GPGA_EINVAL, "velocity_dev must not be NULL with mu > 0");
+    if (nesterov != 0 && nesterov != 1) return fail(c, GPGA_EINVAL, "nesterov must be 0 or 1");
+    if (nesterov && mu == 0.f) return fail(c, GPGA_EINVAL, "nesterov needs mu > 0");
+    if (steps < 0 || steps > 64) return fail(c, GPGA_EINVAL, "steps = %d must be 0..64", steps);
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(cc)) return fail(c, GPGA_EINVAL, "the coefficients must be finite");
+    if (!(std::isfinite(eps) && eps >= 0.f)) return fail(c, GPGA_EINVAL, "eps must be finite and >= 0");
+    if (!std::isfinite(scale)) return fail(c, GPGA_EINVAL, "scale must be finite");
+    const float coefficients[3] = {a, b, cc};
+    const double most = orthogonalize_bound(steps, coefficients);
+    if (!(most <= 64.0)) return fail(c, GPGA_EINVAL, "these coefficients let singular values grow to %.3g: at most 64", most);
+    if (reinterpret_cast<uintptr_t>(velocity) & 3u) return fail(c, GPGA_EINVAL, "velocity_dev is not 4-byte aligned");
+    const RowsShape none = {c->n, 0, 1, 1, GPGA_F32};
+    GPGA_TRY(check_floats(c, none, "velocity_dev", velocity, c->n * size * count, true, nullptr, 0));
+    DeviceGuard guard(c->device);
+    const OrthShape s = {c->n, rows, cols, count};
+    GPGA_TRY(reserve(c, orthogonalize_scratch(s)));
+    const hipError_t e = launch_orthogonalize(c, s, off, velocity, mu, nesterov != 0, steps, coefficients, eps, scale, c->op_scratch);
+    return e == hipSuccess ? GPGA_OK : hip_fail(c, e, "orthogonalisation kernel launch");
+}
+
 }  // extern "C"

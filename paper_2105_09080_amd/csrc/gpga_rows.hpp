@@ -256,6 +256,16 @@ hipError_t launch_gated_ff(const gpga_ctx* c, const FfShape& s, const void* x, v
 hipError_t launch_gated_ff_grad(const gpga_ctx* c, const FfShape& s, const void* dy, const void* x, const void* hidden, void* dx, bool accumulate,
                                 void* scratch);
 
+// Orthogonalised updates (gpga_orthogonalize.hip): `count` matrices of R x C a node, one after another.
+struct OrthShape {
+    int32_t n, R, C, count;
+};
+size_t orthogonalize_scratch(const OrthShape& s);
+// Largest singular value that any of the steps can lead to.
+double orthogonalize_bound(int32_t steps, const float* coefficients);
+hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t off, float* v, float mu, bool nesterov, int32_t steps,
+                                const float* coefficients, float eps, float scale, void* scratch);
+
 // Whether accesses to activation arrays stream past the L2 caches (4 MiB for each of 8 XCDs): arrays of 32 MiB and more whose rows
 // begin on 16-byte boundaries.  Streaming stores that end within a line are written by themselves: 8 x 1537 rows of 3642
 // bf16 took 35 us with them and 25 without.

@@ -364,6 +364,22 @@ class Simulation:
             self._used(dy, x, hidden)
         return dx
 
+    def orthogonalize(self, off: int, rows: int, cols: int, *, count: int = 1, velocity: torch.Tensor | None = None,
+                      mu: float = 0.0, nesterov: bool = False, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315),
+                      eps: float = 1e-7, scale: float = 1.0):
+        """The gradients of ``count`` matrices of rows x cols in G[:, off:] become scale times orthogonalised updates;
+        ``velocity``: (n, count * rows * cols) fp32, the running sums, updated in place."""
+        if velocity is not None:
+            if (velocity.dtype != torch.float32 or tuple(velocity.shape) != (self.n, count * rows * cols) or
+                    not velocity.is_contiguous() or velocity.get_device() != self._device_index):
+                raise ValueError("velocity is a contiguous (n, count * rows * cols) fp32 tensor on the simulation's GPU")
+            if velocity.requires_grad and torch.is_grad_enabled():
+                raise ValueError("velocity requires grad: these calls are not recorded for torch's backward()")
+        a, b, c = coefficients
+        B.gpga_orthogonalize(self.ctx, off, rows, cols, count, velocity, mu, nesterov, steps, a, b, c, eps, scale)
+        if velocity is not None and self._foreign():
+            self._used(velocity)
+
     def tune(self, launches: int = 16):
         """Let the pacing controllers settle (state arrays are left with unspecified contents)."""
         B.gpga_tune(self.ctx, launches)
