@@ -234,31 +234,6 @@ struct FfProduct {
     int accumulate;
 };
 
-// Four columns of a row of activations, as many as there are.
-template <typename E>
-__device__ __forceinline__ void put4(typename E::mem* row, int32_t col, int32_t cols, v4f v) {
-    typedef typename E::mem M;
-    typedef M vec __attribute__((ext_vector_type(4), aligned(alignof(M))));
-    if (col + 4 <= cols) {
-        *reinterpret_cast<vec*>(row + col) = __builtin_convertvector(v, vec);
-    } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (col + k < cols) row[col + k] = E::put(v[k]);
-    }
-}
-template <typename E>
-__device__ __forceinline__ v4f get4(const typename E::mem* row, int32_t col, int32_t cols) {
-    typedef typename E::mem M;
-    typedef M vec __attribute__((ext_vector_type(4), aligned(alignof(M))));
-    if (col + 4 <= cols) return __builtin_convertvector(*reinterpret_cast<const vec*>(row + col), v4f);
-    v4f v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (col + k < cols) v[k] = E::get(row[col + k]);
-    return v;
-}
-
 // h = act(x Wg^T) (x Wu^T): a wavefront's blocks of 32 columns are gate and up of the same 32 f's in turn.
 template <typename S, typename E, int Act, int PH>
 __global__ __launch_bounds__(S::Threads) void k_ff_up(FfProduct a) {
@@ -270,36 +245,29 @@ __global__ __launch_bounds__(S::Threads) void k_ff_up(FfProduct a) {
     acc16 acc[S::NI][S::MI];
     product_tile<S>(a.A, a.B, node, m0, 0, a.K, lds, acc,
                     [&](int row) { return (row >> 5 & 1) * F2 + min(f0 + (row >> 6) * 32 + (row & 31), F2 - 1); });
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int64_t T2 = a.A.rows;
     typedef typename E::mem M;
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i) {
-        const int32_t row = m0 + wave / S::WN * (S::BM / S::WM) + i * 32 + (lane & 31);
-        if (row >= a.M) continue;
+    const int32_t f1 = wave_col<S>(2 * f0) / 2;
+    const int64_t T2 = a.A.rows;
+    each_octet_pair<S>(acc, lds, m0, [&](int32_t row, int32_t col, float* va, float* vb) {
+        const int32_t f = f1 + col;
+        if (row >= a.M || f >= F2) return;
         const int64_t at = node * T2 + row;
         const float xi = a.row_inv[at], up = a.h_up[at];
-        const float* wi = a.col_inv + (int64_t)node * 2 * F2;
-        M* hid = static_cast<M*>(a.hidden) + (int64_t)node * a.hidden_node + (int64_t)row * 2 * a.F;
+        const float* wi = a.col_inv + (int64_t)node * 2 * F2 + f;
+        float h[8];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int32_t f = f0 + wave % S::WN * 32 + q * 8 + (lane >> 5) * 4;
-            if (f >= F2) continue;
-            const v4f gi = *reinterpret_cast<const v4f*>(wi + f), ui = *reinterpret_cast<const v4f*>(wi + F2 + f);
-            v4f va, vb, h;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                va[k] = acc[0][i][q * 4 + k] * (xi * gi[k]);
-                vb[k] = acc[1][i][q * 4 + k] * (xi * ui[k]);
-                h[k] = act_value<Act>(va[k]) * vb[k] * up;
-            }
-            store_planes<PH>(a.h + at * F2 + f, a.h_plane, h);
-            if (a.hidden) {
-                put4<E>(hid, f, a.F, va);
-                put4<E>(hid + a.F, f, a.F, vb);
-            }
+        for (int k = 0; k < 8; ++k) {
+            va[k] *= xi * wi[k];
+            vb[k] *= xi * wi[F2 + k];
+            h[k] = act_value<Act>(va[k]) * vb[k] * up;
         }
-    }
+        store_planes<PH>(a.h + at * F2 + f, a.h_plane, h);
+        if (a.hidden && f < a.F) {
+            M* hid = static_cast<M*>(a.hidden) + (int64_t)node * a.hidden_node + (int64_t)row * 2 * a.F;
+            piece_put<kOct, E>(hid, f, a.F, va);
+            piece_put<kOct, E>(hid + a.F, f, a.F, vb);
+        }
+    });
 }
 
 // Activations out: rows' scales times columns' scales (col_batch < 0: one a node).
@@ -312,19 +280,13 @@ __global__ __launch_bounds__(S::Threads) void k_ff_rows(FfProduct a) {
     acc16 acc[S::NI][S::MI];
     product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return min(n0 + row, a.B.rows - 1); });
     typedef typename E::mem M;
-    each_quad<S>(acc, m0, n0, [&](int32_t row, int32_t col, v4f v) {
+    each_octet<S>(acc, lds, m0, n0, false, [&](int32_t row, int32_t col, float* v) {
         if (row >= a.M || col >= a.N) return;
         const float r = a.row_inv[node * a.row_batch + row];
-        v4f c;
-        if (S::ColsB) {
-            const float w = a.col_inv[node * a.col_batch];
-            c = v4f{w, w, w, w};
-        } else {
-            c = *reinterpret_cast<const v4f*>(a.col_inv + node * a.col_batch + col);
-        }
+        const float* c = a.col_inv + node * a.col_batch + (S::ColsB ? 0 : col);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] *= r * c[k];
-        put4<E>(static_cast<M*>(a.out) + node * a.out_node + (int64_t)row * a.out_ld, col, a.N, v);
+        for (int k = 0; k < 8; ++k) v[k] *= r * c[S::ColsB ? 0 : k];
+        piece_put<kOct, E>(static_cast<M*>(a.out) + node * a.out_node + (int64_t)row * a.out_ld, col, a.N, v);
     });
 }
 
@@ -339,23 +301,28 @@ __global__ __launch_bounds__(S::Threads) void k_ff_down_grad(FfProduct a) {
     acc16 acc[S::NI][S::MI];
     product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return row; });
     typedef typename E::mem M;
-    each_quad<S>(acc, m0, n0, [&](int32_t row, int32_t f, v4f dh) {
+    each_octet<S>(acc, lds, m0, n0, false, [&](int32_t row, int32_t f, float* da) {
         if (row >= T2 || f >= F2) return;
         const int64_t at = (int64_t)node * T2 + row;
-        v4f da = {0.f, 0.f, 0.f, 0.f}, db = da, h = da;
-        if (row < a.M) {
+        float db[8] = {0.f}, h[8] = {0.f};
+        if (row < a.M && f < a.F) {
             const M* hid = static_cast<const M*>(a.hidden) + (int64_t)node * a.hidden_node + (int64_t)row * 2 * a.F;
-            const v4f va = get4<E>(hid, f, a.F), vb = get4<E>(hid + a.F, f, a.F);
-            const float inv = a.row_inv[at], da_up = a.da_up[at], h_up = a.h_up[at];
+            float va[8], vb[8];
+            piece_read<kOct, E>(hid, f, a.F, va);
+            piece_read<kOct, E>(hid + a.F, f, a.F, vb);
+            const float inv = a.row_inv[at] * a.da_up[at], h_up = a.h_up[at];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 8; ++k) {
                 float value, slope;
                 act_both<Act>(va[k], &value, &slope);
-                const float d = dh[k] * inv;
-                da[k] = d * vb[k] * slope * da_up;
-                db[k] = d * value * da_up;
+                const float d = da[k] * inv;
+                da[k] = d * vb[k] * slope;
+                db[k] = d * value;
                 h[k] = value * vb[k] * h_up;
             }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) da[k] = 0.f;
         }
         store_planes<PA>(a.da + at * 2 * F2 + f, a.da_plane, da);
         store_planes<PA>(a.da + at * 2 * F2 + F2 + f, a.da_plane, db);
@@ -364,7 +331,8 @@ __global__ __launch_bounds__(S::Threads) void k_ff_down_grad(FfProduct a) {
 }
 
 // Gradients of matrices: rows of the gate's block, then (from F' on) of the up's; or of the down matrix's alone (off1 < 0).
-template <typename S>
+// G: fp32, narrow where a row of the matrix is.
+template <typename S, typename G>
 __global__ __launch_bounds__(S::Threads) void k_ff_matrix_grad(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t node, ti, tj;
@@ -373,7 +341,7 @@ __global__ __launch_bounds__(S::Threads) void k_ff_matrix_grad(FfProduct a) {
     acc16 acc[S::NI][S::MI];
     product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return row; });
     const float inv = a.row_inv[node];
-    each_quad<S>(acc, m0, n0, [&](int32_t row, int32_t col, v4f v) {
+    each_octet<S>(acc, lds, m0, n0, false, [&](int32_t row, int32_t col, float* v) {
         int64_t off = a.off0;
         if (a.off1 >= 0 && row >= a.A.ld / 2) {
             row -= a.A.ld / 2;
@@ -381,9 +349,15 @@ __global__ __launch_bounds__(S::Threads) void k_ff_matrix_grad(FfProduct a) {
         }
         if (row >= a.M || col >= a.N) return;
         float* to = a.g + (int64_t)node * a.g_ld + off + (int64_t)row * a.N;
-        v4f o = {v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-        if (a.accumulate) o += get4<ElemF32>(to, col, a.N);
-        put4<ElemF32>(to, col, a.N, o);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= inv;
+        if (a.accumulate) {
+            float had[8];
+            piece_read<kOct, G>(to, col, a.N, had);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += had[k];
+        }
+        piece_put<kOct, G>(to, col, a.N, v);
     });
 }
 
@@ -468,22 +442,15 @@ FfScratch carve_ff(const FfShape& s, bool grad, char* base, size_t* bytes) {
 
 Operand rows_operand(const half_t* p, int64_t n, int32_t rows, int32_t cols) { return {p, n * rows * cols, (int64_t)rows * cols, cols, rows}; }
 
-// Tiles of 256 x 256 (8 wavefronts) where they fill the card, of 128 x 128 (4) otherwise.
+// Tiles of 256 x 256 (8 wavefronts) or of 128 x 128 (4).
 template <typename F>
 hipError_t launch_product(const gpga_ctx* c, FfProduct& a, int32_t rows, int32_t cols, bool wide, F&& f) {
-    const int32_t side = wide ? 256 : 128;
-    a.grid.tm = (rows + side - 1) / side;
-    a.grid.tn = (cols + side - 1) / side;
-    a.grid.total = (uint32_t)a.grid.tm * (uint32_t)a.grid.tn * (uint32_t)c->n;
+    a.grid.set(rows, cols, wide ? 256 : 128, c->n, false);
     return launch_blocks(a.grid.blocks(), wide ? 512 : 256, [&](uint32_t first, dim3 grid) {
         a.first_block = first;
         f(grid);
     });
 }
-bool wide_tiles(const gpga_ctx* c, int64_t rows, int64_t cols) {
-    return ((rows + 255) / 256) * ((cols + 255) / 256) * c->n >= c->num_cus * 3 / 4;
-}
-
 template <int PA, int PB, bool CA, bool CB>
 using Wide = Tile<256, 256, 2, 4, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
 template <int PA, int PB, bool CA, bool CB>
@@ -567,7 +534,7 @@ hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hid
         a.h = w.h;
         a.h_plane = (int64_t)s.n * T2 * F2;
         a.h_up = w.h_up;
-        const bool wide = wide_tiles(c, T, 2 * F2);
+        const bool wide = wide_tiles(c->num_cus, T, 2 * F2, D2, s.n, false);
         GPGA_LAUNCH(launch_product(c, a, T, 2 * F2, wide, [&](dim3 grid) {
             with_act(s.act, [&](auto act) {
                 constexpr int kAct = decltype(act)::value;
@@ -588,7 +555,7 @@ hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hid
         b.out = static_cast<M*>(y) + (int64_t)t0 * s.ld;
         b.out_ld = s.ld;
         b.out_node = (int64_t)s.T * s.ld;
-        const bool wide2 = wide_tiles(c, T, D2);
+        const bool wide2 = wide_tiles(c->num_cus, T, D2, F2, s.n, false);
         GPGA_LAUNCH(launch_product(c, b, T, D2, wide2, [&](dim3 grid) {
             if (wide2) k_ff_rows<Wide<PH, PW, false, false>, E><<<grid, dim3(512), 0, c->stream>>>(b);
             else k_ff_rows<Narrow<PH, PW, false, false>, E><<<grid, dim3(256), 0, c->stream>>>(b);
@@ -645,7 +612,7 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         a.da = w.da;
         a.da_plane = n * T2 * 2 * F2;
         a.da_up = w.da_up;
-        const bool wide = wide_tiles(c, T2, F2);
+        const bool wide = wide_tiles(c->num_cus, T2, F2, D2, s.n, false);
         GPGA_LAUNCH(launch_product(c, a, T2, F2, wide, [&](dim3 grid) {
             with_act(s.act, [&](auto act) {
                 constexpr int kAct = decltype(act)::value;
@@ -666,7 +633,7 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         b.out = static_cast<M*>(dx) + skip;
         b.out_ld = s.ld;
         b.out_node = (int64_t)s.T * s.ld;
-        const bool wide2 = wide_tiles(c, T, D2);
+        const bool wide2 = wide_tiles(c->num_cus, T, D2, 2 * F2, s.n, false);
         GPGA_LAUNCH(launch_product(c, b, T, D2, wide2, [&](dim3 grid) {
             if (wide2) k_ff_rows<Wide<PDX, PGU, false, true>, E><<<grid, dim3(512), 0, c->stream>>>(b);
             else k_ff_rows<Narrow<PDX, PGU, false, true>, E><<<grid, dim3(256), 0, c->stream>>>(b);
@@ -683,10 +650,10 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         g.off0 = s.gate_off;
         g.off1 = s.up_off;
         g.accumulate = accumulate || t0 > 0;
-        const bool wide3 = wide_tiles(c, 2 * F2, D2);
+        const bool wide3 = wide_tiles(c->num_cus, 2 * F2, D2, T2, s.n, false);
         GPGA_LAUNCH(launch_product(c, g, 2 * F2, D2, wide3, [&](dim3 grid) {
-            if (wide3) k_ff_matrix_grad<Wide<2, PX, true, true>><<<grid, dim3(512), 0, c->stream>>>(g);
-            else k_ff_matrix_grad<Narrow<2, PX, true, true>><<<grid, dim3(256), 0, c->stream>>>(g);
+            if (wide3) k_ff_matrix_grad<Wide<2, PX, true, true>, Elem<float, E::kNarrow>><<<grid, dim3(512), 0, c->stream>>>(g);
+            else k_ff_matrix_grad<Narrow<2, PX, true, true>, Elem<float, E::kNarrow>><<<grid, dim3(256), 0, c->stream>>>(g);
         }));
         g.A = rows_operand(w.tok_y, n, T2, D2);
         g.B = rows_operand(w.h, n, T2, F2);
@@ -695,10 +662,10 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         g.row_inv = w.node_inv + n;
         g.off0 = s.down_off;
         g.off1 = -1;
-        const bool wide4 = wide_tiles(c, D2, F2);
+        const bool wide4 = wide_tiles(c->num_cus, D2, F2, T2, s.n, false);
         GPGA_LAUNCH(launch_product(c, g, D2, F2, wide4, [&](dim3 grid) {
-            if (wide4) k_ff_matrix_grad<Wide<PX, 2, true, true>><<<grid, dim3(512), 0, c->stream>>>(g);
-            else k_ff_matrix_grad<Narrow<PX, 2, true, true>><<<grid, dim3(256), 0, c->stream>>>(g);
+            if (wide4) k_ff_matrix_grad<Wide<PX, 2, true, true>, Elem<float, E::kNarrow>><<<grid, dim3(512), 0, c->stream>>>(g);
+            else k_ff_matrix_grad<Narrow<PX, 2, true, true>, Elem<float, E::kNarrow>><<<grid, dim3(256), 0, c->stream>>>(g);
         }));
     }
     return hipSuccess;

@@ -127,29 +127,24 @@ __global__ __launch_bounds__(S::Threads) void k_orth_product(OrthProduct a) {
     const int32_t m0 = ti * S::BM, n0 = tj * S::BN;
     acc16 acc[S::NI][S::MI];
     product_tile<S>(a.A, a.B, m, m0, n0, a.K, lds, acc, [&](int row) { return min(n0 + row, a.B.rows - 1); });
-    each_quad<S>(acc, m0, n0, [&](int32_t row, int32_t col, v4f v) {
+    const bool mirror = a.grid.tn == 0 && ti != tj;
+    each_octet<S>(acc, lds, m0, n0, mirror, [&](int32_t row, int32_t col, float* v) {
         if (row >= a.rows2 || col >= a.cols2) return;
         const int64_t at = ((int64_t)m * a.rows2 + row) * a.cols2 + col;
-        v4f o = {v[0] * a.times, v[1] * a.times, v[2] * a.times, v[3] * a.times};
-        if (a.add) {
-            const v4f hi = __builtin_convertvector(*reinterpret_cast<const half4*>(a.add + at), v4f),
-                      lo = __builtin_convertvector(*reinterpret_cast<const half4*>(a.add + a.plane + at), v4f);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) o[k] += a.keep * (hi[k] + lo[k]);
+        for (int k = 0; k < 8; ++k) v[k] *= a.times;
+        if (a.add) {
+            const half8 hi = *reinterpret_cast<const half8*>(a.add + at), lo = *reinterpret_cast<const half8*>(a.add + a.plane + at);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += a.keep * ((float)hi[k] + (float)lo[k]);
         }
         if constexpr (Last) {
             if (row >= a.R || col >= a.C) return;
             float* to = block_of(a.g, a.ld, a.first + m, a.count, (int64_t)a.R * a.C) + (int64_t)row * a.C;
-            typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
-            if (col + 4 <= a.C) {
-                *reinterpret_cast<vec*>(to + col) = vec{o[0], o[1], o[2], o[3]};
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (col + k < a.C) to[col + k] = o[k];
-            }
+            if (a.C < kOct) piece_put<kOct, Elem<float, true>>(to, col, a.C, v);
+            else piece_put<kOct, Elem<float, false>>(to, col, a.C, v);
         } else {
-            store_planes<2>(a.out + at, a.plane, o);
+            store_planes<2>(a.out + at, a.plane, v);
         }
     });
 }
@@ -178,12 +173,9 @@ template <int PA, int PB, bool CA, bool CB>
 using Narrow = Tile<128, 128, 2, 2, 32, PA, PB, CA, CB>;
 
 template <bool CA, bool CB, bool Last>
-hipError_t launch_product(const gpga_ctx* c, OrthProduct& a, int32_t matrices) {
-    const bool wide = (int64_t)((a.rows2 + 255) / 256) * ((a.cols2 + 255) / 256) * matrices >= c->num_cus * 3 / 4;
-    const int32_t side = wide ? 256 : 128;
-    a.grid.tm = (a.rows2 + side - 1) / side;
-    a.grid.tn = (a.cols2 + side - 1) / side;
-    a.grid.total = (uint32_t)a.grid.tm * (uint32_t)a.grid.tn * (uint32_t)matrices;
+hipError_t launch_product(const gpga_ctx* c, OrthProduct& a, int32_t matrices, bool lower) {
+    const bool wide = wide_tiles(c->num_cus, a.rows2, a.cols2, a.K, matrices, lower);
+    a.grid.set(a.rows2, a.cols2, wide ? 256 : 128, matrices, lower);
     return launch_blocks(a.grid.blocks(), wide ? 512 : 256, [&](uint32_t first, dim3 grid) {
         a.first_block = first;
         if (wide) k_orth_product<Wide<2, 2, CA, CB>, Last><<<grid, dim3(512), 0, c->stream>>>(a);
@@ -327,7 +319,7 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             o.plane = gram.plane;
             o.rows2 = o.cols2 = m2;
             o.times = (float)((double)gram_up / x_up / x_up);
-            e = tall ? launch_product<true, true, false>(c, o, matrices) : launch_product<false, false, false>(c, o, matrices);
+            e = tall ? launch_product<true, true, false>(c, o, matrices, true) : launch_product<false, false, false>(c, o, matrices, true);
             if (e != hipSuccess) return e;
             // q A + r A A
             o.A = o.B = gram;
@@ -336,7 +328,7 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             o.out = w.poly;
             o.keep = (float)(q * poly_up / gram_up);
             o.times = (float)(r * poly_up / gram_up / gram_up);
-            e = launch_product<false, false, false>(c, o, matrices);
+            e = launch_product<false, false, false>(c, o, matrices, true);
             if (e != hipSuccess) return e;
             const bool last = k + 1 == steps;
             most = odd_max(p, q, r, most) * 1.001;
@@ -358,8 +350,8 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             o.C = s.C;
             o.count = s.count;
             o.first = (int32_t)b0;
-            if (last) e = tall ? launch_product<false, false, true>(c, o, matrices) : launch_product<false, true, true>(c, o, matrices);
-            else e = tall ? launch_product<false, false, false>(c, o, matrices) : launch_product<false, true, false>(c, o, matrices);
+            if (last) e = tall ? launch_product<false, false, true>(c, o, matrices, false) : launch_product<false, true, true>(c, o, matrices, false);
+            else e = tall ? launch_product<false, false, false>(c, o, matrices, false) : launch_product<false, true, false>(c, o, matrices, false);
             if (e != hipSuccess) return e;
             x_up = (float)out_up;
         }

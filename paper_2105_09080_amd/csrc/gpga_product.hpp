@@ -191,25 +191,102 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
     }
 }
 
-// f(row, column, four columns' values) for every lane's share of a tile's accumulators.
-template <typename S, typename F>
-__device__ __forceinline__ void each_quad(const acc16 (&acc)[S::NI][S::MI], int32_t m0, int32_t n0, F&& f) {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const int32_t row0 = m0 + wave / S::WN * (S::BM / S::WM) + (lane & 31), col0 = n0 + wave % S::WN * (S::BN / S::WN) + (lane >> 5) * 4;
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i)
+// A tile's accumulators by rows: a wavefront leaves 32 rows of its 64 columns at a time in LDS, which the operands no longer need, and
+// every lane takes eight columns of a row from there, so that eight lanes read and write whole lines of memory.  As they come from the
+// matrix unit a lane's columns are 16 bytes apart in 32 rows.
+template <typename S>
+struct Dump {
+    static constexpr int kCols = S::NI * 32, kRow = kCols + 4, kWaveFloats = 32 * kRow;  // rows begin 4 banks apart
+    static_assert(S::NI == 2 && S::Waves * kWaveFloats * 4 <= 2 * S::Stage, "dump");
+    float* own;
+    __device__ __forceinline__ explicit Dump(char* lds) : own(reinterpret_cast<float*>(lds) + threadIdx.x / kWave * kWaveFloats) {}
+    __device__ __forceinline__ void put(const acc16 (&acc)[S::NI][S::MI], int i) const {
+        const int lane = threadIdx.x & (kWave - 1);
+        float* row = own + (lane & 31) * kRow + (lane >> 5) * 4;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int j = 0; j < S::NI; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                f(row0 + i * 32, col0 + j * 32 + q * 8, v4f{acc[j][i][q * 4], acc[j][i][q * 4 + 1], acc[j][i][q * 4 + 2], acc[j][i][q * 4 + 3]});
+                *reinterpret_cast<v4f*>(row + j * 32 + q * 8) =
+                    v4f{acc[j][i][q * 4], acc[j][i][q * 4 + 1], acc[j][i][q * 4 + 2], acc[j][i][q * 4 + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    __device__ __forceinline__ void get(int row, int col, float* v) const {
+        const v4f a = *reinterpret_cast<const v4f*>(own + row * kRow + col), b = *reinterpret_cast<const v4f*>(own + row * kRow + col + 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
+    }
+};
+template <typename S>
+__device__ __forceinline__ int32_t wave_row(int32_t m0) {
+    return m0 + (int32_t)(threadIdx.x / kWave) / S::WN * (S::BM / S::WM);
+}
+template <typename S>
+__device__ __forceinline__ int32_t wave_col(int32_t n0) {
+    return n0 + (int32_t)(threadIdx.x / kWave) % S::WN * (S::BN / S::WN);
+}
+
+// f(row, column, eight columns' values) for a tile; with `mirror` then f(column, row, eight rows' values) too.
+template <typename S, typename F>
+__device__ __forceinline__ void each_octet(const acc16 (&acc)[S::NI][S::MI], char* lds, int32_t m0, int32_t n0, bool mirror, F&& f) {
+    const Dump<S> dump(lds);
+    const int lane = threadIdx.x & (kWave - 1);
+    const int32_t row0 = wave_row<S>(m0), col0 = wave_col<S>(n0);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+        dump.put(acc, i);
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int row = it * 8 + lane / 8, col = lane % 8 * 8;
+            float v[8];
+            dump.get(row, col, v);
+            f(row0 + i * 32 + row, col0 + col, v);
+        }
+        if (mirror) {
+#pragma unroll
+            for (int it = 0; it < 4; ++it) {
+                float v[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = dump.own[(it * 8 + k) * Dump<S>::kRow + lane];
+                f(col0 + lane, row0 + i * 32 + it * 8, v);
+            }
+        }
+    }
+}
+
+// f(row, column, eight values of the wavefront's first 32 columns, the same of its second 32), column counted in the first.
+template <typename S, typename F>
+__device__ __forceinline__ void each_octet_pair(const acc16 (&acc)[S::NI][S::MI], char* lds, int32_t m0, F&& f) {
+    const Dump<S> dump(lds);
+    const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+        dump.put(acc, i);
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+            const int row = it * 16 + lane / 4, col = lane % 4 * 8;
+            float a[8], b[8];
+            dump.get(row, col, a);
+            dump.get(row, col + 32, b);
+            f(wave_row<S>(m0) + i * 32 + row, col, a, b);
+        }
+    }
 }
 
 // Which tile a workgroup takes: the tiles of a batch entry stay on one XCD as far as they go (workgroups go round the eight by their
 // number), and there in groups of kGroup rows of tiles, so that the ones under way together share rows and columns in its L2.
 struct TileGrid {
-    int32_t tm, tn;    // tiles of a batch entry
+    int32_t tm, tn;    // tiles of a batch entry; tn = 0: only those on and below the diagonal of a square of tm
     uint32_t total;    // of all
+    __host__ void set(int32_t rows, int32_t cols, int32_t side, int32_t batch, bool lower) {
+        tm = (rows + side - 1) / side;
+        tn = lower ? 0 : (cols + side - 1) / side;
+        total = (uint32_t)one() * (uint32_t)batch;
+    }
+    __host__ __device__ int32_t one() const { return tn ? tm * tn : tm * (tm + 1) / 2; }
     static constexpr uint32_t kXcds = 8;
     static constexpr int32_t kGroup = 8;
     __host__ uint32_t blocks() const { return (total + kXcds - 1) / kXcds * kXcds; }
@@ -217,15 +294,37 @@ struct TileGrid {
     __device__ __forceinline__ bool at(uint32_t block, int32_t* batch, int32_t* i, int32_t* j) const {
         const uint32_t per = (total + kXcds - 1) / kXcds, id = block % kXcds * per + block / kXcds;
         if (id >= total) return false;
-        const uint32_t one = (uint32_t)(tm * tn);
-        *batch = (int32_t)(id / one);
-        const int32_t in = (int32_t)(id % one), group = in / (kGroup * tn), first = group * kGroup, h = min(kGroup, tm - first),
+        const uint32_t each = (uint32_t)one();
+        *batch = (int32_t)(id / each);
+        const int32_t in = (int32_t)(id % each);
+        if (tn == 0) {  // row i begins at i (i + 1) / 2
+            int32_t row = (int32_t)((sqrtf(8.f * (float)in + 1.f) - 1.f) * 0.5f);
+            while (row * (row + 1) / 2 > in) --row;
+            while ((row + 1) * (row + 2) / 2 <= in) ++row;
+            *i = row;
+            *j = in - row * (row + 1) / 2;
+            return true;
+        }
+        const int32_t group = in / (kGroup * tn), first = group * kGroup, h = min(kGroup, tm - first),
                       rest = in - group * kGroup * tn;
         *i = first + rest % h;
         *j = rest / h;
         return true;
     }
 };
+
+// Whether tiles of 256 x 256 (one workgroup of 8 wavefronts a compute unit) take less time than tiles of 128 x 128 (two of 4), whose ends
+// are hidden behind the other's products.  In units of a term of 256 x 256: a round of wide tiles K + 900, of narrow ones, half as large,
+// (1.2 K + 400) / 2.
+inline bool wide_tiles(int num_cus, int64_t rows, int64_t cols, int64_t K, int64_t batch, bool lower) {
+    auto tiles = [&](int64_t side) {
+        const int64_t i = (rows + side - 1) / side, j = (cols + side - 1) / side;
+        return (lower ? i * (i + 1) / 2 : i * j) * batch;
+    };
+    const double wide = (double)((tiles(256) + num_cus - 1) / num_cus) * (double)(K + 900);
+    const double narrow = (double)((tiles(128) + 2 * num_cus - 1) / (2 * num_cus)) * (0.6 * (double)K + 200);
+    return wide < narrow;
+}
 
 // ---- values as halves ---------------------------------------------------------------------------------------------------
 // The power of two that brings values of at most `bound` below 2^15, and its inverse.  Where there is nothing but zeros the inverse is 0:
@@ -241,15 +340,15 @@ __device__ __forceinline__ Scale scale_for(float bound) {
     return {__uint_as_float((uint32_t)(127 + up) << 23), __uint_as_float((uint32_t)(127 - up) << 23)};
 }
 
-// v as one half or the sum of two.
-__device__ __forceinline__ void split4(v4f v, half4* hi, half4* lo) {
-    *hi = __builtin_convertvector(v, half4);
-    *lo = __builtin_convertvector(v - __builtin_convertvector(*hi, v4f), half4);
-}
+// v as one half or the sum of two, eight at a time.
 template <int Planes>
-__device__ __forceinline__ void store_planes(half_t* to, int64_t plane, v4f v) {
-    half4 hi, lo;
-    split4(v, &hi, &lo);
-    *reinterpret_cast<half4*>(to) = hi;
-    if constexpr (Planes == 2) *reinterpret_cast<half4*>(to + plane) = lo;
+__device__ __forceinline__ void store_planes(half_t* to, int64_t plane, const float* v) {
+    half8 hi, lo;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        hi[k] = (half_t)v[k];
+        lo[k] = (half_t)(v[k] - (float)hi[k]);
+    }
+    *reinterpret_cast<half8*>(to) = hi;
+    if constexpr (Planes == 2) *reinterpret_cast<half8*>(to + plane) = lo;
 }
