@@ -20,23 +20,36 @@ constexpr int kPackRows = kThreads / kWave;  // a wavefront a row
 
 // ---- activation functions -------------------------------------------------------------------------------------------------
 // silu(v) = v s, s = 1 / (1 + exp(-v)); silu' = s + v s (1 - s).  gelu(v) = v P, P = (1 + erf(v / sqrt 2)) / 2; gelu' = P + v exp(-v^2/2) /
-// sqrt(2 pi).  |act(v)| <= |v|, |act'| <= 1.13.
-template <int Act>
-__device__ __forceinline__ float act_value(float v) {
-    if constexpr (Act == GPGA_SILU) return v / (1.f + __expf(-v));
-    return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
-}
+// sqrt(2 pi).  |act(v)| <= |v|, |act'| <= 1.13.  erf by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: with t = 1 /
+// (1 + 0.3275911 z), z >= 0, 1 - erf(z) = (a1 t + .. + a5 t^5) exp(-z^2) to 1.5e-7, what a rounding of 1 + erf to fp32 costs, and its
+// exponential is the slope's; the library's erff took a third of the product's time (8 x 8192 tokens, F = 4096).
 template <int Act>
 __device__ __forceinline__ void act_both(float v, float* value, float* slope) {
     if constexpr (Act == GPGA_SILU) {
-        const float e = __expf(-v), s = 1.f / (1.f + e);
+        const float e = __expf(-v), s = __builtin_amdgcn_rcpf(1.f + e);
         *value = v * s;
         *slope = s + *value * (e > 1e30f ? 1.f : e * s);
     } else {
-        const float p = 0.5f * (1.f + erff(v * 0.70710678118654752f));
+        const float t = __builtin_amdgcn_rcpf(1.f + 0.231641888f * fabsf(v)), e = __expf(-0.5f * v * v);  // 0.3275911 / sqrt 2
+        const float tail = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+        const float p = v < 0.f ? tail : 1.f - tail;
         *value = v * p;
-        *slope = p + v * (__expf(-0.5f * v * v) * 0.39894228040143268f);
+        *slope = p + v * (e * 0.39894228040143268f);
     }
+}
+template <int Act>
+__device__ __forceinline__ float act_value(float v) {
+    float value, slope;
+    act_both<Act>(v, &value, &slope);
+    return value;
+}
+
+__device__ __forceinline__ float block_max(float m) {
+    __shared__ float s[kPackRows];
+    m = wave_all<kWave>(m, max_nan);
+    if ((threadIdx.x & (kWave - 1)) == 0) s[threadIdx.x / kWave] = m;
+    __syncthreads();
+    return max_nan(max_nan(s[0], s[1]), max_nan(s[2], s[3]));
 }
 
 // ---- rows as halves -------------------------------------------------------------------------------------------------------
@@ -51,11 +64,11 @@ struct PackMatrices {
     half_t *gu, *wd;              // planes: (n, 2 F', D') and (n, D', F'), ' padded
     int64_t gu_plane, wd_plane;
     float *gu_inv, *wd_inv;       // n x 2F', n x D'
-    float* norms;                 // n x 2F' row norms of gate and up, or NULL
+    float* norms;                 // n x gu_blocks: largest norm of a workgroup's rows of gate and up, or NULL
     const float* node_max;        // largest |gate|, |up| of a node in kMaxParts parts, or NULL: scales by row
     uint32_t gu_blocks, per_node, first_block;
 };
-constexpr int kMaxParts = 64;
+constexpr int kMaxParts = 256;
 
 template <typename E, int PGU, int PD>
 __global__ __launch_bounds__(kThreads) void k_ff_pack_matrices(PackMatrices a) {
@@ -69,12 +82,16 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_matrices(PackMatrices a) {
         Scale s = {0.f, 0.f};
         if (a.node_max) {
             const float* part = a.node_max + (int64_t)node * kMaxParts;
-            s = scale_for(wave_all<kWave>(part[threadIdx.x & (kWave - 1)], max_nan));
+            const int lane = threadIdx.x & (kWave - 1);
+            s = scale_for(wave_all<kWave>(max_nan(max_nan(part[lane], part[64 + lane]), max_nan(part[128 + lane], part[192 + lane])), max_nan));
         }
         const RowStat r = pack_row<E, PGU>(from, f < a.F ? a.D : 0, D2, nullptr, a.node_max ? &s : nullptr, to, a.gu_plane);
         if ((threadIdx.x & (kWave - 1)) == 0) {
             a.gu_inv[(int64_t)node * 2 * F2 + row] = r.down;
-            if (a.norms) a.norms[(int64_t)node * 2 * F2 + row] = r.norm * r.down;
+        }
+        if (a.norms) {
+            const float most = block_max(r.norm * r.down);
+            if (threadIdx.x == 0) a.norms[(int64_t)node * a.gu_blocks + in] = most;
         }
     } else {
         const int32_t row = (in - (int32_t)a.gu_blocks) * kPackRows + wave;
@@ -86,20 +103,24 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_matrices(PackMatrices a) {
 
 // Largest |gate| and |up| of a node, in kMaxParts parts.
 __global__ __launch_bounds__(kThreads) void k_ff_max(const float* gate, const float* up, int64_t ldx, int64_t count, float* part, uint32_t first) {
+    typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
     const uint32_t block = first + blockIdx.x, node = block / kMaxParts, p = block % kMaxParts;
+    const float* from[2] = {gate + (int64_t)node * ldx, up + (int64_t)node * ldx};
     float m = 0.f;
-    for (int64_t e = (int64_t)p * kThreads + threadIdx.x; e < count; e += (int64_t)kMaxParts * kThreads) {
-        m = max_nan(m, fabsf(gate[(int64_t)node * ldx + e]));
-        m = max_nan(m, fabsf(up[(int64_t)node * ldx + e]));
-    }
-    m = wave_all<kWave>(m, max_nan);
-    __shared__ float s[kPackRows];
-    if ((threadIdx.x & (kWave - 1)) == 0) s[threadIdx.x / kWave] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) part[block] = max_nan(max_nan(s[0], s[1]), max_nan(s[2], s[3]));
+    const int64_t fours = count / 4, at = (int64_t)p * kThreads + threadIdx.x;
+    for (int64_t e = at; e < fours; e += (int64_t)kMaxParts * kThreads)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const vec v = *(reinterpret_cast<const vec*>(from[k]) + e);
+            m = max_nan(m, max_nan(max_nan(fabsf(v[0]), fabsf(v[1])), max_nan(fabsf(v[2]), fabsf(v[3]))));
+        }
+    if (at < count % 4) m = max_nan(m, max_nan(fabsf(from[0][fours * 4 + at]), fabsf(from[1][fours * 4 + at])));
+    m = block_max(m);
+    if (threadIdx.x == 0) part[block] = m;
 }
 
-// Rows of activations of a chunk of tokens, a wavefront a row.
+// Rows of activations of a chunk of tokens: kRowsEach for each of a workgroup's wavefronts.
+constexpr int kRowsEach = 4;
 struct PackRows {
     const void* src;
     int64_t ld, node;          // elements between rows, between nodes
@@ -108,37 +129,29 @@ struct PackRows {
     int64_t plane;
     float* inv;                // n x rows'
     uint32_t per_node, first_block;
-    __device__ __forceinline__ bool at(int32_t* node_, int32_t* row, int32_t* row2) const {
-        const uint32_t block = first_block + blockIdx.x;
-        *node_ = (int32_t)(block / per_node);
-        *row = (int32_t)(block % per_node) * kPackRows + threadIdx.x / kWave;
-        *row2 = padded(rows);
-        return true;
-    }
 };
 
 // Forward: x as halves, and the scale of its row of h: |a|, |b| <= |x| max |w|, |h| <= |a| |b|.
 template <typename E, int P>
 __global__ __launch_bounds__(kThreads) void k_ff_pack_x(PackRows a, const float* norms, int32_t norm_count, float* h_up, float* h_inv) {
-    int32_t node, row, rows2;
-    a.at(&node, &row, &rows2);
-    const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1);
+    const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1), rows2 = padded(a.rows);
+    const uint32_t block = a.first_block + blockIdx.x;
+    const int64_t node = block / a.per_node;
     float w = 0.f;
-    for (int32_t f = threadIdx.x; f < norm_count; f += kThreads) w = max_nan(w, norms[(int64_t)node * norm_count + f]);
-    w = wave_all<kWave>(w, max_nan);
-    __shared__ float s_w[kPackRows];
-    if (lane == 0) s_w[threadIdx.x / kWave] = w;
-    __syncthreads();
-    w = max_nan(max_nan(s_w[0], s_w[1]), max_nan(s_w[2], s_w[3]));
-    const typename E::mem* from = static_cast<const typename E::mem*>(a.src) + (int64_t)node * a.node + (int64_t)row * a.ld;
-    const RowStat r = pack_row<E, P>(from, row < a.rows ? a.cols : 0, cols2, nullptr, nullptr, a.dst + ((int64_t)node * rows2 + row) * cols2, a.plane);
-    if (lane == 0) {
-        const int64_t at = (int64_t)node * rows2 + row;
-        const float most = r.norm * r.down * w;
-        const Scale s = scale_for(most * most * 1.0001f);
-        a.inv[at] = r.down;
-        h_up[at] = s.up;
-        h_inv[at] = s.down;
+    for (int32_t f = threadIdx.x; f < norm_count; f += kThreads) w = max_nan(w, norms[node * norm_count + f]);
+    w = block_max(w);
+    for (int k = 0; k < kRowsEach; ++k) {
+        const int32_t row = ((int32_t)(block % a.per_node) * kRowsEach + k) * kPackRows + threadIdx.x / kWave;
+        const int64_t at = node * rows2 + row;
+        const typename E::mem* from = static_cast<const typename E::mem*>(a.src) + node * a.node + (int64_t)row * a.ld;
+        const RowStat r = pack_row<E, P>(from, row < a.rows ? a.cols : 0, cols2, nullptr, nullptr, a.dst + at * cols2, a.plane);
+        if (lane == 0) {
+            const float most = r.norm * r.down * w;
+            const Scale s = scale_for(most * most * 1.0001f);
+            a.inv[at] = r.down;
+            h_up[at] = s.up;
+            h_inv[at] = s.down;
+        }
     }
 }
 
@@ -149,64 +162,76 @@ template <typename E, int P>
 __global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackRows a, const float* wd_inv, const void* x, const void* hidden, int32_t F,
                                                          int64_t hidden_node, float* da_up, float* da_inv, float* h_up, float* h_inv, float* part) {
     typedef typename E::mem M;
-    int32_t node, row, rows2;
-    a.at(&node, &row, &rows2);
-    const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1);
-    const bool real = row < a.rows;
-    const int64_t from = (int64_t)node * a.node + (int64_t)row * a.ld, at = (int64_t)node * rows2 + row;
-    const RowStat r = pack_row<E, P>(static_cast<const M*>(a.src) + from, real ? a.cols : 0, cols2, wd_inv + (int64_t)node * cols2, nullptr,
-                                     a.dst + at * cols2, a.plane);
-    float xm = 0.f, ym = 0.f, am = 0.f, bm = 0.f;
-    if (real) {
-        const M* h = static_cast<const M*>(hidden) + (int64_t)node * hidden_node + (int64_t)row * 2 * F;
-        xm = row_max<E>(static_cast<const M*>(x) + from, a.cols);
-        ym = row_max<E>(static_cast<const M*>(a.src) + from, a.cols);
-        am = row_max<E>(h, F);
-        bm = row_max<E>(h + F, F);
-    }
-    const float dh = r.sum * r.down * 32768.f * 1.0001f;
-    const Scale sa = scale_for(dh * max_nan(1.14f * bm, am)), sh = scale_for(am * bm);
-    if (lane == 0) {
-        a.inv[at] = r.down;
-        da_up[at] = sa.up;
-        da_inv[at] = sa.down;
-        h_up[at] = sh.up;
-        h_inv[at] = sh.down;
+    const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1), rows2 = padded(a.rows);
+    const uint32_t block = a.first_block + blockIdx.x;
+    const int64_t node = block / a.per_node;
+    float px = 0.f, py = 0.f;
+    {
+        const int32_t row = (int32_t)(block % a.per_node) * kPackRows + threadIdx.x / kWave;
+        const bool real = row < a.rows;
+        const int64_t from = node * a.node + (int64_t)row * a.ld, at = node * rows2 + row;
+        float xm = 0.f, ym = 0.f, am = 0.f, bm = 0.f;
+        if (real) {
+            const M* h = static_cast<const M*>(hidden) + node * hidden_node + (int64_t)row * 2 * F;
+            am = row_max<E>(h, F);
+            bm = row_max<E>(h + F, F);
+            xm = row_max<E>(static_cast<const M*>(x) + from, a.cols);
+            ym = row_max<E>(static_cast<const M*>(a.src) + from, a.cols);
+        }
+        const RowStat r = pack_row<E, P>(static_cast<const M*>(a.src) + from, real ? a.cols : 0, cols2, wd_inv + node * cols2, nullptr,
+                                         a.dst + at * cols2, a.plane);
+        const float dh = r.sum * r.down * 32768.f * 1.0001f;
+        const Scale sa = scale_for(dh * max_nan(1.14f * bm, am)), sh = scale_for(am * bm);
+        if (lane == 0) {
+            a.inv[at] = r.down;
+            da_up[at] = sa.up;
+            da_inv[at] = sa.down;
+            h_up[at] = sh.up;
+            h_inv[at] = sh.down;
+        }
+        px = max_nan(px, xm * sa.down);
+        py = max_nan(py, ym * sh.down);
     }
     __shared__ float s[2][kPackRows];
     if (lane == 0) {
-        s[0][threadIdx.x / kWave] = xm * sa.down;
-        s[1][threadIdx.x / kWave] = ym * sh.down;
+        s[0][threadIdx.x / kWave] = px;
+        s[1][threadIdx.x / kWave] = py;
     }
     __syncthreads();
     if (threadIdx.x < 2) {
         const float* q = s[threadIdx.x];
-        part[((int64_t)node * 2 + threadIdx.x) * a.per_node + blockIdx.x + a.first_block - (uint64_t)node * a.per_node] =
-            max_nan(max_nan(q[0], q[1]), max_nan(q[2], q[3]));
+        part[(node * 2 + threadIdx.x) * a.per_node + block % a.per_node] = max_nan(max_nan(q[0], q[1]), max_nan(q[2], q[3]));
     }
 }
 
-// x / up (which = 0) or dy / up (1) of every token as halves with one scale a node.
+// x / up or dy / up of every token as halves with one scale a node, the first or the second half of the workgroups.
+struct PackTokens {
+    PackRows of[2];            // x, dy; inv: one a node
+    const float* row_inv[2];
+    const float* part;
+    uint32_t parts, half, first_block;
+};
 template <typename E, int P>
-__global__ __launch_bounds__(kThreads) void k_ff_pack_tokens(PackRows a, const float* row_inv, const float* dy_inv, const float* part, uint32_t parts,
-                                                             int which, float* node_inv) {
-    int32_t node, row, rows2;
-    a.at(&node, &row, &rows2);
-    const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1);
-    const float* from = part + ((int64_t)node * 2 + which) * parts;
+__global__ __launch_bounds__(kThreads) void k_ff_pack_tokens(PackTokens t) {
+    uint32_t block = t.first_block + blockIdx.x;
+    const int which = block >= t.half;
+    block -= which ? t.half : 0;
+    const PackRows a = t.of[which];
+    const int32_t cols2 = padded(a.cols), rows2 = padded(a.rows);
+    const int64_t node = block / a.per_node;
+    const float* from = t.part + (node * 2 + which) * t.parts;
     float w = 0.f;
-    for (uint32_t p = threadIdx.x; p < parts; p += kThreads) w = max_nan(w, from[p]);
-    w = wave_all<kWave>(w, max_nan);
-    __shared__ float s_w[kPackRows];
-    if (lane == 0) s_w[threadIdx.x / kWave] = w;
-    __syncthreads();
-    const Scale node_scale = scale_for(max_nan(max_nan(s_w[0], s_w[1]), max_nan(s_w[2], s_w[3])));
-    const int64_t at = (int64_t)node * rows2 + row;
-    const float inv = row < a.rows ? row_inv[at] : 0.f;
-    Scale s = {inv * node_scale.up, 0.f};
-    const typename E::mem* src = static_cast<const typename E::mem*>(a.src) + (int64_t)node * a.node + (int64_t)row * a.ld;
-    pack_row<E, P>(src, row < a.rows ? a.cols : 0, cols2, nullptr, &s, a.dst + at * cols2, a.plane);
-    if (row == 0 && lane == 0) node_inv[node] = node_scale.down;
+    for (uint32_t p = threadIdx.x; p < t.parts; p += kThreads) w = max_nan(w, from[p]);
+    const Scale node_scale = scale_for(block_max(w));
+    for (int k = 0; k < kRowsEach; ++k) {
+        const int32_t row = ((int32_t)(block % a.per_node) * kRowsEach + k) * kPackRows + threadIdx.x / kWave;
+        const int64_t at = node * rows2 + row;
+        const float inv = row < a.rows ? t.row_inv[which][at] : 0.f;
+        const Scale s = {inv * node_scale.up, 0.f};
+        const typename E::mem* src = static_cast<const typename E::mem*>(a.src) + node * a.node + (int64_t)row * a.ld;
+        pack_row<E, P>(src, row < a.rows ? a.cols : 0, cols2, nullptr, &s, a.dst + at * cols2, a.plane);
+        if (row == 0 && (threadIdx.x & (kWave - 1)) == 0) a.inv[node] = node_scale.down;
+    }
 }
 
 // ---- products ---------------------------------------------------------------------------------------------------------------
@@ -236,7 +261,7 @@ struct FfProduct {
 
 // h = act(x Wg^T) (x Wu^T): a wavefront's blocks of 32 columns are gate and up of the same 32 f's in turn.
 template <typename S, typename E, int Act, int PH>
-__global__ __launch_bounds__(S::Threads) void k_ff_up(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, 2) void k_ff_up(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     static_assert(S::NI == 2, "gate and up");
     int32_t node, ti, tj;
@@ -272,7 +297,7 @@ __global__ __launch_bounds__(S::Threads) void k_ff_up(FfProduct a) {
 
 // Activations out: rows' scales times columns' scales (col_batch < 0: one a node).
 template <typename S, typename E>
-__global__ __launch_bounds__(S::Threads) void k_ff_rows(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, 2) void k_ff_rows(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t node, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
@@ -293,7 +318,7 @@ __global__ __launch_bounds__(S::Threads) void k_ff_rows(FfProduct a) {
 // dh = dy Wd, and from it and the kept [a | b] the rows of [da | db] and h as halves.  Rows behind the last token are zeros: the
 // products over tokens take them along.
 template <typename S, typename E, int Act, int PA, int PH>
-__global__ __launch_bounds__(S::Threads) void k_ff_down_grad(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, 2) void k_ff_down_grad(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t node, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
@@ -333,7 +358,7 @@ __global__ __launch_bounds__(S::Threads) void k_ff_down_grad(FfProduct a) {
 // Gradients of matrices: rows of the gate's block, then (from F' on) of the up's; or of the down matrix's alone (off1 < 0).
 // G: fp32, narrow where a row of the matrix is.
 template <typename S, typename G>
-__global__ __launch_bounds__(S::Threads) void k_ff_matrix_grad(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, 2) void k_ff_matrix_grad(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t node, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
@@ -368,6 +393,150 @@ __global__ __launch_bounds__(kThreads) void k_ff_zero(float* g, int64_t g_ld, in
     if (e >= count) return;
     float* row = g + (int64_t)node * g_ld;
     row[off0 + e] = row[off1 + e] = row[off2 + e] = 0.f;
+}
+
+// ---- few tokens ---------------------------------------------------------------------------------------------------------------
+// Up to kFewTokens tokens a node: every matrix is read once, as it lies in X, and that is what takes the time.  A wavefront takes 16 rows of
+// a matrix (16 of gate and the same 16 of up), 64 columns at a time, as bf16 pieces made in registers, which need no scale: three of them
+// hold fp32, two go with bf16 activations.  The wavefronts of a workgroup share a row's columns and add their sums in LDS.
+// A lane holds 16 neighbouring columns of a row, 64 bytes, four lanes a row; which of a matrix instruction's k's they are does not
+// matter as long as both operands agree.
+constexpr int32_t kFewTokens = 64;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Columns c .. c+15 of a row of `cols`, c a multiple of 16; zeros behind the end.
+template <typename E>
+__device__ __forceinline__ void read16(const typename E::mem* row, int32_t c, int32_t cols, float* v) {
+    typedef typename E::mem M;
+    if (c + 16 <= cols) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) piece_read<kOct, Elem<M, false>>(row, c + 8 * k, c + 16, v + 8 * k);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = c + k < cols ? E::get(row[c + k]) : 0.f;
+    }
+}
+// 16 values as P pieces, eight a matrix instruction.
+template <int P>
+__device__ __forceinline__ void pieces16(const float* v, bf16x8 (&out)[P][2]) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        float r = v[k];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const __bf16 b = (__bf16)r;
+            out[p][k / 8][k % 8] = b;
+            if (p + 1 < P) r -= (float)b;
+        }
+    }
+}
+
+struct FewArgs {
+    const void* x;             // activations, or h
+    int64_t x_ld, x_node;
+    const float* w[2];         // gate and up, or down
+    int64_t ldx;
+    int32_t T, K, rows;        // columns and rows of a matrix
+    uint32_t per_node, first_block;
+    void* hidden;              // up: n * T rows of 2 F, or NULL
+    float* h;                  // up: n * T rows of F in fp32
+    void* y;                   // down
+    int64_t ld;
+};
+
+// EX: type of the operand that is read, E: of the result; Mats = 2: gate and up, 1: down.  NB: blocks of 16 tokens.
+template <typename EX, typename E, int Mats, int Act, int PW, int PX, int NB, int Waves>
+__global__ __launch_bounds__(Waves * kWave) void k_ff_few(FewArgs a) {
+    const uint32_t block = a.first_block + blockIdx.x;
+    const int64_t node = block / a.per_node;
+    const int32_t row0 = (int32_t)(block % a.per_node) * 16, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int32_t row = min(row0 + (lane & 15), a.rows - 1), inner = (lane >> 4) * 16;
+    const float* w[Mats];
+#pragma unroll
+    for (int m = 0; m < Mats; ++m) w[m] = a.w[m] + node * a.ldx + (int64_t)row * a.K;
+    const typename EX::mem* x[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) x[b] = static_cast<const typename EX::mem*>(a.x) + node * a.x_node + (int64_t)min(b * 16 + (lane & 15), a.T - 1) * a.x_ld;
+    v4f acc[Mats][NB];
+#pragma unroll
+    for (int m = 0; m < Mats; ++m)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[m][b] = v4f{0.f, 0.f, 0.f, 0.f};
+    auto chunk = [&](const float (&vw)[Mats][16], int32_t c) {
+        bf16x8 pw[Mats][PW][2];
+#pragma unroll
+        for (int m = 0; m < Mats; ++m) pieces16<PW>(vw[m], pw[m]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            float v[16];
+            bf16x8 px[PX][2];
+            read16<EX>(x[b], c, a.K, v);
+            pieces16<PX>(v, px);
+#pragma unroll
+            for (int i = 0; i < PW; ++i)
+#pragma unroll
+                for (int j = 0; j < PX && i + j < PW; ++j)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int m = 0; m < Mats; ++m)
+                            acc[m][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw[m][i][half], px[j][half], acc[m][b], 0, 0, 0);
+        }
+    };
+    // two chunks of the matrices under way
+    const int32_t chunks = (a.K + 63) / 64;
+    float now[Mats][16], next[Mats][16];
+    int32_t k = wave;
+    if (k < chunks) {
+#pragma unroll
+        for (int m = 0; m < Mats; ++m) read16<ElemF32>(w[m], k * 64 + inner, a.K, now[m]);
+    }
+    for (; k < chunks; k += Waves) {
+        const int32_t after = k + Waves;
+        if (after < chunks) {
+#pragma unroll
+            for (int m = 0; m < Mats; ++m) read16<ElemF32>(w[m], after * 64 + inner, a.K, next[m]);
+        }
+        chunk(now, k * 64 + inner);
+#pragma unroll
+        for (int m = 0; m < Mats; ++m)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) now[m][j] = next[m][j];
+    }
+    __shared__ v4f s[Waves][Mats][NB][kWave];
+#pragma unroll
+    for (int m = 0; m < Mats; ++m)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[wave][m][b][lane] = acc[m][b];
+    __syncthreads();
+    // lane l: token l % 16, rows 4 (l / 16) .. + 3
+    for (int b = wave; b < NB; b += Waves) {
+        v4f sum[Mats];
+#pragma unroll
+        for (int m = 0; m < Mats; ++m) {
+            sum[m] = s[0][m][b][lane];
+#pragma unroll
+            for (int v = 1; v < Waves; ++v) sum[m] += s[v][m][b][lane];
+        }
+        const int32_t t = b * 16 + (lane & 15), r = row0 + (lane >> 4) * 4;
+        if (t >= a.T) continue;
+        const int64_t token = node * a.T + t;
+        typedef typename E::mem M;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (r + j >= a.rows) continue;
+            if constexpr (Mats == 2) {
+                a.h[token * a.rows + r + j] = act_value<Act>(sum[0][j]) * sum[1][j];
+                if (a.hidden) {
+                    M* hid = static_cast<M*>(a.hidden) + token * 2 * a.rows + r + j;
+                    hid[0] = E::put(sum[0][j]);
+                    hid[a.rows] = E::put(sum[1][j]);
+                }
+            } else {
+                static_cast<M*>(a.y)[token * a.ld + r + j] = E::put(sum[0][j]);
+            }
+        }
+    }
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------
@@ -442,19 +611,22 @@ FfScratch carve_ff(const FfShape& s, bool grad, char* base, size_t* bytes) {
 
 Operand rows_operand(const half_t* p, int64_t n, int32_t rows, int32_t cols) { return {p, n * rows * cols, (int64_t)rows * cols, cols, rows}; }
 
-// Tiles of 256 x 256 (8 wavefronts) or of 128 x 128 (4).
-template <typename F>
-hipError_t launch_product(const gpga_ctx* c, FfProduct& a, int32_t rows, int32_t cols, bool wide, F&& f) {
-    a.grid.set(rows, cols, wide ? 256 : 128, c->n, false);
-    return launch_blocks(a.grid.blocks(), wide ? 512 : 256, [&](uint32_t first, dim3 grid) {
-        a.first_block = first;
-        f(grid);
-    });
+// f(tile, grid) on the tiles that suit rows x cols with K terms.
+template <int PA, int PB, bool CA, bool CB, typename F>
+hipError_t launch_product(const gpga_ctx* c, FfProduct& a, int32_t rows, int32_t cols, F&& f) {
+    const int side = tile_side(c->num_cus, PA + PB, rows, cols, a.K, c->n, false);
+    a.grid.set(rows, cols, side, c->n, false);
+    auto launch = [&](auto tile) {
+        typedef decltype(tile) S;
+        return launch_blocks(a.grid.blocks(), S::Threads, [&](uint32_t first, dim3 grid) {
+            a.first_block = first;
+            f(tile, grid);
+        });
+    };
+    if (side == 256) return launch(Tile256<PA, PB, CA, CB>());
+    if (side == 128) return launch(Tile128<PA, PB, CA, CB>());
+    return launch(Tile64<PA, PB, CA, CB>());
 }
-template <int PA, int PB, bool CA, bool CB>
-using Wide = Tile<256, 256, 2, 4, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
-template <int PA, int PB, bool CA, bool CB>
-using Narrow = Tile<128, 128, 2, 2, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
 
 // f(a constant) for the kind of activation.
 template <int V>
@@ -504,9 +676,54 @@ hipError_t launch_pack_matrices(const gpga_ctx* c, const FfShape& s, PackMatrice
         if (e_ != hipSuccess) return e_;         \
     } while (0)
 
+template <typename E, int NB>
+hipError_t few(const gpga_ctx* c, const FfShape& s, const void* x, void* hidden, void* y, float* h) {
+    typedef typename E::mem M;
+    constexpr int PW = __is_same(M, __bf16) ? 2 : 3, PX = sizeof(M) == 4 ? 3 : __is_same(M, __bf16) ? 1 : 2, PH = sizeof(M) == 4 ? 3 : 2;
+    FewArgs a = {};
+    a.x = x;
+    a.x_ld = s.ld;
+    a.x_node = (int64_t)s.T * s.ld;
+    a.w[0] = c->x + s.gate_off;
+    a.w[1] = c->x + s.up_off;
+    a.ldx = c->ld;
+    a.T = s.T;
+    a.K = s.D;
+    a.rows = s.F;
+    a.per_node = (uint32_t)((s.F + 15) / 16);
+    a.hidden = hidden;
+    a.h = h;
+    GPGA_LAUNCH(launch_blocks((uint64_t)a.per_node * s.n, 4 * kWave, [&](uint32_t first, dim3 grid) {
+        a.first_block = first;
+        with_act(s.act, [&](auto act) {
+            k_ff_few<E, E, 2, decltype(act)::value, PW, PX, NB, 4><<<grid, dim3(4 * kWave), 0, c->stream>>>(a);
+        });
+    }));
+    a.x = h;
+    a.x_ld = s.F;
+    a.x_node = (int64_t)s.T * s.F;
+    a.w[0] = c->x + s.down_off;
+    a.K = s.F;
+    a.rows = s.D;
+    a.per_node = (uint32_t)((s.D + 15) / 16);
+    a.y = y;
+    a.ld = s.ld;
+    return launch_blocks((uint64_t)a.per_node * s.n, 8 * kWave, [&](uint32_t first, dim3 grid) {
+        a.first_block = first;
+        k_ff_few<ElemF32, E, 1, GPGA_SILU, PW, PH, NB, 8><<<grid, dim3(8 * kWave), 0, c->stream>>>(a);
+    });
+}
+
 template <typename E>
 hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hidden, void* y, char* scratch) {
     typedef typename E::mem M;
+    if (s.T <= kFewTokens) {
+        typedef Elem<M, false> Wide;  // 16 columns at a time, or one by one
+        float* h = reinterpret_cast<float*>(scratch);
+        if (s.T <= 16) return few<Wide, 1>(c, s, x, hidden, y, h);
+        if (s.T <= 32) return few<Wide, 2>(c, s, x, hidden, y, h);
+        return few<Wide, 4>(c, s, x, hidden, y, h);
+    }
     constexpr bool kF32 = sizeof(M) == 4, kBf16 = __is_same(M, __bf16);
     constexpr int PX = kF32 ? 2 : 1, PW = kBf16 ? 1 : 2, PH = PX;
     size_t bytes;
@@ -516,10 +733,10 @@ hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hid
     for (int32_t t0 = 0; t0 < s.T; t0 += w.chunk) {
         const int32_t T = s.T - t0 < w.chunk ? s.T - t0 : w.chunk, T2 = padded(T);
         PackRows p = {static_cast<const M*>(x) + (int64_t)t0 * s.ld, s.ld, (int64_t)s.T * s.ld, T, s.D, w.x, (int64_t)s.n * T2 * D2, w.x_inv,
-                      (uint32_t)(T2 / kPackRows), 0};
+                      (uint32_t)(T2 / (kPackRows * kRowsEach)), 0};
         GPGA_LAUNCH(launch_blocks((uint64_t)p.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
             p.first_block = first;
-            k_ff_pack_x<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(p, w.norms, 2 * F2, w.h_up, w.h_inv);
+            k_ff_pack_x<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(p, w.norms, 2 * F2 / kPackRows, w.h_up, w.h_inv);
         }));
         FfProduct a = {};
         a.A = rows_operand(w.x, s.n, T2, D2);
@@ -534,14 +751,12 @@ hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hid
         a.h = w.h;
         a.h_plane = (int64_t)s.n * T2 * F2;
         a.h_up = w.h_up;
-        const bool wide = wide_tiles(c->num_cus, T, 2 * F2, D2, s.n, false);
-        GPGA_LAUNCH(launch_product(c, a, T, 2 * F2, wide, [&](dim3 grid) {
+        GPGA_LAUNCH((launch_product<PX, PW, false, false>(c, a, T, 2 * F2, [&](auto tile, dim3 grid) {
             with_act(s.act, [&](auto act) {
-                constexpr int kAct = decltype(act)::value;
-                if (wide) k_ff_up<Wide<PX, PW, false, false>, E, kAct, PH><<<grid, dim3(512), 0, c->stream>>>(a);
-                else k_ff_up<Narrow<PX, PW, false, false>, E, kAct, PH><<<grid, dim3(256), 0, c->stream>>>(a);
+                typedef decltype(tile) S;
+                k_ff_up<S, E, decltype(act)::value, PH><<<grid, dim3(S::Threads), 0, c->stream>>>(a);
             });
-        }));
+        })));
         FfProduct b = {};
         b.A = rows_operand(w.h, s.n, T2, F2);
         b.B = rows_operand(w.wd, s.n, D2, F2);
@@ -555,11 +770,10 @@ hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hid
         b.out = static_cast<M*>(y) + (int64_t)t0 * s.ld;
         b.out_ld = s.ld;
         b.out_node = (int64_t)s.T * s.ld;
-        const bool wide2 = wide_tiles(c->num_cus, T, D2, F2, s.n, false);
-        GPGA_LAUNCH(launch_product(c, b, T, D2, wide2, [&](dim3 grid) {
-            if (wide2) k_ff_rows<Wide<PH, PW, false, false>, E><<<grid, dim3(512), 0, c->stream>>>(b);
-            else k_ff_rows<Narrow<PH, PW, false, false>, E><<<grid, dim3(256), 0, c->stream>>>(b);
-        }));
+        GPGA_LAUNCH((launch_product<PH, PW, false, false>(c, b, T, D2, [&](auto tile, dim3 grid) {
+            typedef decltype(tile) S;
+            k_ff_rows<S, E><<<grid, dim3(S::Threads), 0, c->stream>>>(b);
+        })));
     }
     return hipSuccess;
 }
@@ -588,15 +802,17 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
             k_ff_pack_dy<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(p, w.wd_inv, static_cast<const M*>(x) + skip, hid, s.F, hidden_node, w.da_up,
                                                                         w.da_inv, w.h_up, w.h_inv, w.part);
         }));
-        for (int which = 0; which < 2; ++which) {
-            p.src = static_cast<const M*>(which ? dy : x) + skip;
-            p.dst = which ? w.tok_y : w.tok_x;
-            GPGA_LAUNCH(launch_blocks((uint64_t)p.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
-                p.first_block = first;
-                k_ff_pack_tokens<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(p, which ? w.h_inv : w.da_inv, w.x_inv, w.part, p.per_node, which,
-                                                                               w.node_inv + which * n);
-            }));
-        }
+        p.per_node /= kRowsEach;
+        PackTokens tokens = {{p, p}, {w.da_inv, w.h_inv}, w.part, (uint32_t)(T2 / kPackRows), p.per_node * (uint32_t)s.n, 0};
+        tokens.of[0].src = static_cast<const M*>(x) + skip;
+        tokens.of[0].dst = w.tok_x;
+        tokens.of[0].inv = w.node_inv;
+        tokens.of[1].dst = w.tok_y;
+        tokens.of[1].inv = w.node_inv + n;
+        GPGA_LAUNCH(launch_blocks((uint64_t)2 * tokens.half, kThreads, [&](uint32_t first, dim3 grid) {
+            tokens.first_block = first;
+            k_ff_pack_tokens<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(tokens);
+        }));
         FfProduct a = {};
         a.A = rows_operand(w.dy, n, T2, D2);
         a.B = rows_operand(w.wd, n, D2, F2);
@@ -612,14 +828,12 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         a.da = w.da;
         a.da_plane = n * T2 * 2 * F2;
         a.da_up = w.da_up;
-        const bool wide = wide_tiles(c->num_cus, T2, F2, D2, s.n, false);
-        GPGA_LAUNCH(launch_product(c, a, T2, F2, wide, [&](dim3 grid) {
+        GPGA_LAUNCH((launch_product<PX, 2, false, true>(c, a, T2, F2, [&](auto tile, dim3 grid) {
             with_act(s.act, [&](auto act) {
-                constexpr int kAct = decltype(act)::value;
-                if (wide) k_ff_down_grad<Wide<PX, 2, false, true>, E, kAct, 2, 2><<<grid, dim3(512), 0, c->stream>>>(a);
-                else k_ff_down_grad<Narrow<PX, 2, false, true>, E, kAct, 2, 2><<<grid, dim3(256), 0, c->stream>>>(a);
+                typedef decltype(tile) S;
+                k_ff_down_grad<S, E, decltype(act)::value, 2, 2><<<grid, dim3(S::Threads), 0, c->stream>>>(a);
             });
-        }));
+        })));
         FfProduct b = {};
         b.A = rows_operand(w.da, n, T2, 2 * F2);
         b.B = rows_operand(w.gu, n, 2 * F2, D2);
@@ -633,11 +847,10 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         b.out = static_cast<M*>(dx) + skip;
         b.out_ld = s.ld;
         b.out_node = (int64_t)s.T * s.ld;
-        const bool wide2 = wide_tiles(c->num_cus, T, D2, 2 * F2, s.n, false);
-        GPGA_LAUNCH(launch_product(c, b, T, D2, wide2, [&](dim3 grid) {
-            if (wide2) k_ff_rows<Wide<PDX, PGU, false, true>, E><<<grid, dim3(512), 0, c->stream>>>(b);
-            else k_ff_rows<Narrow<PDX, PGU, false, true>, E><<<grid, dim3(256), 0, c->stream>>>(b);
-        }));
+        GPGA_LAUNCH((launch_product<PDX, PGU, false, true>(c, b, T, D2, [&](auto tile, dim3 grid) {
+            typedef decltype(tile) S;
+            k_ff_rows<S, E><<<grid, dim3(S::Threads), 0, c->stream>>>(b);
+        })));
         FfProduct g = {};
         g.A = rows_operand(w.da, n, T2, 2 * F2);
         g.B = rows_operand(w.tok_x, n, T2, D2);
@@ -650,11 +863,10 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         g.off0 = s.gate_off;
         g.off1 = s.up_off;
         g.accumulate = accumulate || t0 > 0;
-        const bool wide3 = wide_tiles(c->num_cus, 2 * F2, D2, T2, s.n, false);
-        GPGA_LAUNCH(launch_product(c, g, 2 * F2, D2, wide3, [&](dim3 grid) {
-            if (wide3) k_ff_matrix_grad<Wide<2, PX, true, true>, Elem<float, E::kNarrow>><<<grid, dim3(512), 0, c->stream>>>(g);
-            else k_ff_matrix_grad<Narrow<2, PX, true, true>, Elem<float, E::kNarrow>><<<grid, dim3(256), 0, c->stream>>>(g);
-        }));
+        GPGA_LAUNCH((launch_product<2, PX, true, true>(c, g, 2 * F2, D2, [&](auto tile, dim3 grid) {
+            typedef decltype(tile) S;
+            k_ff_matrix_grad<S, Elem<float, E::kNarrow>><<<grid, dim3(S::Threads), 0, c->stream>>>(g);
+        })));
         g.A = rows_operand(w.tok_y, n, T2, D2);
         g.B = rows_operand(w.h, n, T2, F2);
         g.M = s.D;
@@ -662,11 +874,10 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         g.row_inv = w.node_inv + n;
         g.off0 = s.down_off;
         g.off1 = -1;
-        const bool wide4 = wide_tiles(c->num_cus, D2, F2, T2, s.n, false);
-        GPGA_LAUNCH(launch_product(c, g, D2, F2, wide4, [&](dim3 grid) {
-            if (wide4) k_ff_matrix_grad<Wide<PX, 2, true, true>, Elem<float, E::kNarrow>><<<grid, dim3(512), 0, c->stream>>>(g);
-            else k_ff_matrix_grad<Narrow<PX, 2, true, true>, Elem<float, E::kNarrow>><<<grid, dim3(256), 0, c->stream>>>(g);
-        }));
+        GPGA_LAUNCH((launch_product<PX, 2, true, true>(c, g, D2, F2, [&](auto tile, dim3 grid) {
+            typedef decltype(tile) S;
+            k_ff_matrix_grad<S, Elem<float, E::kNarrow>><<<grid, dim3(S::Threads), 0, c->stream>>>(g);
+        })));
     }
     return hipSuccess;
 }
@@ -674,9 +885,11 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
 }  // namespace
 
 size_t gated_ff_scratch(const FfShape& s, bool grad) {
+    if (s.T == 0) return 0;
+    if (!grad && s.T <= kFewTokens) return (size_t)s.n * s.T * s.F * sizeof(float);
     size_t bytes;
     carve_ff(s, grad, nullptr, &bytes);
-    return s.T ? bytes : 0;
+    return bytes;
 }
 
 hipError_t launch_gated_ff(const gpga_ctx* c, const FfShape& s, const void* x, void* hidden, void* y, void* scratch) {

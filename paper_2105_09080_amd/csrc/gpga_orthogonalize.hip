@@ -38,20 +38,34 @@ __device__ __forceinline__ float* block_of(float* base, int64_t ld, int32_t b, i
 
 // v <- mu v + g and the sum of squares of u = g + mu v, v or g, in fp64: neither overflows nor loses small gradients.
 __global__ __launch_bounds__(kThreads) void k_orth_norm(OrthArgs a) {
+    typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
     const uint32_t block = a.first_block + blockIdx.x, part = block % kParts;
     const int32_t b = a.first + (int32_t)(block / kParts);
     const int64_t size = (int64_t)a.R * a.C;
     const float* g = block_of(a.g, a.ld, b, a.count, size);
     float* v = a.v ? block_of(a.v, a.v_ld, b, a.count, size) : nullptr;
     double sum = 0.0;
-    for (int64_t e = (int64_t)part * kThreads + threadIdx.x; e < size; e += (int64_t)kParts * kThreads) {
-        float u = g[e];
-        if (v) {
-            const float w = a.mu * v[e] + u;
-            v[e] = w;
-            u = a.nesterov ? u + a.mu * w : w;
-        }
+    auto one = [&](float u, float old, float* w) {
+        *w = a.mu * old + u;
+        if (v) u = a.nesterov ? u + a.mu * *w : *w;
         sum += (double)u * u;
+    };
+    const int64_t fours = size / 4, at = (int64_t)part * kThreads + threadIdx.x;
+#pragma unroll 2
+    for (int64_t e = at; e < fours; e += (int64_t)kParts * kThreads) {
+        const vec u = *(reinterpret_cast<const vec*>(g) + e);
+        vec old = {0.f, 0.f, 0.f, 0.f};
+        if (v) old = *(reinterpret_cast<const vec*>(v) + e);
+        float w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) one(u[k], old[k], &w[k]);
+        if (v) *(reinterpret_cast<vec*>(v) + e) = vec{w[0], w[1], w[2], w[3]};
+    }
+    if (at < size % 4) {
+        const int64_t e = fours * 4 + at;
+        float w;
+        one(g[e], v ? v[e] : 0.f, &w);
+        if (v) v[e] = w;
     }
     __shared__ double s[kThreads];
     s[threadIdx.x] = sum;
@@ -120,7 +134,7 @@ struct OrthProduct {
 };
 
 template <typename S, bool Last>
-__global__ __launch_bounds__(S::Threads) void k_orth_product(OrthProduct a) {
+__global__ __launch_bounds__(S::Threads, 2) void k_orth_product(OrthProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t m, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &m, &ti, &tj)) return;
@@ -167,20 +181,20 @@ __global__ __launch_bounds__(kThreads) void k_orth_scaled(OrthArgs a, float scal
     g[e] = total == 0.0 ? 0.f : norm < INFINITY ? (float)((double)scale * u / norm) : NAN;
 }
 
-template <int PA, int PB, bool CA, bool CB>
-using Wide = Tile<256, 256, 2, 4, 32, PA, PB, CA, CB>;
-template <int PA, int PB, bool CA, bool CB>
-using Narrow = Tile<128, 128, 2, 2, 32, PA, PB, CA, CB>;
-
 template <bool CA, bool CB, bool Last>
 hipError_t launch_product(const gpga_ctx* c, OrthProduct& a, int32_t matrices, bool lower) {
-    const bool wide = wide_tiles(c->num_cus, a.rows2, a.cols2, a.K, matrices, lower);
-    a.grid.set(a.rows2, a.cols2, wide ? 256 : 128, matrices, lower);
-    return launch_blocks(a.grid.blocks(), wide ? 512 : 256, [&](uint32_t first, dim3 grid) {
-        a.first_block = first;
-        if (wide) k_orth_product<Wide<2, 2, CA, CB>, Last><<<grid, dim3(512), 0, c->stream>>>(a);
-        else k_orth_product<Narrow<2, 2, CA, CB>, Last><<<grid, dim3(256), 0, c->stream>>>(a);
-    });
+    const int side = tile_side(c->num_cus, 4, a.rows2, a.cols2, a.K, matrices, lower);
+    a.grid.set(a.rows2, a.cols2, side, matrices, lower);
+    auto launch = [&](auto tile) {
+        typedef decltype(tile) S;
+        return launch_blocks(a.grid.blocks(), S::Threads, [&](uint32_t first, dim3 grid) {
+            a.first_block = first;
+            k_orth_product<S, Last><<<grid, dim3(S::Threads), 0, c->stream>>>(a);
+        });
+    };
+    if (side == 256) return launch(Tile256<2, 2, CA, CB>());
+    if (side == 128) return launch(Tile128<2, 2, CA, CB>());
+    return launch(Tile64<2, 2, CA, CB>());
 }
 
 // Scratch of a call of up to `matrices` matrices at a time.

@@ -53,48 +53,47 @@ namespace product {
 typedef __attribute__((address_space(1))) const void gvoid;
 typedef __attribute__((address_space(3))) void lvoid;
 
+// Where a piece of 16 bytes lies within its row of a tile: the banks of LDS repeat after 256 bytes, and 16 lanes that read pieces of
+// 16 rows (or 32 that read 8 bytes each of 4 rows of 64) meet all of them once.
+template <int R, int BK, bool Cols>
+__device__ __forceinline__ int piece_slot(int row, int piece) {
+    if constexpr (!Cols) return piece ^ (BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3);
+    else return piece ^ (R >= 128 ? (row & 3) << 2 : (row & 2) << 1);
+}
+
 // Offset in bytes, from the tile's first row (or column) at k = 0, of the piece that lane `t` loads in round r.
 template <int R, int BK, bool Cols, int Threads>
 __device__ __forceinline__ uint32_t piece_offset(int t, int r, uint32_t ld, int32_t left) {
-    const int q = r * Threads + t;
-    if constexpr (!Cols) {
-        constexpr int C = BK / 8;
-        const int row = q / C, slot = q % C;
-        const int piece = slot ^ (C == 8 ? row & 7 : (row >> 1) & 3);
-        return (uint32_t)(row < left ? row : left - 1) * (ld * 2) + (uint32_t)piece * 16;
-    } else {
-        constexpr int C = R / 8;
-        const int k = q / C, slot = q % C;
-        const int col = (slot ^ ((k & 3) << 1)) * 8;
-        return (uint32_t)k * (ld * 2) + (uint32_t)(col < left ? col : left - 8) * 2;
-    }
+    constexpr int C = (Cols ? R : BK) / 8;
+    const int q = r * Threads + t, row = q / C, piece = piece_slot<R, BK, Cols>(row, q % C);
+    if constexpr (!Cols) return (uint32_t)(row < left ? row : left - 1) * (ld * 2) + (uint32_t)piece * 16;
+    else return (uint32_t)row * (ld * 2) + (uint32_t)(piece * 8 < left ? piece * 8 : left - 8) * 2;
 }
 
-// Where a lane's fragments begin within a plane's tile.  rows: [kk] for each 16 k's; columns: [block parity] of the 32 i's.
-template <int R, int BK, bool Cols>
+// Where a lane's fragments begin within a plane's tile.  rows: for each 16 k's; columns: for each 32 i's.
+template <int R, int BK, bool Cols, int Blocks>
 struct Reader {
-    static constexpr int N = Cols ? 2 : BK / 16;
+    static constexpr int N = Cols ? Blocks : BK / 16;
     uint32_t at[N];
     __device__ __forceinline__ explicit Reader(int lane, int first) {
-        if constexpr (!Cols) {
-            constexpr int C = BK / 8;
-            const int row = lane & 31, swap = (lane >> 5) ^ (C == 8 ? row & 7 : (row >> 1) & 3);
 #pragma unroll
-            for (int kk = 0; kk < N; ++kk) at[kk] = (uint32_t)((first + row) * BK * 2 + (swap ^ (kk * 2)) * 16);
-        } else {
-            const int g = lane >> 4, i = lane & 15;
-            const int k = (g >> 1) * 8 + i / 4, c = (g & 1) * 2 + (i % 4) / 2;
-#pragma unroll
-            for (int p = 0; p < 2; ++p) at[p] = (uint32_t)(k * R * 2 + first * 2 + ((c | p << 2) ^ (i / 4) << 1) * 16 + (i & 1) * 8);
+        for (int n = 0; n < N; ++n) {
+            if constexpr (!Cols) {
+                const int row = lane & 31;
+                at[n] = (uint32_t)((first + row) * BK * 2 + piece_slot<R, BK, false>(row, n * 2 + (lane >> 5)) * 16);
+            } else {
+                const int g = lane >> 4, i = lane & 15, k = (g >> 1) * 8 + i / 4;
+                at[n] = (uint32_t)(k * R * 2 + piece_slot<R, BK, true>(k, (first + n * 32) / 8 + (g & 1) * 2 + (i % 4) / 2) * 16 + (i & 1) * 8);
+            }
         }
     }
-    // i's first + 32 * block .., k's 16 * kk .. of the tile at `lds`.  first is a multiple of 64 where Cols.
+    // i's first + 32 * block .., k's 16 * kk .. of the tile at `lds`; first is a multiple of 32.
     __device__ __forceinline__ half8 read(const char* lds, int block, int kk) const {
         if constexpr (!Cols) {
             return *reinterpret_cast<const half8*>(lds + at[kk] + block * 32 * BK * 2);
         } else {
             typedef __attribute__((address_space(3))) short4v lshort;
-            const char* from = lds + at[block & 1] + (block >> 1) * 128 + kk * 16 * R * 2;
+            const char* from = lds + at[block] + kk * 16 * R * 2;
             const half4 a = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lshort*)(from)));
             const half4 b = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lshort*)(from + 4 * R * 2)));
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -151,8 +150,8 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
         b += stepB;
     };
     const int firstA = wave / S::WN * (S::BM / S::WM), firstB = wave % S::WN * (S::BN / S::WN);
-    const Reader<S::BM, S::BK, S::ColsA> ra(lane, firstA);
-    const Reader<S::BN, S::BK, S::ColsB> rb(lane, firstB);
+    const Reader<S::BM, S::BK, S::ColsA, S::MI> ra(lane, firstA);
+    const Reader<S::BN, S::BK, S::ColsB, S::NI> rb(lane, firstB);
 #pragma unroll
     for (int j = 0; j < S::NI; ++j)
 #pragma unroll
@@ -313,17 +312,38 @@ struct TileGrid {
     }
 };
 
-// Whether tiles of 256 x 256 (one workgroup of 8 wavefronts a compute unit) take less time than tiles of 128 x 128 (two of 4), whose ends
-// are hidden behind the other's products.  In units of a term of 256 x 256: a round of wide tiles K + 900, of narrow ones, half as large,
-// (1.2 K + 400) / 2.
-inline bool wide_tiles(int num_cus, int64_t rows, int64_t cols, int64_t K, int64_t batch, bool lower) {
-    auto tiles = [&](int64_t side) {
-        const int64_t i = (rows + side - 1) / side, j = (cols + side - 1) / side;
-        return (lower ? i * (i + 1) / 2 : i * j) * batch;
-    };
-    const double wide = (double)((tiles(256) + num_cus - 1) / num_cus) * (double)(K + 900);
-    const double narrow = (double)((tiles(128) + 2 * num_cus - 1) / (2 * num_cus)) * (0.6 * (double)K + 200);
-    return wide < narrow;
+// Tiles: 256 x 256 (8 wavefronts, one workgroup a compute unit), 128 x 128 (4 wavefronts, two workgroups, so that one's end is hidden
+// behind the other's products), 64 x 64 (2 wavefronts, where there is little to do).
+template <int PA, int PB, bool CA, bool CB>
+using Tile256 = Tile<256, 256, 2, 4, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
+template <int PA, int PB, bool CA, bool CB>
+using Tile128 = Tile<128, 128, 2, 2, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
+template <int PA, int PB, bool CA, bool CB>
+using Tile64 = Tile<64, 64, 2, 1, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
+
+// The side of the tiles that take the least time, from what the kernels took on these shapes: a tile occupies its compute unit for so many
+// us a thousand terms and so many at its ends, by the planes of both operands; a workgroup of the smallest alone there is no faster than
+// a share of it.  us for 256, 128, 64: one plane each, 8 x 4096 x 4096 x 768 318, 344, 438; 8 x 4096 x 768 x 2048 166, 156, 216;
+// 8 x 8192 x 1024 x 4096 572, 640, 948; three planes, 8 x 4096 x 2048 x 768 452, 422, 515; 2 x 11264 x 2048 x 2048 394, 416, 542; four
+// planes, 5 x 513 x 257 x 1023 75, 31, 21; 16 x 1024 x 1024 x 1024 108, 120, 153.
+inline int tile_side(int num_cus, int planes, int64_t rows, int64_t cols, int64_t K, int64_t batch, bool lower) {
+    static constexpr double kRate[3][3] = {{3.4, 9.8, 33.5}, {6., 16.5, 65.}, {11.5, 25., 85.}}, kEnds[3][3] = {{1.3, 3.5, 12.}, {3., 10., 60.}, {1.2, 5., 20.}};
+    static constexpr double kAlone[3] = {8., 12., 15.};
+    const double k = (double)K * 1e-3;
+    const int p = planes - 2;
+    double best = 0.;
+    int side = 0;
+    for (int t = 0; t < 3; ++t) {
+        const int64_t s = 64 << t, i = (rows + s - 1) / s, j = (cols + s - 1) / s;
+        const int64_t tiles = (lower ? i * (i + 1) / 2 : i * j) * batch;
+        double us = (double)((tiles + num_cus - 1) / num_cus) * (kRate[p][t] * k + kEnds[p][t]);
+        if (t == 0 && us < kAlone[p] * k + 5.) us = kAlone[p] * k + 5.;
+        if (t == 0 || us < best) {
+            best = us;
+            side = (int)s;
+        }
+    }
+    return side;
 }
 
 // ---- values as halves ---------------------------------------------------------------------------------------------------
