@@ -261,7 +261,7 @@ struct FfProduct {
 
 // h = act(x Wg^T) (x Wu^T): a wavefront's blocks of 32 columns are gate and up of the same 32 f's in turn.
 template <typename S, typename E, int Act, int PH>
-__global__ __launch_bounds__(S::Threads, 2) void k_ff_up(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_up(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     static_assert(S::NI == 2, "gate and up");
     int32_t node, ti, tj;
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(S::Threads, 2) void k_ff_up(FfProduct a) {
 
 // Activations out: rows' scales times columns' scales (col_batch < 0: one a node).
 template <typename S, typename E>
-__global__ __launch_bounds__(S::Threads, 2) void k_ff_rows(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_rows(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t node, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(S::Threads, 2) void k_ff_rows(FfProduct a) {
 // dh = dy Wd, and from it and the kept [a | b] the rows of [da | db] and h as halves.  Rows behind the last token are zeros: the
 // products over tokens take them along.
 template <typename S, typename E, int Act, int PA, int PH>
-__global__ __launch_bounds__(S::Threads, 2) void k_ff_down_grad(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_down_grad(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t node, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(S::Threads, 2) void k_ff_down_grad(FfProduct a) {
 // Gradients of matrices: rows of the gate's block, then (from F' on) of the up's; or of the down matrix's alone (off1 < 0).
 // G: fp32, narrow where a row of the matrix is.
 template <typename S, typename G>
-__global__ __launch_bounds__(S::Threads, 2) void k_ff_matrix_grad(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_matrix_grad(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t node, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
@@ -404,32 +404,45 @@ __global__ __launch_bounds__(kThreads) void k_ff_zero(float* g, int64_t g_ld, in
 constexpr int32_t kFewTokens = 64;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// Columns c .. c+15 of a row of `cols`, c a multiple of 16; zeros behind the end.
-template <typename E>
-__device__ __forceinline__ void read16(const typename E::mem* row, int32_t c, int32_t cols, float* v) {
-    typedef typename E::mem M;
-    if (c + 16 <= cols) {
+// Columns c .. c+15 of a row of `cols`; zeros behind the end.
+template <typename M>
+struct Sixteen {
+    typedef M vec __attribute__((ext_vector_type(8), aligned(alignof(M))));
+    M v[16];
+    __device__ __forceinline__ void load(const M* row, int32_t c, int32_t cols) {
+        if (c + 16 <= cols) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) piece_read<kOct, Elem<M, false>>(row, c + 8 * k, c + 16, v + 8 * k);
-    } else {
+            for (int k = 0; k < 2; ++k) {
+                const vec p = *(reinterpret_cast<const vec*>(row + c) + k);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = c + k < cols ? E::get(row[c + k]) : 0.f;
-    }
-}
-// 16 values as P pieces, eight a matrix instruction.
-template <int P>
-__device__ __forceinline__ void pieces16(const float* v, bf16x8 (&out)[P][2]) {
+                for (int j = 0; j < 8; ++j) v[8 * k + j] = p[j];
+            }
+        } else {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        float r = v[k];
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            const __bf16 b = (__bf16)r;
-            out[p][k / 8][k % 8] = b;
-            if (p + 1 < P) r -= (float)b;
+            for (int k = 0; k < 16; ++k) v[k] = c + k < cols ? row[c + k] : (M)0.f;
         }
     }
-}
+    // as P pieces, eight a matrix instruction
+    template <int P>
+    __device__ __forceinline__ void pieces(bf16x8 (&out)[P][2]) const {
+        typedef __bf16 two __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int k = 0; k < 16; k += 2) {
+            v2f r = {(float)v[k], (float)v[k + 1]};
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const two b = __builtin_convertvector(r, two);
+                out[p][k / 8][k % 8] = b[0];
+                out[p][k / 8][k % 8 + 1] = b[1];
+                if (p + 1 < P) {
+                    const uint32_t w = __builtin_bit_cast(uint32_t, b);
+                    r[0] -= __uint_as_float(w << 16);
+                    r[1] -= __uint_as_float(w & 0xffff0000u);
+                }
+            }
+        }
+    }
+};
 
 struct FewArgs {
     const void* x;             // activations, or h
@@ -446,7 +459,7 @@ struct FewArgs {
 
 // EX: type of the operand that is read, E: of the result; Mats = 2: gate and up, 1: down.  NB: blocks of 16 tokens.
 template <typename EX, typename E, int Mats, int Act, int PW, int PX, int NB, int Waves>
-__global__ __launch_bounds__(Waves * kWave) void k_ff_few(FewArgs a) {
+__global__ __launch_bounds__(Waves * kWave, NB == 1 ? 4 : NB == 2 ? 3 : 2) void k_ff_few(FewArgs a) {
     const uint32_t block = a.first_block + blockIdx.x;
     const int64_t node = block / a.per_node;
     const int32_t row0 = (int32_t)(block % a.per_node) * 16, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -462,16 +475,39 @@ __global__ __launch_bounds__(Waves * kWave) void k_ff_few(FewArgs a) {
     for (int m = 0; m < Mats; ++m)
 #pragma unroll
         for (int b = 0; b < NB; ++b) acc[m][b] = v4f{0.f, 0.f, 0.f, 0.f};
-    auto chunk = [&](const float (&vw)[Mats][16], int32_t c) {
-        bf16x8 pw[Mats][PW][2];
+    // the next chunk of the matrices and, as far as registers go, of the tokens is under way while one is multiplied
+    constexpr bool kAhead = NB <= 2;
+    struct Chunk {
+        Sixteen<float> w[Mats];
+        Sixteen<typename EX::mem> x[kAhead ? NB : 1];
+    } now, next;
+    // Each workgroup begins at another chunk: rows that lie a power of two apart would all be read from the same few channels of memory
+    // at a time (24 tokens on 4 nodes, 1024 x 4096: 63.2 and 59.5 us)
+    const int32_t chunks = (a.K + 63) / 64, begin = (int32_t)(block * Waves % (uint32_t)chunks);
+    auto column = [&](int32_t k) { return (k + begin < chunks ? k + begin : k + begin - chunks) * 64 + inner; };
+    auto load = [&](Chunk& to, int32_t k) {
+        const int32_t c = column(k);
 #pragma unroll
-        for (int m = 0; m < Mats; ++m) pieces16<PW>(vw[m], pw[m]);
+        for (int m = 0; m < Mats; ++m) to.w[m].load(w[m], c, a.K);
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) to.x[b].load(x[b], c, a.K);
+        }
+    };
+    int32_t k = wave;
+    if (k < chunks) load(now, k);
+    for (; k < chunks; k += Waves) {
+        if (k + Waves < chunks) load(next, k + Waves);
+        bf16x8 px[NB][PX][2];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            float v[16];
-            bf16x8 px[PX][2];
-            read16<EX>(x[b], c, a.K, v);
-            pieces16<PX>(v, px);
+            if constexpr (!kAhead) now.x[0].load(x[b], column(k), a.K);
+            now.x[kAhead ? b : 0].template pieces<PX>(px[b]);
+        }
+#pragma unroll
+        for (int m = 0; m < Mats; ++m) {
+            bf16x8 pw[PW][2];
+            now.w[m].template pieces<PW>(pw);
 #pragma unroll
             for (int i = 0; i < PW; ++i)
 #pragma unroll
@@ -479,29 +515,10 @@ __global__ __launch_bounds__(Waves * kWave) void k_ff_few(FewArgs a) {
 #pragma unroll
                     for (int half = 0; half < 2; ++half)
 #pragma unroll
-                        for (int m = 0; m < Mats; ++m)
-                            acc[m][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw[m][i][half], px[j][half], acc[m][b], 0, 0, 0);
+                        for (int b = 0; b < NB; ++b)
+                            acc[m][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pw[i][half], px[b][j][half], acc[m][b], 0, 0, 0);
         }
-    };
-    // two chunks of the matrices under way
-    const int32_t chunks = (a.K + 63) / 64;
-    float now[Mats][16], next[Mats][16];
-    int32_t k = wave;
-    if (k < chunks) {
-#pragma unroll
-        for (int m = 0; m < Mats; ++m) read16<ElemF32>(w[m], k * 64 + inner, a.K, now[m]);
-    }
-    for (; k < chunks; k += Waves) {
-        const int32_t after = k + Waves;
-        if (after < chunks) {
-#pragma unroll
-            for (int m = 0; m < Mats; ++m) read16<ElemF32>(w[m], after * 64 + inner, a.K, next[m]);
-        }
-        chunk(now, k * 64 + inner);
-#pragma unroll
-        for (int m = 0; m < Mats; ++m)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) now[m][j] = next[m][j];
+        now = next;
     }
     __shared__ v4f s[Waves][Mats][NB][kWave];
 #pragma unroll

@@ -76,6 +76,18 @@ __global__ __launch_bounds__(kThreads) void k_orth_norm(OrthArgs a) {
     if (threadIdx.x == 0) a.squares[block] = s[0];
 }
 
+// 1 / (sqrt(squares) + eps) as a product of two floats: of a norm below 2^-100 the reciprocal may be none.  0 for a matrix of zeros, NaN for
+// one with an infinity or NaN.
+struct Reciprocal {
+    float first, second;
+};
+__device__ __forceinline__ Reciprocal reciprocal(double squares, float eps) {
+    if (squares == 0.0) return {0.f, 0.f};
+    const double norm = sqrt(squares) + (double)eps;
+    if (!(norm < INFINITY)) return {NAN, NAN};
+    return norm < 0x1p-100 ? Reciprocal{0x1p100f, (float)(0x1p-100 / norm)} : Reciprocal{1.f, (float)(1.0 / norm)};
+}
+
 // u / (|u| + eps) as halves, a wavefront a row.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_orth_pack(OrthArgs a) {
@@ -84,10 +96,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_pack(OrthArgs a) {
     const int32_t row = (int32_t)(block % a.per_matrix) * (kThreads / kWave) + threadIdx.x / kWave, R2 = padded(a.R), C2 = padded(a.C);
     double total = a.squares[m * kParts + lane];
     for (int h = kWave / 2; h > 0; h >>= 1) total += __shfl_xor(total, h);
-    const double norm = sqrt(total) + (double)a.eps;
-    const float inv = total == 0.0 ? 0.f : norm < INFINITY ? (float)(1.0 / norm) : NAN;
-    // the reciprocal of a norm below 2^-126 is no float: such a gradient is scaled up first
-    const float first = total < 1e-60 ? 0x1p100f : 1.f, second = total < 1e-60 ? (total == 0.0 ? 0.f : (float)(0x1p-100 / norm)) : inv;
+    const Reciprocal inv = reciprocal(total, a.eps);
     const int64_t size = (int64_t)a.R * a.C;
     const float* g = block_of(a.g, a.ld, b, a.count, size) + (int64_t)row * a.C;
     const float* v = a.v ? block_of(a.v, a.v_ld, b, a.count, size) + (int64_t)row * a.C : nullptr;
@@ -109,7 +118,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_pack(OrthArgs a) {
         half8 hi, lo;
 #pragma unroll
         for (int j = 0; j < kOct; ++j) {
-            const float w = u[j] * first * second * a.x_up;
+            const float w = u[j] * inv.first * inv.second * a.x_up;
             hi[j] = (half_t)w;
             lo[j] = (half_t)(w - (float)hi[j]);
         }
@@ -134,7 +143,7 @@ struct OrthProduct {
 };
 
 template <typename S, bool Last>
-__global__ __launch_bounds__(S::Threads, 2) void k_orth_product(OrthProduct a) {
+__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_orth_product(OrthProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t m, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &m, &ti, &tj)) return;
@@ -181,6 +190,175 @@ __global__ __launch_bounds__(kThreads) void k_orth_scaled(OrthArgs a, float scal
     g[e] = total == 0.0 ? 0.f : norm < INFINITY ? (float)((double)scale * u / norm) : NAN;
 }
 
+// ---- small matrices ----------------------------------------------------------------------------------------------------------
+// One workgroup brings a matrix into LDS, in two halves a value, takes all steps there and writes the result: X (short side down the rows) and
+// one matrix of the short side's size that holds A and then q A + r A^2.  Results stay in registers until everybody has read what they
+// replace.  Pieces of 16 bytes lie within their row xored with fold(row), so that 16 lanes that read one piece of 16 rows, and 32 that read
+// 8 bytes each of 4 rows for the transposing read, meet every bank once (rows are odd or even multiples of 128 bytes, and the banks repeat
+// after 256).  20 matrices of 64 x 64 in five steps: 72 us as products of their own, a launch each.
+struct SmallArgs {
+    OrthArgs o;
+    int32_t k2;             // long side, padded
+    int32_t steps;
+    float gram_times, poly_keep, poly_times, x_keep, x_times, last_keep, last_times;
+};
+
+template <int M2, int KMax, int Waves>
+__global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
+    constexpr int kBlocks = (M2 / 32) * (KMax / 32) / Waves, kGramBlocks = (M2 / 32) * (M2 / 32);
+    static_assert(kBlocks * Waves == (M2 / 32) * (KMax / 32) && kGramBlocks <= 2 * Waves, "blocks");
+    constexpr int kGramEach = (kGramBlocks + Waves - 1) / Waves;
+    __shared__ __align__(16) half_t sx[2][M2 * KMax];
+    __shared__ __align__(16) half_t sg[2][M2 * M2];
+    __shared__ double s_sum[Waves];
+    const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave, k2 = a.k2;
+    const int32_t m = (int32_t)(a.o.first_block + blockIdx.x), b = a.o.first + m;
+    const int64_t size = (int64_t)a.o.R * a.o.C;
+    float* g = block_of(a.o.g, a.o.ld, b, a.o.count, size);
+    float* v = a.o.v ? block_of(a.o.v, a.o.v_ld, b, a.o.count, size) : nullptr;
+    const bool tall = a.o.R > a.o.C;
+
+    auto fold = [](int row, int width) { return (width / 64 & 1) ? ((row & 2) << 1 | (row >> 2 & 3)) : ((row & 3) << 2 | (row >> 2 & 3)); };
+    auto at = [&](int row, int col, int width) { return row * width + ((col >> 3 ^ fold(row, width)) << 3) + (col & 7); };
+    // 8 k's of row `first + lane % 32`, or of column `first + ..` of X
+    auto rows8 = [&](const half_t* p, int first, int kk, int width) {
+        return *reinterpret_cast<const half8*>(p + at(first + (lane & 31), kk * 16 + (lane >> 5) * 8, width));
+    };
+    auto cols8 = [&](const half_t* p, int first, int kk) {
+        typedef __attribute__((address_space(3))) short4v lshort;
+        const int group = lane >> 4, i = lane & 15, k = kk * 16 + (group >> 1) * 8 + i / 4, col = first + (group & 1) * 16 + (i & 3) * 4;
+        const half4 lo = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lshort*)(p + at(k, col, k2))));
+        const half4 hi = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lshort*)(p + at(k + 4, col, k2))));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto times3 = [](const half8 (&fb)[2], const half8 (&fa)[2], acc16 c) {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb[0], fa[0], c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb[0], fa[1], c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(fb[1], fa[0], c, 0, 0, 0);
+    };
+
+    double sum = 0.0;
+    for (int32_t r = wave; r < a.o.R; r += Waves)
+        for (int32_t c = lane; c < a.o.C; c += kWave) {
+            const int64_t e = (int64_t)r * a.o.C + c;
+            float u = g[e];
+            if (v) {
+                const float w = a.o.mu * v[e] + u;
+                v[e] = w;
+                u = a.o.nesterov ? u + a.o.mu * w : w;
+            }
+            sum += (double)u * u;
+        }
+    for (int h = kWave / 2; h > 0; h >>= 1) sum += __shfl_xor(sum, h);
+    if (lane == 0) s_sum[wave] = sum;
+    for (int e = t * 8; e < M2 * k2; e += Waves * kWave * 8) {
+        *reinterpret_cast<half8*>(sx[0] + e) = half8{};
+        *reinterpret_cast<half8*>(sx[1] + e) = half8{};
+    }
+    __syncthreads();
+    double total = 0.0;
+    for (int w = 0; w < Waves; ++w) total += s_sum[w];
+    const Reciprocal inv = reciprocal(total, a.o.eps);
+    for (int32_t r = wave; r < a.o.R; r += Waves)
+        for (int32_t c = lane; c < a.o.C; c += kWave) {
+            const int64_t e = (int64_t)r * a.o.C + c;
+            float u = g[e];
+            if (v) u = a.o.nesterov ? u + a.o.mu * v[e] : v[e];
+            u = u * inv.first * inv.second * a.o.x_up;
+            const int to = tall ? at(c, r, k2) : at(r, c, k2);
+            const half_t hi = (half_t)u;
+            sx[0][to] = hi;
+            sx[1][to] = (half_t)(u - (float)hi);
+        }
+    __syncthreads();
+
+    // p[row][col .. col + 3] <- keep * p + times * acc
+    auto put = [&](half_t* p0, half_t* p1, int width, int row0, int col0, const acc16& c, float keep, float times) {
+        const int row = row0 + (lane & 31);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int to = at(row, col0 + q * 8 + (lane >> 5) * 4, width);
+            half4 hi = *reinterpret_cast<const half4*>(p0 + to), lo = *reinterpret_cast<const half4*>(p1 + to);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float o = times * c[q * 4 + k] + (keep != 0.f ? keep * ((float)hi[k] + (float)lo[k]) : 0.f);
+                hi[k] = (half_t)o;
+                lo[k] = (half_t)(o - (float)hi[k]);
+            }
+            *reinterpret_cast<half4*>(p0 + to) = hi;
+            *reinterpret_cast<half4*>(p1 + to) = lo;
+        }
+    };
+    for (int step = 0; step < a.steps; ++step) {
+#pragma unroll
+        for (int turn = 0; turn < 2; ++turn) {  // A = X X^T, then q A + r A A
+            const half_t *p0 = turn ? sg[0] : sx[0], *p1 = turn ? sg[1] : sx[1];
+            const int width = turn ? M2 : k2;
+            acc16 c[kGramEach];
+#pragma unroll
+            for (int n = 0; n < kGramEach; ++n) {
+                c[n] = acc16{};
+                const int block = wave + n * Waves;
+                if (block >= kGramBlocks) continue;
+                const int row0 = block / (M2 / 32) * 32, col0 = block % (M2 / 32) * 32;
+                for (int kk = 0; kk < width / 16; ++kk) {
+                    const half8 fa[2] = {rows8(p0, row0, kk, width), rows8(p1, row0, kk, width)};
+                    const half8 fb[2] = {rows8(p0, col0, kk, width), rows8(p1, col0, kk, width)};
+                    c[n] = times3(fb, fa, c[n]);
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < kGramEach; ++n) {
+                const int block = wave + n * Waves;
+                if (block >= kGramBlocks) continue;
+                put(sg[0], sg[1], M2, block / (M2 / 32) * 32, block % (M2 / 32) * 32, c[n], turn ? a.poly_keep : 0.f, turn ? a.poly_times : a.gram_times);
+            }
+            __syncthreads();
+        }
+        acc16 c[kBlocks];
+        const int across = k2 / 32;
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n) {
+            c[n] = acc16{};
+            const int block = wave + n * Waves;
+            if (block >= M2 / 32 * across) continue;
+            const int row0 = block / across * 32, col0 = block % across * 32;
+#pragma unroll
+            for (int kk = 0; kk < M2 / 16; ++kk) {
+                const half8 fa[2] = {rows8(sg[0], row0, kk, M2), rows8(sg[1], row0, kk, M2)};
+                const half8 fb[2] = {cols8(sx[0], col0, kk), cols8(sx[1], col0, kk)};
+                c[n] = times3(fb, fa, c[n]);
+            }
+        }
+        const bool last = step + 1 == a.steps;
+        if (!last) __syncthreads();
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n) {
+            const int block = wave + n * Waves;
+            if (block >= M2 / 32 * across) continue;
+            const int row0 = block / across * 32, col0 = block % across * 32;
+            if (!last) {
+                put(sx[0], sx[1], k2, row0, col0, c[n], a.x_keep, a.x_times);
+                continue;
+            }
+            const int row = row0 + (lane & 31);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int col = col0 + q * 8 + (lane >> 5) * 4, from = at(row, col, k2);
+                const half4 hi = *reinterpret_cast<const half4*>(sx[0] + from), lo = *reinterpret_cast<const half4*>(sx[1] + from);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float o = a.last_times * c[n][q * 4 + k] + a.last_keep * ((float)hi[k] + (float)lo[k]);
+                    if (row < (tall ? a.o.C : a.o.R) && col + k < (tall ? a.o.R : a.o.C))
+                        g[tall ? (int64_t)(col + k) * a.o.C + row : (int64_t)row * a.o.C + col + k] = o;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
 template <bool CA, bool CB, bool Last>
 hipError_t launch_product(const gpga_ctx* c, OrthProduct& a, int32_t matrices, bool lower) {
     const int side = tile_side(c->num_cus, 4, a.rows2, a.cols2, a.K, matrices, lower);
@@ -220,6 +398,12 @@ OrthScratch carve(const OrthShape& s, char* base, size_t* bytes) {
     w.squares = reinterpret_cast<double*>(take((size_t)w.chunk * kParts * sizeof(double)));
     *bytes = used;
     return w;
+}
+
+// Matrices that one workgroup holds.
+bool small_fits(const OrthShape& s) {
+    const int32_t R2 = padded(s.R), C2 = padded(s.C), m2 = R2 < C2 ? R2 : C2, k2 = R2 < C2 ? C2 : R2;
+    return m2 == 64 ? k2 <= 512 : k2 == 128;
 }
 
 // Power of two that brings values of at most `bound` to 2^14 or below.
@@ -301,16 +485,43 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
         double most = 1.0;
         float x_up = up_for(1.0);
         a.x_up = x_up;
-        hipError_t e = launch_blocks((uint64_t)kParts * matrices, kThreads, [&](uint32_t first, dim3 grid) {
-            a.first_block = first;
-            k_orth_norm<<<grid, dim3(kThreads), 0, c->stream>>>(a);
-        });
-        if (e != hipSuccess) return e;
+        hipError_t e = hipSuccess;
+        const bool small = steps > 0 && small_fits(s);
+        if (!small) {
+            e = launch_blocks((uint64_t)kParts * matrices, kThreads, [&](uint32_t first, dim3 grid) {
+                a.first_block = first;
+                k_orth_norm<<<grid, dim3(kThreads), 0, c->stream>>>(a);
+            });
+            if (e != hipSuccess) return e;
+        }
         if (steps == 0) {
             a.per_matrix = (uint32_t)(((int64_t)s.R * s.C + kThreads - 1) / kThreads);
             e = launch_blocks((uint64_t)a.per_matrix * matrices, kThreads, [&](uint32_t first, dim3 grid) {
                 a.first_block = first;
                 k_orth_scaled<<<grid, dim3(kThreads), 0, c->stream>>>(a, scale);
+            });
+            if (e != hipSuccess) return e;
+            continue;
+        }
+        if (small) {
+            const double bound = orthogonalize_bound(steps, coefficients), g_up = up_for(bound * bound * 1.001),
+                         p_up = up_for(even_max(q, r, bound * bound) * 1.001 + 1e-30);
+            SmallArgs f = {a, R2 > C2 ? R2 : C2, steps, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            const double up = up_for(bound);
+            f.o.x_up = (float)up;
+            f.gram_times = (float)(g_up / up / up);
+            f.poly_keep = (float)(q * p_up / g_up);
+            f.poly_times = (float)(r * p_up / g_up / g_up);
+            f.x_keep = (float)p;
+            f.x_times = (float)(1.0 / p_up);
+            f.last_keep = (float)(p * scale / up);
+            f.last_times = (float)(scale / up / p_up);
+            const int32_t waves = f.k2 > 64 ? 8 : 4;
+            e = launch_blocks((uint64_t)matrices, waves * kWave, [&](uint32_t first, dim3 grid) {
+                f.o.first_block = first;
+                if (f.k2 == 64) k_orth_small<64, 64, 4><<<grid, dim3(256), 0, c->stream>>>(f);
+                else if (m2 == 64) k_orth_small<64, 512, 8><<<grid, dim3(512), 0, c->stream>>>(f);
+                else k_orth_small<128, 128, 8><<<grid, dim3(512), 0, c->stream>>>(f);
             });
             if (e != hipSuccess) return e;
             continue;

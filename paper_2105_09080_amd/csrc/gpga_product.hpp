@@ -319,7 +319,7 @@ using Tile256 = Tile<256, 256, 2, 4, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
 template <int PA, int PB, bool CA, bool CB>
 using Tile128 = Tile<128, 128, 2, 2, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
 template <int PA, int PB, bool CA, bool CB>
-using Tile64 = Tile<64, 64, 2, 1, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
+using Tile64 = Tile<64, 64, 2, 1, 64, PA, PB, CA, CB>;
 
 // The side of the tiles that take the least time, from what the kernels took on these shapes: a tile occupies its compute unit for so many
 // us a thousand terms and so many at its ends, by the planes of both operands; a workgroup of the smallest alone there is no faster than
