@@ -37,11 +37,12 @@ struct Operand {
     int32_t rows;      // rows of memory, padded
 };
 
-template <int kBM, int kBN, int kWM, int kWN, int kBK, int kPA, int kPB, bool kColsA, bool kColsB>
+// WM x WN wavefronts share a tile's rows and columns, KW such groups the terms of a step.
+template <int kBM, int kBN, int kWM, int kWN, int kBK, int kPA, int kPB, bool kColsA, bool kColsB, int kKW = 1>
 struct Tile {
-    static constexpr int BM = kBM, BN = kBN, WM = kWM, WN = kWN, BK = kBK, PA = kPA, PB = kPB;
+    static constexpr int BM = kBM, BN = kBN, WM = kWM, WN = kWN, BK = kBK, PA = kPA, PB = kPB, KW = kKW;
     static constexpr bool ColsA = kColsA, ColsB = kColsB;
-    static constexpr int Waves = WM * WN, Threads = Waves * kWave;
+    static constexpr int Waves = WM * WN, Threads = Waves * KW * kWave;
     static constexpr int MI = BM / WM / 32, NI = BN / WN / 32;             // 32 x 32 blocks of a wavefront
     static constexpr int BytesA = BM * BK * 2, BytesB = BN * BK * 2;       // of a plane
     static constexpr int Stage = PA * BytesA + PB * BytesB;
@@ -70,30 +71,31 @@ __device__ __forceinline__ uint32_t piece_offset(int t, int r, uint32_t ld, int3
     else return (uint32_t)row * (ld * 2) + (uint32_t)(piece * 8 < left ? piece * 8 : left - 8) * 2;
 }
 
-// Where a lane's fragments begin within a plane's tile.  rows: for each 16 k's; columns: for each 32 i's.
-template <int R, int BK, bool Cols, int Blocks>
+// Where a lane's fragments begin within a plane's tile.  rows: for each 16 k's; columns: for each 32 i's.  Of KW groups of wavefronts each
+// takes every KW-th 16 k's.
+template <int R, int BK, bool Cols, int Blocks, int KW>
 struct Reader {
-    static constexpr int N = Cols ? Blocks : BK / 16;
+    static constexpr int N = Cols ? Blocks : BK / 16 / KW;
     uint32_t at[N];
-    __device__ __forceinline__ explicit Reader(int lane, int first) {
+    __device__ __forceinline__ Reader(int lane, int first, int group) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if constexpr (!Cols) {
                 const int row = lane & 31;
-                at[n] = (uint32_t)((first + row) * BK * 2 + piece_slot<R, BK, false>(row, n * 2 + (lane >> 5)) * 16);
+                at[n] = (uint32_t)((first + row) * BK * 2 + piece_slot<R, BK, false>(row, (n * KW + group) * 2 + (lane >> 5)) * 16);
             } else {
                 const int g = lane >> 4, i = lane & 15, k = (g >> 1) * 8 + i / 4;
-                at[n] = (uint32_t)(k * R * 2 + piece_slot<R, BK, true>(k, (first + n * 32) / 8 + (g & 1) * 2 + (i % 4) / 2) * 16 + (i & 1) * 8);
+                at[n] = (uint32_t)((group * 16 + k) * R * 2 + piece_slot<R, BK, true>(k, (first + n * 32) / 8 + (g & 1) * 2 + (i % 4) / 2) * 16 + (i & 1) * 8);
             }
         }
     }
-    // i's first + 32 * block .., k's 16 * kk .. of the tile at `lds`; first is a multiple of 32.
-    __device__ __forceinline__ half8 read(const char* lds, int block, int kk) const {
+    // i's first + 32 * block .., the group's n-th 16 k's of the tile at `lds`; first is a multiple of 32.
+    __device__ __forceinline__ half8 read(const char* lds, int block, int n) const {
         if constexpr (!Cols) {
-            return *reinterpret_cast<const half8*>(lds + at[kk] + block * 32 * BK * 2);
+            return *reinterpret_cast<const half8*>(lds + at[n] + block * 32 * BK * 2);
         } else {
             typedef __attribute__((address_space(3))) short4v lshort;
-            const char* from = lds + at[block] + kk * 16 * R * 2;
+            const char* from = lds + at[block] + n * KW * 16 * R * 2;
             const half4 a = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lshort*)(from)));
             const half4 b = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lshort*)(from + 4 * R * 2)));
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -149,9 +151,10 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
         a += stepA;
         b += stepB;
     };
-    const int firstA = wave / S::WN * (S::BM / S::WM), firstB = wave % S::WN * (S::BN / S::WN);
-    const Reader<S::BM, S::BK, S::ColsA, S::MI> ra(lane, firstA);
-    const Reader<S::BN, S::BK, S::ColsB, S::NI> rb(lane, firstB);
+    const int group = wave / S::Waves;
+    const int firstA = wave % S::Waves / S::WN * (S::BM / S::WM), firstB = wave % S::WN * (S::BN / S::WN);
+    const Reader<S::BM, S::BK, S::ColsA, S::MI, S::KW> ra(lane, firstA, group);
+    const Reader<S::BN, S::BK, S::ColsB, S::NI, S::KW> rb(lane, firstB, group);
 #pragma unroll
     for (int j = 0; j < S::NI; ++j)
 #pragma unroll
@@ -164,7 +167,7 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
         if (s + 1 < steps) fetch((s + 1) & 1);
         const char* at = lds + (s & 1) * S::Stage;
 #pragma unroll
-        for (int kk = 0; kk < S::BK / 16; ++kk) {
+        for (int kk = 0; kk < S::BK / 16 / S::KW; ++kk) {
             half8 fa[S::PA][S::MI], fb[S::PB][S::NI];
 #pragma unroll
             for (int p = 0; p < S::PA; ++p)
@@ -185,6 +188,31 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
                         for (int i = 0; i < S::MI; ++i)
                             acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb[pb][j], fa[pa][i], acc[j][i], 0, 0, 0);
                 }
+        }
+        __syncthreads();
+    }
+    if constexpr (S::KW > 1) {  // the first group adds the others' sums, in their order
+        float* mine = reinterpret_cast<float*>(lds) + (wave - S::Waves) * (S::NI * S::MI * 16 * kWave) + lane;
+        static_assert((S::KW - 1) * S::Waves * S::NI * S::MI * 16 * kWave * 4 <= 2 * S::Stage, "sums");
+        if (group > 0) {
+#pragma unroll
+            for (int j = 0; j < S::NI; ++j)
+#pragma unroll
+                for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) mine[((j * S::MI + i) * 16 + r) * kWave] = acc[j][i][r];
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int g = 1; g < S::KW; ++g)
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j)
+#pragma unroll
+                    for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            acc[j][i][r] += mine[(g * S::Waves * S::NI * S::MI * 16 + (j * S::MI + i) * 16 + r) * kWave];
         }
         __syncthreads();
     }
@@ -231,6 +259,7 @@ __device__ __forceinline__ int32_t wave_col(int32_t n0) {
 // f(row, column, eight columns' values) for a tile; with `mirror` then f(column, row, eight rows' values) too.
 template <typename S, typename F>
 __device__ __forceinline__ void each_octet(const acc16 (&acc)[S::NI][S::MI], char* lds, int32_t m0, int32_t n0, bool mirror, F&& f) {
+    if ((int)threadIdx.x >= S::Waves * kWave) return;  // the first group of wavefronts has the sums
     const Dump<S> dump(lds);
     const int lane = threadIdx.x & (kWave - 1);
     const int32_t row0 = wave_row<S>(m0), col0 = wave_col<S>(n0);
@@ -259,6 +288,7 @@ __device__ __forceinline__ void each_octet(const acc16 (&acc)[S::NI][S::MI], cha
 // f(row, column, eight values of the wavefront's first 32 columns, the same of its second 32), column counted in the first.
 template <typename S, typename F>
 __device__ __forceinline__ void each_octet_pair(const acc16 (&acc)[S::NI][S::MI], char* lds, int32_t m0, F&& f) {
+    if ((int)threadIdx.x >= S::Waves * kWave) return;  // the first group of wavefronts has the sums
     const Dump<S> dump(lds);
     const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
@@ -313,22 +343,23 @@ struct TileGrid {
 };
 
 // Tiles: 256 x 256 (8 wavefronts, one workgroup a compute unit), 128 x 128 (4 wavefronts, two workgroups, so that one's end is hidden
-// behind the other's products), 64 x 64 (2 wavefronts, where there is little to do).
+// behind the other's products), 64 x 64 (two groups of 2
+// wavefronts, where there is little to do: 5 x 320 x 320 x 1024 with four planes 15.7 us in one group, 14.2 with steps twice as long, 13 in two).
 template <int PA, int PB, bool CA, bool CB>
 using Tile256 = Tile<256, 256, 2, 4, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
 template <int PA, int PB, bool CA, bool CB>
 using Tile128 = Tile<128, 128, 2, 2, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
 template <int PA, int PB, bool CA, bool CB>
-using Tile64 = Tile<64, 64, 2, 1, 64, PA, PB, CA, CB>;
+using Tile64 = Tile<64, 64, 2, 1, 64, PA, PB, CA, CB, 2>;
 
-// The side of the tiles that take the least time, from what the kernels took on these shapes: a tile occupies its compute unit for so many
-// us a thousand terms and so many at its ends, by the planes of both operands; a workgroup of the smallest alone there is no faster than
-// a share of it.  us for 256, 128, 64: one plane each, 8 x 4096 x 4096 x 768 318, 344, 438; 8 x 4096 x 768 x 2048 166, 156, 216;
-// 8 x 8192 x 1024 x 4096 572, 640, 948; three planes, 8 x 4096 x 2048 x 768 452, 422, 515; 2 x 11264 x 2048 x 2048 394, 416, 542; four
-// planes, 5 x 513 x 257 x 1023 75, 31, 21; 16 x 1024 x 1024 x 1024 108, 120, 153.
+// The side of the tiles that take the least time, by what the kernels took on these shapes: a tile occupies its compute unit for so many
+// us a thousand terms and so many at its ends, by the planes of both operands; one of the smallest alone there is no faster than
+// kAlone.  us for 256, 128, 64: one plane each, 8 x 4096 x 4096 x 768 304, 346, 449; 8 x 4096 x 768 x 2048 163, 157, 220;
+// 8 x 8192 x 1024 x 4096 558, 644, 956; three planes, 8 x 4096 x 2048 x 768 449, 420, 559; 2 x 11264 x 2048 x 2048 421, 412, 589; four
+// planes, 5 x 513 x 257 x 1023 71, 30, 15.5; 16 x 1024 x 1024 x 1024 110, 120, 185.
 inline int tile_side(int num_cus, int planes, int64_t rows, int64_t cols, int64_t K, int64_t batch, bool lower) {
-    static constexpr double kRate[3][3] = {{3.4, 9.8, 33.5}, {6., 16.5, 65.}, {11.5, 25., 85.}}, kEnds[3][3] = {{1.3, 3.5, 12.}, {3., 10., 60.}, {1.2, 5., 20.}};
-    static constexpr double kAlone[3] = {8., 12., 15.};
+    static constexpr double kRate[3][3] = {{3.8, 9.8, 33.5}, {6.8, 16.5, 65.}, {10., 25., 85.}}, kEnds[3][3] = {{0.8, 3.5, 12.}, {2.5, 10., 60.}, {1., 7., 20.}};
+    static constexpr double kAlone[3] = {6., 8.5, 11.};
     const double k = (double)K * 1e-3;
     const int p = planes - 2;
     double best = 0.;
@@ -337,7 +368,7 @@ inline int tile_side(int num_cus, int planes, int64_t rows, int64_t cols, int64_
         const int64_t s = 64 << t, i = (rows + s - 1) / s, j = (cols + s - 1) / s;
         const int64_t tiles = (lower ? i * (i + 1) / 2 : i * j) * batch;
         double us = (double)((tiles + num_cus - 1) / num_cus) * (kRate[p][t] * k + kEnds[p][t]);
-        if (t == 0 && us < kAlone[p] * k + 5.) us = kAlone[p] * k + 5.;
+        if (t == 0 && us < kAlone[p] * k + 3.) us = kAlone[p] * k + 3.;
         if (t == 0 || us < best) {
             best = us;
             side = (int)s;
