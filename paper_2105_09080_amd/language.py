@@ -4,14 +4,17 @@ Every node predicts the next token of its own text from the last two, with its o
 
     a = sqrt(D) E_i[token[t]],  b = sqrt(D) F_i[token[t-1]]           two embedding tables of V rows (padding before the first)
     y = layer norm of (b + dropout(a)), with gamma_i and beta_i
-    z = y E_i^T                                                       the output layer is the first table again
+    v = y + Wd_i (act(Wg_i y) * Wu_i y)                               with ff > 0 hidden units; v = y without
+    z = v E_i^T                                                       the output layer is the first table again
     f_i = mean cross-entropy of softmax(z) against token[t+1]
 
 The backward pass writes G column block by column block: the output layer's gradient of E_i first, the embedding's is added
-to it.  Then gpga_step (or gpga_aga_step, which takes the nodes' losses as they are) updates and mixes.  Everything but the
-two products with E is the library's; the products are the caller's own, in torch.
+to it.  With ``orthogonal`` the feed-forward block's three gradients become orthogonalised updates in their place.  Then gpga_step
+(or gpga_aga_step, which takes the nodes' losses as they are) updates and mixes.  Everything but the two products with E is the
+library's; the products are the caller's own, in torch.
 
     python -m paper_2105_09080_amd.language --n 16 --iters 300
+    python -m paper_2105_09080_amd.language --n 16 --iters 300 --ff 384 --orthogonal
 """
 from __future__ import annotations
 
@@ -32,13 +35,17 @@ class NextTokenModel:
     """The model above on a simulation's rows.  ``dtype``: type of the activations between the operators."""
 
     def __init__(self, n: int, V: int, D: int, *, topology: str = "ring", H: int = 8, lr: float = 0.5, momentum: float = 0.9,
-                 p: float = 0.1, seed: int = 0, dtype: torch.dtype = torch.float32, stream=None):
+                 p: float = 0.1, seed: int = 0, dtype: torch.dtype = torch.float32, stream=None, ff: int = 0,
+                 act: str = "silu", orthogonal: bool = False):
         self.n, self.V, self.D, self.p, self.seed, self.dtype = n, V, D, p, seed, dtype
+        self.ff, self.act, self.orthogonal = ff, act, orthogonal and ff > 0
         self.E, self.F = 0, V * D                                   # column offsets
         self.gamma, self.beta = 2 * V * D, 2 * V * D + D
         self.scale = math.sqrt(D)
-        x0 = inputs.initial_point(2 * V * D + 2 * D, seed) / self.scale
-        x0[self.gamma:self.beta], x0[self.beta:] = 1.0, 0.0
+        after = 2 * V * D + 2 * D
+        self.gate, self.up, self.down = after, after + ff * D, after + 2 * ff * D
+        x0 = inputs.initial_point(after + 3 * ff * D, seed) / self.scale
+        x0[self.gamma:self.beta], x0[self.beta:after] = 1.0, 0.0
         self.sim = Simulation(n, x0.size, topology=topology, H=H, lr=lr, momentum=momentum, x0=x0, stream=stream)
 
     def table(self, rows: torch.Tensor) -> torch.Tensor:
@@ -50,23 +57,37 @@ class NextTokenModel:
         a = s.embed(tokens, self.E, self.V, self.D, scale=self.scale, dtype=self.dtype)
         b = s.embed(previous, self.F, self.V, self.D, scale=self.scale, dtype=self.dtype)
         y, u, stats = s.layer_norm(a, self.gamma, self.beta, residual=b, p=p, seed=self.seed)
+        v, hidden = y, None
+        if self.ff:
+            h, hidden = s.gated_ff(y, self.gate, self.up, self.down, self.ff, act=self.act, keep=grad)
+            v = y + h
         table = self.table(s.X)
-        z = torch.bmm(y.float(), table.transpose(1, 2).contiguous()).to(self.dtype)
+        z = torch.bmm(v.float(), table.transpose(1, 2).contiguous()).to(self.dtype)
         loss, dz = s.token_loss(z, labels, grad=z if grad else False)   # the gradient takes the logits' place
-        return loss, dz, y, u, stats, table
+        return loss, dz, v, y, hidden, u, stats, table
 
     def gradients(self, tokens, previous, labels) -> torch.Tensor:
         """Losses of the nodes; their gradients in G."""
         s = self.sim
         with torch.cuda.stream(s.stream):
-            loss, dz, y, u, stats, table = self.forward(tokens, previous, labels, self.p, True)
+            loss, dz, v, y, hidden, u, stats, table = self.forward(tokens, previous, labels, self.p, True)
             dz = dz.float()
-            self.table(s.G).copy_(torch.bmm(dz.transpose(1, 2).contiguous(), y.float()))
+            self.table(s.G).copy_(torch.bmm(dz.transpose(1, 2).contiguous(), v.float()))
             dy = torch.bmm(dz, table.contiguous()).to(self.dtype)
+            if self.ff:
+                dy = dy + s.gated_ff_grad(dy, y, hidden, self.gate, self.up, self.down, act=self.act)
+                if self.orthogonal:
+                    s.orthogonalize(self.gate, self.ff, self.D, count=2, scale=self.update_scale(self.ff, self.D))
+                    s.orthogonalize(self.down, self.D, self.ff, scale=self.update_scale(self.D, self.ff))
             du, dx = s.layer_norm_grad(dy, u, stats, self.gamma, self.beta, p=self.p, seed=self.seed)
             s.embed_grad(tokens, dx, self.E, self.V, scale=self.scale, accumulate=True)
             s.embed_grad(previous, du, self.F, self.V, scale=self.scale)
         return loss
+
+    @staticmethod
+    def update_scale(rows: int, cols: int) -> float:
+        """An orthogonalised rows x cols update has about min(rows, cols) singular values of 1: elements of root mean square 0.02."""
+        return 0.02 * math.sqrt(max(rows, cols))
 
     def losses(self, tokens, previous, labels) -> torch.Tensor:
         """Losses without dropout and without gradients."""
@@ -116,11 +137,14 @@ def main():
     ap.add_argument("--lr", type=float, default=0.5)
     ap.add_argument("--dropout", type=float, default=0.1)
     ap.add_argument("--dtype", default="bf16", choices=["f32", "bf16"])
+    ap.add_argument("--ff", type=int, default=0, help="hidden units of a gated feed-forward block (0: none)")
+    ap.add_argument("--activation", default="silu", choices=sorted(B.ACTIVATION))
+    ap.add_argument("--orthogonal", action="store_true", help="orthogonalised updates of the feed-forward matrices")
     ap.add_argument("--adaptive", action="store_true", help="adaptive averaging period (Gossip-AGA)")
     args = ap.parse_args()
     dtype = {"f32": torch.float32, "bf16": torch.bfloat16}[args.dtype]
     model = NextTokenModel(args.n, args.vocabulary, args.width, topology=args.topology, H=args.H, lr=args.lr, p=args.dropout,
-                           dtype=dtype)
+                           dtype=dtype, ff=args.ff, act=args.activation, orthogonal=args.orthogonal)
     text = inputs.markov_text(args.iters, args.n, args.sequences, args.length, args.vocabulary)
     for record in train(model, text, adaptive=args.adaptive):
         print(json.dumps(record), flush=True)

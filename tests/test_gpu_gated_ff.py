@@ -91,7 +91,7 @@ def backward_tolerances(dy, x, a, b, gate, up, down, kind, dtype):
     value, slope = orc.activation(kind, a)
     m = np.abs(dy) @ np.abs(down)                       # magnitudes of dh's terms
     most = np.abs(dy).sum(axis=2) * np.abs(down).max(axis=(1, 2))[:, None]
-    td = ((3 if f32 else 1) * TWO + (D + 16) * E32) * m + 2 * FLOOR * most[..., None]
+    td = ((3 if f32 else 1) * TWO + (D + 16) * E32) * m + 2 * FLOOR * D * (np.abs(dy).max(axis=2) * np.abs(down).max(axis=(1, 2))[:, None])[..., None]
     am, bm = np.abs(a).max(axis=2), np.abs(b).max(axis=2)
     floor = 2 * FLOOR * (most * np.maximum(1.14 * bm, am))[..., None]
     dh = np.abs(dy @ down)
@@ -153,4 +153,309 @@ def test_forward_and_backward(hx, n, T, D, F, off, pad, order, kind, dtype):
         assert np.array_equal(got[:, left], before[:, left].astype(np.float64))
     again = sim.gated_ff_grad(dy, x, hidden, *at, act=kind, accumulate=False)
     assert torch.equal(again, dx)
+    sim.close()
+
+
+def gpu_reference(sim, x, at, D, F, kind):
+    """y in float64 on the GPU, for sizes that the oracle would take long for."""
+    w = [sim.X[:, k:k + D * F].double() for k in at]
+    x = x.double()
+    a, b = (torch.bmm(x, m.reshape(-1, F, D).transpose(1, 2).contiguous()) for m in w[:2])
+    value = a * torch.sigmoid(a) if kind == "silu" else a * torch.special.ndtr(a)
+    return torch.bmm(value * b, w[2].reshape(-1, D, F).transpose(1, 2).contiguous()), a, b, w
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T", [3, 70])
+def test_scales_far_apart(hx, T, dtype):
+    """Tokens, gradients and rows of matrices that lie powers of ten apart: every token's result is as good as if it were alone.  The
+    tolerances take row by row what shares a scale."""
+    if dtype == "f16":
+        spread = [1.0, 1e-2, 30.0]
+    else:
+        spread = [1.0, 1e-9, 1e6]
+    dt, u, sub = TYPES[dtype]
+    n, D, F = 2, 72, 90
+    sim, at, gate, up, down, rng = make(hx, n, D, F, 1, T)
+    for w, k in ((gate, 0), (up, 1), (down, 2)):
+        w[:, ::3] *= 2.0 ** -20
+        w[:, 1] = 0.0
+        sim.X[:, at[k]:at[k] + D * F].copy_(torch.as_tensor(w.reshape(n, -1)).float())
+    x = rows(rng, (n, T, D), dt)
+    x *= torch.tensor([spread[t % 3] for t in range(T)], device="cuda").to(dt)[None, :, None]
+    x[0, 0] = 0.0
+    y, hidden = sim.gated_ff(x, *at, F, keep=True)
+    (wy, wa, wb), (ty, ta, tb) = forward_tolerances(host(x), gate, up, down, "silu", dtype)
+    close(hidden[..., :F], wa, ta + u * (np.abs(wa) + ta) + sub, "a")
+    close(hidden[..., F:], wb, tb + u * (np.abs(wb) + tb) + sub, "b")
+    close(y, wy, ty + u * (np.abs(wy) + ty) + sub, "y")
+    assert not y[0, 0].any() and not hidden[0, 0].any()
+
+    dy = rows(rng, (n, T, D), dt, scale=0.1)
+    dy *= torch.tensor([spread[(t + 1) % 3] for t in range(T)], device="cuda").to(dt)[None, :, None]
+    dy[:, T // 2] = 0.0
+    a, b = host(hidden[..., :F]), host(hidden[..., F:])
+    want = orc.gated_ff_grad(host(dy), host(x), a, b, gate, up, down, "silu")
+    tdx, tg = backward_tolerances(host(dy), host(x), a, b, gate, up, down, "silu", dtype)
+    dx = sim.gated_ff_grad(dy, x, hidden, *at)
+    close(dx, want[0], tdx + u * (np.abs(want[0]) + tdx) + sub, "dx")
+    assert not dx[:, T // 2].any()
+    for k in range(3):
+        close(sim.G[:, at[k]:at[k] + D * F], want[k + 1].reshape(n, -1), tg[k].reshape(n, -1) + 2 * E32 * np.abs(want[k + 1]).reshape(n, -1), f"gradient {k}")
+    sim.close()
+
+
+@pytest.mark.parametrize("T", [5, 66])
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_infinities_and_nan_stay_in_their_token(hx, bad, T):
+    n, D, F = 2, 40, 70
+    sim, at, gate, up, down, rng = make(hx, n, D, F, 0, 3)
+    x, dy = rows(rng, (n, T, D), torch.float32), rows(rng, (n, T, D), torch.float32)
+    y0, hidden = sim.gated_ff(x, *at, F, keep=True)
+    dx0 = sim.gated_ff_grad(dy, x, hidden, *at)
+    g0 = sim.G.clone()
+    x1 = x.clone()
+    x1[0, 2, 7] = bad
+    y1, _ = sim.gated_ff(x1, *at, F)
+    assert not torch.isfinite(y1[0, 2]).any()
+    y1[0, 2] = y0[0, 2]
+    assert torch.equal(y1, y0)
+    sim.gated_ff_grad(dy, x1, hidden, *at)
+    assert torch.isnan(sim.G[0, at[0]:at[0] + 2 * D * F]).any() and torch.equal(sim.G[1], g0[1])
+    for which in range(2):
+        dy1, h1 = dy.clone(), hidden.clone()
+        (dy1 if which else h1)[1, 3, 5] = bad
+        dx1 = sim.gated_ff_grad(dy1, x, h1, *at)
+        assert torch.isnan(dx1[1, 3]).all()
+        dx1[1, 3] = dx0[1, 3]
+        assert torch.equal(dx1, dx0)
+        assert torch.isnan(sim.G[1, :3 * D * F]).all() and torch.equal(sim.G[0], g0[0])
+    # a matrix's infinity reaches its node alone
+    sim.X[1, at[0] + 5] = bad
+    y2, _ = sim.gated_ff(x, *at, F)
+    assert not torch.isfinite(y2[1]).any() and torch.equal(y2[0], y0[0])
+    dx2 = sim.gated_ff_grad(dy, x, hidden, *at)
+    assert not torch.isfinite(dx2[1]).any() and torch.equal(dx2[0], dx0[0])
+    sim.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [4, 80])
+def test_outputs_in_the_place_of_inputs(hx, T, dtype):
+    from paper_2105_09080_amd import binding as B
+    dt = TYPES[dtype][0]
+    n, D, F = 3, 24, 50
+    sim, at, *_, rng = make(hx, n, D, F, 2, 9)
+    x, dy = rows(rng, (n, T, D), dt), rows(rng, (n, T, D), dt)
+    y, hidden = sim.gated_ff(x, *at, F, keep=True)
+    dx = sim.gated_ff_grad(dy, x, hidden, *at)
+    code = {"f32": B.GPGA_F32, "bf16": B.GPGA_BF16}[dtype]
+    xy = x.clone()
+    B.gpga_gated_ff(sim.ctx, xy, T, D, F, D, code, B.GPGA_SILU, *at, None, xy)
+    assert torch.equal(xy, y)
+    for into in (dy, x):
+        d, xx = dy.clone(), x.clone()
+        out = d if into is dy else xx
+        B.gpga_gated_ff_grad(sim.ctx, d, xx, hidden, T, D, F, D, code, B.GPGA_SILU, *at, out, False)
+        assert torch.equal(out, dx)
+    sim.close()
+
+
+def test_no_tokens(hx):
+    n, D, F = 2, 9, 70
+    sim, at, *_ , rng = make(hx, n, D, F, 3, 1)
+    sim.G.fill_(2.0)
+    x = torch.empty(n, 0, D, device="cuda")
+    y, hidden = sim.gated_ff(x, *at, F, keep=True)
+    assert y.shape == (n, 0, D) and hidden.shape == (n, 0, 2 * F)
+    sim.gated_ff_grad(x, x, hidden, *at, accumulate=True)
+    assert bool((sim.G == 2.0).all())
+    sim.gated_ff_grad(x, x, hidden, *at)
+    assert not sim.G[:, 3:3 + 3 * D * F].any() and bool((sim.G[:, :3] == 2.0).all()) and bool((sim.G[:, 3 + 3 * D * F:] == 2.0).all())
+    sim.close()
+
+
+@pytest.mark.parametrize("n,T,D,F", [(64, 4300, 16, 8192), (16, 2700, 16, 8192)])
+def test_more_tokens_than_scratch_takes_at_once(hx, n, T, D, F):
+    """Scratch of some 4 GiB holds 3840 tokens of these 64 nodes forwards and 2560 of 16 backwards."""
+    sim, at, *_ = make(hx, 1, D, F, 0, 2)
+    X0 = sim.X.clone()
+    sim.close()
+    sim = hx.Simulation(n, X0.shape[1], topology="ring", H=4, lr=0.1)
+    sim.X.copy_(X0.expand(n, -1))
+    sim.X[:, ::7] *= 0.5
+    rng = torch.Generator(device="cuda")
+    rng.manual_seed(1)
+    x = torch.randn((n, T, D), device="cuda", generator=rng).to(torch.bfloat16)
+    backward = n == 16
+    y, hidden = sim.gated_ff(x, *at, F, keep=backward)
+    for i in (0, n // 2, n - 1):                                    # one node at a time in float64
+        w = [sim.X[i:i + 1, k:k + D * F].double() for k in at]
+        a, b = (torch.bmm(x[i:i + 1].double(), m.reshape(1, F, D).transpose(1, 2).contiguous()) for m in w[:2])
+        want = torch.bmm(a * torch.sigmoid(a) * b, w[2].reshape(1, D, F).transpose(1, 2).contiguous())
+        # rounding of y, 2^-8 of its value; operands in one piece each, 2^-11, of 8192 terms as often up as down: 8 sigma of the whole
+        assert float((y[i] - want[0]).norm() / want.norm()) <= 2.0 ** -8
+        assert float((y[i] - want[0]).abs().max()) <= 2.0 ** -8 * float(want.abs().max()) + 8 * 2.0 ** -10 * float(want.norm()) / (T * D) ** 0.5
+        if backward:
+            dy = torch.randn((n, T, D), device="cuda", generator=rng).to(torch.bfloat16)
+            dx = sim.gated_ff_grad(dy, x, hidden, *at)
+            a, b = hidden[i:i + 1, :, :F].double(), hidden[i:i + 1, :, F:].double()
+            s = torch.sigmoid(a)
+            dh = torch.bmm(dy[i:i + 1].double(), w[2].reshape(1, D, F))
+            da, db, h = dh * b * (s + a * s * (1 - s)), dh * a * s, a * s * b
+            want = torch.bmm(da, w[0].reshape(1, F, D)) + torch.bmm(db, w[1].reshape(1, F, D))
+            assert float((dx[i] - want[0]).norm() / want.norm()) <= 2.0 ** -8
+            grads = [torch.bmm(da.transpose(1, 2).contiguous(), x[i:i + 1].double()), torch.bmm(db.transpose(1, 2).contiguous(), x[i:i + 1].double()),
+                     torch.bmm(dy[i:i + 1].double().transpose(1, 2).contiguous(), h)]
+            for k in range(3):
+                got = sim.G[i, at[k]:at[k] + D * F].double()
+                # fp32 sums of 2700 terms, two pieces of an operand: errors as often up as down, (4 + sqrt(T)) 2^-24 of the norm at most
+                assert float((got - grads[k].reshape(-1)).norm() / grads[k].norm()) <= (8 + T ** 0.5) * E32
+    sim.close()
+
+
+@pytest.mark.parametrize("T", [3, 68])
+def test_rows_beyond_32_bit_offsets(hx, T):
+    """Rows 2^27 elements apart: the last ones begin beyond 2^32 bytes."""
+    n, D, F = 1, 20, 30
+    ld = (1 << 33) // (2 * T) + 5
+    sim, at, gate, up, down, rng = make(hx, n, D, F, 0, 8)
+    big = torch.empty(T * ld + 64, dtype=torch.bfloat16, device="cuda")
+    x = big.as_strided((n, T, D), (T * ld, ld, 1))
+    dense = rows(rng, (n, T, D), torch.bfloat16)
+    x.copy_(dense)
+    y, hidden = sim.gated_ff(x, *at, F, keep=True)
+    want, hid = sim.gated_ff(dense, *at, F, keep=True)
+    assert y.stride(1) == ld and torch.equal(y, want) and torch.equal(hidden, hid)
+    dx = sim.gated_ff_grad(y, x, hidden, *at)
+    assert torch.equal(dx, sim.gated_ff_grad(want, dense, hid, *at))
+    sim.close()
+
+
+def test_another_stream_and_device_state(hx):
+    """A simulation on a stream of its own, called while another one is current; inputs made and dropped on that one."""
+    n, T, D, F = 4, 130, 64, 96
+    own = torch.cuda.Stream()
+    sim, at, gate, up, down, rng = make(hx, n, D, F, 0, 4, stream=own)
+    x0, dy0 = rows(rng, (n, T, D), torch.float32), rows(rng, (n, T, D), torch.float32)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(own):
+        y0, h0 = sim.gated_ff(x0, *at, F, keep=True)
+        dx0 = sim.gated_ff_grad(dy0, x0, h0, *at)
+    own.synchronize()
+    g0 = sim.G.clone()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        x, dy = x0.clone(), dy0.clone()
+        own.wait_stream(torch.cuda.current_stream())
+        y, h = sim.gated_ff(x, *at, F, keep=True)
+        dx = sim.gated_ff_grad(dy, x, h, *at)
+        del x, dy
+        junk = [torch.full((n, T, D), 7.0, device="cuda") for _ in range(3)]
+        torch.cuda.current_stream().wait_stream(own)
+        assert torch.equal(y, y0) and torch.equal(dx, dx0) and torch.equal(sim.G, g0)
+        del junk
+    sim.close()
+
+
+@pytest.mark.parametrize("T", [6, 140])
+def test_captured_and_replayed(hx, T):
+    """Forward and backward in a graph, replayed on new inputs with eager calls that outgrow the scratch between."""
+    n, D, F = 3, 72, 100
+    stream = torch.cuda.Stream()
+    sim, at, gate, up, down, rng = make(hx, n, D, F, 0, 4, stream=stream)
+    x, dy = (rows(rng, (n, T, D), torch.bfloat16) for _ in range(2))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        y, h = sim.gated_ff(x, *at, F, keep=True)
+        dx = sim.gated_ff_grad(dy, x, h, *at)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            y, h = sim.gated_ff(x, *at, F, keep=True)
+            dx = sim.gated_ff_grad(dy, x, h, *at)
+        for r in range(4):
+            x.copy_(torch.randn((n, T, D), device="cuda").to(torch.bfloat16))
+            dy.copy_(torch.randn((n, T, D), device="cuda").to(torch.bfloat16))
+            graph.replay()
+            stream.synchronize()
+            got = [t.clone() for t in (y, h, dx, sim.G)]
+            big = torch.randn((n, 300 * (r + 1), D), device="cuda").to(torch.bfloat16)
+            yb, hb = sim.gated_ff(big, *at, F, keep=True)
+            sim.gated_ff_grad(big, big, hb, *at)
+            stream.synchronize()
+            ye, he = sim.gated_ff(x, *at, F, keep=True)
+            dxe = sim.gated_ff_grad(dy, x, he, *at)
+            stream.synchronize()
+            for a, b, name in zip(got, (ye, he, dxe, sim.G), ("y", "hidden", "dx", "G")):
+                assert torch.equal(a, b), (r, name)
+    sim.close()
+
+
+def test_gradients_against_differences(hx):
+    """dx and the matrices' gradients of L = sum(dy * y) along a direction, against (L(+e) - L(-e)) / 2e of the forward pass."""
+    n, T, D, F = 2, 70, 48, 80
+    sim, at, gate, up, down, rng = make(hx, n, D, F, 0, 12)
+    x, dy = rows(rng, (n, T, D), torch.float32), rows(rng, (n, T, D), torch.float32)
+    X0 = sim.X.clone()
+    y, hidden = sim.gated_ff(x, *at, F, act="gelu", keep=True)
+    dx = sim.gated_ff_grad(dy, x, hidden, *at, act="gelu")
+    G = sim.G.clone()
+    e = 2.0 ** -7
+
+    def loss(x, X):
+        sim.X.copy_(X)
+        return float((dy.double() * sim.gated_ff(x, *at, F, act="gelu")[0].double()).sum())
+
+    dirx = rows(rng, (n, T, D), torch.float32)
+    size = float((dy.double().abs() * y.double().abs()).sum())
+    # the loss is a smooth function: its third derivative times e^2 / 6, and the forward pass's 2^-20 of the terms over e
+    got, want = (loss(x + e * dirx, X0) - loss(x - e * dirx, X0)) / (2 * e), float((dx.double() * dirx.double()).sum())
+    assert abs(got - want) <= 2e-3 * max(abs(want), float((dx.double() * dirx.double()).norm())) + 2.0 ** -20 * size / e
+    for k in range(3):
+        step = torch.zeros_like(X0)
+        step[:, at[k]:at[k] + D * F] = torch.as_tensor(rng.normal(size=(n, D * F)).astype(np.float32) * 0.1).cuda()
+        got = (loss(x, X0 + e * step) - loss(x, X0 - e * step)) / (2 * e)
+        want = float((G.double() * step.double()).sum())
+        assert abs(got - want) <= 2e-3 * max(abs(want), float((G.double() * step.double()).norm())) + 2.0 ** -20 * size / e, k
+    sim.close()
+
+
+def test_refusals(hx):
+    from paper_2105_09080_amd import binding as B
+    n, T, D, F = 2, 4, 8, 12
+    sim, at, *_, rng = make(hx, n, D, F, 0, 1)
+    x, dy = rows(rng, (n, T, D), torch.float32), rows(rng, (n, T, D), torch.float32)
+    y, hidden = sim.gated_ff(x, *at, F, keep=True)
+    good = dict(x=x, T=T, D=D, F=F, ld=D, dtype=0, act=0, g=at[0], u=at[1], d=at[2], hidden=hidden, y=y)
+
+    def forward(**kw):
+        a = {**good, **kw}
+        B.gpga_gated_ff(sim.ctx, a["x"], a["T"], a["D"], a["F"], a["ld"], a["dtype"], a["act"], a["g"], a["u"], a["d"], a["hidden"], a["y"])
+
+    def backward(**kw):
+        a = {**good, "dy": dy, "dx": torch.empty_like(x), "accumulate": 0, **kw}
+        B.gpga_gated_ff_grad(sim.ctx, a["dy"], a["x"], a["hidden"], a["T"], a["D"], a["F"], a["ld"], a["dtype"], a["act"], a["g"], a["u"],
+                             a["d"], a["dx"], a["accumulate"])
+
+    both = [dict(T=-1), dict(D=0), dict(F=0), dict(F=-3), dict(ld=D - 1), dict(dtype=3), dict(act=2), dict(act=-1), dict(g=-1), dict(u=at[2] + 10),
+            dict(d=sim.d - D * F + 1), dict(x=None), dict(F=(1 << 21) + 1), dict(D=(1 << 21) + 1, ld=1 << 22), dict(F=1 << 20, D=1 << 11, ld=1 << 11),
+            dict(x=x.data_ptr() + 2), dict(hidden=hidden.data_ptr() + 2)]
+    for call, more in ((forward, [dict(y=None), dict(hidden=x), dict(hidden=y), dict(y=sim.g), dict(hidden=sim._bufs[0]), dict(y=x.data_ptr() + 4)]),
+                       (backward, [dict(dy=None), dict(hidden=None), dict(dx=None), dict(accumulate=2), dict(u=at[0] + 1), dict(dx=hidden), dict(dy=sim.g),
+                                   dict(x=sim.g), dict(hidden=sim.g), dict(dx=sim._bufs[0]), dict(dx=x.data_ptr() + 4)])):
+        call()
+        before = sim.G.clone()
+        for bad in both + more:
+            with pytest.raises(B.GpgaError) as e:
+                call(**bad)
+            assert e.value.status == B.GPGA_EINVAL, bad
+        torch.cuda.synchronize()
+        assert torch.equal(sim.G, before)
+    for bad in (dict(act="relu"), dict(F=0)):
+        with pytest.raises((ValueError, B.GpgaError)):
+            sim.gated_ff(x, *at, bad.get("F", F), act=bad.get("act", "silu"))
+    for h in (hidden[..., :-1], hidden[:, :2], hidden.double(), hidden.transpose(1, 2)):
+        with pytest.raises(ValueError, match="hidden"):
+            sim.gated_ff_grad(dy, x, h, *at)
     sim.close()

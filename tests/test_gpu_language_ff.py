@@ -1,0 +1,126 @@
+"""The language model example with a feed-forward block and orthogonalised updates: its trajectory against one made of the float64
+oracles (operators and iteration), a captured iteration, and that it runs."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import gpga_oracle, matrix_oracle, token_oracle as orc
+from paper_2105_09080_amd import inputs
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lm():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2105_09080_amd import language
+    return language
+
+
+def oracle_gradients(X, tokens, previous, labels, model, k):
+    n, V, D, F = X.shape[0], model.V, model.D, model.ff
+    scale = math.sqrt(D)
+    E, table2 = X[:, :V * D].reshape(n, V, D), X[:, V * D:2 * V * D].reshape(n, V, D)
+    gamma, beta = X[:, model.gamma:model.beta], X[:, model.beta:model.gate]
+    gate, up = (X[:, at:at + F * D].reshape(n, F, D) for at in (model.gate, model.up))
+    down = X[:, model.down:].reshape(n, D, F)
+    u = orc.dropout(orc.embed(E, tokens, scale), orc.embed(table2, previous, scale), model.p, model.seed, 0, k)
+    y, mean, rstd = orc.layer_norm(u, gamma, beta, 1e-5)
+    h, a, b = matrix_oracle.gated_ff(y, gate, up, down, model.act)
+    v = y + h
+    loss, dz = orc.token_loss(np.matmul(v, E.transpose(0, 2, 1)), labels)
+    dv = np.matmul(dz, E)
+    dx, dgate, dup, ddown = matrix_oracle.gated_ff_grad(dv, y, a, b, gate, up, down, model.act)
+    if model.orthogonal:
+        p, eps = [float(np.float32(c)) for c in (3.4445, -4.7750, 2.0315)], float(np.float32(1e-7))
+        dgate, dup = (matrix_oracle.orthogonalize(g, None, 0.0, False, 5, p, eps, model.update_scale(F, D))[0] for g in (dgate, dup))
+        ddown = matrix_oracle.orthogonalize(ddown, None, 0.0, False, 5, p, eps, model.update_scale(D, F))[0]
+    du, dgamma, dbeta = orc.layer_norm_grad(dv + dx, u, mean, rstd, gamma)
+    dE = np.matmul(dz.transpose(0, 2, 1), v) + orc.embed_grad(tokens, orc.dropout(du, None, model.p, model.seed, 0, k), V, scale)[0]
+    dF = orc.embed_grad(previous, du, V, scale)[0]
+    flat = lambda *g: [w.reshape(n, -1) for w in g]
+    return loss, np.concatenate(flat(dE, dF) + [dgamma, dbeta] + flat(dgate, dup, ddown), axis=1)
+
+
+@pytest.mark.parametrize("act,orthogonal", [("silu", False), ("gelu", True)])
+def test_trajectory_against_the_oracles(lm, act, orthogonal):
+    """Gradients: fp32 throughout, as in the model without the block.  Orthogonalised ones: a gradient that is off by 1e-5 of its norm
+    moves singular values by as much, and five steps enlarge what is small by at most 3.4445^5 = 485; of D = 12 singular values none is
+    smaller than 1e-3 of the norm here or it weighs 1e-3 * 485 at most."""
+    n, V, D, T = 4, 23, 12, 5
+    text = inputs.markov_text(T, n, 3, 9, V, seed=1)
+    model = lm.NextTokenModel(n, V, D, H=3, lr=0.05, momentum=0.9, p=0.2, seed=3, ff=40, act=act, orthogonal=orthogonal)
+    tables = model.batches(text)
+    ref = gpga_oracle.GossipPGA(n, model.sim.d, topology="ring", H=3, lr=0.05, momentum=0.9, x0=model.sim.X[0].cpu().numpy())
+    for k in range(T):
+        tokens, previous, labels = (t[k] for t in tables)
+        loss = model.gradients(tokens, previous, labels)
+        torch.cuda.synchronize()
+        want, G = oracle_gradients(model.sim.X.double().cpu().numpy(), tokens.cpu().numpy(), previous.cpu().numpy(),
+                                   labels.cpu().numpy(), model, k)
+        assert np.allclose(loss.cpu().numpy(), want, rtol=1e-5)
+        got = model.sim.G.double().cpu().numpy()
+        plain = slice(0, model.gate)
+        assert np.linalg.norm(got[:, plain] - G[:, plain]) <= 1e-5 * np.linalg.norm(G[:, plain])
+        rest = slice(model.gate, None)
+        tol = 485 * 1e-5 if orthogonal else 1e-5
+        assert np.linalg.norm(got[:, rest] - G[:, rest]) <= tol * np.linalg.norm(G[:, rest])
+        model.sim.step()
+        ref.step(got)
+        X = model.sim.X.double().cpu().numpy()
+        assert np.linalg.norm(X - ref.X) <= 1e-5 * np.linalg.norm(ref.X)
+
+
+def test_two_iterations_replayed_from_a_graph(lm):
+    """An even number of iterations with their steps in a graph, replayed with eager work between: the same bits as without.  Every
+    replay of the graph has the dropout masks of its capture, so there is none here."""
+    n, V, D = 8, 100, 64
+    text = inputs.markov_text(8, n, 2, 33, V, seed=5)
+    models = [lm.NextTokenModel(n, V, D, H=2, lr=0.05, p=0.0, dtype=torch.bfloat16, ff=200, orthogonal=True, stream=torch.cuda.Stream())
+              for _ in range(2)]
+    tables = [m.batches(text) for m in models]
+    fixed = [t[0].clone() for t in tables[1]]
+    fixed2 = [t[0].clone() for t in tables[1]]
+    torch.cuda.synchronize()
+
+    def two(m, first, second):
+        for b in (first, second):
+            m.gradients(*b)
+            m.sim.step()
+
+    eager, captured = models
+    two(eager, [t[0] for t in tables[0]], [t[1] for t in tables[0]])
+    for dst, src in zip(fixed + fixed2, [t[0] for t in tables[1]] + [t[1] for t in tables[1]]):
+        dst.copy_(src)
+    torch.cuda.synchronize()
+    two(captured, fixed, fixed2)
+    captured.sim.stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=captured.sim.stream):
+        two(captured, fixed, fixed2)
+    for r in range(1, 4):
+        for dst, src in zip(fixed + fixed2, [t[2 * r] for t in tables[1]] + [t[2 * r + 1] for t in tables[1]]):
+            dst.copy_(src)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(captured.sim.stream):
+            graph.replay()
+        two(eager, [t[2 * r] for t in tables[0]], [t[2 * r + 1] for t in tables[0]])
+        captured.losses(*(t[7] for t in tables[1]))                # eager work on the same scratch
+        torch.cuda.synchronize()
+        assert torch.equal(eager.sim.X, captured.sim.X), r
+        assert bool(torch.isfinite(eager.sim.X).all())
+
+
+@pytest.mark.parametrize("dtype,adaptive", [(torch.float32, False), (torch.bfloat16, True)])
+def test_it_runs(lm, dtype, adaptive):
+    n, V = 8, 100
+    model = lm.NextTokenModel(n, V, 64, H=4, lr=0.1, p=0.1, dtype=dtype, ff=192, orthogonal=True)
+    text = inputs.markov_text(41, n, 8, 32, V, seed=2)
+    records = list(lm.train(model, text[:40], every=20, adaptive=adaptive))
+    assert [r["iteration"] for r in records] == [20, 40] and all(math.isfinite(r["loss"]) for r in records)
+    held_out = model.losses(*(t[40] for t in model.batches(text)))
+    torch.cuda.synchronize()
+    assert held_out.shape == (n,) and bool(torch.isfinite(held_out).all())

@@ -81,3 +81,136 @@ def test_update(hx, n, rows, cols, count, off, kind, mu, nesterov, steps, coeffi
         close = np.abs(velocity.double().cpu().numpy() - v.reshape(n, size)) <= 2.0 ** -23 * (np.abs(mu * v0) + np.abs(before[:, off:off + size]))
         assert close.all()
     sim.close()
+
+
+def test_zeros_infinities_and_nan_stay_in_their_matrix(hx):
+    for rows, cols in ((40, 60), (130, 90), (300, 70)):
+        n, count = 2, 2
+        size = rows * cols
+        sim = hx.Simulation(n, count * size, topology="ring", H=4, lr=0.1)
+        rng = np.random.default_rng(3)
+        G = rng.normal(size=(n, count * size)).astype(np.float32)
+        sim.set_state(G=G)
+        sim.orthogonalize(0, rows, cols, count=count)
+        fine = sim.G.clone()
+        G[0, :size] = 0.0
+        G[1, 5], G[1, size + 7] = np.inf, np.nan
+        sim.set_state(G=G)
+        sim.orthogonalize(0, rows, cols, count=count, eps=0.0)
+        assert not sim.G[0, :size].any() and torch.isnan(sim.G[1]).all()
+        assert float((sim.G[0, size:] - fine[0, size:]).abs().max()) <= 1e-4
+        sim.close()
+
+
+def test_singular_vectors_stay(hx):
+    """U = P diag(s) Q^T with s from 0.05 to 1 of the largest: the polynomial, five times over, of s / |s| and the same P and Q."""
+    n, rows, cols = 2, 96, 200
+    rng = np.random.default_rng(11)
+    P, Q = (np.linalg.qr(rng.normal(size=(n, k, rows)))[0] for k in (rows, cols))
+    s = np.linspace(1.0, 0.05, rows)
+    sim = hx.Simulation(n, rows * cols, topology="ring", H=4, lr=0.1)
+    sim.set_state(G=((P * s) @ Q.transpose(0, 2, 1)).reshape(n, -1).astype(np.float32))
+    sim.orthogonalize(0, rows, cols, eps=0.0)
+    z = s / np.sqrt((s * s).sum())
+    for _ in range(5):
+        z = QUINTIC[0] * z + QUINTIC[1] * z ** 3 + QUINTIC[2] * z ** 5
+    got = sim.G.double().cpu().numpy().reshape(n, rows, cols)
+    want = (P * z) @ Q.transpose(0, 2, 1)
+    far = np.sqrt(((got - want) ** 2).sum(axis=(1, 2)))
+    # the input's own rounding, 2^-24 of elements, is enlarged like any other error of the first step
+    assert far.max() <= tolerance(rows, cols, 5, QUINTIC, 1.0) + 2.0 ** -24 * QUINTIC[0] ** 5
+    assert 0.6 < np.linalg.svd(got, compute_uv=False).min() and np.linalg.svd(got, compute_uv=False).max() < 1.3
+    sim.close()
+
+
+def test_more_matrices_than_scratch_takes_at_once(hx):
+    """Some 4 GiB hold 255 matrices of 1024 x 1024; the 260th comes out like the first, which it equals."""
+    n, side, count = 52, 1024, 5
+    sim = hx.Simulation(n, count * side * side, topology="ring", H=4, lr=0.1)
+    one = torch.randn((2, side * side), device="cuda")
+    for k in range(count):
+        sim.G[:, k * side * side:(k + 1) * side * side] = one[k % 2]
+    sim.orthogonalize(0, side, side, count=count)
+    first, second = sim.G[0, :side * side].clone(), sim.G[0, side * side:2 * side * side].clone()
+    for i in (0, 25, 50, 51):
+        for k in range(count):
+            got = sim.G[i, k * side * side:(k + 1) * side * side]
+            assert float((got - (second if k % 2 else first)).norm()) <= tolerance(side, side, 5, QUINTIC, 1.0), (i, k)
+    sim.close()
+
+
+@pytest.mark.parametrize("rows,cols", [(50, 60), (200, 330)])
+def test_captured_replayed_and_on_another_stream(hx, rows, cols):
+    n, size = 3, rows * cols
+    stream = torch.cuda.Stream()
+    sim = hx.Simulation(n, size, topology="ring", H=4, lr=0.1, stream=stream)
+    v, g = torch.randn((n, size), device="cuda"), torch.randn((n, size), device="cuda")
+    torch.cuda.synchronize()
+
+    def step():
+        sim.G.copy_(g)
+        sim.orthogonalize(0, rows, cols, velocity=v, mu=0.9, nesterov=True)
+
+    with torch.cuda.stream(stream):
+        step()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        for r in range(4):
+            g.copy_(torch.randn((n, size), device="cuda"))
+            v0 = v.clone()
+            graph.replay()
+            stream.synchronize()
+            got, gv = sim.G.clone(), v.clone()
+            sim.G.copy_(torch.randn((n, size), device="cuda"))
+            sim.orthogonalize(0, cols, rows)                         # eager work on the same scratch
+            v.copy_(v0)
+            step()
+            stream.synchronize()
+            assert torch.equal(got, sim.G) and torch.equal(gv, v), r
+        want, wv = sim.G.clone(), v.clone()
+        v.copy_(v0)
+        sim.G.copy_(g)
+    torch.cuda.current_stream().wait_stream(stream)
+    other = v.clone()
+    stream.wait_stream(torch.cuda.current_stream())
+    sim.orthogonalize(0, rows, cols, velocity=other, mu=0.9, nesterov=True)      # torch's current stream is another one
+    torch.cuda.synchronize()
+    assert torch.equal(sim.G, want) and torch.equal(other, wv)
+    sim.close()
+
+
+def test_refusals(hx):
+    from paper_2105_09080_amd import binding as B
+    n, rows, cols = 2, 6, 9
+    sim = hx.Simulation(n, 3 * rows * cols, topology="ring", H=4, lr=0.1)
+    sim.G.normal_()
+    v = torch.zeros((n, 2 * rows * cols), device="cuda")
+    good = dict(off=0, rows=rows, cols=cols, count=2, v=v, mu=0.9, nesterov=1, steps=5, a=QUINTIC[0], b=QUINTIC[1], c=QUINTIC[2], eps=1e-7, scale=1.0)
+
+    def call(**kw):
+        a = {**good, **kw}
+        B.gpga_orthogonalize(sim.ctx, a["off"], a["rows"], a["cols"], a["count"], a["v"], a["mu"], a["nesterov"], a["steps"], a["a"], a["b"],
+                             a["c"], a["eps"], a["scale"])
+
+    call()
+    before, vb = sim.G.clone(), v.clone()
+    inf, nan = float("inf"), float("nan")
+    for bad in (dict(off=-1), dict(off=rows * cols + 1), dict(rows=0), dict(cols=-2), dict(count=0), dict(count=4), dict(rows=(1 << 21) + 1), dict(mu=1.0),
+                dict(mu=-0.1), dict(mu=nan), dict(v=None), dict(v=None, mu=0.0), dict(mu=0.0), dict(nesterov=2), dict(steps=-1), dict(steps=65),
+                dict(a=inf), dict(b=nan), dict(c=inf), dict(a=100.0), dict(a=3.0, b=3.0), dict(eps=-1.0), dict(eps=inf), dict(scale=nan), dict(scale=inf),
+                dict(v=v.data_ptr() + 2), dict(v=sim.g), dict(v=sim._bufs[1])):
+        with pytest.raises(B.GpgaError) as e:
+            call(**bad)
+        assert e.value.status == B.GPGA_EINVAL, bad
+    for wide in (2 ** 31, 2 ** 32 + 6):
+        with pytest.raises(B.GpgaError, match="32 bits"):
+            call(rows=wide)
+    for wrong in (v[:, :-1], v.double(), v.t(), v[:1]):
+        with pytest.raises(ValueError, match="velocity"):
+            sim.orthogonalize(0, rows, cols, count=2, velocity=wrong, mu=0.9)
+    torch.cuda.synchronize()
+    assert torch.equal(sim.G, before) and torch.equal(v, vb)
+    call(v=None, mu=0.0, nesterov=0)
+    sim.close()
