@@ -70,44 +70,58 @@ struct PackMatrices {
 };
 constexpr int kMaxParts = 256;
 
-template <typename E, int PGU, int PD>
-__global__ __launch_bounds__(kThreads) void k_ff_pack_matrices(PackMatrices a) {
-    const uint32_t block = a.first_block + blockIdx.x, node = block / a.per_node;
-    const int32_t in = (int32_t)(block % a.per_node), wave = threadIdx.x / kWave;
-    const int32_t D2 = padded(a.D), F2 = padded(a.F);
-    if (in < (int32_t)a.gu_blocks) {
-        const int32_t row = in * kPackRows + wave, f = row < F2 ? row : row - F2;
-        const float* from = (row < F2 ? a.gate : a.up) + (int64_t)node * a.ldx + (int64_t)f * a.D;
-        half_t* to = a.gu + ((int64_t)node * 2 * F2 + row) * D2;
-        Scale s = {0.f, 0.f};
-        if (a.node_max) {
-            const float* part = a.node_max + (int64_t)node * kMaxParts;
-            const int lane = threadIdx.x & (kWave - 1);
-            s = scale_for(wave_all<kWave>(max_nan(max_nan(part[lane], part[64 + lane]), max_nan(part[128 + lane], part[192 + lane])), max_nan));
-        }
-        const RowStat r = pack_row<E, PGU>(from, f < a.F ? a.D : 0, D2, nullptr, a.node_max ? &s : nullptr, to, a.gu_plane);
-        if ((threadIdx.x & (kWave - 1)) == 0) {
-            a.gu_inv[(int64_t)node * 2 * F2 + row] = r.down;
-        }
-        if (a.norms) {
-            const float most = block_max(r.norm * r.down);
-            if (threadIdx.x == 0) a.norms[(int64_t)node * a.gu_blocks + in] = most;
-        }
-    } else {
-        const int32_t row = (in - (int32_t)a.gu_blocks) * kPackRows + wave;
-        const RowStat r = pack_row<E, PD>(a.down + (int64_t)node * a.ldx + (int64_t)row * a.F, row < a.D ? a.F : 0, F2, nullptr, nullptr,
-                                          a.wd + ((int64_t)node * D2 + row) * F2, a.wd_plane);
-        if ((threadIdx.x & (kWave - 1)) == 0) a.wd_inv[(int64_t)node * D2 + row] = r.down;
+// Workgroup `in` of a node's for gate and up.
+template <typename E, int P>
+__device__ __forceinline__ void pack_gate_up(const PackMatrices& a, int64_t node, int32_t in) {
+    const int32_t D2 = padded(a.D), F2 = padded(a.F), row = in * kPackRows + threadIdx.x / kWave, f = row < F2 ? row : row - F2;
+    const int lane = threadIdx.x & (kWave - 1);
+    const float* from = (row < F2 ? a.gate : a.up) + node * a.ldx + (int64_t)f * a.D;
+    Scale s = {0.f, 0.f};
+    if (a.node_max) {
+        const float* part = a.node_max + node * kMaxParts;
+        s = scale_for(wave_all<kWave>(max_nan(max_nan(part[lane], part[64 + lane]), max_nan(part[128 + lane], part[192 + lane])), max_nan));
+    }
+    const RowStat r = pack_row<E, P>(from, f < a.F ? a.D : 0, D2, nullptr, a.node_max ? &s : nullptr, a.gu + (node * 2 * F2 + row) * D2, a.gu_plane);
+    if (lane == 0) a.gu_inv[node * 2 * F2 + row] = r.down;
+    if (a.norms) {
+        const float most = block_max(r.norm * r.down);
+        if (threadIdx.x == 0) a.norms[node * a.gu_blocks + in] = most;
     }
 }
+// And for the down matrix.
+template <typename E, int P>
+__device__ __forceinline__ void pack_down(const PackMatrices& a, int64_t node, int32_t in) {
+    const int32_t D2 = padded(a.D), F2 = padded(a.F), row = in * kPackRows + threadIdx.x / kWave;
+    const RowStat r = pack_row<E, P>(a.down + node * a.ldx + (int64_t)row * a.F, row < a.D ? a.F : 0, F2, nullptr, nullptr, a.wd + (node * D2 + row) * F2,
+                                     a.wd_plane);
+    if ((threadIdx.x & (kWave - 1)) == 0) a.wd_inv[node * D2 + row] = r.down;
+}
 
-// Largest |gate| and |up| of a node, in kMaxParts parts.
-__global__ __launch_bounds__(kThreads) void k_ff_max(const float* gate, const float* up, int64_t ldx, int64_t count, float* part, uint32_t first) {
+// Forward: all three.
+template <typename E, int P>
+__global__ __launch_bounds__(kThreads) void k_ff_pack_matrices(PackMatrices a) {
+    const uint32_t block = a.first_block + blockIdx.x;
+    const int64_t node = block / a.per_node;
+    const int32_t in = (int32_t)(block % a.per_node);
+    if (in < (int32_t)a.gu_blocks) pack_gate_up<E, P>(a, node, in);
+    else pack_down<E, P>(a, node, in - (int32_t)a.gu_blocks);
+}
+
+// Backward, first: the down matrix, and the largest |gate| and |up| of a node in kMaxParts parts.
+template <typename E>
+__global__ __launch_bounds__(kThreads) void k_ff_pack_down(PackMatrices a, float* parts) {
     typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
-    const uint32_t block = first + blockIdx.x, node = block / kMaxParts, p = block % kMaxParts;
-    const float* from[2] = {gate + (int64_t)node * ldx, up + (int64_t)node * ldx};
+    const uint32_t block = a.first_block + blockIdx.x;
+    const int64_t node = block / a.per_node;
+    const int32_t p = (int32_t)(block % a.per_node);
+    if (p >= kMaxParts) {
+        pack_down<E, 2>(a, node, p - kMaxParts);
+        return;
+    }
+    const float* from[2] = {a.gate + node * a.ldx, a.up + node * a.ldx};
     float m = 0.f;
-    const int64_t fours = count / 4, at = (int64_t)p * kThreads + threadIdx.x;
+    const int64_t count = (int64_t)a.F * a.D, fours = count / 4, at = (int64_t)p * kThreads + threadIdx.x;
+#pragma unroll 2
     for (int64_t e = at; e < fours; e += (int64_t)kMaxParts * kThreads)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -116,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void k_ff_max(const float* gate, const fl
         }
     if (at < count % 4) m = max_nan(m, max_nan(fabsf(from[0][fours * 4 + at]), fabsf(from[1][fours * 4 + at])));
     m = block_max(m);
-    if (threadIdx.x == 0) part[block] = m;
+    if (threadIdx.x == 0) parts[node * kMaxParts + p] = m;
 }
 
 // Rows of activations of a chunk of tokens: kRowsEach for each of a workgroup's wavefronts.
@@ -155,15 +169,21 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_x(PackRows a, const float*
     }
 }
 
-// Backward: dy times the scales of the down matrix's rows as halves, and the scales of its token's rows of [da | db] and h, from
+// Backward, second: gate and up by the node's largest value; dy times the scales of the down matrix's rows as halves, and the scales of its
+// token's rows of [da | db] and h, from
 // |dh| <= sum |dy| |w| and the largest |a|, |b| of the token.  For the products over tokens, da = da' / up and so on leaves factors
 // that go into the other operand (k_ff_pack_tokens): the largest |x| / up and |dy| / up of a workgroup's tokens.
 template <typename E, int P>
-__global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackRows a, const float* wd_inv, const void* x, const void* hidden, int32_t F,
+__global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackMatrices w, uint32_t matrix_blocks, PackRows a, const float* wd_inv, const void* x, const void* hidden, int32_t F,
                                                          int64_t hidden_node, float* da_up, float* da_inv, float* h_up, float* h_inv, float* part) {
     typedef typename E::mem M;
     const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1), rows2 = padded(a.rows);
-    const uint32_t block = a.first_block + blockIdx.x;
+    uint32_t block = a.first_block + blockIdx.x;
+    if (block < matrix_blocks) {
+        pack_gate_up<Elem<float, E::kNarrow>, P>(w, block / w.gu_blocks, (int32_t)(block % w.gu_blocks));
+        return;
+    }
+    block -= matrix_blocks;
     const int64_t node = block / a.per_node;
     float px = 0.f, py = 0.f;
     {
@@ -262,7 +282,7 @@ struct FfProduct {
 
 // h = act(x Wg^T) (x Wu^T): a wavefront's blocks of 32 columns are gate and up of the same 32 f's in turn.
 template <typename S, typename E, int Act, int PH>
-__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_up(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, 2) void k_ff_up(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     static_assert(S::NI == 2, "gate and up");
     int32_t node, ti, tj;
@@ -298,10 +318,9 @@ __global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_up
 
 // Activations out: rows' scales times columns' scales (col_batch < 0: one a node).
 template <typename S, typename E>
-__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_rows(FfProduct a) {
-    __shared__ __align__(16) char lds[2 * S::Stage];
+__device__ __forceinline__ void rows_product(const FfProduct& a, uint32_t block, char* lds) {
     int32_t node, ti, tj;
-    if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
+    if (!a.grid.at(block, &node, &ti, &tj)) return;
     const int32_t m0 = ti * S::BM, n0 = tj * S::BN;
     acc16 acc[S::NI][S::MI];
     product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return min(n0 + row, a.B.rows - 1); });
@@ -316,10 +335,16 @@ __global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_ro
     });
 }
 
+template <typename S, typename E>
+__global__ __launch_bounds__(S::Threads, 2) void k_ff_rows(FfProduct a) {
+    __shared__ __align__(16) char lds[2 * S::Stage];
+    rows_product<S, E>(a, a.first_block + blockIdx.x, lds);
+}
+
 // dh = dy Wd, and from it and the kept [a | b] the rows of [da | db] and h as halves.  Rows behind the last token are zeros: the
 // products over tokens take them along.
 template <typename S, typename E, int Act, int PA, int PH>
-__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_down_grad(FfProduct a) {
+__global__ __launch_bounds__(S::Threads, 2) void k_ff_down_grad(FfProduct a) {
     __shared__ __align__(16) char lds[2 * S::Stage];
     int32_t node, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
@@ -359,10 +384,9 @@ __global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_do
 // Gradients of matrices: rows of the gate's block, then (from F' on) of the up's; or of the down matrix's alone (off1 < 0).
 // G: fp32, narrow where a row of the matrix is.
 template <typename S, typename G>
-__global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_matrix_grad(FfProduct a) {
-    __shared__ __align__(16) char lds[2 * S::Stage];
+__device__ __forceinline__ void matrix_grad(const FfProduct& a, uint32_t block, char* lds) {
     int32_t node, ti, tj;
-    if (!a.grid.at(a.first_block + blockIdx.x, &node, &ti, &tj)) return;
+    if (!a.grid.at(block, &node, &ti, &tj)) return;
     const int32_t m0 = ti * S::BM, n0 = tj * S::BN;
     acc16 acc[S::NI][S::MI];
     product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return row; });
@@ -385,6 +409,26 @@ __global__ __launch_bounds__(S::Threads, S::Threads >= 256 ? 2 : 1) void k_ff_ma
         }
         piece_put<kOct, G>(to, col, a.N, v);
     });
+}
+
+// dx, the gradients of gate and up and that of down wait for the same things only, and are one launch: 7 x 333 tokens, 511 x 1021, fp32, took 37
+// and twice 28 us by themselves.
+template <bool WithX, typename SX, typename SG, typename SD, typename E>
+__global__ __launch_bounds__(SG::Threads, 2) void k_ff_grads(FfProduct x, FfProduct g, FfProduct d) {
+    constexpr int kG = SG::Stage > SD::Stage ? SG::Stage : SD::Stage, kLds = WithX && SX::Stage > kG ? SX::Stage : kG;
+    static_assert(SX::Threads == SG::Threads && SX::Threads == SD::Threads, "one shape of workgroup");
+    __shared__ __align__(16) char lds[2 * kLds];
+    typedef Elem<float, E::kNarrow> G;
+    uint32_t block = g.first_block + blockIdx.x;
+    if constexpr (WithX) {
+        if (block < x.grid.blocks()) {
+            rows_product<SX, E>(x, block, lds);
+            return;
+        }
+        block -= x.grid.blocks();
+    }
+    if (block < g.grid.blocks()) matrix_grad<SG, G>(g, block, lds);
+    else matrix_grad<SD, G>(d, block - g.grid.blocks(), lds);
 }
 
 __global__ __launch_bounds__(kThreads) void k_ff_zero(float* g, int64_t g_ld, int64_t off0, int64_t off1, int64_t off2, int64_t count, uint32_t per_node,
@@ -680,20 +724,50 @@ PackMatrices pack_matrices(const gpga_ctx* c, const FfShape& s, const FfScratch&
     return a;
 }
 
-template <int PGU, int PD>
-hipError_t launch_pack_matrices(const gpga_ctx* c, const FfShape& s, PackMatrices a) {
-    return launch_blocks((uint64_t)a.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
-        a.first_block = first;
-        if (s.D < kOct || s.F < kOct) k_ff_pack_matrices<Elem<float, true>, PGU, PD><<<grid, dim3(kThreads), 0, c->stream>>>(a);
-        else k_ff_pack_matrices<Elem<float, false>, PGU, PD><<<grid, dim3(kThreads), 0, c->stream>>>(a);
-    });
-}
-
 #define GPGA_LAUNCH(call)                        \
     do {                                         \
         const hipError_t e_ = (call);            \
         if (e_ != hipSuccess) return e_;         \
     } while (0)
+
+// The three products of the backward pass on tiles of one side: what all tiles take on all compute units and, for the end, half of the
+// longest one.
+template <int PDX, int PGU, int PX, typename E>
+hipError_t launch_grads(const gpga_ctx* c, FfProduct& x, FfProduct& g, FfProduct& d, int32_t T, int32_t D2, int32_t F2) {
+    // one plane of each operand makes tiles whose steps are longer: with them two workgroups of 128 x 128 fit a compute unit in place of
+    // three (8 x 4096 tokens, 768 x 2048, bf16: 1110 us together, 302 and 667 apart)
+    constexpr bool kWithX = PDX + PGU > 2;
+    if constexpr (!kWithX)
+        GPGA_LAUNCH((launch_product<PDX, PGU, false, true>(c, x, T, D2, [&](auto tile, dim3 grid) {
+            typedef decltype(tile) S;
+            k_ff_rows<S, E><<<grid, dim3(S::Threads), 0, c->stream>>>(x);
+        })));
+    int side = 0;
+    double best = 0.;
+    for (int t = 0; t < 3; ++t) {
+        const TileTime a(t, PDX + PGU, T, D2, x.K, c->n, false), b(t, 2 + PX, 2 * F2, D2, g.K, c->n, false), e(t, PX + 2, D2, F2, d.K, c->n, false);
+        double us = ((kWithX ? a.tiles * a.us : 0.) + b.tiles * b.us + e.tiles * e.us) / c->num_cus + 0.5 * (kWithX ? fmax(a.us, b.us) : b.us);
+        if (t == 0) us = fmax(us, fmax(kWithX ? TileTime::alone(PDX + PGU, x.K) : 0., TileTime::alone(2 + PX, g.K)));
+        if (t == 0 || us < best) {
+            best = us;
+            side = 64 << t;
+        }
+    }
+    if (kWithX) x.grid.set(T, D2, side, c->n, false);
+    g.grid.set(2 * F2, D2, side, c->n, false);
+    d.grid.set(D2, F2, side, c->n, false);
+    auto launch = [&](auto sx, auto sg, auto sd) {
+        typedef decltype(sx) SX;
+        const uint64_t blocks = (uint64_t)(kWithX ? x.grid.blocks() : 0) + g.grid.blocks() + d.grid.blocks();
+        return launch_blocks(blocks, SX::Threads, [&](uint32_t first, dim3 grid) {
+            g.first_block = first;
+            k_ff_grads<kWithX, SX, decltype(sg), decltype(sd), E><<<grid, dim3(SX::Threads), 0, c->stream>>>(x, g, d);
+        });
+    };
+    if (side == 256) return launch(Tile256<PDX, PGU, false, true>(), Tile256<2, PX, true, true>(), Tile256<PX, 2, true, true>());
+    if (side == 128) return launch(Tile128<PDX, PGU, false, true>(), Tile128<2, PX, true, true>(), Tile128<PX, 2, true, true>());
+    return launch(Tile64<PDX, PGU, false, true>(), Tile64<2, PX, true, true>(), Tile64<PX, 2, true, true>());
+}
 
 template <typename E, int NB>
 hipError_t few(const gpga_ctx* c, const FfShape& s, const void* x, void* hidden, void* y, float* h) {
@@ -748,7 +822,11 @@ hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hid
     size_t bytes;
     const FfScratch w = carve_ff(s, false, scratch, &bytes);
     const int32_t D2 = padded(s.D), F2 = padded(s.F);
-    GPGA_LAUNCH((launch_pack_matrices<PW, PW>(c, s, pack_matrices(c, s, w))));
+    PackMatrices m = pack_matrices(c, s, w);
+    GPGA_LAUNCH(launch_blocks((uint64_t)m.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+        m.first_block = first;
+        k_ff_pack_matrices<Elem<float, E::kNarrow>, PW><<<grid, dim3(kThreads), 0, c->stream>>>(m);
+    }));
     for (int32_t t0 = 0; t0 < s.T; t0 += w.chunk) {
         const int32_t T = s.T - t0 < w.chunk ? s.T - t0 : w.chunk, T2 = padded(T);
         PackRows p = {static_cast<const M*>(x) + (int64_t)t0 * s.ld, s.ld, (int64_t)s.T * s.ld, T, s.D, w.x, (int64_t)s.n * T2 * D2, w.x_inv,
@@ -808,19 +886,22 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
     const FfScratch w = carve_ff(s, true, scratch, &bytes);
     const int32_t D2 = padded(s.D), F2 = padded(s.F);
     const int64_t n = s.n;
-    GPGA_LAUNCH(launch_blocks((uint64_t)kMaxParts * s.n, kThreads, [&](uint32_t first, dim3 grid) {
-        k_ff_max<<<grid, dim3(kThreads), 0, c->stream>>>(c->x + s.gate_off, c->x + s.up_off, c->ld, (int64_t)s.F * s.D, w.node_max, first);
+    PackMatrices m = pack_matrices(c, s, w);
+    m.per_node = kMaxParts + (uint32_t)(D2 / kPackRows);
+    GPGA_LAUNCH(launch_blocks((uint64_t)m.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+        m.first_block = first;
+        k_ff_pack_down<Elem<float, E::kNarrow>><<<grid, dim3(kThreads), 0, c->stream>>>(m, w.node_max);
     }));
-    GPGA_LAUNCH((launch_pack_matrices<PGU, 2>(c, s, pack_matrices(c, s, w))));
     for (int32_t t0 = 0; t0 < s.T; t0 += w.chunk) {
         const int32_t T = s.T - t0 < w.chunk ? s.T - t0 : w.chunk, T2 = padded(T);
         const int64_t skip = (int64_t)t0 * s.ld;
         const M* hid = static_cast<const M*>(hidden) + (int64_t)t0 * 2 * s.F;
         const int64_t hidden_node = (int64_t)s.T * 2 * s.F;
         PackRows p = {static_cast<const M*>(dy) + skip, s.ld, (int64_t)s.T * s.ld, T, s.D, w.dy, n * T2 * D2, w.x_inv, (uint32_t)(T2 / kPackRows), 0};
-        GPGA_LAUNCH(launch_blocks((uint64_t)p.per_node * s.n, kThreads, [&](uint32_t first, dim3 grid) {
+        const uint32_t matrix_blocks = t0 ? 0 : m.gu_blocks * (uint32_t)s.n;
+        GPGA_LAUNCH(launch_blocks((uint64_t)p.per_node * s.n + matrix_blocks, kThreads, [&](uint32_t first, dim3 grid) {
             p.first_block = first;
-            k_ff_pack_dy<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(p, w.wd_inv, static_cast<const M*>(x) + skip, hid, s.F, hidden_node, w.da_up,
+            k_ff_pack_dy<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(m, matrix_blocks, p, w.wd_inv, static_cast<const M*>(x) + skip, hid, s.F, hidden_node, w.da_up,
                                                                         w.da_inv, w.h_up, w.h_inv, w.part);
         }));
         p.per_node /= kRowsEach;
@@ -868,10 +949,6 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         b.out = static_cast<M*>(dx) + skip;
         b.out_ld = s.ld;
         b.out_node = (int64_t)s.T * s.ld;
-        GPGA_LAUNCH((launch_product<PDX, PGU, false, true>(c, b, T, D2, [&](auto tile, dim3 grid) {
-            typedef decltype(tile) S;
-            k_ff_rows<S, E><<<grid, dim3(S::Threads), 0, c->stream>>>(b);
-        })));
         FfProduct g = {};
         g.A = rows_operand(w.da, n, T2, 2 * F2);
         g.B = rows_operand(w.tok_x, n, T2, D2);
@@ -884,21 +961,15 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         g.off0 = s.gate_off;
         g.off1 = s.up_off;
         g.accumulate = accumulate || t0 > 0;
-        GPGA_LAUNCH((launch_product<2, PX, true, true>(c, g, 2 * F2, D2, [&](auto tile, dim3 grid) {
-            typedef decltype(tile) S;
-            k_ff_matrix_grad<S, Elem<float, E::kNarrow>><<<grid, dim3(S::Threads), 0, c->stream>>>(g);
-        })));
-        g.A = rows_operand(w.tok_y, n, T2, D2);
-        g.B = rows_operand(w.h, n, T2, F2);
-        g.M = s.D;
-        g.N = s.F;
-        g.row_inv = w.node_inv + n;
-        g.off0 = s.down_off;
-        g.off1 = -1;
-        GPGA_LAUNCH((launch_product<PX, 2, true, true>(c, g, D2, F2, [&](auto tile, dim3 grid) {
-            typedef decltype(tile) S;
-            k_ff_matrix_grad<S, Elem<float, E::kNarrow>><<<grid, dim3(S::Threads), 0, c->stream>>>(g);
-        })));
+        FfProduct d = g;
+        d.A = rows_operand(w.tok_y, n, T2, D2);
+        d.B = rows_operand(w.h, n, T2, F2);
+        d.M = s.D;
+        d.N = s.F;
+        d.row_inv = w.node_inv + n;
+        d.off0 = s.down_off;
+        d.off1 = -1;
+        GPGA_LAUNCH((launch_grads<PDX, PGU, PX, E>(c, b, g, d, T, D2, F2)));
     }
     return hipSuccess;
 }

@@ -38,10 +38,11 @@ struct Operand {
 };
 
 // WM x WN wavefronts share a tile's rows and columns, KW such groups the terms of a step.
-template <int kBM, int kBN, int kWM, int kWN, int kBK, int kPA, int kPB, bool kColsA, bool kColsB, int kKW = 1>
+template <int kBM, int kBN, int kWM, int kWN, int kBK, int kPA, int kPB, bool kColsA, bool kColsB, int kKW = 1, bool kFull = false>
 struct Tile {
     static constexpr int BM = kBM, BN = kBN, WM = kWM, WN = kWN, BK = kBK, PA = kPA, PB = kPB, KW = kKW;
     static constexpr bool ColsA = kColsA, ColsB = kColsB;
+    static constexpr bool Full = kFull;  // lo lo too
     static constexpr int Waves = WM * WN, Threads = Waves * KW * kWave;
     static constexpr int MI = BM / WM / 32, NI = BN / WN / 32;             // 32 x 32 blocks of a wavefront
     static constexpr int BytesA = BM * BK * 2, BytesB = BN * BK * 2;       // of a plane
@@ -181,7 +182,7 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
             for (int pa = 0; pa < S::PA; ++pa)
 #pragma unroll
                 for (int pb = 0; pb < S::PB; ++pb) {
-                    if (pa + pb == 2) continue;
+                    if (pa + pb == 2 && !S::Full) continue;
 #pragma unroll
                     for (int j = 0; j < S::NI; ++j)
 #pragma unroll
@@ -318,7 +319,7 @@ struct TileGrid {
     __host__ __device__ int32_t one() const { return tn ? tm * tn : tm * (tm + 1) / 2; }
     static constexpr uint32_t kXcds = 8;
     static constexpr int32_t kGroup = 8;
-    __host__ uint32_t blocks() const { return (total + kXcds - 1) / kXcds * kXcds; }
+    __host__ __device__ uint32_t blocks() const { return (total + kXcds - 1) / kXcds * kXcds; }
     // false: none is left for this workgroup
     __device__ __forceinline__ bool at(uint32_t block, int32_t* batch, int32_t* i, int32_t* j) const {
         const uint32_t per = (total + kXcds - 1) / kXcds, id = block % kXcds * per + block / kXcds;
@@ -357,21 +358,30 @@ using Tile64 = Tile<64, 64, 2, 1, 64, PA, PB, CA, CB, 2>;
 // kAlone.  us for 256, 128, 64: one plane each, 8 x 4096 x 4096 x 768 304, 346, 449; 8 x 4096 x 768 x 2048 163, 157, 220;
 // 8 x 8192 x 1024 x 4096 558, 644, 956; three planes, 8 x 4096 x 2048 x 768 449, 420, 559; 2 x 11264 x 2048 x 2048 421, 412, 589; four
 // planes, 5 x 513 x 257 x 1023 71, 30, 15.5; 16 x 1024 x 1024 x 1024 110, 120, 185.
+struct TileTime {
+    double tiles, us;  // tiles of a product, us each
+    // t: side 64 << t
+    TileTime(int t, int planes, int64_t rows, int64_t cols, int64_t K, int64_t batch, bool lower) {
+        static constexpr double kRate[3][3] = {{3.8, 9.8, 33.5}, {6.8, 16.5, 65.}, {11.5, 25., 85.}}, kEnds[3][3] = {{0.8, 3.5, 12.}, {2.5, 10., 60.}, {1., 7., 20.}};
+        const int64_t s = 64 << t, i = (rows + s - 1) / s, j = (cols + s - 1) / s;
+        tiles = (double)((lower ? i * (i + 1) / 2 : i * j) * batch);
+        us = kRate[planes - 2][t] * 1e-3 * (double)K + kEnds[planes - 2][t];
+    }
+    static double alone(int planes, int64_t K) {
+        static constexpr double kAlone[3] = {6., 8.5, 11.};
+        return kAlone[planes - 2] * 1e-3 * (double)K + 3.;
+    }
+};
 inline int tile_side(int num_cus, int planes, int64_t rows, int64_t cols, int64_t K, int64_t batch, bool lower) {
-    static constexpr double kRate[3][3] = {{3.8, 9.8, 33.5}, {6.8, 16.5, 65.}, {10., 25., 85.}}, kEnds[3][3] = {{0.8, 3.5, 12.}, {2.5, 10., 60.}, {1., 7., 20.}};
-    static constexpr double kAlone[3] = {6., 8.5, 11.};
-    const double k = (double)K * 1e-3;
-    const int p = planes - 2;
     double best = 0.;
     int side = 0;
     for (int t = 0; t < 3; ++t) {
-        const int64_t s = 64 << t, i = (rows + s - 1) / s, j = (cols + s - 1) / s;
-        const int64_t tiles = (lower ? i * (i + 1) / 2 : i * j) * batch;
-        double us = (double)((tiles + num_cus - 1) / num_cus) * (kRate[p][t] * k + kEnds[p][t]);
-        if (t == 0 && us < kAlone[p] * k + 3.) us = kAlone[p] * k + 3.;
+        const TileTime tile(t, planes, rows, cols, K, batch, lower);
+        double us = ceil(tile.tiles / num_cus) * tile.us;
+        if (t == 0 && us < TileTime::alone(planes, K)) us = TileTime::alone(planes, K);
         if (t == 0 || us < best) {
             best = us;
-            side = (int)s;
+            side = 64 << t;
         }
     }
     return side;
