@@ -392,7 +392,7 @@ gpga_status gpga_query(gpga_ctx* ctx, const char* name, double* value_out);
  * an input, another output or a bound array is EINVAL (columns of one wider array do not overlap), and so are inputs of a
  * gradient within g_dev.  tokens_dev and
  * labels_dev are n x T int32.  Results do not depend on the order in which workgroups run: the same call gives the same
- * bits.  Asynchronous on the bound stream; the embedding's and the layer norm's gradients and the loss use scratch, which
+ * bits.  Asynchronous on the bound stream; the embedding's and the layer norm's gradients, the loss and the operators with matrices use scratch, which
  * grows with the largest call and stays until gpga_destroy (a first call of its size cannot be captured into a graph).  All
  * calls of a context share it: after gpga_bind with another stream, and for a graph that is replayed on another stream, the
  * caller sees to it that they follow each other.
@@ -457,15 +457,18 @@ gpga_status gpga_token_loss(gpga_ctx* ctx, const void* logits_dev, const int32_t
  * 1 <= D, F <= 2^21, D*F with both rounded up to multiples of 64 below 2^30.
  * Products are made of fp16 pieces of the operands, scaled by powers of two, with fp32 sums: with fp32 activations two
  * pieces each (2^-22 of an operand's largest value in its row), with fp16 two of one operand and one (2^-11) of the other, with bf16 one
- * each; the gradients of the matrices take two whatever the type.  A token with an infinity or NaN in its row of x, or whose |a b| may
- * pass 2^126, gets NaN; so does all of a node whose matrices hold an infinity. */
+ * each; the gradients of the matrices take two whatever the type.  A token with an infinity or NaN in its row of x has no finite
+ * result, and may have none where |x| times the largest |row| of Wg_i or Wu_i (2-norms) passes 2^63; other tokens are not touched.
+ * An infinity or NaN in a matrix leaves no finite y that it enters.  Scratch: the matrices in fp16 pieces, and up to some 4 GiB for tokens
+ * (more go through in turn); up to 64 tokens a node need n*T*F floats only. */
 typedef enum { GPGA_SILU = 0, GPGA_GELU = 1 } gpga_activation;
 gpga_status gpga_gated_ff(gpga_ctx* ctx, const void* x_dev, int32_t T, int32_t D, int32_t F, int64_t ld, int32_t dtype,
                           int32_t act, int64_t gate_off, int64_t up_off, int64_t down_off, void* hidden_dev, void* y_dev);
 /* Backward, from the gradient dy of y, x and the kept [a | b]: with dh = Wd_i^T dy, da = dh * b * act'(a) and db = dh * act(a),
  * dx = Wg_i^T da + Wu_i^T db, and into g_dev the sums over the node's tokens dWg_i = sum da x^T, dWu_i = sum db x^T,
- * dWd_i = sum dy h^T.  The three column blocks must not overlap.  T = 0 leaves zeros (or, added, nothing).  An infinity or NaN in dy, x
- * or hidden makes the node's gradients NaN. */
+ * dWd_i = sum dy h^T.  The three column blocks must not overlap.  T = 0 leaves zeros (or, added, nothing).  An infinity or NaN in dy or
+ * hidden makes its token's dx and the node's gradients NaN, one in x those of Wg_i and Wu_i, one in a matrix the node's dx and
+ * possibly its gradients. */
 gpga_status gpga_gated_ff_grad(gpga_ctx* ctx, const void* dy_dev, const void* x_dev, const void* hidden_dev, int32_t T,
                                int32_t D, int32_t F, int64_t ld, int32_t dtype, int32_t act, int64_t gate_off,
                                int64_t up_off, int64_t down_off, void* dx_dev, int32_t accumulate);

@@ -81,7 +81,7 @@ __device__ __forceinline__ void pack_gate_up(const PackMatrices& a, int64_t node
         const float* part = a.node_max + node * kMaxParts;
         s = scale_for(wave_all<kWave>(max_nan(max_nan(part[lane], part[64 + lane]), max_nan(part[128 + lane], part[192 + lane])), max_nan));
     }
-    const RowStat r = pack_row<E, P>(from, f < a.F ? a.D : 0, D2, nullptr, a.node_max ? &s : nullptr, a.gu + (node * 2 * F2 + row) * D2, a.gu_plane);
+    const RowStat r = pack_row<E, P>(from, f < a.F ? a.D : 0, D2, nullptr, !a.node_max, s, a.gu + (node * 2 * F2 + row) * D2, a.gu_plane);
     if (lane == 0) a.gu_inv[node * 2 * F2 + row] = r.down;
     if (a.norms) {
         const float most = block_max(r.norm * r.down);
@@ -92,7 +92,7 @@ __device__ __forceinline__ void pack_gate_up(const PackMatrices& a, int64_t node
 template <typename E, int P>
 __device__ __forceinline__ void pack_down(const PackMatrices& a, int64_t node, int32_t in) {
     const int32_t D2 = padded(a.D), F2 = padded(a.F), row = in * kPackRows + threadIdx.x / kWave;
-    const RowStat r = pack_row<E, P>(a.down + node * a.ldx + (int64_t)row * a.F, row < a.D ? a.F : 0, F2, nullptr, nullptr, a.wd + (node * D2 + row) * F2,
+    const RowStat r = pack_row<E, P>(a.down + node * a.ldx + (int64_t)row * a.F, row < a.D ? a.F : 0, F2, nullptr, true, {}, a.wd + (node * D2 + row) * F2,
                                      a.wd_plane);
     if ((threadIdx.x & (kWave - 1)) == 0) a.wd_inv[node * D2 + row] = r.down;
 }
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_x(PackRows a, const float*
         const int32_t row = ((int32_t)(block % a.per_node) * kRowsEach + k) * kPackRows + threadIdx.x / kWave;
         const int64_t at = node * rows2 + row;
         const typename E::mem* from = static_cast<const typename E::mem*>(a.src) + node * a.node + (int64_t)row * a.ld;
-        const RowStat r = pack_row<E, P>(from, row < a.rows ? a.cols : 0, cols2, nullptr, nullptr, a.dst + at * cols2, a.plane);
+        const RowStat r = pack_row<E, P>(from, row < a.rows ? a.cols : 0, cols2, nullptr, true, {}, a.dst + at * cols2, a.plane);
         if (lane == 0) {
             const float most = r.norm * r.down * w;
             const Scale s = scale_for(most * most * 1.0001f);
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackMatrices w, uint32_
             xm = row_max<E>(static_cast<const M*>(x) + from, a.cols);
             ym = row_max<E>(static_cast<const M*>(a.src) + from, a.cols);
         }
-        const RowStat r = pack_row<E, P>(static_cast<const M*>(a.src) + from, real ? a.cols : 0, cols2, wd_inv + node * cols2, nullptr,
+        const RowStat r = pack_row<E, P>(static_cast<const M*>(a.src) + from, real ? a.cols : 0, cols2, wd_inv + node * cols2, true, {},
                                          a.dst + at * cols2, a.plane);
         const float dh = r.sum * r.down * 32768.f * 1.0001f;
         const Scale sa = scale_for(dh * max_nan(1.14f * bm, am)), sh = scale_for(am * bm);
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_tokens(PackTokens t) {
         const float inv = row < a.rows ? t.row_inv[which][at] : 0.f;
         const Scale s = {inv * node_scale.up, 0.f};
         const typename E::mem* src = static_cast<const typename E::mem*>(a.src) + node * a.node + (int64_t)row * a.ld;
-        pack_row<E, P>(src, row < a.rows ? a.cols : 0, cols2, nullptr, &s, a.dst + at * cols2, a.plane);
+        pack_row<E, P>(src, row < a.rows ? a.cols : 0, cols2, nullptr, false, s, a.dst + at * cols2, a.plane);
         if (row == 0 && (threadIdx.x & (kWave - 1)) == 0) a.inv[node] = node_scale.down;
     }
 }
@@ -505,7 +505,7 @@ struct FewArgs {
 
 // EX: type of the operand that is read, E: of the result; Mats = 2: gate and up, 1: down.  NB: blocks of 16 tokens.
 template <typename EX, typename E, int Mats, int Act, int PW, int PX, int NB, int Waves>
-__global__ __launch_bounds__(Waves * kWave, NB == 1 ? 4 : NB == 2 ? 3 : 2) void k_ff_few(FewArgs a) {
+__global__ __launch_bounds__(Waves * kWave, (NB == 1 ? 4 : NB == 2 ? 3 : 2) - (PX == 3 && NB < 4 ? 1 : 0)) void k_ff_few(FewArgs a) {
     const uint32_t block = a.first_block + blockIdx.x;
     const int64_t node = block / a.per_node;
     const int32_t row0 = (int32_t)(block % a.per_node) * 16, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -615,11 +615,13 @@ struct Carve {
     }
 };
 
-// Tokens of a node that go through together: scratch stays below some 4 GiB (and the least of a tile, whatever the width).
+// Tokens of a node that go through together: scratch stays below some 4 GiB (and the least of a tile, whatever the width), and every
+// workgroup of k_ff_pack_tokens reads a number of every four of them.
 int32_t chunk_tokens(const FfShape& s, int64_t halves) {
+    constexpr int64_t kMost = 1 << 16;
     const int64_t bytes = 2 * halves * s.n;
     const int64_t most = ((int64_t)4 << 30) / bytes / 256 * 256;
-    const int64_t want = most < 256 ? 256 : most;
+    const int64_t want = most < 256 ? 256 : most < kMost ? most : kMost;
     return s.T < want ? s.T : (int32_t)want;
 }
 

@@ -76,8 +76,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_norm(OrthArgs a) {
     if (threadIdx.x == 0) a.squares[block] = s[0];
 }
 
-// 1 / (sqrt(squares) + eps) as a product of two floats: of a norm below 2^-100 the reciprocal may be none.  0 for a matrix of zeros, NaN for
-// one with an infinity or NaN.
+// 1 / (sqrt(squares) + eps) as a product of two floats: of a norm beyond 2^100 or below 2^-100 the reciprocal may be subnormal or none.  0 for
+// a matrix of zeros, NaN for one with an infinity or NaN.
 struct Reciprocal {
     float first, second;
 };
@@ -85,6 +85,7 @@ __device__ __forceinline__ Reciprocal reciprocal(double squares, float eps) {
     if (squares == 0.0) return {0.f, 0.f};
     const double norm = sqrt(squares) + (double)eps;
     if (!(norm < INFINITY)) return {NAN, NAN};
+    if (norm > 0x1p100) return {0x1p-100f, (float)(0x1p100 / norm)};
     return norm < 0x1p-100 ? Reciprocal{0x1p100f, (float)(0x1p-100 / norm)} : Reciprocal{1.f, (float)(1.0 / norm)};
 }
 
@@ -207,7 +208,7 @@ template <int M2, int KMax, int Waves>
 __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
     constexpr int kBlocks = (M2 / 32) * (KMax / 32) / Waves, kGramBlocks = (M2 / 32) * (M2 / 32);
     static_assert(kBlocks * Waves == (M2 / 32) * (KMax / 32) && kGramBlocks <= 2 * Waves, "blocks");
-    constexpr int kGramEach = (kGramBlocks + Waves - 1) / Waves;
+    constexpr int kGramEach = (kGramBlocks + Waves - 1) / Waves, kUnroll = KMax == 64 ? 4 : 1;  // more spills registers
     __shared__ __align__(16) half_t sx[2][M2 * KMax];
     __shared__ __align__(16) half_t sg[2][M2 * M2];
     __shared__ double s_sum[Waves];
@@ -302,6 +303,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
                 const int block = wave + n * Waves;
                 if (block >= kGramBlocks) continue;
                 const int row0 = block / (M2 / 32) * 32, col0 = block % (M2 / 32) * 32;
+#pragma unroll(kUnroll)
                 for (int kk = 0; kk < width / 16; ++kk) {
                     const half8 fa[2] = {rows8(p0, row0, kk, width), rows8(p1, row0, kk, width)};
                     const half8 fb[2] = {rows8(p0, col0, kk, width), rows8(p1, col0, kk, width)};
@@ -325,7 +327,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
             const int block = wave + n * Waves;
             if (block >= M2 / 32 * across) continue;
             const int row0 = block / across * 32, col0 = block % across * 32;
-#pragma unroll
+#pragma unroll(kUnroll)
             for (int kk = 0; kk < M2 / 16; ++kk) {
                 const half8 fa[2] = {rows8(sg[0], row0, kk, M2), rows8(sg[1], row0, kk, M2)};
                 const half8 fb[2] = {cols8(sx[0], col0, kk), cols8(sx[1], col0, kk)};
@@ -411,7 +413,7 @@ OrthScratch carve(const OrthShape& s, char* base, size_t* bytes) {
 // Matrices that one workgroup holds.
 bool small_fits(const OrthShape& s) {
     const int32_t R2 = padded(s.R), C2 = padded(s.C), m2 = R2 < C2 ? R2 : C2, k2 = R2 < C2 ? C2 : R2;
-    return m2 == 64 ? k2 <= 512 : k2 == 128;
+    return m2 == 64 ? k2 <= 256 : k2 == 128;
 }
 
 // Power of two that brings values of at most `bound` to 2^14 or below.
@@ -528,7 +530,7 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             e = launch_blocks((uint64_t)matrices, waves * kWave, [&](uint32_t first, dim3 grid) {
                 f.o.first_block = first;
                 if (f.k2 == 64) k_orth_small<64, 64, 4><<<grid, dim3(256), 0, c->stream>>>(f);
-                else if (m2 == 64) k_orth_small<64, 512, 8><<<grid, dim3(512), 0, c->stream>>>(f);
+                else if (m2 == 64) k_orth_small<64, 256, 8><<<grid, dim3(512), 0, c->stream>>>(f);
                 else k_orth_small<128, 128, 8><<<grid, dim3(512), 0, c->stream>>>(f);
             });
             if (e != hipSuccess) return e;

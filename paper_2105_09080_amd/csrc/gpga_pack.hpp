@@ -24,10 +24,10 @@ __device__ __forceinline__ float row_max(const typename E::mem* row, int32_t col
     return wave_all<kWave>(m, max_nan);
 }
 
-// `cols` values, times fold[column] if there is one, times the row's scale (or `given`), into `cols2` halves and as many in the
+// `cols` values, times fold[column] if there is one, times the row's scale (or `given`, where that is not `own`), into `cols2` halves and as many in the
 // second plane; zeros behind the values.
 template <typename E, int Planes>
-__device__ __forceinline__ RowStat pack_row(const typename E::mem* row, int32_t cols, int32_t cols2, const float* fold, const Scale* given, half_t* to,
+__device__ __forceinline__ RowStat pack_row(const typename E::mem* row, int32_t cols, int32_t cols2, const float* fold, bool own, Scale given, half_t* to,
                                             int64_t plane) {
     const int32_t lane = (int32_t)(threadIdx.x & (kWave - 1));
     auto read = [&](int32_t c, float* v) {
@@ -43,8 +43,8 @@ __device__ __forceinline__ RowStat pack_row(const typename E::mem* row, int32_t 
         }
     };
     Scale s;
-    if (given) {
-        s = *given;
+    if (!own) {
+        s = given;
     } else {
         float m = 0.f;
         for (int32_t c = lane * kOct; c < cols; c += kWave * kOct) {

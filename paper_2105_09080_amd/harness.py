@@ -337,6 +337,8 @@ class Simulation:
         T, D, ld, dt = self._rows(x)
         if act not in B.ACTIVATION:
             raise ValueError(f"act must be one of {sorted(B.ACTIVATION)}, got {act!r}")
+        if not 1 <= F <= 1 << 21:
+            raise ValueError(f"F must be 1..2^21, got {F}")
         foreign = self._foreign()
         y = self._like(x, ld, foreign)
         hidden = self._empty((self.n, T, 2 * F), x.dtype, foreign) if keep else None

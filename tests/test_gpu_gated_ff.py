@@ -205,6 +205,25 @@ def test_scales_far_apart(hx, T, dtype):
     sim.close()
 
 
+@pytest.mark.parametrize("T", [6, 70])
+def test_one_column_far_above_the_others(hx, T):
+    """A column of x 2^20 times the others meets zeros in both matrices: what is left comes from pieces that are subnormal in fp16."""
+    n, D, F = 2, 72, 90
+    sim, at, gate, up, down, rng = make(hx, n, D, F, 1, T)
+    for w, k in ((gate, 0), (up, 1)):
+        w[:, :, 3] = 0.0
+        sim.X[:, at[k]:at[k] + D * F].copy_(torch.as_tensor(w.reshape(n, -1)).float())
+    x = rows(rng, (n, T, D), torch.float32)
+    x[..., 3] *= 2.0 ** 20
+    y, hidden = sim.gated_ff(x, *at, F, keep=True)
+    (wy, wa, wb), (ty, ta, tb) = forward_tolerances(host(x), gate, up, down, "silu", "f32")
+    assert np.median(ta / np.abs(wa)) < 1e-4                        # the tolerance tells
+    close(hidden[..., :F], wa, ta + E32 * np.abs(wa), "a")
+    close(hidden[..., F:], wb, tb + E32 * np.abs(wb), "b")
+    close(y, wy, ty + E32 * np.abs(wy), "y")
+    sim.close()
+
+
 @pytest.mark.parametrize("T", [5, 66])
 @pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
 def test_infinities_and_nan_stay_in_their_token(hx, bad, T):
@@ -452,8 +471,8 @@ def test_refusals(hx):
             assert e.value.status == B.GPGA_EINVAL, bad
         torch.cuda.synchronize()
         assert torch.equal(sim.G, before)
-    for bad in (dict(act="relu"), dict(F=0)):
-        with pytest.raises((ValueError, B.GpgaError)):
+    for bad in (dict(act="relu"), dict(F=0), dict(F=-4), dict(F=1 << 22)):
+        with pytest.raises(ValueError):
             sim.gated_ff(x, *at, bad.get("F", F), act=bad.get("act", "silu"))
     for h in (hidden[..., :-1], hidden[:, :2], hidden.double(), hidden.transpose(1, 2)):
         with pytest.raises(ValueError, match="hidden"):

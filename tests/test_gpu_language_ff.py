@@ -75,43 +75,60 @@ def test_trajectory_against_the_oracles(lm, act, orthogonal):
 
 
 def test_two_iterations_replayed_from_a_graph(lm):
-    """An even number of iterations with their steps in a graph, replayed with eager work between: the same bits as without.  Every
-    replay of the graph has the dropout masks of its capture, so there is none here."""
-    n, V, D = 8, 100, 64
-    text = inputs.markov_text(8, n, 2, 33, V, seed=5)
-    models = [lm.NextTokenModel(n, V, D, H=2, lr=0.05, p=0.0, dtype=torch.bfloat16, ff=200, orthogonal=True, stream=torch.cuda.Stream())
-              for _ in range(2)]
-    tables = [m.batches(text) for m in models]
-    fixed = [t[0].clone() for t in tables[1]]
-    fixed2 = [t[0].clone() for t in tables[1]]
-    torch.cuda.synchronize()
+    """Norm, feed-forward block, their gradients, orthogonalised updates with momentum and the step, an even number of iterations in a
+    graph, replayed on new inputs with eager work on the same scratch between: the same bits as without."""
+    from paper_2105_09080_amd.harness import Simulation
+    n, T, D, F = 6, 70, 64, 200
+    gamma, beta, gate, up, down = 0, D, 2 * D, 2 * D + F * D, 2 * D + 2 * F * D
+    x0 = inputs.initial_point(2 * D + 3 * F * D, 4) / math.sqrt(D)
+    x0[:D], x0[D:2 * D] = 1.0, 0.0
 
-    def two(m, first, second):
-        for b in (first, second):
-            m.gradients(*b)
-            m.sim.step()
+    class Run:
+        def __init__(self):
+            self.sim = Simulation(n, x0.size, topology="ring", H=2, lr=0.02, x0=x0, stream=torch.cuda.Stream())
+            self.x, self.want = (torch.zeros((n, T, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            self.v = torch.zeros((n, 2 * F * D), device="cuda")
+            torch.cuda.synchronize()
 
-    eager, captured = models
-    two(eager, [t[0] for t in tables[0]], [t[1] for t in tables[0]])
-    for dst, src in zip(fixed + fixed2, [t[0] for t in tables[1]] + [t[1] for t in tables[1]]):
-        dst.copy_(src)
-    torch.cuda.synchronize()
-    two(captured, fixed, fixed2)
-    captured.sim.stream.synchronize()
+        def inputs(self, r):
+            g = torch.Generator(device="cuda")
+            g.manual_seed(r)
+            self.x.copy_(torch.randn((n, T, D), device="cuda", generator=g))
+            self.want.copy_(torch.randn((n, T, D), device="cuda", generator=g))
+            torch.cuda.synchronize()
+
+        def two(self):
+            s = self.sim
+            with torch.cuda.stream(s.stream):
+                for _ in range(2):
+                    y, u, stats = s.layer_norm(self.x, gamma, beta)
+                    h, hidden = s.gated_ff(y, gate, up, down, F, act="gelu", keep=True)
+                    dy = s.gated_ff_grad((y + h - self.want) / T, y, hidden, gate, up, down, act="gelu")
+                    s.layer_norm_grad(dy, u, stats, gamma, beta)
+                    s.orthogonalize(gate, F, D, count=2, velocity=self.v, mu=0.9, nesterov=True)
+                    s.orthogonalize(down, D, F, scale=0.5)
+                    s.step()
+
+    eager, captured = Run(), Run()
+    for run in (eager, captured):
+        run.inputs(0)
+        run.two()
+        run.sim.stream.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=captured.sim.stream):
-        two(captured, fixed, fixed2)
+        captured.two()
     for r in range(1, 4):
-        for dst, src in zip(fixed + fixed2, [t[2 * r] for t in tables[1]] + [t[2 * r + 1] for t in tables[1]]):
-            dst.copy_(src)
-        torch.cuda.synchronize()
+        for run in (eager, captured):
+            run.inputs(r)
         with torch.cuda.stream(captured.sim.stream):
             graph.replay()
-        two(eager, [t[2 * r] for t in tables[0]], [t[2 * r + 1] for t in tables[0]])
-        captured.losses(*(t[7] for t in tables[1]))                # eager work on the same scratch
+            captured.sim.gated_ff(captured.x, gate, up, down, F)    # eager work on the same scratch
+        eager.two()
         torch.cuda.synchronize()
-        assert torch.equal(eager.sim.X, captured.sim.X), r
+        assert torch.equal(eager.sim.X, captured.sim.X) and torch.equal(eager.v, captured.v), r
         assert bool(torch.isfinite(eager.sim.X).all())
+    eager.sim.close()
+    captured.sim.close()
 
 
 @pytest.mark.parametrize("dtype,adaptive", [(torch.float32, False), (torch.bfloat16, True)])

@@ -43,6 +43,8 @@ def gradients(rng, k, rows, cols, kind):
         g *= 1e-33
     if kind == "huge":
         g *= 1e30
+    if kind == "largest":                                            # the norm passes fp32's range, the elements do not
+        g *= 5e37
     return g.astype(np.float32)
 
 
@@ -53,6 +55,10 @@ CASES = [  # n, rows, cols, count, off, kind of gradient, momentum, Nesterov, st
     (1, 257, 300, 1, 0, "tiny", None, False, 5, QUINTIC, 1.0), (1, 300, 257, 1, 0, "huge", None, False, 5, QUINTIC, -1.0),
     (3, 40, 600, 1, 7, "noise", 0.5, False, 3, CUBIC, 1.0), (3, 600, 40, 1, 7, "noise", 0.0, False, 8, CUBIC, 1.0),
     (2, 33, 20, 1, 0, "noise", 0.9, True, 0, QUINTIC, 3.0), (2, 128, 128, 2, 0, "noise", None, False, 1, QUINTIC, 1.0),
+    (2, 300, 200, 1, 0, "largest", None, False, 5, QUINTIC, 1.0), (2, 40, 64, 1, 0, "largest", None, False, 5, QUINTIC, 1.0),
+    (2, 40, 64, 1, 0, "tiny", None, False, 5, QUINTIC, 1.0), (3, 30, 1500, 1, 1, "noise", 0.9, True, 5, QUINTIC, 1.0), (3, 1500, 30, 1, 1, "noise", None, False, 5, QUINTIC, 1.0),
+    (3, 50, 256, 2, 1, "noise", 0.9, True, 5, QUINTIC, 1.0), (3, 250, 33, 1, 0, "strong", 0.9, False, 5, QUINTIC, 1.0), (2, 64, 257, 1, 0, "noise", None, False, 5, QUINTIC, 1.0),
+    (2, 100, 128, 2, 3, "noise", None, False, 5, QUINTIC, 1.0), (2, 128, 65, 1, 0, "strong", 0.5, True, 5, QUINTIC, 1.0), (300, 20, 30, 3, 0, "noise", None, False, 5, QUINTIC, 1.0),
     (40, 200, 900, 2, 0, "strong", None, False, 5, QUINTIC, 1.0), (40, 520, 300, 2, 1, "noise", 0.95, True, 5, QUINTIC, 1.0),
 ]
 
