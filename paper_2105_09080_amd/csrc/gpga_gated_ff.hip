@@ -169,10 +169,10 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_x(PackRows a, const float*
     }
 }
 
-// Backward, second: gate and up by the node's largest value; dy times the scales of the down matrix's rows as halves, and the scales of its
-// token's rows of [da | db] and h, from
-// |dh| <= sum |dy| |w| and the largest |a|, |b| of the token.  For the products over tokens, da = da' / up and so on leaves factors
-// that go into the other operand (k_ff_pack_tokens): the largest |x| / up and |dy| / up of a workgroup's tokens.
+// Backward, second: gate and up by the node's largest value; dy times the scales of the down matrix's rows as halves, and the scales of
+// its token's rows of [da | db] and h, from |dh| <= sum |dy| |w| and the largest |a|, |b| of the token.  For the products over tokens,
+// da = da' / up and so on leaves factors that go into the other operand (k_ff_pack_tokens): the largest |x| / up and |dy| / up of a
+// workgroup's tokens.
 template <typename E, int P>
 __global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackMatrices w, uint32_t matrix_blocks, PackRows a, const float* wd_inv, const void* x, const void* hidden, int32_t F,
                                                          int64_t hidden_node, float* da_up, float* da_inv, float* h_up, float* h_inv, float* part) {
@@ -441,10 +441,11 @@ __global__ __launch_bounds__(kThreads) void k_ff_zero(float* g, int64_t g_ld, in
 }
 
 // ---- few tokens ---------------------------------------------------------------------------------------------------------------
-// Up to kFewTokens tokens a node: every matrix is read once, as it lies in X, and that is what takes the time (4 nodes, 1024 x 4096, fp16, 1, 16,
-// 32 and 64 tokens: 42, 47, 63 and 87 us, the tiles' way 180 to 187; 20 nodes, 128 x 512: 10, 10, 13 and 18, the tiles' way 30 to 35).  A wavefront takes 16 rows of
-// a matrix (16 of gate and the same 16 of up), 64 columns at a time, as bf16 pieces made in registers, which need no scale: three of them
-// hold fp32, two go with bf16 activations.  The wavefronts of a workgroup share a row's columns and add their sums in LDS.
+// Up to kFewTokens tokens a node: every matrix is read once, as it lies in X, and that is what takes the time (4 nodes, 1024 x 4096, fp16,
+// 1, 16, 32 and 64 tokens: 42, 47, 63 and 87 us, the tiles' way 180 to 187; 20 nodes, 128 x 512: 10, 10, 13 and 18, the tiles' way 30 to
+// 35).  A wavefront takes 16 rows of a matrix (16 of gate and the same 16 of up), 64 columns at a time, as bf16 pieces made in registers,
+// which need no scale: three of them hold fp32, two go with bf16 activations.  The wavefronts of a workgroup share a row's columns and
+// add their sums in LDS.
 // A lane holds 16 neighbouring columns of a row, 64 bytes, four lanes a row; which of a matrix instruction's k's they are does not
 // matter as long as both operands agree.
 constexpr int32_t kFewTokens = 64;

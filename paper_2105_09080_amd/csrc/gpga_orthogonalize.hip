@@ -196,7 +196,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_scaled(OrthArgs a, float scal
 // one matrix of the short side's size that holds A and then q A + r A^2.  Results stay in registers until everybody has read what they
 // replace.  Pieces of 16 bytes lie within their row xored with fold(row), so that 16 lanes that read one piece of 16 rows, and 32 that read
 // 8 bytes each of 4 rows for the transposing read, meet every bank once (rows are odd or even multiples of 128 bytes, and the banks repeat
-// after 256).  20 matrices of 64 x 64 in five steps: 72 us as products of their own, a launch each.
+// after 256).  20 matrices in five steps, here and as products with a launch each: 64 x 64 25 and 72 us; 64 x 256 49, where 64 x 320 takes
+// 90 in launches; 128 x 128 77, 192 x 192 in launches 114.
 struct SmallArgs {
     OrthArgs o;
     int32_t k2;             // long side, padded
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
     __shared__ __align__(16) half_t sx[2][M2 * KMax];
     __shared__ __align__(16) half_t sg[2][M2 * M2];
     __shared__ double s_sum[Waves];
-    const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave, k2 = a.k2;
+    const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave, k2 = KMax == M2 ? KMax : a.k2;
     const int32_t m = (int32_t)(a.o.first_block + blockIdx.x), b = a.o.first + m;
     const int64_t size = (int64_t)a.o.R * a.o.C;
     float* g = block_of(a.o.g, a.o.ld, b, a.o.count, size);
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
                 const int block = wave + n * Waves;
                 if (block >= kGramBlocks) continue;
                 const int row0 = block / (M2 / 32) * 32, col0 = block % (M2 / 32) * 32;
-#pragma unroll(kUnroll)
+#pragma unroll kUnroll
                 for (int kk = 0; kk < width / 16; ++kk) {
                     const half8 fa[2] = {rows8(p0, row0, kk, width), rows8(p1, row0, kk, width)};
                     const half8 fb[2] = {rows8(p0, col0, kk, width), rows8(p1, col0, kk, width)};
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
             const int block = wave + n * Waves;
             if (block >= M2 / 32 * across) continue;
             const int row0 = block / across * 32, col0 = block % across * 32;
-#pragma unroll(kUnroll)
+#pragma unroll kUnroll
             for (int kk = 0; kk < M2 / 16; ++kk) {
                 const half8 fa[2] = {rows8(sg[0], row0, kk, M2), rows8(sg[1], row0, kk, M2)};
                 const half8 fb[2] = {cols8(sx[0], col0, kk), cols8(sx[1], col0, kk)};

@@ -8,8 +8,8 @@
 __device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }  // NaN if either is
 
 struct RowStat {
-    float up, down;  // scale of the row and its inverse
-    float norm, sum; // of the scaled values: root of the sum of squares, sum of magnitudes
+    float down;       // inverse of the row's scale
+    float norm, sum;  // of the scaled values: root of the sum of squares, sum of magnitudes
 };
 
 template <typename E>
@@ -71,5 +71,5 @@ __device__ __forceinline__ RowStat pack_row(const typename E::mem* row, int32_t 
         *reinterpret_cast<half8*>(to + c) = hi;
         if constexpr (Planes == 2) *reinterpret_cast<half8*>(to + plane + c) = lo;
     }
-    return {s.up, s.down, sqrtf(wave_sum<kWave>(squares)), wave_sum<kWave>(sum)};
+    return {s.down, sqrtf(wave_sum<kWave>(squares)), wave_sum<kWave>(sum)};
 }

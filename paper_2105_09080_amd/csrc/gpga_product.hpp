@@ -108,7 +108,7 @@ struct Reader {
 
 // The tile of rows m0 .., columns n0 .. of one batch entry, K (a multiple of kPad) terms: acc[block of 32 columns][block of 32
 // rows], in which lane l holds row l % 32 and columns 8 (r / 4) + 4 (l / 32) + r % 4.
-// `offB(row)`: row of B's memory that holds column n0 + row (rows operands only; nullptr_t: n0 + row itself).
+// `row_b(row)`: row of B's memory that holds column n0 + row (rows operands only).
 template <typename S, typename RowB>
 __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B, int64_t batch, int32_t m0, int32_t n0, int32_t K, char* lds,
                                              acc16 (&acc)[S::NI][S::MI], RowB&& row_b) {
@@ -344,8 +344,8 @@ struct TileGrid {
 };
 
 // Tiles: 256 x 256 (8 wavefronts, one workgroup a compute unit), 128 x 128 (4 wavefronts, two workgroups, so that one's end is hidden
-// behind the other's products), 64 x 64 (two groups of 2
-// wavefronts, where there is little to do: 5 x 320 x 320 x 1024 with four planes 15.7 us in one group, 14.2 with steps twice as long, 13 in two).
+// behind the other's products), 64 x 64 (two groups of 2 wavefronts, where there is little to do: 5 x 320 x 320 x 1024 with four planes
+// 15.7 us in one group, 14.2 with steps twice as long, 13 in two).
 template <int PA, int PB, bool CA, bool CB>
 using Tile256 = Tile<256, 256, 2, 4, PA + PB == 2 ? 64 : 32, PA, PB, CA, CB>;
 template <int PA, int PB, bool CA, bool CB>
