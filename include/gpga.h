@@ -456,9 +456,12 @@ gpga_status gpga_token_loss(gpga_ctx* ctx, const void* logits_dev, const int32_t
  * a and b, n*T dense rows [a | b] of 2F elements of the activations' type; y comes from a and b before they are rounded.
  * 1 <= D, F <= 2^21, D*F with both rounded up to multiples of 64 below 2^30.
  * Products are made of fp16 pieces of the operands, scaled by powers of two, with fp32 sums: with fp32 activations two
- * pieces each (2^-22 of an operand's largest value in its row), with fp16 two of one operand and one (2^-11) of the other, with bf16 one
- * each; the gradients of the matrices take two whatever the type.  A token with an infinity or NaN in its row of x has no finite
- * result, and may have none where |x| times the largest |row| of Wg_i or Wu_i (2-norms) passes 2^63; other tokens are not touched.
+ * pieces each (2^-22 of a value, and no less than 2^-39 of the largest one that shares its scale: a token's row of x, a row of a matrix, of Wd_i with column f
+ * weighted by |row f of Wg_i| |row f of Wu_i|), with fp16 two of one operand and one (2^-11) of the other, with bf16 one
+ * each; h is scaled element by element, whatever the sizes of the matrices and of their rows beside each other's.  Up to 64 tokens a node no scales are needed.
+ * The gradients of the matrices take two pieces whatever the type.  A token with an infinity or NaN in its row of x has no finite result, and may have
+ * none where |x| or a |row| of Wg_i or Wu_i (2-norms) passes 2^126, or |row f of Wg_i| |row f of Wu_i| 2^100, alone or times an element of Wd_i's
+ * column f 2^127; other tokens are not touched.
  * An infinity or NaN in a matrix leaves no finite y that it enters.  Scratch: the matrices in fp16 pieces, and up to some 4 GiB for tokens
  * (more go through in turn); up to 64 tokens a node need n*T*F floats only. */
 typedef enum { GPGA_SILU = 0, GPGA_GELU = 1 } gpga_activation;

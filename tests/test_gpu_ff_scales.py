@@ -1,0 +1,125 @@
+"""The gated feed-forward block on matrices, rows and kept values of very different sizes, against the float64 oracle.  64 tokens of a node go
+through one kernel and 65 through others; both have to be right.
+
+Tolerances are taken from the terms that make up a result, each with its own size, and from no bound over several of them.  With e for
+the pieces of an operand (2^-22 for two, 2^-11 for one, 0 where one is exact), a sum of K terms p_k q_k is off by
+(e + (sqrt K + 16) 2^-24) times the sum of |p_k q_k|, or |p| |q| in 2-norms, which is more: K roundings of fp32 that go up as often as down, each
+of a partial sum of at most that.
+What falls below fp16's subnormals is 2^-39 of the largest value that shares the scale, 2^-40 where that is a power of two above it.  Errors of the elements of a
+vector are independent, so a product takes them by the root of the sum of their squares.  Rounding to the activations' type: u = eps / 2.
+"""
+import numpy as np
+import pytest
+
+from oracle import matrix_oracle as orc
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": (torch.float32, 2.0 ** -24), "bf16": (torch.bfloat16, 2.0 ** -8), "f16": (torch.float16, 2.0 ** -11)}
+E32, FN, FLOOR, ONE, TWO = 2.0 ** -24, 2.0 ** -20, 2.0 ** -39, 2.0 ** -11, 2.0 ** -22
+N, D, F = 2, 72, 90
+
+
+@pytest.fixture(scope="module")
+def hx():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2105_09080_amd import harness
+    return harness
+
+
+def norm(v, axis):
+    return np.sqrt((v * v).sum(axis=axis))
+
+
+def t(v):
+    return v.transpose(0, 2, 1)
+
+
+def sums(k):
+    return (np.sqrt(k) + 16) * E32
+
+
+def spread_matrices(kind, rng):
+    gate, up, down = rng.normal(size=(N, F, D)) / np.sqrt(D), rng.normal(size=(N, F, D)) / np.sqrt(D), rng.normal(size=(N, D, F)) / np.sqrt(F)
+    if kind == "up small":
+        up *= 1e-6
+    if kind == "gate small":
+        gate *= 1e-6
+    if kind == "one gate row":
+        gate[:, 5] *= 1e4
+    if kind == "one up row":
+        up[:, 5] *= 1e4
+    if kind == "apart":                                              # neither has the other's size
+        gate *= 2.0 ** -60
+        up *= 2.0 ** 60
+    if kind == "every row":                                          # rows from 2^-30 to 2^30, and the columns that they meet
+        s = 2.0 ** np.linspace(-30, 30, F).round()
+        rng.shuffle(s)
+        up *= s[None, :, None]
+        down /= s[None, None, :]
+    if kind == "zero rows":
+        gate[:, ::3] = 0.0
+        up[:, 1::3] = 0.0
+        up[0] *= 1e-6
+    return [w.astype(np.float32).astype(np.float64) for w in (gate, up, down)]
+
+
+def make(hx, gate, up, down):
+    sim = hx.Simulation(N, 3 * D * F, topology="ring", H=4, lr=0.1)
+    sim.set_state(X=np.concatenate([w.reshape(N, -1) for w in (gate, up, down)], axis=1).astype(np.float32))
+    return sim, (0, D * F, 2 * D * F)
+
+
+def activations(rng, shape, dt, scale=1.0):
+    v = torch.as_tensor(rng.normal(size=shape) * scale).to(dt).cuda()
+    return v, v.double().cpu().numpy()
+
+
+def forward_tolerances(x, gate, up, down, kind, dtype):
+    """(y, a, b) and how far they may be off: of y the 2-norm of a token's error, of a and b each element's."""
+    ex, ew = {"f32": (TWO, TWO + TWO), "bf16": (0.0, ONE), "f16": (0.0, TWO)}[dtype]
+    eh, ed = {"f32": (TWO, TWO + TWO), "bf16": (ONE, ONE), "f16": (ONE, TWO)}[dtype]
+    y, a, b = orc.gated_ff(x, gate, up, down, kind)
+    xn = norm(x, 2)[..., None]
+    ta, tb = ((ex + ew + sums(D)) * xn * norm(w, 2)[:, None, :] for w in (gate, up))
+    value = orc.activation(kind, a)[0]
+    tv = np.maximum(np.abs(orc.activation(kind, a + ta)[0] - value), np.abs(orc.activation(kind, a - ta)[0] - value)) + FN * np.abs(a)
+    h, size = value * b, (norm(gate, 2) * norm(up, 2))[:, None, :]
+    # the bound of an element of h is up to 2^3 above |x|^2 |wg_f| |wu_f|; that of one of the down matrix's row 2^2 above the largest of them
+    th = tv * (np.abs(b) + tb) + np.abs(value) * tb + eh * np.abs(h) + 8 * FLOOR * xn ** 2 * size
+    most = (np.abs(down) * size).max(axis=2)                         # n, D
+    low = 4 * FLOOR * np.einsum("ntf,nd->ntd", np.abs(h) / np.where(size > 0, size, 1.0), most)
+    ty = np.sqrt((th ** 2) @ t(down ** 2)) + (ed + sums(F)) * (np.abs(h) @ t(np.abs(down))) + low
+    return (y, a, b), (norm(ty, 2), ta, tb)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("T", [64, 65])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("kind", ["alike", "up small", "gate small", "one gate row", "one up row", "apart", "every row", "zero rows"])
+def test_forward(hx, kind, act, T, dtype):
+    if dtype == "f16" and kind in ("apart", "every row"):
+        pytest.skip("the kept values would not be in fp16's range")
+    dt, u = TYPES[dtype]
+    rng = np.random.default_rng(len(kind) + T)
+    gate, up, down = spread_matrices(kind, rng)
+    sim, at = make(hx, gate, up, down)
+    x, xd = activations(rng, (N, T, D), dt)
+    y, hidden = sim.gated_ff(x, *at, F, act=act, keep=True)
+    with np.errstate(over="ignore"):
+        (wy, wa, wb), (ty, ta, tb) = forward_tolerances(xd, gate, up, down, act, dtype)
+    sub = 2.0 ** -25 if dtype == "f16" else 0.0                       # below fp16's smallest normal numbers
+    hidden, y = hidden.double().cpu().numpy(), y.double().cpu().numpy()
+    assert (np.abs(hidden[..., :F] - wa) <= ta + u * (np.abs(wa) + ta) + sub).all()
+    assert (np.abs(hidden[..., F:] - wb) <= tb + u * (np.abs(wb) + tb) + sub).all()
+    off, tol = norm(y - wy, 2), ty * (1 + u) + u * norm(wy, 2) + sub * np.sqrt(D)
+    if dtype == "f32":
+        # the tolerance tells.  A row 10^4 above the others has a's error of (2^-20 + 25 2^-24) |x| |w| = 2.4e-6 * 8.5 * 10^4 = 0.2, and tokens where it
+        # is not the whole result (a large and negative) or all of it (large) are few enough for y's median to be off by 10^-4 or so
+        far = float(np.median(ty / norm(wy, 2)))
+        assert far < (1e-3 if kind.startswith("one") else 1e-4), far
+    worst = float((off / norm(wy, 2)).max())
+    assert (off <= tol).all(), worst
+    sim.close()
