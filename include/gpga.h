@@ -471,7 +471,9 @@ gpga_status gpga_gated_ff(gpga_ctx* ctx, const void* x_dev, int32_t T, int32_t D
  * dx = Wg_i^T da + Wu_i^T db, and into g_dev the sums over the node's tokens dWg_i = sum da x^T, dWu_i = sum db x^T,
  * dWd_i = sum dy h^T.  The three column blocks must not overlap.  T = 0 leaves zeros (or, added, nothing).  An infinity or NaN in dy or
  * hidden makes its token's dx and the node's gradients NaN, one in x those of Wg_i and Wu_i, one in a matrix the node's dx and
- * possibly its gradients. */
+ * possibly its gradients.  Each of da, db and h has scales of its own, a token's, with what falls below 2^-39 of s max |b|, s max |act(a)| and max |act(a)|
+ * max |b| lost, s the sum of |dy_j| max |row j of Wd_i|; where one of these passes 2^127 the token counts as infinite.  For dx Wg_i and
+ * Wu_i have one scale each. */
 gpga_status gpga_gated_ff_grad(gpga_ctx* ctx, const void* dy_dev, const void* x_dev, const void* hidden_dev, int32_t T,
                                int32_t D, int32_t F, int64_t ld, int32_t dtype, int32_t act, int64_t gate_off,
                                int64_t up_off, int64_t down_off, void* dx_dev, int32_t accumulate);

@@ -9,8 +9,8 @@
 // not exact in one; what is rounded to fp16 gets two for one operand of each product, so that it is off by little more than its own
 // rounding; what is rounded to bf16 (by up to 2^-8) gets one (2^-11) everywhere.
 // Scales: rows of x and of the matrices by their largest value; h, da and db, which are rounded in the epilogue that makes them, by
-// bounds that are known before (forward Cauchy-Schwarz for a and b, element by element; backward the largest |a| and |b| of the token and the
-// sum of |dy| for dh): some 2^8 .. 2^14 above typical values, which halves' 29 binades below 2^15 have room for.
+// bounds that are known before (forward Cauchy-Schwarz for a and b, element by element; backward the largest |act(a)| and |b| of the token and
+// the sum of |dy| for dh, each of the three by its own): some 2^8 .. 2^14 above typical values, which halves' 29 binades below 2^15 have room for.
 #include "gpga_pack.hpp"
 
 namespace {
@@ -44,6 +44,8 @@ __device__ __forceinline__ float act_value(float v) {
     return value;
 }
 
+// Another Slot for another maximum without a barrier between.
+template <int Slot = 0>
 __device__ __forceinline__ float block_max(float m) {
     __shared__ float s[kPackRows];
     m = wave_all<kWave>(m, max_nan);
@@ -70,7 +72,7 @@ struct PackMatrices {
     float *gu_inv, *wd_inv;       // n x 2F', n x D'
     float* gu_up;                 // forward: n x 2F', 2^-eg and 2^(15-eu); 0 for a row of zeros
     float* fold;                  // forward: n x F', 2^(eg + eu)
-    const float* node_max;        // backward: largest |gate|, |up| of a node in kMaxParts parts
+    const float* node_max;        // backward: largest |gate| and largest |up| of a node, n x 2 x kMaxParts parts
     uint32_t gu_blocks, per_node, first_block;
 };
 constexpr int kMaxParts = 256;
@@ -100,16 +102,18 @@ __device__ __forceinline__ void pack_gate_up_rows(const PackMatrices& a, uint32_
     a.gu_up[node * 2 * F2 + F2 + first] = e == -INFINITY ? 0.f : ldexpf(power_of_two(eg), (int)(e != e ? 0.f : 15.f - e));
 }
 
-// Workgroup `in` of a node's for gate and up, with one scale a node.
+// Backward: the scale of a node's gate (0) or up (1) matrix.
+__device__ __forceinline__ Scale matrix_scale(const float* node_max, int64_t node, int which) {
+    const float* part = node_max + (node * 2 + which) * kMaxParts + (threadIdx.x & (kWave - 1));
+    return scale_for(wave_all<kWave>(max_nan(max_nan(part[0], part[64]), max_nan(part[128], part[192])), max_nan));
+}
+
+// Workgroup `in` of a node's for gate and up, with one scale each.
 template <typename E, int P>
 __device__ __forceinline__ void pack_gate_up(const PackMatrices& a, int64_t node, int32_t in) {
     const int32_t D2 = padded(a.D), F2 = padded(a.F), row = in * kPackRows + threadIdx.x / kWave, f = row < F2 ? row : row - F2;
-    const int lane = threadIdx.x & (kWave - 1);
     const float* from = (row < F2 ? a.gate : a.up) + node * a.ldx + (int64_t)f * a.D;
-    const float* part = a.node_max + node * kMaxParts;
-    const Scale s = scale_for(wave_all<kWave>(max_nan(max_nan(part[lane], part[64 + lane]), max_nan(part[128 + lane], part[192 + lane])), max_nan));
-    const RowStat r = pack_row<E, P>(from, f < a.F ? a.D : 0, D2, false, s, a.gu + (node * 2 * F2 + row) * D2, a.gu_plane);
-    if (lane == 0) a.gu_inv[node * 2 * F2 + row] = r.down;
+    pack_row<E, P>(from, f < a.F ? a.D : 0, D2, false, matrix_scale(a.node_max, node, row >= F2), a.gu + (node * 2 * F2 + row) * D2, a.gu_plane);
 }
 // And for the down matrix, with scales by row.
 template <typename E, int P, typename Fold = NoFold>
@@ -131,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_down_folded(PackMatrices a
     });
 }
 
-// Backward, first: the down matrix, and the largest |gate| and |up| of a node in kMaxParts parts.
+// Backward, first: the down matrix, and the largest |gate| and the largest |up| of a node in kMaxParts parts each.
 template <typename E>
 __global__ __launch_bounds__(kThreads) void k_ff_pack_down(PackMatrices a, float* parts) {
     typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
@@ -143,18 +147,25 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_down(PackMatrices a, float
         return;
     }
     const float* from[2] = {a.gate + node * a.ldx, a.up + node * a.ldx};
-    float m = 0.f;
+    float m[2] = {0.f, 0.f};
     const int64_t count = (int64_t)a.F * a.D, fours = count / 4, at = (int64_t)p * kThreads + threadIdx.x;
 #pragma unroll 2
     for (int64_t e = at; e < fours; e += (int64_t)kMaxParts * kThreads)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const vec v = *(reinterpret_cast<const vec*>(from[k]) + e);
-            m = max_nan(m, max_nan(max_nan(fabsf(v[0]), fabsf(v[1])), max_nan(fabsf(v[2]), fabsf(v[3]))));
+            m[k] = max_nan(m[k], max_nan(max_nan(fabsf(v[0]), fabsf(v[1])), max_nan(fabsf(v[2]), fabsf(v[3]))));
         }
-    if (at < count % 4) m = max_nan(m, max_nan(fabsf(from[0][fours * 4 + at]), fabsf(from[1][fours * 4 + at])));
-    m = block_max(m);
-    if (threadIdx.x == 0) parts[node * kMaxParts + p] = m;
+    if (at < count % 4) {
+        m[0] = max_nan(m[0], fabsf(from[0][fours * 4 + at]));
+        m[1] = max_nan(m[1], fabsf(from[1][fours * 4 + at]));
+    }
+    m[0] = block_max<0>(m[0]);
+    m[1] = block_max<1>(m[1]);
+    if (threadIdx.x == 0) {
+        parts[node * 2 * kMaxParts + p] = m[0];
+        parts[(node * 2 + 1) * kMaxParts + p] = m[1];
+    }
 }
 
 // Rows of activations of a chunk of tokens: kRowsEach for each of a workgroup's wavefronts.
@@ -194,13 +205,42 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_x(PackMatrices w, uint32_t
     }
 }
 
-// Backward, second: gate and up by the node's largest value; dy times the scales of the down matrix's rows as halves, and the scales of
-// its token's rows of [da | db] and h, from |dh| <= sum |dy| |w| and the largest |a|, |b| of the token.  For the products over tokens,
-// da = da' / up and so on leaves factors that go into the other operand (k_ff_pack_tokens): the largest |x| / up and |dy| / up of a
-// workgroup's tokens.
+// The largest |a| of a row, and the largest a: |act(a)| is at most a where a > 0 and min(|a| / 2, 0.28) where not.
+struct RowRange {
+    float size, most;
+    __device__ __forceinline__ float act_bound() const { return size < INFINITY ? fmaxf(most, fminf(size * 0.5f, 0.28f)) : size; }
+};
+template <typename E>
+__device__ __forceinline__ RowRange row_range(const typename E::mem* row, int32_t cols) {
+    RowRange r = {0.f, 0.f};
+    for (int32_t c = (int32_t)(threadIdx.x & (kWave - 1)) * kOct; c < cols; c += kWave * kOct) {
+        float v[kOct];
+        piece_read<kOct, E>(row, c, cols, v);
+#pragma unroll
+        for (int j = 0; j < kOct; ++j) {
+            r.size = max_nan(r.size, fabsf(v[j]));
+            r.most = fmaxf(r.most, v[j]);
+        }
+    }
+    return {wave_all<kWave>(r.size, max_nan), wave_max<kWave>(r.most)};
+}
+
+// Backward, what a token's rows of da, db and h are scaled by, each by a bound of its own: |dh| <= sum |dy| |w|, |da| <= 1.14 |dh| max |b|,
+// |db| <= |dh| max |act(a)|, |h| <= max |act(a)| max |b|.  dx adds da Wg and db Wu in one sum: after the first the sums are brought to the second's
+// scale, by 2^-120 to 2^70: sums of up to 2^51 stay in fp32's range.  Of scales further apart the finer one is made coarser.
+struct TokenScales {
+    float *da_up, *da_inv, *db_up, *db_inv, *h_up, *h_inv;  // a power of two, its inverse (0: the row is zeros)
+    float* dx_middle;                                      // factor of the sums of da Wg
+    int32_t* dx_exp;                                       // dx = 2^dx_exp times the sums
+    float* part;                                           // n x 3 x workgroups of a node: largest |x| da_inv, |x| db_inv, |dy| h_inv
+};
+__device__ __forceinline__ int exponent_of(float power) { return (int)(__float_as_uint(power) >> 23) - 127; }
+
+// Backward, second: gate and up by their largest values; dy times the scales of the down matrix's rows as halves, and its tokens' scales.
+// For the products over tokens da = da' / up and so on leaves factors that go into the other operand (k_ff_pack_tokens).
 template <typename E, int P>
-__global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackMatrices w, uint32_t matrix_blocks, PackRows a, const float* wd_inv, const void* x, const void* hidden, int32_t F,
-                                                         int64_t hidden_node, float* da_up, float* da_inv, float* h_up, float* h_inv, float* part) {
+__global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackMatrices w, uint32_t matrix_blocks, PackRows a, const void* x, const void* hidden, int64_t hidden_node,
+                                                         TokenScales t) {
     typedef typename E::mem M;
     const int32_t cols2 = padded(a.cols), lane = threadIdx.x & (kWave - 1), rows2 = padded(a.rows);
     uint32_t block = a.first_block + blockIdx.x;
@@ -210,65 +250,84 @@ __global__ __launch_bounds__(kThreads) void k_ff_pack_dy(PackMatrices w, uint32_
     }
     block -= matrix_blocks;
     const int64_t node = block / a.per_node;
-    float px = 0.f, py = 0.f;
+    float p[3] = {0.f, 0.f, 0.f};
     {
         const int32_t row = (int32_t)(block % a.per_node) * kPackRows + threadIdx.x / kWave;
         const bool real = row < a.rows;
         const int64_t from = node * a.node + (int64_t)row * a.ld, at = node * rows2 + row;
-        float xm = 0.f, ym = 0.f, am = 0.f, bm = 0.f;
+        const Scale gate = matrix_scale(w.node_max, node, 0), up = matrix_scale(w.node_max, node, 1);
+        float xm = 0.f, ym = 0.f, vm = 0.f, bm = 0.f;
         if (real) {
-            const M* h = static_cast<const M*>(hidden) + node * hidden_node + (int64_t)row * 2 * F;
-            am = row_max<E>(h, F);
-            bm = row_max<E>(h + F, F);
+            const M* h = static_cast<const M*>(hidden) + node * hidden_node + (int64_t)row * 2 * w.F;
+            vm = row_range<E>(h, w.F).act_bound();
+            bm = row_max<E>(h + w.F, w.F);
+            if (!(fmaxf(vm, bm) < INFINITY) || vm != vm || bm != bm) vm = bm = NAN;  // the token has no gradient then
             xm = row_max<E>(static_cast<const M*>(x) + from, a.cols);
             ym = row_max<E>(static_cast<const M*>(a.src) + from, a.cols);
         }
-        const float* inv = wd_inv + node * cols2;
+        const float* inv = w.wd_inv + node * cols2;
         const RowStat r = pack_row<E, P>(static_cast<const M*>(a.src) + from, real ? a.cols : 0, cols2, true, {}, a.dst + at * cols2, a.plane,
                                          [&](int32_t c, float* v) {
 #pragma unroll
                                              for (int j = 0; j < kOct; ++j) v[j] *= inv[c + j];
                                          });
         const float dh = r.sum * r.down * 32768.f * 1.0001f;
-        const Scale sa = scale_for(dh * max_nan(1.14f * bm, am)), sh = scale_for(am * bm);
+        Scale sa = scale_for(dh * (1.14f * bm)), sb = scale_for(dh * vm);
+        const Scale sh = scale_for(vm * bm);
+        const bool no_a = sa.down == 0.f || gate.down == 0.f, no_b = sb.down == 0.f || up.down == 0.f;
+        const bool bad = sa.up != sa.up || sb.up != sb.up || gate.up != gate.up || up.up != up.up;
+        int ea = exponent_of(sa.up), eb = exponent_of(sb.up), apart = eb + exponent_of(up.up) - ea - exponent_of(gate.up);
+        if (!bad && !no_a && !no_b) {
+            constexpr int kMost = 70, kLeast = -120;
+            if (apart > kMost) eb = max(eb - (apart - kMost), -126);
+            if (apart < kLeast) ea = max(ea - (kLeast - apart), -126);
+            apart = min(max(apart, kLeast), kMost);
+            sa = {ldexpf(1.f, ea), ldexpf(1.f, -ea)};
+            sb = {ldexpf(1.f, eb), ldexpf(1.f, -eb)};
+        }
         if (lane == 0) {
             a.inv[at] = r.down;
-            da_up[at] = sa.up;
-            da_inv[at] = sa.down;
-            h_up[at] = sh.up;
-            h_inv[at] = sh.down;
+            t.da_up[at] = sa.up;
+            t.da_inv[at] = sa.down;
+            t.db_up[at] = sb.up;
+            t.db_inv[at] = sb.down;
+            t.h_up[at] = sh.up;
+            t.h_inv[at] = sh.down;
+            t.dx_middle[at] = bad ? NAN : no_a ? 0.f : no_b ? 1.f : ldexpf(1.f, apart);
+            t.dx_exp[at] = bad ? 0 : no_b ? -ea - exponent_of(gate.up) : -eb - exponent_of(up.up);
         }
-        px = max_nan(px, xm * sa.down);
-        py = max_nan(py, ym * sh.down);
+        p[0] = xm * sa.down;
+        p[1] = xm * sb.down;
+        p[2] = ym * sh.down;
     }
-    __shared__ float s[2][kPackRows];
+    __shared__ float s[3][kPackRows];
     if (lane == 0) {
-        s[0][threadIdx.x / kWave] = px;
-        s[1][threadIdx.x / kWave] = py;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) s[k][threadIdx.x / kWave] = p[k];
     }
     __syncthreads();
-    if (threadIdx.x < 2) {
+    if (threadIdx.x < 3) {
         const float* q = s[threadIdx.x];
-        part[(node * 2 + threadIdx.x) * a.per_node + block % a.per_node] = max_nan(max_nan(q[0], q[1]), max_nan(q[2], q[3]));
+        t.part[(node * 3 + threadIdx.x) * a.per_node + block % a.per_node] = max_nan(max_nan(q[0], q[1]), max_nan(q[2], q[3]));
     }
 }
 
-// x / up or dy / up of every token as halves with one scale a node, the first or the second half of the workgroups.
+// x / up of da, x / up of db or dy / up of h of every token as halves with one scale a node, a third of the workgroups each.
 struct PackTokens {
-    PackRows of[2];            // x, dy; inv: one a node
-    const float* row_inv[2];
+    PackRows of[3];            // inv: one a node
+    const float* row_inv[3];
     const float* part;
-    uint32_t parts, half, first_block;
+    uint32_t parts, each, first_block;
 };
 template <typename E, int P>
 __global__ __launch_bounds__(kThreads) void k_ff_pack_tokens(PackTokens t) {
     uint32_t block = t.first_block + blockIdx.x;
-    const int which = block >= t.half;
-    block -= which ? t.half : 0;
+    const uint32_t which = block / t.each;
+    block -= which * t.each;
     const PackRows a = t.of[which];
     const int32_t cols2 = padded(a.cols), rows2 = padded(a.rows);
     const int64_t node = block / a.per_node;
-    const float* from = t.part + (node * 2 + which) * t.parts;
+    const float* from = t.part + (node * 3 + which) * t.parts;
     float w = 0.f;
     for (uint32_t p = threadIdx.x; p < t.parts; p += kThreads) w = max_nan(w, from[p]);
     const Scale node_scale = scale_for(block_max(w));
@@ -292,8 +351,7 @@ struct FfProduct {
     const float* row_inv;     // scales of A's rows, n x rows of A's memory (or of k_ff_pack_tokens, one a node)
     const float* col_inv;     // of B's rows
     const float* gu_up;
-    int64_t row_batch, col_batch;
-    int32_t F;
+    int32_t F, nodes;
     // activations in or out
     void* out;
     int64_t out_ld, out_node;
@@ -303,10 +361,14 @@ struct FfProduct {
     // planes out
     half_t *h, *da;
     int64_t h_plane, da_plane;
-    const float *h_up, *da_up;
+    const float *h_up, *da_up, *db_up;
+    // dx: TokenScales
+    const float* middle;
+    const int32_t* exp;
     // gradients out
     float* g;
-    int64_t g_ld, off0, off1;  // columns of gate's and up's blocks
+    int64_t g_ld, off0, off1;  // columns of the blocks of gate and up, or down's
+    int64_t second;            // halves from the B that gate's takes to up's, or 0: a single matrix
     int accumulate;
 };
 
@@ -346,24 +408,30 @@ __global__ __launch_bounds__(S::Threads, 2) void k_ff_up(FfProduct a) {
     });
 }
 
-// Activations out.  Backward (B by columns): a scale of the row and one of the node; forward: of the column and twice of the row,
-// and the 2^15 that h is held in.
+// Activations out.  Forward: a scale of the column and twice the row's, and the 2^15 that h is held in; backward (B by columns): da Wg and db Wu, each
+// half of the terms, with the row's power of two (TokenScales).
 template <typename S, typename E>
 __device__ __forceinline__ void rows_product(const FfProduct& a, uint32_t block, char* lds) {
     int32_t node, ti, tj;
     if (!a.grid.at(block, &node, &ti, &tj)) return;
     const int32_t m0 = ti * S::BM, n0 = tj * S::BN;
     acc16 acc[S::NI][S::MI];
-    product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return min(n0 + row, a.B.rows - 1); });
+    const int64_t rows = (int64_t)node * a.A.rows;
+    if constexpr (S::ColsB)
+        product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [](int row) { return row; },
+                        [&](int32_t row) { return a.middle[rows + min(row, a.A.rows - 1)]; });
+    else
+        product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return min(n0 + row, a.B.rows - 1); });
     typedef typename E::mem M;
     each_octet<S>(acc, lds, m0, n0, false, [&](int32_t row, int32_t col, float* v) {
         if (row >= a.M || col >= a.N) return;
-        const float r = a.row_inv[node * a.row_batch + row];
-        const float* c = a.col_inv + node * a.col_batch;
         if constexpr (S::ColsB) {
+            const int e = a.exp[rows + row];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] *= r * c[0];
+            for (int k = 0; k < 8; ++k) v[k] = ldexpf(v[k], e);
         } else {
+            const float r = a.row_inv[rows + row];
+            const float* c = a.col_inv + (int64_t)node * a.B.rows;
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = v[k] * (c[col + k] * 0x1p-15f) * r * r;
         }
@@ -397,14 +465,13 @@ __global__ __launch_bounds__(S::Threads, 2) void k_ff_down_grad(FfProduct a) {
             float va[8], vb[8];
             piece_read<kOct, E>(hid, f, a.F, va);
             piece_read<kOct, E>(hid + a.F, f, a.F, vb);
-            const float inv = a.row_inv[at] * a.da_up[at], h_up = a.h_up[at];
+            const float inv = a.row_inv[at], da_up = inv * a.da_up[at], db_up = inv * a.db_up[at], h_up = a.h_up[at];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 float value, slope;
                 act_both<Act>(va[k], &value, &slope);
-                const float d = da[k] * inv;
-                da[k] = d * vb[k] * slope;
-                db[k] = d * value;
+                db[k] = da[k] * db_up * value;
+                da[k] = da[k] * da_up * vb[k] * slope;
                 h[k] = value * vb[k] * h_up;
             }
         } else {
@@ -417,22 +484,23 @@ __global__ __launch_bounds__(S::Threads, 2) void k_ff_down_grad(FfProduct a) {
     });
 }
 
-// Gradients of matrices: rows of the gate's block, then (from F' on) of the up's; or of the down matrix's alone (off1 < 0).
+// Gradients of matrices: of gate and of up, two to a node, which are the first and the second half of A's columns; or of the down matrix's.
 // G: fp32, narrow where a row of the matrix is.
 template <typename S, typename G>
 __device__ __forceinline__ void matrix_grad(const FfProduct& a, uint32_t block, char* lds) {
     int32_t node, ti, tj;
     if (!a.grid.at(block, &node, &ti, &tj)) return;
-    const int32_t m0 = ti * S::BM, n0 = tj * S::BN;
+    const int32_t up = a.second ? node & 1 : 0, base = up * (a.A.ld / 2);
+    if (a.second) node >>= 1;
+    Operand B = a.B;
+    B.p += up * a.second;
+    const int32_t m0 = base + ti * S::BM, n0 = tj * S::BN;
     acc16 acc[S::NI][S::MI];
-    product_tile<S>(a.A, a.B, node, m0, n0, a.K, lds, acc, [&](int row) { return row; });
-    const float inv = a.row_inv[node];
+    product_tile<S>(a.A, B, node, m0, n0, a.K, lds, acc, [&](int row) { return row; });
+    const float inv = a.row_inv[up * a.nodes + node];
+    const int64_t off = up ? a.off1 : a.off0;
     each_octet<S>(acc, lds, m0, n0, false, [&](int32_t row, int32_t col, float* v) {
-        int64_t off = a.off0;
-        if (a.off1 >= 0 && row >= a.A.ld / 2) {
-            row -= a.A.ld / 2;
-            off = a.off1;
-        }
+        row -= base;
         if (row >= a.M || col >= a.N) return;
         float* to = a.g + (int64_t)node * a.g_ld + off + (int64_t)row * a.N;
 #pragma unroll
@@ -665,8 +733,9 @@ int32_t chunk_tokens(const FfShape& s, int64_t halves) {
 struct FfScratch {
     int32_t chunk;
     int px, pgu, pd, ph, pa;  // planes
-    half_t *gu, *wd, *x, *h, *dy, *da, *tok_x, *tok_y;
-    float *gu_inv, *wd_inv, *gu_up, *fold, *node_max, *x_inv, *h_up, *h_inv, *da_up, *da_inv, *part, *node_inv;
+    half_t *gu, *wd, *x, *h, *dy, *da, *tokens[3];
+    float *gu_inv, *wd_inv, *gu_up, *fold, *node_max, *x_inv, *h_up, *h_inv, *node_inv;
+    TokenScales t;
 };
 
 FfScratch carve_ff(const FfShape& s, bool grad, char* base, size_t* bytes) {
@@ -682,7 +751,7 @@ FfScratch carve_ff(const FfShape& s, bool grad, char* base, size_t* bytes) {
     } else {
         w.pgu = f32 ? 2 : 1;
         w.pd = w.ph = w.pa = 2;
-        w.chunk = chunk_tokens(s, (int64_t)3 * w.px * D2 + (int64_t)6 * F2);
+        w.chunk = chunk_tokens(s, (int64_t)4 * w.px * D2 + (int64_t)6 * F2);
     }
     const int64_t n = s.n, T2 = padded(w.chunk);
     w.gu = c.take<half_t>(n * 2 * F2 * D2 * w.pgu);
@@ -698,15 +767,20 @@ FfScratch carve_ff(const FfShape& s, bool grad, char* base, size_t* bytes) {
         w.fold = c.take<float>(n * F2);
         w.x = c.take<half_t>(n * T2 * D2 * w.px);
     } else {
-        w.node_max = c.take<float>(n * kMaxParts);
+        w.node_max = c.take<float>(n * 2 * kMaxParts);
         w.dy = c.take<half_t>(n * T2 * D2 * w.px);
-        w.tok_x = c.take<half_t>(n * T2 * D2 * w.px);
-        w.tok_y = c.take<half_t>(n * T2 * D2 * w.px);
+        for (half_t*& p : w.tokens) p = c.take<half_t>(n * T2 * D2 * w.px);
         w.da = c.take<half_t>(n * T2 * 2 * F2 * w.pa);
-        w.da_up = c.take<float>(n * T2);
-        w.da_inv = c.take<float>(n * T2);
-        w.part = c.take<float>(n * 2 * (T2 / kPackRows));
-        w.node_inv = c.take<float>(2 * n);
+        w.t.da_up = c.take<float>(n * T2);
+        w.t.da_inv = c.take<float>(n * T2);
+        w.t.db_up = c.take<float>(n * T2);
+        w.t.db_inv = c.take<float>(n * T2);
+        w.t.h_up = w.h_up;
+        w.t.h_inv = w.h_inv;
+        w.t.dx_middle = c.take<float>(n * T2);
+        w.t.dx_exp = c.take<int32_t>(n * T2);
+        w.t.part = c.take<float>(n * 3 * (T2 / kPackRows));
+        w.node_inv = c.take<float>(3 * n);
     }
     *bytes = c.used;
     return w;
@@ -786,7 +860,7 @@ hipError_t launch_grads(const gpga_ctx* c, FfProduct& x, FfProduct& g, FfProduct
     int side = 0;
     double best = 0.;
     for (int t = 0; t < 3; ++t) {
-        const TileTime a(t, PDX + PGU, T, D2, x.K, c->n, false), b(t, 2 + PX, 2 * F2, D2, g.K, c->n, false), e(t, PX + 2, D2, F2, d.K, c->n, false);
+        const TileTime a(t, PDX + PGU, T, D2, x.K, c->n, false), b(t, 2 + PX, F2, D2, g.K, 2 * c->n, false), e(t, PX + 2, D2, F2, d.K, c->n, false);
         double us = ((kWithX ? a.tiles * a.us : 0.) + b.tiles * b.us + e.tiles * e.us) / c->num_cus + 0.5 * (kWithX ? fmax(a.us, b.us) : b.us);
         if (t == 0) us = fmax(us, fmax(kWithX ? TileTime::alone(PDX + PGU, x.K) : 0., TileTime::alone(2 + PX, g.K)));
         if (t == 0 || us < best) {
@@ -795,7 +869,7 @@ hipError_t launch_grads(const gpga_ctx* c, FfProduct& x, FfProduct& g, FfProduct
         }
     }
     if (kWithX) x.grid.set(T, D2, side, c->n, false);
-    g.grid.set(2 * F2, D2, side, c->n, false);
+    g.grid.set(F2, D2, side, 2 * c->n, false);
     d.grid.set(D2, F2, side, c->n, false);
     auto launch = [&](auto sx, auto sg, auto sd) {
         typedef decltype(sx) SX;
@@ -907,9 +981,7 @@ hipError_t forward(const gpga_ctx* c, const FfShape& s, const void* x, void* hid
         b.N = s.D;
         b.K = F2;
         b.row_inv = w.h_inv;
-        b.row_batch = T2;
         b.col_inv = w.wd_inv;
-        b.col_batch = D2;
         b.out = static_cast<M*>(y) + (int64_t)t0 * s.ld;
         b.out_ld = s.ld;
         b.out_node = (int64_t)s.T * s.ld;
@@ -945,17 +1017,16 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         const uint32_t matrix_blocks = t0 ? 0 : m.gu_blocks * (uint32_t)s.n;
         GPGA_LAUNCH(launch_blocks((uint64_t)p.per_node * s.n + matrix_blocks, kThreads, [&](uint32_t first, dim3 grid) {
             p.first_block = first;
-            k_ff_pack_dy<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(m, matrix_blocks, p, w.wd_inv, static_cast<const M*>(x) + skip, hid, s.F, hidden_node, w.da_up,
-                                                                        w.da_inv, w.h_up, w.h_inv, w.part);
+            k_ff_pack_dy<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(m, matrix_blocks, p, static_cast<const M*>(x) + skip, hid, hidden_node, w.t);
         }));
         p.per_node /= kRowsEach;
-        PackTokens tokens = {{p, p}, {w.da_inv, w.h_inv}, w.part, (uint32_t)(T2 / kPackRows), p.per_node * (uint32_t)s.n, 0};
-        tokens.of[0].src = static_cast<const M*>(x) + skip;
-        tokens.of[0].dst = w.tok_x;
-        tokens.of[0].inv = w.node_inv;
-        tokens.of[1].dst = w.tok_y;
-        tokens.of[1].inv = w.node_inv + n;
-        GPGA_LAUNCH(launch_blocks((uint64_t)2 * tokens.half, kThreads, [&](uint32_t first, dim3 grid) {
+        PackTokens tokens = {{p, p, p}, {w.t.da_inv, w.t.db_inv, w.h_inv}, w.t.part, (uint32_t)(T2 / kPackRows), p.per_node * (uint32_t)s.n, 0};
+        for (int k = 0; k < 3; ++k) {
+            if (k < 2) tokens.of[k].src = static_cast<const M*>(x) + skip;
+            tokens.of[k].dst = w.tokens[k];
+            tokens.of[k].inv = w.node_inv + k * n;
+        }
+        GPGA_LAUNCH(launch_blocks((uint64_t)3 * tokens.each, kThreads, [&](uint32_t first, dim3 grid) {
             tokens.first_block = first;
             k_ff_pack_tokens<E, PX><<<grid, dim3(kThreads), 0, c->stream>>>(tokens);
         }));
@@ -973,7 +1044,8 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         a.h_up = w.h_up;
         a.da = w.da;
         a.da_plane = n * T2 * 2 * F2;
-        a.da_up = w.da_up;
+        a.da_up = w.t.da_up;
+        a.db_up = w.t.db_up;
         GPGA_LAUNCH((launch_product<PX, 2, false, true>(c, a, T2, F2, [&](auto tile, dim3 grid) {
             with_act(s.act, [&](auto act) {
                 typedef decltype(tile) S;
@@ -986,16 +1058,16 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         b.M = T;
         b.N = s.D;
         b.K = 2 * F2;
-        b.row_inv = w.da_inv;
-        b.row_batch = T2;
-        b.col_inv = w.gu_inv;
-        b.col_batch = 2 * F2;
+        b.middle = w.t.dx_middle;
+        b.exp = w.t.dx_exp;
         b.out = static_cast<M*>(dx) + skip;
         b.out_ld = s.ld;
         b.out_node = (int64_t)s.T * s.ld;
         FfProduct g = {};
         g.A = rows_operand(w.da, n, T2, 2 * F2);
-        g.B = rows_operand(w.tok_x, n, T2, D2);
+        g.B = rows_operand(w.tokens[0], n, T2, D2);
+        g.second = w.tokens[1] - w.tokens[0];
+        g.nodes = s.n;
         g.M = s.F;
         g.N = s.D;
         g.K = T2;
@@ -1006,13 +1078,13 @@ hipError_t backward(const gpga_ctx* c, const FfShape& s, const void* dy, const v
         g.off1 = s.up_off;
         g.accumulate = accumulate || t0 > 0;
         FfProduct d = g;
-        d.A = rows_operand(w.tok_y, n, T2, D2);
+        d.A = rows_operand(w.tokens[2], n, T2, D2);
+        d.second = 0;
         d.B = rows_operand(w.h, n, T2, F2);
         d.M = s.D;
         d.N = s.F;
-        d.row_inv = w.node_inv + n;
+        d.row_inv = w.node_inv + 2 * n;
         d.off0 = s.down_off;
-        d.off1 = -1;
         GPGA_LAUNCH((launch_grads<PDX, PGU, PX, E>(c, b, g, d, T, D2, F2)));
     }
     return hipSuccess;

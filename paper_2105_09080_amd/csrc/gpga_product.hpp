@@ -108,10 +108,13 @@ struct Reader {
 
 // The tile of rows m0 .., columns n0 .. of one batch entry, K (a multiple of kPad) terms: acc[block of 32 columns][block of 32
 // rows], in which lane l holds row l % 32 and columns 8 (r / 4) + 4 (l / 32) + r % 4.
-// `row_b(row)`: row of B's memory that holds column n0 + row (rows operands only).
-template <typename S, typename RowB>
+// `row_b(row)`: row of B's memory that holds column n0 + row (rows operands only).  `middle(row)`, if there is one: what the sum over the first half of
+// the terms is multiplied by, for halves of two scales (K a multiple of 2 kPad then).
+struct NoMiddle {};
+template <typename S, typename RowB, typename Middle = NoMiddle>
 __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B, int64_t batch, int32_t m0, int32_t n0, int32_t K, char* lds,
-                                             acc16 (&acc)[S::NI][S::MI], RowB&& row_b) {
+                                             acc16 (&acc)[S::NI][S::MI], RowB&& row_b, Middle&& middle = {}) {
+    constexpr bool kMiddle = !__is_same(__remove_cvref(Middle), NoMiddle);
     using namespace product;
     const int t = threadIdx.x, lane = t & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(t / kWave);
     constexpr int RA = S::BytesA / 16 / S::Threads, RB = S::BytesB / 16 / S::Threads;
@@ -161,11 +164,24 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
 #pragma unroll
         for (int i = 0; i < S::MI; ++i) acc[j][i] = acc16{};
 
+    float factor[kMiddle ? S::MI : 1];
+    if constexpr (kMiddle) {
+#pragma unroll
+        for (int i = 0; i < S::MI; ++i) factor[i] = middle(m0 + firstA + i * 32 + (lane & 31));
+    }
     const int steps = K / S::BK;
     fetch(0);
     __syncthreads();
     for (int s = 0; s < steps; ++s) {
         if (s + 1 < steps) fetch((s + 1) & 1);
+        if constexpr (kMiddle) {
+            if (s == steps / 2) {
+#pragma unroll
+                for (int j = 0; j < S::NI; ++j)
+#pragma unroll
+                    for (int i = 0; i < S::MI; ++i) acc[j][i] *= factor[i];
+            }
+        }
         const char* at = lds + (s & 1) * S::Stage;
 #pragma unroll
         for (int kk = 0; kk < S::BK / 16 / S::KW; ++kk) {

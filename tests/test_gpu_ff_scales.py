@@ -123,3 +123,103 @@ def test_forward(hx, kind, act, T, dtype):
     worst = float((off / norm(wy, 2)).max())
     assert (off <= tol).all(), worst
     sim.close()
+
+
+def backward_tolerances(dy, x, a, b, gate, up, down, kind, dtype):
+    """dx and the matrices' gradients, and how far they may be off: 2-norms of dx's tokens and of the gradients' matrices."""
+    T = x.shape[1]
+    f32 = dtype == "f32"
+    value, slope = orc.activation(kind, a)
+    dh = dy @ down
+    # dh: dy exact but with fp32, the matrix in two pieces by rows; dh's bound is the sum of |dy| max |row|
+    wide = np.abs(down).max(axis=2)
+    th = ((3 if f32 else 1) * TWO + sums(D)) * (np.abs(dy) @ np.abs(down)) + 2 * FLOOR * D * (np.abs(dy) * wide[:, None, :]).max(axis=2)[..., None]
+    most = (np.abs(dy) * wide[:, None, :]).sum(axis=2)[..., None]
+    vm, bm = np.abs(value).max(axis=2)[..., None], np.abs(b).max(axis=2)[..., None]
+    # bounds: 1.14 for the slope, for act(a) a where it is positive and at most 2^2 too much where all are not; powers of two above them
+    near = np.where(np.abs(a) < 40, np.abs(a), 1.0)                  # act is good to 2^-20 of it, its slope to 2^-18; beyond, a or nothing
+    tda = th * np.abs(b * slope) + (4 * FN * (1 + near) + TWO) * np.abs(dh * b) + 4 * FLOOR * most * bm
+    tdb = th * np.abs(value) + TWO * np.abs(dh * value) + FN * np.abs(dh) * near + 8 * FLOOR * most * vm
+    thh = TWO * np.abs(value * b) + FN * np.abs(b) * near + 8 * FLOOR * vm * bm
+    da, db, h = dh * b * slope, dh * value, value * b
+    want = [da @ gate + db @ up, t(da) @ x, t(db) @ x, t(dy) @ h]
+    # of dx: pieces of da, db and of the matrices, each by a scale of the whole matrix
+    px = {"f32": 4 * TWO, "bf16": 2 * ONE, "f16": ONE + TWO}[dtype]
+    root = lambda v, w: np.sqrt((v ** 2) @ (w ** 2))
+    tdx = root(tda, gate) + root(tdb, up) + px * (root(da, gate) + root(db, up)) + sums(2 * F) * (np.abs(da) @ np.abs(gate) + np.abs(db) @ np.abs(up))
+    for v, w in ((da, gate), (db, up)):
+        tdx = tdx + 2 * FLOOR * np.abs(w).max(axis=(1, 2))[:, None, None] * norm(v, 2)[..., None]
+    po = (3 * TWO if f32 else TWO) + sums(T)
+    tol = [norm(tdx, 2)]
+    for tv, v, w, bound in ((tda, da, x, most * bm), (tdb, db, x, most * vm), (thh, h, dy, vm * bm)):
+        # the other operand is exact (two pieces with fp32), but for what falls below the subnormals of the node's scale
+        low = 8 * FLOOR * (np.abs(w).max(axis=2)[..., None] * bound).max(axis=1)[..., None] / np.where(bound > 0, bound, 1.0)
+        e = root(t(tv), np.abs(w)) + po * (t(np.abs(v)) @ np.abs(w)) + root(t(np.abs(v)), low * np.ones_like(w))
+        tol.append(np.sqrt((e ** 2).sum(axis=(1, 2))))
+    return want, tol
+
+
+KEPT = ["alike", "b small", "a small", "a large and negative", "up small", "gate small", "one gate row", "one up row", "apart", "column", "zero rows", "no b", "no a", "no gate",
+        "b far", "a far"]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("T", [7, 130])
+@pytest.mark.parametrize("kind", KEPT)
+def test_backward(hx, kind, T, act, dtype):
+    """The kept [a | b] of one token, or of all, may be of any size beside each other, as the matrices may."""
+    if dtype == "f16" and kind in ("apart", "column", "b far", "a far"):
+        pytest.skip("not in fp16's range")
+    dt, u = TYPES[dtype]
+    rng = np.random.default_rng(len(kind) + T)
+    gate, up, down = spread_matrices(kind, rng)
+    if kind == "column":                                             # a column of x that gate sees and up does not
+        up[:, :, 3] = 0.0
+    if kind == "no gate":
+        gate[:] = 0.0
+    sim, at = make(hx, gate, up, down)
+    x, xd = activations(rng, (N, T, D), dt)
+    if kind == "column":
+        x[..., 3] *= 2.0 ** 20
+        xd = x.double().cpu().numpy()
+    dy, dyd = activations(rng, (N, T, D), dt, 2.0 ** -5)
+    _, a, b = orc.gated_ff(xd, gate, up, down, act)
+    if kind == "b small":
+        b *= 2.0 ** -20
+    if kind == "b far":
+        b *= 2.0 ** -100
+    if kind == "a far":
+        a *= 2.0 ** -60
+    if kind == "a small":
+        a *= 2.0 ** -14
+        a[:, 1] *= 2.0 ** 20                                         # and a token where it is not
+    if kind == "a large and negative":                              # where act(a) and its slope are nothing
+        a[..., ::2] = -2.0 ** 15
+    if kind == "no b":
+        b[:] = 0.0
+    if kind == "no a":
+        a[:] = 0.0
+    hidden = torch.as_tensor(np.concatenate([a, b], axis=2)).to(dt).cuda()
+    kept = hidden.double().cpu().numpy()
+    a, b = kept[..., :F], kept[..., F:]
+    with np.errstate(over="ignore"):
+        want, tol = backward_tolerances(dyd, xd, a, b, gate, up, down, act, dtype)
+    dx = sim.gated_ff_grad(dy, x, hidden, *at, act=act).double().cpu().numpy()
+    sub = 2.0 ** -25 * np.sqrt(D) if dtype == "f16" else 0.0
+    off, size = norm(dx - want[0], 2), norm(want[0], 2)
+    if dtype == "f32" and kind != "no gate" and size.any():
+        far = float(np.median(tol[0] / np.maximum(size, 1e-300)))
+        assert far < 1e-3, far
+    worst = float((off / np.maximum(size, 1e-300)).max())
+    assert (off <= tol[0] * (1 + u) + u * size + sub).all(), worst
+    G = sim.G.double().cpu().numpy()
+    for k in range(3):
+        got = G[:, at[k]:at[k] + D * F].reshape(want[k + 1].shape)
+        size = np.sqrt((want[k + 1] ** 2).sum(axis=(1, 2)))
+        off = np.sqrt(((got - want[k + 1]) ** 2).sum(axis=(1, 2)))
+        if size.all():
+            far = float((tol[k + 1] / size).max())
+            assert far < 1e-3, (k, far)
+        assert (off <= tol[k + 1] + E32 * size).all(), (k, float((off / np.maximum(size, 1e-300)).max()), float((tol[k + 1] / np.maximum(size, 1e-300)).max()))
+    sim.close()
