@@ -3,7 +3,8 @@
 //
 // Activations are n * T rows, row i*T + t = token t of node i, of D elements (fp32, bf16 or fp16) with a common leading
 // dimension ld >= D in elements.  Parameters are fp32 and lie in row i of X; their gradients go to the same columns of g.
-// All arithmetic is fp32; a result is rounded to the activations' type once, where it is stored.
+// All arithmetic is fp32, but for the products of the operators with matrices, whose operands are pieces of 11 to 24 bits with fp32 sums
+// (gpga_product.hpp); a result is rounded to the activations' type once, where it is stored.
 #pragma once
 
 #include "gpga_internal.hpp"
