@@ -5,8 +5,8 @@
 //
 // which maps every singular value s to p s + q s^3 + r s^5 and leaves the singular vectors.  A has the shorter side's size.  Small singular
 // values grow by p a step, and so do errors in them: everything is held in two halves (22 bits), fp32's precision, three matrix
-// instructions a step (gpga_product.hpp).  Singular values are at most 1 to begin with; the host follows the largest that a step can make
-// of them, so all scales are known constants.
+// instructions a step (gpga_product.hpp).  Singular values are at most 1 to begin with; the largest that a step can make of them is
+// followed, so all scales are known constants, whether values grow or shrink.
 #include "gpga_pack.hpp"
 
 #include <cmath>
@@ -15,6 +15,71 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kParts = 64;  // parts of a matrix's sum of squares
+
+// ---- scales ------------------------------------------------------------------------------------------------------------------
+// Largest |a s + b s^3 + c s^5| over 0 <= s <= most.
+double odd_max(double a, double b, double c, double most) {
+    auto f = [&](double s) { return fabs(s * (a + s * s * (b + s * s * c))); };
+    double best = f(most);
+    // a + 3 b z + 5 c z^2 = 0, z = s^2
+    const double d = 9.0 * b * b - 20.0 * a * c;
+    double z[2] = {-1.0, -1.0};
+    if (c != 0.0 && d >= 0.0) {
+        z[0] = (-3.0 * b + sqrt(d)) / (10.0 * c);
+        z[1] = (-3.0 * b - sqrt(d)) / (10.0 * c);
+    } else if (c == 0.0 && b != 0.0) {
+        z[0] = -a / (3.0 * b);
+    }
+    for (double v : z)
+        if (v > 0.0 && v < most * most) best = fmax(best, f(sqrt(v)));
+    return best;
+}
+// Largest |b z + c z^2| over 0 <= z <= most.
+double even_max(double b, double c, double most) {
+    double best = fabs(b * most + c * most * most);
+    if (c != 0.0) {
+        const double z = -b / (2.0 * c);
+        if (z > 0.0 && z < most) best = fmax(best, fabs(b * z + c * z * z));
+    }
+    return best;
+}
+// The exponent of the power of two that brings values of at most `bound` to 2^14 or below; of `none` where the bound is 0.
+int up_exponent(double bound, int none) {
+    int e;
+    frexp(bound, &e);
+    return bound == 0.0 ? none : 14 - e;
+}
+
+// What the products of a step are multiplied by, with X, A and B = q A + r A^2 held as 2^x, 2^g and 2^b times their values.  Each of these exponents
+// may be far beyond a float's; the factors, in which they meet, are about 2^-14 (or nothing, where a term is nothing beside another).
+struct OrthStep {
+    float gram;                   // A from X X^T
+    float poly_keep, poly_times;  // B from A and A^2
+    float keep, times;            // X from X and B X
+};
+constexpr int kMaxSteps = 64;
+struct OrthScales {
+    OrthStep step[kMaxSteps];
+    int first;                    // exponent of the first X
+    float finish[2];              // `scale` and what the last X is held in
+};
+
+// Singular values of at most `most` to begin with.
+void follow_steps(int32_t steps, double p, double q, double r, double scale, double most, OrthScales* out) {
+    int x = up_exponent(most, 0);
+    out->first = x;
+    for (int32_t k = 0; k < steps; ++k) {
+        const double z = most * most;
+        const int g = up_exponent(z * 1.001, 0), b = up_exponent(even_max(q, r, z) * 1.001, 0);
+        most = odd_max(p, q, r, most) * 1.001;
+        const int next = up_exponent(most, x);
+        out->step[k] = {(float)ldexp(1.0, g - 2 * x), (float)ldexp(q, b - g), (float)ldexp(r, b - 2 * g), (float)ldexp(p, next - x), (float)ldexp(1.0, next - x - b)};
+        x = next;
+    }
+    const int half = x > 120 ? -120 : x < -120 ? 120 : -x;
+    out->finish[0] = (float)ldexp(1.0, half);
+    out->finish[1] = (float)ldexp(scale, -x - half);
+}
 
 struct OrthArgs {
     float* g;              // the first matrix of node 0
@@ -138,6 +203,7 @@ struct OrthProduct {
     int64_t plane;
     int32_t rows2, cols2;     // of the result, padded
     float keep, times;
+    float finish[2];
     float* g;                 // last step: fp32 into the gradient's place
     int64_t ld;
     int32_t R, C, count, first;
@@ -165,6 +231,8 @@ __global__ __launch_bounds__(S::Threads, 2) void k_orth_product(OrthProduct a) {
         if constexpr (Last) {
             if (row >= a.R || col >= a.C) return;
             float* to = block_of(a.g, a.ld, a.first + m, a.count, (int64_t)a.R * a.C) + (int64_t)row * a.C;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = v[k] * a.finish[0] * a.finish[1];
             if (a.C < kOct) piece_put<kOct, Elem<float, true>>(to, col, a.C, v);
             else piece_put<kOct, Elem<float, false>>(to, col, a.C, v);
         } else {
@@ -417,39 +485,8 @@ bool small_fits(const OrthShape& s) {
     return m2 == 64 ? k2 <= 256 : k2 == 128;
 }
 
-// Power of two that brings values of at most `bound` to 2^14 or below.
-float up_for(double bound) {
-    int e;
-    std::frexp(bound, &e);
-    return (float)std::ldexp(1.0, 14 - e);
-}
-
-// Largest |a s + b s^3 + c s^5| over 0 <= s <= most.
-double odd_max(double a, double b, double c, double most) {
-    auto f = [&](double s) { return std::fabs(s * (a + s * s * (b + s * s * c))); };
-    double best = f(most);
-    // a + 3 b z + 5 c z^2 = 0, z = s^2
-    const double d = 9.0 * b * b - 20.0 * a * c;
-    double z[2] = {-1.0, -1.0};
-    if (c != 0.0 && d >= 0.0) {
-        z[0] = (-3.0 * b + std::sqrt(d)) / (10.0 * c);
-        z[1] = (-3.0 * b - std::sqrt(d)) / (10.0 * c);
-    } else if (c == 0.0 && b != 0.0) {
-        z[0] = -a / (3.0 * b);
-    }
-    for (double v : z)
-        if (v > 0.0 && v < most * most) best = std::fmax(best, f(std::sqrt(v)));
-    return best;
-}
-// Largest |b z + c z^2| over 0 <= z <= most.
-double even_max(double b, double c, double most) {
-    double best = std::fabs(b * most + c * most * most);
-    if (c != 0.0) {
-        const double z = -b / (2.0 * c);
-        if (z > 0.0 && z < most) best = std::fmax(best, std::fabs(b * z + c * z * z));
-    }
-    return best;
-}
+// What k_orth_small's scales are, for values of at most `bound`.
+float up_for(double bound) { return (float)ldexp(1.0, up_exponent(bound, 0)); }
 
 }  // namespace
 
@@ -476,6 +513,8 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
     const bool tall = s.R > s.C;
     const int64_t all = (int64_t)s.n * s.count;
     const double p = coefficients[0], q = coefficients[1], r = coefficients[2];
+    OrthScales scales;
+    follow_steps(steps, p, q, r, scale, 1.0, &scales);
     for (int64_t b0 = 0; b0 < all; b0 += w.chunk) {
         const int32_t matrices = (int32_t)(all - b0 < w.chunk ? all - b0 : w.chunk);
         OrthArgs a = {};
@@ -493,9 +532,7 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
         a.squares = w.squares;
         a.x = w.x[0];
         a.plane = (int64_t)matrices * R2 * C2;
-        double most = 1.0;
-        float x_up = up_for(1.0);
-        a.x_up = x_up;
+        a.x_up = ldexpf(1.f, scales.first);
         hipError_t e = hipSuccess;
         const bool small = steps > 0 && small_fits(s);
         if (!small) {
@@ -547,14 +584,14 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
         for (int32_t k = 0; k < steps; ++k) {
             const Operand x = {w.x[k & 1], (int64_t)matrices * R2 * C2, (int64_t)R2 * C2, C2, R2};
             const Operand gram = {w.gram, (int64_t)matrices * m2 * m2, (int64_t)m2 * m2, m2, m2}, poly = {w.poly, gram.plane, gram.batch, m2, m2};
-            const float gram_up = up_for(most * most * 1.001), poly_up = up_for(even_max(q, r, most * most) * 1.001 + 1e-30);
+            const OrthStep& step = scales.step[k];
             OrthProduct o = {};
             o.A = o.B = x;
             o.K = tall ? R2 : C2;
             o.out = w.gram;
             o.plane = gram.plane;
             o.rows2 = o.cols2 = m2;
-            o.times = (float)((double)gram_up / x_up / x_up);
+            o.times = step.gram;
             e = tall ? launch_product<true, true, false>(c, o, matrices, true) : launch_product<false, false, false>(c, o, matrices, true);
             if (e != hipSuccess) return e;
             // q A + r A A
@@ -562,13 +599,11 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             o.K = m2;
             o.add = w.gram;
             o.out = w.poly;
-            o.keep = (float)(q * poly_up / gram_up);
-            o.times = (float)(r * poly_up / gram_up / gram_up);
+            o.keep = step.poly_keep;
+            o.times = step.poly_times;
             e = launch_product<false, false, false>(c, o, matrices, true);
             if (e != hipSuccess) return e;
             const bool last = k + 1 == steps;
-            most = odd_max(p, q, r, most) * 1.001;
-            const double out_up = last ? (double)scale : (double)up_for(most);
             o = {};
             o.A = tall ? x : poly;
             o.B = tall ? poly : x;
@@ -578,8 +613,10 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             o.plane = x.plane;
             o.rows2 = R2;
             o.cols2 = C2;
-            o.keep = (float)(p * out_up / x_up);
-            o.times = (float)(out_up / x_up / poly_up);
+            o.keep = step.keep;
+            o.times = step.times;
+            o.finish[0] = scales.finish[0];
+            o.finish[1] = scales.finish[1];
             o.g = c->g + off;
             o.ld = c->ld;
             o.R = s.R;
@@ -589,7 +626,6 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             if (last) e = tall ? launch_product<false, false, true>(c, o, matrices, false) : launch_product<false, true, true>(c, o, matrices, false);
             else e = tall ? launch_product<false, false, false>(c, o, matrices, false) : launch_product<false, true, false>(c, o, matrices, false);
             if (e != hipSuccess) return e;
-            x_up = (float)out_up;
         }
     }
     return hipSuccess;
