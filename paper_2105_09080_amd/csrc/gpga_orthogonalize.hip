@@ -270,7 +270,7 @@ struct SmallArgs {
     OrthArgs o;
     int32_t k2;             // long side, padded
     int32_t steps;
-    float gram_times, poly_keep, poly_times, x_keep, x_times, last_keep, last_times;
+    OrthScales scales;
 };
 
 template <int M2, int KMax, int Waves>
@@ -361,6 +361,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
         }
     };
     for (int step = 0; step < a.steps; ++step) {
+        const OrthStep scale = a.scales.step[step];
 #pragma unroll
         for (int turn = 0; turn < 2; ++turn) {  // A = X X^T, then q A + r A A
             const half_t *p0 = turn ? sg[0] : sx[0], *p1 = turn ? sg[1] : sx[1];
@@ -384,7 +385,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
             for (int n = 0; n < kGramEach; ++n) {
                 const int block = wave + n * Waves;
                 if (block >= kGramBlocks) continue;
-                put(sg[0], sg[1], M2, block / (M2 / 32) * 32, block % (M2 / 32) * 32, c[n], turn ? a.poly_keep : 0.f, turn ? a.poly_times : a.gram_times);
+                put(sg[0], sg[1], M2, block / (M2 / 32) * 32, block % (M2 / 32) * 32, c[n], turn ? scale.poly_keep : 0.f, turn ? scale.poly_times : scale.gram);
             }
             __syncthreads();
         }
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
             if (block >= M2 / 32 * across) continue;
             const int row0 = block / across * 32, col0 = block % across * 32;
             if (!last) {
-                put(sx[0], sx[1], k2, row0, col0, c[n], a.x_keep, a.x_times);
+                put(sx[0], sx[1], k2, row0, col0, c[n], scale.keep, scale.times);
                 continue;
             }
             const int row = row0 + (lane & 31);
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
                 const half4 hi = *reinterpret_cast<const half4*>(sx[0] + from), lo = *reinterpret_cast<const half4*>(sx[1] + from);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float o = a.last_times * c[n][q * 4 + k] + a.last_keep * ((float)hi[k] + (float)lo[k]);
+                    const float o = (scale.times * c[n][q * 4 + k] + scale.keep * ((float)hi[k] + (float)lo[k])) * a.scales.finish[0] * a.scales.finish[1];
                     if (row < (tall ? a.o.C : a.o.R) && col + k < (tall ? a.o.R : a.o.C))
                         g[tall ? (int64_t)(col + k) * a.o.C + row : (int64_t)row * a.o.C + col + k] = o;
                 }
@@ -484,9 +485,6 @@ bool small_fits(const OrthShape& s) {
     const int32_t R2 = padded(s.R), C2 = padded(s.C), m2 = R2 < C2 ? R2 : C2, k2 = R2 < C2 ? C2 : R2;
     return m2 == 64 ? k2 <= 256 : k2 == 128;
 }
-
-// What k_orth_small's scales are, for values of at most `bound`.
-float up_for(double bound) { return (float)ldexp(1.0, up_exponent(bound, 0)); }
 
 }  // namespace
 
@@ -552,18 +550,7 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             continue;
         }
         if (small) {
-            const double bound = orthogonalize_bound(steps, coefficients), g_up = up_for(bound * bound * 1.001),
-                         p_up = up_for(even_max(q, r, bound * bound) * 1.001 + 1e-30);
-            SmallArgs f = {a, R2 > C2 ? R2 : C2, steps, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            const double up = up_for(bound);
-            f.o.x_up = (float)up;
-            f.gram_times = (float)(g_up / up / up);
-            f.poly_keep = (float)(q * p_up / g_up);
-            f.poly_times = (float)(r * p_up / g_up / g_up);
-            f.x_keep = (float)p;
-            f.x_times = (float)(1.0 / p_up);
-            f.last_keep = (float)(p * scale / up);
-            f.last_times = (float)(scale / up / p_up);
+            SmallArgs f = {a, R2 > C2 ? R2 : C2, steps, scales};
             const int32_t waves = f.k2 > 64 ? 8 : 4;
             e = launch_blocks((uint64_t)matrices, waves * kWave, [&](uint32_t first, dim3 grid) {
                 f.o.first_block = first;

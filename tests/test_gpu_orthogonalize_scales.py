@@ -13,7 +13,7 @@ from oracle import matrix_oracle as orc
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-SHAPES = [(200, 330), (300, 200)]
+SHAPES = [(40, 60), (64, 200), (128, 100), (200, 330), (300, 200)]   # by one workgroup, by launches
 
 
 @pytest.fixture(scope="module")
