@@ -185,8 +185,10 @@ __global__ __launch_bounds__(kThreads) void k_orth_pack(OrthArgs a) {
 #pragma unroll
         for (int j = 0; j < kOct; ++j) {
             const float w = u[j] * inv.first * inv.second * a.x_up;
-            hi[j] = (half_t)w;
-            lo[j] = (half_t)(w - (float)hi[j]);
+            half_t h, l;
+            split(w, &h, &l);
+            hi[j] = h;
+            lo[j] = l;
         }
         *reinterpret_cast<half8*>(to + c) = hi;
         *reinterpret_cast<half8*>(to + a.plane + c) = lo;
@@ -337,9 +339,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
             if (v) u = a.o.nesterov ? u + a.o.mu * v[e] : v[e];
             u = u * inv.first * inv.second * a.o.x_up;
             const int to = tall ? at(c, r, k2) : at(r, c, k2);
-            const half_t hi = (half_t)u;
-            sx[0][to] = hi;
-            sx[1][to] = (half_t)(u - (float)hi);
+            split(u, &sx[0][to], &sx[1][to]);
         }
     __syncthreads();
 
@@ -353,8 +353,10 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float o = times * c[q * 4 + k] + (keep != 0.f ? keep * ((float)hi[k] + (float)lo[k]) : 0.f);
-                hi[k] = (half_t)o;
-                lo[k] = (half_t)(o - (float)hi[k]);
+                half_t h, l;
+                split(o, &h, &l);
+                hi[k] = h;
+                lo[k] = l;
             }
             *reinterpret_cast<half4*>(p0 + to) = hi;
             *reinterpret_cast<half4*>(p1 + to) = lo;

@@ -63,8 +63,10 @@ __device__ __forceinline__ RowStat pack_row(const typename E::mem* row, int32_t 
 #pragma unroll
         for (int j = 0; j < kOct; ++j) {
             const float w = v[j] * s.up;
-            hi[j] = (half_t)w;
-            lo[j] = (half_t)(w - (float)hi[j]);
+            half_t h, l;
+            split(w, &h, &l);
+            hi[j] = h;
+            lo[j] = l;
             squares += w * w;
             sum += fabsf(w);
         }

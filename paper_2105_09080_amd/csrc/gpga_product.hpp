@@ -417,14 +417,24 @@ __device__ __forceinline__ Scale scale_for(float bound) {
     return {__uint_as_float((uint32_t)(127 + up) << 23), __uint_as_float((uint32_t)(127 - up) << 23)};
 }
 
+// v as the sum of two halves.  A product or sum that is rounded to a half in one instruction (v_fma_mix) can come out as another half than by way of
+// fp32, where that lies in the middle of two: lo would then be what is left of a neighbour of hi.  So v is fixed before.
+__device__ __forceinline__ void split(float v, half_t* hi, half_t* lo) {
+    asm("" : "+v"(v));
+    *hi = (half_t)v;
+    *lo = (half_t)(v - (float)*hi);
+}
+
 // v as one half or the sum of two, eight at a time.
 template <int Planes>
 __device__ __forceinline__ void store_planes(half_t* to, int64_t plane, const float* v) {
     half8 hi, lo;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        hi[k] = (half_t)v[k];
-        lo[k] = (half_t)(v[k] - (float)hi[k]);
+        half_t h, l;
+        split(v[k], &h, &l);
+        hi[k] = h;
+        lo[k] = l;
     }
     *reinterpret_cast<half8*>(to) = hi;
     if constexpr (Planes == 2) *reinterpret_cast<half8*>(to + plane) = lo;

@@ -223,3 +223,61 @@ def test_backward(hx, kind, T, act, dtype):
             assert far < 1e-3, (k, far)
         assert (off <= tol[k + 1] + E32 * size).all(), (k, float((off / np.maximum(size, 1e-300)).max()), float((tol[k + 1] / np.maximum(size, 1e-300)).max()))
     sim.close()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("n,T,D", [(3, 2000, 64), (8, 4096, 320), (200, 70, 64)])
+def test_both_pieces_of_every_h(hx, n, T, D, act):
+    """Diagonal matrices: y_j = act(g_j x_j) (u_j x_j) w_j, every element by itself: some twenty roundings to 2^-22 and of fp32 and an act that is good
+    to 2^-20 of a, 2^-16 of |a| |b| |w| together, and what falls below the subnormals of |x|^2.  A second piece that does not go with the first
+    leaves 2^-11."""
+    rng = np.random.default_rng(T)
+    g, u, w = (rng.uniform(0.5, 2.0, size=(3, n, D))).astype(np.float32).astype(np.float64)
+    sim = hx.Simulation(n, 3 * D * D, topology="ring", H=4, lr=0.1)
+    X = torch.zeros((n, 3, D, D), device="cuda")
+    for k, v in enumerate((g, u, w)):
+        X[:, k].diagonal(dim1=1, dim2=2).copy_(torch.as_tensor(v).cuda())
+    sim.X.copy_(X.view(n, -1))
+    x, xd = activations(rng, (n, T, D), torch.float32, 2.0)
+    y = sim.gated_ff(x, 0, D * D, 2 * D * D, D, act=act)[0].double()
+    sim.close()
+    gt, ut, wt, xt = (torch.as_tensor(v).cuda() for v in (g[:, None], u[:, None], w[:, None], xd))
+    a, b = gt * xt, ut * xt
+    want = (a * torch.sigmoid(a) if act == "silu" else a * torch.special.ndtr(a)) * b * wt
+    tol = 2.0 ** -16 * (torch.where(a < 0, a.abs().clamp(max=1.0), a) * b * wt).abs() * torch.where(a < 0, 2.0 ** -3, 1.0)
+    tol = tol + 2.0 ** -19 * (b * wt).abs() * (a < 0) + 2.0 ** -34 * xt.square().sum(dim=2, keepdim=True) * 8
+    bad = (y - want).abs() > tol
+    assert not bad.any(), (int(bad.sum()), float(((y - want).abs() / tol).max()))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("n,D,F", [(300, 64, 128), (40, 512, 640), (2, 2048, 2048)])
+def test_both_pieces_of_every_da(hx, n, D, F, act):
+    """One token a node: the matrices' gradients are products of one da_f, db_f or h_f and one x_j or dy_j, every element by itself.  dy has one element
+    other than 0, so dh_f = dy_j Wd_jf."""
+    rng = np.random.default_rng(D)
+    sim = hx.Simulation(n, 3 * D * F, topology="ring", H=4, lr=0.1)
+    sim.X.normal_()
+    down = sim.X[:, 2 * D * F:].view(n, D, F)[:, 5].double()
+    x, _ = activations(rng, (n, 1, D), torch.float32)
+    dy = torch.zeros((n, 1, D), device="cuda")
+    dy[:, 0, 5] = torch.as_tensor(rng.uniform(0.5, 2.0, size=n).astype(np.float32)).cuda()
+    hidden, _ = activations(rng, (n, 1, 2 * F), torch.float32)
+    sim.gated_ff_grad(dy, x, hidden, 0, D * F, 2 * D * F, act=act)
+    a, b = hidden[:, 0, :F].double(), hidden[:, 0, F:].double()
+    s = torch.sigmoid(a) if act == "silu" else torch.special.ndtr(a)
+    slope = s + a * s * (1 - s) if act == "silu" else s + a * torch.exp(-a * a / 2) / np.sqrt(2 * np.pi)
+    dh, xs = dy[:, 0, 5].double()[:, None] * down, x[:, 0].double()
+    rest = {"da": (dh * b * slope, 2.0 ** -17 * (dh * b).abs()), "db": (dh * a * s, 2.0 ** -17 * dh.abs() * a.abs().clamp(min=0.1))}
+    for k, name in enumerate(rest):
+        v, tol = rest[name]
+        got = sim.G[:, k * D * F:(k + 1) * D * F].view(n, F, D).double()
+        # the bound of da is some 2^6 above it, x's scale its largest value: 2^-39 of either
+        most = v.abs().amax(dim=1, keepdim=True) * 2.0 ** -31
+        off = (got - v[:, :, None] * xs[:, None]).abs() / ((tol + most)[:, :, None] * xs[:, None].abs() + v.abs()[:, :, None] * 2.0 ** -36)
+        assert not (off > 1).any(), (name, int((off > 1).sum()), float(off.max()))
+    h = a * s * b
+    got = sim.G[:, 2 * D * F:].view(n, D, F)[:, 5].double()
+    off = (got - h * dy[:, 0, 5].double()[:, None]).abs() / (2.0 ** -17 * (b.abs() * a.abs().clamp(min=0.1)) + h.abs().amax(dim=1, keepdim=True) * 2.0 ** -31) / dy[:, 0, 5].double()[:, None]
+    assert not (off > 1).any(), ("h", int((off > 1).sum()), float(off.max()))
+    sim.close()

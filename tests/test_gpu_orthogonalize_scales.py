@@ -57,3 +57,21 @@ def test_values_that_shrink_and_grow(hx, rows, cols, steps, coefficients, c, sca
     tol = steps * (2.0 ** -20 + 3 * sums(max(rows, cols)) * c) * norm(want) + 2.0 ** -149 * np.sqrt(rows * cols)
     assert np.isfinite(got).all()
     assert (norm(got - want) <= tol).all(), (norm(got - want) / np.maximum(norm(want), 1e-300)).max()
+
+
+@pytest.mark.parametrize("n,rows,cols", [(4, 40, 60), (4, 60, 250), (4, 120, 100), (4, 64, 400), (4, 130, 200), (4, 330, 200), (40, 520, 300), (16, 1024, 1024), (8, 700, 2048)])
+@pytest.mark.parametrize("p,steps", [(0.77, 3), (0.01, 9), (1.3, 4)])
+def test_both_pieces_of_every_element(hx, n, rows, cols, p, steps):
+    """X <- p X: every element by itself, 2^-20 of it a step, and what falls below the subnormals of the largest, 2^-36 of the norm.  A second
+    piece that does not go with the first leaves 2^-11."""
+    g = np.random.default_rng(rows).normal(size=(n, rows, cols)).astype(np.float32)
+    sim = hx.Simulation(n, rows * cols, topology="ring", H=4, lr=0.1)
+    sim.set_state(G=g.reshape(n, -1))
+    sim.orthogonalize(0, rows, cols, steps=steps, coefficients=(p, 0.0, 0.0), eps=0.0, scale=0.9)
+    got = sim.G.double().cpu().numpy().reshape(g.shape)
+    sim.close()
+    g = g.astype(np.float64)
+    want = g / norm(g)[:, None, None] * float(np.float32(p)) ** steps * float(np.float32(0.9))
+    off = np.abs(got - want) / ((steps + 2) * (2.0 ** -20 * np.abs(want) + 2.0 ** -36 * norm(want)[:, None, None]))
+    bad = int((off > 1).sum())
+    assert bad == 0, (bad, float(off.max()))
