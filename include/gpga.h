@@ -486,8 +486,9 @@ gpga_status gpga_gated_ff_grad(gpga_ctx* ctx, const void* dy_dev, const void* x_
  * g + mu V with nesterov = 1 (mu > 0).  A gpga_step then takes the updates as it takes gradients; with a context momentum it sums them
  * up in m, so momentum belongs in one of the two places.  A matrix of zeros gives zeros; one with an infinity or NaN gives NaN, whole.
  * Sides up to 2^21, their product with both rounded up to multiples of 64 below 2^30, n * count <= 2^24.
- * Products are made of two fp16 pieces an operand with fp32 sums.  EINVAL if the coefficients let a singular value of at most 1
- * pass 64 in these steps.  Asynchronous; scratch as above. */
+ * Products are made of two fp16 pieces an operand with fp32 sums, by scales that follow each matrix's values from |U| / (|U| + eps)
+ * on, step by step.  EINVAL if the coefficients let a singular value of at most 1 pass 64 in these steps.  Asynchronous; scratch as
+ * above. */
 gpga_status gpga_orthogonalize(gpga_ctx* ctx, int64_t off, int32_t rows, int32_t cols, int32_t count, float* velocity_dev,
                                float mu, int32_t nesterov, int32_t steps, float a, float b, float c, float eps, float scale);
 

@@ -5,11 +5,12 @@
 //
 // which maps every singular value s to p s + q s^3 + r s^5 and leaves the singular vectors.  A has the shorter side's size.  Small singular
 // values grow by p a step, and so do errors in them: everything is held in two halves (22 bits), fp32's precision, three matrix
-// instructions a step (gpga_product.hpp).  Singular values are at most 1 to begin with; the largest that a step can make of them is
+// instructions a step (gpga_product.hpp).  Singular values are at most |U|_F / (|U|_F + eps) to begin with; the largest that a step can make of them is
 // followed, so all scales are known constants, whether values grow or shrink.
 #include "gpga_pack.hpp"
 
 #include <cmath>
+#include <cstddef>
 
 namespace {
 
@@ -18,7 +19,7 @@ constexpr int kParts = 64;  // parts of a matrix's sum of squares
 
 // ---- scales ------------------------------------------------------------------------------------------------------------------
 // Largest |a s + b s^3 + c s^5| over 0 <= s <= most.
-double odd_max(double a, double b, double c, double most) {
+__host__ __device__ double odd_max(double a, double b, double c, double most) {
     auto f = [&](double s) { return fabs(s * (a + s * s * (b + s * s * c))); };
     double best = f(most);
     // a + 3 b z + 5 c z^2 = 0, z = s^2
@@ -35,7 +36,7 @@ double odd_max(double a, double b, double c, double most) {
     return best;
 }
 // Largest |b z + c z^2| over 0 <= z <= most.
-double even_max(double b, double c, double most) {
+__host__ __device__ double even_max(double b, double c, double most) {
     double best = fabs(b * most + c * most * most);
     if (c != 0.0) {
         const double z = -b / (2.0 * c);
@@ -44,7 +45,7 @@ double even_max(double b, double c, double most) {
     return best;
 }
 // The exponent of the power of two that brings values of at most `bound` to 2^14 or below; of `none` where the bound is 0.
-int up_exponent(double bound, int none) {
+__host__ __device__ int up_exponent(double bound, int none) {
     int e;
     frexp(bound, &e);
     return bound == 0.0 ? none : 14 - e;
@@ -59,26 +60,33 @@ struct OrthStep {
 };
 constexpr int kMaxSteps = 64;
 struct OrthScales {
-    OrthStep step[kMaxSteps];
-    int first;                    // exponent of the first X
+    OrthStep step[kMaxSteps];     // first: the products count floats from here
     float finish[2];              // `scale` and what the last X is held in
 };
 
-// Singular values of at most `most` to begin with.
-void follow_steps(int32_t steps, double p, double q, double r, double scale, double most, OrthScales* out) {
-    int x = up_exponent(most, 0);
-    out->first = x;
-    for (int32_t k = 0; k < steps; ++k) {
+struct OrthPolynomial {
+    double p, q, r, scale;
+    int32_t steps;
+};
+
+// The first X is held in 2^(13 - k) for singular values of at most 2^k.
+constexpr int kFirst = 13;
+__host__ __device__ void follow_steps(const OrthPolynomial& c, int k, OrthScales* out) {
+    const double p = c.p, q = c.q, r = c.r;
+    const int32_t steps = c.steps;
+    int x = kFirst - k;
+    double most = ldexp(1.0, k);
+    for (int32_t i = 0; i < steps; ++i) {
         const double z = most * most;
         const int g = up_exponent(z * 1.001, 0), b = up_exponent(even_max(q, r, z) * 1.001, 0);
         most = odd_max(p, q, r, most) * 1.001;
         const int next = up_exponent(most, x);
-        out->step[k] = {(float)ldexp(1.0, g - 2 * x), (float)ldexp(q, b - g), (float)ldexp(r, b - 2 * g), (float)ldexp(p, next - x), (float)ldexp(1.0, next - x - b)};
+        out->step[i] = {(float)ldexp(1.0, g - 2 * x), (float)ldexp(q, b - g), (float)ldexp(r, b - 2 * g), (float)ldexp(p, next - x), (float)ldexp(1.0, next - x - b)};
         x = next;
     }
     const int half = x > 120 ? -120 : x < -120 ? 120 : -x;
     out->finish[0] = (float)ldexp(1.0, half);
-    out->finish[1] = (float)ldexp(scale, -x - half);
+    out->finish[1] = (float)ldexp(c.scale, -x - half);
 }
 
 struct OrthArgs {
@@ -93,7 +101,7 @@ struct OrthArgs {
     double* squares;       // kParts a matrix
     half_t* x;             // (matrices, R', C') in two planes
     int64_t plane;
-    float x_up;
+    OrthScales* scales;    // one a matrix
     uint32_t per_matrix, first_block;
 };
 
@@ -141,28 +149,40 @@ __global__ __launch_bounds__(kThreads) void k_orth_norm(OrthArgs a) {
     if (threadIdx.x == 0) a.squares[block] = s[0];
 }
 
-// 1 / (sqrt(squares) + eps) as a product of two floats: of a norm beyond 2^100 or below 2^-100 the reciprocal may be subnormal or none.  0 for
-// a matrix of zeros, NaN for one with an infinity or NaN.
-struct Reciprocal {
+// What turns U into the first X: 2^(13 - k) / (|U| + eps), a product of two floats since it may be beyond one, with |U| / (|U| + eps) at most 2^k,
+// k = 0 unless eps is above |U|.  0 for a matrix of zeros, NaN for one with an infinity or NaN.
+struct OrthStart {
     float first, second;
+    int k;
 };
-__device__ __forceinline__ Reciprocal reciprocal(double squares, float eps) {
-    if (squares == 0.0) return {0.f, 0.f};
-    const double norm = sqrt(squares) + (double)eps;
-    if (!(norm < INFINITY)) return {NAN, NAN};
-    if (norm > 0x1p100) return {0x1p-100f, (float)(0x1p100 / norm)};
-    return norm < 0x1p-100 ? Reciprocal{0x1p100f, (float)(0x1p-100 / norm)} : Reciprocal{1.f, (float)(1.0 / norm)};
+__device__ __forceinline__ OrthStart orth_start(double squares, float eps) {
+    if (squares == 0.0) return {0.f, 0.f, 0};
+    const double norm = sqrt(squares), whole = norm + (double)eps;
+    if (!(whole < INFINITY)) return {NAN, NAN, 0};
+    const double inv = 1.0 / whole;
+    int k = 0, e;
+    if (norm * 2.0 < whole) frexp(norm * inv, &k);
+    const double f = frexp(ldexp(inv, kFirst - k), &e);
+    return {ldexpf(1.f, e / 2), (float)ldexp(f, e - e / 2), k};
 }
 
 // u / (|u| + eps) as halves, a wavefront a row.
 template <typename E>
-__global__ __launch_bounds__(kThreads) void k_orth_pack(OrthArgs a) {
+__global__ __launch_bounds__(kThreads) void k_orth_pack(OrthArgs a, OrthPolynomial c0, OrthScales usual) {
     const uint32_t block = a.first_block + blockIdx.x;
     const int32_t m = (int32_t)(block / a.per_matrix), b = a.first + m, lane = threadIdx.x & (kWave - 1);
     const int32_t row = (int32_t)(block % a.per_matrix) * (kThreads / kWave) + threadIdx.x / kWave, R2 = padded(a.R), C2 = padded(a.C);
     double total = a.squares[m * kParts + lane];
     for (int h = kWave / 2; h > 0; h >>= 1) total += __shfl_xor(total, h);
-    const Reciprocal inv = reciprocal(total, a.eps);
+    const OrthStart start = orth_start(total, a.eps);
+    if (block % a.per_matrix == 0 && threadIdx.x < kWave) {
+        if (start.k != 0) {
+            if (lane == 0) follow_steps(c0, start.k, a.scales + m);
+        } else {
+            constexpr int kWords = (int)(sizeof(OrthScales) / sizeof(float));
+            for (int i = lane; i < kWords; i += kWave) reinterpret_cast<float*>(a.scales + m)[i] = reinterpret_cast<const float*>(&usual)[i];
+        }
+    }
     const int64_t size = (int64_t)a.R * a.C;
     const float* g = block_of(a.g, a.ld, b, a.count, size) + (int64_t)row * a.C;
     const float* v = a.v ? block_of(a.v, a.v_ld, b, a.count, size) + (int64_t)row * a.C : nullptr;
@@ -184,7 +204,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_pack(OrthArgs a) {
         half8 hi, lo;
 #pragma unroll
         for (int j = 0; j < kOct; ++j) {
-            const float w = u[j] * inv.first * inv.second * a.x_up;
+            const float w = u[j] * start.first * start.second;
             half_t h, l;
             split(w, &h, &l);
             hi[j] = h;
@@ -204,8 +224,8 @@ struct OrthProduct {
     half_t* out;
     int64_t plane;
     int32_t rows2, cols2;     // of the result, padded
-    float keep, times;
-    float finish[2];
+    const OrthScales* scales; // one a matrix
+    int32_t keep_at, times_at; // which of its floats are keep and times
     float* g;                 // last step: fp32 into the gradient's place
     int64_t ld;
     int32_t R, C, count, first;
@@ -217,24 +237,35 @@ __global__ __launch_bounds__(S::Threads, 2) void k_orth_product(OrthProduct a) {
     int32_t m, ti, tj;
     if (!a.grid.at(a.first_block + blockIdx.x, &m, &ti, &tj)) return;
     const int32_t m0 = ti * S::BM, n0 = tj * S::BN;
+    float keep, times, finish[2];
     acc16 acc[S::NI][S::MI];
-    product_tile<S>(a.A, a.B, m, m0, n0, a.K, lds, acc, [&](int row) { return min(n0 + row, a.B.rows - 1); });
+    product_tile<S>(
+        a.A, a.B, m, m0, n0, a.K, lds, acc, [&](int row) { return min(n0 + row, a.B.rows - 1); }, NoMiddle{},
+        [&] {
+            // a matrix's own factors; 5 x 257 x 1023 in 15 launches 180 us with the call's in their arguments, 189 so, 192 to 194 with these loads before
+            // the tiles' or after the sums
+            const float* factors = reinterpret_cast<const float*>(a.scales + m);
+            keep = factors[a.keep_at];
+            times = factors[a.times_at];
+            finish[0] = a.scales[m].finish[0];
+            finish[1] = a.scales[m].finish[1];
+        });
     const bool mirror = a.grid.tn == 0 && ti != tj;
     each_octet<S>(acc, lds, m0, n0, mirror, [&](int32_t row, int32_t col, float* v) {
         if (row >= a.rows2 || col >= a.cols2) return;
         const int64_t at = ((int64_t)m * a.rows2 + row) * a.cols2 + col;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= a.times;
+        for (int k = 0; k < 8; ++k) v[k] *= times;
         if (a.add) {
             const half8 hi = *reinterpret_cast<const half8*>(a.add + at), lo = *reinterpret_cast<const half8*>(a.add + a.plane + at);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] += a.keep * ((float)hi[k] + (float)lo[k]);
+            for (int k = 0; k < 8; ++k) v[k] += keep * ((float)hi[k] + (float)lo[k]);
         }
         if constexpr (Last) {
             if (row >= a.R || col >= a.C) return;
             float* to = block_of(a.g, a.ld, a.first + m, a.count, (int64_t)a.R * a.C) + (int64_t)row * a.C;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = v[k] * a.finish[0] * a.finish[1];
+            for (int k = 0; k < 8; ++k) v[k] = v[k] * finish[0] * finish[1];
             if (a.C < kOct) piece_put<kOct, Elem<float, true>>(to, col, a.C, v);
             else piece_put<kOct, Elem<float, false>>(to, col, a.C, v);
         } else {
@@ -271,8 +302,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_scaled(OrthArgs a, float scal
 struct SmallArgs {
     OrthArgs o;
     int32_t k2;             // long side, padded
-    int32_t steps;
-    OrthScales scales;
+    OrthPolynomial c;
+    OrthScales usual;       // for k = 0
 };
 
 template <int M2, int KMax, int Waves>
@@ -283,6 +314,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
     __shared__ __align__(16) half_t sx[2][M2 * KMax];
     __shared__ __align__(16) half_t sg[2][M2 * M2];
     __shared__ double s_sum[Waves];
+    __shared__ OrthScales s_scales;
     const int t = threadIdx.x, lane = t & (kWave - 1), wave = t / kWave, k2 = KMax == M2 ? KMax : a.k2;
     const int32_t m = (int32_t)(a.o.first_block + blockIdx.x), b = a.o.first + m;
     const int64_t size = (int64_t)a.o.R * a.o.C;
@@ -331,13 +363,19 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
     __syncthreads();
     double total = 0.0;
     for (int w = 0; w < Waves; ++w) total += s_sum[w];
-    const Reciprocal inv = reciprocal(total, a.o.eps);
+    const OrthStart start = orth_start(total, a.o.eps);
+    if (start.k == 0) {
+        constexpr int kWords = (int)(sizeof(OrthScales) / sizeof(float));
+        for (int i = t; i < kWords; i += Waves * kWave) reinterpret_cast<float*>(&s_scales)[i] = reinterpret_cast<const float*>(&a.usual)[i];
+    } else if (t == 0) {
+        follow_steps(a.c, start.k, &s_scales);
+    }
     for (int32_t r = wave; r < a.o.R; r += Waves)
         for (int32_t c = lane; c < a.o.C; c += kWave) {
             const int64_t e = (int64_t)r * a.o.C + c;
             float u = g[e];
             if (v) u = a.o.nesterov ? u + a.o.mu * v[e] : v[e];
-            u = u * inv.first * inv.second * a.o.x_up;
+            u = u * start.first * start.second;
             const int to = tall ? at(c, r, k2) : at(r, c, k2);
             split(u, &sx[0][to], &sx[1][to]);
         }
@@ -362,8 +400,8 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
             *reinterpret_cast<half4*>(p1 + to) = lo;
         }
     };
-    for (int step = 0; step < a.steps; ++step) {
-        const OrthStep scale = a.scales.step[step];
+    for (int step = 0; step < a.c.steps; ++step) {
+        const OrthStep scale = s_scales.step[step];
 #pragma unroll
         for (int turn = 0; turn < 2; ++turn) {  // A = X X^T, then q A + r A A
             const half_t *p0 = turn ? sg[0] : sx[0], *p1 = turn ? sg[1] : sx[1];
@@ -406,7 +444,8 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
                 c[n] = times(fb, fa, c[n]);
             }
         }
-        const bool last = step + 1 == a.steps;
+        const bool last = step + 1 == a.c.steps;
+        const float finish[2] = {s_scales.finish[0], s_scales.finish[1]};
         if (!last) __syncthreads();
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n) {
@@ -424,7 +463,7 @@ __global__ __launch_bounds__(Waves * kWave) void k_orth_small(SmallArgs a) {
                 const half4 hi = *reinterpret_cast<const half4*>(sx[0] + from), lo = *reinterpret_cast<const half4*>(sx[1] + from);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float o = (scale.times * c[n][q * 4 + k] + scale.keep * ((float)hi[k] + (float)lo[k])) * a.scales.finish[0] * a.scales.finish[1];
+                    const float o = (scale.times * c[n][q * 4 + k] + scale.keep * ((float)hi[k] + (float)lo[k])) * finish[0] * finish[1];
                     if (row < (tall ? a.o.C : a.o.R) && col + k < (tall ? a.o.R : a.o.C))
                         g[tall ? (int64_t)(col + k) * a.o.C + row : (int64_t)row * a.o.C + col + k] = o;
                 }
@@ -462,6 +501,7 @@ struct OrthScratch {
     int32_t chunk;
     half_t *x[2], *gram, *poly;
     double* squares;
+    OrthScales* scales;
 };
 OrthScratch carve(const OrthShape& s, char* base, size_t* bytes) {
     const int64_t R2 = padded(s.R), C2 = padded(s.C), m2 = R2 < C2 ? R2 : C2, all = (int64_t)s.n * s.count;
@@ -478,6 +518,7 @@ OrthScratch carve(const OrthShape& s, char* base, size_t* bytes) {
     w.gram = reinterpret_cast<half_t*>(take((size_t)w.chunk * m2 * m2 * 4));
     w.poly = reinterpret_cast<half_t*>(take((size_t)w.chunk * m2 * m2 * 4));
     w.squares = reinterpret_cast<double*>(take((size_t)w.chunk * kParts * sizeof(double)));
+    w.scales = reinterpret_cast<OrthScales*>(take((size_t)w.chunk * sizeof(OrthScales)));
     *bytes = used;
     return w;
 }
@@ -512,9 +553,9 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
     const int32_t R2 = padded(s.R), C2 = padded(s.C), m2 = R2 < C2 ? R2 : C2;
     const bool tall = s.R > s.C;
     const int64_t all = (int64_t)s.n * s.count;
-    const double p = coefficients[0], q = coefficients[1], r = coefficients[2];
-    OrthScales scales;
-    follow_steps(steps, p, q, r, scale, 1.0, &scales);
+    const OrthPolynomial polynomial = {coefficients[0], coefficients[1], coefficients[2], scale, steps};
+    OrthScales usual = {};
+    follow_steps(polynomial, 0, &usual);
     for (int64_t b0 = 0; b0 < all; b0 += w.chunk) {
         const int32_t matrices = (int32_t)(all - b0 < w.chunk ? all - b0 : w.chunk);
         OrthArgs a = {};
@@ -532,7 +573,7 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
         a.squares = w.squares;
         a.x = w.x[0];
         a.plane = (int64_t)matrices * R2 * C2;
-        a.x_up = ldexpf(1.f, scales.first);
+        a.scales = w.scales;
         hipError_t e = hipSuccess;
         const bool small = steps > 0 && small_fits(s);
         if (!small) {
@@ -552,7 +593,7 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             continue;
         }
         if (small) {
-            SmallArgs f = {a, R2 > C2 ? R2 : C2, steps, scales};
+            SmallArgs f = {a, R2 > C2 ? R2 : C2, polynomial, usual};
             const int32_t waves = f.k2 > 64 ? 8 : 4;
             e = launch_blocks((uint64_t)matrices, waves * kWave, [&](uint32_t first, dim3 grid) {
                 f.o.first_block = first;
@@ -566,21 +607,23 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
         a.per_matrix = (uint32_t)(R2 / (kThreads / kWave));
         e = launch_blocks((uint64_t)a.per_matrix * matrices, kThreads, [&](uint32_t first, dim3 grid) {
             a.first_block = first;
-            if (s.C < kOct) k_orth_pack<Elem<float, true>><<<grid, dim3(kThreads), 0, c->stream>>>(a);
-            else k_orth_pack<Elem<float, false>><<<grid, dim3(kThreads), 0, c->stream>>>(a);
+            if (s.C < kOct) k_orth_pack<Elem<float, true>><<<grid, dim3(kThreads), 0, c->stream>>>(a, polynomial, usual);
+            else k_orth_pack<Elem<float, false>><<<grid, dim3(kThreads), 0, c->stream>>>(a, polynomial, usual);
         });
         if (e != hipSuccess) return e;
         for (int32_t k = 0; k < steps; ++k) {
             const Operand x = {w.x[k & 1], (int64_t)matrices * R2 * C2, (int64_t)R2 * C2, C2, R2};
             const Operand gram = {w.gram, (int64_t)matrices * m2 * m2, (int64_t)m2 * m2, m2, m2}, poly = {w.poly, gram.plane, gram.batch, m2, m2};
-            const OrthStep& step = scales.step[k];
             OrthProduct o = {};
             o.A = o.B = x;
             o.K = tall ? R2 : C2;
             o.out = w.gram;
             o.plane = gram.plane;
             o.rows2 = o.cols2 = m2;
-            o.times = step.gram;
+            constexpr int32_t kStep = (int32_t)(sizeof(OrthStep) / sizeof(float));
+            auto factor = [&](size_t member) { return k * kStep + (int32_t)(member / sizeof(float)); };
+            o.scales = w.scales;
+            o.keep_at = o.times_at = factor(offsetof(OrthStep, gram));
             e = tall ? launch_product<true, true, false>(c, o, matrices, true) : launch_product<false, false, false>(c, o, matrices, true);
             if (e != hipSuccess) return e;
             // q A + r A A
@@ -588,8 +631,8 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             o.K = m2;
             o.add = w.gram;
             o.out = w.poly;
-            o.keep = step.poly_keep;
-            o.times = step.poly_times;
+            o.keep_at = factor(offsetof(OrthStep, poly_keep));
+            o.times_at = factor(offsetof(OrthStep, poly_times));
             e = launch_product<false, false, false>(c, o, matrices, true);
             if (e != hipSuccess) return e;
             const bool last = k + 1 == steps;
@@ -602,10 +645,9 @@ hipError_t launch_orthogonalize(const gpga_ctx* c, const OrthShape& s, int64_t o
             o.plane = x.plane;
             o.rows2 = R2;
             o.cols2 = C2;
-            o.keep = step.keep;
-            o.times = step.times;
-            o.finish[0] = scales.finish[0];
-            o.finish[1] = scales.finish[1];
+            o.scales = w.scales;
+            o.keep_at = factor(offsetof(OrthStep, keep));
+            o.times_at = factor(offsetof(OrthStep, times));
             o.g = c->g + off;
             o.ld = c->ld;
             o.R = s.R;

@@ -109,11 +109,14 @@ struct Reader {
 // The tile of rows m0 .., columns n0 .. of one batch entry, K (a multiple of kPad) terms: acc[block of 32 columns][block of 32
 // rows], in which lane l holds row l % 32 and columns 8 (r / 4) + 4 (l / 32) + r % 4.
 // `row_b(row)`: row of B's memory that holds column n0 + row (rows operands only).  `middle(row)`, if there is one: what the sum over the first half of
-// the terms is multiplied by, for halves of two scales (K a multiple of 2 kPad then).
+// the terms is multiplied by, for halves of two scales (K a multiple of 2 kPad then).  `under_way()` runs while the first tiles arrive.
 struct NoMiddle {};
-template <typename S, typename RowB, typename Middle = NoMiddle>
+struct Nothing {
+    __device__ __forceinline__ void operator()() const {}
+};
+template <typename S, typename RowB, typename Middle = NoMiddle, typename UnderWay = Nothing>
 __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B, int64_t batch, int32_t m0, int32_t n0, int32_t K, char* lds,
-                                             acc16 (&acc)[S::NI][S::MI], RowB&& row_b, Middle&& middle = {}) {
+                                             acc16 (&acc)[S::NI][S::MI], RowB&& row_b, Middle&& middle = {}, UnderWay&& under_way = {}) {
     constexpr bool kMiddle = !__is_same(__remove_cvref(Middle), NoMiddle);
     using namespace product;
     const int t = threadIdx.x, lane = t & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(t / kWave);
@@ -171,6 +174,7 @@ __device__ __forceinline__ void product_tile(const Operand& A, const Operand& B,
     }
     const int steps = K / S::BK;
     fetch(0);
+    under_way();
     __syncthreads();
     for (int s = 0; s < steps; ++s) {
         if (s + 1 < steps) fetch((s + 1) & 1);

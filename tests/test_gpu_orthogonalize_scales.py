@@ -75,3 +75,27 @@ def test_both_pieces_of_every_element(hx, n, rows, cols, p, steps):
     off = np.abs(got - want) / ((steps + 2) * (2.0 ** -20 * np.abs(want) + 2.0 ** -36 * norm(want)[:, None, None]))
     bad = int((off > 1).sum())
     assert bad == 0, (bad, float(off.max()))
+
+
+@pytest.mark.parametrize("factor", [1e3, 1e5, 1e9, 1e20])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_eps_far_above_the_norm(hx, rows, cols, factor):
+    """X0 = U / (|U| + eps) is small then: five steps make it p^5 as large and little else (c: 4.775 / 3.4445 of the square of a
+    singular value, at most 1e-3 * 3.4445^5 / 5 or so).  In the same call matrices far above eps."""
+    rng = np.random.default_rng(rows)
+    coefficients = (3.4445, -4.7750, 2.0315)
+    g = rng.normal(size=(4, rows, cols))
+    g /= norm(g)[:, None, None]
+    g[1] *= 1e4 * factor
+    g[2] = 0.0
+    got, want = run(hx, g, 5, coefficients, factor)
+    assert not got[2].any()
+    tol = 5 * (2.0 ** -20 + 3 * sums(max(rows, cols)) * 0.1) * norm(want)
+    off = norm(got - want)
+    for i in (0, 3):
+        assert off[i] <= tol[i], off[i] / norm(want)[i]
+    assert np.isfinite(got).all() and off[1] <= 1e-4 * norm(want)[1]
+    velocity = rng.normal(size=g.shape) * 1e-2
+    got, want = run(hx, g, 5, coefficients, factor, velocity=velocity, mu=0.9, nesterov=True)
+    off = norm(got - want)
+    assert (off[[0, 2, 3]] <= (tol[0] / norm(want)[0] + 2.0 ** -22) * 2 * norm(want)[[0, 2, 3]]).all(), off / norm(want)
