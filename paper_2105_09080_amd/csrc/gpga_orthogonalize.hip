@@ -297,8 +297,8 @@ __global__ __launch_bounds__(kThreads) void k_orth_scaled(OrthArgs a, float scal
 // one matrix of the short side's size that holds A and then q A + r A^2.  Results stay in registers until everybody has read what they
 // replace.  Pieces of 16 bytes lie within their row xored with fold(row), so that 16 lanes that read one piece of 16 rows, and 32 that read
 // 8 bytes each of 4 rows for the transposing read, meet every bank once (rows are odd or even multiples of 128 bytes, and the banks repeat
-// after 256).  20 matrices in five steps, here and as products with a launch each: 64 x 64 25 and 72 us; 64 x 256 49, where 64 x 320 takes
-// 90 in launches; 128 x 128 77, 192 x 192 in launches 114.
+// after 256).  20 matrices in five steps, here and as products with a launch each: 64 x 64 25 and 72 us; 64 x 256 48, where 64 x 320 takes
+// 98 in launches; 128 x 128 72, 192 x 192 in launches 121.
 struct SmallArgs {
     OrthArgs o;
     int32_t k2;             // long side, padded

@@ -8,7 +8,9 @@
 //
 // An operand lies in memory with k along its rows ("rows") or down its columns ("columns": row k holds the i's); planes have rows and
 // columns padded with zeros to multiples of kPad, so k needs no checks.  Tiles go to LDS by loads that bypass the registers, 16 bytes
-// a lane, two buffers: the next tile arrives while this one is multiplied.  Rows of a "rows" tile are read as they are (ds_read_b128,
+// a lane, two buffers: where both operands are rows, the next tile arrives while this one is multiplied.  Where one is columns it does not: the
+// compiler takes the transposing read to meet any such load and waits for the tile just asked for before it reads this one, so
+// there only the other workgroups of a compute unit hide that wait.  Rows of a "rows" tile are read as they are (ds_read_b128,
 // 8 k's of one i); of a "columns" tile through the transposing read (ds_read_b64_tr_b16, 16 lanes fetch 4 rows of 16 and get a column of
 // 4 each).  LDS gets 16-byte pieces in an order xored with the row, by loading them so, and no two lanes that are served together
 // meet in a bank.
