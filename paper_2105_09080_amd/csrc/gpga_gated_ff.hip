@@ -550,7 +550,7 @@ __global__ __launch_bounds__(kThreads) void k_ff_zero(float* g, int64_t g_ld, in
 // Up to kFewTokens tokens a node: every matrix is read once, as it lies in X, and that is what takes the time (4 nodes, 1024 x 4096, fp16,
 // 1, 16, 32 and 64 tokens: 42, 47, 63 and 87 us, the tiles' way 180 to 187; 20 nodes, 128 x 512: 10, 10, 13 and 18, the tiles' way 30 to
 // 35).  A wavefront takes 16 rows of a matrix (16 of gate and the same 16 of up), 64 columns at a time, as bf16 pieces made in registers,
-// which need no scale: three of them hold fp32, two go with bf16 activations.  The wavefronts of a workgroup share a row's columns and
+// which need no scale: three of them hold fp32; two (2^-17) go with bf16 activations, and hold h where y is rounded to 16 bits.  The wavefronts of a workgroup share a row's columns and
 // add their sums in LDS.
 // A lane holds 16 neighbouring columns of a row, 64 bytes, four lanes a row; which of a matrix instruction's k's they are does not
 // matter as long as both operands agree.
