@@ -460,8 +460,8 @@ gpga_status gpga_token_loss(gpga_ctx* ctx, const void* logits_dev, const int32_t
  * weighted by |row f of Wg_i| |row f of Wu_i|), with fp16 two of one operand and one (2^-11) of the other, with bf16 one
  * each; h is scaled element by element, whatever the sizes of the matrices and of their rows beside each other's.  Up to 64 tokens a node no scales are needed.
  * The gradients of the matrices take two pieces whatever the type.  A token with an infinity or NaN in its row of x has no finite result, and may have
- * none where |x| or a |row| of Wg_i or Wu_i (2-norms) passes 2^126, or |row f of Wg_i| |row f of Wu_i| 2^100, alone or times an element of Wd_i's
- * column f 2^127; other tokens are not touched.
+ * none where |x| or a |row| of Wg_i or Wu_i (2-norms) passes 2^126, or |row f of Wg_i| |row f of Wu_i| 2^120, alone or times an element of Wd_i's
+ * column f 2^127; other tokens are not touched.  Where that product is below 2^-112 its h loses bits.
  * An infinity or NaN in a matrix leaves no finite y that it enters.  Scratch: the matrices in fp16 pieces, and up to some 4 GiB for tokens
  * (more go through in turn); up to 64 tokens a node need n*T*F floats only. */
 typedef enum { GPGA_SILU = 0, GPGA_GELU = 1 } gpga_activation;

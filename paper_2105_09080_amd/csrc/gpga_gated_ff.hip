@@ -98,7 +98,7 @@ __device__ __forceinline__ void pack_gate_up_rows(const PackMatrices& a, uint32_
     const int64_t first = (int64_t)(block % a.gu_blocks) * 2 + threadIdx.x;
     const float eg = s[threadIdx.x], eu = s[threadIdx.x + 2], both = eg + eu;
     // a float's range, and room in it for the down matrix's values: beyond it up's part is what is left
-    const float e = both != both || both == -INFINITY ? both : fminf(fmaxf(both, -100.f), 100.f);
+    const float e = both != both || both == -INFINITY ? both : fminf(fmaxf(both, -112.f), 120.f);
     a.fold[node * F2 + first] = power_of_two(e);
     a.gu_up[node * 2 * F2 + first] = power_of_two(-eg);
     a.gu_up[node * 2 * F2 + F2 + first] = e == -INFINITY ? 0.f : ldexpf(power_of_two(eg), (int)(e != e ? 0.f : 15.f - e));

@@ -54,6 +54,12 @@ def spread_matrices(kind, rng):
     if kind == "apart":                                              # neither has the other's size
         gate *= 2.0 ** -60
         up *= 2.0 ** 60
+    if kind == "huge":
+        gate *= 2.0 ** 55
+        up *= 2.0 ** 55
+    if kind == "tiny":
+        gate *= 2.0 ** -52
+        up *= 2.0 ** -52
     if kind == "every row":                                          # rows from 2^-30 to 2^30, and the columns that they meet
         s = 2.0 ** np.linspace(-30, 30, F).round()
         rng.shuffle(s)
@@ -95,7 +101,7 @@ def forward_tolerances(x, gate, up, down, kind, dtype):
     return (y, a, b), (norm(ty, 2), ta, tb)
 
 
-MATRICES = ["alike", "up small", "gate small", "one gate row", "one up row", "apart", "every row", "zero rows"]
+MATRICES = ["alike", "up small", "gate small", "one gate row", "one up row", "apart", "every row", "zero rows", "huge", "tiny"]
 
 
 def with_types(kinds, not_fp16):
@@ -103,7 +109,7 @@ def with_types(kinds, not_fp16):
     return [(k, d) for k in kinds for d in TYPES if d != "f16" or k not in not_fp16]
 
 
-@pytest.mark.parametrize("kind,dtype", with_types(MATRICES, ("apart", "every row")))
+@pytest.mark.parametrize("kind,dtype", with_types(MATRICES, ("apart", "every row", "huge", "tiny")))
 @pytest.mark.parametrize("T", [64, 65])
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 def test_forward(hx, kind, act, T, dtype):
@@ -113,7 +119,7 @@ def test_forward(hx, kind, act, T, dtype):
     sim, at = make(hx, gate, up, down)
     x, xd = activations(rng, (N, T, D), dt)
     y, hidden = sim.gated_ff(x, *at, F, act=act, keep=True)
-    with np.errstate(over="ignore"):
+    with np.errstate(over="ignore", invalid="ignore"):
         (wy, wa, wb), (ty, ta, tb) = forward_tolerances(xd, gate, up, down, act, dtype)
     sub = 2.0 ** -25 if dtype == "f16" else 0.0                       # below fp16's smallest normal numbers
     hidden, y = hidden.double().cpu().numpy(), y.double().cpu().numpy()
